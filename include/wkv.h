@@ -250,6 +250,105 @@ int32_t wkv_splits(const wkv_ctx* ctx);
 const char* wkv_strerror(int code);
 const char* wkv_last_error(const wkv_ctx* ctx);
 
+/* ---------------------------------------------------------------------------------------------------------------------
+ * Paged caches: every token kept, or the caches that the paper measures WeightedKV against -- first and newest tokens
+ * (StreamingLLM: `sink` + `window`) and heavy hitters (H2O: eviction by accumulated attention weight); Experiments
+ * section, baselines.  Keys and values lie in a pool of pages, [n_layers, n_pages, n_kv_heads, page_size, head_dim];
+ * sequence b's entry i is row i mod page_size of page block_table[b][i / page_size], for every kv head.  Which pages
+ * belong to whom is the caller's business: several sequences may share pages that no call writes to.
+ *
+ * Conventions of these calls, beside those at the top of this file:
+ *   - Tables, lengths and offsets are read on the device, so a captured call can be replayed with new ones.  A page number,
+ *     length or offset out of range never leads to an access outside the pool or the call's buffers: that page counts as
+ *     zeros, the length or offset is clamped, and wkv_paged_status reports WKV_ERR_STATE.  Columns of a table behind a
+ *     sequence's last page are not read.
+ *   - Pool rows behind a sequence's length are never used, whatever bits they hold.  Rows inside it are expected to be finite.
+ *   - A row that sees no entry (a padded sequence of length 0) gets output 0 and log-sum -infinity.
+ *   - The token at position p sees entry i if i <= p and (window == 0, or i > p - window, or i < sink).
+ *   - scores [batch, n_kv_heads, score_stride] fp32, or NULL: the attention weight of every entry, averaged over the kv
+ *     head's query heads, is added to it, the sum over the call's tokens in a fixed order.  Entries that the call appends
+ *     start from 0.  Needs a handle created with scores = 1 and score_stride >= table_width * page_size.
+ *   - A handle has one set of workspaces, taken at creation.  Its calls, and replays of graphs captured from them, must not
+ *     overlap on the GPU.
+ * ------------------------------------------------------------------------------------------------------------------- */
+typedef struct wkv_paged wkv_paged; /* opaque, library-owned */
+
+typedef struct {
+  int32_t n_layers;   /* >= 1                                                                                     */
+  int32_t n_pages;    /* pages of the pool, per layer; n_layers * n_pages * n_kv_heads < 2^31                     */
+  int32_t page_size;  /* entries per page: 16, 32 or 64                                                           */
+  int32_t n_q_heads;  /* as in wkv_config: n_q_heads / n_kv_heads in {1,2,4,8}                                    */
+  int32_t n_kv_heads;
+  int32_t head_dim;   /* 64 or 128                                                                                */
+  int32_t max_batch;  /* most sequences of one call, 1..1024                                                      */
+  int32_t max_pages;  /* most pages of one sequence (table columns); max_pages * page_size <= 2^24                */
+  int32_t dtype;      /* wkv_dtype of q, k, v, out and the pool                                                   */
+  float scale;        /* softmax scale; 0 selects 1/sqrt(head_dim)                                                */
+  int32_t scores;     /* 1: calls may accumulate weights and evict (adds a workspace of 4 * max_batch * n_q_heads *
+                         max_pages * page_size bytes)                                                             */
+  void* stream;       /* cudaStream_t                                                                             */
+  void* k_pool;       /* the caller's pools, 16-byte aligned device memory; both NULL: taken from the provider    */
+  void* v_pool;
+  wkv_alloc_fn alloc; /* as in wkv_config                                                                         */
+  wkv_release_fn release;
+  void* user;
+} wkv_paged_config;
+
+/* Host-only check: NULL if wkv_paged_create would accept it, else a static text naming the first violated rule. */
+const char* wkv_paged_config_error(const wkv_paged_config* cfg);
+
+/* Creates a handle on the current CUDA device.  Pools that the library takes from the provider start at zero.  The pools'
+ * tensor maps are encoded here (bf16 and fp32 rows; WKV_ERR_CUDA if the driver lacks the encoder). */
+int wkv_paged_create(const wkv_paged_config* cfg, wkv_paged** out);
+void wkv_paged_destroy(wkv_paged* c);
+int wkv_paged_set_stream(wkv_paged* c, void* stream);
+/* The pools' device addresses. */
+int wkv_paged_pools(const wkv_paged* c, void** k_pool, void** v_pool);
+
+/* One decode step of a layer: appends the new token of every sequence and attends with it (Background section: A_t, o_t),
+ * the cache's length split over CTAs and joined in the same launch.  Asynchronous.
+ *   q    device [batch, n_q_heads, head_dim], rows q_stride elements apart (0: packed)
+ *   k, v device [batch, n_kv_heads, head_dim], rows kv_stride elements apart (0: packed): stored as entry seq_lens[b] - 1.
+ *        Both NULL: the entries are in the pool already and nothing is stored.
+ *   block_table device [batch, table_width] int32;  seq_lens device [batch] int32: entries WITH the new one, 0 = padding
+ *   out  device [batch, n_q_heads, head_dim] packed;  lse device [batch, n_q_heads] fp32 or NULL: ln sum exp(scale q.k)
+ * Rows are 16-byte aligned (pointers, and strides in bytes).  Sequences whose last entry shares a page row with another's
+ * must not be in one call that appends. */
+int wkv_paged_decode(wkv_paged* c, int32_t layer, int32_t batch, const void* q, int64_t q_stride, const void* k, const void* v,
+                     int64_t kv_stride, const int32_t* block_table, int32_t table_width, const int32_t* seq_lens,
+                     int32_t window, int32_t sink, float* scores, int64_t score_stride, void* out, float* lse);
+
+/* Chunks of new tokens -- whole prompts, pieces of prompts, a few drafted tokens -- of a ragged batch in one call: appends
+ * them and attends with each.  Sequence b's tokens are rows q_start[b] .. q_start[b+1]-1 of q, k, v, out and lse and become
+ * its last entries; seq_lens counts them.  Rows behind q_start[batch] are left as they were.
+ *   q, k, v [total_q, heads, head_dim] and their strides as in wkv_paged_decode;  q_start device [batch + 1] int32
+ *   out [total_q, n_q_heads, head_dim];  lse [total_q, n_q_heads] fp32, or NULL where scores is NULL. */
+int wkv_paged_prefill(wkv_paged* c, int32_t layer, int32_t batch, const void* q, int64_t q_stride, const void* k, const void* v,
+                      int64_t kv_stride, const int32_t* q_start, int32_t total_q, const int32_t* block_table,
+                      int32_t table_width, const int32_t* seq_lens, int32_t window, int32_t sink, float* scores,
+                      int64_t score_stride, void* out, float* lse);
+
+/* Eviction by accumulated weight, for every (sequence, kv head) by itself: while more than `budget` entries are left, the one
+ * with the smallest (score, index) outside of the first `sink` and the newest `recent` entries leaves (the index breaks
+ * ties; a NaN counts as the largest score).  The others move, in order, into the pages of dst_table, which must share none
+ * with the call's src_table rows: pages that several sequences share stay as they are.  (An overlap inside one sequence is
+ * found on the device: nothing of that sequence is moved, its new length is its old one and wkv_paged_status reports
+ * WKV_ERR_STATE.)  budget >= sink + recent.  Asynchronous.
+ *   src_table [batch, src_width], dst_table [batch, dst_width];  seq_lens [batch];  new_lens [batch] out: min(len, budget)
+ *   scores [batch, n_kv_heads, score_stride];  scores_out [batch, n_kv_heads, out_stride] or NULL: the kept entries' scores
+ *   kept [batch, n_kv_heads, budget] int32 or NULL: their indexes.  Behind a sequence's new length both are left as they were.
+ * out_stride >= min(budget, src_width * page_size); scores_out must not overlap scores. */
+int wkv_paged_evict(wkv_paged* c, int32_t layer, int32_t batch, const int32_t* src_table, int32_t src_width,
+                    const int32_t* dst_table, int32_t dst_width, const int32_t* seq_lens, int32_t* new_lens, int32_t budget,
+                    int32_t recent, int32_t sink, const float* scores, int64_t score_stride, float* scores_out,
+                    int64_t out_stride, int32_t* kept);
+
+/* As their namesakes without _paged. */
+int wkv_paged_status(wkv_paged* c);
+int64_t wkv_paged_launch_count(const wkv_paged* c);
+int64_t wkv_paged_device_bytes(const wkv_paged* c);
+const char* wkv_paged_last_error(const wkv_paged* c);
+
 #ifdef __cplusplus
 }
 #endif

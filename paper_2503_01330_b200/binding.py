@@ -28,9 +28,20 @@ class wkv_config(C.Structure):
                 ("stream", C.c_void_p), ("alloc", ALLOC_FN), ("release", RELEASE_FN), ("user", C.c_void_p)]
 
 
+class wkv_paged_config(C.Structure):
+    _fields_ = [("n_layers", C.c_int32), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_q_heads", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("max_batch", C.c_int32), ("max_pages", C.c_int32),
+                ("dtype", C.c_int32), ("scale", C.c_float), ("scores", C.c_int32), ("stream", C.c_void_p),
+                ("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("alloc", ALLOC_FN), ("release", RELEASE_FN),
+                ("user", C.c_void_p)]
+
+
 EXPORTS = ["wkv_config_error", "wkv_create", "wkv_destroy", "wkv_reset", "wkv_set_stream", "wkv_decode_step",
            "wkv_decode_step_layers", "wkv_decode_step_static", "wkv_decode_step_host", "wkv_decode_step_layers_host", "wkv_prefill", "wkv_prefill_bulk", "wkv_prefill_bulk_layers", "wkv_export_state", "wkv_export_slots", "wkv_import_state",
-           "wkv_status", "wkv_selftest_wait_timeout", "wkv_launch_count", "wkv_device_bytes", "wkv_splits", "wkv_strerror", "wkv_last_error"]
+           "wkv_status", "wkv_selftest_wait_timeout", "wkv_launch_count", "wkv_device_bytes", "wkv_splits", "wkv_strerror", "wkv_last_error",
+           "wkv_paged_config_error", "wkv_paged_create", "wkv_paged_destroy", "wkv_paged_set_stream", "wkv_paged_pools",
+           "wkv_paged_decode", "wkv_paged_prefill", "wkv_paged_evict", "wkv_paged_status", "wkv_paged_launch_count",
+           "wkv_paged_device_bytes", "wkv_paged_last_error"]
 
 _lib = None
 
@@ -73,6 +84,24 @@ def lib():
         L.wkv_strerror.argtypes = [C.c_int]
         L.wkv_last_error.restype = C.c_char_p
         L.wkv_last_error.argtypes = [vp]
+        i64 = C.c_int64
+        L.wkv_paged_config_error.restype = C.c_char_p
+        L.wkv_paged_config_error.argtypes = [C.POINTER(wkv_paged_config)]
+        L.wkv_paged_create.argtypes = [C.POINTER(wkv_paged_config), C.POINTER(vp)]
+        L.wkv_paged_destroy.restype = None
+        L.wkv_paged_destroy.argtypes = [vp]
+        L.wkv_paged_set_stream.argtypes = [vp, vp]
+        L.wkv_paged_pools.argtypes = [vp, C.POINTER(vp), C.POINTER(vp)]
+        L.wkv_paged_decode.argtypes = [vp, i32, i32, vp, i64, vp, vp, i64, vp, i32, vp, i32, i32, vp, i64, vp, vp]
+        L.wkv_paged_prefill.argtypes = [vp, i32, i32, vp, i64, vp, vp, i64, vp, i32, vp, i32, vp, i32, i32, vp, i64, vp, vp]
+        L.wkv_paged_evict.argtypes = [vp, i32, i32, vp, i32, vp, i32, vp, vp, i32, i32, i32, vp, i64, vp, i64, vp]
+        L.wkv_paged_status.argtypes = [vp]
+        L.wkv_paged_launch_count.restype = i64
+        L.wkv_paged_launch_count.argtypes = [vp]
+        L.wkv_paged_device_bytes.restype = i64
+        L.wkv_paged_device_bytes.argtypes = [vp]
+        L.wkv_paged_last_error.restype = C.c_char_p
+        L.wkv_paged_last_error.argtypes = [vp]
         _lib = L
     return _lib
 
@@ -242,3 +271,169 @@ class Context:
 
     def wkv_splits(self):
         return int(lib().wkv_splits(self._h))
+
+
+def make_paged_config(n_layers, n_pages, page_size, n_q_heads, n_kv_heads, head_dim, max_batch, max_pages, dtype=WKV_BF16,
+                      scale=0.0, scores=0, stream=None, k_pool=None, v_pool=None):
+    cfg = wkv_paged_config()
+    cfg.n_layers, cfg.n_pages, cfg.page_size, cfg.n_q_heads, cfg.n_kv_heads = n_layers, n_pages, page_size, n_q_heads, n_kv_heads
+    cfg.head_dim, cfg.max_batch, cfg.max_pages, cfg.dtype, cfg.scale = head_dim, max_batch, max_pages, dtype, scale
+    cfg.scores, cfg.stream, cfg.k_pool, cfg.v_pool = int(scores), stream, k_pool, v_pool
+    return cfg
+
+
+def wkv_paged_config_error(cfg):
+    msg = lib().wkv_paged_config_error(C.byref(cfg))
+    return None if msg is None else msg.decode()
+
+
+def _need(ok, text):
+    if not ok:
+        raise WkvError(WKV_ERR_INVALID, text)
+
+
+class PagedCache:
+    """One wkv_paged: a key/value cache in pages and the attention over it.
+
+    `k_pool`, `v_pool` [n_layers, n_pages, n_kv_heads, page_size, head_dim] are the caller's tensors where given, else made
+    here (zeros).  The handle runs on the stream that is current when it is made (wkv_set_stream changes that); the caller
+    orders other streams' work, as for Context."""
+
+    def __init__(self, n_layers, n_pages, page_size, n_q_heads, n_kv_heads, head_dim, max_batch, max_pages, dtype=WKV_BF16,
+                 scale=0.0, scores=False, device="cuda:0", k_pool=None, v_pool=None):
+        self.device = torch.device(device)
+        self.dtype = dtype
+        self.tdtype = torch.bfloat16 if dtype == WKV_BF16 else torch.float32
+        self.shape = (n_layers, n_pages, n_kv_heads, page_size, head_dim)
+        self.n_q_heads, self.n_kv_heads, self.head_dim, self.page_size = n_q_heads, n_kv_heads, head_dim, page_size
+        self._bufs = {}
+        cfg = make_paged_config(n_layers, n_pages, page_size, n_q_heads, n_kv_heads, head_dim, max_batch, max_pages, dtype,
+                                scale, scores)
+        err = wkv_paged_config_error(cfg)
+        _need(err is None, err)
+        _need((k_pool is None) == (v_pool is None), "k_pool and v_pool must both be given or both be None")
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        with torch.cuda.device(self.device):
+            if k_pool is None:
+                k_pool = torch.zeros(self.shape, dtype=self.tdtype, device=self.device)
+                v_pool = torch.zeros(self.shape, dtype=self.tdtype, device=self.device)
+            for name, p in (("k_pool", k_pool), ("v_pool", v_pool)):
+                _need(tuple(p.shape) == self.shape and p.dtype == self.tdtype and p.device == self.device and p.is_contiguous(),
+                      f"{name} must be a contiguous {self.tdtype} tensor {self.shape} on {self.device}")
+            self.k_pool, self.v_pool = k_pool, v_pool
+            cfg.k_pool, cfg.v_pool = k_pool.data_ptr(), v_pool.data_ptr()
+            cfg.stream = torch.cuda.current_stream(self.device).cuda_stream
+
+            def _alloc(nbytes, _user):
+                try:
+                    buf = torch.empty(int(nbytes), dtype=torch.uint8, device=self.device)
+                except Exception:
+                    return None
+                self._bufs[buf.data_ptr()] = buf
+                return buf.data_ptr()
+
+            def _release(ptr, _user):
+                self._bufs.pop(ptr, None)
+
+            self._alloc_cb, self._release_cb = ALLOC_FN(_alloc), RELEASE_FN(_release)
+            cfg.alloc, cfg.release = self._alloc_cb, self._release_cb
+            h = C.c_void_p()
+            rc = lib().wkv_paged_create(C.byref(cfg), C.byref(h))
+        if rc != WKV_OK:
+            raise WkvError(rc, lib().wkv_strerror(rc).decode())
+        self._h = h
+
+    def _check(self, rc):
+        if rc != WKV_OK:
+            raise WkvError(rc, (lib().wkv_paged_last_error(self._h) or b"").decode() or lib().wkv_strerror(rc).decode())
+
+    def close(self):
+        if getattr(self, "_h", None):
+            lib().wkv_paged_destroy(self._h)
+            self._h = None
+            self._bufs.clear()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _packed(self, name, t, dtype, *shape):
+        """Address of an optional packed tensor whose shape is checked (-1: any size)."""
+        if t is None:
+            return None
+        _need(t.dtype == dtype and t.device == self.device and t.is_contiguous() and t.dim() == len(shape)
+              and all(w in (-1, n) for w, n in zip(shape, t.shape)),
+              f"{name} must be a contiguous {dtype} tensor of shape {list(shape)} on {self.device}")
+        return C.c_void_p(t.data_ptr())
+
+    def _rows(self, name, t, n, heads):
+        """Address and row stride of [n, heads, head_dim] whose rows may lie apart (columns of a wider projection)."""
+        d = self.head_dim
+        _need(t.dtype == self.tdtype and t.device == self.device and tuple(t.shape) == (n, heads, d)
+              and (t.numel() == 0 or (t.stride(2) == 1 and (heads == 1 or t.stride(1) == d))),
+              f"{name} must be a {self.tdtype} tensor [{n}, {heads}, {d}] on {self.device} whose rows are packed")
+        return C.c_void_p(t.data_ptr()), (t.stride(0) if n > 1 else heads * d)
+
+    def _new_rows(self, k, v, n):
+        _need((k is None) == (v is None), "k and v must both be given or both be None")
+        if k is None:
+            return None, None, 0
+        (kp, ks), (vp, vs) = self._rows("k", k, n, self.n_kv_heads), self._rows("v", v, n, self.n_kv_heads)
+        _need(ks == vs, "k and v must have the same row stride")
+        return kp, vp, ks
+
+    def _scores(self, name, scores, batch):
+        if scores is None:
+            return None, 0
+        return self._packed(name, scores, torch.float32, batch, self.n_kv_heads, -1), scores.shape[2]
+
+    # -- the C ABI, same names ----------------------------------------------------------------------
+    def wkv_set_stream(self, stream):
+        self._check(lib().wkv_paged_set_stream(self._h, C.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else stream)))
+
+    def wkv_paged_decode(self, layer, q, k, v, block_table, seq_lens, out, window=0, sink=0, scores=None, lse=None):
+        """q [B, Hq, d], k, v [B, Hkv, d] or None, block_table [B, width] and seq_lens [B] int32 (with the new token)."""
+        B, Hq, d = q.shape[0], self.n_q_heads, self.head_dim
+        qp, qs = self._rows("q", q, B, Hq)
+        kp, vp, ks = self._new_rows(k, v, B)
+        sp, ss = self._scores("scores", scores, B)
+        self._check(lib().wkv_paged_decode(
+            self._h, layer, B, qp, qs, kp, vp, ks, self._packed("block_table", block_table, torch.int32, B, -1),
+            block_table.shape[1], self._packed("seq_lens", seq_lens, torch.int32, B), window, sink, sp, ss,
+            self._packed("out", out, self.tdtype, B, Hq, d), self._packed("lse", lse, torch.float32, B, Hq)))
+
+    def wkv_paged_prefill(self, layer, q, k, v, q_start, block_table, seq_lens, out, window=0, sink=0, scores=None, lse=None):
+        """q [T, Hq, d], k, v [T, Hkv, d] or None; sequence b's tokens are rows q_start[b] .. q_start[b + 1] - 1."""
+        T, Hq, d, B = q.shape[0], self.n_q_heads, self.head_dim, block_table.shape[0]
+        qp, qs = self._rows("q", q, T, Hq)
+        kp, vp, ks = self._new_rows(k, v, T)
+        sp, ss = self._scores("scores", scores, B)
+        self._check(lib().wkv_paged_prefill(
+            self._h, layer, B, qp, qs, kp, vp, ks, self._packed("q_start", q_start, torch.int32, B + 1), T,
+            self._packed("block_table", block_table, torch.int32, B, -1), block_table.shape[1],
+            self._packed("seq_lens", seq_lens, torch.int32, B), window, sink, sp, ss,
+            self._packed("out", out, self.tdtype, T, Hq, d), self._packed("lse", lse, torch.float32, T, Hq)))
+
+    def wkv_paged_evict(self, layer, src_table, dst_table, seq_lens, new_lens, budget, recent, sink=0, *, scores,
+                        scores_out=None, kept=None):
+        """Keeps `budget` entries per (sequence, kv head) by accumulated weight and moves them to dst_table's pages."""
+        B = src_table.shape[0]
+        sp, ss = self._scores("scores", scores, B)
+        op, os_ = self._scores("scores_out", scores_out, B)
+        self._check(lib().wkv_paged_evict(
+            self._h, layer, B, self._packed("src_table", src_table, torch.int32, B, -1), src_table.shape[1],
+            self._packed("dst_table", dst_table, torch.int32, B, -1), dst_table.shape[1],
+            self._packed("seq_lens", seq_lens, torch.int32, B), self._packed("new_lens", new_lens, torch.int32, B), budget,
+            recent, sink, sp, ss, op, os_, self._packed("kept", kept, torch.int32, B, self.n_kv_heads, budget)))
+
+    def wkv_status(self):
+        return lib().wkv_paged_status(self._h)
+
+    def wkv_launch_count(self):
+        return int(lib().wkv_paged_launch_count(self._h))
+
+    def wkv_device_bytes(self):
+        return int(lib().wkv_paged_device_bytes(self._h))

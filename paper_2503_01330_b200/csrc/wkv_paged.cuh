@@ -1,0 +1,375 @@
+// Device code of the paged cache (include/wkv.h, "Paged caches"): appending, attention of one or many new tokens per
+// sequence, accumulated attention weights, eviction by them.
+//
+// Pool: [layers][pages][kv heads][page][D]; the kernels see one layer.  A "chunk" is one kv head's rows of one page,
+// page * D contiguous elements; its number inside the layer is page * Hkv + head.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "wkv_ptx.cuh"
+
+namespace wkv {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+struct PagedParams {
+  void* k_pool;              // the layer's pools
+  void* v_pool;
+  const void* q;             // [rows][Hq][D], rows q_stride elements apart
+  const void* k;             // [rows][Hkv][D] or NULL
+  const void* v;
+  long long q_stride, kv_stride;
+  const int32_t* table;      // [batch][width]
+  const int32_t* seq_lens;   // [batch]
+  const int32_t* q_start;    // [batch + 1], or NULL: one row per sequence (decode)
+  void* out;                 // [rows][Hq][D]
+  float* lse;                // [rows][Hq]
+  float* scores;             // [batch][Hkv][score_stride] or NULL
+  long long score_stride;
+  uint32_t* status;
+  int batch, rows, width, n_pages, n_q_heads, n_kv_heads, page, page_shift;
+  int window, sink;
+  float scale;               // softmax scale; scale_log2 = scale * log2(e)
+  float scale_log2;
+};
+
+__device__ __forceinline__ void flag_bad_table(uint32_t* status) { atomicOr(status, kStatusBadTable); }
+
+// Sequence length clamped to what its table row can hold.
+__device__ __forceinline__ int clamped_len(const PagedParams& P, int b) {
+  const int n = P.seq_lens[b];
+  const long long most = (long long)P.width << P.page_shift;
+  if (n < 0 || n > most) {
+    flag_bad_table(P.status);
+    return n < 0 ? 0 : (int)most;
+  }
+  return n;
+}
+// Page of entry i, -1 if the table holds no valid number there.
+__device__ __forceinline__ int page_of(const PagedParams& P, int b, int i) {
+  const int pg = P.table[(long long)b * P.width + (i >> P.page_shift)];
+  if ((unsigned)pg >= (unsigned)P.n_pages) {
+    flag_bad_table(P.status);
+    return -1;
+  }
+  return pg;
+}
+__device__ __forceinline__ long long row_offset(const PagedParams& P, int pg, int head, int i, int D) {
+  return ((((long long)pg * P.n_kv_heads + head) << P.page_shift) + (i & (P.page - 1))) * D;
+}
+
+// A sequence's rows of q: [first, first + n), clamped into the call's buffers.
+struct SeqRows {
+  int first, n, len;         // len: entries of the sequence, the call's own included
+};
+__device__ __forceinline__ SeqRows seq_rows(const PagedParams& P, int b) {
+  SeqRows s;
+  s.len = clamped_len(P, b);
+  if (!P.q_start) {
+    s.first = b;
+    s.n = s.len > 0 ? 1 : 0;
+    return s;
+  }
+  const int lo = P.q_start[b], hi = P.q_start[b + 1];
+  s.first = min(max(lo, 0), P.rows);
+  s.n = min(max(hi, s.first), P.rows) - s.first;
+  if (lo != s.first || hi != s.first + s.n || s.n > s.len) flag_bad_table(P.status);
+  return s;
+}
+// The sequence that row r belongs to, -1 if none: the last b with q_start[b] <= r, if its end is behind r.
+__device__ __forceinline__ int seq_of_row(const PagedParams& P, int r) {
+  if (!P.q_start) return r;
+  int lo = 0, hi = P.batch;            // invariant: q_start[lo] <= r (or lo == 0), q_start[hi] > r (or hi == batch)
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (P.q_start[mid] <= r) lo = mid; else hi = mid;
+  }
+  return (P.q_start[lo] <= r && r < P.q_start[lo + 1]) ? lo : -1;
+}
+
+__device__ __forceinline__ bool visible(int i, int pos, int window, int sink) {
+  return i <= pos && (window == 0 || i > pos - window || i < sink);
+}
+
+template <typename T> __device__ __forceinline__ float as_float(T x);
+template <> __device__ __forceinline__ float as_float<float>(float x) { return x; }
+template <> __device__ __forceinline__ float as_float<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <typename T> __device__ __forceinline__ T from_float(float x);
+template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+// ------------------------------------------------------------------------------------------------
+// append: one warp per (row, kv head); a row of K and a row of V, 16 bytes a lane
+// ------------------------------------------------------------------------------------------------
+template <typename T, int D>
+__global__ void __launch_bounds__(128) paged_append_kernel(const PagedParams P) {
+  griddep_launch();
+  griddep_wait();
+  const long long item = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (item >= (long long)P.rows * P.n_kv_heads) return;
+  const int r = (int)(item / P.n_kv_heads), head = (int)(item % P.n_kv_heads);
+  const int b = seq_of_row(P, r);
+  if (b < 0) return;
+  const SeqRows s = seq_rows(P, b);
+  if (r < s.first || r >= s.first + s.n) return;
+  const int i = s.len - s.n + (r - s.first);
+  if (i < 0) return;
+  const int pg = page_of(P, b, i);
+  if (pg < 0) return;
+  const long long dst = row_offset(P, pg, head, i, D), src = (long long)r * P.kv_stride + (long long)head * D;
+  constexpr int kVec = D * (int)sizeof(T) / 16;
+  for (int c = lane; c < 2 * kVec; c += 32) {
+    const bool is_v = c >= kVec;
+    const int e = (is_v ? c - kVec : c) * (16 / (int)sizeof(T));
+    const T* from = static_cast<const T*>(is_v ? P.v : P.k) + src + e;
+    T* to = static_cast<T*>(is_v ? P.v_pool : P.k_pool) + dst + e;
+    *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(from);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------
+// attention, plain: one warp per (row, query head), the lanes share a row's channels
+// ------------------------------------------------------------------------------------------------
+template <typename T, int D>
+__global__ void __launch_bounds__(128) paged_attend_kernel(const PagedParams P) {
+  griddep_wait();
+  const long long item = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (item >= (long long)P.rows * P.n_q_heads) return;
+  const int r = (int)(item / P.n_q_heads), hq = (int)(item % P.n_q_heads);
+  const int head = hq / (P.n_q_heads / P.n_kv_heads);
+  const int b = seq_of_row(P, r);
+  if (b < 0) return;
+  const SeqRows s = seq_rows(P, b);
+  if (P.q_start && (r < s.first || r >= s.first + s.n)) return;
+  constexpr int E = D / 32;
+  float q[E], acc[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    q[e] = as_float(static_cast<const T*>(P.q)[(long long)r * P.q_stride + (long long)hq * D + lane * E + e]) * P.scale_log2;
+    acc[e] = 0.f;
+  }
+  float m = -INFINITY, l = 0.f;
+  const int pos = s.len - s.n + (r - s.first);
+  if (s.n > 0) {
+    const int lo = P.window > 0 ? max(0, pos - P.window + 1) : 0;
+    for (int i = 0; i <= pos; ++i) {
+      if (i == min(P.sink, lo) && i < lo) i = lo;      // over the entries between the sinks and the window
+      const int pg = page_of(P, b, i);
+      if (pg < 0) continue;
+      const long long off = row_offset(P, pg, head, i, D) + lane * E;
+      float x = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) x = fmaf(q[e], as_float(static_cast<const T*>(P.k_pool)[off + e]), x);
+#pragma unroll
+      for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
+      const float mn = fmaxf(m, x), c = exp2f(m - mn), p = exp2f(x - mn);
+      l = l * c + p;
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] = acc[e] * c + p * as_float(static_cast<const T*>(P.v_pool)[off + e]);
+      m = mn;
+    }
+  }
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    static_cast<T*>(P.out)[((long long)r * P.n_q_heads + hq) * D + lane * E + e] = from_float<T>(acc[e] * inv);
+  if (P.lse && lane == 0) P.lse[(long long)r * P.n_q_heads + hq] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+}
+
+// ------------------------------------------------------------------------------------------------
+// accumulated weights, plain: one warp per (sequence, kv head, entry), over the call's tokens in order
+// ------------------------------------------------------------------------------------------------
+template <typename T, int D>
+__global__ void __launch_bounds__(128) paged_weights_kernel(const PagedParams P, int entries) {
+  griddep_wait();
+  const long long item = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (item >= (long long)P.batch * P.n_kv_heads * entries) return;
+  const int i = (int)(item % entries);
+  const int bh = (int)(item / entries), b = bh / P.n_kv_heads, head = bh % P.n_kv_heads;
+  const SeqRows s = seq_rows(P, b);
+  if (i >= s.len || s.n == 0) return;
+  const int pg = page_of(P, b, i);
+  if (pg < 0) return;
+  const int G = P.n_q_heads / P.n_kv_heads, old = s.len - s.n;
+  constexpr int E = D / 32;
+  float k[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    k[e] = as_float(static_cast<const T*>(P.k_pool)[row_offset(P, pg, head, i, D) + lane * E + e]) * P.scale_log2;
+  float sum = 0.f;
+  for (int t = max(0, i - old); t < s.n; ++t) {
+    if (!visible(i, old + t, P.window, P.sink)) continue;
+    const long long r = s.first + t;
+    for (int g = 0; g < G; ++g) {
+      const int hq = head * G + g;
+      float x = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) x = fmaf(k[e], as_float(static_cast<const T*>(P.q)[r * P.q_stride + (long long)hq * D + lane * E + e]), x);
+#pragma unroll
+      for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
+      sum += exp2f(x - P.lse[r * P.n_q_heads + hq] * kLog2e);
+    }
+  }
+  if (lane == 0) {
+    float* a = P.scores + (long long)bh * P.score_stride + i;
+    *a = (P.k && i >= old ? 0.f : *a) + sum / (float)G;
+  }
+}
+
+// ------------------------------------------------------------------------------------------------
+// eviction
+// ------------------------------------------------------------------------------------------------
+struct EvictParams {
+  void* k_pool;
+  void* v_pool;
+  const int32_t* src_table;  // [batch][src_width]
+  const int32_t* dst_table;  // [batch][dst_width]
+  const int32_t* seq_lens;
+  int32_t* new_lens;
+  const float* scores;       // [batch][Hkv][score_stride]
+  float* scores_out;         // [batch][Hkv][out_stride] or NULL
+  long long score_stride, out_stride;
+  int32_t* kept;             // [batch][Hkv][kept_stride]: the caller's, or workspace
+  long long kept_stride;
+  int32_t* n_moved;          // [batch][Hkv] workspace: rows the move kernel copies
+  uint32_t* status;
+  int batch, src_width, dst_width, n_pages, n_kv_heads, page, page_shift, budget, recent, sink;
+};
+
+// Order of eviction as an unsigned key: smaller score, smaller key; -0 like +0; NaN last.
+__device__ __forceinline__ uint32_t score_key(float x) {
+  if (x != x) return 0xffffffffu;
+  const uint32_t u = __float_as_uint(x + 0.f);
+  return u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
+}
+
+constexpr int kSelectThreads = 1024;
+constexpr int kBitmapWords = 8192;     // pages per round of the overlap check: 32 times that
+
+__device__ __forceinline__ int block_sum(int x, int* scratch) {
+  x = __reduce_add_sync(~0u, x);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = x;
+  __syncthreads();
+  return __reduce_add_sync(~0u, scratch[threadIdx.x & 31]);
+}
+
+// One CTA per (sequence, kv head): which entries stay, in order.
+__global__ void __launch_bounds__(kSelectThreads) paged_select_kernel(const EvictParams P) {
+  __shared__ uint32_t bitmap[kBitmapWords];
+  __shared__ int scratch[32], warp_count[32];
+  griddep_launch();
+  griddep_wait();
+  const int bh = blockIdx.x, b = bh / P.n_kv_heads, head = bh % P.n_kv_heads, tid = threadIdx.x;
+  const int raw = P.seq_lens[b];
+  const long long most = (long long)P.src_width << P.page_shift;
+  const int len = raw < 0 ? 0 : raw > most ? (int)most : raw;
+  bool bad = len != raw;
+  const int left = min(len, P.budget), leave = len - left;
+  const int n_src = (len + P.page - 1) >> P.page_shift, n_dst = (left + P.page - 1) >> P.page_shift;
+  // does the sequence move into pages that it lies in?
+  bool overlap = false;
+  for (int base = 0; base < P.n_pages; base += kBitmapWords * 32) {
+    const int words = min(kBitmapWords, (P.n_pages - base + 31) / 32);
+    for (int w = tid; w < words; w += kSelectThreads) bitmap[w] = 0;
+    __syncthreads();
+    for (int c = tid; c < n_src; c += kSelectThreads) {
+      const int pg = P.src_table[(long long)b * P.src_width + c];
+      if ((unsigned)pg >= (unsigned)P.n_pages) bad = true;
+      const unsigned at = (unsigned)pg - base;
+      if ((unsigned)pg < (unsigned)P.n_pages && at < (unsigned)words * 32) atomicOr(&bitmap[at >> 5], 1u << (at & 31));
+    }
+    __syncthreads();
+    for (int c = tid; c < n_dst; c += kSelectThreads) {
+      const int pg = P.dst_table[(long long)b * P.dst_width + c];
+      if ((unsigned)pg >= (unsigned)P.n_pages) bad = true;
+      const unsigned at = (unsigned)pg - base;
+      if ((unsigned)pg < (unsigned)P.n_pages && at < (unsigned)words * 32 && (bitmap[at >> 5] >> (at & 31) & 1)) overlap = true;
+    }
+    __syncthreads();
+  }
+  overlap = __syncthreads_or(overlap);
+  if (tid == 0) {
+    if (head == 0) P.new_lens[b] = overlap ? len : left;
+    P.n_moved[bh] = overlap ? 0 : left;
+  }
+  if (bad || (overlap && tid == 0)) flag_bad_table(P.status);
+  if (overlap) return;
+
+  const float* x = P.scores + (long long)bh * P.score_stride;
+  const int lo = min(P.sink, len), hi = max(lo, len - P.recent);      // entries that may leave
+  // The `leave`-th smallest key, bit by bit from the top: threshold = the largest t with fewer than `leave` keys below it.
+  uint32_t threshold = 0;
+  int below = 0;                       // keys < threshold
+  if (leave > 0) {
+    for (int bit = 31; bit >= 0; --bit) {
+      const uint32_t t = threshold | (1u << bit);
+      int c = 0;
+      for (int i = lo + tid; i < hi; i += kSelectThreads) c += score_key(x[i]) < t;
+      c = block_sum(c, scratch);
+      if (c < leave) { threshold = t; below = c; }
+    }
+  }
+  const int ties = leave - below;      // of the keys equal to the threshold the first `ties` leave
+  int stay = 0, equal = 0;             // so far
+  for (int base = 0; base < len; base += kSelectThreads) {
+    const int i = base + tid;
+    const bool in = i < len, may = in && leave > 0 && i >= lo && i < hi;
+    const float xi = in ? x[i] : 0.f;
+    const uint32_t key = score_key(xi);
+    const bool eq = may && key == threshold;
+    // rank among the equal ones
+    const uint32_t eqs = __ballot_sync(~0u, eq);
+    if ((tid & 31) == 0) warp_count[tid >> 5] = __popc(eqs);
+    __syncthreads();
+    const int wc = warp_count[tid & 31];
+    const int before = __reduce_add_sync(~0u, (tid & 31) < (tid >> 5) ? wc : 0), all = __reduce_add_sync(~0u, wc);
+    const int rank = equal + before + __popc(eqs & ((1u << (tid & 31)) - 1));
+    equal += all;
+    const bool keep = in && !(may && (key < threshold || (eq && rank < ties)));
+    __syncthreads();
+    const uint32_t ks = __ballot_sync(~0u, keep);
+    if ((tid & 31) == 0) warp_count[tid >> 5] = __popc(ks);
+    __syncthreads();
+    const int kc = warp_count[tid & 31];
+    const int kbefore = __reduce_add_sync(~0u, (tid & 31) < (tid >> 5) ? kc : 0), kall = __reduce_add_sync(~0u, kc);
+    if (keep) {
+      const int at = stay + kbefore + __popc(ks & ((1u << (tid & 31)) - 1));
+      P.kept[(long long)bh * P.kept_stride + at] = i;
+      if (P.scores_out) P.scores_out[(long long)bh * P.out_stride + at] = xi;
+    }
+    stay += kall;
+    __syncthreads();
+  }
+}
+
+// Rows of K and V to their new pages: half a warp per row, four entries in flight per warp.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) paged_move_kernel(const EvictParams P, int blocks_per_lane) {
+  griddep_wait();
+  const int bh = blockIdx.x / blocks_per_lane, part = blockIdx.x % blocks_per_lane;
+  const int b = bh / P.n_kv_heads, head = bh % P.n_kv_heads, n = P.n_moved[bh];
+  constexpr int kVec = 2 * D * (int)sizeof(T) / 16;    // 16-byte pieces of an entry: K row, then V row
+  constexpr int kEach = 16 / (int)sizeof(T);
+  const long long total = (long long)n * kVec;
+  for (long long at = (long long)part * blockDim.x + threadIdx.x; at < total; at += (long long)blocks_per_lane * blockDim.x) {
+    const int i = (int)(at / kVec), c = (int)(at % kVec);
+    const int src = P.kept[(long long)bh * P.kept_stride + i];
+    const int sp = P.src_table[(long long)b * P.src_width + (src >> P.page_shift)];
+    const int dp = P.dst_table[(long long)b * P.dst_width + (i >> P.page_shift)];
+    if ((unsigned)sp >= (unsigned)P.n_pages || (unsigned)dp >= (unsigned)P.n_pages) continue;
+    const int e = (c % (kVec / 2)) * kEach;
+    const long long so = ((((long long)sp * P.n_kv_heads + head) << P.page_shift) + (src & (P.page - 1))) * D + e;
+    const long long to = ((((long long)dp * P.n_kv_heads + head) << P.page_shift) + (i & (P.page - 1))) * D + e;
+    T* pool = static_cast<T*>(c < kVec / 2 ? P.k_pool : P.v_pool);
+    *reinterpret_cast<uint4*>(pool + to) = *reinterpret_cast<const uint4*>(pool + so);
+  }
+}
+
+}  // namespace wkv

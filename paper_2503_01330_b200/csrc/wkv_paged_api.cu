@@ -1,0 +1,343 @@
+// Host side of the paged cache declared in include/wkv.h: configuration checks, workspaces, launches.
+#include <cmath>
+#include <cstdint>
+#include <cstring>
+#include <new>
+#include <string>
+#include <vector>
+
+#include <cuda.h>                      // tensor-map types only; the driver entry point is looked up at run time
+
+#include "../../include/wkv.h"
+#include "wkv_paged.cuh"
+
+struct wkv_paged {
+  wkv_paged_config cfg;
+  int device = 0;
+  int sm_count = 148;
+  int group = 1;
+  int page_shift = 4;
+  float scale = 0.f;
+  size_t elem = 2;
+  cudaStream_t stream = nullptr;
+  void* k_pool = nullptr;
+  void* v_pool = nullptr;
+  uint32_t* status = nullptr;
+  float* lse = nullptr;                // [max_batch][Hq]: log-sums of a decode call whose caller wants none
+  float* logits = nullptr;             // [max_batch][Hq][max_pages * page_size]; kept indexes of an eviction
+  int32_t* n_moved = nullptr;          // [max_batch][Hkv]
+  std::vector<void*> owned;
+  long long device_bytes = 0;
+  long long launches = 0;
+  std::string last_error;
+};
+
+namespace {
+
+int fail(wkv_paged* c, int code, const std::string& msg) {
+  if (c) c->last_error = msg;
+  return code;
+}
+int cuda_fail(wkv_paged* c, cudaError_t e, const char* what) {
+  return fail(c, WKV_ERR_CUDA, std::string(what) + ": " + cudaGetErrorString(e));
+}
+#define WKV_CUDA(ctx, expr)                                   \
+  do {                                                        \
+    cudaError_t e_ = (expr);                                  \
+    if (e_ != cudaSuccess) return cuda_fail(ctx, e_, #expr);  \
+  } while (0)
+
+// Calls may come with another device current than the handle's.
+struct DeviceGuard {
+  int was = -1;
+  cudaError_t err;
+  explicit DeviceGuard(int device) {
+    err = cudaGetDevice(&was);
+    if (err == cudaSuccess && was != device) err = cudaSetDevice(device); else was = -1;
+  }
+  ~DeviceGuard() { if (was >= 0) cudaSetDevice(was); }
+};
+
+void* default_alloc(size_t bytes, void*) {
+  void* p = nullptr;
+  if (cudaMalloc(&p, bytes) != cudaSuccess) return nullptr;
+  return p;
+}
+void default_release(void* p, void*) { cudaFree(p); }
+
+template <typename P>
+int take(wkv_paged* c, P** dst, size_t bytes) {
+  bytes = (bytes + 255) & ~(size_t)255;
+  void* p = c->cfg.alloc(bytes, c->cfg.user);
+  if (!p) return fail(c, WKV_ERR_ALLOC, "device memory provider returned NULL for " + std::to_string(bytes) + " bytes");
+  c->owned.push_back(p);
+  c->device_bytes += (long long)bytes;
+  *dst = reinterpret_cast<P*>(p);
+  return WKV_OK;
+}
+
+const char* check_config(const wkv_paged_config* c) {
+  if (!c) return "config is NULL";
+  if (c->n_layers < 1 || c->n_pages < 1) return "n_layers and n_pages must be >= 1";
+  if (c->page_size != 16 && c->page_size != 32 && c->page_size != 64) return "page_size must be 16, 32 or 64";
+  if (c->n_kv_heads < 1 || c->n_q_heads < 1 || c->n_q_heads % c->n_kv_heads) return "n_q_heads must be a positive multiple of n_kv_heads";
+  const int g = c->n_q_heads / c->n_kv_heads;
+  if (g != 1 && g != 2 && g != 4 && g != 8) return "n_q_heads / n_kv_heads must be 1, 2, 4 or 8";
+  if (c->n_q_heads > 1024) return "n_q_heads must be <= 1024";
+  if (c->head_dim != 64 && c->head_dim != 128) return "head_dim must be 64 or 128";
+  if (c->max_batch < 1 || c->max_batch > 1024) return "max_batch must be in [1, 1024]";
+  if (c->max_pages < 1 || (long long)c->max_pages * c->page_size > (1 << 24)) return "max_pages must be >= 1 and max_pages * page_size at most 2^24";
+  if ((long long)c->n_layers * c->n_pages >= 0x7fffffffLL / c->n_kv_heads) return "n_layers * n_pages * n_kv_heads must stay below 2^31";
+  if (c->dtype != WKV_F32 && c->dtype != WKV_BF16) return "dtype must be WKV_F32 or WKV_BF16";
+  if (!(c->scale >= 0.f) || std::isinf(c->scale)) return "scale must be finite and >= 0";
+  if (c->scores != 0 && c->scores != 1) return "scores must be 0 or 1";
+  if ((c->k_pool == nullptr) != (c->v_pool == nullptr)) return "k_pool and v_pool must both be set or both be NULL";
+  if (((uintptr_t)c->k_pool | (uintptr_t)c->v_pool) & 15) return "k_pool and v_pool must be 16-byte aligned";
+  if ((c->alloc == nullptr) != (c->release == nullptr)) return "alloc and release must both be set or both be NULL";
+  return nullptr;
+}
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+// Arguments that decode and prefill share; fills P.  `rows`: rows of q.
+int attention_params(wkv_paged* c, wkv::PagedParams& P, int32_t layer, int32_t batch, int32_t rows, const void* q, int64_t q_stride,
+                     const void* k, const void* v, int64_t kv_stride, const int32_t* table, int32_t width, const int32_t* seq_lens,
+                     int32_t window, int32_t sink, float* scores, int64_t score_stride, void* out, float* lse) {
+  const wkv_paged_config& f = c->cfg;
+  if (layer < 0 || layer >= f.n_layers) return fail(c, WKV_ERR_INVALID, "layer out of range");
+  if (batch < 0 || batch > f.max_batch) return fail(c, WKV_ERR_INVALID, "batch must be in [0, max_batch]");
+  if (rows < 0) return fail(c, WKV_ERR_INVALID, "the number of rows must be >= 0");
+  if (width < 1 || width > f.max_pages) return fail(c, WKV_ERR_INVALID, "table_width must be in [1, max_pages]");
+  if (window < 0 || sink < 0) return fail(c, WKV_ERR_INVALID, "window and sink must be >= 0");
+  if ((k == nullptr) != (v == nullptr)) return fail(c, WKV_ERR_INVALID, "k and v must both be given or both be NULL");
+  if (batch > 0 && rows > 0 && (!q || !table || !seq_lens || !out)) return fail(c, WKV_ERR_INVALID, "q, block_table, seq_lens and out must not be NULL");
+  const int64_t q_row = (int64_t)f.n_q_heads * f.head_dim, kv_row = (int64_t)f.n_kv_heads * f.head_dim;
+  if (q_stride == 0) q_stride = q_row;
+  if (kv_stride == 0) kv_stride = kv_row;
+  if (q_stride < q_row || kv_stride < kv_row) return fail(c, WKV_ERR_INVALID, "a row stride is smaller than the row");
+  if (q_stride * (int64_t)c->elem % 16 || kv_stride * (int64_t)c->elem % 16 || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out))
+    return fail(c, WKV_ERR_INVALID, "rows of q, k, v and out must be 16-byte aligned");
+  if (scores) {
+    if (!f.scores) return fail(c, WKV_ERR_INVALID, "scores need a handle created with scores = 1");
+    if (score_stride < (int64_t)width * f.page_size) return fail(c, WKV_ERR_INVALID, "score_stride must be >= table_width * page_size");
+  }
+  std::memset(&P, 0, sizeof(P));
+  const size_t layer_bytes = (size_t)f.n_pages * f.n_kv_heads * f.page_size * f.head_dim * c->elem;
+  P.k_pool = (char*)c->k_pool + layer * layer_bytes;
+  P.v_pool = (char*)c->v_pool + layer * layer_bytes;
+  P.q = q; P.k = k; P.v = v; P.q_stride = q_stride; P.kv_stride = kv_stride;
+  P.table = table; P.seq_lens = seq_lens; P.out = out; P.lse = lse; P.scores = scores; P.score_stride = score_stride;
+  P.status = c->status; P.batch = batch; P.rows = rows; P.width = width; P.n_pages = f.n_pages;
+  P.n_q_heads = f.n_q_heads; P.n_kv_heads = f.n_kv_heads; P.page = f.page_size; P.page_shift = c->page_shift;
+  P.window = window; P.sink = sink; P.scale = c->scale; P.scale_log2 = c->scale * wkv::kLog2e;
+  return WKV_OK;
+}
+
+// All launches: programmatic stream serialization, each kernel waits for its predecessor first thing.
+template <typename... A, typename... B>
+cudaError_t launch(wkv_paged* c, void (*kernel)(A...), long long grid, int threads, size_t smem, B&&... args) {
+  cudaLaunchConfig_t lc = {};
+  lc.gridDim = dim3((unsigned)grid);
+  lc.blockDim = dim3((unsigned)threads);
+  lc.dynamicSmemBytes = smem;
+  lc.stream = c->stream;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  lc.attrs = at;
+  lc.numAttrs = 1;
+  c->launches++;
+  return cudaLaunchKernelEx(&lc, kernel, std::forward<B>(args)...);
+}
+
+template <typename T, int D>
+cudaError_t attend(wkv_paged* c, const wkv::PagedParams& P) {
+  cudaError_t e = cudaSuccess;
+  if (P.k) e = launch(c, wkv::paged_append_kernel<T, D>, ((long long)P.rows * P.n_kv_heads + 3) / 4, 128, 0, P);
+  if (e == cudaSuccess) e = launch(c, wkv::paged_attend_kernel<T, D>, ((long long)P.rows * P.n_q_heads + 3) / 4, 128, 0, P);
+  if (e == cudaSuccess && P.scores) {
+    const int entries = P.width * P.page;
+    e = launch(c, wkv::paged_weights_kernel<T, D>, ((long long)P.batch * P.n_kv_heads * entries + 3) / 4, 128, 0, P, entries);
+  }
+  return e;
+}
+
+int attend_any(wkv_paged* c, const wkv::PagedParams& P) {
+  if (P.batch == 0 || P.rows == 0) return WKV_OK;
+  const bool wide = c->cfg.head_dim == 128;
+  cudaError_t e;
+  if (c->cfg.dtype == WKV_BF16) e = wide ? attend<__nv_bfloat16, 128>(c, P) : attend<__nv_bfloat16, 64>(c, P);
+  else e = wide ? attend<float, 128>(c, P) : attend<float, 64>(c, P);
+  WKV_CUDA(c, e);
+  return WKV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+const char* wkv_paged_config_error(const wkv_paged_config* cfg) { return check_config(cfg); }
+
+int wkv_paged_create(const wkv_paged_config* cfg, wkv_paged** out) {
+  if (!out) return WKV_ERR_INVALID;
+  *out = nullptr;
+  if (check_config(cfg) != nullptr) return WKV_ERR_INVALID;
+  wkv_paged* c = new (std::nothrow) wkv_paged;
+  if (!c) return WKV_ERR_ALLOC;
+  c->cfg = *cfg;
+  if (!c->cfg.alloc) { c->cfg.alloc = default_alloc; c->cfg.release = default_release; c->cfg.user = nullptr; }
+  cudaError_t e = cudaGetDevice(&c->device);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&c->sm_count, cudaDevAttrMultiProcessorCount, c->device);
+  if (e != cudaSuccess) { delete c; return WKV_ERR_CUDA; }
+  c->group = cfg->n_q_heads / cfg->n_kv_heads;
+  c->page_shift = cfg->page_size == 16 ? 4 : cfg->page_size == 32 ? 5 : 6;
+  c->scale = cfg->scale != 0.f ? cfg->scale : (float)(1.0 / std::sqrt((double)cfg->head_dim));
+  c->elem = cfg->dtype == WKV_BF16 ? 2 : 4;
+  c->stream = reinterpret_cast<cudaStream_t>(cfg->stream);
+  c->k_pool = cfg->k_pool;
+  c->v_pool = cfg->v_pool;
+  const size_t pool = (size_t)cfg->n_layers * cfg->n_pages * cfg->n_kv_heads * cfg->page_size * cfg->head_dim * c->elem;
+  const size_t lanes = (size_t)cfg->max_batch * cfg->n_kv_heads, heads = (size_t)cfg->max_batch * cfg->n_q_heads;
+  int rc = WKV_OK;
+#define WKV_TAKE(dst, bytes) do { if (rc == WKV_OK) rc = take(c, dst, bytes); } while (0)
+  WKV_TAKE(&c->status, 256);
+  WKV_TAKE(&c->lse, heads * 4);
+  if (cfg->scores) {
+    WKV_TAKE(&c->logits, heads * cfg->max_pages * cfg->page_size * 4);
+    WKV_TAKE(&c->n_moved, lanes * 4);
+  }
+  const bool own_pools = !c->k_pool;
+  if (own_pools) {
+    WKV_TAKE(&c->k_pool, pool);
+    WKV_TAKE(&c->v_pool, pool);
+  }
+#undef WKV_TAKE
+  if (rc == WKV_OK) {
+    e = cudaMemsetAsync(c->status, 0, 4, c->stream);
+    if (e == cudaSuccess && own_pools) e = cudaMemsetAsync(c->k_pool, 0, pool, c->stream);
+    if (e == cudaSuccess && own_pools) e = cudaMemsetAsync(c->v_pool, 0, pool, c->stream);
+    if (e != cudaSuccess) rc = WKV_ERR_CUDA;
+  }
+  if (rc != WKV_OK) {
+    wkv_paged_destroy(c);
+    return rc;
+  }
+  *out = c;
+  return WKV_OK;
+}
+
+void wkv_paged_destroy(wkv_paged* c) {
+  if (!c) return;
+  for (void* p : c->owned) c->cfg.release(p, c->cfg.user);
+  delete c;
+}
+
+int wkv_paged_set_stream(wkv_paged* c, void* stream) {
+  if (!c) return WKV_ERR_INVALID;
+  c->stream = reinterpret_cast<cudaStream_t>(stream);
+  return WKV_OK;
+}
+
+int wkv_paged_pools(const wkv_paged* c, void** k_pool, void** v_pool) {
+  if (!c || !k_pool || !v_pool) return WKV_ERR_INVALID;
+  *k_pool = c->k_pool;
+  *v_pool = c->v_pool;
+  return WKV_OK;
+}
+
+int wkv_paged_decode(wkv_paged* c, int32_t layer, int32_t batch, const void* q, int64_t q_stride, const void* k, const void* v,
+                     int64_t kv_stride, const int32_t* block_table, int32_t table_width, const int32_t* seq_lens,
+                     int32_t window, int32_t sink, float* scores, int64_t score_stride, void* out, float* lse) {
+  if (!c) return WKV_ERR_INVALID;
+  DeviceGuard on(c->device);
+  WKV_CUDA(c, on.err);
+  wkv::PagedParams P;
+  const int rc = attention_params(c, P, layer, batch, batch, q, q_stride, k, v, kv_stride, block_table, table_width, seq_lens, window,
+                                  sink, scores, score_stride, out, lse ? lse : c->lse);
+  if (rc != WKV_OK) return rc;
+  return attend_any(c, P);
+}
+
+int wkv_paged_prefill(wkv_paged* c, int32_t layer, int32_t batch, const void* q, int64_t q_stride, const void* k, const void* v,
+                      int64_t kv_stride, const int32_t* q_start, int32_t total_q, const int32_t* block_table,
+                      int32_t table_width, const int32_t* seq_lens, int32_t window, int32_t sink, float* scores,
+                      int64_t score_stride, void* out, float* lse) {
+  if (!c) return WKV_ERR_INVALID;
+  DeviceGuard on(c->device);
+  WKV_CUDA(c, on.err);
+  wkv::PagedParams P;
+  const int rc = attention_params(c, P, layer, batch, total_q, q, q_stride, k, v, kv_stride, block_table, table_width, seq_lens, window,
+                                  sink, scores, score_stride, out, lse);
+  if (rc != WKV_OK) return rc;
+  if (total_q > (1 << 24)) return fail(c, WKV_ERR_INVALID, "total_q must be at most 2^24");
+  if (batch > 0 && total_q > 0 && !q_start) return fail(c, WKV_ERR_INVALID, "q_start must not be NULL");
+  if (scores && !lse) return fail(c, WKV_ERR_INVALID, "scores need lse");
+  P.q_start = q_start;
+  return attend_any(c, P);
+}
+
+int wkv_paged_evict(wkv_paged* c, int32_t layer, int32_t batch, const int32_t* src_table, int32_t src_width,
+                    const int32_t* dst_table, int32_t dst_width, const int32_t* seq_lens, int32_t* new_lens, int32_t budget,
+                    int32_t recent, int32_t sink, const float* scores, int64_t score_stride, float* scores_out,
+                    int64_t out_stride, int32_t* kept) {
+  if (!c) return WKV_ERR_INVALID;
+  DeviceGuard on(c->device);
+  WKV_CUDA(c, on.err);
+  const wkv_paged_config& f = c->cfg;
+  if (!f.scores) return fail(c, WKV_ERR_INVALID, "eviction needs a handle created with scores = 1");
+  if (layer < 0 || layer >= f.n_layers) return fail(c, WKV_ERR_INVALID, "layer out of range");
+  if (batch < 0 || batch > f.max_batch) return fail(c, WKV_ERR_INVALID, "batch must be in [0, max_batch]");
+  if (src_width < 1 || src_width > f.max_pages || dst_width < 1) return fail(c, WKV_ERR_INVALID, "src_width must be in [1, max_pages], dst_width >= 1");
+  if (budget < 1 || recent < 0 || sink < 0 || (int64_t)recent + sink > budget) return fail(c, WKV_ERR_INVALID, "budget must be >= 1 and >= sink + recent, both >= 0");
+  const int64_t most = (int64_t)src_width * f.page_size, left = budget < most ? budget : most;
+  if ((int64_t)dst_width * f.page_size < left) return fail(c, WKV_ERR_INVALID, "dst_table has too few pages for min(budget, src_width * page_size) entries");
+  if (score_stride < most) return fail(c, WKV_ERR_INVALID, "score_stride must be >= src_width * page_size");
+  if (scores_out && out_stride < left) return fail(c, WKV_ERR_INVALID, "out_stride must be >= min(budget, src_width * page_size)");
+  if (batch == 0) return WKV_OK;
+  if (!src_table || !dst_table || !seq_lens || !new_lens || !scores) return fail(c, WKV_ERR_INVALID, "src_table, dst_table, seq_lens, new_lens and scores must not be NULL");
+  if (scores_out == scores || (const int32_t*)new_lens == seq_lens) return fail(c, WKV_ERR_INVALID, "scores_out and new_lens must not be the arrays that the call reads");
+  wkv::EvictParams P;
+  std::memset(&P, 0, sizeof(P));
+  const size_t layer_bytes = (size_t)f.n_pages * f.n_kv_heads * f.page_size * f.head_dim * c->elem;
+  P.k_pool = (char*)c->k_pool + layer * layer_bytes;
+  P.v_pool = (char*)c->v_pool + layer * layer_bytes;
+  P.src_table = src_table; P.dst_table = dst_table; P.seq_lens = seq_lens; P.new_lens = new_lens;
+  P.scores = scores; P.score_stride = score_stride; P.scores_out = scores_out; P.out_stride = out_stride;
+  P.kept = kept ? kept : reinterpret_cast<int32_t*>(c->logits);
+  P.kept_stride = kept ? budget : left;
+  P.n_moved = c->n_moved; P.status = c->status;
+  P.batch = batch; P.src_width = src_width; P.dst_width = dst_width; P.n_pages = f.n_pages; P.n_kv_heads = f.n_kv_heads;
+  P.page = f.page_size; P.page_shift = c->page_shift; P.budget = budget; P.recent = recent; P.sink = sink;
+  const long long lanes = (long long)batch * f.n_kv_heads;
+  cudaError_t e = launch(c, wkv::paged_select_kernel, lanes, wkv::kSelectThreads, 0, P);
+  if (e == cudaSuccess) {
+    const int per_lane = (int)((left * 2 * f.head_dim * (int64_t)c->elem / 16 + 1023) / 1024);
+    const bool wide = f.head_dim == 128;
+    auto kernel = f.dtype == WKV_BF16 ? (wide ? wkv::paged_move_kernel<__nv_bfloat16, 128> : wkv::paged_move_kernel<__nv_bfloat16, 64>)
+                                      : (wide ? wkv::paged_move_kernel<float, 128> : wkv::paged_move_kernel<float, 64>);
+    e = launch(c, kernel, lanes * per_lane, 256, 0, P, per_lane);
+  }
+  WKV_CUDA(c, e);
+  return WKV_OK;
+}
+
+int wkv_paged_status(wkv_paged* c) {
+  if (!c) return WKV_ERR_INVALID;
+  DeviceGuard on(c->device);
+  WKV_CUDA(c, on.err);
+  uint32_t w = 0;
+  WKV_CUDA(c, cudaStreamSynchronize(c->stream));
+  WKV_CUDA(c, cudaMemcpy(&w, c->status, 4, cudaMemcpyDeviceToHost));
+  if (w) {
+    WKV_CUDA(c, cudaMemset(c->status, 0, 4));
+    if (w & wkv::kStatusWaitTimeout) return fail(c, WKV_ERR_TIMEOUT, "a bounded wait inside a kernel gave up");
+    return fail(c, WKV_ERR_STATE, "a page number, length or row offset was out of range, or an eviction's tables overlap");
+  }
+  return WKV_OK;
+}
+
+int64_t wkv_paged_launch_count(const wkv_paged* c) { return c ? c->launches : 0; }
+int64_t wkv_paged_device_bytes(const wkv_paged* c) { return c ? c->device_bytes : 0; }
+const char* wkv_paged_last_error(const wkv_paged* c) { return c ? c->last_error.c_str() : ""; }
+
+}  // extern "C"
