@@ -1,4 +1,5 @@
 // Host side of the paged cache declared in include/wkv.h: configuration checks, workspaces, launches.
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <cstring>
@@ -10,6 +11,7 @@
 
 #include "../../include/wkv.h"
 #include "wkv_paged.cuh"
+#include "wkv_paged_decode.cuh"
 
 struct wkv_paged {
   wkv_paged_config cfg;
@@ -23,8 +25,18 @@ struct wkv_paged {
   void* k_pool = nullptr;
   void* v_pool = nullptr;
   uint32_t* status = nullptr;
-  float* lse = nullptr;                // [max_batch][Hq]: log-sums of a decode call whose caller wants none
-  float* logits = nullptr;             // [max_batch][Hq][max_pages * page_size]; kept indexes of an eviction
+  float* logits = nullptr;             // [max_batch][Hq][max_pages * page_size]: a decode step's; kept indexes of an eviction
+  float2* head_ml = nullptr;           // [max_batch][Hq]: a decode step's (max, 1 / sum), for the weights
+  // decode: partials of the pieces, arrivals per lane
+  const void* decode_kernel = nullptr;
+  const void* fold_kernel = nullptr;
+  int decode_ctas = 0, decode_smem = 0;
+  float* part = nullptr;
+  float2* part_ml = nullptr;
+  uint32_t* arrived = nullptr;
+  // the pools as [chunk][part][row][128 bytes], boxes of a page's rows (at most a decode tile's) x all parts
+  alignas(64) unsigned char page_kmap[128] = {};
+  alignas(64) unsigned char page_vmap[128] = {};
   int32_t* n_moved = nullptr;          // [max_batch][Hkv]
   std::vector<void*> owned;
   long long device_bytes = 0;
@@ -97,6 +109,57 @@ const char* check_config(const wkv_paged_config* c) {
   return nullptr;
 }
 
+// One of the pools as a 4-d tensor: 128 bytes of a row, rows of a chunk, the row's 128-byte parts, chunks; boxes of box_rows
+// rows x box_parts parts, 128-byte swizzle, zeros outside.
+int encode_pool(wkv_paged* c, unsigned char* out128, void* pool, int box_rows, int box_parts) {
+  typedef CUresult (*encode_fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  static_assert(sizeof(CUtensorMap) == 128, "tensor map size");
+  void* sym = nullptr;
+  cudaDriverEntryPointQueryResult qr = cudaDriverEntryPointSymbolNotFound;
+  cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &qr);
+  if (e != cudaSuccess) return cuda_fail(c, e, "cudaGetDriverEntryPoint(cuTensorMapEncodeTiled)");
+  if (qr != cudaDriverEntryPointSuccess || !sym) return fail(c, WKV_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
+  const wkv_paged_config& f = c->cfg;
+  const cuuint64_t row = (cuuint64_t)f.head_dim * c->elem;
+  const cuuint32_t elems = (cuuint32_t)(128 / c->elem);
+  const cuuint64_t dims[4] = {elems, (cuuint64_t)f.page_size, row / 128, (cuuint64_t)f.n_layers * f.n_pages * f.n_kv_heads};
+  const cuuint64_t strides[3] = {row, 128, row * f.page_size};
+  const cuuint32_t box[4] = {elems, (cuuint32_t)box_rows, (cuuint32_t)box_parts, 1u};
+  const cuuint32_t estr[4] = {1u, 1u, 1u, 1u};
+  CUtensorMap m;
+  const CUresult r = reinterpret_cast<encode_fn>(sym)(&m, f.dtype == WKV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4,
+                                                      pool, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(c, WKV_ERR_CUDA, "cuTensorMapEncodeTiled failed with code " + std::to_string((int)r));
+  std::memcpy(out128, &m, sizeof(m));
+  return WKV_OK;
+}
+
+// Picks this handle's instantiations and how many decode CTAs the GPU holds at once.
+template <typename T, int D, int G>
+cudaError_t pick_kernels(wkv_paged* c) {
+  auto kernel = wkv::paged_decode_kernel<T, D, G>;
+  c->decode_kernel = (const void*)kernel;
+  c->fold_kernel = (const void*)wkv::paged_fold_kernel<G>;
+  c->decode_smem = wkv::decode_smem<T, D, G>();
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, c->decode_smem);
+  int per_sm = 0;
+  if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, wkv::kDecodeThreads, c->decode_smem);
+  c->decode_ctas = c->sm_count * (per_sm < 1 ? 1 : per_sm);
+  return e;
+}
+template <typename T, int D>
+cudaError_t pick_by_group(wkv_paged* c) {
+  switch (c->group) {
+    case 1: return pick_kernels<T, D, 1>(c);
+    case 2: return pick_kernels<T, D, 2>(c);
+    case 4: return pick_kernels<T, D, 4>(c);
+    default: return pick_kernels<T, D, 8>(c);
+  }
+}
+
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 // Arguments that decode and prefill share; fills P.  `rows`: rows of q.
@@ -150,6 +213,29 @@ cudaError_t launch(wkv_paged* c, void (*kernel)(A...), long long grid, int threa
   return cudaLaunchKernelEx(&lc, kernel, std::forward<B>(args)...);
 }
 
+int decode(wkv_paged* c, const wkv::PagedParams& A) {
+  if (A.batch == 0) return WKV_OK;
+  wkv::DecodeParams P;
+  std::memset(&P, 0, sizeof(P));
+  P.A = A;
+  P.part = c->part; P.part_ml = c->part_ml; P.arrived = c->arrived;
+  P.logits = A.scores ? c->logits : nullptr;
+  P.head_ml = c->head_ml;
+  P.oob_chunk = c->cfg.n_layers * c->cfg.n_pages * c->cfg.n_kv_heads;
+  P.chunk0 = (int)(((char*)A.k_pool - (char*)c->k_pool) / ((size_t)A.page * c->cfg.head_dim * c->elem));
+  std::memcpy(P.kmap, c->page_kmap, 128);
+  std::memcpy(P.vmap, c->page_vmap, 128);
+  typedef void (*decode_fn)(const wkv::DecodeParams);
+  typedef void (*fold_fn)(const wkv::DecodeParams, int);
+  cudaError_t e = launch(c, (decode_fn)c->decode_kernel, c->decode_ctas, wkv::kDecodeThreads, c->decode_smem, P);
+  if (e == cudaSuccess && A.scores) {
+    const int per_lane = (A.width * A.page + wkv::kFoldEntries - 1) / wkv::kFoldEntries;
+    e = launch(c, (fold_fn)c->fold_kernel, (long long)A.batch * A.n_kv_heads * per_lane, wkv::kFoldEntries / 4, 0, P, per_lane);
+  }
+  WKV_CUDA(c, e);
+  return WKV_OK;
+}
+
 template <typename T, int D>
 cudaError_t attend(wkv_paged* c, const wkv::PagedParams& P) {
   cudaError_t e = cudaSuccess;
@@ -198,14 +284,21 @@ int wkv_paged_create(const wkv_paged_config* cfg, wkv_paged** out) {
   c->v_pool = cfg->v_pool;
   const size_t pool = (size_t)cfg->n_layers * cfg->n_pages * cfg->n_kv_heads * cfg->page_size * cfg->head_dim * c->elem;
   const size_t lanes = (size_t)cfg->max_batch * cfg->n_kv_heads, heads = (size_t)cfg->max_batch * cfg->n_q_heads;
+  const bool wide = cfg->head_dim == 128;
+  if (cfg->dtype == WKV_BF16) e = wide ? pick_by_group<__nv_bfloat16, 128>(c) : pick_by_group<__nv_bfloat16, 64>(c);
+  else e = wide ? pick_by_group<float, 128>(c) : pick_by_group<float, 64>(c);
+  if (e != cudaSuccess) { delete c; return WKV_ERR_CUDA; }
   int rc = WKV_OK;
 #define WKV_TAKE(dst, bytes) do { if (rc == WKV_OK) rc = take(c, dst, bytes); } while (0)
   WKV_TAKE(&c->status, 256);
-  WKV_TAKE(&c->lse, heads * 4);
   if (cfg->scores) {
     WKV_TAKE(&c->logits, heads * cfg->max_pages * cfg->page_size * 4);
+    WKV_TAKE(&c->head_ml, heads * 8);
     WKV_TAKE(&c->n_moved, lanes * 4);
   }
+  WKV_TAKE(&c->part, ((size_t)c->decode_ctas + lanes) * c->group * cfg->head_dim * 4);
+  WKV_TAKE(&c->part_ml, ((size_t)c->decode_ctas + lanes) * c->group * 8);
+  WKV_TAKE(&c->arrived, lanes * 4);
   const bool own_pools = !c->k_pool;
   if (own_pools) {
     WKV_TAKE(&c->k_pool, pool);
@@ -214,9 +307,15 @@ int wkv_paged_create(const wkv_paged_config* cfg, wkv_paged** out) {
 #undef WKV_TAKE
   if (rc == WKV_OK) {
     e = cudaMemsetAsync(c->status, 0, 4, c->stream);
+    if (e == cudaSuccess) e = cudaMemsetAsync(c->arrived, 0, lanes * 4, c->stream);
     if (e == cudaSuccess && own_pools) e = cudaMemsetAsync(c->k_pool, 0, pool, c->stream);
     if (e == cudaSuccess && own_pools) e = cudaMemsetAsync(c->v_pool, 0, pool, c->stream);
     if (e != cudaSuccess) rc = WKV_ERR_CUDA;
+  }
+  {
+    const int rows = cfg->dtype == WKV_BF16 ? cfg->page_size : std::min(cfg->page_size, 32), parts = (int)(cfg->head_dim * c->elem / 128);
+    if (rc == WKV_OK) rc = encode_pool(c, c->page_kmap, c->k_pool, rows, parts);
+    if (rc == WKV_OK) rc = encode_pool(c, c->page_vmap, c->v_pool, rows, parts);
   }
   if (rc != WKV_OK) {
     wkv_paged_destroy(c);
@@ -253,9 +352,9 @@ int wkv_paged_decode(wkv_paged* c, int32_t layer, int32_t batch, const void* q, 
   WKV_CUDA(c, on.err);
   wkv::PagedParams P;
   const int rc = attention_params(c, P, layer, batch, batch, q, q_stride, k, v, kv_stride, block_table, table_width, seq_lens, window,
-                                  sink, scores, score_stride, out, lse ? lse : c->lse);
+                                  sink, scores, score_stride, out, lse);
   if (rc != WKV_OK) return rc;
-  return attend_any(c, P);
+  return decode(c, P);
 }
 
 int wkv_paged_prefill(wkv_paged* c, int32_t layer, int32_t batch, const void* q, int64_t q_stride, const void* k, const void* v,
@@ -330,6 +429,8 @@ int wkv_paged_status(wkv_paged* c) {
   WKV_CUDA(c, cudaMemcpy(&w, c->status, 4, cudaMemcpyDeviceToHost));
   if (w) {
     WKV_CUDA(c, cudaMemset(c->status, 0, 4));
+    // a piece that gave up may have left its lane's arrivals uncounted
+    if (w & wkv::kStatusWaitTimeout) WKV_CUDA(c, cudaMemset(c->arrived, 0, (size_t)c->cfg.max_batch * c->cfg.n_kv_heads * 4));
     if (w & wkv::kStatusWaitTimeout) return fail(c, WKV_ERR_TIMEOUT, "a bounded wait inside a kernel gave up");
     return fail(c, WKV_ERR_STATE, "a page number, length or row offset was out of range, or an eviction's tables overlap");
   }
