@@ -314,6 +314,7 @@ class PagedCache:
         _need((k_pool is None) == (v_pool is None), "k_pool and v_pool must both be given or both be None")
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index
         with torch.cuda.device(self.device):
             if k_pool is None:
                 k_pool = torch.zeros(self.shape, dtype=self.tdtype, device=self.device)
@@ -360,29 +361,34 @@ class PagedCache:
         except Exception:
             pass
 
+    # A call's checks run on every step of a decode loop: each is a few attribute reads, and the text is made on failure only.
     def _packed(self, name, t, dtype, *shape):
-        """Address of an optional packed tensor whose shape is checked (-1: any size)."""
+        """Address of an optional packed tensor whose shape is checked (a last size of -1: any)."""
         if t is None:
             return None
-        _need(t.dtype == dtype and t.device == self.device and t.is_contiguous() and t.dim() == len(shape)
-              and all(w in (-1, n) for w, n in zip(shape, t.shape)),
-              f"{name} must be a contiguous {dtype} tensor of shape {list(shape)} on {self.device}")
-        return C.c_void_p(t.data_ptr())
+        got = t.shape
+        if (t.dtype is not dtype or t.get_device() != self._index or not t.is_contiguous()
+                or (got != shape and (shape[-1] != -1 or len(got) != len(shape) or got[:-1] != shape[:-1]))):
+            raise WkvError(WKV_ERR_INVALID, f"{name} must be a contiguous {dtype} tensor of shape {list(shape)} on {self.device}")
+        return t.data_ptr()
 
     def _rows(self, name, t, n, heads):
         """Address and row stride of [n, heads, head_dim] whose rows may lie apart (columns of a wider projection)."""
         d = self.head_dim
-        _need(t.dtype == self.tdtype and t.device == self.device and tuple(t.shape) == (n, heads, d)
-              and (t.numel() == 0 or (t.stride(2) == 1 and (heads == 1 or t.stride(1) == d))),
-              f"{name} must be a {self.tdtype} tensor [{n}, {heads}, {d}] on {self.device} whose rows are packed")
-        return C.c_void_p(t.data_ptr()), (t.stride(0) if n > 1 else heads * d)
+        row, head, one = t.stride() if t.dim() == 3 else (0, 0, 0)
+        if (t.dtype is not self.tdtype or t.get_device() != self._index or t.shape != (n, heads, d)
+                or (n > 0 and (one != 1 or (heads > 1 and head != d)))):
+            raise WkvError(WKV_ERR_INVALID, f"{name} must be a {self.tdtype} tensor [{n}, {heads}, {d}] on {self.device} whose rows are packed")
+        return t.data_ptr(), (row if n > 1 else heads * d)
 
     def _new_rows(self, k, v, n):
-        _need((k is None) == (v is None), "k and v must both be given or both be None")
+        if (k is None) != (v is None):
+            raise WkvError(WKV_ERR_INVALID, "k and v must both be given or both be None")
         if k is None:
             return None, None, 0
         (kp, ks), (vp, vs) = self._rows("k", k, n, self.n_kv_heads), self._rows("v", v, n, self.n_kv_heads)
-        _need(ks == vs, "k and v must have the same row stride")
+        if ks != vs:
+            raise WkvError(WKV_ERR_INVALID, "k and v must have the same row stride")
         return kp, vp, ks
 
     def _scores(self, name, scores, batch):

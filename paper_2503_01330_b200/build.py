@@ -13,7 +13,8 @@ HEADER = os.path.join("..", "..", "include", "wkv.h")
 # source -> what it includes; each is compiled to an object of its own, rebuilt when one of them is newer
 UNITS = {
     "wkv_api.cu": ["wkv_ptx.cuh", "wkv_kernels.cuh", "wkv_prefill.cuh", "wkv_block.cuh", HEADER],
-    "wkv_paged_api.cu": ["wkv_ptx.cuh", "wkv_paged.cuh", "wkv_paged_decode.cuh", HEADER],
+    "wkv_paged_api.cu": ["wkv_ptx.cuh", "wkv_paged.cuh", "wkv_paged_decode.cuh",
+                         "wkv_paged_prefill.cuh", "wkv_tcgen05.cuh", HEADER],
 }
 SOURCES = list(UNITS)
 DEPS = sorted(set(SOURCES) | {d for deps in UNITS.values() for d in deps})

@@ -12,6 +12,7 @@
 #include "../../include/wkv.h"
 #include "wkv_paged.cuh"
 #include "wkv_paged_decode.cuh"
+#include "wkv_paged_prefill.cuh"
 
 struct wkv_paged {
   wkv_paged_config cfg;
@@ -37,6 +38,10 @@ struct wkv_paged {
   // the pools as [chunk][part][row][128 bytes], boxes of a page's rows (at most a decode tile's) x all parts
   alignas(64) unsigned char page_kmap[128] = {};
   alignas(64) unsigned char page_vmap[128] = {};
+  // ... in boxes of one part, for prompts on bf16 rows
+  alignas(64) unsigned char part_kmap[128] = {};
+  alignas(64) unsigned char part_vmap[128] = {};
+  void* encode = nullptr;              // the driver's cuTensorMapEncodeTiled
   int32_t* n_moved = nullptr;          // [max_batch][Hkv]
   std::vector<void*> owned;
   long long device_bytes = 0;
@@ -109,32 +114,42 @@ const char* check_config(const wkv_paged_config* c) {
   return nullptr;
 }
 
-// One of the pools as a 4-d tensor: 128 bytes of a row, rows of a chunk, the row's 128-byte parts, chunks; boxes of box_rows
-// rows x box_parts parts, 128-byte swizzle, zeros outside.
-int encode_pool(wkv_paged* c, unsigned char* out128, void* pool, int box_rows, int box_parts) {
+// Tensor maps: 4-d, the innermost dimension 128 bytes wide, 128-byte swizzle, zeros outside.
+int encode_map(wkv_paged* c, unsigned char* out128, const void* base, const cuuint64_t (&dims)[4], const cuuint64_t (&strides)[3],
+               const cuuint32_t (&box)[4]) {
   typedef CUresult (*encode_fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
   static_assert(sizeof(CUtensorMap) == 128, "tensor map size");
-  void* sym = nullptr;
-  cudaDriverEntryPointQueryResult qr = cudaDriverEntryPointSymbolNotFound;
-  cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &qr);
-  if (e != cudaSuccess) return cuda_fail(c, e, "cudaGetDriverEntryPoint(cuTensorMapEncodeTiled)");
-  if (qr != cudaDriverEntryPointSuccess || !sym) return fail(c, WKV_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
-  const wkv_paged_config& f = c->cfg;
-  const cuuint64_t row = (cuuint64_t)f.head_dim * c->elem;
-  const cuuint32_t elems = (cuuint32_t)(128 / c->elem);
-  const cuuint64_t dims[4] = {elems, (cuuint64_t)f.page_size, row / 128, (cuuint64_t)f.n_layers * f.n_pages * f.n_kv_heads};
-  const cuuint64_t strides[3] = {row, 128, row * f.page_size};
-  const cuuint32_t box[4] = {elems, (cuuint32_t)box_rows, (cuuint32_t)box_parts, 1u};
+  if (!c->encode) {
+    cudaDriverEntryPointQueryResult qr = cudaDriverEntryPointSymbolNotFound;
+    const cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &c->encode, cudaEnableDefault, &qr);
+    if (e != cudaSuccess) return cuda_fail(c, e, "cudaGetDriverEntryPoint(cuTensorMapEncodeTiled)");
+    if (qr != cudaDriverEntryPointSuccess || !c->encode) return fail(c, WKV_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
+  }
   const cuuint32_t estr[4] = {1u, 1u, 1u, 1u};
   CUtensorMap m;
-  const CUresult r = reinterpret_cast<encode_fn>(sym)(&m, f.dtype == WKV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4,
-                                                      pool, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                                                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  const CUresult r = reinterpret_cast<encode_fn>(c->encode)(
+      &m, c->cfg.dtype == WKV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, const_cast<void*>(base), dims, strides,
+      box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return fail(c, WKV_ERR_CUDA, "cuTensorMapEncodeTiled failed with code " + std::to_string((int)r));
   std::memcpy(out128, &m, sizeof(m));
   return WKV_OK;
+}
+// A pool: 128 bytes of a row, rows of a chunk, the row's 128-byte parts, chunks; boxes of box_rows rows x box_parts parts.
+int encode_pool(wkv_paged* c, unsigned char* out128, void* pool, int box_rows, int box_parts) {
+  const wkv_paged_config& f = c->cfg;
+  const cuuint64_t row = (cuuint64_t)f.head_dim * c->elem;
+  const cuuint32_t elems = (cuuint32_t)(128 / c->elem);
+  return encode_map(c, out128, pool, {elems, (cuuint64_t)f.page_size, row / 128, (cuuint64_t)f.n_layers * f.n_pages * f.n_kv_heads},
+                    {row, 128, row * f.page_size}, {elems, (cuuint32_t)box_rows, (cuuint32_t)box_parts, 1u});
+}
+// A call's q: 128 bytes of a row, heads, tokens, parts; boxes of 128 rows (token, head of a group) x one part.
+int encode_queries(wkv_paged* c, unsigned char* out128, const wkv::PagedParams& P) {
+  const cuuint64_t row = (cuuint64_t)c->cfg.head_dim * c->elem;
+  const cuuint32_t elems = (cuuint32_t)(128 / c->elem), G = (cuuint32_t)c->group;
+  return encode_map(c, out128, P.q, {elems, (cuuint64_t)P.n_q_heads, (cuuint64_t)P.rows, row / 128}, {row, (cuuint64_t)P.q_stride * c->elem, 128},
+                    {elems, G, 128u / G, 1u});
 }
 
 // Picks this handle's instantiations and how many decode CTAs the GPU holds at once.
@@ -148,6 +163,10 @@ cudaError_t pick_kernels(wkv_paged* c) {
   int per_sm = 0;
   if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, wkv::kDecodeThreads, c->decode_smem);
   c->decode_ctas = c->sm_count * (per_sm < 1 ? 1 : per_sm);
+  if constexpr (sizeof(T) == 2) {
+    if (e == cudaSuccess)
+      e = cudaFuncSetAttribute(wkv::paged_prefill_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, wkv::PrefillShape<D>::kSmem);
+  }
   return e;
 }
 template <typename T, int D>
@@ -213,6 +232,11 @@ cudaError_t launch(wkv_paged* c, void (*kernel)(A...), long long grid, int threa
   return cudaLaunchKernelEx(&lc, kernel, std::forward<B>(args)...);
 }
 
+// The layer's first chunk.
+int chunk0(const wkv_paged* c, const wkv::PagedParams& P) {
+  return (int)(((char*)P.k_pool - (char*)c->k_pool) / ((size_t)P.page * c->cfg.head_dim * c->elem));
+}
+
 int decode(wkv_paged* c, const wkv::PagedParams& A) {
   if (A.batch == 0) return WKV_OK;
   wkv::DecodeParams P;
@@ -222,7 +246,7 @@ int decode(wkv_paged* c, const wkv::PagedParams& A) {
   P.logits = A.scores ? c->logits : nullptr;
   P.head_ml = c->head_ml;
   P.oob_chunk = c->cfg.n_layers * c->cfg.n_pages * c->cfg.n_kv_heads;
-  P.chunk0 = (int)(((char*)A.k_pool - (char*)c->k_pool) / ((size_t)A.page * c->cfg.head_dim * c->elem));
+  P.chunk0 = chunk0(c, A);
   std::memcpy(P.kmap, c->page_kmap, 128);
   std::memcpy(P.vmap, c->page_vmap, 128);
   typedef void (*decode_fn)(const wkv::DecodeParams);
@@ -236,26 +260,48 @@ int decode(wkv_paged* c, const wkv::PagedParams& A) {
   return WKV_OK;
 }
 
-template <typename T, int D>
-cudaError_t attend(wkv_paged* c, const wkv::PagedParams& P) {
-  cudaError_t e = cudaSuccess;
-  if (P.k) e = launch(c, wkv::paged_append_kernel<T, D>, ((long long)P.rows * P.n_kv_heads + 3) / 4, 128, 0, P);
-  if (e == cudaSuccess) e = launch(c, wkv::paged_attend_kernel<T, D>, ((long long)P.rows * P.n_q_heads + 3) / 4, 128, 0, P);
-  if (e == cudaSuccess && P.scores) {
-    const int entries = P.width * P.page;
-    e = launch(c, wkv::paged_weights_kernel<T, D>, ((long long)P.batch * P.n_kv_heads * entries + 3) / 4, 128, 0, P, entries);
-  }
-  return e;
+// Prompt attention on bf16 rows (tensor cores) ...
+template <int D>
+int prefill_bf16(wkv_paged* c, const wkv::PagedParams& A) {
+  wkv::PrefillParams P;
+  std::memset(&P, 0, sizeof(P));
+  P.A = A;
+  P.g_shift = c->group == 1 ? 0 : c->group == 2 ? 1 : c->group == 4 ? 2 : 3;
+  P.blocks = (int)(((long long)A.rows * c->group >> 8) + A.batch);
+  P.oob_chunk = c->cfg.n_layers * c->cfg.n_pages * c->cfg.n_kv_heads;
+  P.chunk0 = chunk0(c, A);
+  const int rc = encode_queries(c, P.qmap, A);
+  if (rc != WKV_OK) return rc;
+  std::memcpy(P.kmap, c->part_kmap, 128);
+  std::memcpy(P.vmap, c->part_vmap, 128);
+  constexpr int smem = wkv::PrefillShape<D>::kSmem;
+  WKV_CUDA(c, launch(c, wkv::paged_prefill_kernel<D>, (long long)P.blocks * A.n_kv_heads, wkv::kPrefillThreads, smem, P));
+  return WKV_OK;
+}
+// ... and on fp32 rows.
+template <int D>
+int prefill_f32(wkv_paged* c, const wkv::PagedParams& P) {
+  WKV_CUDA(c, launch(c, wkv::paged_attend_kernel<float, D>, ((long long)P.rows * P.n_q_heads + 3) / 4, 128, 0, P));
+  return WKV_OK;
 }
 
-int attend_any(wkv_paged* c, const wkv::PagedParams& P) {
+template <typename T, int D>
+int prefill_typed(wkv_paged* c, const wkv::PagedParams& P) {
+  if (P.k) WKV_CUDA(c, launch(c, wkv::paged_append_kernel<T, D>, ((long long)P.rows * P.n_kv_heads + 3) / 4, 128, 0, P));
+  int rc;
+  if constexpr (sizeof(T) == 2) rc = prefill_bf16<D>(c, P); else rc = prefill_f32<D>(c, P);
+  if (rc == WKV_OK && P.scores) {
+    const int entries = P.width * P.page;
+    WKV_CUDA(c, launch(c, wkv::paged_weights_kernel<T, D>, ((long long)P.batch * P.n_kv_heads * entries + 3) / 4, 128, 0, P, entries));
+  }
+  return rc;
+}
+
+int prefill(wkv_paged* c, const wkv::PagedParams& P) {
   if (P.batch == 0 || P.rows == 0) return WKV_OK;
   const bool wide = c->cfg.head_dim == 128;
-  cudaError_t e;
-  if (c->cfg.dtype == WKV_BF16) e = wide ? attend<__nv_bfloat16, 128>(c, P) : attend<__nv_bfloat16, 64>(c, P);
-  else e = wide ? attend<float, 128>(c, P) : attend<float, 64>(c, P);
-  WKV_CUDA(c, e);
-  return WKV_OK;
+  if (c->cfg.dtype == WKV_BF16) return wide ? prefill_typed<__nv_bfloat16, 128>(c, P) : prefill_typed<__nv_bfloat16, 64>(c, P);
+  return wide ? prefill_typed<float, 128>(c, P) : prefill_typed<float, 64>(c, P);
 }
 
 }  // namespace
@@ -316,6 +362,8 @@ int wkv_paged_create(const wkv_paged_config* cfg, wkv_paged** out) {
     const int rows = cfg->dtype == WKV_BF16 ? cfg->page_size : std::min(cfg->page_size, 32), parts = (int)(cfg->head_dim * c->elem / 128);
     if (rc == WKV_OK) rc = encode_pool(c, c->page_kmap, c->k_pool, rows, parts);
     if (rc == WKV_OK) rc = encode_pool(c, c->page_vmap, c->v_pool, rows, parts);
+    if (rc == WKV_OK && cfg->dtype == WKV_BF16) rc = encode_pool(c, c->part_kmap, c->k_pool, cfg->page_size, 1);
+    if (rc == WKV_OK && cfg->dtype == WKV_BF16) rc = encode_pool(c, c->part_vmap, c->v_pool, cfg->page_size, 1);
   }
   if (rc != WKV_OK) {
     wkv_paged_destroy(c);
@@ -372,7 +420,7 @@ int wkv_paged_prefill(wkv_paged* c, int32_t layer, int32_t batch, const void* q,
   if (batch > 0 && total_q > 0 && !q_start) return fail(c, WKV_ERR_INVALID, "q_start must not be NULL");
   if (scores && !lse) return fail(c, WKV_ERR_INVALID, "scores need lse");
   P.q_start = q_start;
-  return attend_any(c, P);
+  return prefill(c, P);
 }
 
 int wkv_paged_evict(wkv_paged* c, int32_t layer, int32_t batch, const int32_t* src_table, int32_t src_width,

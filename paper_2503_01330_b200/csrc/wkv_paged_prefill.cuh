@@ -1,0 +1,379 @@
+// Paged prompt attention on bf16 rows: chunks of new tokens of a ragged batch against their sequences' pages, under a window
+// with sinks.  Same formulas as the decode step, a causal limit per token.
+//
+// Bound: tensor cores and exponentials, 4 D flops and one exponential per (query head, visible entry); a 128 x 128 tile of
+// logits takes the SM's tensor cores 2 x 512 cycles at D = 128 and its 16 exponentials a cycle 1024 cycles, so the two have
+// to overlap.
+//
+// A CTA owns 256 rows of one kv head, a row being (token, query head of the group), token-major: grouped heads share a tile,
+// so a row tile spans 128 / G tokens and a window wastes little of it.  Two row tiles of 128 take turns: while one's logits
+// are in its softmax warps, the tensor cores work on the other's.  Warps 0-3 and 4-7: softmax of row tile 0 and 1, a thread
+// per row (a TMEM lane), so statistics need no shuffles; warp 8 issues all matrix instructions; warp 9 all copies
+// (10 and 11 idle).
+// TMEM, 512 columns: logits of both tiles (fp32, 128 columns each; the weights overwrite them as bf16, 64 columns, and are the A
+// operand of P.V straight from TMEM) and both outputs (D columns each).  An output is rescaled in place, and only when a row's
+// maximum has grown by more than 2^8 since its reference was taken.
+#pragma once
+#include "wkv_paged.cuh"
+#include "wkv_paged_decode.cuh"
+#include "wkv_tcgen05.cuh"
+
+namespace wkv {
+
+// Three warpgroups of 168 registers a thread at launch; the softmax ones hold a row of logits (128) and take what the third
+// does not need: 2 * 208 + 88 = 3 * 168.
+constexpr int kPrefillThreads = 384;
+constexpr int kPrefillKeys = 128;            // entries per tile
+
+struct PrefillParams {
+  PagedParams A;
+  int g_shift;               // log2 of the query heads per kv head
+  int blocks;                // row blocks of one kv head over all sequences, at most
+  int oob_chunk, chunk0;
+  alignas(64) unsigned char qmap[128];   // q as [part][token][head][64 elements], boxes of a row tile
+  alignas(64) unsigned char kmap[128];   // pool as [chunk][part][row][64 elements], boxes of a page x one part
+  alignas(64) unsigned char vmap[128];
+};
+
+template <int D>
+struct PrefillShape {
+  static constexpr int kParts = D / 64;
+  static constexpr int kPartBytes = 128 * 128;                    // 128 rows x 128 bytes
+  static constexpr int kTileBytes = kParts * kPartBytes;          // of Q (one row tile), K or V
+  static constexpr int kStages = D == 128 ? 5 : 8;
+  static constexpr int kSmem = 1024 + 2 * kTileBytes + kStages * kTileBytes + (2 * kStages + 8) * 8 + 32;
+};
+
+// The row block of a CTA: which sequence, which rows; and the key tiles it walks: those with sinks, then the others.
+struct PrefillBlock {
+  int b, head, first, n, len, old;      // old: entries before the chunk
+  int row0;                             // first row (token * G + g) of the block
+  int sinks, sink_tiles, first_tile, tiles;
+  __device__ __forceinline__ int tile(int v) const { return v < sink_tiles ? v : first_tile + v - sink_tiles; }
+};
+// Positions of a row tile's first and last token; none if it has no rows.
+struct RowTile {
+  bool any;
+  int pos_lo, pos_hi;
+};
+__device__ __forceinline__ RowTile row_tile(const PrefillBlock& B, int row0, int g_shift) {
+  RowTile t;
+  t.any = row0 < B.n << g_shift;
+  t.pos_lo = B.old + (row0 >> g_shift);
+  t.pos_hi = min(B.old + ((row0 + 127) >> g_shift), B.len - 1);
+  return t;
+}
+__device__ __forceinline__ bool tile_seen(const RowTile& t, int e0, int window, int sink) {
+  return t.any && e0 <= t.pos_hi && (window == 0 || e0 + kPrefillKeys > t.pos_lo - window + 1 || e0 < sink);
+}
+
+// The rb-th row block (256 rows) over all sequences; false if there is none.  Every warp searches for itself.
+__device__ __forceinline__ bool find_block(const PagedParams& A, int g_shift, int rb, int head, PrefillBlock& B) {
+  const int lane = threadIdx.x & 31;
+  int before = 0;
+  for (int base = 0; base < A.batch; base += 32) {
+    const int b = base + lane;
+    int n = 0;
+    if (b < A.batch) {
+      const int lo = min(max(A.q_start[b], 0), A.rows), hi = min(max(A.q_start[b + 1], lo), A.rows);
+      n = (int)((((long long)(hi - lo) << g_shift) + 255) >> 8);
+    }
+    int upto = n;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int y = __shfl_up_sync(~0u, upto, off);
+      if (lane >= off) upto += y;
+    }
+    const uint32_t behind = __ballot_sync(~0u, rb < before + upto);
+    if (behind) {
+      const int at = __ffs(behind) - 1;
+      const int blocks = __shfl_sync(~0u, n, at), skipped = before + __shfl_sync(~0u, upto, at) - blocks;
+      const SeqRows s = seq_rows(A, base + at);
+      B.b = base + at; B.head = head; B.first = s.first; B.n = s.n; B.len = s.len; B.old = s.len - s.n;
+      B.row0 = (blocks - 1 - (rb - skipped)) << 8;     // a sequence's last rows see most: they start first
+      const int p0 = B.old + (B.row0 >> g_shift);                              // positions of the block's tokens
+      const int p1 = min(B.old + ((B.row0 + 255) >> g_shift), B.len - 1);
+      const int lo_key = A.window > 0 ? max(0, p0 - A.window + 1) : 0;
+      B.sinks = min(A.sink, lo_key);
+      B.first_tile = lo_key / kPrefillKeys;
+      B.sink_tiles = min((B.sinks + kPrefillKeys - 1) / kPrefillKeys, B.first_tile);
+      B.tiles = p1 < 0 ? 0 : B.sink_tiles + p1 / kPrefillKeys + 1 - B.first_tile;
+      return true;
+    }
+    before += __shfl_sync(~0u, upto, 31);
+  }
+  return false;
+}
+
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t fma2_(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+  return d;
+}
+__device__ __forceinline__ void unpair(uint64_t d, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(d)); }
+
+template <int D>
+__global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const __grid_constant__ PrefillParams P) {
+  using Sh = PrefillShape<D>;
+  constexpr int STAGES = Sh::kStages;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* sq = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  unsigned char* ring = sq + 2 * Sh::kTileBytes;
+  uint64_t* full = reinterpret_cast<uint64_t*>(ring + STAGES * Sh::kTileBytes);
+  uint64_t* empty = full + STAGES;
+  uint64_t* q_full = empty + STAGES;
+  uint64_t* s_full = q_full + 1;       // [2] logits of a row tile are in TMEM (and its last P.V is done)
+  uint64_t* p_ready = s_full + 2;      // [2] weights are in TMEM, the output is rescaled
+  uint64_t* o_full = p_ready + 2;      // all matrix instructions are done
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_full + 1);
+
+  const PagedParams& A = P.A;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < STAGES; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
+    mbar_init(q_full, 1);
+    for (int t = 0; t < 2; ++t) { mbar_init(&s_full[t], 1); mbar_init(&p_ready[t], 128); }
+    mbar_init(o_full, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  griddep_launch();
+  griddep_wait();
+  PrefillBlock B;
+  if (!find_block(A, P.g_shift, blockIdx.x / A.n_kv_heads, blockIdx.x % A.n_kv_heads, B)) return;    // the grid is an upper bound
+  if (warp == 8) tmem_take(tmem_slot);
+  tcgen05_before_sync();
+  __syncthreads();
+  tcgen05_after_sync();
+  const uint32_t tmem = *tmem_slot;
+  const int G = 1 << P.g_shift;
+
+  {
+    const RowTile rt[2] = {row_tile(B, B.row0, P.g_shift), row_tile(B, B.row0 + 128, P.g_shift)};
+    if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if (warp == 9) {
+      // ---- copies
+      const int pr = A.page, boxes = kPrefillKeys >> A.page_shift;
+      fence_proxy_async();                                     // rows that the append kernel stored
+      if (lane == 0) {
+        const int tiles = rt[1].any ? 2 : 1;
+        mbar_expect_tx(q_full, tiles * Sh::kTileBytes);
+        for (int t = 0; t < tiles; ++t)
+          for (int p = 0; p < Sh::kParts; ++p)
+            asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
+                             smem_u32(sq + t * Sh::kTileBytes + p * Sh::kPartBytes)),
+                         "l"(P.qmap), "r"(0), "r"(B.head * G), "r"(B.first + ((B.row0 + t * 128) >> P.g_shift)), "r"(p), "r"(smem_u32(q_full))
+                         : "memory");
+      }
+      const bool mine = lane < boxes * Sh::kParts;
+      const int box = lane & (boxes - 1), part = mine ? lane / boxes : 0;
+      const int lo_key = B.first_tile * kPrefillKeys;
+      for (int v = 0, it = 0; v < B.tiles; ++v) {
+        const int i = B.tile(v) * kPrefillKeys + box * pr;
+        int chunk = P.oob_chunk;
+        if (mine && i < B.len && (i >= lo_key || i < B.sinks)) {
+          const int pg = page_of(A, B.b, i);
+          if (pg >= 0) chunk = P.chunk0 + pg * A.n_kv_heads + B.head;
+        }
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv, ++it) {
+          const int st = it % STAGES;
+          if (it >= STAGES) mbar_wait(&empty[st], ((it / STAGES) & 1) ^ 1, A.status);
+          if (lane == 0) mbar_expect_tx(&full[st], Sh::kTileBytes);
+          __syncwarp();
+          if (mine)
+            asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
+                             smem_u32(ring + st * Sh::kTileBytes + part * Sh::kPartBytes + box * pr * 128)),
+                         "l"(kv ? P.vmap : P.kmap), "r"(0), "r"(0), "r"(part), "r"(chunk), "r"(smem_u32(&full[st]))
+                         : "memory");
+        }
+      }
+    } else if (warp == 8) {
+      // ---- matrix instructions, all by one thread
+      if (lane == 0) {
+        const uint32_t s_at[2] = {tmem, tmem + 128}, o_at[2] = {tmem + 256, tmem + 256 + D};
+        bool pending[2] = {false, false}, started[2] = {false, false};
+        uint32_t p_phase[2] = {0, 0};
+        auto weights_times_values = [&](int t, int v) {
+          const int it = 2 * v + 1, st = it % STAGES;
+          mbar_wait(&full[st], (it / STAGES) & 1, A.status);
+          mbar_wait(&p_ready[t], p_phase[t], A.status);
+          p_phase[t] ^= 1;
+          tcgen05_after_sync();
+          const uint32_t base = smem_u32(ring + st * Sh::kTileBytes);
+#pragma unroll
+          for (int k = 0; k < kPrefillKeys / 16; ++k) {
+            mma_tmem(o_at[t], s_at[t] + k * 8, smem_matrix(base + k * 2048, Sh::kPartBytes), mma_shape(D, true), started[t] || k > 0);
+          }
+          started[t] = true;
+          pending[t] = false;
+        };
+        mbar_wait(q_full, 0, A.status);
+        for (int v = 0; v < B.tiles; ++v) {
+          const int it = 2 * v, st = it % STAGES, e0 = B.tile(v) * kPrefillKeys;
+          const uint32_t base = smem_u32(ring + st * Sh::kTileBytes);
+          bool waited = false;
+          for (int t = 0; t < 2; ++t) {
+            if (pending[t]) weights_times_values(t, v - 1);
+            if (!tile_seen(rt[t], e0, A.window, A.sink)) continue;
+            if (!waited) { mbar_wait(&full[st], (it / STAGES) & 1, A.status); waited = true; tcgen05_after_sync(); }
+            const uint32_t qb = smem_u32(sq + t * Sh::kTileBytes);
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+              const uint32_t off = (k >> 2) * Sh::kPartBytes + (k & 3) * 32;
+              mma_smem(s_at[t], smem_matrix(qb + off, 16), smem_matrix(base + off, 16), mma_shape(kPrefillKeys, false), k > 0);
+            }
+            tcgen05_commit(&s_full[t]);
+            pending[t] = true;
+          }
+          if (!waited) mbar_wait(&full[st], (it / STAGES) & 1, A.status);     // nobody saw it: its copy is done all the same
+          tcgen05_commit(&empty[st]);
+          if (v > 0) tcgen05_commit(&empty[(it - 1) % STAGES]);
+          if (!pending[0] && !pending[1]) mbar_wait(&full[(it + 1) % STAGES], ((it + 1) / STAGES) & 1, A.status);
+        }
+        for (int t = 0; t < 2; ++t)
+          if (pending[t]) weights_times_values(t, B.tiles - 1);
+        tcgen05_commit(o_full);
+        mbar_wait(o_full, 0, A.status);
+      }
+      __syncwarp();
+    }
+    } else {
+      // ---- softmax: this thread's row
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+      const int t = warp >> 2, row = tid & 127, R = B.row0 + t * 128 + row;
+      const RowTile my = t ? rt[1] : rt[0];
+      const int pos = B.old + (R >> P.g_shift);
+      const bool live = R < B.n << P.g_shift;
+      const int lo_key = A.window > 0 ? pos - A.window + 1 : 0;
+      const uint32_t lanes = (uint32_t)(warp & 3) << 21;        // 32 TMEM lanes per warp, lane number in bits 16..
+      const uint32_t s_at = tmem + lanes + t * 128, o_at = tmem + lanes + 256 + t * D;
+      const float c = A.scale_log2;
+      float m = -INFINITY, l = 0.f;                             // m: reference of the exponentials, in logits
+      uint32_t phase = 0;
+      bool first = true;
+      for (int v = 0; v < B.tiles; ++v) {
+        const int e0 = B.tile(v) * kPrefillKeys;
+        if (!tile_seen(my, e0, A.window, A.sink)) continue;
+        mbar_wait(&s_full[t], phase, A.status);
+        phase ^= 1;
+        tcgen05_after_sync();
+        uint32_t x[128];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tmem_load32(s_at + i * 32, x + i * 32);
+        tmem_wait_loads();
+        // a tile that every row of the row tile sees whole needs no mask
+        const bool whole = e0 + kPrefillKeys - 1 <= my.pos_lo &&
+                           (A.window == 0 || e0 >= my.pos_hi - A.window + 1 || e0 + kPrefillKeys <= A.sink);
+        if (!whole) {
+          const int top = pos - e0, low = max(lo_key, 0) - e0, sinks = A.sink - e0;
+#pragma unroll
+          for (int i = 0; i < 128; ++i)
+            if (i > top || (i < low && i >= sinks)) x[i] = 0xff800000u;
+        }
+        float mx = __uint_as_float(x[0]);
+#pragma unroll
+        for (int i = 1; i < 127; i += 2) mx = fmaxf(mx, fmaxf(__uint_as_float(x[i]), __uint_as_float(x[i + 1])));
+        mx = fmaxf(mx, __uint_as_float(x[127]));
+        if (first) {
+          m = mx;
+          first = false;
+        } else {
+          const bool grow = (mx - m) * c > 8.f;                 // true too where m is still -infinity and mx is not
+          if (__any_sync(~0u, grow)) {
+            const float f = grow ? exp2_fast((m - mx) * c) : 1.f;
+            if (grow) m = mx;
+            l *= f;
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {
+              uint32_t o[32];
+              tmem_load32(o_at + i * 32, o);
+              tmem_wait_loads();
+#pragma unroll
+              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+              tmem_store32(o_at + i * 32, o);
+            }
+          }
+        }
+        const float shift = m == -INFINITY ? 0.f : -m * c;
+        const uint64_t c2 = pair(c, c), shift2 = pair(shift, shift);
+        uint64_t sum2 = 0, sum2b = 0;
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+          uint32_t w[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float p0, p1;
+            unpair(fma2_(pair(__uint_as_float(x[h * 32 + 2 * i]), __uint_as_float(x[h * 32 + 2 * i + 1])), c2, shift2), p0, p1);
+            p0 = exp2_fast(p0);
+            p1 = exp2_fast(p1);
+            if (i & 1) sum2b = add2(sum2b, pair(p0, p1)); else sum2 = add2(sum2, pair(p0, p1));
+            w[i] = pack_bf16(p0, p1);
+          }
+          tmem_store16(s_at + h * 16, w);
+        }
+        float a0, a1;
+        unpair(add2(sum2, sum2b), a0, a1);
+        l += a0 + a1;
+        if (e0 + kPrefillKeys > B.len) {
+          // rows behind the sequence may hold anything: their weights are zero, their values have to be finite
+          const int it = 2 * v + 1, st = it % STAGES;
+          mbar_wait(&full[st], (it / STAGES) & 1, A.status);
+          for (int e = row + (B.len - e0) * 8 * Sh::kParts; e < kPrefillKeys * 8 * Sh::kParts; e += 128) {
+            const int r = e / (8 * Sh::kParts), piece = e % (8 * Sh::kParts);
+            *reinterpret_cast<uint4*>(ring + st * Sh::kTileBytes + (piece >> 3) * Sh::kPartBytes + r * 128 + (piece & 7) * 16) = make_uint4(0, 0, 0, 0);
+          }
+          fence_proxy_async();
+        }
+        tmem_wait_stores();
+        tcgen05_before_sync();
+        mbar_arrive(&p_ready[t]);
+      }
+      // ---- output
+      if (my.any) {
+        mbar_wait(o_full, 0, A.status);
+        tcgen05_after_sync();
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const int tok = B.first + (R >> P.g_shift), hq = B.head * G + (R & (G - 1));
+        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + ((long long)tok * A.n_q_heads + hq) * D;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+          uint32_t o[32];
+          tmem_load32(o_at + i * 32, o);
+          tmem_wait_loads();
+          if (live) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              uint4 y;                                           // a row that saw nothing: its TMEM lane may hold anything
+              if (l > 0.f) {} else for (int z = 0; z < 8; ++z) o[e * 8 + z] = 0;
+              y.x = pack_bf16(__uint_as_float(o[e * 8]) * inv, __uint_as_float(o[e * 8 + 1]) * inv);
+              y.y = pack_bf16(__uint_as_float(o[e * 8 + 2]) * inv, __uint_as_float(o[e * 8 + 3]) * inv);
+              y.z = pack_bf16(__uint_as_float(o[e * 8 + 4]) * inv, __uint_as_float(o[e * 8 + 5]) * inv);
+              y.w = pack_bf16(__uint_as_float(o[e * 8 + 6]) * inv, __uint_as_float(o[e * 8 + 7]) * inv);
+              reinterpret_cast<uint4*>(out)[i * 4 + e] = y;
+            }
+          }
+        }
+        if (live && A.lse) A.lse[(long long)tok * A.n_q_heads + hq] = l > 0.f ? (m * c + log2f(l)) * kLn2 : -INFINITY;
+        tcgen05_before_sync();
+      }
+    }
+  }
+  __syncthreads();
+  if (warp == 8) {
+    tcgen05_after_sync();
+    tmem_give_back(tmem);
+  }
+}
+
+}  // namespace wkv
