@@ -105,6 +105,11 @@ __device__ __forceinline__ bool find_block(const PagedParams& A, int g_shift, in
   return false;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   uint64_t d;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
@@ -199,54 +204,63 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
         }
       }
     } else if (warp == 8) {
-      // ---- matrix instructions, all by one thread
-      if (lane == 0) {
-        const uint32_t s_at[2] = {tmem, tmem + 128}, o_at[2] = {tmem + 256, tmem + 256 + D};
-        bool pending[2] = {false, false}, started[2] = {false, false};
-        uint32_t p_phase[2] = {0, 0};
-        auto weights_times_values = [&](int t, int v) {
-          const int it = 2 * v + 1, st = it % STAGES;
-          mbar_wait(&full[st], (it / STAGES) & 1, A.status);
-          mbar_wait(&p_ready[t], p_phase[t], A.status);
-          p_phase[t] ^= 1;
-          tcgen05_after_sync();
-          const uint32_t base = smem_u32(ring + st * Sh::kTileBytes);
+      // ---- matrix instructions: the warp walks the tiles together, one thread issues
+      const uint32_t s_at[2] = {tmem, tmem + 128}, o_at[2] = {tmem + 256, tmem + 256 + D};
+      const uint64_t q_at[2] = {smem_matrix(smem_u32(sq), 16), smem_matrix(smem_u32(sq + Sh::kTileBytes), 16)};
+      const uint64_t k_ring = smem_matrix(smem_u32(ring), 16), v_ring = smem_matrix(smem_u32(ring), Sh::kPartBytes);
+      bool pending[2] = {false, false}, started[2] = {false, false};
+      uint32_t p_phase[2] = {0, 0};
+      auto weights_times_values = [&](int t, int v) {
+        const int it = 2 * v + 1, st = it % STAGES;
+        mbar_wait(&full[st], (it / STAGES) & 1, A.status);
+        mbar_wait(&p_ready[t], p_phase[t], A.status);
+        p_phase[t] ^= 1;
+        tcgen05_after_sync();
+        const uint64_t vd = v_ring + (uint32_t)(st * (Sh::kTileBytes >> 4));
+        if (elect_one()) {
+          mma_tmem(o_at[t], s_at[t], vd, mma_shape(D, true), started[t]);
 #pragma unroll
-          for (int k = 0; k < kPrefillKeys / 16; ++k) {
-            mma_tmem(o_at[t], s_at[t] + k * 8, smem_matrix(base + k * 2048, Sh::kPartBytes), mma_shape(D, true), started[t] || k > 0);
-          }
-          started[t] = true;
-          pending[t] = false;
-        };
-        mbar_wait(q_full, 0, A.status);
-        for (int v = 0; v < B.tiles; ++v) {
-          const int it = 2 * v, st = it % STAGES, e0 = B.tile(v) * kPrefillKeys;
-          const uint32_t base = smem_u32(ring + st * Sh::kTileBytes);
-          bool waited = false;
-          for (int t = 0; t < 2; ++t) {
-            if (pending[t]) weights_times_values(t, v - 1);
-            if (!tile_seen(rt[t], e0, A.window, A.sink)) continue;
-            if (!waited) { mbar_wait(&full[st], (it / STAGES) & 1, A.status); waited = true; tcgen05_after_sync(); }
-            const uint32_t qb = smem_u32(sq + t * Sh::kTileBytes);
+          for (int k = 1; k < kPrefillKeys / 16; ++k) mma_tmem(o_at[t], s_at[t] + k * 8, vd + k * 128, mma_shape(D, true), true);
+        }
+        __syncwarp();
+        started[t] = true;
+        pending[t] = false;
+      };
+      mbar_wait(q_full, 0, A.status);
+      for (int v = 0; v < B.tiles; ++v) {
+        const int it = 2 * v, st = it % STAGES, e0 = B.tile(v) * kPrefillKeys;
+        const uint64_t kd = k_ring + (uint32_t)(st * (Sh::kTileBytes >> 4));
+        bool waited = false;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          if (pending[t]) weights_times_values(t, v - 1);
+          if (!tile_seen(rt[t], e0, A.window, A.sink)) continue;
+          if (!waited) { mbar_wait(&full[st], (it / STAGES) & 1, A.status); waited = true; tcgen05_after_sync(); }
+          if (elect_one()) {
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
-              const uint32_t off = (k >> 2) * Sh::kPartBytes + (k & 3) * 32;
-              mma_smem(s_at[t], smem_matrix(qb + off, 16), smem_matrix(base + off, 16), mma_shape(kPrefillKeys, false), k > 0);
+              constexpr int kPart = Sh::kPartBytes >> 4;
+              mma_smem(s_at[t], q_at[t] + (k >> 2) * kPart + (k & 3) * 2, kd + (k >> 2) * kPart + (k & 3) * 2, mma_shape(kPrefillKeys, false), k > 0);
             }
             tcgen05_commit(&s_full[t]);
-            pending[t] = true;
           }
-          if (!waited) mbar_wait(&full[st], (it / STAGES) & 1, A.status);     // nobody saw it: its copy is done all the same
+          __syncwarp();
+          pending[t] = true;
+        }
+        if (!waited) mbar_wait(&full[st], (it / STAGES) & 1, A.status);     // nobody saw it: its copy is done all the same
+        if (elect_one()) {
           tcgen05_commit(&empty[st]);
           if (v > 0) tcgen05_commit(&empty[(it - 1) % STAGES]);
-          if (!pending[0] && !pending[1]) mbar_wait(&full[(it + 1) % STAGES], ((it + 1) / STAGES) & 1, A.status);
         }
-        for (int t = 0; t < 2; ++t)
-          if (pending[t]) weights_times_values(t, B.tiles - 1);
-        tcgen05_commit(o_full);
-        mbar_wait(o_full, 0, A.status);
+        __syncwarp();
+        if (!pending[0] && !pending[1]) mbar_wait(&full[(it + 1) % STAGES], ((it + 1) / STAGES) & 1, A.status);
       }
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        if (pending[t]) weights_times_values(t, B.tiles - 1);
+      if (elect_one()) tcgen05_commit(o_full);
       __syncwarp();
+      mbar_wait(o_full, 0, A.status);
     }
     } else {
       // ---- softmax: this thread's row
@@ -281,10 +295,16 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
           for (int i = 0; i < 128; ++i)
             if (i > top || (i < low && i >= sinks)) x[i] = 0xff800000u;
         }
-        float mx = __uint_as_float(x[0]);
+        float mx4[4];                                           // four chains: the latency of one would show
 #pragma unroll
-        for (int i = 1; i < 127; i += 2) mx = fmaxf(mx, fmaxf(__uint_as_float(x[i]), __uint_as_float(x[i + 1])));
-        mx = fmaxf(mx, __uint_as_float(x[127]));
+        for (int i = 0; i < 4; ++i) mx4[i] = max3(__uint_as_float(x[i]), __uint_as_float(x[4 + i]), __uint_as_float(x[8 + i]));
+#pragma unroll
+        for (int i = 12; i < 124; i += 8)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) mx4[e] = max3(mx4[e], __uint_as_float(x[i + e]), __uint_as_float(x[i + 4 + e]));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mx4[e] = fmaxf(mx4[e], __uint_as_float(x[124 + e]));
+        const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
         if (first) {
           m = mx;
           first = false;
@@ -307,7 +327,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
         }
         const float shift = m == -INFINITY ? 0.f : -m * c;
         const uint64_t c2 = pair(c, c), shift2 = pair(shift, shift);
-        uint64_t sum2 = 0, sum2b = 0;
+        uint64_t sum2[4] = {0, 0, 0, 0};
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
           uint32_t w[16];
@@ -317,13 +337,13 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
             unpair(fma2_(pair(__uint_as_float(x[h * 32 + 2 * i]), __uint_as_float(x[h * 32 + 2 * i + 1])), c2, shift2), p0, p1);
             p0 = exp2_fast(p0);
             p1 = exp2_fast(p1);
-            if (i & 1) sum2b = add2(sum2b, pair(p0, p1)); else sum2 = add2(sum2, pair(p0, p1));
+            sum2[i & 3] = add2(sum2[i & 3], pair(p0, p1));
             w[i] = pack_bf16(p0, p1);
           }
           tmem_store16(s_at + h * 16, w);
         }
         float a0, a1;
-        unpair(add2(sum2, sum2b), a0, a1);
+        unpair(add2(add2(sum2[0], sum2[1]), add2(sum2[2], sum2[3])), a0, a1);
         l += a0 + a1;
         if (e0 + kPrefillKeys > B.len) {
           // rows behind the sequence may hold anything: their weights are zero, their values have to be finite

@@ -24,6 +24,14 @@ __device__ __forceinline__ void tcgen05_commit(uint64_t* bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 
+// One thread of a converged warp.  Matrix instructions take their operands from uniform registers: issued under this choice, and
+// not under a comparison of the lane number, they need no round trip through the vector registers each.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t chosen;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(chosen));
+  return chosen != 0;
+}
+
 // Shared-memory matrix in rows of 128 bytes under the 128-byte swizzle, groups of 8 rows 1024 bytes apart.  `atom_stride`:
 // bytes between the 64-element columns of a matrix whose contiguous dimension is not the contracted one (else unused).
 __device__ __forceinline__ uint64_t smem_matrix(uint32_t addr, uint32_t atom_stride) {
