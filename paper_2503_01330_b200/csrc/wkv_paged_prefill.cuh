@@ -41,7 +41,7 @@ struct PrefillShape {
   static constexpr int kPartBytes = 128 * 128;                    // 128 rows x 128 bytes
   static constexpr int kTileBytes = kParts * kPartBytes;          // of Q (one row tile), K or V
   static constexpr int kStages = D == 128 ? 5 : 8;
-  static constexpr int kSmem = 1024 + 2 * kTileBytes + kStages * kTileBytes + (2 * kStages + 8) * 8 + 32;
+  static constexpr int kSmem = 2 * kTileBytes + kStages * kTileBytes + (2 * kStages + 10) * 8 + 32;
 };
 
 // The row block of a CTA: which sequence, which rows; and the key tiles it walks: those with sinks, then the others.
@@ -127,19 +127,38 @@ __device__ __forceinline__ uint64_t pair(float lo, float hi) {
 }
 __device__ __forceinline__ void unpair(uint64_t d, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(d)); }
 
+// 2^x of a pair without the exponential unit: x = n + f, |f| <= 1/2, a polynomial of degree 5 in f (least-squares fit weighted
+// towards its largest relative error, 9.2e-8), n into the exponent.  -infinity and everything below -127 give exactly 0.
+__device__ __forceinline__ void exp2_pair(float& x0, float& x1) {
+  constexpr float kMagic = 12582912.f;                          // 1.5 * 2^23: adding it rounds to a whole number
+  const uint64_t x = pair(fmaxf(x0, -127.f), fmaxf(x1, -127.f));
+  const uint64_t n = add2(x, pair(kMagic, kMagic));
+  const uint64_t f = fma2_(add2(n, pair(-kMagic, -kMagic)), pair(-1.f, -1.f), x);
+  uint64_t p = pair(0.001326472614891827f, 0.001326472614891827f);
+  p = fma2_(p, f, pair(0.009671512991189957f, 0.009671512991189957f));
+  p = fma2_(p, f, pair(0.05550733581185341f, 0.05550733581185341f));
+  p = fma2_(p, f, pair(0.24022242426872253f, 0.24022242426872253f));
+  p = fma2_(p, f, pair(0.6931470036506653f, 0.6931470036506653f));
+  p = fma2_(p, f, pair(1.f, 1.f));
+  float n0, n1;
+  unpair(n, n0, n1);
+  unpair(p, x0, x1);
+  x0 = __uint_as_float(__float_as_uint(x0) + (__float_as_uint(n0) << 23));
+  x1 = __uint_as_float(__float_as_uint(x1) + (__float_as_uint(n1) << 23));
+}
+
 template <int D>
 __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const __grid_constant__ PrefillParams P) {
   using Sh = PrefillShape<D>;
   constexpr int STAGES = Sh::kStages;
-  extern __shared__ unsigned char smem_raw[];
-  unsigned char* sq = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  extern __shared__ __align__(1024) unsigned char sq[];               // Q, then the ring: there is no room to align by hand
   unsigned char* ring = sq + 2 * Sh::kTileBytes;
   uint64_t* full = reinterpret_cast<uint64_t*>(ring + STAGES * Sh::kTileBytes);
   uint64_t* empty = full + STAGES;
   uint64_t* q_full = empty + STAGES;
   uint64_t* s_full = q_full + 1;       // [2] logits of a row tile are in TMEM (and its last P.V is done)
-  uint64_t* p_ready = s_full + 2;      // [2] weights are in TMEM, the output is rescaled
-  uint64_t* o_full = p_ready + 2;      // all matrix instructions are done
+  uint64_t* p_ready = s_full + 2;      // [2][2] a half of the weights is in TMEM, the output is rescaled
+  uint64_t* o_full = p_ready + 4;      // all matrix instructions are done
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_full + 1);
 
   const PagedParams& A = P.A;
@@ -147,7 +166,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
   if (tid == 0) {
     for (int i = 0; i < STAGES; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
     mbar_init(q_full, 1);
-    for (int t = 0; t < 2; ++t) { mbar_init(&s_full[t], 1); mbar_init(&p_ready[t], 128); }
+    for (int t = 0; t < 2; ++t) { mbar_init(&s_full[t], 1); mbar_init(&p_ready[2 * t], 4); mbar_init(&p_ready[2 * t + 1], 4); }
     mbar_init(o_full, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -159,7 +178,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
   tcgen05_before_sync();
   __syncthreads();
   tcgen05_after_sync();
-  const uint32_t tmem = *tmem_slot;
+  const uint32_t tmem = __shfl_sync(~0u, *tmem_slot, 0);
   const int G = 1 << P.g_shift;
 
   {
@@ -193,7 +212,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv, ++it) {
           const int st = it % STAGES;
-          if (it >= STAGES) mbar_wait(&empty[st], ((it / STAGES) & 1) ^ 1, A.status);
+          if (it >= STAGES) mbar_wait_fast(&empty[st], ((it / STAGES) & 1) ^ 1, A.status);
           if (lane == 0) mbar_expect_tx(&full[st], Sh::kTileBytes);
           __syncwarp();
           if (mine)
@@ -204,63 +223,57 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
         }
       }
     } else if (warp == 8) {
-      // ---- matrix instructions: the warp walks the tiles together, one thread issues
+      // ---- matrix instructions, all by one elected thread
+      if (elect_one()) {
       const uint32_t s_at[2] = {tmem, tmem + 128}, o_at[2] = {tmem + 256, tmem + 256 + D};
       const uint64_t q_at[2] = {smem_matrix(smem_u32(sq), 16), smem_matrix(smem_u32(sq + Sh::kTileBytes), 16)};
       const uint64_t k_ring = smem_matrix(smem_u32(ring), 16), v_ring = smem_matrix(smem_u32(ring), Sh::kPartBytes);
       bool pending[2] = {false, false}, started[2] = {false, false};
       uint32_t p_phase[2] = {0, 0};
-      auto weights_times_values = [&](int t, int v) {
-        const int it = 2 * v + 1, st = it % STAGES;
-        mbar_wait(&full[st], (it / STAGES) & 1, A.status);
-        mbar_wait(&p_ready[t], p_phase[t], A.status);
-        p_phase[t] ^= 1;
-        tcgen05_after_sync();
-        const uint64_t vd = v_ring + (uint32_t)(st * (Sh::kTileBytes >> 4));
-        if (elect_one()) {
-          mma_tmem(o_at[t], s_at[t], vd, mma_shape(D, true), started[t]);
+      auto weights_times_values = [&](int t, uint64_t vd) {
 #pragma unroll
-          for (int k = 1; k < kPrefillKeys / 16; ++k) mma_tmem(o_at[t], s_at[t] + k * 8, vd + k * 128, mma_shape(D, true), true);
+        for (int half = 0; half < 2; ++half) {
+          mbar_wait_fast(&p_ready[2 * t + half], p_phase[t], A.status);
+          tcgen05_after_sync();
+#pragma unroll
+          for (int k = half * 4; k < half * 4 + 4; ++k) mma_tmem(o_at[t], s_at[t] + k * 8, vd + k * 128, mma_shape(D, true), started[t] || k > 0);
         }
-        __syncwarp();
+        p_phase[t] ^= 1;
         started[t] = true;
         pending[t] = false;
       };
-      mbar_wait(q_full, 0, A.status);
-      for (int v = 0; v < B.tiles; ++v) {
-        const int it = 2 * v, st = it % STAGES, e0 = B.tile(v) * kPrefillKeys;
+      mbar_wait_fast(q_full, 0, A.status);
+      uint64_t vd = 0;                                          // values of the tile before
+      for (int v = 0, it = 0; v < B.tiles; ++v, it += 2) {
+        const int st = it % STAGES, e0 = B.tile(v) * kPrefillKeys;
         const uint64_t kd = k_ring + (uint32_t)(st * (Sh::kTileBytes >> 4));
-        bool waited = false;
+        // both copies ahead of the weights, so that P.V and the next logits of a row tile are issued in one go
+        mbar_wait_fast(&full[st], (it / STAGES) & 1, A.status);
+        if (v > 0) mbar_wait_fast(&full[(it - 1) % STAGES], ((it - 1) / STAGES) & 1, A.status);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          if (pending[t]) weights_times_values(t, v - 1);
+          if (pending[t]) weights_times_values(t, vd);
           if (!tile_seen(rt[t], e0, A.window, A.sink)) continue;
-          if (!waited) { mbar_wait(&full[st], (it / STAGES) & 1, A.status); waited = true; tcgen05_after_sync(); }
-          if (elect_one()) {
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-              constexpr int kPart = Sh::kPartBytes >> 4;
-              mma_smem(s_at[t], q_at[t] + (k >> 2) * kPart + (k & 3) * 2, kd + (k >> 2) * kPart + (k & 3) * 2, mma_shape(kPrefillKeys, false), k > 0);
-            }
-            tcgen05_commit(&s_full[t]);
+          for (int k = 0; k < D / 16; ++k) {
+            constexpr int kPart = Sh::kPartBytes >> 4;
+            mma_smem(s_at[t], q_at[t] + (k >> 2) * kPart + (k & 3) * 2, kd + (k >> 2) * kPart + (k & 3) * 2, mma_shape(kPrefillKeys, false), k > 0);
           }
-          __syncwarp();
+          tcgen05_commit(&s_full[t]);
           pending[t] = true;
         }
-        if (!waited) mbar_wait(&full[st], (it / STAGES) & 1, A.status);     // nobody saw it: its copy is done all the same
-        if (elect_one()) {
-          tcgen05_commit(&empty[st]);
-          if (v > 0) tcgen05_commit(&empty[(it - 1) % STAGES]);
-        }
-        __syncwarp();
-        if (!pending[0] && !pending[1]) mbar_wait(&full[(it + 1) % STAGES], ((it + 1) / STAGES) & 1, A.status);
+        tcgen05_commit(&empty[st]);
+        if (v > 0) tcgen05_commit(&empty[(it - 1) % STAGES]);
+        vd = v_ring + (uint32_t)(((it + 1) % STAGES) * (Sh::kTileBytes >> 4));
       }
+      if (B.tiles > 0) mbar_wait_fast(&full[(2 * B.tiles - 1) % STAGES], ((2 * B.tiles - 1) / STAGES) & 1, A.status);
 #pragma unroll
       for (int t = 0; t < 2; ++t)
-        if (pending[t]) weights_times_values(t, B.tiles - 1);
-      if (elect_one()) tcgen05_commit(o_full);
+        if (pending[t]) weights_times_values(t, vd);
+      tcgen05_commit(o_full);
+      mbar_wait_fast(o_full, 0, A.status);
+      }
       __syncwarp();
-      mbar_wait(o_full, 0, A.status);
     }
     } else {
       // ---- softmax: this thread's row
@@ -279,7 +292,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
       for (int v = 0; v < B.tiles; ++v) {
         const int e0 = B.tile(v) * kPrefillKeys;
         if (!tile_seen(my, e0, A.window, A.sink)) continue;
-        mbar_wait(&s_full[t], phase, A.status);
+        mbar_wait_fast(&s_full[t], phase, A.status);
         phase ^= 1;
         tcgen05_after_sync();
         uint32_t x[128];
@@ -315,15 +328,25 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
             if (grow) m = mx;
             l *= f;
 #pragma unroll
-            for (int i = 0; i < D / 32; ++i) {
-              uint32_t o[32];
-              tmem_load32(o_at + i * 32, o);
+            for (int i = 0; i < D / 16; ++i) {
+              uint32_t o[16];
+              tmem_load16(o_at + i * 16, o);
               tmem_wait_loads();
 #pragma unroll
-              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-              tmem_store32(o_at + i * 32, o);
+              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+              tmem_store16(o_at + i * 16, o);
             }
           }
+        }
+        if (e0 + kPrefillKeys > B.len) {
+          // rows behind the sequence may hold anything: their weights are zero, their values have to be finite
+          const int it = 2 * v + 1, st = it % STAGES;
+          mbar_wait_fast(&full[st], (it / STAGES) & 1, A.status);
+          for (int e = row + (B.len - e0) * 8 * Sh::kParts; e < kPrefillKeys * 8 * Sh::kParts; e += 128) {
+            const int r = e / (8 * Sh::kParts), piece = e % (8 * Sh::kParts);
+            *reinterpret_cast<uint4*>(ring + st * Sh::kTileBytes + (piece >> 3) * Sh::kPartBytes + r * 128 + (piece & 7) * 16) = make_uint4(0, 0, 0, 0);
+          }
+          fence_proxy_async();
         }
         const float shift = m == -INFINITY ? 0.f : -m * c;
         const uint64_t c2 = pair(c, c), shift2 = pair(shift, shift);
@@ -335,33 +358,30 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
           for (int i = 0; i < 16; ++i) {
             float p0, p1;
             unpair(fma2_(pair(__uint_as_float(x[h * 32 + 2 * i]), __uint_as_float(x[h * 32 + 2 * i + 1])), c2, shift2), p0, p1);
-            p0 = exp2_fast(p0);
-            p1 = exp2_fast(p1);
+            if ((i & 3) == 3) {
+              exp2_pair(p0, p1);
+            } else {
+              p0 = exp2_fast(p0);
+              p1 = exp2_fast(p1);
+            }
             sum2[i & 3] = add2(sum2[i & 3], pair(p0, p1));
             w[i] = pack_bf16(p0, p1);
           }
           tmem_store16(s_at + h * 16, w);
+          if (h & 1) {                                          // half of the weights: its products may start
+            tmem_wait_stores();
+            tcgen05_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&p_ready[2 * t + (h >> 1)]);
+          }
         }
         float a0, a1;
         unpair(add2(add2(sum2[0], sum2[1]), add2(sum2[2], sum2[3])), a0, a1);
         l += a0 + a1;
-        if (e0 + kPrefillKeys > B.len) {
-          // rows behind the sequence may hold anything: their weights are zero, their values have to be finite
-          const int it = 2 * v + 1, st = it % STAGES;
-          mbar_wait(&full[st], (it / STAGES) & 1, A.status);
-          for (int e = row + (B.len - e0) * 8 * Sh::kParts; e < kPrefillKeys * 8 * Sh::kParts; e += 128) {
-            const int r = e / (8 * Sh::kParts), piece = e % (8 * Sh::kParts);
-            *reinterpret_cast<uint4*>(ring + st * Sh::kTileBytes + (piece >> 3) * Sh::kPartBytes + r * 128 + (piece & 7) * 16) = make_uint4(0, 0, 0, 0);
-          }
-          fence_proxy_async();
-        }
-        tmem_wait_stores();
-        tcgen05_before_sync();
-        mbar_arrive(&p_ready[t]);
       }
       // ---- output
       if (my.any) {
-        mbar_wait(o_full, 0, A.status);
+        mbar_wait_fast(o_full, 0, A.status);
         tcgen05_after_sync();
         const float inv = l > 0.f ? 1.f / l : 0.f;
         const int tok = B.first + (R >> P.g_shift), hq = B.head * G + (R & (G - 1));

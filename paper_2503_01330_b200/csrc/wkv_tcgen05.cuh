@@ -68,17 +68,17 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t* r) {
       : "r"(addr)
       : "memory");
 }
+__device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : WKV_R8(r, 0), WKV_R8(r, 8)
+      : "r"(addr)
+      : "memory");
+}
 __device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t* r) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(addr),
       WKV_I8(r, 0), WKV_I8(r, 8)
-      : "memory");
-}
-__device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t* r) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(addr),
-      WKV_I8(r, 0), WKV_I8(r, 8), WKV_I8(r, 16), WKV_I8(r, 24)
       : "memory");
 }
 #undef WKV_R8
