@@ -166,6 +166,8 @@ cudaError_t pick_kernels(wkv_paged* c) {
   if constexpr (sizeof(T) == 2) {
     if (e == cudaSuccess)
       e = cudaFuncSetAttribute(wkv::paged_prefill_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, wkv::PrefillShape<D>::kSmem);
+    if (e == cudaSuccess)
+      e = cudaFuncSetAttribute(wkv::paged_weights_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, wkv::WeightsShape<D>::kSmem);
   }
   return e;
 }
@@ -276,25 +278,27 @@ int prefill_bf16(wkv_paged* c, const wkv::PagedParams& A) {
   std::memcpy(P.vmap, c->part_vmap, 128);
   constexpr int smem = wkv::PrefillShape<D>::kSmem;
   WKV_CUDA(c, launch(c, wkv::paged_prefill_kernel<D>, (long long)P.blocks * A.n_kv_heads, wkv::kPrefillThreads, smem, P));
+  if (A.scores) {
+    const long long blocks = ((long long)A.width * A.page + 255) / 256;
+    WKV_CUDA(c, launch(c, wkv::paged_weights_tc_kernel<D>, blocks * A.batch * A.n_kv_heads, wkv::kWeightsThreads, wkv::WeightsShape<D>::kSmem, P));
+  }
   return WKV_OK;
 }
 // ... and on fp32 rows.
 template <int D>
 int prefill_f32(wkv_paged* c, const wkv::PagedParams& P) {
   WKV_CUDA(c, launch(c, wkv::paged_attend_kernel<float, D>, ((long long)P.rows * P.n_q_heads + 3) / 4, 128, 0, P));
+  if (P.scores) {
+    const int entries = P.width * P.page;
+    WKV_CUDA(c, launch(c, wkv::paged_weights_kernel<float, D>, ((long long)P.batch * P.n_kv_heads * entries + 3) / 4, 128, 0, P, entries));
+  }
   return WKV_OK;
 }
 
 template <typename T, int D>
 int prefill_typed(wkv_paged* c, const wkv::PagedParams& P) {
   if (P.k) WKV_CUDA(c, launch(c, wkv::paged_append_kernel<T, D>, ((long long)P.rows * P.n_kv_heads + 3) / 4, 128, 0, P));
-  int rc;
-  if constexpr (sizeof(T) == 2) rc = prefill_bf16<D>(c, P); else rc = prefill_f32<D>(c, P);
-  if (rc == WKV_OK && P.scores) {
-    const int entries = P.width * P.page;
-    WKV_CUDA(c, launch(c, wkv::paged_weights_kernel<T, D>, ((long long)P.batch * P.n_kv_heads * entries + 3) / 4, 128, 0, P, entries));
-  }
-  return rc;
+  if constexpr (sizeof(T) == 2) return prefill_bf16<D>(c, P); else return prefill_f32<D>(c, P);
 }
 
 int prefill(wkv_paged* c, const wkv::PagedParams& P) {

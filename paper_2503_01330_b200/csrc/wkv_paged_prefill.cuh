@@ -44,6 +44,13 @@ struct PrefillShape {
   static constexpr int kSmem = 2 * kTileBytes + kStages * kTileBytes + (2 * kStages + 10) * 8 + 32;
 };
 
+__device__ __forceinline__ void tensor_g2s_4d(void* dst, const void* tmap, int x, int y, int z, int w, uint64_t* bar) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
+                   smem_u32(dst)),
+               "l"(tmap), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
+               : "memory");
+}
+
 // The row block of a CTA: which sequence, which rows; and the key tiles it walks: those with sinks, then the others.
 struct PrefillBlock {
   int b, head, first, n, len, old;      // old: entries before the chunk
@@ -194,10 +201,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
         mbar_expect_tx(q_full, tiles * Sh::kTileBytes);
         for (int t = 0; t < tiles; ++t)
           for (int p = 0; p < Sh::kParts; ++p)
-            asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
-                             smem_u32(sq + t * Sh::kTileBytes + p * Sh::kPartBytes)),
-                         "l"(P.qmap), "r"(0), "r"(B.head * G), "r"(B.first + ((B.row0 + t * 128) >> P.g_shift)), "r"(p), "r"(smem_u32(q_full))
-                         : "memory");
+            tensor_g2s_4d(sq + t * Sh::kTileBytes + p * Sh::kPartBytes, P.qmap, 0, B.head * G, B.first + ((B.row0 + t * 128) >> P.g_shift), p, q_full);
       }
       const bool mine = lane < boxes * Sh::kParts;
       const int box = lane & (boxes - 1), part = mine ? lane / boxes : 0;
@@ -216,10 +220,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
           if (lane == 0) mbar_expect_tx(&full[st], Sh::kTileBytes);
           __syncwarp();
           if (mine)
-            asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
-                             smem_u32(ring + st * Sh::kTileBytes + part * Sh::kPartBytes + box * pr * 128)),
-                         "l"(kv ? P.vmap : P.kmap), "r"(0), "r"(0), "r"(part), "r"(chunk), "r"(smem_u32(&full[st]))
-                         : "memory");
+            tensor_g2s_4d(ring + st * Sh::kTileBytes + part * Sh::kPartBytes + box * pr * 128, kv ? P.vmap : P.kmap, 0, 0, part, chunk, &full[st]);
         }
       }
     } else if (warp == 8) {
@@ -383,7 +384,8 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
       if (my.any) {
         mbar_wait_fast(o_full, 0, A.status);
         tcgen05_after_sync();
-        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const bool seen = !(l <= 0.f);                          // else the row's TMEM lane may hold anything
+        const float inv = seen ? 1.f / l : 0.f;
         const int tok = B.first + (R >> P.g_shift), hq = B.head * G + (R & (G - 1));
         __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + ((long long)tok * A.n_q_heads + hq) * D;
 #pragma unroll
@@ -394,8 +396,9 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
           if (live) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              uint4 y;                                           // a row that saw nothing: its TMEM lane may hold anything
-              if (l > 0.f) {} else for (int z = 0; z < 8; ++z) o[e * 8 + z] = 0;
+              uint4 y;
+#pragma unroll
+              for (int z = 0; z < 8; ++z) o[e * 8 + z] = seen ? o[e * 8 + z] : 0u;
               y.x = pack_bf16(__uint_as_float(o[e * 8]) * inv, __uint_as_float(o[e * 8 + 1]) * inv);
               y.y = pack_bf16(__uint_as_float(o[e * 8 + 2]) * inv, __uint_as_float(o[e * 8 + 3]) * inv);
               y.z = pack_bf16(__uint_as_float(o[e * 8 + 4]) * inv, __uint_as_float(o[e * 8 + 5]) * inv);
@@ -404,13 +407,206 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
             }
           }
         }
-        if (live && A.lse) A.lse[(long long)tok * A.n_q_heads + hq] = l > 0.f ? (m * c + log2f(l)) * kLn2 : -INFINITY;
+        if (live && A.lse) A.lse[(long long)tok * A.n_q_heads + hq] = seen ? (m * c + log2f(l)) * kLn2 : -INFINITY;
         tcgen05_before_sync();
       }
     }
   }
   __syncthreads();
   if (warp == 8) {
+    tcgen05_after_sync();
+    tmem_give_back(tmem);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------
+// accumulated weights of a prompt on bf16 rows
+// ------------------------------------------------------------------------------------------------
+// scores[i] += 1/G sum over the call's tokens t that see i and the group's heads g of exp(scale q_tg.k_i - lse_tg): column sums of the
+// attention matrix, which needs the finished log-sums and so a second pass over the logits.  The transposed product K Q^T puts an
+// entry's column into one TMEM lane: a thread adds up its own entry's weights, no shuffles, no atomics, a fixed order (a tile's sum
+// first, then the tiles).  A CTA owns 256 entries (two key tiles, loaded once) of one kv head and walks the row tiles that see any
+// of them; logits are double buffered (4 x 128 TMEM columns), so the tensor cores run ahead.  Bound: the exponentials, 16 a cycle
+// and SM -- half as many matrix flops per exponential as the attention itself.
+constexpr int kWeightsThreads = 640;
+
+template <int D>
+struct WeightsShape {
+  static constexpr int kPartBytes = 128 * 128;
+  static constexpr int kTileBytes = D / 64 * kPartBytes;
+  static constexpr int kStages = D == 128 ? 4 : 6;
+  static constexpr int kSmem = (2 + kStages) * kTileBytes + (2 * kStages + 12) * 8 + 16 + 2 * 128 * 4 + 256 * 4;
+};
+
+template <int D>
+__global__ void __launch_bounds__(kWeightsThreads, 1) paged_weights_tc_kernel(const __grid_constant__ PrefillParams P) {
+  using Sh = WeightsShape<D>;
+  constexpr int STAGES = Sh::kStages;
+  extern __shared__ __align__(1024) unsigned char sk[];               // two key tiles, then the ring of row tiles
+  unsigned char* ring = sk + 2 * Sh::kTileBytes;
+  uint64_t* full = reinterpret_cast<uint64_t*>(ring + STAGES * Sh::kTileBytes);
+  uint64_t* empty = full + STAGES;
+  uint64_t* k_full = empty + STAGES;
+  uint64_t* s_full = k_full + 1;       // [key tile][buffer]
+  uint64_t* s_empty = s_full + 4;
+  uint64_t* lse_full = s_empty + 4;    // [buffer]
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(lse_full + 2);
+  float* lse = reinterpret_cast<float*>(tmem_slot + 6);                 // [buffer][128] base-2 log-sums of a row tile
+  float* sums = lse + 256;                                            // [key tile][128] from the second halves
+
+  const PagedParams& A = P.A;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, G = 1 << P.g_shift;
+  griddep_launch();
+  griddep_wait();
+  const int head = blockIdx.x % A.n_kv_heads, b = blockIdx.x / A.n_kv_heads % A.batch, e0 = blockIdx.x / A.n_kv_heads / A.batch * 256;
+  const SeqRows s = seq_rows(A, b);
+  const int old = s.len - s.n;
+  if (e0 >= s.len || s.n == 0 || old < 0) return;
+  // row tiles that see an entry of the block: tokens from the first entry's on, to the window's end of the last one
+  const int t_lo = max(0, e0 - old), e_last = min(e0 + 255, s.len - 1);
+  const long long t_end = A.window == 0 || e0 < A.sink ? s.n : min((long long)s.n, (long long)e_last - old + A.window);   // first token that sees none
+  const int tile0 = (t_lo << P.g_shift) >> 7, tiles = t_end <= t_lo ? 0 : (int)(((t_end << P.g_shift) + 127) >> 7) - tile0;
+  if (tiles == 0) return;                                             // entries that came with the call are seen by their own tokens
+  if (tid == 0) {
+    for (int i = 0; i < STAGES; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
+    mbar_init(k_full, 1);
+    for (int i = 0; i < 4; ++i) { mbar_init(&s_full[i], 1); mbar_init(&s_empty[i], 8); }
+    for (int i = 0; i < 2; ++i) mbar_init(&lse_full[i], 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 16) tmem_take(tmem_slot);
+  tcgen05_before_sync();
+  __syncthreads();
+  tcgen05_after_sync();
+  const uint32_t tmem = __shfl_sync(~0u, *tmem_slot, 0);
+
+  if (warp == 17) {
+    // ---- copies
+    const int pr = A.page, boxes = 256 >> A.page_shift;
+    fence_proxy_async();
+    if (lane == 0) mbar_expect_tx(k_full, 2 * Sh::kTileBytes);
+    __syncwarp();
+    for (int j = lane; j < boxes * (D / 64); j += 32) {
+      const int box = j & (boxes - 1), part = j / boxes, i = e0 + box * pr, at = box * pr;      // row of the block
+      int chunk = P.oob_chunk;
+      if (i < s.len) {
+        const int pg = page_of(A, b, i);
+        if (pg >= 0) chunk = P.chunk0 + pg * A.n_kv_heads + head;
+      }
+      tensor_g2s_4d(sk + (at >> 7) * Sh::kTileBytes + part * Sh::kPartBytes + (at & 127) * 128, P.kmap, 0, 0, part, chunk, k_full);
+    }
+    for (int it = 0; it < tiles; ++it) {
+      const int st = it % STAGES;
+      if (it >= STAGES) mbar_wait_fast(&empty[st], ((it / STAGES) & 1) ^ 1, A.status);
+      if (lane == 0) mbar_expect_tx(&full[st], Sh::kTileBytes);
+      __syncwarp();
+      if (lane < D / 64)
+        tensor_g2s_4d(ring + st * Sh::kTileBytes + lane * Sh::kPartBytes, P.qmap, 0, head * G, s.first + (((tile0 + it) * 128) >> P.g_shift), lane, &full[st]);
+    }
+  } else if (warp == 18) {
+    // ---- log-sums of the row tiles
+    for (int it = 0; it < tiles; ++it) {
+      const int buf = it & 1;
+      float x[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int R = (tile0 + it) * 128 + j * 32 + lane, tok = R >> P.g_shift;
+        x[j] = tok < s.n ? A.lse[(long long)(s.first + tok) * A.n_q_heads + head * G + (R & (G - 1))] * kLog2e : 0.f;
+      }
+      if (it >= 2)
+        for (int t = 0; t < 2; ++t) mbar_wait_fast(&s_empty[t * 2 + buf], ((it >> 1) & 1) ^ 1, A.status);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) lse[buf * 128 + j * 32 + lane] = x[j];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&lse_full[buf]);
+    }
+  } else if (warp == 16) {
+    // ---- matrix instructions, all by one elected thread
+    if (elect_one()) {
+      const uint64_t k_at[2] = {smem_matrix(smem_u32(sk), 16), smem_matrix(smem_u32(sk + Sh::kTileBytes), 16)}, q_ring = smem_matrix(smem_u32(ring), 16);
+      mbar_wait_fast(k_full, 0, A.status);
+      for (int it = 0; it < tiles; ++it) {
+        const int st = it % STAGES, buf = it & 1;
+        const uint64_t qd = q_ring + (uint32_t)(st * (Sh::kTileBytes >> 4));
+        mbar_wait_fast(&full[st], (it / STAGES) & 1, A.status);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          if (it >= 2) mbar_wait_fast(&s_empty[t * 2 + buf], ((it >> 1) & 1) ^ 1, A.status);
+          tcgen05_after_sync();
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k) {
+            constexpr int kPart = Sh::kPartBytes >> 4;
+            mma_smem(tmem + (t * 2 + buf) * 128, k_at[t] + (k >> 2) * kPart + (k & 3) * 2, qd + (k >> 2) * kPart + (k & 3) * 2, mma_shape(128, false), k > 0);
+          }
+          tcgen05_commit(&s_full[t * 2 + buf]);
+        }
+        tcgen05_commit(&empty[st]);
+      }
+      // the last copies and instructions are done before the CTA ends
+      for (int t = 0; t < 2; ++t) mbar_wait_fast(&s_full[t * 2 + ((tiles - 1) & 1)], ((tiles - 1) >> 1) & 1, A.status);
+    }
+    __syncwarp();
+  } else if (warp < 16) {
+    // ---- an entry and half of a row tile's rows per thread
+    const int t = warp >> 3, half = (warp >> 2) & 1, e = e0 + t * 128 + (tid & 127);
+    const uint32_t s_at = tmem + ((uint32_t)(warp & 3) << 21) + t * 256 + half * 64;
+    const float c = A.scale_log2;
+    // rows [r_lo, r_hi) of the sequence see the entry
+    const int r_lo = max(0, e - old) << P.g_shift;
+    const long long t_hi = A.window == 0 || e < A.sink ? s.n : min((long long)s.n, (long long)e - old + A.window);
+    const int r_hi = e < s.len ? (int)(max(t_hi, 0LL) << P.g_shift) : 0;
+    float total = 0.f;
+    for (int it = 0; it < tiles; ++it) {
+      const int buf = it & 1, row0 = (tile0 + it) * 128 + half * 64;
+      mbar_wait_fast(&lse_full[buf], (it >> 1) & 1, A.status);
+      mbar_wait_fast(&s_full[t * 2 + buf], (it >> 1) & 1, A.status);
+      tcgen05_after_sync();
+      const bool whole = __all_sync(~0u, row0 >= r_lo && row0 + 64 <= r_hi);
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+      for (int h = 0; h < 2; ++h) {
+        uint32_t x[32];
+        tmem_load32(s_at + buf * 128 + h * 32, x);
+        tmem_wait_loads();
+        const float4* ls = reinterpret_cast<const float4*>(lse + buf * 128 + half * 64 + h * 32);
+        if (whole) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float4 z = ls[i];
+            sum[0] += exp2_fast(fmaf(__uint_as_float(x[4 * i]), c, -z.x));
+            sum[1] += exp2_fast(fmaf(__uint_as_float(x[4 * i + 1]), c, -z.y));
+            sum[2] += exp2_fast(fmaf(__uint_as_float(x[4 * i + 2]), c, -z.z));
+            sum[3] += exp2_fast(fmaf(__uint_as_float(x[4 * i + 3]), c, -z.w));
+          }
+        } else {
+          const int lo = r_lo - row0 - h * 32, hi = r_hi - row0 - h * 32;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float4 z = ls[i];
+            const float w0 = exp2_fast(fmaf(__uint_as_float(x[4 * i]), c, -z.x)), w1 = exp2_fast(fmaf(__uint_as_float(x[4 * i + 1]), c, -z.y));
+            const float w2 = exp2_fast(fmaf(__uint_as_float(x[4 * i + 2]), c, -z.z)), w3 = exp2_fast(fmaf(__uint_as_float(x[4 * i + 3]), c, -z.w));
+            sum[0] += 4 * i >= lo && 4 * i < hi ? w0 : 0.f;
+            sum[1] += 4 * i + 1 >= lo && 4 * i + 1 < hi ? w1 : 0.f;
+            sum[2] += 4 * i + 2 >= lo && 4 * i + 2 < hi ? w2 : 0.f;
+            sum[3] += 4 * i + 3 >= lo && 4 * i + 3 < hi ? w3 : 0.f;
+          }
+        }
+      }
+      total += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      tcgen05_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&s_empty[t * 2 + buf]);
+    }
+    if (half) sums[t * 128 + (tid & 127)] = total;
+    asm volatile("bar.sync 1, 512;" ::: "memory");
+    if (!half && e < s.len) {
+      float* a = A.scores + ((long long)b * A.n_kv_heads + head) * A.score_stride + e;
+      *a = (A.k && e >= old ? 0.f : *a) + (total + sums[t * 128 + (tid & 127)]) * (1.f / G);
+    }
+  }
+  tcgen05_before_sync();
+  __syncthreads();
+  if (warp == 16) {
     tcgen05_after_sync();
     tmem_give_back(tmem);
   }
