@@ -35,6 +35,10 @@ struct wkv_paged {
   float* part = nullptr;
   float2* part_ml = nullptr;
   uint32_t* arrived = nullptr;
+  // prompts on bf16 rows: the runs' outputs, next item
+  float* run_part = nullptr;
+  float2* run_ml = nullptr;
+  uint32_t* item_counter = nullptr;
   // the pools as [chunk][part][row][128 bytes], boxes of a page's rows (at most a decode tile's) x all parts
   alignas(64) unsigned char page_kmap[128] = {};
   alignas(64) unsigned char page_vmap[128] = {};
@@ -263,13 +267,20 @@ int decode(wkv_paged* c, const wkv::PagedParams& A) {
 }
 
 // Prompt attention on bf16 rows (tensor cores) ...
+constexpr int kMaxRuns = 2;            // per SM, over all row blocks
 template <int D>
 int prefill_bf16(wkv_paged* c, const wkv::PagedParams& A) {
   wkv::PrefillParams P;
   std::memset(&P, 0, sizeof(P));
   P.A = A;
   P.g_shift = c->group == 1 ? 0 : c->group == 2 ? 1 : c->group == 4 ? 2 : 3;
-  P.blocks = (int)(((long long)A.rows * c->group >> 8) + A.batch);
+  const long long units = (((long long)A.rows * c->group >> 8) + A.batch) * A.n_kv_heads;
+  // Runs of the key tiles: as many as the SMs can use when the row blocks alone are fewer, at least four tiles each.
+  const long long tiles = ((long long)A.width * A.page + wkv::kPrefillKeys - 1) / wkv::kPrefillKeys;
+  P.splits = (int)std::max<long long>(1, std::min<long long>(kMaxRuns * c->sm_count / units, tiles / 4));
+  if (units * P.splits > 0x3fffffff) return fail(c, WKV_ERR_INVALID, "total_q * n_q_heads is too large");
+  P.items = (int)(units * P.splits);
+  P.counter = c->item_counter; P.part = c->run_part; P.part_ml = c->run_ml;
   P.oob_chunk = c->cfg.n_layers * c->cfg.n_pages * c->cfg.n_kv_heads;
   P.chunk0 = chunk0(c, A);
   const int rc = encode_queries(c, P.qmap, A);
@@ -277,7 +288,8 @@ int prefill_bf16(wkv_paged* c, const wkv::PagedParams& A) {
   std::memcpy(P.kmap, c->part_kmap, 128);
   std::memcpy(P.vmap, c->part_vmap, 128);
   constexpr int smem = wkv::PrefillShape<D>::kSmem;
-  WKV_CUDA(c, launch(c, wkv::paged_prefill_kernel<D>, (long long)P.blocks * A.n_kv_heads, wkv::kPrefillThreads, smem, P));
+  WKV_CUDA(c, launch(c, wkv::paged_prefill_kernel<D>, std::min(P.items, c->sm_count), wkv::kPrefillThreads, smem, P));
+  if (P.splits > 1) WKV_CUDA(c, launch(c, wkv::paged_prefill_join_kernel<D>, units * 8, 256, 0, P));
   if (A.scores) {
     const long long blocks = ((long long)A.width * A.page + 255) / 256;
     WKV_CUDA(c, launch(c, wkv::paged_weights_tc_kernel<D>, blocks * A.batch * A.n_kv_heads, wkv::kWeightsThreads, wkv::WeightsShape<D>::kSmem, P));
@@ -349,6 +361,11 @@ int wkv_paged_create(const wkv_paged_config* cfg, wkv_paged** out) {
   WKV_TAKE(&c->part, ((size_t)c->decode_ctas + lanes) * c->group * cfg->head_dim * 4);
   WKV_TAKE(&c->part_ml, ((size_t)c->decode_ctas + lanes) * c->group * 8);
   WKV_TAKE(&c->arrived, lanes * 4);
+  if (cfg->dtype == WKV_BF16) {
+    WKV_TAKE(&c->run_part, (size_t)kMaxRuns * c->sm_count * 256 * cfg->head_dim * 4);
+    WKV_TAKE(&c->run_ml, (size_t)kMaxRuns * c->sm_count * 256 * 8);
+    WKV_TAKE(&c->item_counter, 4);
+  }
   const bool own_pools = !c->k_pool;
   if (own_pools) {
     WKV_TAKE(&c->k_pool, pool);
@@ -358,6 +375,7 @@ int wkv_paged_create(const wkv_paged_config* cfg, wkv_paged** out) {
   if (rc == WKV_OK) {
     e = cudaMemsetAsync(c->status, 0, 4, c->stream);
     if (e == cudaSuccess) e = cudaMemsetAsync(c->arrived, 0, lanes * 4, c->stream);
+    if (e == cudaSuccess && c->item_counter) e = cudaMemsetAsync(c->item_counter, 0, 4, c->stream);
     if (e == cudaSuccess && own_pools) e = cudaMemsetAsync(c->k_pool, 0, pool, c->stream);
     if (e == cudaSuccess && own_pools) e = cudaMemsetAsync(c->v_pool, 0, pool, c->stream);
     if (e != cudaSuccess) rc = WKV_ERR_CUDA;

@@ -5,11 +5,15 @@
 // logits takes the SM's tensor cores 2 x 512 cycles at D = 128 and its 16 exponentials a cycle 1024 cycles, so the two have
 // to overlap.
 //
-// A CTA owns 256 rows of one kv head, a row being (token, query head of the group), token-major: grouped heads share a tile,
-// so a row tile spans 128 / G tokens and a window wastes little of it.  Two row tiles of 128 take turns: while one's logits
-// are in its softmax warps, the tensor cores work on the other's.  Warps 0-3 and 4-7: softmax of row tile 0 and 1, a thread
-// per row (a TMEM lane), so statistics need no shuffles; warp 8 issues all matrix instructions; warp 9 all copies
-// (10 and 11 idle).
+// An item of work is 256 rows of one kv head -- a row being (token, query head of the group), token-major: grouped heads share a
+// tile, so a row tile spans 128 / G tokens and a window wastes little of it -- and a share of the key tiles that they see: all of
+// them, or one of `splits` equal runs where there are too few row blocks to fill the GPU (chunks of a few tokens behind long
+// contexts); paged_prefill_join_kernel then joins the runs.  One CTA per SM takes items from a counter until there are none: the
+// copies of the next item run while the last one's outputs are written.
+//
+// Two row tiles of 128 take turns: while one's logits are in its softmax warps, the tensor cores work on the other's.  Warps 0-3
+// and 4-7: softmax of row tile 0 and 1, a thread per row (a TMEM lane), so statistics need no shuffles; warp 8 issues all matrix
+// instructions; warp 9 all copies; warp 10 fetches items (11 idles).
 // TMEM, 512 columns: logits of both tiles (fp32, 128 columns each; the weights overwrite them as bf16, 64 columns, and are the A
 // operand of P.V straight from TMEM) and both outputs (D columns each).  An output is rescaled in place, and only when a row's
 // maximum has grown by more than 2^8 since its reference was taken.
@@ -28,7 +32,11 @@ constexpr int kPrefillKeys = 128;            // entries per tile
 struct PrefillParams {
   PagedParams A;
   int g_shift;               // log2 of the query heads per kv head
-  int blocks;                // row blocks of one kv head over all sequences, at most
+  int items;                 // row blocks (at most) x kv heads x splits
+  int splits;
+  uint32_t* counter;         // next item; zero between launches
+  float* part;               // [row block x kv head][split][256][D] outputs, where splits > 1
+  float2* part_ml;           // [row block x kv head][split][256] (maximum in base-2 logits, sum)
   int oob_chunk, chunk0;
   alignas(64) unsigned char qmap[128];   // q as [part][token][head][64 elements], boxes of a row tile
   alignas(64) unsigned char kmap[128];   // pool as [chunk][part][row][64 elements], boxes of a page x one part
@@ -41,7 +49,7 @@ struct PrefillShape {
   static constexpr int kPartBytes = 128 * 128;                    // 128 rows x 128 bytes
   static constexpr int kTileBytes = kParts * kPartBytes;          // of Q (one row tile), K or V
   static constexpr int kStages = D == 128 ? 5 : 8;
-  static constexpr int kSmem = 2 * kTileBytes + kStages * kTileBytes + (2 * kStages + 10) * 8 + 32;
+  static constexpr int kSmem = 2 * kTileBytes + kStages * kTileBytes + (2 * kStages + 18) * 8 + 16 + 2 * 64;
 };
 
 __device__ __forceinline__ void tensor_g2s_4d(void* dst, const void* tmap, int x, int y, int z, int w, uint64_t* bar) {
@@ -154,6 +162,17 @@ __device__ __forceinline__ void exp2_pair(float& x0, float& x1) {
   x1 = __uint_as_float(__float_as_uint(x1) + (__float_as_uint(n1) << 23));
 }
 
+// What warp 10 tells the others about an item.
+struct PrefillItem {
+  PrefillBlock B;
+  int v0, v1;                // its key tiles
+  int slot;                  // (row block x kv head) * splits + split; -1: no more items
+};
+static_assert(sizeof(PrefillItem) <= 64, "two of them in 128 bytes of shared memory");
+
+// Visible columns of a 32-column piece as bits: columns 0..top, of these low.. and those below sinks.
+__device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
+
 template <int D>
 __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const __grid_constant__ PrefillParams P) {
   using Sh = PrefillShape<D>;
@@ -163,134 +182,212 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
   uint64_t* full = reinterpret_cast<uint64_t*>(ring + STAGES * Sh::kTileBytes);
   uint64_t* empty = full + STAGES;
   uint64_t* q_full = empty + STAGES;
-  uint64_t* s_full = q_full + 1;       // [2] logits of a row tile are in TMEM (and its last P.V is done)
+  uint64_t* q_free = q_full + 1;       // the item's last logits are done
+  uint64_t* s_full = q_free + 1;       // [2] logits of a row tile are in TMEM (and its last P.V is done)
   uint64_t* p_ready = s_full + 2;      // [2][2] a half of the weights is in TMEM, the output is rescaled
-  uint64_t* o_full = p_ready + 4;      // all matrix instructions are done
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_full + 1);
+  uint64_t* o_full = p_ready + 4;      // all of the item's matrix instructions are done
+  uint64_t* o_free = o_full + 1;       // [2] a row tile's output has been read
+  uint64_t* item_full = o_free + 2;    // [2]
+  uint64_t* item_empty = item_full + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(item_empty + 2);
+  unsigned char* item_smem = reinterpret_cast<unsigned char*>(tmem_slot + 4);
 
   const PagedParams& A = P.A;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, G = 1 << P.g_shift;
   if (tid == 0) {
     for (int i = 0; i < STAGES; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
     mbar_init(q_full, 1);
-    for (int t = 0; t < 2; ++t) { mbar_init(&s_full[t], 1); mbar_init(&p_ready[2 * t], 4); mbar_init(&p_ready[2 * t + 1], 4); }
+    mbar_init(q_free, 1);
     mbar_init(o_full, 1);
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(&s_full[t], 1); mbar_init(&p_ready[2 * t], 4); mbar_init(&p_ready[2 * t + 1], 4); mbar_init(&o_free[t], 4);
+      mbar_init(&item_full[t], 1); mbar_init(&item_empty[t], 10);
+    }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   griddep_launch();
-  griddep_wait();
-  PrefillBlock B;
-  if (!find_block(A, P.g_shift, blockIdx.x / A.n_kv_heads, blockIdx.x % A.n_kv_heads, B)) return;    // the grid is an upper bound
   if (warp == 8) tmem_take(tmem_slot);
   tcgen05_before_sync();
+  griddep_wait();
   __syncthreads();
   tcgen05_after_sync();
   const uint32_t tmem = __shfl_sync(~0u, *tmem_slot, 0);
-  const int G = 1 << P.g_shift;
 
-  {
-    const RowTile rt[2] = {row_tile(B, B.row0, P.g_shift), row_tile(B, B.row0 + 128, P.g_shift)};
-    if (warp >= 8) {
+  // the n-th item of this CTA, once it is there; every reader tells when it has its copy
+  auto take_item = [&](int n, PrefillItem& item) {
+    mbar_wait_fast(&item_full[n & 1], (n >> 1) & 1, A.status);
+    item = *reinterpret_cast<const PrefillItem*>(item_smem + (n & 1) * 64);
+  };
+
+  if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-    if (warp == 9) {
+    if (warp == 10) {
+      // ---- items
+      for (int n = 0;; ++n) {
+        PrefillItem item;
+        item.slot = -1;
+        for (;;) {
+          uint32_t w = 0;
+          if (lane == 0) w = atomicAdd(P.counter, 1u);
+          w = __shfl_sync(~0u, w, 0);
+          if (w >= (uint32_t)P.items) {
+            if (lane == 0 && w == (uint32_t)P.items + gridDim.x - 1) *P.counter = 0;      // the last CTA to ask
+            break;
+          }
+          const int split = w % P.splits, unit = w / P.splits;
+          if (!find_block(A, P.g_shift, unit / A.n_kv_heads, unit % A.n_kv_heads, item.B)) continue;     // `items` is an upper bound
+          item.v0 = item.B.tiles * split / P.splits;
+          item.v1 = item.B.tiles * (split + 1) / P.splits;
+          item.slot = (int)w;
+          break;
+        }
+        if (n >= 2) mbar_wait_fast(&item_empty[n & 1], ((n >> 1) & 1) ^ 1, A.status);
+        if (lane == 0) {
+          *reinterpret_cast<PrefillItem*>(item_smem + (n & 1) * 64) = item;
+          mbar_arrive(&item_full[n & 1]);
+        }
+        __syncwarp();
+        if (item.slot < 0) break;
+      }
+    } else if (warp == 9) {
       // ---- copies
       const int pr = A.page, boxes = kPrefillKeys >> A.page_shift;
-      fence_proxy_async();                                     // rows that the append kernel stored
-      if (lane == 0) {
-        const int tiles = rt[1].any ? 2 : 1;
-        mbar_expect_tx(q_full, tiles * Sh::kTileBytes);
-        for (int t = 0; t < tiles; ++t)
-          for (int p = 0; p < Sh::kParts; ++p)
-            tensor_g2s_4d(sq + t * Sh::kTileBytes + p * Sh::kPartBytes, P.qmap, 0, B.head * G, B.first + ((B.row0 + t * 128) >> P.g_shift), p, q_full);
-      }
       const bool mine = lane < boxes * Sh::kParts;
       const int box = lane & (boxes - 1), part = mine ? lane / boxes : 0;
-      const int lo_key = B.first_tile * kPrefillKeys;
-      for (int v = 0, it = 0; v < B.tiles; ++v) {
-        const int i = B.tile(v) * kPrefillKeys + box * pr;
-        int chunk = P.oob_chunk;
-        if (mine && i < B.len && (i >= lo_key || i < B.sinks)) {
-          const int pg = page_of(A, B.b, i);
-          if (pg >= 0) chunk = P.chunk0 + pg * A.n_kv_heads + B.head;
+      fence_proxy_async();                                     // rows that the append kernel stored
+      int it = 0;
+      for (int n = 0;; ++n) {
+        PrefillItem item;
+        take_item(n, item);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&item_empty[n & 1]);
+        if (item.slot < 0) break;
+        const PrefillBlock& B = item.B;
+        if (n > 0) mbar_wait_fast(q_free, (n & 1) ^ 1, A.status);
+        if (lane == 0) {
+          const int tiles = B.row0 + 128 < B.n << P.g_shift ? 2 : 1;
+          mbar_expect_tx(q_full, tiles * Sh::kTileBytes);
+          for (int t = 0; t < tiles; ++t)
+            for (int p = 0; p < Sh::kParts; ++p)
+              tensor_g2s_4d(sq + t * Sh::kTileBytes + p * Sh::kPartBytes, P.qmap, 0, B.head * G, B.first + ((B.row0 + t * 128) >> P.g_shift), p, q_full);
         }
+        __syncwarp();
+        const int lo_key = B.first_tile * kPrefillKeys;
+        for (int v = item.v0; v < item.v1; ++v) {
+          const int i = B.tile(v) * kPrefillKeys + box * pr;
+          int chunk = P.oob_chunk;
+          if (mine && i < B.len && (i >= lo_key || i < B.sinks)) {
+            const int pg = page_of(A, B.b, i);
+            if (pg >= 0) chunk = P.chunk0 + pg * A.n_kv_heads + B.head;
+          }
 #pragma unroll
-        for (int kv = 0; kv < 2; ++kv, ++it) {
-          const int st = it % STAGES;
-          if (it >= STAGES) mbar_wait_fast(&empty[st], ((it / STAGES) & 1) ^ 1, A.status);
-          if (lane == 0) mbar_expect_tx(&full[st], Sh::kTileBytes);
-          __syncwarp();
-          if (mine)
-            tensor_g2s_4d(ring + st * Sh::kTileBytes + part * Sh::kPartBytes + box * pr * 128, kv ? P.vmap : P.kmap, 0, 0, part, chunk, &full[st]);
+          for (int kv = 0; kv < 2; ++kv, ++it) {
+            const int st = it % STAGES;
+            if (it >= STAGES) mbar_wait_fast(&empty[st], ((it / STAGES) & 1) ^ 1, A.status);
+            if (lane == 0) mbar_expect_tx(&full[st], Sh::kTileBytes);
+            __syncwarp();
+            if (mine)
+              tensor_g2s_4d(ring + st * Sh::kTileBytes + part * Sh::kPartBytes + box * pr * 128, kv ? P.vmap : P.kmap, 0, 0, part, chunk, &full[st]);
+          }
         }
       }
     } else if (warp == 8) {
       // ---- matrix instructions, all by one elected thread
       if (elect_one()) {
-      const uint32_t s_at[2] = {tmem, tmem + 128}, o_at[2] = {tmem + 256, tmem + 256 + D};
-      const uint64_t q_at[2] = {smem_matrix(smem_u32(sq), 16), smem_matrix(smem_u32(sq + Sh::kTileBytes), 16)};
-      const uint64_t k_ring = smem_matrix(smem_u32(ring), 16), v_ring = smem_matrix(smem_u32(ring), Sh::kPartBytes);
-      bool pending[2] = {false, false}, started[2] = {false, false};
-      uint32_t p_phase[2] = {0, 0};
-      auto weights_times_values = [&](int t, uint64_t vd) {
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          mbar_wait_fast(&p_ready[2 * t + half], p_phase[t], A.status);
-          tcgen05_after_sync();
-#pragma unroll
-          for (int k = half * 4; k < half * 4 + 4; ++k) mma_tmem(o_at[t], s_at[t] + k * 8, vd + k * 128, mma_shape(D, true), started[t] || k > 0);
-        }
-        p_phase[t] ^= 1;
-        started[t] = true;
-        pending[t] = false;
-      };
-      mbar_wait_fast(q_full, 0, A.status);
-      uint64_t vd = 0;                                          // values of the tile before
-      for (int v = 0, it = 0; v < B.tiles; ++v, it += 2) {
-        const int st = it % STAGES, e0 = B.tile(v) * kPrefillKeys;
-        const uint64_t kd = k_ring + (uint32_t)(st * (Sh::kTileBytes >> 4));
-        // both copies ahead of the weights, so that P.V and the next logits of a row tile are issued in one go
-        mbar_wait_fast(&full[st], (it / STAGES) & 1, A.status);
-        if (v > 0) mbar_wait_fast(&full[(it - 1) % STAGES], ((it - 1) / STAGES) & 1, A.status);
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          if (pending[t]) weights_times_values(t, vd);
-          if (!tile_seen(rt[t], e0, A.window, A.sink)) continue;
-#pragma unroll
-          for (int k = 0; k < D / 16; ++k) {
-            constexpr int kPart = Sh::kPartBytes >> 4;
-            mma_smem(s_at[t], q_at[t] + (k >> 2) * kPart + (k & 3) * 2, kd + (k >> 2) * kPart + (k & 3) * 2, mma_shape(kPrefillKeys, false), k > 0);
+        const uint32_t s_at[2] = {tmem, tmem + 128}, o_at[2] = {tmem + 256, tmem + 256 + D};
+        const uint64_t q_at[2] = {smem_matrix(smem_u32(sq), 16), smem_matrix(smem_u32(sq + Sh::kTileBytes), 16)};
+        const uint64_t k_ring = smem_matrix(smem_u32(ring), 16), v_ring = smem_matrix(smem_u32(ring), Sh::kPartBytes);
+        uint32_t p_phase[2] = {0, 0};
+        int it = 0;
+        for (int n = 0;; ++n) {
+          PrefillItem item;
+          take_item(n, item);
+          mbar_arrive(&item_empty[n & 1]);
+          if (item.slot < 0) {
+            if (n > 0) mbar_wait_fast(o_full, (n & 1) ^ 1, A.status);        // nothing is in flight when the CTA ends
+            break;
           }
-          tcgen05_commit(&s_full[t]);
-          pending[t] = true;
-        }
-        tcgen05_commit(&empty[st]);
-        if (v > 0) tcgen05_commit(&empty[(it - 1) % STAGES]);
-        vd = v_ring + (uint32_t)(((it + 1) % STAGES) * (Sh::kTileBytes >> 4));
-      }
-      if (B.tiles > 0) mbar_wait_fast(&full[(2 * B.tiles - 1) % STAGES], ((2 * B.tiles - 1) / STAGES) & 1, A.status);
+          const PrefillBlock& B = item.B;
+          const RowTile rt[2] = {row_tile(B, B.row0, P.g_shift), row_tile(B, B.row0 + 128, P.g_shift)};
+          bool pending[2] = {false, false}, started[2] = {false, false};
+          uint64_t vd = 0;                                        // values of the tile before
+          auto weights_times_values = [&](int t) {
+            if (!started[t] && n > 0) mbar_wait_fast(&o_free[t], (n & 1) ^ 1, A.status);
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
-        if (pending[t]) weights_times_values(t, vd);
-      tcgen05_commit(o_full);
-      mbar_wait_fast(o_full, 0, A.status);
+            for (int half = 0; half < 2; ++half) {
+              mbar_wait_fast(&p_ready[2 * t + half], p_phase[t], A.status);
+              tcgen05_after_sync();
+#pragma unroll
+              for (int k = half * 4; k < half * 4 + 4; ++k) mma_tmem(o_at[t], s_at[t] + k * 8, vd + k * 128, mma_shape(D, true), started[t] || k > 0);
+            }
+            p_phase[t] ^= 1;
+            started[t] = true;
+            pending[t] = false;
+          };
+          mbar_wait_fast(q_full, n & 1, A.status);
+          for (int v = item.v0; v < item.v1; ++v, it += 2) {
+            const int st = it % STAGES, e0 = B.tile(v) * kPrefillKeys;
+            const uint64_t kd = k_ring + (uint32_t)(st * (Sh::kTileBytes >> 4));
+            // both copies ahead of the weights, so that P.V and the next logits of a row tile are issued in one go
+            mbar_wait_fast(&full[st], (it / STAGES) & 1, A.status);
+            if (v > item.v0) mbar_wait_fast(&full[(it - 1) % STAGES], ((it - 1) / STAGES) & 1, A.status);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              if (pending[t]) weights_times_values(t);
+              if (!tile_seen(rt[t], e0, A.window, A.sink)) continue;
+              tcgen05_after_sync();
+#pragma unroll
+              for (int k = 0; k < D / 16; ++k) {
+                constexpr int kPart = Sh::kPartBytes >> 4;
+                mma_smem(s_at[t], q_at[t] + (k >> 2) * kPart + (k & 3) * 2, kd + (k >> 2) * kPart + (k & 3) * 2, mma_shape(kPrefillKeys, false), k > 0);
+              }
+              tcgen05_commit(&s_full[t]);
+              pending[t] = true;
+            }
+            tcgen05_commit(&empty[st]);
+            if (v > item.v0) tcgen05_commit(&empty[(it - 1) % STAGES]);
+            vd = v_ring + (uint32_t)(((it + 1) % STAGES) * (Sh::kTileBytes >> 4));
+          }
+          tcgen05_commit(q_free);
+          if (item.v1 > item.v0) {
+            mbar_wait_fast(&full[(it - 1) % STAGES], ((it - 1) / STAGES) & 1, A.status);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+              if (pending[t]) weights_times_values(t);
+            tcgen05_commit(&empty[(it - 1) % STAGES]);
+          }
+          // a row tile without products in this item: its readers' word on the last item is still due
+          for (int t = 0; t < 2; ++t)
+            if (!started[t] && n > 0) mbar_wait_fast(&o_free[t], (n & 1) ^ 1, A.status);
+          tcgen05_commit(o_full);
+        }
       }
       __syncwarp();
     }
-    } else {
-      // ---- softmax: this thread's row
-      asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-      const int t = warp >> 2, row = tid & 127, R = B.row0 + t * 128 + row;
-      const RowTile my = t ? rt[1] : rt[0];
+  } else {
+    // ---- softmax: this thread's row
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    const int t = warp >> 2, row = tid & 127;
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21;          // 32 TMEM lanes per warp, lane number in bits 16..
+    const uint32_t s_at = tmem + lanes + t * 128, o_at = tmem + lanes + 256 + t * D;
+    const float c = A.scale_log2;
+    uint32_t phase = 0;
+    int it = 1;                                                 // ring position of the item's first values
+    for (int n = 0;; ++n) {
+      PrefillItem item;
+      take_item(n, item);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&item_empty[n & 1]);
+      if (item.slot < 0) break;
+      const PrefillBlock& B = item.B;
+      const int R = B.row0 + t * 128 + row;
+      const RowTile my = row_tile(B, B.row0 + t * 128, P.g_shift);
       const int pos = B.old + (R >> P.g_shift);
       const bool live = R < B.n << P.g_shift;
-      const int lo_key = A.window > 0 ? pos - A.window + 1 : 0;
-      const uint32_t lanes = (uint32_t)(warp & 3) << 21;        // 32 TMEM lanes per warp, lane number in bits 16..
-      const uint32_t s_at = tmem + lanes + t * 128, o_at = tmem + lanes + 256 + t * D;
-      const float c = A.scale_log2;
+      const int lo_key = A.window > 0 ? max(0, pos - A.window + 1) : 0;
       float m = -INFINITY, l = 0.f;                             // m: reference of the exponentials, in logits
-      uint32_t phase = 0;
       bool first = true;
-      for (int v = 0; v < B.tiles; ++v) {
+      for (int v = item.v0; v < item.v1; ++v) {
         const int e0 = B.tile(v) * kPrefillKeys;
         if (!tile_seen(my, e0, A.window, A.sink)) continue;
         mbar_wait_fast(&s_full[t], phase, A.status);
@@ -304,10 +401,14 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
         const bool whole = e0 + kPrefillKeys - 1 <= my.pos_lo &&
                            (A.window == 0 || e0 >= my.pos_hi - A.window + 1 || e0 + kPrefillKeys <= A.sink);
         if (!whole) {
-          const int top = pos - e0, low = max(lo_key, 0) - e0, sinks = A.sink - e0;
 #pragma unroll
-          for (int i = 0; i < 128; ++i)
-            if (i > top || (i < low && i >= sinks)) x[i] = 0xff800000u;
+          for (int h = 0; h < 4; ++h) {
+            const int at = e0 + h * 32;
+            const uint32_t see = low_bits(pos + 1 - at) & (~low_bits(lo_key - at) | low_bits(A.sink - at));
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (!(see >> i & 1)) x[h * 32 + i] = 0xff800000u;
+          }
         }
         float mx4[4];                                           // four chains: the latency of one would show
 #pragma unroll
@@ -341,8 +442,8 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
         }
         if (e0 + kPrefillKeys > B.len) {
           // rows behind the sequence may hold anything: their weights are zero, their values have to be finite
-          const int it = 2 * v + 1, st = it % STAGES;
-          mbar_wait_fast(&full[st], (it / STAGES) & 1, A.status);
+          const int at = it + 2 * (v - item.v0), st = at % STAGES;
+          mbar_wait_fast(&full[st], (at / STAGES) & 1, A.status);
           for (int e = row + (B.len - e0) * 8 * Sh::kParts; e < kPrefillKeys * 8 * Sh::kParts; e += 128) {
             const int r = e / (8 * Sh::kParts), piece = e % (8 * Sh::kParts);
             *reinterpret_cast<uint4*>(ring + st * Sh::kTileBytes + (piece >> 3) * Sh::kPartBytes + r * 128 + (piece & 7) * 16) = make_uint4(0, 0, 0, 0);
@@ -380,11 +481,12 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
         unpair(add2(add2(sum2[0], sum2[1]), add2(sum2[2], sum2[3])), a0, a1);
         l += a0 + a1;
       }
+      it += 2 * (item.v1 - item.v0);
       // ---- output
-      if (my.any) {
-        mbar_wait_fast(o_full, 0, A.status);
-        tcgen05_after_sync();
-        const bool seen = !(l <= 0.f);                          // else the row's TMEM lane may hold anything
+      mbar_wait_fast(o_full, n & 1, A.status);
+      tcgen05_after_sync();
+      const bool seen = !(l <= 0.f);                            // else the row's TMEM lane may hold anything
+      if (P.splits == 1) {
         const float inv = seen ? 1.f / l : 0.f;
         const int tok = B.first + (R >> P.g_shift), hq = B.head * G + (R & (G - 1));
         __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + ((long long)tok * A.n_q_heads + hq) * D;
@@ -396,27 +498,77 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
           if (live) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              uint4 y;
+              uint32_t y[4];
 #pragma unroll
-              for (int z = 0; z < 8; ++z) o[e * 8 + z] = seen ? o[e * 8 + z] : 0u;
-              y.x = pack_bf16(__uint_as_float(o[e * 8]) * inv, __uint_as_float(o[e * 8 + 1]) * inv);
-              y.y = pack_bf16(__uint_as_float(o[e * 8 + 2]) * inv, __uint_as_float(o[e * 8 + 3]) * inv);
-              y.z = pack_bf16(__uint_as_float(o[e * 8 + 4]) * inv, __uint_as_float(o[e * 8 + 5]) * inv);
-              y.w = pack_bf16(__uint_as_float(o[e * 8 + 6]) * inv, __uint_as_float(o[e * 8 + 7]) * inv);
-              reinterpret_cast<uint4*>(out)[i * 4 + e] = y;
+              for (int z = 0; z < 4; ++z)
+                y[z] = seen ? pack_bf16(__uint_as_float(o[e * 8 + 2 * z]) * inv, __uint_as_float(o[e * 8 + 2 * z + 1]) * inv) : 0u;
+              reinterpret_cast<uint4*>(out)[i * 4 + e] = make_uint4(y[0], y[1], y[2], y[3]);
             }
           }
         }
         if (live && A.lse) A.lse[(long long)tok * A.n_q_heads + hq] = seen ? (m * c + log2f(l)) * kLn2 : -INFINITY;
-        tcgen05_before_sync();
+      } else {
+        const long long at = (long long)item.slot * 256 + t * 128 + row;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+          uint32_t o[32];
+          tmem_load32(o_at + i * 32, o);
+          tmem_wait_loads();
+          if (live && seen) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) reinterpret_cast<uint4*>(P.part + at * D)[i * 8 + e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+          }
+        }
+        if (live) P.part_ml[at] = make_float2(seen ? m * c : -INFINITY, seen ? l : 0.f);
       }
+      tcgen05_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&o_free[t]);
     }
   }
+  tcgen05_before_sync();
   __syncthreads();
   if (warp == 8) {
     tcgen05_after_sync();
     tmem_give_back(tmem);
   }
+}
+
+// The runs of a row block joined: eight threads per row, 32 rows per CTA.
+template <int D>
+__global__ void __launch_bounds__(256) paged_prefill_join_kernel(const __grid_constant__ PrefillParams P) {
+  griddep_wait();
+  const PagedParams& A = P.A;
+  const int unit = blockIdx.x >> 3, G = 1 << P.g_shift;
+  PrefillBlock B;
+  if (!find_block(A, P.g_shift, unit / A.n_kv_heads, unit % A.n_kv_heads, B)) return;
+  const int row = (blockIdx.x & 7) * 32 + (threadIdx.x >> 3), R = B.row0 + row, c0 = threadIdx.x & 7;
+  if (R >= B.n << P.g_shift) return;
+  float m = -INFINITY;
+  for (int s = 0; s < P.splits; ++s) m = fmaxf(m, P.part_ml[((long long)unit * P.splits + s) * 256 + row].x);
+  constexpr int V = D / 32;                                       // float4s per thread
+  float4 acc[V] = {};
+  float l = 0.f;
+  for (int s = 0; s < P.splits; ++s) {
+    const long long at = ((long long)unit * P.splits + s) * 256 + row;
+    const float2 ml = P.part_ml[at];
+    if (ml.x == -INFINITY) continue;                              // a run that the row sees nothing of wrote no output
+    const float f = exp2_fast(ml.x - m);
+    l = fmaf(ml.y, f, l);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float4 x = reinterpret_cast<const float4*>(P.part + at * D)[i * 8 + c0];
+      acc[i].x = fmaf(x.x, f, acc[i].x); acc[i].y = fmaf(x.y, f, acc[i].y); acc[i].z = fmaf(x.z, f, acc[i].z); acc[i].w = fmaf(x.w, f, acc[i].w);
+    }
+  }
+  const bool seen = !(l <= 0.f);
+  const float inv = seen ? 1.f / l : 0.f;
+  const long long tok = B.first + (R >> P.g_shift), hq = B.head * G + (R & (G - 1));
+  __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + (tok * A.n_q_heads + hq) * D;
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    reinterpret_cast<uint2*>(out)[i * 8 + c0] = make_uint2(pack_bf16(acc[i].x * inv, acc[i].y * inv), pack_bf16(acc[i].z * inv, acc[i].w * inv));
+  if (A.lse && c0 == 0) A.lse[tok * A.n_q_heads + hq] = seen ? (m + log2f(l)) * kLn2 : -INFINITY;
 }
 
 // ------------------------------------------------------------------------------------------------
