@@ -59,12 +59,14 @@ __device__ __forceinline__ void tensor_g2s_4d(void* dst, const void* tmap, int x
                : "memory");
 }
 
-// The row block of a CTA: which sequence, which rows; and the key tiles it walks: those with sinks, then the others.
+// A row block: which sequence, which rows, and the entries it walks -- the pages with sinks, then those from the page of the first
+// row's window on, end to end: tile v holds the 128 of them from 128 v on, so neither a few sinks nor a window's start in the
+// middle of nowhere takes a tile of its own.
 struct PrefillBlock {
   int b, head, first, n, len, old;      // old: entries before the chunk
   int row0;                             // first row (token * G + g) of the block
-  int sinks, sink_tiles, first_tile, tiles;
-  __device__ __forceinline__ int tile(int v) const { return v < sink_tiles ? v : first_tile + v - sink_tiles; }
+  int sink_rows, start, tiles;          // sink_rows, start: multiples of the page
+  __device__ __forceinline__ int entry(int i) const { return i < sink_rows ? i : i - sink_rows + start; }
 };
 // Positions of a row tile's first and last token; none if it has no rows.
 struct RowTile {
@@ -78,8 +80,20 @@ __device__ __forceinline__ RowTile row_tile(const PrefillBlock& B, int row0, int
   t.pos_hi = min(B.old + ((row0 + 127) >> g_shift), B.len - 1);
   return t;
 }
-__device__ __forceinline__ bool tile_seen(const RowTile& t, int e0, int window, int sink) {
-  return t.any && e0 <= t.pos_hi && (window == 0 || e0 + kPrefillKeys > t.pos_lo - window + 1 || e0 < sink);
+// Does any row of the row tile see an entry of tile v?
+__device__ __forceinline__ bool tile_seen(const PrefillBlock& B, const RowTile& t, int v, int window, int sink) {
+  const int at = v * kPrefillKeys;
+  if (!t.any) return false;
+  if (at < B.sink_rows) return true;
+  const int e0 = B.entry(at);
+  return e0 <= t.pos_hi && (window == 0 || e0 + kPrefillKeys > t.pos_lo - window + 1 || e0 < sink);
+}
+// Does every row see all of it?
+__device__ __forceinline__ bool tile_whole(const PrefillBlock& B, const RowTile& t, int v, int window, int sink) {
+  const int at = v * kPrefillKeys;
+  if (at < B.sink_rows) return at + kPrefillKeys <= min(sink, B.sink_rows);
+  const int e0 = B.entry(at);
+  return e0 + kPrefillKeys - 1 <= t.pos_lo && (window == 0 || e0 >= t.pos_hi - window + 1 || e0 + kPrefillKeys <= sink);
 }
 
 // The rb-th row block (256 rows) over all sequences; false if there is none.  Every warp searches for itself.
@@ -109,10 +123,9 @@ __device__ __forceinline__ bool find_block(const PagedParams& A, int g_shift, in
       const int p0 = B.old + (B.row0 >> g_shift);                              // positions of the block's tokens
       const int p1 = min(B.old + ((B.row0 + 255) >> g_shift), B.len - 1);
       const int lo_key = A.window > 0 ? max(0, p0 - A.window + 1) : 0;
-      B.sinks = min(A.sink, lo_key);
-      B.first_tile = lo_key / kPrefillKeys;
-      B.sink_tiles = min((B.sinks + kPrefillKeys - 1) / kPrefillKeys, B.first_tile);
-      B.tiles = p1 < 0 ? 0 : B.sink_tiles + p1 / kPrefillKeys + 1 - B.first_tile;
+      B.start = lo_key & ~(A.page - 1);
+      B.sink_rows = (min(A.sink, B.start) + A.page - 1) & ~(A.page - 1);
+      B.tiles = p1 < 0 ? 0 : (B.sink_rows + p1 + 1 - B.start + kPrefillKeys - 1) / kPrefillKeys;
       return true;
     }
     before += __shfl_sync(~0u, upto, 31);
@@ -272,11 +285,10 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
               tensor_g2s_4d(sq + t * Sh::kTileBytes + p * Sh::kPartBytes, P.qmap, 0, B.head * G, B.first + ((B.row0 + t * 128) >> P.g_shift), p, q_full);
         }
         __syncwarp();
-        const int lo_key = B.first_tile * kPrefillKeys;
         for (int v = item.v0; v < item.v1; ++v) {
-          const int i = B.tile(v) * kPrefillKeys + box * pr;
+          const int i = B.entry(v * kPrefillKeys + box * pr);
           int chunk = P.oob_chunk;
-          if (mine && i < B.len && (i >= lo_key || i < B.sinks)) {
+          if (mine && i < B.len) {
             const int pg = page_of(A, B.b, i);
             if (pg >= 0) chunk = P.chunk0 + pg * A.n_kv_heads + B.head;
           }
@@ -326,7 +338,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
           };
           mbar_wait_fast(q_full, n & 1, A.status);
           for (int v = item.v0; v < item.v1; ++v, it += 2) {
-            const int st = it % STAGES, e0 = B.tile(v) * kPrefillKeys;
+            const int st = it % STAGES;
             const uint64_t kd = k_ring + (uint32_t)(st * (Sh::kTileBytes >> 4));
             // both copies ahead of the weights, so that P.V and the next logits of a row tile are issued in one go
             mbar_wait_fast(&full[st], (it / STAGES) & 1, A.status);
@@ -334,7 +346,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
               if (pending[t]) weights_times_values(t);
-              if (!tile_seen(rt[t], e0, A.window, A.sink)) continue;
+              if (!tile_seen(B, rt[t], v, A.window, A.sink)) continue;
               tcgen05_after_sync();
 #pragma unroll
               for (int k = 0; k < D / 16; ++k) {
@@ -388,8 +400,8 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
       float m = -INFINITY, l = 0.f;                             // m: reference of the exponentials, in logits
       bool first = true;
       for (int v = item.v0; v < item.v1; ++v) {
-        const int e0 = B.tile(v) * kPrefillKeys;
-        if (!tile_seen(my, e0, A.window, A.sink)) continue;
+        const int v_at = v * kPrefillKeys;
+        if (!tile_seen(B, my, v, A.window, A.sink)) continue;
         mbar_wait_fast(&s_full[t], phase, A.status);
         phase ^= 1;
         tcgen05_after_sync();
@@ -398,13 +410,15 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
         for (int i = 0; i < 4; ++i) tmem_load32(s_at + i * 32, x + i * 32);
         tmem_wait_loads();
         // a tile that every row of the row tile sees whole needs no mask
-        const bool whole = e0 + kPrefillKeys - 1 <= my.pos_lo &&
-                           (A.window == 0 || e0 >= my.pos_hi - A.window + 1 || e0 + kPrefillKeys <= A.sink);
-        if (!whole) {
+        if (!tile_whole(B, my, v, A.window, A.sink)) {
 #pragma unroll
           for (int h = 0; h < 4; ++h) {
-            const int at = e0 + h * 32;
-            const uint32_t see = low_bits(pos + 1 - at) & (~low_bits(lo_key - at) | low_bits(A.sink - at));
+            const int at = v_at + h * 32, e0 = at - B.sink_rows + B.start;      // of the entries behind the sinks' pages
+            uint32_t see = low_bits(pos + 1 - e0) & (~low_bits(lo_key - e0) | low_bits(A.sink - e0));
+            if (at < B.sink_rows) {
+              const uint32_t front = low_bits(B.sink_rows - at);
+              see = (front & low_bits(min(A.sink, pos + 1) - at)) | (~front & see);
+            }
 #pragma unroll
             for (int i = 0; i < 32; ++i)
               if (!(see >> i & 1)) x[h * 32 + i] = 0xff800000u;
@@ -440,11 +454,12 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
             }
           }
         }
-        if (e0 + kPrefillKeys > B.len) {
+        const int v_len = B.len - B.start + B.sink_rows;          // where the sequence ends
+        if (v_at + kPrefillKeys > v_len) {
           // rows behind the sequence may hold anything: their weights are zero, their values have to be finite
           const int at = it + 2 * (v - item.v0), st = at % STAGES;
           mbar_wait_fast(&full[st], (at / STAGES) & 1, A.status);
-          for (int e = row + (B.len - e0) * 8 * Sh::kParts; e < kPrefillKeys * 8 * Sh::kParts; e += 128) {
+          for (int e = row + (v_len - v_at) * 8 * Sh::kParts; e < kPrefillKeys * 8 * Sh::kParts; e += 128) {
             const int r = e / (8 * Sh::kParts), piece = e % (8 * Sh::kParts);
             *reinterpret_cast<uint4*>(ring + st * Sh::kTileBytes + (piece >> 3) * Sh::kPartBytes + r * 128 + (piece & 7) * 16) = make_uint4(0, 0, 0, 0);
           }
