@@ -14,7 +14,7 @@ HEADER = os.path.join("..", "..", "include", "wkv.h")
 UNITS = {
     "wkv_api.cu": ["wkv_ptx.cuh", "wkv_kernels.cuh", "wkv_prefill.cuh", "wkv_block.cuh", HEADER],
     "wkv_paged_api.cu": ["wkv_ptx.cuh", "wkv_paged.cuh", "wkv_paged_decode.cuh",
-                         "wkv_paged_prefill.cuh", "wkv_tcgen05.cuh", HEADER],
+                         "wkv_paged_prefill.cuh", "wkv_paged_f32.cuh", "wkv_tcgen05.cuh", HEADER],
 }
 SOURCES = list(UNITS)
 DEPS = sorted(set(SOURCES) | {d for deps in UNITS.values() for d in deps})

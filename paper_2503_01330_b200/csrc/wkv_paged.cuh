@@ -94,13 +94,6 @@ __device__ __forceinline__ bool visible(int i, int pos, int window, int sink) {
   return i <= pos && (window == 0 || i > pos - window || i < sink);
 }
 
-template <typename T> __device__ __forceinline__ float as_float(T x);
-template <> __device__ __forceinline__ float as_float<float>(float x) { return x; }
-template <> __device__ __forceinline__ float as_float<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
-template <typename T> __device__ __forceinline__ T from_float(float x);
-template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
-template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
-
 // ------------------------------------------------------------------------------------------------
 // append: one warp per (row, kv head); a row of K and a row of V, 16 bytes a lane
 // ------------------------------------------------------------------------------------------------
@@ -128,97 +121,6 @@ __global__ void __launch_bounds__(128) paged_append_kernel(const PagedParams P) 
     const T* from = static_cast<const T*>(is_v ? P.v : P.k) + src + e;
     T* to = static_cast<T*>(is_v ? P.v_pool : P.k_pool) + dst + e;
     *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(from);
-  }
-}
-
-// ------------------------------------------------------------------------------------------------
-// attention, plain: one warp per (row, query head), the lanes share a row's channels
-// ------------------------------------------------------------------------------------------------
-template <typename T, int D>
-__global__ void __launch_bounds__(128) paged_attend_kernel(const PagedParams P) {
-  griddep_wait();
-  const long long item = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
-  if (item >= (long long)P.rows * P.n_q_heads) return;
-  const int r = (int)(item / P.n_q_heads), hq = (int)(item % P.n_q_heads);
-  const int head = hq / (P.n_q_heads / P.n_kv_heads);
-  const int b = seq_of_row(P, r);
-  if (b < 0) return;
-  const SeqRows s = seq_rows(P, b);
-  if (P.q_start && (r < s.first || r >= s.first + s.n)) return;
-  constexpr int E = D / 32;
-  float q[E], acc[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    q[e] = as_float(static_cast<const T*>(P.q)[(long long)r * P.q_stride + (long long)hq * D + lane * E + e]) * P.scale_log2;
-    acc[e] = 0.f;
-  }
-  float m = -INFINITY, l = 0.f;
-  const int pos = s.len - s.n + (r - s.first);
-  if (s.n > 0) {
-    const int lo = P.window > 0 ? max(0, pos - P.window + 1) : 0;
-    for (int i = 0; i <= pos; ++i) {
-      if (i == min(P.sink, lo) && i < lo) i = lo;      // over the entries between the sinks and the window
-      const int pg = page_of(P, b, i);
-      if (pg < 0) continue;
-      const long long off = row_offset(P, pg, head, i, D) + lane * E;
-      float x = 0.f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) x = fmaf(q[e], as_float(static_cast<const T*>(P.k_pool)[off + e]), x);
-#pragma unroll
-      for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
-      const float mn = fmaxf(m, x), c = exp2f(m - mn), p = exp2f(x - mn);
-      l = l * c + p;
-#pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] = acc[e] * c + p * as_float(static_cast<const T*>(P.v_pool)[off + e]);
-      m = mn;
-    }
-  }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
-#pragma unroll
-  for (int e = 0; e < E; ++e)
-    static_cast<T*>(P.out)[((long long)r * P.n_q_heads + hq) * D + lane * E + e] = from_float<T>(acc[e] * inv);
-  if (P.lse && lane == 0) P.lse[(long long)r * P.n_q_heads + hq] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
-}
-
-// ------------------------------------------------------------------------------------------------
-// accumulated weights, plain: one warp per (sequence, kv head, entry), over the call's tokens in order
-// ------------------------------------------------------------------------------------------------
-template <typename T, int D>
-__global__ void __launch_bounds__(128) paged_weights_kernel(const PagedParams P, int entries) {
-  griddep_wait();
-  const long long item = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
-  if (item >= (long long)P.batch * P.n_kv_heads * entries) return;
-  const int i = (int)(item % entries);
-  const int bh = (int)(item / entries), b = bh / P.n_kv_heads, head = bh % P.n_kv_heads;
-  const SeqRows s = seq_rows(P, b);
-  if (i >= s.len || s.n == 0) return;
-  const int pg = page_of(P, b, i);
-  if (pg < 0) return;
-  const int G = P.n_q_heads / P.n_kv_heads, old = s.len - s.n;
-  constexpr int E = D / 32;
-  float k[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e)
-    k[e] = as_float(static_cast<const T*>(P.k_pool)[row_offset(P, pg, head, i, D) + lane * E + e]) * P.scale_log2;
-  float sum = 0.f;
-  for (int t = max(0, i - old); t < s.n; ++t) {
-    if (!visible(i, old + t, P.window, P.sink)) continue;
-    const long long r = s.first + t;
-    for (int g = 0; g < G; ++g) {
-      const int hq = head * G + g;
-      float x = 0.f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) x = fmaf(k[e], as_float(static_cast<const T*>(P.q)[r * P.q_stride + (long long)hq * D + lane * E + e]), x);
-#pragma unroll
-      for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
-      sum += exp2f(x - P.lse[r * P.n_q_heads + hq] * kLog2e);
-    }
-  }
-  if (lane == 0) {
-    float* a = P.scores + (long long)bh * P.score_stride + i;
-    *a = (P.k && i >= old ? 0.f : *a) + sum / (float)G;
   }
 }
 

@@ -13,6 +13,7 @@
 #include "wkv_paged.cuh"
 #include "wkv_paged_decode.cuh"
 #include "wkv_paged_prefill.cuh"
+#include "wkv_paged_f32.cuh"
 
 struct wkv_paged {
   wkv_paged_config cfg;
@@ -35,7 +36,7 @@ struct wkv_paged {
   float* part = nullptr;
   float2* part_ml = nullptr;
   uint32_t* arrived = nullptr;
-  // prompts on bf16 rows: the runs' outputs, next item
+  // prompts: the runs' outputs, next item
   float* run_part = nullptr;
   float2* run_ml = nullptr;
   uint32_t* item_counter = nullptr;
@@ -156,6 +157,12 @@ int encode_queries(wkv_paged* c, unsigned char* out128, const wkv::PagedParams& 
                     {elems, G, 128u / G, 1u});
 }
 
+// Rows of partial outputs that the runs of a prompt call may have: two row blocks per SM on bf16 rows, eight of the smaller ones on
+// fp32 rows.
+size_t run_rows(const wkv_paged* c) {
+  return (size_t)c->sm_count * (c->cfg.dtype == WKV_BF16 ? 2 * wkv::kPrefillRows : 8 * wkv::kF32Rows);
+}
+
 // Picks this handle's instantiations and how many decode CTAs the GPU holds at once.
 template <typename T, int D, int G>
 cudaError_t pick_kernels(wkv_paged* c) {
@@ -167,6 +174,10 @@ cudaError_t pick_kernels(wkv_paged* c) {
   int per_sm = 0;
   if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, wkv::kDecodeThreads, c->decode_smem);
   c->decode_ctas = c->sm_count * (per_sm < 1 ? 1 : per_sm);
+  if constexpr (sizeof(T) == 4) {
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(wkv::paged_prefill_f32_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, wkv::F32Shape<D>::kSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(wkv::paged_weights_f32_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, wkv::F32Shape<D>::kWeightsSmem);
+  }
   if constexpr (sizeof(T) == 2) {
     if (e == cudaSuccess)
       e = cudaFuncSetAttribute(wkv::paged_prefill_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, wkv::PrefillShape<D>::kSmem);
@@ -266,30 +277,35 @@ int decode(wkv_paged* c, const wkv::PagedParams& A) {
   return WKV_OK;
 }
 
-// Prompt attention on bf16 rows (tensor cores) ...
-constexpr int kMaxRuns = 2;            // per SM, over all row blocks
-template <int D>
-int prefill_bf16(wkv_paged* c, const wkv::PagedParams& A) {
-  wkv::PrefillParams P;
+// What the prompt kernels share: row blocks of ROWS rows, and runs of the key tiles -- as many as the SMs can use when the row
+// blocks alone are fewer, at least `least` entries each.
+int prefill_params(wkv_paged* c, wkv::PrefillParams& P, const wkv::PagedParams& A, int rows, long long least, long long* units) {
   std::memset(&P, 0, sizeof(P));
   P.A = A;
   P.g_shift = c->group == 1 ? 0 : c->group == 2 ? 1 : c->group == 4 ? 2 : 3;
-  const long long units = (((long long)A.rows * c->group >> 8) + A.batch) * A.n_kv_heads;
-  // Runs of the key tiles: as many as the SMs can use when the row blocks alone are fewer, at least four tiles each.
-  const long long tiles = ((long long)A.width * A.page + wkv::kPrefillKeys - 1) / wkv::kPrefillKeys;
-  P.splits = (int)std::max<long long>(1, std::min<long long>(kMaxRuns * c->sm_count / units, tiles / 4));
-  if (units * P.splits > 0x3fffffff) return fail(c, WKV_ERR_INVALID, "total_q * n_q_heads is too large");
-  P.items = (int)(units * P.splits);
+  *units = ((long long)A.rows * c->group / rows + A.batch) * A.n_kv_heads;
+  const long long most = run_rows(c) / rows;
+  P.splits = (int)std::max<long long>(1, std::min<long long>(most / *units, (long long)A.width * A.page / least));
+  if (*units * P.splits > 0x3fffffff) return fail(c, WKV_ERR_INVALID, "total_q * n_q_heads is too large");
+  P.items = (int)(*units * P.splits);
   P.counter = c->item_counter; P.part = c->run_part; P.part_ml = c->run_ml;
   P.oob_chunk = c->cfg.n_layers * c->cfg.n_pages * c->cfg.n_kv_heads;
   P.chunk0 = chunk0(c, A);
-  const int rc = encode_queries(c, P.qmap, A);
+  return WKV_OK;
+}
+
+// Prompt attention on bf16 rows (tensor cores) ...
+template <int D>
+int prefill_bf16(wkv_paged* c, const wkv::PagedParams& A) {
+  wkv::PrefillParams P;
+  long long units;
+  int rc = prefill_params(c, P, A, wkv::kPrefillRows, 4 * wkv::kPrefillKeys, &units);
+  if (rc == WKV_OK) rc = encode_queries(c, P.qmap, A);
   if (rc != WKV_OK) return rc;
   std::memcpy(P.kmap, c->part_kmap, 128);
   std::memcpy(P.vmap, c->part_vmap, 128);
-  constexpr int smem = wkv::PrefillShape<D>::kSmem;
-  WKV_CUDA(c, launch(c, wkv::paged_prefill_kernel<D>, std::min(P.items, c->sm_count), wkv::kPrefillThreads, smem, P));
-  if (P.splits > 1) WKV_CUDA(c, launch(c, wkv::paged_prefill_join_kernel<D>, units * 8, 256, 0, P));
+  WKV_CUDA(c, launch(c, wkv::paged_prefill_kernel<D>, std::min(P.items, c->sm_count), wkv::kPrefillThreads, wkv::PrefillShape<D>::kSmem, P));
+  if (P.splits > 1) WKV_CUDA(c, launch(c, wkv::paged_prefill_join_kernel<__nv_bfloat16, D, wkv::kPrefillRows>, units * (wkv::kPrefillRows / 32), 256, 0, P));
   if (A.scores) {
     const long long blocks = ((long long)A.width * A.page + 255) / 256;
     WKV_CUDA(c, launch(c, wkv::paged_weights_tc_kernel<D>, blocks * A.batch * A.n_kv_heads, wkv::kWeightsThreads, wkv::WeightsShape<D>::kSmem, P));
@@ -298,11 +314,16 @@ int prefill_bf16(wkv_paged* c, const wkv::PagedParams& A) {
 }
 // ... and on fp32 rows.
 template <int D>
-int prefill_f32(wkv_paged* c, const wkv::PagedParams& P) {
-  WKV_CUDA(c, launch(c, wkv::paged_attend_kernel<float, D>, ((long long)P.rows * P.n_q_heads + 3) / 4, 128, 0, P));
-  if (P.scores) {
-    const int entries = P.width * P.page;
-    WKV_CUDA(c, launch(c, wkv::paged_weights_kernel<float, D>, ((long long)P.batch * P.n_kv_heads * entries + 3) / 4, 128, 0, P, entries));
+int prefill_f32(wkv_paged* c, const wkv::PagedParams& A) {
+  wkv::PrefillParams P;
+  long long units;
+  const int rc = prefill_params(c, P, A, wkv::kF32Rows, 4 * wkv::kF32Keys, &units);
+  if (rc != WKV_OK) return rc;
+  WKV_CUDA(c, launch(c, wkv::paged_prefill_f32_kernel<D>, P.items, wkv::kF32Threads, wkv::F32Shape<D>::kSmem, P));
+  if (P.splits > 1) WKV_CUDA(c, launch(c, wkv::paged_prefill_join_kernel<float, D, wkv::kF32Rows>, units * (wkv::kF32Rows / 32), 256, 0, P));
+  if (A.scores) {
+    const long long blocks = ((long long)A.width * A.page + wkv::kF32Rows - 1) / wkv::kF32Rows;
+    WKV_CUDA(c, launch(c, wkv::paged_weights_f32_kernel<D>, blocks * A.batch * A.n_kv_heads, wkv::kF32Threads, wkv::F32Shape<D>::kWeightsSmem, P));
   }
   return WKV_OK;
 }
@@ -361,11 +382,9 @@ int wkv_paged_create(const wkv_paged_config* cfg, wkv_paged** out) {
   WKV_TAKE(&c->part, ((size_t)c->decode_ctas + lanes) * c->group * cfg->head_dim * 4);
   WKV_TAKE(&c->part_ml, ((size_t)c->decode_ctas + lanes) * c->group * 8);
   WKV_TAKE(&c->arrived, lanes * 4);
-  if (cfg->dtype == WKV_BF16) {
-    WKV_TAKE(&c->run_part, (size_t)kMaxRuns * c->sm_count * 256 * cfg->head_dim * 4);
-    WKV_TAKE(&c->run_ml, (size_t)kMaxRuns * c->sm_count * 256 * 8);
-    WKV_TAKE(&c->item_counter, 4);
-  }
+  WKV_TAKE(&c->run_part, run_rows(c) * cfg->head_dim * 4);
+  WKV_TAKE(&c->run_ml, run_rows(c) * 8);
+  WKV_TAKE(&c->item_counter, 4);
   const bool own_pools = !c->k_pool;
   if (own_pools) {
     WKV_TAKE(&c->k_pool, pool);
@@ -375,7 +394,7 @@ int wkv_paged_create(const wkv_paged_config* cfg, wkv_paged** out) {
   if (rc == WKV_OK) {
     e = cudaMemsetAsync(c->status, 0, 4, c->stream);
     if (e == cudaSuccess) e = cudaMemsetAsync(c->arrived, 0, lanes * 4, c->stream);
-    if (e == cudaSuccess && c->item_counter) e = cudaMemsetAsync(c->item_counter, 0, 4, c->stream);
+    if (e == cudaSuccess) e = cudaMemsetAsync(c->item_counter, 0, 4, c->stream);
     if (e == cudaSuccess && own_pools) e = cudaMemsetAsync(c->k_pool, 0, pool, c->stream);
     if (e == cudaSuccess && own_pools) e = cudaMemsetAsync(c->v_pool, 0, pool, c->stream);
     if (e != cudaSuccess) rc = WKV_ERR_CUDA;

@@ -27,6 +27,7 @@ namespace wkv {
 // Three warpgroups of 168 registers a thread at launch; the softmax ones hold a row of logits (128) and take what the third
 // does not need: 2 * 208 + 88 = 3 * 168.
 constexpr int kPrefillThreads = 384;
+constexpr int kPrefillRows = 256;            // rows of an item
 constexpr int kPrefillKeys = 128;            // entries per tile
 
 struct PrefillParams {
@@ -65,7 +66,7 @@ __device__ __forceinline__ void tensor_g2s_4d(void* dst, const void* tmap, int x
 struct PrefillBlock {
   int b, head, first, n, len, old;      // old: entries before the chunk
   int row0;                             // first row (token * G + g) of the block
-  int sink_rows, start, tiles;          // sink_rows, start: multiples of the page
+  int sink_rows, start, entries;        // sink_rows, start: multiples of the page; entries walked
   __device__ __forceinline__ int entry(int i) const { return i < sink_rows ? i : i - sink_rows + start; }
 };
 // Positions of a row tile's first and last token; none if it has no rows.
@@ -96,7 +97,8 @@ __device__ __forceinline__ bool tile_whole(const PrefillBlock& B, const RowTile&
   return e0 + kPrefillKeys - 1 <= t.pos_lo && (window == 0 || e0 >= t.pos_hi - window + 1 || e0 + kPrefillKeys <= sink);
 }
 
-// The rb-th row block (256 rows) over all sequences; false if there is none.  Every warp searches for itself.
+// The rb-th block of ROWS rows over all sequences; false if there is none.  Every warp searches for itself.
+template <int ROWS>
 __device__ __forceinline__ bool find_block(const PagedParams& A, int g_shift, int rb, int head, PrefillBlock& B) {
   const int lane = threadIdx.x & 31;
   int before = 0;
@@ -105,7 +107,7 @@ __device__ __forceinline__ bool find_block(const PagedParams& A, int g_shift, in
     int n = 0;
     if (b < A.batch) {
       const int lo = min(max(A.q_start[b], 0), A.rows), hi = min(max(A.q_start[b + 1], lo), A.rows);
-      n = (int)((((long long)(hi - lo) << g_shift) + 255) >> 8);
+      n = (int)((((long long)(hi - lo) << g_shift) + ROWS - 1) / ROWS);
     }
     int upto = n;
 #pragma unroll
@@ -119,13 +121,13 @@ __device__ __forceinline__ bool find_block(const PagedParams& A, int g_shift, in
       const int blocks = __shfl_sync(~0u, n, at), skipped = before + __shfl_sync(~0u, upto, at) - blocks;
       const SeqRows s = seq_rows(A, base + at);
       B.b = base + at; B.head = head; B.first = s.first; B.n = s.n; B.len = s.len; B.old = s.len - s.n;
-      B.row0 = (blocks - 1 - (rb - skipped)) << 8;     // a sequence's last rows see most: they start first
+      B.row0 = (blocks - 1 - (rb - skipped)) * ROWS;   // a sequence's last rows see most: they start first
       const int p0 = B.old + (B.row0 >> g_shift);                              // positions of the block's tokens
-      const int p1 = min(B.old + ((B.row0 + 255) >> g_shift), B.len - 1);
+      const int p1 = min(B.old + ((B.row0 + ROWS - 1) >> g_shift), B.len - 1);
       const int lo_key = A.window > 0 ? max(0, p0 - A.window + 1) : 0;
       B.start = lo_key & ~(A.page - 1);
       B.sink_rows = (min(A.sink, B.start) + A.page - 1) & ~(A.page - 1);
-      B.tiles = p1 < 0 ? 0 : (B.sink_rows + p1 + 1 - B.start + kPrefillKeys - 1) / kPrefillKeys;
+      B.entries = p1 < 0 ? 0 : B.sink_rows + p1 + 1 - B.start;
       return true;
     }
     before += __shfl_sync(~0u, upto, 31);
@@ -248,9 +250,10 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
             break;
           }
           const int split = w % P.splits, unit = w / P.splits;
-          if (!find_block(A, P.g_shift, unit / A.n_kv_heads, unit % A.n_kv_heads, item.B)) continue;     // `items` is an upper bound
-          item.v0 = item.B.tiles * split / P.splits;
-          item.v1 = item.B.tiles * (split + 1) / P.splits;
+          if (!find_block<kPrefillRows>(A, P.g_shift, unit / A.n_kv_heads, unit % A.n_kv_heads, item.B)) continue;     // `items` is an upper bound
+          const int tiles = (item.B.entries + kPrefillKeys - 1) / kPrefillKeys;
+          item.v0 = (int)((long long)tiles * split / P.splits);
+          item.v1 = (int)((long long)tiles * (split + 1) / P.splits);
           item.slot = (int)w;
           break;
         }
@@ -549,23 +552,25 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
   }
 }
 
-// The runs of a row block joined: eight threads per row, 32 rows per CTA.
-template <int D>
+// The runs of a row block (ROWS rows) joined: eight threads per row, 32 rows per CTA.
+template <typename T, int D, int ROWS>
 __global__ void __launch_bounds__(256) paged_prefill_join_kernel(const __grid_constant__ PrefillParams P) {
+  griddep_launch();
   griddep_wait();
   const PagedParams& A = P.A;
-  const int unit = blockIdx.x >> 3, G = 1 << P.g_shift;
+  const int unit = blockIdx.x / (ROWS / 32), G = 1 << P.g_shift;
   PrefillBlock B;
-  if (!find_block(A, P.g_shift, unit / A.n_kv_heads, unit % A.n_kv_heads, B)) return;
-  const int row = (blockIdx.x & 7) * 32 + (threadIdx.x >> 3), R = B.row0 + row, c0 = threadIdx.x & 7;
+  if (!find_block<ROWS>(A, P.g_shift, unit / A.n_kv_heads, unit % A.n_kv_heads, B)) return;
+  const int row = blockIdx.x % (ROWS / 32) * 32 + (threadIdx.x >> 3), R = B.row0 + row, c0 = threadIdx.x & 7;
   if (R >= B.n << P.g_shift) return;
+  const long long at0 = (long long)unit * P.splits * ROWS + row;
   float m = -INFINITY;
-  for (int s = 0; s < P.splits; ++s) m = fmaxf(m, P.part_ml[((long long)unit * P.splits + s) * 256 + row].x);
+  for (int s = 0; s < P.splits; ++s) m = fmaxf(m, P.part_ml[at0 + (long long)s * ROWS].x);
   constexpr int V = D / 32;                                       // float4s per thread
   float4 acc[V] = {};
   float l = 0.f;
   for (int s = 0; s < P.splits; ++s) {
-    const long long at = ((long long)unit * P.splits + s) * 256 + row;
+    const long long at = at0 + (long long)s * ROWS;
     const float2 ml = P.part_ml[at];
     if (ml.x == -INFINITY) continue;                              // a run that the row sees nothing of wrote no output
     const float f = exp2_fast(ml.x - m);
@@ -579,10 +584,13 @@ __global__ void __launch_bounds__(256) paged_prefill_join_kernel(const __grid_co
   const bool seen = !(l <= 0.f);
   const float inv = seen ? 1.f / l : 0.f;
   const long long tok = B.first + (R >> P.g_shift), hq = B.head * G + (R & (G - 1));
-  __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + (tok * A.n_q_heads + hq) * D;
+  T* out = static_cast<T*>(A.out) + (tok * A.n_q_heads + hq) * D;
 #pragma unroll
-  for (int i = 0; i < V; ++i)
-    reinterpret_cast<uint2*>(out)[i * 8 + c0] = make_uint2(pack_bf16(acc[i].x * inv, acc[i].y * inv), pack_bf16(acc[i].z * inv, acc[i].w * inv));
+  for (int i = 0; i < V; ++i) {
+    const float4 y = make_float4(acc[i].x * inv, acc[i].y * inv, acc[i].z * inv, acc[i].w * inv);
+    if constexpr (sizeof(T) == 2) reinterpret_cast<uint2*>(out)[i * 8 + c0] = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
+    else reinterpret_cast<float4*>(out)[i * 8 + c0] = y;
+  }
   if (A.lse && c0 == 0) A.lse[tok * A.n_q_heads + hq] = seen ? (m + log2f(l)) * kLn2 : -INFINITY;
 }
 
