@@ -152,30 +152,43 @@ __device__ __forceinline__ uint32_t score_key(float x) {
 }
 
 constexpr int kSelectThreads = 1024;
+constexpr int kSelectStaged = 32768;   // lanes of up to so many entries are read into shared memory once
 constexpr int kBitmapWords = 8192;     // pages per round of the overlap check: 32 times that
+constexpr int kSelectBins = 2048;
 
-__device__ __forceinline__ int block_sum(int x, int* scratch) {
-  x = __reduce_add_sync(~0u, x);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = x;
-  __syncthreads();
-  return __reduce_add_sync(~0u, scratch[threadIdx.x & 31]);
-}
-
-// One CTA per (sequence, kv head): which entries stay, in order.
-__global__ void __launch_bounds__(kSelectThreads) paged_select_kernel(const EvictParams P) {
-  __shared__ uint32_t bitmap[kBitmapWords];
-  __shared__ int scratch[32], warp_count[32];
+// Which entries stay, in order: one CTA per (sequence, kv head).  The `leave`-th smallest key among the entries that may leave is
+// found by three rounds of counting digits of 11, 11 and 10 bits (increments by one of shared counters: lanes that meet on one
+// counter are taken together, so the few exponents that scores have cost little).  Ties and places: a warp owns a contiguous run of
+// entries, so they need one exchange of the warps' totals, and ballots.  All counts are whole numbers: the same result every time.
+// Latency bound, about 12000 cycles for 32768 entries; a bit-by-bit search of 32 rounds took 68 us there.
+__global__ void __launch_bounds__(kSelectThreads) paged_select_kernel(const EvictParams P, int staged) {
+  extern __shared__ __align__(16) float stage[];        // [staged] scores, where they fit
+  __shared__ uint32_t bitmap[kBitmapWords];             // overlap check, then the digit counters
+  __shared__ int warp_sum[32], warp_below[32], warp_equal[32], found[2];
   griddep_launch();
   griddep_wait();
-  const int bh = blockIdx.x, b = bh / P.n_kv_heads, head = bh % P.n_kv_heads, tid = threadIdx.x;
+  const int bh = blockIdx.x, b = bh / P.n_kv_heads, head = bh % P.n_kv_heads, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int raw = P.seq_lens[b];
   const long long most = (long long)P.src_width << P.page_shift;
   const int len = raw < 0 ? 0 : raw > most ? (int)most : raw;
-  bool bad = len != raw;
+  const float* x = P.scores + (long long)bh * P.score_stride;
   const int left = min(len, P.budget), leave = len - left;
-  const int n_src = (len + P.page - 1) >> P.page_shift, n_dst = (left + P.page - 1) >> P.page_shift;
+  const int lo = min(P.sink, len), hi = max(lo, len - P.recent);      // entries that may leave
+  const bool in_stage = len <= staged;
+  if (in_stage && leave > 0) {
+    int i = tid;
+    for (; i + 7 * kSelectThreads < len; i += 8 * kSelectThreads) {
+      float y[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y[k] = x[i + k * kSelectThreads];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) stage[i + k * kSelectThreads] = y[k];
+    }
+    for (; i < len; i += kSelectThreads) stage[i] = x[i];
+  }
   // does the sequence move into pages that it lies in?
+  bool bad = len != raw;
+  const int n_src = (len + P.page - 1) >> P.page_shift, n_dst = (left + P.page - 1) >> P.page_shift;
   bool overlap = false;
   for (int base = 0; base < P.n_pages; base += kBitmapWords * 32) {
     const int words = min(kBitmapWords, (P.n_pages - base + 31) / 32);
@@ -194,9 +207,8 @@ __global__ void __launch_bounds__(kSelectThreads) paged_select_kernel(const Evic
       const unsigned at = (unsigned)pg - base;
       if ((unsigned)pg < (unsigned)P.n_pages && at < (unsigned)words * 32 && (bitmap[at >> 5] >> (at & 31) & 1)) overlap = true;
     }
-    __syncthreads();
+    overlap = __syncthreads_or(overlap);
   }
-  overlap = __syncthreads_or(overlap);
   if (tid == 0) {
     if (head == 0) P.new_lens[b] = overlap ? len : left;
     P.n_moved[bh] = overlap ? 0 : left;
@@ -204,74 +216,111 @@ __global__ void __launch_bounds__(kSelectThreads) paged_select_kernel(const Evic
   if (bad || (overlap && tid == 0)) flag_bad_table(P.status);
   if (overlap) return;
 
-  const float* x = P.scores + (long long)bh * P.score_stride;
-  const int lo = min(P.sink, len), hi = max(lo, len - P.recent);      // entries that may leave
-  // The `leave`-th smallest key, bit by bit from the top: threshold = the largest t with fewer than `leave` keys below it.
-  uint32_t threshold = 0;
-  int below = 0;                       // keys < threshold
-  if (leave > 0) {
-    for (int bit = 31; bit >= 0; --bit) {
-      const uint32_t t = threshold | (1u << bit);
-      int c = 0;
-      for (int i = lo + tid; i < hi; i += kSelectThreads) c += score_key(x[i]) < t;
-      c = block_sum(c, scratch);
-      if (c < leave) { threshold = t; below = c; }
+  int32_t* kept = P.kept + (long long)bh * P.kept_stride;
+  float* scores_out = P.scores_out ? P.scores_out + (long long)bh * P.out_stride : nullptr;
+  if (leave == 0) {
+    for (int i = tid; i < len; i += kSelectThreads) {
+      kept[i] = i;
+      if (scores_out) scores_out[i] = x[i];
     }
+    return;
   }
-  const int ties = leave - below;      // of the keys equal to the threshold the first `ties` leave
-  int stay = 0, equal = 0;             // so far
-  for (int base = 0; base < len; base += kSelectThreads) {
-    const int i = base + tid;
-    const bool in = i < len, may = in && leave > 0 && i >= lo && i < hi;
-    const float xi = in ? x[i] : 0.f;
-    const uint32_t key = score_key(xi);
-    const bool eq = may && key == threshold;
-    // rank among the equal ones
-    const uint32_t eqs = __ballot_sync(~0u, eq);
-    if ((tid & 31) == 0) warp_count[tid >> 5] = __popc(eqs);
+  const float* src = in_stage ? stage : x;
+  uint32_t threshold = 0;              // the `leave`-th smallest key, its digits found so far
+  int rank = leave;                    // its rank among the keys with these digits
+  for (int round = 0; round < 3; ++round) {
+    const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, bits = round == 2 ? 10 : 11;
+    for (int w = tid; w < kSelectBins; w += kSelectThreads) bitmap[w] = 0;
     __syncthreads();
-    const int wc = warp_count[tid & 31];
-    const int before = __reduce_add_sync(~0u, (tid & 31) < (tid >> 5) ? wc : 0), all = __reduce_add_sync(~0u, wc);
-    const int rank = equal + before + __popc(eqs & ((1u << (tid & 31)) - 1));
-    equal += all;
-    const bool keep = in && !(may && (key < threshold || (eq && rank < ties)));
-    __syncthreads();
-    const uint32_t ks = __ballot_sync(~0u, keep);
-    if ((tid & 31) == 0) warp_count[tid >> 5] = __popc(ks);
-    __syncthreads();
-    const int kc = warp_count[tid & 31];
-    const int kbefore = __reduce_add_sync(~0u, (tid & 31) < (tid >> 5) ? kc : 0), kall = __reduce_add_sync(~0u, kc);
-    if (keep) {
-      const int at = stay + kbefore + __popc(ks & ((1u << (tid & 31)) - 1));
-      P.kept[(long long)bh * P.kept_stride + at] = i;
-      if (P.scores_out) P.scores_out[(long long)bh * P.out_stride + at] = xi;
+    for (int i = lo + tid; i < hi; i += kSelectThreads) {
+      const uint32_t key = score_key(src[i]);
+      if ((uint64_t)key >> (shift + bits) == threshold) atomicAdd(&bitmap[key >> shift & ((1u << bits) - 1)], 1u);
     }
-    stay += kall;
     __syncthreads();
+    const int c0 = bitmap[2 * tid], c1 = bitmap[2 * tid + 1];
+    int upto = c0 + c1;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int y = __shfl_up_sync(~0u, upto, off);
+      if (lane >= off) upto += y;
+    }
+    if (lane == 31) warp_sum[warp] = upto;
+    __syncthreads();
+    upto += __reduce_add_sync(~0u, lane < warp ? warp_sum[lane] : 0);
+    const int before1 = upto - c1, before0 = before1 - c0;
+    if (before0 < rank && rank <= before1) { found[0] = 2 * tid; found[1] = before0; }
+    if (before1 < rank && rank <= upto) { found[0] = 2 * tid + 1; found[1] = before1; }
+    __syncthreads();
+    threshold = threshold << bits | (uint32_t)found[0];
+    rank -= found[1];
+    __syncthreads();
+  }
+  const int ties = rank;               // of the keys equal to the threshold so many leave, the first ones
+  // a warp's entries: `run` times 32 in a row
+  const int run = (len + kSelectThreads - 1) / kSelectThreads, first = warp * run * 32;
+  int wb = 0, we = 0;
+  for (int j = 0; j < run; ++j) {
+    const int i = first + j * 32 + lane;
+    const bool may = i >= lo && i < hi;
+    const uint32_t key = may ? score_key(src[i]) : 0u;
+    wb += __popc(__ballot_sync(~0u, may && key < threshold));
+    we += __popc(__ballot_sync(~0u, may && key == threshold));
+  }
+  if (lane == 0) { warp_below[warp] = wb; warp_equal[warp] = we; }
+  __syncthreads();
+  int equal = __reduce_add_sync(~0u, lane < warp ? warp_equal[lane] : 0);                        // before this warp's entries
+  int at = min(first, len) - __reduce_add_sync(~0u, lane < warp ? warp_below[lane] : 0) - min(equal, ties);
+  for (int j = 0; j < run; ++j) {
+    const int i = first + j * 32 + lane;
+    const uint32_t before = (1u << lane) - 1;
+    const bool may = i >= lo && i < hi;
+    const float xi = i < len ? src[i] : 0.f;
+    const uint32_t key = score_key(xi);
+    const uint32_t eqs = __ballot_sync(~0u, may && key == threshold);
+    const bool leaves = may && (key < threshold || (key == threshold && equal + __popc(eqs & before) < ties));
+    const bool keep = i < len && !leaves;
+    const uint32_t ks = __ballot_sync(~0u, keep);
+    if (keep) {
+      const int to = at + __popc(ks & before);
+      kept[to] = i;
+      if (scores_out) scores_out[to] = xi;
+    }
+    equal += __popc(eqs);
+    at += __popc(ks);
   }
 }
 
-// Rows of K and V to their new pages: half a warp per row, four entries in flight per warp.
+// Rows of K and V to their new pages, 16 bytes a step, kMoveSteps steps of a thread in flight together (the chain of loads in
+// front of each -- kept index, page, row -- is what takes the time).
+constexpr int kMoveThreads = 256, kMoveSteps = 4;
 template <typename T, int D>
-__global__ void __launch_bounds__(256) paged_move_kernel(const EvictParams P, int blocks_per_lane) {
+__global__ void __launch_bounds__(kMoveThreads) paged_move_kernel(const EvictParams P, int blocks_per_lane) {
   griddep_wait();
   const int bh = blockIdx.x / blocks_per_lane, part = blockIdx.x % blocks_per_lane;
   const int b = bh / P.n_kv_heads, head = bh % P.n_kv_heads, n = P.n_moved[bh];
   constexpr int kVec = 2 * D * (int)sizeof(T) / 16;    // 16-byte pieces of an entry: K row, then V row
   constexpr int kEach = 16 / (int)sizeof(T);
-  const long long total = (long long)n * kVec;
-  for (long long at = (long long)part * blockDim.x + threadIdx.x; at < total; at += (long long)blocks_per_lane * blockDim.x) {
+  const long long total = (long long)n * kVec, at0 = (long long)part * kMoveThreads * kMoveSteps + threadIdx.x;
+  uint4 piece[kMoveSteps];
+  T* to[kMoveSteps];
+#pragma unroll
+  for (int k = 0; k < kMoveSteps; ++k) {
+    const long long at = at0 + k * kMoveThreads;
+    to[k] = nullptr;
+    if (at >= total) continue;
     const int i = (int)(at / kVec), c = (int)(at % kVec);
     const int src = P.kept[(long long)bh * P.kept_stride + i];
     const int sp = P.src_table[(long long)b * P.src_width + (src >> P.page_shift)];
     const int dp = P.dst_table[(long long)b * P.dst_width + (i >> P.page_shift)];
     if ((unsigned)sp >= (unsigned)P.n_pages || (unsigned)dp >= (unsigned)P.n_pages) continue;
     const int e = (c % (kVec / 2)) * kEach;
-    const long long so = ((((long long)sp * P.n_kv_heads + head) << P.page_shift) + (src & (P.page - 1))) * D + e;
-    const long long to = ((((long long)dp * P.n_kv_heads + head) << P.page_shift) + (i & (P.page - 1))) * D + e;
     T* pool = static_cast<T*>(c < kVec / 2 ? P.k_pool : P.v_pool);
-    *reinterpret_cast<uint4*>(pool + to) = *reinterpret_cast<const uint4*>(pool + so);
+    piece[k] = __ldcs(reinterpret_cast<const uint4*>(pool + ((((long long)sp * P.n_kv_heads + head) << P.page_shift) + (src & (P.page - 1))) * D + e));
+    to[k] = pool + ((((long long)dp * P.n_kv_heads + head) << P.page_shift) + (i & (P.page - 1))) * D + e;
   }
+#pragma unroll
+  for (int k = 0; k < kMoveSteps; ++k)
+    if (to[k]) *reinterpret_cast<uint4*>(to[k]) = piece[k];
 }
 
 }  // namespace wkv

@@ -368,6 +368,8 @@ int wkv_paged_create(const wkv_paged_config* cfg, wkv_paged** out) {
   const size_t pool = (size_t)cfg->n_layers * cfg->n_pages * cfg->n_kv_heads * cfg->page_size * cfg->head_dim * c->elem;
   const size_t lanes = (size_t)cfg->max_batch * cfg->n_kv_heads, heads = (size_t)cfg->max_batch * cfg->n_q_heads;
   const bool wide = cfg->head_dim == 128;
+  e = cudaFuncSetAttribute(wkv::paged_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, wkv::kSelectStaged * 4);
+  if (e != cudaSuccess) { delete c; return WKV_ERR_CUDA; }
   if (cfg->dtype == WKV_BF16) e = wide ? pick_by_group<__nv_bfloat16, 128>(c) : pick_by_group<__nv_bfloat16, 64>(c);
   else e = wide ? pick_by_group<float, 128>(c) : pick_by_group<float, 64>(c);
   if (e != cudaSuccess) { delete c; return WKV_ERR_CUDA; }
@@ -497,13 +499,14 @@ int wkv_paged_evict(wkv_paged* c, int32_t layer, int32_t batch, const int32_t* s
   P.batch = batch; P.src_width = src_width; P.dst_width = dst_width; P.n_pages = f.n_pages; P.n_kv_heads = f.n_kv_heads;
   P.page = f.page_size; P.page_shift = c->page_shift; P.budget = budget; P.recent = recent; P.sink = sink;
   const long long lanes = (long long)batch * f.n_kv_heads;
-  cudaError_t e = launch(c, wkv::paged_select_kernel, lanes, wkv::kSelectThreads, 0, P);
+  const int staged = (int)std::min<int64_t>(most, wkv::kSelectStaged);
+  cudaError_t e = launch(c, wkv::paged_select_kernel, lanes, wkv::kSelectThreads, (size_t)staged * 4, P, staged);
   if (e == cudaSuccess) {
-    const int per_lane = (int)((left * 2 * f.head_dim * (int64_t)c->elem / 16 + 1023) / 1024);
+    const int per_lane = (int)((left * 2 * f.head_dim * (int64_t)c->elem / 16 + wkv::kMoveThreads * wkv::kMoveSteps - 1) / (wkv::kMoveThreads * wkv::kMoveSteps));
     const bool wide = f.head_dim == 128;
     auto kernel = f.dtype == WKV_BF16 ? (wide ? wkv::paged_move_kernel<__nv_bfloat16, 128> : wkv::paged_move_kernel<__nv_bfloat16, 64>)
                                       : (wide ? wkv::paged_move_kernel<float, 128> : wkv::paged_move_kernel<float, 64>);
-    e = launch(c, kernel, lanes * per_lane, 256, 0, P, per_lane);
+    e = launch(c, kernel, lanes * per_lane, wkv::kMoveThreads, 0, P, per_lane);
   }
   WKV_CUDA(c, e);
   return WKV_OK;

@@ -139,6 +139,15 @@ def test_evict_long(d, hk):
     _evict([9000], 700, 64, 4, hk=1, d=d, page=64, seed=2)
 
 
+def test_evict_past_the_register_form():
+    """Lanes around 32768 entries, where keys no longer fit registers, and beyond."""
+    _evict([32768, 32769, 40001], 33, 5, 2, hk=1, d=64, page=64, seed=6)
+
+    def few(x):
+        x.copy_((x * 5).floor())
+    _evict([40000, 32767], 20000, 50, 4, hk=1, d=64, page=64, seed=7, scores=few)
+
+
 def test_evict_ties_and_special_scores():
     def few(x):
         x.copy_((x * 3).floor())                    # many equal scores
