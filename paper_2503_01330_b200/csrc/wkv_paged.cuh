@@ -144,25 +144,35 @@ struct EvictParams {
   int batch, src_width, dst_width, n_pages, n_kv_heads, page, page_shift, budget, recent, sink;
 };
 
-// Order of eviction as an unsigned key: smaller score, smaller key; -0 like +0; NaN last.
+// Order of eviction as an unsigned key: smaller score, smaller key; -0 like +0; NaN last, but for the entries that stay anyway.
+constexpr uint32_t kKeyNan = 0xfffffffeu, kKeyStays = 0xffffffffu;
 __device__ __forceinline__ uint32_t score_key(float x) {
-  if (x != x) return 0xffffffffu;
   const uint32_t u = __float_as_uint(x + 0.f);
-  return u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
+  return x != x ? kKeyNan : u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
 constexpr int kSelectThreads = 1024;
 constexpr int kSelectStaged = 32768;   // lanes of up to so many entries are read into shared memory once
 constexpr int kBitmapWords = 8192;     // pages per round of the overlap check: 32 times that
-constexpr int kSelectBins = 2048;
+static_assert(kBitmapWords == 256 * 32, "a counter per digit and lane");
 
 // Which entries stay, in order: one CTA per (sequence, kv head).  The `leave`-th smallest key among the entries that may leave is
-// found by three rounds of counting digits of 11, 11 and 10 bits (increments by one of shared counters: lanes that meet on one
-// counter are taken together, so the few exponents that scores have cost little).  Ties and places: a warp owns a contiguous run of
+// found by four rounds of counting digits of 8 bits, a counter per digit and lane: scores share a few exponents, and lanes that met
+// on one counter would queue (33 us with one counter per digit of 11 bits).  Ties and places: a warp owns a contiguous run of
 // entries, so they need one exchange of the warps' totals, and ballots.  All counts are whole numbers: the same result every time.
-// Latency bound, about 12000 cycles for 32768 entries; a bit-by-bit search of 32 rounds took 68 us there.
+// Bound by instruction issue and latency: about 65 instructions per 32 entries.
+struct StagedKeys {
+  const uint32_t* key;
+  __device__ __forceinline__ uint32_t operator()(int i) const { return key[i]; }
+};
+struct GlobalKeys {
+  const float* x;
+  int lo, hi;
+  __device__ __forceinline__ uint32_t operator()(int i) const { return i >= lo && i < hi ? score_key(x[i]) : kKeyStays; }
+};
+
 __global__ void __launch_bounds__(kSelectThreads) paged_select_kernel(const EvictParams P, int staged) {
-  extern __shared__ __align__(16) float stage[];        // [staged] scores, where they fit
+  extern __shared__ __align__(16) uint32_t stage[];     // [staged] keys, where they fit
   __shared__ uint32_t bitmap[kBitmapWords];             // overlap check, then the digit counters
   __shared__ int warp_sum[32], warp_below[32], warp_equal[32], found[2];
   griddep_launch();
@@ -174,17 +184,19 @@ __global__ void __launch_bounds__(kSelectThreads) paged_select_kernel(const Evic
   const float* x = P.scores + (long long)bh * P.score_stride;
   const int left = min(len, P.budget), leave = len - left;
   const int lo = min(P.sink, len), hi = max(lo, len - P.recent);      // entries that may leave
-  const bool in_stage = len <= staged;
+  const int up = (len + kSelectThreads - 1) & ~(kSelectThreads - 1);  // whole passes of the CTA
+  const bool in_stage = up <= staged;
+  const GlobalKeys from_memory{x, lo, hi};
   if (in_stage && leave > 0) {
     int i = tid;
-    for (; i + 7 * kSelectThreads < len; i += 8 * kSelectThreads) {
-      float y[8];
+    for (; i + 7 * kSelectThreads < up; i += 8 * kSelectThreads) {
+      uint32_t y[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) y[k] = x[i + k * kSelectThreads];
+      for (int k = 0; k < 8; ++k) y[k] = from_memory(i + k * kSelectThreads);
 #pragma unroll
       for (int k = 0; k < 8; ++k) stage[i + k * kSelectThreads] = y[k];
     }
-    for (; i < len; i += kSelectThreads) stage[i] = x[i];
+    for (; i < up; i += kSelectThreads) stage[i] = from_memory(i);
   }
   // does the sequence move into pages that it lies in?
   bool bad = len != raw;
@@ -225,69 +237,74 @@ __global__ void __launch_bounds__(kSelectThreads) paged_select_kernel(const Evic
     }
     return;
   }
-  const float* src = in_stage ? stage : x;
-  uint32_t threshold = 0;              // the `leave`-th smallest key, its digits found so far
-  int rank = leave;                    // its rank among the keys with these digits
-  for (int round = 0; round < 3; ++round) {
-    const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, bits = round == 2 ? 10 : 11;
-    for (int w = tid; w < kSelectBins; w += kSelectThreads) bitmap[w] = 0;
-    __syncthreads();
-    for (int i = lo + tid; i < hi; i += kSelectThreads) {
-      const uint32_t key = score_key(src[i]);
-      if ((uint64_t)key >> (shift + bits) == threshold) atomicAdd(&bitmap[key >> shift & ((1u << bits) - 1)], 1u);
-    }
-    __syncthreads();
-    const int c0 = bitmap[2 * tid], c1 = bitmap[2 * tid + 1];
-    int upto = c0 + c1;
+  __shared__ uint32_t found_threshold;
+  auto select = [&](auto key_of) {
+    uint32_t threshold = 0;            // the `leave`-th smallest key, its digits found so far
+    int rank = leave;                  // its rank among the keys with these digits
 #pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const int y = __shfl_up_sync(~0u, upto, off);
-      if (lane >= off) upto += y;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+      for (int w = tid; w < kBitmapWords; w += kSelectThreads) bitmap[w] = 0;
+      __syncthreads();
+#pragma unroll 8
+      for (int i = tid; i < up; i += kSelectThreads) {
+        const uint32_t key = key_of(i);
+        if (shift == 24 || key >> (shift + 8 & 31) == threshold) atomicAdd(&bitmap[(key >> shift & 255) * 32 + lane], 1u);
+      }
+      __syncthreads();
+      // four threads per digit, eight counters each (rotated, so that they sit on different banks), then a scan over the digits
+      const int digit = tid >> 2;
+      int c = 0;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) c += bitmap[digit * 32 + (tid & 3) * 8 + ((k + digit) & 7)];
+      c += __shfl_xor_sync(~0u, c, 1);
+      c += __shfl_xor_sync(~0u, c, 2);
+      int upto = (tid & 3) == 3 ? c : 0;
+#pragma unroll
+      for (int off = 1; off < 32; off <<= 1) {
+        const int y = __shfl_up_sync(~0u, upto, off);
+        if (lane >= off) upto += y;
+      }
+      if (lane == 31) warp_sum[warp] = upto;
+      __syncthreads();
+      upto += __reduce_add_sync(~0u, lane < warp ? warp_sum[lane] : 0);
+      if ((tid & 3) == 3 && upto - c < rank && rank <= upto) { found_threshold = (uint32_t)digit; found[0] = upto - c; }
+      __syncthreads();
+      threshold = threshold << 8 | found_threshold;
+      rank -= found[0];
+      __syncthreads();
     }
-    if (lane == 31) warp_sum[warp] = upto;
+    const int ties = rank;             // of the keys equal to the threshold so many leave, the first ones
+    // a warp's entries: `run` times 32 in a row
+    const int run = up / kSelectThreads, first = warp * run * 32 + lane;
+    int wb = 0, we = 0;
+#pragma unroll 8
+    for (int j = 0; j < run; ++j) {
+      const uint32_t key = key_of(first + j * 32);
+      wb += __popc(__ballot_sync(~0u, key < threshold));
+      we += __popc(__ballot_sync(~0u, key == threshold));
+    }
+    if (lane == 0) { warp_below[warp] = wb; warp_equal[warp] = we; }
     __syncthreads();
-    upto += __reduce_add_sync(~0u, lane < warp ? warp_sum[lane] : 0);
-    const int before1 = upto - c1, before0 = before1 - c0;
-    if (before0 < rank && rank <= before1) { found[0] = 2 * tid; found[1] = before0; }
-    if (before1 < rank && rank <= upto) { found[0] = 2 * tid + 1; found[1] = before1; }
-    __syncthreads();
-    threshold = threshold << bits | (uint32_t)found[0];
-    rank -= found[1];
-    __syncthreads();
-  }
-  const int ties = rank;               // of the keys equal to the threshold so many leave, the first ones
-  // a warp's entries: `run` times 32 in a row
-  const int run = (len + kSelectThreads - 1) / kSelectThreads, first = warp * run * 32;
-  int wb = 0, we = 0;
-  for (int j = 0; j < run; ++j) {
-    const int i = first + j * 32 + lane;
-    const bool may = i >= lo && i < hi;
-    const uint32_t key = may ? score_key(src[i]) : 0u;
-    wb += __popc(__ballot_sync(~0u, may && key < threshold));
-    we += __popc(__ballot_sync(~0u, may && key == threshold));
-  }
-  if (lane == 0) { warp_below[warp] = wb; warp_equal[warp] = we; }
-  __syncthreads();
-  int equal = __reduce_add_sync(~0u, lane < warp ? warp_equal[lane] : 0);                        // before this warp's entries
-  int at = min(first, len) - __reduce_add_sync(~0u, lane < warp ? warp_below[lane] : 0) - min(equal, ties);
-  for (int j = 0; j < run; ++j) {
-    const int i = first + j * 32 + lane;
+    int equal = __reduce_add_sync(~0u, lane < warp ? warp_equal[lane] : 0);                        // before this warp's entries
+    int at = min(warp * run * 32, len) - __reduce_add_sync(~0u, lane < warp ? warp_below[lane] : 0) - min(equal, ties);
     const uint32_t before = (1u << lane) - 1;
-    const bool may = i >= lo && i < hi;
-    const float xi = i < len ? src[i] : 0.f;
-    const uint32_t key = score_key(xi);
-    const uint32_t eqs = __ballot_sync(~0u, may && key == threshold);
-    const bool leaves = may && (key < threshold || (key == threshold && equal + __popc(eqs & before) < ties));
-    const bool keep = i < len && !leaves;
-    const uint32_t ks = __ballot_sync(~0u, keep);
-    if (keep) {
-      const int to = at + __popc(ks & before);
-      kept[to] = i;
-      if (scores_out) scores_out[to] = xi;
+#pragma unroll 4
+    for (int j = 0; j < run; ++j) {
+      const int i = first + j * 32;
+      const uint32_t key = key_of(i), eqs = __ballot_sync(~0u, key == threshold);
+      const float xi = i < len && scores_out ? x[i] : 0.f;
+      const bool keep = i < len && (key > threshold || (key == threshold && equal + __popc(eqs & before) >= ties));
+      const uint32_t ks = __ballot_sync(~0u, keep);
+      if (keep) {
+        const int to = at + __popc(ks & before);
+        kept[to] = i;
+        if (scores_out) scores_out[to] = xi;
+      }
+      equal += __popc(eqs);
+      at += __popc(ks);
     }
-    equal += __popc(eqs);
-    at += __popc(ks);
-  }
+  };
+  if (in_stage) select(StagedKeys{stage}); else select(from_memory);
 }
 
 // Rows of K and V to their new pages, 16 bytes a step, kMoveSteps steps of a thread in flight together (the chain of loads in

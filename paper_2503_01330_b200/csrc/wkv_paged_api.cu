@@ -499,7 +499,7 @@ int wkv_paged_evict(wkv_paged* c, int32_t layer, int32_t batch, const int32_t* s
   P.batch = batch; P.src_width = src_width; P.dst_width = dst_width; P.n_pages = f.n_pages; P.n_kv_heads = f.n_kv_heads;
   P.page = f.page_size; P.page_shift = c->page_shift; P.budget = budget; P.recent = recent; P.sink = sink;
   const long long lanes = (long long)batch * f.n_kv_heads;
-  const int staged = (int)std::min<int64_t>(most, wkv::kSelectStaged);
+  const int staged = (int)std::min<int64_t>((most + wkv::kSelectThreads - 1) / wkv::kSelectThreads * wkv::kSelectThreads, wkv::kSelectStaged);
   cudaError_t e = launch(c, wkv::paged_select_kernel, lanes, wkv::kSelectThreads, (size_t)staged * 4, P, staged);
   if (e == cudaSuccess) {
     const int per_lane = (int)((left * 2 * f.head_dim * (int64_t)c->elem / 16 + wkv::kMoveThreads * wkv::kMoveSteps - 1) / (wkv::kMoveThreads * wkv::kMoveSteps));
