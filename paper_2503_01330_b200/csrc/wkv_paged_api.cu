@@ -317,7 +317,7 @@ template <int D>
 int prefill_f32(wkv_paged* c, const wkv::PagedParams& A) {
   wkv::PrefillParams P;
   long long units;
-  const int rc = prefill_params(c, P, A, wkv::kF32Rows, 4 * wkv::kF32Keys, &units);
+  const int rc = prefill_params(c, P, A, wkv::kF32Rows, 2 * wkv::kF32Keys, &units);
   if (rc != WKV_OK) return rc;
   WKV_CUDA(c, launch(c, wkv::paged_prefill_f32_kernel<D>, P.items, wkv::kF32Threads, wkv::F32Shape<D>::kSmem, P));
   if (P.splits > 1) WKV_CUDA(c, launch(c, wkv::paged_prefill_join_kernel<float, D, wkv::kF32Rows>, units * (wkv::kF32Rows / 32), 256, 0, P));

@@ -3,7 +3,8 @@
 //
 // Bound: fp32 FMAs, 4 D flops per (query head, visible entry).  A CTA of 128 threads owns 64 rows (token, query head) and walks
 // tiles of 32 entries: a thread computes 4 x 4 logits from 16-byte pieces in shared memory (8 loads for 64 FMAs) and 4 rows x D / 8
-// channels of the output (20 loads for 256 FMAs at D = 128).  Row statistics stay among the eight threads of a row.
+// channels of the output (20 loads for 256 FMAs at D = 128).  Row statistics stay among the eight threads of a row.  The next tile
+// is copied (cp.async, zeros where there is no row) while this one is worked on.
 #pragma once
 #include "wkv_paged.cuh"
 #include "wkv_paged_prefill.cuh"
@@ -18,8 +19,8 @@ template <int D>
 struct F32Shape {
   static constexpr int kStride = D + 4;                                     // rows on different banks
   static constexpr int kPStride = kF32Keys + 4;
-  static constexpr int kSmem = ((kF32Rows + kF32Keys) * kStride + kF32Keys * D + kF32Rows * kPStride) * 4;
-  static constexpr int kWeightsSmem = ((kF32Rows + kF32Keys) * kStride + kF32Keys) * 4;
+  static constexpr int kSmem = ((kF32Rows + 2 * kF32Keys) * kStride + 2 * kF32Keys * D + kF32Rows * kPStride) * 4;
+  static constexpr int kWeightsSmem = ((kF32Rows + 2 * kF32Keys) * kStride + 2 * kF32Keys) * 4;
 };
 
 // acc[i][j] = a[ty + 16 i] . b[tx + 8 j]
@@ -45,11 +46,13 @@ __device__ __forceinline__ void dot_tile(const float* a, const float* b, int ty,
   }
 }
 
-// Row r of a tile, by D / 4 threads: zeros where src is NULL.
-template <int D>
-__device__ __forceinline__ void stage_row(float* dst, const float* src, int c) {
-  *reinterpret_cast<float4*>(dst + c * 4) = src ? reinterpret_cast<const float4*>(src)[c] : make_float4(0.f, 0.f, 0.f, 0.f);
+// 16 bytes of a row into shared memory, asynchronously: zeros where src is NULL.
+__device__ __forceinline__ void stage_piece(float* dst, const float* src, const float* any) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src ? src : any), "r"(src ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void stage_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void stage_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 // Query row R = token * G + g of a row block.
 __device__ __forceinline__ const float* query_row(const PagedParams& A, int first, int n, int head, int g_shift, int R, int D) {
   const int tok = R >> g_shift;
@@ -62,9 +65,9 @@ __global__ void __launch_bounds__(kF32Threads) paged_prefill_f32_kernel(const __
   using Sh = F32Shape<D>;
   extern __shared__ __align__(16) float f32_smem[];
   float* sq = f32_smem;                                       // [64][kStride]
-  float* sk = sq + kF32Rows * Sh::kStride;                    // [32][kStride]
-  float* sv = sk + kF32Keys * Sh::kStride;                    // [32][D]
-  float* sp = sv + kF32Keys * D;                              // [64][kPStride]
+  float* sk = sq + kF32Rows * Sh::kStride;                    // [2][32][kStride]
+  float* sv = sk + 2 * kF32Keys * Sh::kStride;                // [2][32][D]
+  float* sp = sv + 2 * kF32Keys * D;                          // [64][kPStride]
   const PagedParams& A = P.A;
   griddep_launch();
   griddep_wait();
@@ -74,8 +77,29 @@ __global__ void __launch_bounds__(kF32Threads) paged_prefill_f32_kernel(const __
   const int tid = threadIdx.x, ty = tid >> 3, tx = tid & 7;
   const int tiles = (B.entries + kF32Keys - 1) / kF32Keys, v0 = (int)((long long)tiles * split / P.splits), v1 = (int)((long long)tiles * (split + 1) / P.splits);
   constexpr int kVec = D / 4, kRowsPerPass = kF32Threads / kVec;
-  for (int r = tid / kVec; r < kF32Rows; r += kRowsPerPass)
-    stage_row<D>(sq + r * Sh::kStride, query_row(A, B.first, B.n, B.head, P.g_shift, B.row0 + r, D), tid % kVec);
+  const int vec = tid % kVec;
+#pragma unroll 8
+  for (int r = tid / kVec; r < kF32Rows; r += kRowsPerPass) {
+    const float* q = query_row(A, B.first, B.n, B.head, P.g_shift, B.row0 + r, D);
+    stage_piece(sq + r * Sh::kStride + vec * 4, q ? q + vec * 4 : nullptr, static_cast<const float*>(A.q));
+  }
+  auto load_tile = [&](int v) {
+    const int buf = v & 1;
+#pragma unroll
+    for (int k = 0; k < kF32Keys / kRowsPerPass; ++k) {
+      const int r = tid / kVec + k * kRowsPerPass, at = v * kF32Keys + r, i = B.entry(at);
+      long long off = -1;
+      if (at < B.entries && i < B.len) {
+        const int pg = page_of(A, B.b, i);
+        if (pg >= 0) off = row_offset(A, pg, B.head, i, D) + vec * 4;
+      }
+      const float *kp = static_cast<const float*>(A.k_pool), *vp = static_cast<const float*>(A.v_pool);
+      stage_piece(sk + (buf * kF32Keys + r) * Sh::kStride + vec * 4, off < 0 ? nullptr : kp + off, kp);
+      stage_piece(sv + (buf * kF32Keys + r) * D + vec * 4, off < 0 ? nullptr : vp + off, vp);
+    }
+    stage_commit();
+  };
+  if (v0 < v1) load_tile(v0);
   constexpr int kPieces = D / 32;                             // float4s of a row that a thread accumulates: channels tx * 4 + 32 j
   float4 o[4][kPieces];
   float m[4], l[4];
@@ -90,19 +114,12 @@ __global__ void __launch_bounds__(kF32Threads) paged_prefill_f32_kernel(const __
   }
   for (int v = v0; v < v1; ++v) {
     __syncthreads();                                          // the tile before has been read
-    for (int r = tid / kVec; r < kF32Keys; r += kRowsPerPass) {
-      const int at = v * kF32Keys + r, i = B.entry(at);
-      long long off = -1;
-      if (at < B.entries && i < B.len) {
-        const int pg = page_of(A, B.b, i);
-        if (pg >= 0) off = row_offset(A, pg, B.head, i, D);
-      }
-      stage_row<D>(sk + r * Sh::kStride, off < 0 ? nullptr : static_cast<const float*>(A.k_pool) + off, tid % kVec);
-      stage_row<D>(sv + r * D, off < 0 ? nullptr : static_cast<const float*>(A.v_pool) + off, tid % kVec);
-    }
+    if (v + 1 < v1) load_tile(v + 1);
+    if (v + 1 < v1) stage_wait<1>(); else stage_wait<0>();
     __syncthreads();
+    const float *tk = sk + (v & 1) * kF32Keys * Sh::kStride, *tv = sv + (v & 1) * kF32Keys * D;
     float x[4][4];
-    dot_tile<D>(sq, sk, ty, tx, x);
+    dot_tile<D>(sq, tk, ty, tx, x);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float mx = m[i];
@@ -139,7 +156,7 @@ __global__ void __launch_bounds__(kF32Threads) paged_prefill_f32_kernel(const __
       for (int k = 0; k < 4; ++k)
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
-          const float4 y = *reinterpret_cast<const float4*>(sv + (e + k) * D + j * 32 + tx * 4);
+          const float4 y = *reinterpret_cast<const float4*>(tv + (e + k) * D + j * 32 + tx * 4);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float w = k == 0 ? p[i].x : k == 1 ? p[i].y : k == 2 ? p[i].z : p[i].w;
@@ -180,8 +197,8 @@ __global__ void __launch_bounds__(kF32Threads) paged_weights_f32_kernel(const __
   using Sh = F32Shape<D>;
   extern __shared__ __align__(16) float f32_smem[];
   float* sk = f32_smem;                                       // [64][kStride]
-  float* sq = sk + kF32Rows * Sh::kStride;                    // [32][kStride]
-  float* sl = sq + kF32Keys * Sh::kStride;                    // [32] base-2 log-sums
+  float* sq = sk + kF32Rows * Sh::kStride;                    // [2][32][kStride]
+  float* sl = sq + 2 * kF32Keys * Sh::kStride;                // [2][32] base-2 log-sums
   const PagedParams& A = P.A;
   griddep_launch();
   griddep_wait();
@@ -194,23 +211,38 @@ __global__ void __launch_bounds__(kF32Threads) paged_weights_f32_kernel(const __
   if (t_end <= t_lo) return;
   const int tile0 = (t_lo << gs) / kF32Keys, tile1 = (int)(((t_end << gs) + kF32Keys - 1) / kF32Keys);
   constexpr int kVec = D / 4, kRowsPerPass = kF32Threads / kVec;
+  const int vec = tid % kVec;
+#pragma unroll 8
   for (int r = tid / kVec; r < kF32Rows; r += kRowsPerPass) {
     const int i = e0 + r;
     const int pg = i < s.len ? page_of(A, b, i) : -1;
-    stage_row<D>(sk + r * Sh::kStride, pg < 0 ? nullptr : static_cast<const float*>(A.k_pool) + row_offset(A, pg, head, i, D), tid % kVec);
+    const float* kp = static_cast<const float*>(A.k_pool);
+    stage_piece(sk + r * Sh::kStride + vec * 4, pg < 0 ? nullptr : kp + row_offset(A, pg, head, i, D) + vec * 4, kp);
   }
+  auto load_tile = [&](int it) {
+    const int buf = it & 1;
+#pragma unroll
+    for (int k = 0; k < kF32Keys / kRowsPerPass; ++k) {
+      const int r = tid / kVec + k * kRowsPerPass;
+      const float* q = query_row(A, s.first, s.n, head, gs, it * kF32Keys + r, D);
+      stage_piece(sq + (buf * kF32Keys + r) * Sh::kStride + vec * 4, q ? q + vec * 4 : nullptr, static_cast<const float*>(A.q));
+    }
+    if (tid < kF32Keys) {
+      const int R = it * kF32Keys + tid, tok = R >> gs;
+      sl[buf * kF32Keys + tid] = tok < s.n ? A.lse[(long long)(s.first + tok) * A.n_q_heads + (head << gs) + (R & ((1 << gs) - 1))] * kLog2e : 0.f;
+    }
+    stage_commit();
+  };
+  load_tile(tile0);
   float total[4] = {0.f, 0.f, 0.f, 0.f};
   for (int it = tile0; it < tile1; ++it) {
     __syncthreads();
-    for (int r = tid / kVec; r < kF32Keys; r += kRowsPerPass)
-      stage_row<D>(sq + r * Sh::kStride, query_row(A, s.first, s.n, head, gs, it * kF32Keys + r, D), tid % kVec);
-    if (tid < kF32Keys) {
-      const int R = it * kF32Keys + tid, tok = R >> gs;
-      sl[tid] = tok < s.n ? A.lse[(long long)(s.first + tok) * A.n_q_heads + (head << gs) + (R & ((1 << gs) - 1))] * kLog2e : 0.f;
-    }
+    if (it + 1 < tile1) load_tile(it + 1);
+    if (it + 1 < tile1) stage_wait<1>(); else stage_wait<0>();
     __syncthreads();
+    const float *tq = sq + (it & 1) * kF32Keys * Sh::kStride, *tl = sl + (it & 1) * kF32Keys;
     float x[4][4];
-    dot_tile<D>(sk, sq, ty, tx, x);
+    dot_tile<D>(sk, tq, ty, tx, x);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int e = e0 + ty + 16 * i;
@@ -218,7 +250,7 @@ __global__ void __launch_bounds__(kF32Threads) paged_weights_f32_kernel(const __
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int R = it * kF32Keys + tx + 8 * j, tok = R >> gs;
-        if (tok < s.n && visible(e, old + tok, A.window, A.sink)) sum += exp2_fast(fmaf(x[i][j], A.scale_log2, -sl[tx + 8 * j]));
+        if (tok < s.n && visible(e, old + tok, A.window, A.sink)) sum += exp2_fast(fmaf(x[i][j], A.scale_log2, -tl[tx + 8 * j]));
       }
       total[i] += sum;
     }
