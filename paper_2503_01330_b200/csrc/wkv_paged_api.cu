@@ -323,7 +323,7 @@ int prefill_f32(wkv_paged* c, const wkv::PagedParams& A) {
   if (P.splits > 1) WKV_CUDA(c, launch(c, wkv::paged_prefill_join_kernel<float, D, wkv::kF32Rows>, units * (wkv::kF32Rows / 32), 256, 0, P));
   if (A.scores) {
     const long long blocks = ((long long)A.width * A.page + wkv::kF32Rows - 1) / wkv::kF32Rows;
-    WKV_CUDA(c, launch(c, wkv::paged_weights_f32_kernel<D>, blocks * A.batch * A.n_kv_heads, wkv::kF32Threads, wkv::F32Shape<D>::kWeightsSmem, P));
+    WKV_CUDA(c, launch(c, wkv::paged_weights_f32_kernel<D>, blocks * A.batch * A.n_kv_heads, wkv::kF32Groups * wkv::kF32Threads, wkv::F32Shape<D>::kWeightsSmem, P));
   }
   return WKV_OK;
 }

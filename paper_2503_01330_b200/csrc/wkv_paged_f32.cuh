@@ -14,13 +14,14 @@ namespace wkv {
 constexpr int kF32Rows = 64;
 constexpr int kF32Keys = 32;
 constexpr int kF32Threads = 128;
+constexpr int kF32Groups = 4;                // of the weights' kernel: 128 threads each
 
 template <int D>
 struct F32Shape {
   static constexpr int kStride = D + 4;                                     // rows on different banks
   static constexpr int kPStride = kF32Keys + 4;
   static constexpr int kSmem = ((kF32Rows + 2 * kF32Keys) * kStride + 2 * kF32Keys * D + kF32Rows * kPStride) * 4;
-  static constexpr int kWeightsSmem = ((kF32Rows + 2 * kF32Keys) * kStride + 2 * kF32Keys) * 4;
+  static constexpr int kWeightsSmem = (kF32Rows * kStride + kF32Groups * 2 * kF32Keys * (kStride + 1)) * 4;
 };
 
 // acc[i][j] = a[ty + 16 i] . b[tx + 8 j]
@@ -191,20 +192,23 @@ __global__ void __launch_bounds__(kF32Threads) paged_prefill_f32_kernel(const __
   }
 }
 
-// scores of 64 entries of one kv head, over all row tiles (32 rows) that see any of them, in order.
+// scores of 64 entries of one kv head, over all row tiles (32 rows) that see any of them: four groups of 128 threads take every
+// fourth tile each, so that an SM has 16 warps however few blocks of entries there are; their sums are added in the groups' order.
 template <int D>
-__global__ void __launch_bounds__(kF32Threads) paged_weights_f32_kernel(const __grid_constant__ PrefillParams P) {
+__global__ void __launch_bounds__(kF32Groups * kF32Threads) paged_weights_f32_kernel(const __grid_constant__ PrefillParams P) {
   using Sh = F32Shape<D>;
   extern __shared__ __align__(16) float f32_smem[];
   float* sk = f32_smem;                                       // [64][kStride]
-  float* sq = sk + kF32Rows * Sh::kStride;                    // [2][32][kStride]
-  float* sl = sq + 2 * kF32Keys * Sh::kStride;                // [2][32] base-2 log-sums
+  const int group = threadIdx.x / kF32Threads;
+  float* sq = sk + (kF32Rows + group * 2 * kF32Keys) * Sh::kStride;                       // [2][32][kStride] of this group
+  float* sl = sk + (kF32Rows + kF32Groups * 2 * kF32Keys) * Sh::kStride + group * 2 * kF32Keys;      // [2][32] base-2 log-sums
   const PagedParams& A = P.A;
   griddep_launch();
   griddep_wait();
   const int head = blockIdx.x % A.n_kv_heads, b = blockIdx.x / A.n_kv_heads % A.batch, e0 = blockIdx.x / A.n_kv_heads / A.batch * kF32Rows;
   const SeqRows s = seq_rows(A, b);
-  const int old = s.len - s.n, gs = P.g_shift, tid = threadIdx.x, ty = tid >> 3, tx = tid & 7;
+  const int old = s.len - s.n, gs = P.g_shift, tid = threadIdx.x % kF32Threads, ty = tid >> 3, tx = tid & 7;
+  auto group_sync = [&] { asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory"); };
   if (e0 >= s.len || s.n == 0 || old < 0) return;
   const int t_lo = max(0, e0 - old), e_last = min(e0 + kF32Rows - 1, s.len - 1);
   const long long t_end = A.window == 0 || e0 < A.sink ? s.n : min((long long)s.n, (long long)e_last - old + A.window);
@@ -213,14 +217,13 @@ __global__ void __launch_bounds__(kF32Threads) paged_weights_f32_kernel(const __
   constexpr int kVec = D / 4, kRowsPerPass = kF32Threads / kVec;
   const int vec = tid % kVec;
 #pragma unroll 8
-  for (int r = tid / kVec; r < kF32Rows; r += kRowsPerPass) {
+  for (int r = threadIdx.x / kVec; r < kF32Rows; r += kF32Groups * kRowsPerPass) {
     const int i = e0 + r;
     const int pg = i < s.len ? page_of(A, b, i) : -1;
     const float* kp = static_cast<const float*>(A.k_pool);
     stage_piece(sk + r * Sh::kStride + vec * 4, pg < 0 ? nullptr : kp + row_offset(A, pg, head, i, D) + vec * 4, kp);
   }
-  auto load_tile = [&](int it) {
-    const int buf = it & 1;
+  auto load_tile = [&](int it, int buf) {
 #pragma unroll
     for (int k = 0; k < kF32Keys / kRowsPerPass; ++k) {
       const int r = tid / kVec + k * kRowsPerPass;
@@ -233,14 +236,20 @@ __global__ void __launch_bounds__(kF32Threads) paged_weights_f32_kernel(const __
     }
     stage_commit();
   };
-  load_tile(tile0);
+  // copies of a thread: its part of K, then a tile each; `buf` alternates with the group's tiles
+  const int it0 = tile0 + group;
+  if (it0 < tile1) load_tile(it0, 0);
+  else stage_commit();
+  stage_wait<0>();
+  __syncthreads();                                            // K is complete
   float total[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int it = tile0; it < tile1; ++it) {
-    __syncthreads();
-    if (it + 1 < tile1) load_tile(it + 1);
-    if (it + 1 < tile1) stage_wait<1>(); else stage_wait<0>();
-    __syncthreads();
-    const float *tq = sq + (it & 1) * kF32Keys * Sh::kStride, *tl = sl + (it & 1) * kF32Keys;
+  for (int it = it0, buf = 0; it < tile1; it += kF32Groups, buf ^= 1) {
+    if (it != it0) {
+      stage_wait<0>();
+      group_sync();                                           // this tile is there, and the one before has been read
+    }
+    if (it + kF32Groups < tile1) load_tile(it + kF32Groups, buf ^ 1);
+    const float *tq = sq + buf * kF32Keys * Sh::kStride, *tl = sl + buf * kF32Keys;
     float x[4][4];
     dot_tile<D>(sk, tq, ty, tx, x);
 #pragma unroll
@@ -255,16 +264,22 @@ __global__ void __launch_bounds__(kF32Threads) paged_weights_f32_kernel(const __
       total[i] += sum;
     }
   }
+  __syncthreads();                                            // K has been read: its place takes the groups' sums
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     float w = total[i];
 #pragma unroll
     for (int d = 1; d < 8; d <<= 1) w += __shfl_xor_sync(~0u, w, d);
-    const int e = e0 + ty + 16 * i;
-    if (tx == 0 && e < s.len) {
-      float* a = A.scores + ((long long)b * A.n_kv_heads + head) * A.score_stride + e;
-      *a = (A.k && e >= old ? 0.f : *a) + w / (float)(1 << gs);
-    }
+    if (tx == 0) sk[group * kF32Rows + ty + 16 * i] = w;
+  }
+  __syncthreads();
+  const int e = e0 + threadIdx.x;
+  if (threadIdx.x < kF32Rows && e < s.len) {
+    float w = 0.f;
+#pragma unroll
+    for (int g = 0; g < kF32Groups; ++g) w += sk[g * kF32Rows + threadIdx.x];
+    float* a = A.scores + ((long long)b * A.n_kv_heads + head) * A.score_stride + e;
+    *a = (A.k && e >= old ? 0.f : *a) + w / (float)(1 << gs);
   }
 }
 
