@@ -95,32 +95,48 @@ __device__ __forceinline__ bool visible(int i, int pos, int window, int sink) {
 }
 
 // ------------------------------------------------------------------------------------------------
-// append: one warp per (row, kv head); a row of K and a row of V, 16 bytes a lane
+// append: a CTA per kAppendTokens tokens.  Each of its warps finds the page of one; then all threads copy, 16 bytes a step and four
+// steps in flight.  Bound: HBM, each new row read and written once.
 // ------------------------------------------------------------------------------------------------
+constexpr int kAppendThreads = 256, kAppendTokens = 4;
 template <typename T, int D>
-__global__ void __launch_bounds__(128) paged_append_kernel(const PagedParams P) {
+__global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(const PagedParams P) {
+  __shared__ int where[kAppendTokens][2];               // page (-1: nowhere), row of the page
   griddep_launch();
   griddep_wait();
-  const long long item = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
-  if (item >= (long long)P.rows * P.n_kv_heads) return;
-  const int r = (int)(item / P.n_kv_heads), head = (int)(item % P.n_kv_heads);
-  const int b = seq_of_row(P, r);
-  if (b < 0) return;
-  const SeqRows s = seq_rows(P, b);
-  if (r < s.first || r >= s.first + s.n) return;
-  const int i = s.len - s.n + (r - s.first);
-  if (i < 0) return;
-  const int pg = page_of(P, b, i);
-  if (pg < 0) return;
-  const long long dst = row_offset(P, pg, head, i, D), src = (long long)r * P.kv_stride + (long long)head * D;
-  constexpr int kVec = D * (int)sizeof(T) / 16;
-  for (int c = lane; c < 2 * kVec; c += 32) {
-    const bool is_v = c >= kVec;
-    const int e = (is_v ? c - kVec : c) * (16 / (int)sizeof(T));
-    const T* from = static_cast<const T*>(is_v ? P.v : P.k) + src + e;
-    T* to = static_cast<T*>(is_v ? P.v_pool : P.k_pool) + dst + e;
-    *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(from);
+  const int r0 = blockIdx.x * kAppendTokens, warp = threadIdx.x >> 5;
+  if (warp < kAppendTokens && (threadIdx.x & 31) == 0) {
+    const int r = r0 + warp, b = r < P.rows ? seq_of_row(P, r) : -1;
+    int pg = -1, slot = 0;
+    if (b >= 0) {
+      const SeqRows s = seq_rows(P, b);
+      const int i = s.len - s.n + (r - s.first);
+      if (r >= s.first && r < s.first + s.n && i >= 0) { pg = page_of(P, b, i); slot = i & (P.page - 1); }
+    }
+    where[warp][0] = pg;
+    where[warp][1] = slot;
+  }
+  __syncthreads();
+  constexpr int kVec = D * (int)sizeof(T) / 16, kEach = 16 / (int)sizeof(T), kSteps = 4;
+  const int per_row = P.n_kv_heads * kVec, total = kAppendTokens * 2 * per_row;      // pieces: a token's K row, its V row, ...
+  for (int base = threadIdx.x; base < total; base += kSteps * kAppendThreads) {
+    uint4 piece[kSteps];
+    T* to[kSteps];
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+      const int at = base + k * kAppendThreads;
+      to[k] = nullptr;
+      if (at >= total) continue;
+      const int row = at / per_row, c = at % per_row, tok = row >> 1, pg = where[tok][0];
+      if (pg < 0) continue;
+      const bool is_v = row & 1;
+      const int head = c / kVec, e = c % kVec * kEach;
+      piece[k] = *reinterpret_cast<const uint4*>(static_cast<const T*>(is_v ? P.v : P.k) + (long long)(r0 + tok) * P.kv_stride + (long long)head * D + e);
+      to[k] = static_cast<T*>(is_v ? P.v_pool : P.k_pool) + row_offset(P, pg, head, where[tok][1], D) + e;
+    }
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k)
+      if (to[k]) *reinterpret_cast<uint4*>(to[k]) = piece[k];
   }
 }
 

@@ -330,7 +330,7 @@ int prefill_f32(wkv_paged* c, const wkv::PagedParams& A) {
 
 template <typename T, int D>
 int prefill_typed(wkv_paged* c, const wkv::PagedParams& P) {
-  if (P.k) WKV_CUDA(c, launch(c, wkv::paged_append_kernel<T, D>, ((long long)P.rows * P.n_kv_heads + 3) / 4, 128, 0, P));
+  if (P.k) WKV_CUDA(c, launch(c, wkv::paged_append_kernel<T, D>, (P.rows + wkv::kAppendTokens - 1) / wkv::kAppendTokens, wkv::kAppendThreads, 0, P));
   if constexpr (sizeof(T) == 2) return prefill_bf16<D>(c, P); else return prefill_f32<D>(c, P);
 }
 

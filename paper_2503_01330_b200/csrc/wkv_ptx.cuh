@@ -44,14 +44,13 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, uint32
   return false;
 }
 // The same for waits on a kernel's critical path: one instruction when the barrier is ready (a fifth of mbar_wait's cycles, whose
-// loop the compiler guards for divergence); while it is not, the thread is suspended for up to a microsecond a poll, so that
-// waiting warps leave the issue slots to the others.  At most kFastPolls polls.
-constexpr uint32_t kFastPolls = 1u << 20;
+// loop the compiler guards for divergence), no sleeping while it is not.  At most kFastPolls polls.
+constexpr uint32_t kFastPolls = 1u << 26;
 __device__ __forceinline__ bool mbar_wait_fast(uint64_t* bar, uint32_t parity, uint32_t* status) {
   uint32_t left;
   asm volatile(
       "{\n\t.reg .pred done, more;\n\t.reg .u32 n;\n\tmov.u32 n, %3;\n"
-      "POLL:\n\tmbarrier.try_wait.parity.shared::cta.b64 done, [%1], %2, 1000;\n\t@done bra OUT;\n\t"
+      "POLL:\n\tmbarrier.try_wait.parity.shared::cta.b64 done, [%1], %2;\n\t@done bra OUT;\n\t"
       "sub.u32 n, n, 1;\n\tsetp.ne.u32 more, n, 0;\n\t@more bra POLL;\n"
       "OUT:\n\tmov.u32 %0, n;\n\t}"
       : "=r"(left)
