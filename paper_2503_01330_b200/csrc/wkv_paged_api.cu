@@ -461,7 +461,7 @@ int wkv_paged_prefill(wkv_paged* c, int32_t layer, int32_t batch, const void* q,
   if (rc != WKV_OK) return rc;
   if (total_q > (1 << 24)) return fail(c, WKV_ERR_INVALID, "total_q must be at most 2^24");
   if (batch > 0 && total_q > 0 && !q_start) return fail(c, WKV_ERR_INVALID, "q_start must not be NULL");
-  if (scores && !lse) return fail(c, WKV_ERR_INVALID, "scores need lse");
+  if (scores && !lse && total_q > 0) return fail(c, WKV_ERR_INVALID, "scores need lse");
   P.q_start = q_start;
   return prefill(c, P);
 }

@@ -21,7 +21,8 @@ U = 2.0 ** -24
 
 class Case:
     def __init__(self, lens, new, hq=4, hk=2, d=64, dtype="bf16", page=16, window=0, sink=0, scores=False, layers=1, seed=0,
-                 strided=False, extra_cols=0, extra_rows=0, append=True, prefill=None, spare=3, garbage=float("nan"), width=None):
+                 strided=False, extra_cols=0, extra_rows=0, append=True, prefill=None, spare=3, garbage=float("nan"), width=None,
+                 spikes=0.0):
         self.lens, self.new = list(lens), list(new)
         self.hq, self.hk, self.d, self.page, self.G = hq, hk, d, page, hq // hk
         self.window, self.sink, self.append, self.layers = window, sink, append, layers
@@ -48,6 +49,8 @@ class Case:
         for b, n in enumerate(self.lens):
             k, v = torch.randn(n, hk, d, generator=g), torch.randn(n, hk, d, generator=g)
             k[..., :2] *= 3.0
+            if spikes:                               # a few keys whose logits tower over all before them
+                k[torch.rand(n, generator=g) < spikes] *= 25.0
             self.K.append(k.to(self.tdt))
             self.V.append(v.to(self.tdt))
             there = n - (self.new[b] if append else 0)
