@@ -188,6 +188,24 @@ static_assert(sizeof(PrefillItem) <= 64, "two of them in 128 bytes of shared mem
 // Visible columns of a 32-column piece as bits: columns 0..top, of these low.. and those below sinks.
 __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
 
+// Eight lanes with 128 bytes of a row each, in 16-byte pieces: lane i gets piece i of all eight rows.  Stored piece by piece, every
+// lane its own row, a row tile's output took 6900 cycles (32 lines a store); now a store writes four rows' full lines.
+__device__ __forceinline__ void exchange_pieces(uint32_t (&y)[8][4]) {
+#pragma unroll
+  for (int s = 1; s < 8; s <<= 1) {
+    const bool up = threadIdx.x & s;
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+      if (p & s) continue;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t got = __shfl_xor_sync(~0u, up ? y[p][w] : y[p | s][w], s);
+        if (up) y[p][w] = got; else y[p | s][w] = got;
+      }
+    }
+  }
+}
+
 template <int D>
 __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const __grid_constant__ PrefillParams P) {
   using Sh = PrefillShape<D>;
@@ -504,40 +522,48 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
       mbar_wait_fast(o_full, n & 1, A.status);
       tcgen05_after_sync();
       const bool seen = !(l <= 0.f);                            // else the row's TMEM lane may hold anything
+      const float inv = !seen ? 0.f : P.splits == 1 ? 1.f / l : 1.f;
+      // rows of the eight lanes that exchange pieces, and this lane's 16-byte piece of 128
+      const int row8 = t * 128 + (row & ~7), piece = lane & 7;
       if (P.splits == 1) {
-        const float inv = seen ? 1.f / l : 0.f;
-        const int tok = B.first + (R >> P.g_shift), hq = B.head * G + (R & (G - 1));
-        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + ((long long)tok * A.n_q_heads + hq) * D;
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-          uint32_t o[32];
-          tmem_load32(o_at + i * 32, o);
+#pragma unroll 1
+        for (int i = 0; i < D / 64; ++i) {
+          uint32_t o[64], y[8][4];
+          tmem_load32(o_at + i * 64, o);
+          tmem_load32(o_at + i * 64 + 32, o + 32);
           tmem_wait_loads();
-          if (live) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              uint32_t y[4];
+          for (int e = 0; e < 32; ++e)
+            y[e >> 2][e & 3] = seen ? pack_bf16(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv) : 0u;
+          exchange_pieces(y);
 #pragma unroll
-              for (int z = 0; z < 4; ++z)
-                y[z] = seen ? pack_bf16(__uint_as_float(o[e * 8 + 2 * z]) * inv, __uint_as_float(o[e * 8 + 2 * z + 1]) * inv) : 0u;
-              reinterpret_cast<uint4*>(out)[i * 4 + e] = make_uint4(y[0], y[1], y[2], y[3]);
-            }
+          for (int r = 0; r < 8; ++r) {
+            const int Rr = B.row0 + row8 + r, tok = Rr >> P.g_shift;
+            if (tok >= B.n) break;
+            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + ((long long)(B.first + tok) * A.n_q_heads + B.head * G + (Rr & (G - 1))) * D + i * 64;
+            reinterpret_cast<uint4*>(out)[piece] = make_uint4(y[r][0], y[r][1], y[r][2], y[r][3]);
           }
         }
-        if (live && A.lse) A.lse[(long long)tok * A.n_q_heads + hq] = seen ? (m * c + log2f(l)) * kLn2 : -INFINITY;
+        if (live && A.lse) {
+          const long long at = (long long)(B.first + (R >> P.g_shift)) * A.n_q_heads + B.head * G + (R & (G - 1));
+          A.lse[at] = seen ? (m * c + log2f(l)) * kLn2 : -INFINITY;
+        }
       } else {
-        const long long at = (long long)item.slot * 256 + t * 128 + row;
-#pragma unroll
+#pragma unroll 1
         for (int i = 0; i < D / 32; ++i) {
-          uint32_t o[32];
+          uint32_t o[32], y[8][4];
           tmem_load32(o_at + i * 32, o);
           tmem_wait_loads();
-          if (live && seen) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) reinterpret_cast<uint4*>(P.part + at * D)[i * 8 + e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+          for (int e = 0; e < 32; ++e) y[e >> 2][e & 3] = seen ? o[e] : 0u;
+          exchange_pieces(y);
+#pragma unroll
+          for (int r = 0; r < 8; ++r) {
+            if ((B.row0 + row8 + r) >> P.g_shift >= B.n) break;
+            reinterpret_cast<uint4*>(P.part + ((long long)item.slot * 256 + row8 + r) * D + i * 32)[piece] = make_uint4(y[r][0], y[r][1], y[r][2], y[r][3]);
           }
         }
-        if (live) P.part_ml[at] = make_float2(seen ? m * c : -INFINITY, seen ? l : 0.f);
+        if (live) P.part_ml[(long long)item.slot * 256 + t * 128 + row] = make_float2(seen ? m * c : -INFINITY, seen ? l : 0.f);
       }
       tcgen05_before_sync();
       __syncwarp();
