@@ -95,49 +95,66 @@ __device__ __forceinline__ bool visible(int i, int pos, int window, int sink) {
 }
 
 // ------------------------------------------------------------------------------------------------
-// append: a CTA per kAppendTokens tokens.  Each of its warps finds the page of one; then all threads copy, 16 bytes a step and four
-// steps in flight.  Bound: HBM, each new row read and written once.
+// append
 // ------------------------------------------------------------------------------------------------
-constexpr int kAppendThreads = 256, kAppendTokens = 4;
+// Where row r of a prompt call's k and v goes: page (-1: nowhere) and entry.  `inner`: nowhere too for the rows of the page that
+// their chunk starts in the middle of.
+struct NewRow {
+  int page, entry;
+};
+__device__ __forceinline__ NewRow new_row(const PagedParams& P, int r, bool inner) {
+  NewRow w{-1, 0};
+  const int b = r < P.rows ? seq_of_row(P, r) : -1;
+  if (b < 0) return w;
+  const SeqRows s = seq_rows(P, b);
+  const int old = s.len - s.n;
+  w.entry = old + (r - s.first);
+  if (r < s.first || r >= s.first + s.n || w.entry < 0) return w;
+  if (inner && (w.entry & ~(P.page - 1)) < old) return w;
+  w.page = page_of(P, b, w.entry);
+  return w;
+}
+// The row copied by THREADS threads (this one: `me`), 16 bytes a step and STEPS steps in flight.
+template <typename T, int D, int THREADS, int STEPS>
+__device__ __forceinline__ void append_row(const PagedParams& P, int r, const NewRow& w, int me) {
+  if (w.page < 0) return;
+  constexpr int kVec = D * (int)sizeof(T) / 16, kEach = 16 / (int)sizeof(T);
+  const int per_row = P.n_kv_heads * kVec;              // pieces: the K row, then the V row
+  const long long to = row_offset(P, w.page, 0, w.entry, D);
+  for (int base = me; base < 2 * per_row; base += STEPS * THREADS) {
+    uint4 piece[STEPS];
+#pragma unroll
+    for (int k = 0; k < STEPS; ++k) {
+      const int at = base + k * THREADS, c = at >= per_row ? at - per_row : at;
+      if (at < 2 * per_row) piece[k] = *reinterpret_cast<const uint4*>(static_cast<const T*>(at >= per_row ? P.v : P.k) + (long long)r * P.kv_stride + (long long)c * kEach);
+    }
+#pragma unroll
+    for (int k = 0; k < STEPS; ++k) {
+      const int at = base + k * THREADS, c = at >= per_row ? at - per_row : at;
+      if (at < 2 * per_row)
+        *reinterpret_cast<uint4*>(static_cast<T*>(at >= per_row ? P.v_pool : P.k_pool) + to + ((long long)(c / kVec) * P.page) * D + c % kVec * kEach) = piece[k];
+    }
+  }
+}
+
+// All new rows: a CTA per token.
+constexpr int kAppendThreads = 128;
 template <typename T, int D>
 __global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(const PagedParams P) {
-  __shared__ int where[kAppendTokens][2];               // page (-1: nowhere), row of the page
   griddep_launch();
   griddep_wait();
-  const int r0 = blockIdx.x * kAppendTokens, warp = threadIdx.x >> 5;
-  if (warp < kAppendTokens && (threadIdx.x & 31) == 0) {
-    const int r = r0 + warp, b = r < P.rows ? seq_of_row(P, r) : -1;
-    int pg = -1, slot = 0;
-    if (b >= 0) {
-      const SeqRows s = seq_rows(P, b);
-      const int i = s.len - s.n + (r - s.first);
-      if (r >= s.first && r < s.first + s.n && i >= 0) { pg = page_of(P, b, i); slot = i & (P.page - 1); }
-    }
-    where[warp][0] = pg;
-    where[warp][1] = slot;
-  }
-  __syncthreads();
-  constexpr int kVec = D * (int)sizeof(T) / 16, kEach = 16 / (int)sizeof(T), kSteps = 4;
-  const int per_row = P.n_kv_heads * kVec, total = kAppendTokens * 2 * per_row;      // pieces: a token's K row, its V row, ...
-  for (int base = threadIdx.x; base < total; base += kSteps * kAppendThreads) {
-    uint4 piece[kSteps];
-    T* to[kSteps];
-#pragma unroll
-    for (int k = 0; k < kSteps; ++k) {
-      const int at = base + k * kAppendThreads;
-      to[k] = nullptr;
-      if (at >= total) continue;
-      const int row = at / per_row, c = at % per_row, tok = row >> 1, pg = where[tok][0];
-      if (pg < 0) continue;
-      const bool is_v = row & 1;
-      const int head = c / kVec, e = c % kVec * kEach;
-      piece[k] = *reinterpret_cast<const uint4*>(static_cast<const T*>(is_v ? P.v : P.k) + (long long)(r0 + tok) * P.kv_stride + (long long)head * D + e);
-      to[k] = static_cast<T*>(is_v ? P.v_pool : P.k_pool) + row_offset(P, pg, head, where[tok][1], D) + e;
-    }
-#pragma unroll
-    for (int k = 0; k < kSteps; ++k)
-      if (to[k]) *reinterpret_cast<uint4*>(to[k]) = piece[k];
-  }
+  append_row<T, D, kAppendThreads, 8>(P, blockIdx.x, new_row(P, blockIdx.x, false), threadIdx.x);
+}
+// The new rows of the page that a chunk starts in the middle of: a CTA per sequence and row of a page.
+template <typename T, int D>
+__global__ void __launch_bounds__(kAppendThreads) paged_append_edge_kernel(const PagedParams P) {
+  griddep_launch();
+  griddep_wait();
+  const int b = blockIdx.x >> P.page_shift, k = blockIdx.x & (P.page - 1);
+  const SeqRows s = seq_rows(P, b);
+  const int old = s.len - s.n, i = (old & ~(P.page - 1)) + k;      // the k-th entry of the page
+  if (i < old || i >= s.len || !(old & (P.page - 1))) return;
+  append_row<T, D, kAppendThreads, 8>(P, s.first + i - old, new_row(P, s.first + i - old, false), threadIdx.x);
 }
 
 // ------------------------------------------------------------------------------------------------

@@ -149,12 +149,13 @@ int encode_pool(wkv_paged* c, unsigned char* out128, void* pool, int box_rows, i
   return encode_map(c, out128, pool, {elems, (cuuint64_t)f.page_size, row / 128, (cuuint64_t)f.n_layers * f.n_pages * f.n_kv_heads},
                     {row, 128, row * f.page_size}, {elems, (cuuint32_t)box_rows, (cuuint32_t)box_parts, 1u});
 }
-// A call's q: 128 bytes of a row, heads, tokens, parts; boxes of 128 rows (token, head of a group) x one part.
-int encode_queries(wkv_paged* c, unsigned char* out128, const wkv::PagedParams& P) {
+// A call's q, k or v ([tokens][heads][D], tokens `stride` elements apart): 128 bytes of a row, heads, tokens, parts; boxes of
+// box_heads x box_tokens rows x one part.
+int encode_rows(wkv_paged* c, unsigned char* out128, const void* base, int64_t stride, int heads, int tokens, int box_heads, int box_tokens) {
   const cuuint64_t row = (cuuint64_t)c->cfg.head_dim * c->elem;
-  const cuuint32_t elems = (cuuint32_t)(128 / c->elem), G = (cuuint32_t)c->group;
-  return encode_map(c, out128, P.q, {elems, (cuuint64_t)P.n_q_heads, (cuuint64_t)P.rows, row / 128}, {row, (cuuint64_t)P.q_stride * c->elem, 128},
-                    {elems, G, 128u / G, 1u});
+  const cuuint32_t elems = (cuuint32_t)(128 / c->elem);
+  return encode_map(c, out128, base, {elems, (cuuint64_t)heads, (cuuint64_t)tokens, row / 128}, {row, (cuuint64_t)stride * c->elem, 128},
+                    {elems, (cuuint32_t)box_heads, (cuuint32_t)box_tokens, 1u});
 }
 
 // Rows of partial outputs that the runs of a prompt call may have: two row blocks per SM on bf16 rows, eight of the smaller ones on
@@ -300,8 +301,14 @@ int prefill_bf16(wkv_paged* c, const wkv::PagedParams& A) {
   wkv::PrefillParams P;
   long long units;
   int rc = prefill_params(c, P, A, wkv::kPrefillRows, 4 * wkv::kPrefillKeys, &units);
-  if (rc == WKV_OK) rc = encode_queries(c, P.qmap, A);
+  if (rc == WKV_OK) rc = encode_rows(c, P.qmap, A.q, A.q_stride, A.n_q_heads, A.rows, c->group, 128 / c->group);
+  if (rc == WKV_OK && A.k) {
+    P.append = 1;
+    rc = encode_rows(c, P.kinmap, A.k, A.kv_stride, A.n_kv_heads, A.rows, 1, A.page);
+    if (rc == WKV_OK) rc = encode_rows(c, P.vinmap, A.v, A.kv_stride, A.n_kv_heads, A.rows, 1, A.page);
+  }
   if (rc != WKV_OK) return rc;
+  if (A.k) WKV_CUDA(c, launch(c, wkv::paged_append_edge_kernel<__nv_bfloat16, D>, (long long)A.batch * A.page, wkv::kAppendThreads, 0, A));
   std::memcpy(P.kmap, c->part_kmap, 128);
   std::memcpy(P.vmap, c->part_vmap, 128);
   WKV_CUDA(c, launch(c, wkv::paged_prefill_kernel<D>, std::min(P.items, c->sm_count), wkv::kPrefillThreads, wkv::PrefillShape<D>::kSmem, P));
@@ -319,6 +326,7 @@ int prefill_f32(wkv_paged* c, const wkv::PagedParams& A) {
   long long units;
   const int rc = prefill_params(c, P, A, wkv::kF32Rows, 2 * wkv::kF32Keys, &units);
   if (rc != WKV_OK) return rc;
+  if (A.k) WKV_CUDA(c, launch(c, wkv::paged_append_kernel<float, D>, A.rows, wkv::kAppendThreads, 0, A));
   WKV_CUDA(c, launch(c, wkv::paged_prefill_f32_kernel<D>, P.items, wkv::kF32Threads, wkv::F32Shape<D>::kSmem, P));
   if (P.splits > 1) WKV_CUDA(c, launch(c, wkv::paged_prefill_join_kernel<float, D, wkv::kF32Rows>, units * (wkv::kF32Rows / 32), 256, 0, P));
   if (A.scores) {
@@ -328,17 +336,11 @@ int prefill_f32(wkv_paged* c, const wkv::PagedParams& A) {
   return WKV_OK;
 }
 
-template <typename T, int D>
-int prefill_typed(wkv_paged* c, const wkv::PagedParams& P) {
-  if (P.k) WKV_CUDA(c, launch(c, wkv::paged_append_kernel<T, D>, (P.rows + wkv::kAppendTokens - 1) / wkv::kAppendTokens, wkv::kAppendThreads, 0, P));
-  if constexpr (sizeof(T) == 2) return prefill_bf16<D>(c, P); else return prefill_f32<D>(c, P);
-}
-
 int prefill(wkv_paged* c, const wkv::PagedParams& P) {
   if (P.batch == 0 || P.rows == 0) return WKV_OK;
   const bool wide = c->cfg.head_dim == 128;
-  if (c->cfg.dtype == WKV_BF16) return wide ? prefill_typed<__nv_bfloat16, 128>(c, P) : prefill_typed<__nv_bfloat16, 64>(c, P);
-  return wide ? prefill_typed<float, 128>(c, P) : prefill_typed<float, 64>(c, P);
+  if (c->cfg.dtype == WKV_BF16) return wide ? prefill_bf16<128>(c, P) : prefill_bf16<64>(c, P);
+  return wide ? prefill_f32<128>(c, P) : prefill_f32<64>(c, P);
 }
 
 }  // namespace

@@ -13,7 +13,11 @@
 //
 // Two row tiles of 128 take turns: while one's logits are in its softmax warps, the tensor cores work on the other's.  Warps 0-3
 // and 4-7: softmax of row tile 0 and 1, a thread per row (a TMEM lane), so statistics need no shuffles; warp 8 issues all matrix
-// instructions; warp 9 all copies; warp 10 fetches items (11 idles).
+// instructions; warp 9 all copies; warp 10 fetches items; warp 11 stores the call's new rows.
+//
+// New rows come to the tensor cores straight from the call's k and v; storing them in their pages (41 us for 8192 tokens of 32 x
+// 128 by a kernel of its own) runs beside the products, whose time leaves HBM idle.  Only the page that a chunk starts in the middle
+// of is read back from the pool: paged_append_edge_kernel has stored its new rows before.
 // TMEM, 512 columns: logits of both tiles (fp32, 128 columns each; the weights overwrite them as bf16, 64 columns, and are the A
 // operand of P.V straight from TMEM) and both outputs (D columns each).  An output is rescaled in place, and only when a row's
 // maximum has grown by more than 2^8 since its reference was taken.
@@ -39,9 +43,12 @@ struct PrefillParams {
   float* part;               // [row block x kv head][split][256][D] outputs, where splits > 1
   float2* part_ml;           // [row block x kv head][split][256] (maximum in base-2 logits, sum)
   int oob_chunk, chunk0;
+  int append;                // the call brings k and v, and this kernel stores what paged_append_edge_kernel has not
   alignas(64) unsigned char qmap[128];   // q as [part][token][head][64 elements], boxes of a row tile
   alignas(64) unsigned char kmap[128];   // pool as [chunk][part][row][64 elements], boxes of a page x one part
   alignas(64) unsigned char vmap[128];
+  alignas(64) unsigned char kinmap[128]; // the call's k and v as [part][token][head][64 elements], boxes of one head's `page` tokens
+  alignas(64) unsigned char vinmap[128];
 };
 
 template <int D>
@@ -156,26 +163,6 @@ __device__ __forceinline__ uint64_t pair(float lo, float hi) {
   return d;
 }
 __device__ __forceinline__ void unpair(uint64_t d, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(d)); }
-
-// 2^x of a pair without the exponential unit: x = n + f, |f| <= 1/2, a polynomial of degree 5 in f (least-squares fit weighted
-// towards its largest relative error, 9.2e-8), n into the exponent.  -infinity and everything below -127 give exactly 0.
-__device__ __forceinline__ void exp2_pair(float& x0, float& x1) {
-  constexpr float kMagic = 12582912.f;                          // 1.5 * 2^23: adding it rounds to a whole number
-  const uint64_t x = pair(fmaxf(x0, -127.f), fmaxf(x1, -127.f));
-  const uint64_t n = add2(x, pair(kMagic, kMagic));
-  const uint64_t f = fma2_(add2(n, pair(-kMagic, -kMagic)), pair(-1.f, -1.f), x);
-  uint64_t p = pair(0.001326472614891827f, 0.001326472614891827f);
-  p = fma2_(p, f, pair(0.009671512991189957f, 0.009671512991189957f));
-  p = fma2_(p, f, pair(0.05550733581185341f, 0.05550733581185341f));
-  p = fma2_(p, f, pair(0.24022242426872253f, 0.24022242426872253f));
-  p = fma2_(p, f, pair(0.6931470036506653f, 0.6931470036506653f));
-  p = fma2_(p, f, pair(1.f, 1.f));
-  float n0, n1;
-  unpair(n, n0, n1);
-  unpair(p, x0, x1);
-  x0 = __uint_as_float(__float_as_uint(x0) + (__float_as_uint(n0) << 23));
-  x1 = __uint_as_float(__float_as_uint(x1) + (__float_as_uint(n1) << 23));
-}
 
 // What warp 10 tells the others about an item.
 struct PrefillItem {
@@ -308,8 +295,9 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
         __syncwarp();
         for (int v = item.v0; v < item.v1; ++v) {
           const int i = B.entry(v * kPrefillKeys + box * pr);
+          const bool fresh = P.append && i >= B.old;            // a box of the call's own rows (tokens behind the chunk: never used)
           int chunk = P.oob_chunk;
-          if (mine && i < B.len) {
+          if (mine && i < B.len && !fresh) {
             const int pg = page_of(A, B.b, i);
             if (pg >= 0) chunk = P.chunk0 + pg * A.n_kv_heads + B.head;
           }
@@ -319,8 +307,21 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
             if (it >= STAGES) mbar_wait_fast(&empty[st], ((it / STAGES) & 1) ^ 1, A.status);
             if (lane == 0) mbar_expect_tx(&full[st], Sh::kTileBytes);
             __syncwarp();
-            if (mine)
-              tensor_g2s_4d(ring + st * Sh::kTileBytes + part * Sh::kPartBytes + box * pr * 128, kv ? P.vmap : P.kmap, 0, 0, part, chunk, &full[st]);
+            unsigned char* dst = ring + st * Sh::kTileBytes + part * Sh::kPartBytes + box * pr * 128;
+            if (mine && fresh) tensor_g2s_4d(dst, kv ? P.vinmap : P.kinmap, 0, B.head, B.first + i - B.old, part, &full[st]);
+            else if (mine) tensor_g2s_4d(dst, kv ? P.vmap : P.kmap, 0, 0, part, chunk, &full[st]);
+          }
+        }
+      }
+    } else if (warp == 11) {
+      // ---- the call's new rows into their pages: 32 tokens looked up together, then copied one after the other
+      if (P.append) {
+        for (int r0 = blockIdx.x; r0 < A.rows; r0 += 32 * gridDim.x) {
+          const NewRow mine = new_row(A, (int)min((long long)r0 + (long long)lane * gridDim.x, 0x7fffffffLL), true);
+#pragma unroll 1
+          for (int j = 0; j < 32; ++j) {
+            const NewRow w{__shfl_sync(~0u, mine.page, j), __shfl_sync(~0u, mine.entry, j)};
+            append_row<__nv_bfloat16, D, 32, 8>(A, r0 + j * gridDim.x, w, lane);
           }
         }
       }
@@ -496,12 +497,8 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
           for (int i = 0; i < 16; ++i) {
             float p0, p1;
             unpair(fma2_(pair(__uint_as_float(x[h * 32 + 2 * i]), __uint_as_float(x[h * 32 + 2 * i + 1])), c2, shift2), p0, p1);
-            if ((i & 3) == 3) {
-              exp2_pair(p0, p1);
-            } else {
-              p0 = exp2_fast(p0);
-              p1 = exp2_fast(p1);
-            }
+            p0 = exp2_fast(p0);
+            p1 = exp2_fast(p1);
             sum2[i & 3] = add2(sum2[i & 3], pair(p0, p1));
             w[i] = pack_bf16(p0, p1);
           }
