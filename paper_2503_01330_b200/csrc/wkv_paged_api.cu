@@ -388,7 +388,7 @@ int wkv_paged_create(const wkv_paged_config* cfg, wkv_paged** out) {
   WKV_TAKE(&c->arrived, lanes * 4);
   WKV_TAKE(&c->run_part, run_rows(c) * cfg->head_dim * 4);
   WKV_TAKE(&c->run_ml, run_rows(c) * 8);
-  WKV_TAKE(&c->item_counter, 4);
+  WKV_TAKE(&c->item_counter, 8);
   const bool own_pools = !c->k_pool;
   if (own_pools) {
     WKV_TAKE(&c->k_pool, pool);
@@ -398,7 +398,7 @@ int wkv_paged_create(const wkv_paged_config* cfg, wkv_paged** out) {
   if (rc == WKV_OK) {
     e = cudaMemsetAsync(c->status, 0, 4, c->stream);
     if (e == cudaSuccess) e = cudaMemsetAsync(c->arrived, 0, lanes * 4, c->stream);
-    if (e == cudaSuccess) e = cudaMemsetAsync(c->item_counter, 0, 4, c->stream);
+    if (e == cudaSuccess) e = cudaMemsetAsync(c->item_counter, 0, 8, c->stream);
     if (e == cudaSuccess && own_pools) e = cudaMemsetAsync(c->k_pool, 0, pool, c->stream);
     if (e == cudaSuccess && own_pools) e = cudaMemsetAsync(c->v_pool, 0, pool, c->stream);
     if (e != cudaSuccess) rc = WKV_ERR_CUDA;

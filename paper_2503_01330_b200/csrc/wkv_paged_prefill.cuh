@@ -13,7 +13,8 @@
 //
 // Two row tiles of 128 take turns: while one's logits are in its softmax warps, the tensor cores work on the other's.  Warps 0-3
 // and 4-7: softmax of row tile 0 and 1, a thread per row (a TMEM lane), so statistics need no shuffles; warp 8 issues all matrix
-// instructions; warp 9 all copies; warp 10 fetches items; warp 11 stores the call's new rows.
+// instructions; warp 9 all copies; warp 10 fetches items; warp 11 stores the call's new rows,
+// with the softmax warps' help when they have run out of items.
 //
 // New rows come to the tensor cores straight from the call's k and v; storing them in their pages (41 us for 8192 tokens of 32 x
 // 128 by a kernel of its own) runs beside the products, whose time leaves HBM idle.  Only the page that a chunk starts in the middle
@@ -31,6 +32,7 @@ namespace wkv {
 // Three warpgroups of 168 registers a thread at launch; the softmax ones hold a row of logits (128) and take what the third
 // does not need: 2 * 208 + 88 = 3 * 168.
 constexpr int kPrefillThreads = 384;
+constexpr int kPrefillSoftmaxWarps = 8;
 constexpr int kPrefillRows = 256;            // rows of an item
 constexpr int kPrefillKeys = 128;            // entries per tile
 
@@ -39,7 +41,7 @@ struct PrefillParams {
   int g_shift;               // log2 of the query heads per kv head
   int items;                 // row blocks (at most) x kv heads x splits
   int splits;
-  uint32_t* counter;         // next item; zero between launches
+  uint32_t* counter;         // next item, next eight new rows; zero between launches
   float* part;               // [row block x kv head][split][256][D] outputs, where splits > 1
   float2* part_ml;           // [row block x kv head][split][256] (maximum in base-2 logits, sum)
   int oob_chunk, chunk0;
@@ -193,6 +195,30 @@ __device__ __forceinline__ void exchange_pieces(uint32_t (&y)[8][4]) {
   }
 }
 
+// New rows into their pages, by one warp of several on every CTA (`takers`): eight tokens at a time from a counter, looked up
+// together, then copied one after the other.
+template <int D>
+__device__ __forceinline__ void append_rows(const PrefillParams& P, int takers) {
+  const int lane = threadIdx.x & 31;
+  const uint32_t chunks = (uint32_t)(P.A.rows + 7) / 8;
+  for (;;) {
+    uint32_t w = 0;
+    if (lane == 0) w = atomicAdd(P.counter + 1, 1u);
+    w = __shfl_sync(~0u, w, 0);
+    if (w >= chunks) {
+      if (lane == 0 && w == chunks + (uint32_t)takers * gridDim.x - 1) P.counter[1] = 0;      // the last one to ask
+      return;
+    }
+    const int r0 = (int)w * 8;
+    const NewRow mine = new_row(P.A, r0 + (lane & 7), true);
+#pragma unroll 1
+    for (int j = 0; j < 8; ++j) {
+      const NewRow row{__shfl_sync(~0u, mine.page, j), __shfl_sync(~0u, mine.entry, j)};
+      append_row<__nv_bfloat16, D, 32, 8>(P.A, r0 + j, row, lane);
+    }
+  }
+}
+
 template <int D>
 __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const __grid_constant__ PrefillParams P) {
   using Sh = PrefillShape<D>;
@@ -314,17 +340,8 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
         }
       }
     } else if (warp == 11) {
-      // ---- the call's new rows into their pages: 32 tokens looked up together, then copied one after the other
-      if (P.append) {
-        for (int r0 = blockIdx.x; r0 < A.rows; r0 += 32 * gridDim.x) {
-          const NewRow mine = new_row(A, (int)min((long long)r0 + (long long)lane * gridDim.x, 0x7fffffffLL), true);
-#pragma unroll 1
-          for (int j = 0; j < 32; ++j) {
-            const NewRow w{__shfl_sync(~0u, mine.page, j), __shfl_sync(~0u, mine.entry, j)};
-            append_row<__nv_bfloat16, D, 32, 8>(A, r0 + j * gridDim.x, w, lane);
-          }
-        }
-      }
+      // ---- the call's new rows into their pages
+      if (P.append) append_rows<D>(P, 1 + kPrefillSoftmaxWarps);
     } else if (warp == 8) {
       // ---- matrix instructions, all by one elected thread
       if (elect_one()) {
@@ -566,6 +583,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
       __syncwarp();
       if (lane == 0) mbar_arrive(&o_free[t]);
     }
+    if (P.append) append_rows<D>(P, 1 + kPrefillSoftmaxWarps);     // what warp 11 has not come to
   }
   tcgen05_before_sync();
   __syncthreads();
