@@ -439,6 +439,24 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
     w.begin(static_cast<const T*>(A.q) + (long long)b * A.q_stride + (long long)hq0 * D, scratch + warp * Warp::kScratch);
     const long long logit_stride = (long long)A.width << A.page_shift;
     float* logits = P.logits ? P.logits + lane_no * G * logit_stride : nullptr;
+    // the call's own entry: the warp that owns it in the piece's last tile fetches its rows now, and stores them when it comes to
+    // that tile
+    constexpr int kPieces = Sh::kRowBytes / 16, kNew = 2 * kPieces / 32 > 0 ? 2 * kPieces / 32 : 1;
+    const bool brings = A.k && s.len > 0 && v + n == s.tiles && (s.len - 1) % TILE / Sh::kEach == warp;
+    uint4 news[kNew];
+    int new_page = -1;
+    if (brings) {
+      new_page = page_of(A, b, s.len - 1);
+      const long long src = (long long)b * A.kv_stride + (long long)head * D;
+#pragma unroll
+      for (int j = 0; j < kNew; ++j) {
+        const int e = lane + 32 * j;
+        if (e >= 2 * kPieces) continue;
+        const bool is_v = e >= kPieces;
+        const int c = (is_v ? e - kPieces : e) * (16 / (int)sizeof(T));
+        news[j] = *reinterpret_cast<const uint4*>(static_cast<const T*>(is_v ? A.v : A.k) + src + c);
+      }
+    }
     for (int k = 0; k < n; ++k, ++it, ++v) {
       const int st = it % STAGES;
       unsigned char* tk = ring + st * 2 * Sh::kTileBytes;
@@ -449,26 +467,24 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
       const bool any = i0 < s.len && (i0 + Sh::kEach > s.lo || i0 < s.sinks);
       if (any) {
         const bool all = i0 + Sh::kEach <= s.len && (i0 >= s.lo || i0 + Sh::kEach <= s.sinks);
-        const bool fresh = A.k && s.len - 1 >= i0 && s.len - 1 < i0 + Sh::kEach;
+        const bool fresh = brings && k == n - 1;
         if (!all || fresh) {
           // rows that nobody sees may hold anything: their weight is zero, their values have to be finite
-          constexpr int kPieces = Sh::kRowBytes / 16;
           for (int e = lane; e < Sh::kEach * kPieces; e += 32) {
             const int r = e / kPieces;
             if (!s.sees(i0 + r))
               *reinterpret_cast<uint4*>(tv + tile_offset<Sh::kParts>(row0 + r, e % kPieces, pr, pr_shift)) = make_uint4(0, 0, 0, 0);
           }
           if (fresh) {
-            // the call's own entry: from its row into the tile, and into its page
-            const int i = s.len - 1, pg = page_of(A, b, i);
-            const long long src = (long long)b * A.kv_stride + (long long)head * D;
-            for (int e = lane; e < 2 * kPieces; e += 32) {
+#pragma unroll
+            for (int j = 0; j < kNew; ++j) {
+              const int e = lane + 32 * j;
+              if (e >= 2 * kPieces) continue;
               const bool is_v = e >= kPieces;
-              const int c = is_v ? e - kPieces : e;
-              const uint4 x = *reinterpret_cast<const uint4*>(static_cast<const T*>(is_v ? A.v : A.k) + src + c * (16 / (int)sizeof(T)));
-              *reinterpret_cast<uint4*>((is_v ? tv : tk) + tile_offset<Sh::kParts>(i - i0 + row0, c, pr, pr_shift)) = x;
-              if (pg >= 0)
-                *reinterpret_cast<uint4*>(static_cast<T*>(is_v ? A.v_pool : A.k_pool) + row_offset(A, pg, head, i, D) + c * (16 / (int)sizeof(T))) = x;
+              *reinterpret_cast<uint4*>((is_v ? tv : tk) + tile_offset<Sh::kParts>(s.len - 1 - i0 + row0, e % kPieces, pr, pr_shift)) = news[j];
+              if (new_page >= 0)
+                *reinterpret_cast<uint4*>(static_cast<T*>(is_v ? A.v_pool : A.k_pool) + row_offset(A, new_page, head, s.len - 1, D) +
+                                          e % kPieces * (16 / (int)sizeof(T))) = news[j];
             }
           }
           __syncwarp();
@@ -521,17 +537,30 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
         const long long slot0 = c0 + lane_no;
         for (int e = tid; e < G * D / 4; e += 128) {
           const int g = e / (D / 4), c = e % (D / 4) * 4;
-          float mm = -INFINITY;
-          for (int i = 0; i < pieces; ++i) mm = fmaxf(mm, __ldcg(&P.part_ml[(slot0 + i) * G + g]).x);
-          float sum = 0.f;
+          float mm = -INFINITY, sum = 0.f;
           float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-          for (int i = 0; i < pieces; ++i) {
-            const float2 ml = __ldcg(&P.part_ml[(slot0 + i) * G + g]);
-            const float4 x = __ldcg(&reinterpret_cast<const float4*>(P.part + (slot0 + i) * G * D)[e]);
-            const float f = ml.x == -INFINITY ? 0.f : exp2_fast(ml.x - mm);
-            sum = fmaf(ml.y, f, sum);
-            acc.x = fmaf(x.x, f, acc.x); acc.y = fmaf(x.y, f, acc.y); acc.z = fmaf(x.z, f, acc.z); acc.w = fmaf(x.w, f, acc.w);
+          for (int i0 = 0; i0 < pieces; i0 += 8) {         // eight pieces' loads in flight together
+            float2 ml[8];
+            float4 x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const bool in = i0 + i < pieces;
+              ml[i] = in ? __ldcg(&P.part_ml[(slot0 + i0 + i) * G + g]) : make_float2(-INFINITY, 0.f);
+              x[i] = in ? __ldcg(&reinterpret_cast<const float4*>(P.part + (slot0 + i0 + i) * G * D)[e]) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+            float mn = mm;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) mn = fmaxf(mn, ml[i].x);
+            const float f0 = mm == -INFINITY ? 0.f : exp2_fast(mm - mn);
+            sum *= f0;
+            acc.x *= f0; acc.y *= f0; acc.z *= f0; acc.w *= f0;
+            mm = mn;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float f = ml[i].x == -INFINITY ? 0.f : exp2_fast(ml[i].x - mm);
+              sum = fmaf(ml[i].y, f, sum);
+              acc.x = fmaf(x[i].x, f, acc.x); acc.y = fmaf(x[i].y, f, acc.y); acc.z = fmaf(x[i].z, f, acc.z); acc.w = fmaf(x[i].w, f, acc.w);
+            }
           }
           *reinterpret_cast<float4*>(sm_out + g * Sh::kOutStride + c) = acc;
           if (c == 0) { sm_m[g] = mm; sm_l[g] = sum; }
