@@ -300,6 +300,7 @@ const char* wkv_paged_config_error(const wkv_paged_config* cfg);
 /* Creates a handle on the current CUDA device.  Pools that the library takes from the provider start at zero.  The pools'
  * tensor maps are encoded here (bf16 and fp32 rows; WKV_ERR_CUDA if the driver lacks the encoder). */
 int wkv_paged_create(const wkv_paged_config* cfg, wkv_paged** out);
+/* Releases what the provider gave; the handle's calls are done by then.  NULL is accepted. */
 void wkv_paged_destroy(wkv_paged* c);
 int wkv_paged_set_stream(wkv_paged* c, void* stream);
 /* The pools' device addresses. */

@@ -344,6 +344,7 @@ class PagedCache:
         if rc != WKV_OK:
             raise WkvError(rc, lib().wkv_strerror(rc).decode())
         self._h = h
+        self._lib = lib()
 
     def _check(self, rc):
         if rc != WKV_OK:
@@ -375,11 +376,11 @@ class PagedCache:
     def _rows(self, name, t, n, heads):
         """Address and row stride of [n, heads, head_dim] whose rows may lie apart (columns of a wider projection)."""
         d = self.head_dim
-        row, head, one = t.stride() if t.dim() == 3 else (0, 0, 0)
+        strides = t.stride()
         if (t.dtype is not self.tdtype or t.get_device() != self._index or t.shape != (n, heads, d)
-                or (n > 0 and (one != 1 or (heads > 1 and head != d)))):
+                or (n > 0 and (strides[2] != 1 or (heads > 1 and strides[1] != d)))):
             raise WkvError(WKV_ERR_INVALID, f"{name} must be a {self.tdtype} tensor [{n}, {heads}, {d}] on {self.device} whose rows are packed")
-        return t.data_ptr(), (row if n > 1 else heads * d)
+        return t.data_ptr(), (strides[0] if n > 1 else heads * d)
 
     def _new_rows(self, k, v, n):
         if (k is None) != (v is None):
@@ -398,6 +399,9 @@ class PagedCache:
 
     # -- the C ABI, same names ----------------------------------------------------------------------
     def wkv_set_stream(self, stream):
+        if isinstance(stream, torch.cuda.Stream):
+            for buf in self._bufs.values():          # workspaces freed while that stream still uses them wait for it
+                buf.record_stream(stream)
         self._check(lib().wkv_paged_set_stream(self._h, C.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else stream)))
 
     def wkv_paged_decode(self, layer, q, k, v, block_table, seq_lens, out, window=0, sink=0, scores=None, lse=None):
@@ -405,11 +409,14 @@ class PagedCache:
         B, Hq, d = q.shape[0], self.n_q_heads, self.head_dim
         qp, qs = self._rows("q", q, B, Hq)
         kp, vp, ks = self._new_rows(k, v, B)
-        sp, ss = self._scores("scores", scores, B)
-        self._check(lib().wkv_paged_decode(
-            self._h, layer, B, qp, qs, kp, vp, ks, self._packed("block_table", block_table, torch.int32, B, -1),
-            block_table.shape[1], self._packed("seq_lens", seq_lens, torch.int32, B), window, sink, sp, ss,
-            self._packed("out", out, self.tdtype, B, Hq, d), self._packed("lse", lse, torch.float32, B, Hq)))
+        sp, ss = self._scores("scores", scores, B) if scores is not None else (None, 0)
+        tp = self._packed("block_table", block_table, torch.int32, B, -1)
+        np_ = self._packed("seq_lens", seq_lens, torch.int32, B)
+        op = self._packed("out", out, self.tdtype, B, Hq, d)
+        rc = self._lib.wkv_paged_decode(self._h, layer, B, qp, qs, kp, vp, ks, tp, block_table.shape[1], np_, window, sink, sp, ss, op,
+                                        None if lse is None else self._packed("lse", lse, torch.float32, B, Hq))
+        if rc:
+            self._check(rc)
 
     def wkv_paged_prefill(self, layer, q, k, v, q_start, block_table, seq_lens, out, window=0, sink=0, scores=None, lse=None):
         """q [T, Hq, d], k, v [T, Hkv, d] or None; sequence b's tokens are rows q_start[b] .. q_start[b + 1] - 1."""

@@ -236,6 +236,7 @@ int attention_params(wkv_paged* c, wkv::PagedParams& P, int32_t layer, int32_t b
 // All launches: programmatic stream serialization, each kernel waits for its predecessor first thing.
 template <typename... A, typename... B>
 cudaError_t launch(wkv_paged* c, void (*kernel)(A...), long long grid, int threads, size_t smem, B&&... args) {
+  if (grid < 1 || grid > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
   cudaLaunchConfig_t lc = {};
   lc.gridDim = dim3((unsigned)grid);
   lc.blockDim = dim3((unsigned)threads);
@@ -524,7 +525,10 @@ int wkv_paged_status(wkv_paged* c) {
   if (w) {
     WKV_CUDA(c, cudaMemset(c->status, 0, 4));
     // a piece that gave up may have left its lane's arrivals uncounted
-    if (w & wkv::kStatusWaitTimeout) WKV_CUDA(c, cudaMemset(c->arrived, 0, (size_t)c->cfg.max_batch * c->cfg.n_kv_heads * 4));
+    if (w & wkv::kStatusWaitTimeout) {
+      WKV_CUDA(c, cudaMemset(c->arrived, 0, (size_t)c->cfg.max_batch * c->cfg.n_kv_heads * 4));
+      WKV_CUDA(c, cudaMemset(c->item_counter, 0, 8));
+    }
     if (w & wkv::kStatusWaitTimeout) return fail(c, WKV_ERR_TIMEOUT, "a bounded wait inside a kernel gave up");
     return fail(c, WKV_ERR_STATE, "a page number, length or row offset was out of range, or an eviction's tables overlap");
   }

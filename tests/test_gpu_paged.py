@@ -300,6 +300,68 @@ def test_captured_steps_follow_new_lengths_and_tables():
     cache.close()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_captured_prompt_and_eviction(dtype):
+    """A prompt call and an eviction captured once, replayed for batches of other lengths, interleaved with a second handle's
+    calls on another stream."""
+    B, hq, hk, d, page, T, width = 3, 8, 2, 64, 16, 300, 24
+    tdt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    base = Case(lens=[1] * B, new=[1] * B, hq=hq, hk=hk, d=d, dtype=dtype, page=page, scores=True, seed=31, spare=2 * B * width, width=width)
+    pages = torch.randperm(base.n_pages, generator=torch.Generator().manual_seed(5)).int()
+    table, dst = pages[:B * width].reshape(B, width).cuda(), pages[B * width:2 * B * width].reshape(B, width).cuda()
+    cache = base.cache()
+    side, other_stream = torch.cuda.Stream(), torch.cuda.Stream()
+    other = Case(lens=[200, 3], new=[150, 3], hq=hq, hk=hk, d=d, dtype=dtype, page=page, scores=True, seed=32)
+    with torch.cuda.stream(other_stream):
+        other_cache = other.cache()
+    q, k, v = (torch.zeros(T, h, d, dtype=tdt, device="cuda") for h in (hq, hk, hk))
+    out, lse = torch.zeros(T, hq, d, dtype=tdt, device="cuda"), torch.zeros(T, hq, device="cuda")
+    scores, kept = torch.zeros(B, hk, width * page, device="cuda"), torch.zeros(B, hk, 40, dtype=torch.int32, device="cuda")
+    scores_out = torch.zeros(B, hk, 40, device="cuda")
+    starts, lens, new_lens = (torch.zeros(n, dtype=torch.int32, device="cuda") for n in (B + 1, B, B))
+    cache.wkv_set_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        cache.wkv_paged_prefill(0, q, k, v, starts, table, lens, out, window=70, sink=3, scores=scores, lse=lse)
+        cache.wkv_paged_evict(0, table, dst, lens, new_lens, 40, 10, 3, scores=scores, scores_out=scores_out, kept=kept)
+    for new in ([100, 1, 30], [0, 299, 1], [64, 65, 128]):
+        c = Case(lens=new, new=new, hq=hq, hk=hk, d=d, dtype=dtype, page=page, scores=True, seed=sum(new), width=width, window=70, sink=3,
+                 prefill=True, extra_rows=T - sum(new))
+        cq, ck, cv = c.rows()
+        q.copy_(cq); k.copy_(ck); v.copy_(cv)
+        out.fill_(7); lse.fill_(7); scores.copy_(c.scores); kept.fill_(-1)
+        starts.copy_(torch.tensor(c.starts, dtype=torch.int32)); lens.copy_(torch.tensor(new, dtype=torch.int32))
+        torch.cuda.synchronize()
+        graph.replay()
+        with torch.cuda.stream(other_stream):
+            result = other.run(other_cache)
+        torch.cuda.synchronize()
+        c.check_pool = lambda what="": None
+        c.check(out, lse, scores, f"replay {new}")
+        other.check(*result, "beside it")
+        assert new_lens.tolist() == [min(n, 40) for n in new]
+        for b in range(B):
+            for h in range(hk):
+                i = kept[b, h, :min(new[b], 40)].long().cpu()
+                assert torch.equal(scores_out[b, h, :len(i)].cpu(), scores[b, h].cpu()[i]) and (i[1:] > i[:-1]).all()
+                for at in range(0, len(i), 7):
+                    got = base.gk[0, int(dst[b, at // page]), h, at % page].cpu()
+                    assert torch.equal(got, c.K[b][int(i[at]), h])
+    assert cache.wkv_status() == 0 and other_cache.wkv_status() == 0
+    del graph
+    cache.close()
+    other_cache.close()
+
+
+@pytest.mark.parametrize("prefill", [False, True])
+def test_logits_that_tower_over_all_before(prefill):
+    """The softmax's running reference has to follow: keys 25 times as long as the others turn up late."""
+    for dtype in ("bf16", "f32"):
+        run_and_check("spikes", lens=[700, 300], new=[700, 130] if prefill else [1, 1], hq=8, hk=2, d=128, dtype=dtype, page=16, scores=True,
+                      seed=41, spikes=0.02, prefill=prefill)
+
+
 @pytest.mark.parametrize("prefill", [False, True])
 def test_bad_tables_and_lengths_are_reported_and_touch_nothing_else(prefill):
     new = [40, 30, 20] if prefill else [1, 1, 1]
