@@ -439,6 +439,46 @@ def test_large_pool_offsets():
     cache.close()
 
 
+def test_memory_provider_failing_at_every_request():
+    """wkv_paged_create asks for one block after the other; whichever is refused, it returns WKV_ERR_ALLOC and hands all back."""
+    import ctypes as C
+    L = binding.lib()
+    for pools in (False, True):
+        kp, vp = (torch.zeros(2, 4, 2, 16, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        fail_at, n = 0, 1
+        while fail_at < n:
+            live, count = {}, [0]
+
+            def alloc(nbytes, _user):
+                count[0] += 1
+                if count[0] - 1 == fail_at:
+                    return None
+                buf = torch.empty(int(nbytes), dtype=torch.uint8, device="cuda")
+                live[buf.data_ptr()] = buf
+                return buf.data_ptr()
+
+            a, r = binding.ALLOC_FN(alloc), binding.RELEASE_FN(lambda p, _user: live.__delitem__(p))
+            cfg = binding.make_paged_config(2, 4, 16, 4, 2, 64, 2, 4, scores=1, k_pool=kp.data_ptr() if pools else None,
+                                            v_pool=vp.data_ptr() if pools else None)
+            cfg.alloc, cfg.release = a, r
+            h = C.c_void_p()
+            rc = L.wkv_paged_create(C.byref(cfg), C.byref(h))
+            if fail_at == 0 and n == 1:                       # how many requests a creation makes
+                assert rc == binding.WKV_ERR_ALLOC and not h.value and not live
+                fail_at = 1 << 30
+                count[0] = 0
+                rc = L.wkv_paged_create(C.byref(cfg), C.byref(h))
+                assert rc == binding.WKV_OK and L.wkv_paged_device_bytes(h) > 0
+                n, fail_at = count[0], 1
+                torch.cuda.synchronize()
+                L.wkv_paged_destroy(h)
+                assert not live
+                continue
+            assert rc == binding.WKV_ERR_ALLOC and not h.value and not live, f"request {fail_at}"
+            fail_at += 1
+        assert n >= (8 if pools else 10)
+
+
 def test_refusals():
     c = Case(lens=[40, 20], new=[1, 1], hq=4, hk=2, d=64, page=16, scores=True, seed=14)
     cache = c.cache()
