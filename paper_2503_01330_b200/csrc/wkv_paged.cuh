@@ -340,37 +340,47 @@ __global__ void __launch_bounds__(kSelectThreads) paged_select_kernel(const Evic
   if (in_stage) select(StagedKeys{stage}); else select(from_memory);
 }
 
-// Rows of K and V to their new pages, 16 bytes a step, kMoveSteps steps of a thread in flight together (the chain of loads in
-// front of each -- kept index, page, row -- is what takes the time).
-constexpr int kMoveThreads = 256, kMoveSteps = 4;
+// Rows of K and V to their new pages.  A warp takes 32 entries: each lane looks one up (kept index, page, new page -- the chain of
+// loads is what would take the time otherwise), then the warp copies them together, 16 bytes a lane and kMoveSteps steps in flight.
+constexpr int kMoveThreads = 256, kMoveEntries = kMoveThreads, kMoveSteps = 8;     // entries per CTA: 32 a warp
 template <typename T, int D>
 __global__ void __launch_bounds__(kMoveThreads) paged_move_kernel(const EvictParams P, int blocks_per_lane) {
   griddep_wait();
-  const int bh = blockIdx.x / blocks_per_lane, part = blockIdx.x % blocks_per_lane;
+  const int bh = blockIdx.x / blocks_per_lane, part = blockIdx.x % blocks_per_lane, lane = threadIdx.x & 31;
   const int b = bh / P.n_kv_heads, head = bh % P.n_kv_heads, n = P.n_moved[bh];
-  constexpr int kVec = 2 * D * (int)sizeof(T) / 16;    // 16-byte pieces of an entry: K row, then V row
-  constexpr int kEach = 16 / (int)sizeof(T);
-  const long long total = (long long)n * kVec, at0 = (long long)part * kMoveThreads * kMoveSteps + threadIdx.x;
-  uint4 piece[kMoveSteps];
-  T* to[kMoveSteps];
-#pragma unroll
-  for (int k = 0; k < kMoveSteps; ++k) {
-    const long long at = at0 + k * kMoveThreads;
-    to[k] = nullptr;
-    if (at >= total) continue;
-    const int i = (int)(at / kVec), c = (int)(at % kVec);
+  const int first = part * kMoveEntries + (threadIdx.x >> 5) * 32, i = first + lane;
+  if (first >= n) return;
+  constexpr uint32_t kNone = 0xffffffffu;
+  uint32_t from = kNone, to = kNone;                   // rows of the layer's pools (a row is 128 bytes at least: 32 bits suffice)
+  if (i < n) {
     const int src = P.kept[(long long)bh * P.kept_stride + i];
     const int sp = P.src_table[(long long)b * P.src_width + (src >> P.page_shift)];
     const int dp = P.dst_table[(long long)b * P.dst_width + (i >> P.page_shift)];
-    if ((unsigned)sp >= (unsigned)P.n_pages || (unsigned)dp >= (unsigned)P.n_pages) continue;
-    const int e = (c % (kVec / 2)) * kEach;
-    T* pool = static_cast<T*>(c < kVec / 2 ? P.k_pool : P.v_pool);
-    piece[k] = __ldcs(reinterpret_cast<const uint4*>(pool + ((((long long)sp * P.n_kv_heads + head) << P.page_shift) + (src & (P.page - 1))) * D + e));
-    to[k] = pool + ((((long long)dp * P.n_kv_heads + head) << P.page_shift) + (i & (P.page - 1))) * D + e;
+    if ((unsigned)sp < (unsigned)P.n_pages && (unsigned)dp < (unsigned)P.n_pages) {
+      from = (((uint32_t)sp * P.n_kv_heads + head) << P.page_shift) + (src & (P.page - 1));
+      to = (((uint32_t)dp * P.n_kv_heads + head) << P.page_shift) + (i & (P.page - 1));
+    }
   }
+  constexpr int kVec = 2 * D * (int)sizeof(T) / 16;    // 16-byte pieces of an entry: K row, then V row
+  constexpr int kEach = 16 / (int)sizeof(T);
+#pragma unroll 1
+  for (int s0 = 0; s0 < kVec; s0 += kMoveSteps) {
+    uint4 piece[kMoveSteps];
 #pragma unroll
-  for (int k = 0; k < kMoveSteps; ++k)
-    if (to[k]) *reinterpret_cast<uint4*>(to[k]) = piece[k];
+    for (int k = 0; k < kMoveSteps; ++k) {
+      const int at = (s0 + k) * 32 + lane, c = at % kVec;
+      const uint32_t row = __shfl_sync(~0u, from, at / kVec);
+      const T* pool = static_cast<const T*>(c < kVec / 2 ? P.k_pool : P.v_pool);
+      if (row != kNone) piece[k] = __ldcs(reinterpret_cast<const uint4*>(pool + (long long)row * D + c % (kVec / 2) * kEach));
+    }
+#pragma unroll
+    for (int k = 0; k < kMoveSteps; ++k) {
+      const int at = (s0 + k) * 32 + lane, c = at % kVec;
+      const uint32_t row = __shfl_sync(~0u, to, at / kVec);
+      T* pool = static_cast<T*>(c < kVec / 2 ? P.k_pool : P.v_pool);
+      if (row != kNone) *reinterpret_cast<uint4*>(pool + (long long)row * D + c % (kVec / 2) * kEach) = piece[k];
+    }
+  }
 }
 
 }  // namespace wkv

@@ -505,7 +505,7 @@ int wkv_paged_evict(wkv_paged* c, int32_t layer, int32_t batch, const int32_t* s
   const int staged = (int)std::min<int64_t>((most + wkv::kSelectThreads - 1) / wkv::kSelectThreads * wkv::kSelectThreads, wkv::kSelectStaged);
   cudaError_t e = launch(c, wkv::paged_select_kernel, lanes, wkv::kSelectThreads, (size_t)staged * 4, P, staged);
   if (e == cudaSuccess) {
-    const int per_lane = (int)((left * 2 * f.head_dim * (int64_t)c->elem / 16 + wkv::kMoveThreads * wkv::kMoveSteps - 1) / (wkv::kMoveThreads * wkv::kMoveSteps));
+    const int per_lane = (int)((left + wkv::kMoveEntries - 1) / wkv::kMoveEntries);
     const bool wide = f.head_dim == 128;
     auto kernel = f.dtype == WKV_BF16 ? (wide ? wkv::paged_move_kernel<__nv_bfloat16, 128> : wkv::paged_move_kernel<__nv_bfloat16, 64>)
                                       : (wide ? wkv::paged_move_kernel<float, 128> : wkv::paged_move_kernel<float, 64>);
