@@ -37,7 +37,7 @@ struct wkv_paged {
   float2* part_ml = nullptr;
   uint32_t* arrived = nullptr;
   // prompts: the runs' outputs, next item
-  float* run_part = nullptr;
+  float4* run_part = nullptr;
   float2* run_ml = nullptr;
   uint32_t* item_counter = nullptr;
   // the pools as [chunk][part][row][128 bytes], boxes of a page's rows (at most a decode tile's) x all parts
@@ -279,17 +279,18 @@ int decode(wkv_paged* c, const wkv::PagedParams& A) {
   return WKV_OK;
 }
 
-// What the prompt kernels share: row blocks of ROWS rows, and runs of the key tiles -- as many as the SMs can use when the row
-// blocks alone are fewer, at least `least` entries each.
-int prefill_params(wkv_paged* c, wkv::PrefillParams& P, const wkv::PagedParams& A, int rows, long long least, long long* units) {
+// What the prompt kernels share.  units: row blocks (of `rows` rows) x kv heads, at most; items: with the runs that they may be cut
+// into (see work_plan), at most.  A call whose tokens alone make row blocks enough for half the slots is not cut.
+int prefill_params(wkv_paged* c, wkv::PrefillParams& P, const wkv::PagedParams& A, int rows, int keys, long long* units, long long* items) {
   std::memset(&P, 0, sizeof(P));
   P.A = A;
   P.g_shift = c->group == 1 ? 0 : c->group == 2 ? 1 : c->group == 4 ? 2 : 3;
-  *units = ((long long)A.rows * c->group / rows + A.batch) * A.n_kv_heads;
-  const long long most = run_rows(c) / rows;
-  P.splits = (int)std::max<long long>(1, std::min<long long>(most / *units, (long long)A.width * A.page / least));
-  if (*units * P.splits > 0x3fffffff) return fail(c, WKV_ERR_INVALID, "total_q * n_q_heads is too large");
-  P.items = (int)(*units * P.splits);
+  const long long slots = (long long)(run_rows(c) / rows), full = (long long)A.rows * c->group / rows;
+  if (2 * A.n_kv_heads * std::max(1LL, full - A.batch) <= slots) P.slots = (int)slots;
+  *units = (full + A.batch) * A.n_kv_heads;
+  if (*units > 0x3fffffff) return fail(c, WKV_ERR_INVALID, "total_q * n_q_heads is too large");
+  const long long tiles = ((long long)A.width * A.page + keys - 1) / keys;
+  *items = std::max<long long>(*units, std::min<long long>(P.slots, *units * tiles));
   P.counter = c->item_counter; P.part = c->run_part; P.part_ml = c->run_ml;
   P.oob_chunk = c->cfg.n_layers * c->cfg.n_pages * c->cfg.n_kv_heads;
   P.chunk0 = chunk0(c, A);
@@ -300,8 +301,8 @@ int prefill_params(wkv_paged* c, wkv::PrefillParams& P, const wkv::PagedParams& 
 template <int D>
 int prefill_bf16(wkv_paged* c, const wkv::PagedParams& A) {
   wkv::PrefillParams P;
-  long long units;
-  int rc = prefill_params(c, P, A, wkv::kPrefillRows, 4 * wkv::kPrefillKeys, &units);
+  long long units, items;
+  int rc = prefill_params(c, P, A, wkv::kPrefillRows, wkv::kPrefillKeys, &units, &items);
   if (rc == WKV_OK) rc = encode_rows(c, P.qmap, A.q, A.q_stride, A.n_q_heads, A.rows, c->group, 128 / c->group);
   if (rc == WKV_OK && A.k) {
     P.append = 1;
@@ -312,8 +313,8 @@ int prefill_bf16(wkv_paged* c, const wkv::PagedParams& A) {
   if (A.k) WKV_CUDA(c, launch(c, wkv::paged_append_edge_kernel<__nv_bfloat16, D>, (long long)A.batch * A.page, wkv::kAppendThreads, 0, A));
   std::memcpy(P.kmap, c->part_kmap, 128);
   std::memcpy(P.vmap, c->part_vmap, 128);
-  WKV_CUDA(c, launch(c, wkv::paged_prefill_kernel<D>, std::min(P.items, c->sm_count), wkv::kPrefillThreads, wkv::PrefillShape<D>::kSmem, P));
-  if (P.splits > 1) WKV_CUDA(c, launch(c, wkv::paged_prefill_join_kernel<__nv_bfloat16, D, wkv::kPrefillRows>, units * (wkv::kPrefillRows / 32), 256, 0, P));
+  WKV_CUDA(c, launch(c, wkv::paged_prefill_kernel<D>, (int)std::min<long long>(items, c->sm_count), wkv::kPrefillThreads, wkv::PrefillShape<D>::kSmem, P));
+  if (P.slots) WKV_CUDA(c, launch(c, wkv::paged_prefill_join_kernel<__nv_bfloat16, D, wkv::kPrefillRows, wkv::kPrefillKeys>, units * (wkv::kPrefillRows / 32), 256, 0, P));
   if (A.scores) {
     const long long blocks = ((long long)A.width * A.page + 255) / 256;
     WKV_CUDA(c, launch(c, wkv::paged_weights_tc_kernel<D>, blocks * A.batch * A.n_kv_heads, wkv::kWeightsThreads, wkv::WeightsShape<D>::kSmem, P));
@@ -324,12 +325,12 @@ int prefill_bf16(wkv_paged* c, const wkv::PagedParams& A) {
 template <int D>
 int prefill_f32(wkv_paged* c, const wkv::PagedParams& A) {
   wkv::PrefillParams P;
-  long long units;
-  const int rc = prefill_params(c, P, A, wkv::kF32Rows, 2 * wkv::kF32Keys, &units);
+  long long units, items;
+  const int rc = prefill_params(c, P, A, wkv::kF32Rows, wkv::kF32Keys, &units, &items);
   if (rc != WKV_OK) return rc;
   if (A.k) WKV_CUDA(c, launch(c, wkv::paged_append_kernel<float, D>, A.rows, wkv::kAppendThreads, 0, A));
-  WKV_CUDA(c, launch(c, wkv::paged_prefill_f32_kernel<D>, P.items, wkv::kF32Threads, wkv::F32Shape<D>::kSmem, P));
-  if (P.splits > 1) WKV_CUDA(c, launch(c, wkv::paged_prefill_join_kernel<float, D, wkv::kF32Rows>, units * (wkv::kF32Rows / 32), 256, 0, P));
+  WKV_CUDA(c, launch(c, wkv::paged_prefill_f32_kernel<D>, items, wkv::kF32Threads, wkv::F32Shape<D>::kSmem, P));
+  if (P.slots) WKV_CUDA(c, launch(c, wkv::paged_prefill_join_kernel<float, D, wkv::kF32Rows, wkv::kF32Keys>, units * (wkv::kF32Rows / 32), 256, 0, P));
   if (A.scores) {
     const long long blocks = ((long long)A.width * A.page + wkv::kF32Rows - 1) / wkv::kF32Rows;
     WKV_CUDA(c, launch(c, wkv::paged_weights_f32_kernel<D>, blocks * A.batch * A.n_kv_heads, wkv::kF32Groups * wkv::kF32Threads, wkv::F32Shape<D>::kWeightsSmem, P));
@@ -389,7 +390,7 @@ int wkv_paged_create(const wkv_paged_config* cfg, wkv_paged** out) {
   WKV_TAKE(&c->arrived, lanes * 4);
   WKV_TAKE(&c->run_part, run_rows(c) * cfg->head_dim * 4);
   WKV_TAKE(&c->run_ml, run_rows(c) * 8);
-  WKV_TAKE(&c->item_counter, 8);
+  WKV_TAKE(&c->item_counter, 12);
   const bool own_pools = !c->k_pool;
   if (own_pools) {
     WKV_TAKE(&c->k_pool, pool);

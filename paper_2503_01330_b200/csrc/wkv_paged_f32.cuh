@@ -72,11 +72,15 @@ __global__ void __launch_bounds__(kF32Threads) paged_prefill_f32_kernel(const __
   const PagedParams& A = P.A;
   griddep_launch();
   griddep_wait();
-  const int split = blockIdx.x % P.splits, unit = blockIdx.x / P.splits;
+  const WorkPlan plan = work_plan<kF32Rows, kF32Keys>(A, P.g_shift, P.slots);
+  if (blockIdx.x == 0 && threadIdx.x == 0) P.counter[2] = (uint32_t)plan.run;      // for the join
+  if ((int)blockIdx.x >= plan.items) return;                // the grid is an upper bound
   PrefillBlock B;
-  if (!find_block<kF32Rows>(A, P.g_shift, unit / A.n_kv_heads, unit % A.n_kv_heads, B)) return;
+  int r, runs, first_item, v0, v1;
+  if (!find_item<kF32Rows, kF32Keys, false>(A, P.g_shift, plan.run, blockIdx.x / A.n_kv_heads, blockIdx.x % A.n_kv_heads, B, r, runs, first_item) ||
+      !run_of<kF32Keys>(B, r, runs, plan.run, v0, v1))
+    return;
   const int tid = threadIdx.x, ty = tid >> 3, tx = tid & 7;
-  const int tiles = (B.entries + kF32Keys - 1) / kF32Keys, v0 = (int)((long long)tiles * split / P.splits), v1 = (int)((long long)tiles * (split + 1) / P.splits);
   constexpr int kVec = D / 4, kRowsPerPass = kF32Threads / kVec;
   const int vec = tid % kVec;
 #pragma unroll 8
@@ -175,7 +179,7 @@ __global__ void __launch_bounds__(kF32Threads) paged_prefill_f32_kernel(const __
     const int row = ty + 16 * i, R = B.row0 + row;
     if (R >= B.n << P.g_shift) continue;
     const bool seen = !(sum <= 0.f);
-    if (P.splits == 1) {
+    if (plan.run == 0x7fffffff) {
       const float inv = seen ? 1.f / sum : 0.f;
       const long long at = (long long)(B.first + (R >> P.g_shift)) * A.n_q_heads + (B.head << P.g_shift) + (R & ((1 << P.g_shift) - 1));
 #pragma unroll
@@ -184,10 +188,9 @@ __global__ void __launch_bounds__(kF32Threads) paged_prefill_f32_kernel(const __
             make_float4(o[i][j].x * inv, o[i][j].y * inv, o[i][j].z * inv, o[i][j].w * inv);
       if (A.lse && tx == 0) A.lse[at] = seen ? (m[i] + log2f(sum)) * kLn2 : -INFINITY;
     } else {
-      const long long at = (long long)blockIdx.x * kF32Rows + row;
 #pragma unroll
-      for (int j = 0; j < kPieces; ++j) *reinterpret_cast<float4*>(P.part + at * D + j * 32 + tx * 4) = o[i][j];
-      if (tx == 0) P.part_ml[at] = make_float2(seen ? m[i] : -INFINITY, seen ? sum : 0.f);
+      for (int j = 0; j < kPieces; ++j) P.part[((long long)blockIdx.x * (D / 4) + j * 8 + tx) * kF32Rows + row] = o[i][j];
+      if (tx == 0) P.part_ml[(long long)blockIdx.x * kF32Rows + row] = make_float2(seen ? m[i] : -INFINITY, seen ? sum : 0.f);
     }
   }
 }

@@ -7,8 +7,8 @@
 //
 // An item of work is 256 rows of one kv head -- a row being (token, query head of the group), token-major: grouped heads share a
 // tile, so a row tile spans 128 / G tokens and a window wastes little of it -- and a share of the key tiles that they see: all of
-// them, or one of `splits` equal runs where there are too few row blocks to fill the GPU (chunks of a few tokens behind long
-// contexts); paged_prefill_join_kernel then joins the runs.  One CTA per SM takes items from a counter until there are none: the
+// them, or a run of a few tiles where there are too few row blocks to fill the GPU (chunks of a few tokens behind long contexts);
+// paged_prefill_join_kernel then joins the runs.  One CTA per SM takes items from a counter until there are none: the
 // copies of the next item run while the last one's outputs are written.
 //
 // Two row tiles of 128 take turns: while one's logits are in its softmax warps, the tensor cores work on the other's.  Warps 0-3
@@ -39,11 +39,10 @@ constexpr int kPrefillKeys = 128;            // entries per tile
 struct PrefillParams {
   PagedParams A;
   int g_shift;               // log2 of the query heads per kv head
-  int items;                 // row blocks (at most) x kv heads x splits
-  int splits;
-  uint32_t* counter;         // next item, next eight new rows; zero between launches
-  float* part;               // [row block x kv head][split][256][D] outputs, where splits > 1
-  float2* part_ml;           // [row block x kv head][split][256] (maximum in base-2 logits, sum)
+  int slots;                 // items that a call whose row blocks are cut into runs may have; 0: this call is not cut
+  uint32_t* counter;         // next item, next eight new rows (zero between launches); tiles of a run
+  float4* part;              // [item][D / 4][rows] outputs of runs, four channels of a row together
+  float2* part_ml;           // [item][rows] (maximum in base-2 logits, sum)
   int oob_chunk, chunk0;
   int append;                // the call brings k and v, and this kernel stores what paged_append_edge_kernel has not
   alignas(64) unsigned char qmap[128];   // q as [part][token][head][64 elements], boxes of a row tile
@@ -106,31 +105,80 @@ __device__ __forceinline__ bool tile_whole(const PrefillBlock& B, const RowTile&
   return e0 + kPrefillKeys - 1 <= t.pos_lo && (window == 0 || e0 >= t.pos_hi - window + 1 || e0 + kPrefillKeys <= sink);
 }
 
-// The rb-th block of ROWS rows over all sequences; false if there is none.  Every warp searches for itself.
-template <int ROWS>
-__device__ __forceinline__ bool find_block(const PagedParams& A, int g_shift, int rb, int head, PrefillBlock& B) {
+// How a call's work is cut: row blocks of ROWS rows, and where there are too few of them to fill the GPU, their key tiles (KEYS
+// entries) into runs of `run` tiles, so that no more than `slots` items come out: a sequence whose row blocks walk t tiles has
+// ceil(t / run) <= t / run + 1 runs each.  Every warp computes it from the lengths, so that a captured call follows new ones, and a
+// ragged batch's short sequences are not cut as finely as its longest.
+struct WorkPlan {
+  int run;                   // tiles of a run; the largest int where nothing is cut
+  int items;                 // (row block, run, kv head)
+};
+// Row blocks of sequence b (0 behind the last), and the tiles that one walks at most.
+template <int ROWS, int KEYS>
+__device__ __forceinline__ void sequence_work(const PagedParams& A, int g_shift, int b, int& blocks, int& tiles) {
+  blocks = tiles = 0;
+  if (b >= A.batch) return;
+  const int lo = min(max(A.q_start[b], 0), A.rows), hi = min(max(A.q_start[b + 1], lo), A.rows);
+  blocks = (int)((((long long)(hi - lo) << g_shift) + ROWS - 1) / ROWS);
+  const long long len = clamped_len(A, b), walked = A.window > 0 ? min(len, (long long)A.window + A.sink + ROWS + 2 * A.page) : len;
+  tiles = (int)((walked + KEYS - 1) / KEYS);
+}
+__device__ __forceinline__ int runs_of(int tiles, int run) { return tiles <= run ? 1 : (tiles + run - 1) / run; }
+
+template <int ROWS, int KEYS>
+__device__ __forceinline__ WorkPlan work_plan(const PagedParams& A, int g_shift, int slots) {
   const int lane = threadIdx.x & 31;
-  int before = 0;
-  for (int base = 0; base < A.batch; base += 32) {
-    const int b = base + lane;
-    int n = 0;
-    if (b < A.batch) {
-      const int lo = min(max(A.q_start[b], 0), A.rows), hi = min(max(A.q_start[b + 1], lo), A.rows);
-      n = (int)((((long long)(hi - lo) << g_shift) + ROWS - 1) / ROWS);
+  WorkPlan w{0x7fffffff, 0};
+#pragma unroll 1
+  for (int pass = 0; pass < 2; ++pass) {
+    long long units = 0, all = 0;                      // row blocks; their tiles, then their runs
+    for (int b = lane; b < A.batch; b += 32) {
+      int blocks, tiles;
+      sequence_work<ROWS, KEYS>(A, g_shift, b, blocks, tiles);
+      units += blocks;
+      all += (long long)blocks * (pass == 0 ? tiles : runs_of(tiles, w.run));
     }
-    int upto = n;
+#pragma unroll
+    for (int off = 16; off; off >>= 1) {
+      units += __shfl_xor_sync(~0u, units, off);
+      all += __shfl_xor_sync(~0u, all, off);
+    }
+    w.items = (int)((pass == 0 ? units : all) * A.n_kv_heads);
+    if (pass == 1) break;
+    const long long more = (long long)slots - w.items;
+    if (more < w.items) break;                         // the row blocks are many enough
+    w.run = (int)max(KEYS < 64 ? 2LL : 4LL, (all * A.n_kv_heads + more - 1) / more);
+  }
+  return w;
+}
+
+// Item x of one kv head's -- or, UNIT, the first item of row block x: row block, run r of its `runs`, and that first item's number;
+// false if there is none.  Every warp searches for itself.
+template <int ROWS, int KEYS, bool UNIT>
+__device__ __forceinline__ bool find_item(const PagedParams& A, int g_shift, int run, int x, int head, PrefillBlock& B, int& r, int& runs, int& first_item) {
+  const int lane = threadIdx.x & 31;
+  int before = 0, items = 0;                           // what x counts, and items, of the sequences before
+  for (int base = 0; base < A.batch; base += 32) {
+    int blocks, tiles;
+    sequence_work<ROWS, KEYS>(A, g_shift, base + lane, blocks, tiles);
+    const int n = runs_of(tiles, run), mine = UNIT ? blocks : blocks * n;
+    int upto = mine, upto_items = blocks * n;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
-      const int y = __shfl_up_sync(~0u, upto, off);
-      if (lane >= off) upto += y;
+      const int y = __shfl_up_sync(~0u, upto, off), z = __shfl_up_sync(~0u, upto_items, off);
+      if (lane >= off) { upto += y; upto_items += z; }
     }
-    const uint32_t behind = __ballot_sync(~0u, rb < before + upto);
+    const uint32_t behind = __ballot_sync(~0u, x < before + upto);
     if (behind) {
       const int at = __ffs(behind) - 1;
-      const int blocks = __shfl_sync(~0u, n, at), skipped = before + __shfl_sync(~0u, upto, at) - blocks;
+      const int all = __shfl_sync(~0u, blocks, at), y = x - before - __shfl_sync(~0u, upto - mine, at);
+      runs = __shfl_sync(~0u, n, at);
+      r = UNIT ? 0 : y % runs;
+      const int block = UNIT ? y : y / runs;
+      first_item = items + __shfl_sync(~0u, upto_items - blocks * n, at) + block * runs;
       const SeqRows s = seq_rows(A, base + at);
       B.b = base + at; B.head = head; B.first = s.first; B.n = s.n; B.len = s.len; B.old = s.len - s.n;
-      B.row0 = (blocks - 1 - (rb - skipped)) * ROWS;   // a sequence's last rows see most: they start first
+      B.row0 = (all - 1 - block) * ROWS;               // a sequence's last rows see most: they start first
       const int p0 = B.old + (B.row0 >> g_shift);                              // positions of the block's tokens
       const int p1 = min(B.old + ((B.row0 + ROWS - 1) >> g_shift), B.len - 1);
       const int lo_key = A.window > 0 ? max(0, p0 - A.window + 1) : 0;
@@ -140,8 +188,17 @@ __device__ __forceinline__ bool find_block(const PagedParams& A, int g_shift, in
       return true;
     }
     before += __shfl_sync(~0u, upto, 31);
+    items += __shfl_sync(~0u, upto_items, 31);
   }
   return false;
+}
+// Run r of a row block: its tiles [v0, v1); false if it has none, but for the first run.
+template <int KEYS>
+__device__ __forceinline__ bool run_of(const PrefillBlock& B, int r, int runs, int run, int& v0, int& v1) {
+  const int tiles = (B.entries + KEYS - 1) / KEYS;
+  v0 = (int)min((long long)tiles, (long long)r * run);
+  v1 = r == runs - 1 ? tiles : (int)min((long long)tiles, (long long)(r + 1) * run);
+  return r == 0 || v0 < v1;
 }
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -170,7 +227,8 @@ __device__ __forceinline__ void unpair(uint64_t d, float& lo, float& hi) { asm("
 struct PrefillItem {
   PrefillBlock B;
   int v0, v1;                // its key tiles
-  int slot;                  // (row block x kv head) * splits + split; -1: no more items
+  int slot;                  // -1: no more items
+  int whole;                 // not a run: the output is final
 };
 static_assert(sizeof(PrefillItem) <= 64, "two of them in 128 bytes of shared memory");
 
@@ -269,6 +327,8 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == 10) {
       // ---- items
+      const WorkPlan plan = work_plan<kPrefillRows, kPrefillKeys>(A, P.g_shift, P.slots);
+      if (blockIdx.x == 0 && lane == 0) P.counter[2] = (uint32_t)plan.run;       // for the join
       for (int n = 0;; ++n) {
         PrefillItem item;
         item.slot = -1;
@@ -276,15 +336,15 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
           uint32_t w = 0;
           if (lane == 0) w = atomicAdd(P.counter, 1u);
           w = __shfl_sync(~0u, w, 0);
-          if (w >= (uint32_t)P.items) {
-            if (lane == 0 && w == (uint32_t)P.items + gridDim.x - 1) *P.counter = 0;      // the last CTA to ask
+          if (w >= (uint32_t)plan.items) {
+            if (lane == 0 && w == (uint32_t)plan.items + gridDim.x - 1) *P.counter = 0;      // the last CTA to ask
             break;
           }
-          const int split = w % P.splits, unit = w / P.splits;
-          if (!find_block<kPrefillRows>(A, P.g_shift, unit / A.n_kv_heads, unit % A.n_kv_heads, item.B)) continue;     // `items` is an upper bound
-          const int tiles = (item.B.entries + kPrefillKeys - 1) / kPrefillKeys;
-          item.v0 = (int)((long long)tiles * split / P.splits);
-          item.v1 = (int)((long long)tiles * (split + 1) / P.splits);
+          int r, runs, first_item;
+          if (!find_item<kPrefillRows, kPrefillKeys, false>(A, P.g_shift, plan.run, w / A.n_kv_heads, w % A.n_kv_heads, item.B, r, runs, first_item) ||
+              !run_of<kPrefillKeys>(item.B, r, runs, plan.run, item.v0, item.v1))
+            continue;
+          item.whole = plan.run == 0x7fffffff;
           item.slot = (int)w;
           break;
         }
@@ -536,10 +596,10 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
       mbar_wait_fast(o_full, n & 1, A.status);
       tcgen05_after_sync();
       const bool seen = !(l <= 0.f);                            // else the row's TMEM lane may hold anything
-      const float inv = !seen ? 0.f : P.splits == 1 ? 1.f / l : 1.f;
+      const float inv = seen ? 1.f / l : 0.f;
       // rows of the eight lanes that exchange pieces, and this lane's 16-byte piece of 128
       const int row8 = t * 128 + (row & ~7), piece = lane & 7;
-      if (P.splits == 1) {
+      if (item.whole) {
 #pragma unroll 1
         for (int i = 0; i < D / 64; ++i) {
           uint32_t o[64], y[8][4];
@@ -563,21 +623,21 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
           A.lse[at] = seen ? (m * c + log2f(l)) * kLn2 : -INFINITY;
         }
       } else {
+        // a warp's store covers 32 rows' same four channels, which lie side by side
+        float4* part = P.part + (long long)item.slot * (D / 4) * kPrefillRows + t * 128 + row;
 #pragma unroll 1
         for (int i = 0; i < D / 32; ++i) {
-          uint32_t o[32], y[8][4];
+          uint32_t o[32];
           tmem_load32(o_at + i * 32, o);
           tmem_wait_loads();
+          if (live && seen) {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) y[e >> 2][e & 3] = seen ? o[e] : 0u;
-          exchange_pieces(y);
-#pragma unroll
-          for (int r = 0; r < 8; ++r) {
-            if ((B.row0 + row8 + r) >> P.g_shift >= B.n) break;
-            reinterpret_cast<uint4*>(P.part + ((long long)item.slot * 256 + row8 + r) * D + i * 32)[piece] = make_uint4(y[r][0], y[r][1], y[r][2], y[r][3]);
+            for (int e = 0; e < 8; ++e)
+              part[(i * 8 + e) * kPrefillRows] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]),
+                                                             __uint_as_float(o[4 * e + 3]));
           }
         }
-        if (live) P.part_ml[(long long)item.slot * 256 + t * 128 + row] = make_float2(seen ? m * c : -INFINITY, seen ? l : 0.f);
+        if (live) P.part_ml[(long long)item.slot * kPrefillRows + t * 128 + row] = make_float2(seen ? m * c : -INFINITY, seen ? l : 0.f);
       }
       tcgen05_before_sync();
       __syncwarp();
@@ -593,33 +653,38 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
   }
 }
 
-// The runs of a row block (ROWS rows) joined: eight threads per row, 32 rows per CTA.
-template <typename T, int D, int ROWS>
+// The runs of a row block (ROWS rows) joined: 32 rows per CTA, eight threads per row, a warp on the same channels of all of them.
+// The grid is an upper bound; a call that was not cut leaves nothing to do.
+template <typename T, int D, int ROWS, int KEYS>
 __global__ void __launch_bounds__(256) paged_prefill_join_kernel(const __grid_constant__ PrefillParams P) {
   griddep_launch();
   griddep_wait();
   const PagedParams& A = P.A;
-  const int unit = blockIdx.x / (ROWS / 32), G = 1 << P.g_shift;
+  const int unit = blockIdx.x / (ROWS / 32), G = 1 << P.g_shift, head = unit % A.n_kv_heads;
+  const int run = (int)P.counter[2];
+  if (run == 0x7fffffff) return;
   PrefillBlock B;
-  if (!find_block<ROWS>(A, P.g_shift, unit / A.n_kv_heads, unit % A.n_kv_heads, B)) return;
-  const int row = blockIdx.x % (ROWS / 32) * 32 + (threadIdx.x >> 3), R = B.row0 + row, c0 = threadIdx.x & 7;
+  int r, runs, first_item;
+  if (!find_item<ROWS, KEYS, true>(A, P.g_shift, run, unit / A.n_kv_heads, head, B, r, runs, first_item)) return;
+  const int row = blockIdx.x % (ROWS / 32) * 32 + (threadIdx.x & 31), R = B.row0 + row, c0 = threadIdx.x >> 5;
   if (R >= B.n << P.g_shift) return;
-  const long long at0 = (long long)unit * P.splits * ROWS + row;
+  int there = 1, v0, v1;                                          // runs that have tiles
+  while (there < runs && run_of<KEYS>(B, there, runs, run, v0, v1)) ++there;
+  auto slot = [&](int s) { return (long long)(first_item + s) * A.n_kv_heads + head; };
   float m = -INFINITY;
-  for (int s = 0; s < P.splits; ++s) m = fmaxf(m, P.part_ml[at0 + (long long)s * ROWS].x);
+  for (int s = 0; s < there; ++s) m = fmaxf(m, P.part_ml[slot(s) * ROWS + row].x);
   constexpr int V = D / 32;                                       // float4s per thread
   float4 acc[V] = {};
   float l = 0.f;
-  for (int s = 0; s < P.splits; ++s) {
-    const long long at = at0 + (long long)s * ROWS;
-    const float2 ml = P.part_ml[at];
+  for (int s = 0; s < there; ++s) {
+    const float2 ml = P.part_ml[slot(s) * ROWS + row];
     if (ml.x == -INFINITY) continue;                              // a run that the row sees nothing of wrote no output
     const float f = exp2_fast(ml.x - m);
     l = fmaf(ml.y, f, l);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const float4 x = reinterpret_cast<const float4*>(P.part + at * D)[i * 8 + c0];
-      acc[i].x = fmaf(x.x, f, acc[i].x); acc[i].y = fmaf(x.y, f, acc[i].y); acc[i].z = fmaf(x.z, f, acc[i].z); acc[i].w = fmaf(x.w, f, acc[i].w);
+      const float4 x4 = P.part[(slot(s) * (D / 4) + i * 8 + c0) * ROWS + row];
+      acc[i].x = fmaf(x4.x, f, acc[i].x); acc[i].y = fmaf(x4.y, f, acc[i].y); acc[i].z = fmaf(x4.z, f, acc[i].z); acc[i].w = fmaf(x4.w, f, acc[i].w);
     }
   }
   const bool seen = !(l <= 0.f);
