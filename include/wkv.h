@@ -298,7 +298,8 @@ typedef struct {
 const char* wkv_paged_config_error(const wkv_paged_config* cfg);
 
 /* Creates a handle on the current CUDA device.  Pools that the library takes from the provider start at zero.  The pools'
- * tensor maps are encoded here (bf16 and fp32 rows; WKV_ERR_CUDA if the driver lacks the encoder). */
+ * tensor maps are encoded here (WKV_ERR_CUDA if the driver lacks the encoder).  Workspaces, besides that of `scores`: partial
+ * outputs, about 300 KB an SM with bf16 rows of 128 channels. */
 int wkv_paged_create(const wkv_paged_config* cfg, wkv_paged** out);
 /* Releases what the provider gave; the handle's calls are done by then.  NULL is accepted. */
 void wkv_paged_destroy(wkv_paged* c);
@@ -321,7 +322,8 @@ int wkv_paged_decode(wkv_paged* c, int32_t layer, int32_t batch, const void* q, 
 
 /* Chunks of new tokens -- whole prompts, pieces of prompts, a few drafted tokens -- of a ragged batch in one call: appends
  * them and attends with each.  Sequence b's tokens are rows q_start[b] .. q_start[b+1]-1 of q, k, v, out and lse and become
- * its last entries; seq_lens counts them.  Rows behind q_start[batch] are left as they were.
+ * its last entries; seq_lens counts them.  Rows behind q_start[batch] are left as they were.  No page that the call stores to
+ * may be read by another of its sequences.
  *   q, k, v [total_q, heads, head_dim] and their strides as in wkv_paged_decode;  q_start device [batch + 1] int32
  *   out [total_q, n_q_heads, head_dim];  lse [total_q, n_q_heads] fp32, or NULL where scores is NULL. */
 int wkv_paged_prefill(wkv_paged* c, int32_t layer, int32_t batch, const void* q, int64_t q_stride, const void* k, const void* v,

@@ -32,8 +32,7 @@ struct PagedParams {
   uint32_t* status;
   int batch, rows, width, n_pages, n_q_heads, n_kv_heads, page, page_shift;
   int window, sink;
-  float scale;               // softmax scale; scale_log2 = scale * log2(e)
-  float scale_log2;
+  float scale_log2;          // softmax scale * log2(e)
 };
 
 __device__ __forceinline__ void flag_bad_table(uint32_t* status) { atomicOr(status, kStatusBadTable); }

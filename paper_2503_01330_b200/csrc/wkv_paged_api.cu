@@ -229,7 +229,7 @@ int attention_params(wkv_paged* c, wkv::PagedParams& P, int32_t layer, int32_t b
   P.table = table; P.seq_lens = seq_lens; P.out = out; P.lse = lse; P.scores = scores; P.score_stride = score_stride;
   P.status = c->status; P.batch = batch; P.rows = rows; P.width = width; P.n_pages = f.n_pages;
   P.n_q_heads = f.n_q_heads; P.n_kv_heads = f.n_kv_heads; P.page = f.page_size; P.page_shift = c->page_shift;
-  P.window = window; P.sink = sink; P.scale = c->scale; P.scale_log2 = c->scale * wkv::kLog2e;
+  P.window = window; P.sink = sink; P.scale_log2 = c->scale * wkv::kLog2e;
   return WKV_OK;
 }
 
