@@ -61,7 +61,7 @@ struct PrefillShape {
   static constexpr int kPartBytes = 128 * 128;                    // 128 rows x 128 bytes
   static constexpr int kTileBytes = kParts * kPartBytes;          // of Q (one row tile), K or V
   static constexpr int kStages = D == 128 ? 5 : 8;
-  static constexpr int kSmem = 2 * kTileBytes + kStages * kTileBytes + (2 * kStages + 18) * 8 + 16 + 2 * 64;
+  static constexpr int kSmem = 2 * kTileBytes + kStages * kTileBytes + (2 * kStages + 19) * 8 + 16 + 2 * 64;
 };
 
 __device__ __forceinline__ void tensor_g2s_4d(void* dst, const void* tmap, int x, int y, int z, int w, uint64_t* bar) {
@@ -292,8 +292,8 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
   uint64_t* q_free = q_full + 1;       // the item's last logits are done
   uint64_t* s_full = q_free + 1;       // [2] logits of a row tile are in TMEM (and its last P.V is done)
   uint64_t* p_ready = s_full + 2;      // [2][2] a half of the weights is in TMEM, the output is rescaled
-  uint64_t* o_full = p_ready + 4;      // all of the item's matrix instructions are done
-  uint64_t* o_free = o_full + 1;       // [2] a row tile's output has been read
+  uint64_t* o_full = p_ready + 4;      // [2] the item's products of a row tile are done
+  uint64_t* o_free = o_full + 2;       // [2] a row tile's output has been read
   uint64_t* item_full = o_free + 2;    // [2]
   uint64_t* item_empty = item_full + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(item_empty + 2);
@@ -305,8 +305,8 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
     for (int i = 0; i < STAGES; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
     mbar_init(q_full, 1);
     mbar_init(q_free, 1);
-    mbar_init(o_full, 1);
     for (int t = 0; t < 2; ++t) {
+      mbar_init(&o_full[t], 1);
       mbar_init(&s_full[t], 1); mbar_init(&p_ready[2 * t], 4); mbar_init(&p_ready[2 * t + 1], 4); mbar_init(&o_free[t], 4);
       mbar_init(&item_full[t], 1); mbar_init(&item_empty[t], 10);
     }
@@ -418,7 +418,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
           take_item(n, item);
           mbar_arrive(&item_empty[n & 1]);
           if (item.slot < 0) {
-            if (n > 0) mbar_wait_fast(o_full, (n & 1) ^ 1, A.status);        // nothing is in flight when the CTA ends
+            for (int t = 0; t < 2 && n > 0; ++t) mbar_wait_fast(&o_full[t], (n & 1) ^ 1, A.status);      // nothing is in flight when the CTA ends
             break;
           }
           const PrefillBlock& B = item.B;
@@ -463,17 +463,23 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
             vd = v_ring + (uint32_t)(((it + 1) % STAGES) * (Sh::kTileBytes >> 4));
           }
           tcgen05_commit(q_free);
+          bool told = false;
           if (item.v1 > item.v0) {
             mbar_wait_fast(&full[(it - 1) % STAGES], ((it - 1) / STAGES) & 1, A.status);
 #pragma unroll
             for (int t = 0; t < 2; ++t)
-              if (pending[t]) weights_times_values(t);
+              if (pending[t]) {
+                weights_times_values(t);
+                if (t == 0) tcgen05_commit(&o_full[0]);        // its rows need not wait for the other row tile
+                told = told || t == 0;
+              }
             tcgen05_commit(&empty[(it - 1) % STAGES]);
           }
           // a row tile without products in this item: its readers' word on the last item is still due
           for (int t = 0; t < 2; ++t)
             if (!started[t] && n > 0) mbar_wait_fast(&o_free[t], (n & 1) ^ 1, A.status);
-          tcgen05_commit(o_full);
+          if (!told) tcgen05_commit(&o_full[0]);
+          tcgen05_commit(&o_full[1]);
         }
       }
       __syncwarp();
@@ -596,7 +602,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
       }
       it += 2 * (item.v1 - item.v0);
       // ---- output
-      mbar_wait_fast(o_full, n & 1, A.status);
+      mbar_wait_fast(&o_full[t], n & 1, A.status);
       tcgen05_after_sync();
       const bool seen = !(l <= 0.f);                            // else the row's TMEM lane may hold anything
       const float inv = seen ? 1.f / l : 0.f;
