@@ -264,6 +264,7 @@ int decode(wkv_paged* c, const wkv::PagedParams& A) {
   P.part = c->part; P.part_ml = c->part_ml; P.arrived = c->arrived;
   P.logits = A.scores ? c->logits : nullptr;
   P.head_ml = c->head_ml;
+  P.fold_inside = A.scores && A.width * A.page <= wkv::kFoldInside;
   P.oob_chunk = c->cfg.n_layers * c->cfg.n_pages * c->cfg.n_kv_heads;
   P.chunk0 = chunk0(c, A);
   std::memcpy(P.kmap, c->page_kmap, 128);
@@ -271,7 +272,7 @@ int decode(wkv_paged* c, const wkv::PagedParams& A) {
   typedef void (*decode_fn)(const wkv::DecodeParams);
   typedef void (*fold_fn)(const wkv::DecodeParams, int);
   cudaError_t e = launch(c, (decode_fn)c->decode_kernel, c->decode_ctas, wkv::kDecodeThreads, c->decode_smem, P);
-  if (e == cudaSuccess && A.scores) {
+  if (e == cudaSuccess && A.scores && !P.fold_inside) {
     const int per_lane = (A.width * A.page + wkv::kFoldEntries - 1) / wkv::kFoldEntries;
     e = launch(c, (fold_fn)c->fold_kernel, (long long)A.batch * A.n_kv_heads * per_lane, wkv::kFoldEntries / 4, 0, P, per_lane);
   }

@@ -15,7 +15,7 @@
 // carry the weights' low halves, p - bf16(p), so that the output keeps fp32-like weights at no extra instruction.
 //
 // Measured: 16 sequences of 8192..16384 tokens, 32 x 128 heads, 487 us = 6.66 TB/s (1.02 of the measured copy rate); one sequence of
-// 611 tokens, 32/8 heads, 8.8 us in a captured graph, the length of its chain of dependent loads.
+// 611 tokens, 32/8 heads, 8.7 us in a captured graph, the length of its chain of dependent loads.
 #pragma once
 #include "wkv_paged.cuh"
 
@@ -25,6 +25,7 @@ constexpr int kDecodeWarps = 4;                           // consumers
 constexpr int kDecodeThreads = (kDecodeWarps + 1) * 32;
 constexpr int kDecodeRing = 96 * 1024;
 constexpr int kMaxSequences = 1024;
+constexpr int kJoinTiles = 4;
 
 struct DecodeParams {
   PagedParams A;
@@ -33,6 +34,7 @@ struct DecodeParams {
   uint32_t* arrived;         // [lanes], zero between launches
   float* logits;             // [lanes][G][width * page] base-2 logits, or NULL
   float2* head_ml;           // [rows][Hq] (max, 1 / sum) for the fold
+  int fold_inside;           // the CTA that completes a lane folds its weights, no second kernel
   int oob_chunk;             // a chunk number outside the pool
   int chunk0;                // the layer's first chunk
   alignas(64) unsigned char kmap[128];   // pool as [chunk][part][row][128 bytes], boxes of one page (or tile) x all parts
@@ -328,6 +330,27 @@ template <int D, int G> struct DecodeWarp<float, D, G> : DecodeWarpF32<D, G> {
   static constexpr int kScratch = G * 4 * (D / 4 + 4);   // floats per warp
 };
 
+// Weights into the running sums: four entries from i0 on, from the parked base-2 logits and the heads' (max, 1 / sum).
+template <int G>
+__device__ __forceinline__ void fold_entries(const DecodeParams& P, const DecodeSpan& s, long long lane_no, int i0, const float2 (&ml)[G]) {
+  const PagedParams& A = P.A;
+  if (i0 >= s.len || (i0 + 4 <= s.lo && i0 >= s.sinks)) return;
+  const long long stride = (long long)A.width << A.page_shift;
+  float w[4] = {};
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    const float4 x = __ldcg(reinterpret_cast<const float4*>(P.logits + (lane_no * G + g) * stride + i0));
+    w[0] = fmaf(exp2_fast(x.x - ml[g].x), ml[g].y, w[0]);
+    w[1] = fmaf(exp2_fast(x.y - ml[g].x), ml[g].y, w[1]);
+    w[2] = fmaf(exp2_fast(x.z - ml[g].x), ml[g].y, w[2]);
+    w[3] = fmaf(exp2_fast(x.w - ml[g].x), ml[g].y, w[3]);
+  }
+  float* a = A.scores + lane_no * A.score_stride + i0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (s.sees(i0 + e)) a[e] = (A.k && i0 + e == s.len - 1 ? 0.f : a[e]) + w[e] * (1.f / G);
+}
+
 __device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
 template <typename T, int D, int G>
@@ -361,7 +384,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
   for (int b = tid; b < A.batch; b += kDecodeThreads) lens[b] = clamped_len(A, b);
   __syncthreads();
   if (warp == 0) {
-    int run = 0;
+    int run = 0, most = 0;
     for (int base = 0; base < A.batch; base += 32) {
       const int b = base + lane;
       int n = b < A.batch ? decode_span<TILE>(lens[b], A.window, A.sink).tiles : 0;
@@ -373,14 +396,24 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
       }
       if (b < A.batch) cum[b] = run + x - n;
       run += __shfl_sync(~0u, x, 31);
+      most = max(most, __reduce_max_sync(~0u, n));
     }
-    if (lane == 0) cum[A.batch] = run;
+    if (lane == 0) { cum[A.batch] = run; cum[A.batch + 1] = most; }
   }
   __syncthreads();
   const int H = A.n_kv_heads, cta = blockIdx.x;
   const long long total = (long long)cum[A.batch] * H;
   const long long chunk = (total + gridDim.x - 1) / gridDim.x;
-  const long long t0 = cta * chunk, t1 = min(total, t0 + chunk);
+  long long t0 = cta * chunk, t1 = min(total, t0 + chunk);
+  // Few lanes of nearly equal length: a lane each.  Joining a lane costs about as much as four tiles (7000 cycles; under a window of
+  // 508, 232 lanes of ten tiles, 21.5 us with lanes cut every eight tiles, 17.2 us whole).
+  const long long lanes = (long long)A.batch * H;
+  if (lanes <= gridDim.x && cum[A.batch + 1] <= chunk + kJoinTiles) {
+    if (cta >= lanes) return;
+    const int bb = cta / H, tiles = cum[bb + 1] - cum[bb];
+    t0 = (long long)cum[bb] * H + (long long)(cta % H) * tiles;
+    t1 = t0 + tiles;
+  }
   if (t0 >= t1) return;
   // the first piece: sequence, head, tile
   int b = 0;
@@ -583,7 +616,13 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
       if (tid < G) {
         const long long at = (long long)b * A.n_q_heads + hq0 + tid;
         if (A.lse) A.lse[at] = sm_l[tid] > 0.f ? (sm_m[tid] + log2f(sm_l[tid])) * kLn2 : -INFINITY;
-        if (P.logits) P.head_ml[at] = make_float2(sm_m[tid], sm_l[tid] > 0.f ? 1.f / sm_l[tid] : 0.f);
+        if (P.logits && !P.fold_inside) P.head_ml[at] = make_float2(sm_m[tid], sm_l[tid] > 0.f ? 1.f / sm_l[tid] : 0.f);
+      }
+      if (P.fold_inside) {
+        float2 ml[G];
+#pragma unroll
+        for (int g = 0; g < G; ++g) ml[g] = make_float2(sm_m[g], sm_l[g] > 0.f ? 1.f / sm_l[g] : 0.f);
+        for (int i0 = tid * 4; i0 < s.len; i0 += 512) fold_entries<G>(P, s, lane_no, i0, ml);
       }
     }
     consumers_sync();                                      // sm_* are free for the next piece
@@ -598,31 +637,19 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
   }
 }
 
-// Weights into the running sums: 4 entries a thread, from the parked logits and the finished (max, 1 / sum).
+// The fold as a kernel of its own, for lanes that may be long: 1024 entries a CTA.
 constexpr int kFoldEntries = 1024;
+constexpr int kFoldInside = 2048;      // entries that the decode kernel folds itself: 512 a consumer warp, less than a launch takes
 template <int G>
 __global__ void __launch_bounds__(kFoldEntries / 4) paged_fold_kernel(const __grid_constant__ DecodeParams P, int blocks_per_lane) {
   griddep_wait();
   const PagedParams& A = P.A;
   const int lane_no = blockIdx.x / blocks_per_lane, b = lane_no / A.n_kv_heads, head = lane_no % A.n_kv_heads;
   const int i0 = blockIdx.x % blocks_per_lane * kFoldEntries + threadIdx.x * 4;
-  const DecodeSpan s = decode_span<64>(clamped_len(A, b), A.window, A.sink);
-  if (i0 >= s.len || (i0 + 4 <= s.lo && i0 >= s.sinks)) return;
-  const long long stride = (long long)A.width << A.page_shift;
-  float w[4] = {};
+  float2 ml[G];
 #pragma unroll
-  for (int g = 0; g < G; ++g) {
-    const float2 ml = P.head_ml[(long long)b * A.n_q_heads + head * G + g];
-    const float4 x = *reinterpret_cast<const float4*>(P.logits + ((long long)lane_no * G + g) * stride + i0);
-    w[0] = fmaf(exp2_fast(x.x - ml.x), ml.y, w[0]);
-    w[1] = fmaf(exp2_fast(x.y - ml.x), ml.y, w[1]);
-    w[2] = fmaf(exp2_fast(x.z - ml.x), ml.y, w[2]);
-    w[3] = fmaf(exp2_fast(x.w - ml.x), ml.y, w[3]);
-  }
-  float* a = A.scores + (long long)lane_no * A.score_stride + i0;
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (s.sees(i0 + e)) a[e] = (A.k && i0 + e == s.len - 1 ? 0.f : a[e]) + w[e] * (1.f / G);
+  for (int g = 0; g < G; ++g) ml[g] = P.head_ml[(long long)b * A.n_q_heads + head * G + g];
+  fold_entries<G>(P, decode_span<64>(clamped_len(A, b), A.window, A.sink), lane_no, i0, ml);
 }
 
 }  // namespace wkv

@@ -23,7 +23,7 @@
 // operand of P.V straight from TMEM) and both outputs (D columns each).  An output is rescaled in place, and only when a row's
 // maximum has grown by more than 2^8 since its reference was taken.
 //
-// Measured: 8192 tokens, 32 x 128 heads, 478 us = 1150 TFLOP/s alone, 569 us in a long series at the power limit; a pair of tiles
+// Measured: 8192 tokens, 32 x 128 heads, 478 us = 1150 TFLOP/s alone, 560 us in a long series at the power limit; a pair of tiles
 // takes 2900..3100 cycles (tensor cores 2048): TMEM holds no third row tile that could hide the chain logits, softmax, weights.
 #pragma once
 #include "wkv_paged.cuh"
