@@ -44,8 +44,9 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, uint32
   return false;
 }
 // The same for waits on a kernel's critical path: one instruction when the barrier is ready (a fifth of mbar_wait's cycles, whose
-// loop the compiler guards for divergence), no sleeping while it is not.  At most kFastPolls polls.
-constexpr uint32_t kFastPolls = 1u << 26;
+// loop the compiler guards for divergence), no sleeping while it is not.  At most kFastPolls polls (some tenths
+// of a second, where a wait in a working kernel takes microseconds).
+constexpr uint32_t kFastPolls = 1u << 23;
 __device__ __forceinline__ bool mbar_wait_fast(uint64_t* bar, uint32_t parity, uint32_t* status) {
   uint32_t left;
   asm volatile(
