@@ -374,12 +374,14 @@ class PagedCache:
         return t.data_ptr()
 
     def _rows(self, name, t, n, heads):
-        """Address and row stride of [n, heads, head_dim] whose rows may lie apart (columns of a wider projection)."""
+        """Address and row stride of [n, heads, head_dim] whose rows may lie apart (columns of a wider projection), but not on one
+        another: a row broadcast over the batch has stride 0, which the C call takes for packed rows."""
         d = self.head_dim
         strides = t.stride()
         if (t.dtype is not self.tdtype or t.get_device() != self._index or t.shape != (n, heads, d)
-                or (n > 0 and (strides[2] != 1 or (heads > 1 and strides[1] != d)))):
-            raise WkvError(WKV_ERR_INVALID, f"{name} must be a {self.tdtype} tensor [{n}, {heads}, {d}] on {self.device} whose rows are packed")
+                or (n > 0 and (strides[2] != 1 or (heads > 1 and strides[1] != d))) or (n > 1 and strides[0] < heads * d)):
+            raise WkvError(WKV_ERR_INVALID, f"{name} must be a {self.tdtype} tensor [{n}, {heads}, {d}] on {self.device} "
+                                            "whose rows are packed and do not overlap (no broadcast rows)")
         return t.data_ptr(), (strides[0] if n > 1 else heads * d)
 
     def _new_rows(self, k, v, n):

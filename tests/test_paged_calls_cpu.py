@@ -1,0 +1,64 @@
+"""The binding's checks of a paged call's arguments, without a GPU: a cache on CPU tensors whose C calls are recorded."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2503_01330_b200 import binding
+
+
+class Recorder:
+    """Stands in for the C library: notes every call and accepts it."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        if name.startswith("wkv_"):
+            return lambda *a: self.calls.append((name, a)) or 0
+        raise AttributeError(name)
+
+
+@pytest.fixture
+def cache(monkeypatch):
+    rec = Recorder()
+    monkeypatch.setattr(binding, "lib", lambda: rec)
+    c = binding.PagedCache.__new__(binding.PagedCache)
+    c.device, c._index, c.dtype, c.tdtype = torch.device("cpu"), -1, binding.WKV_BF16, torch.bfloat16
+    c.n_q_heads, c.n_kv_heads, c.head_dim, c.page_size = 4, 2, 64, 16
+    c._bufs, c._h, c._lib = {}, C.c_void_p(1), rec
+    yield c
+    c._h = None
+
+
+def call(cache, q, k, v, prefill):
+    n = q.shape[0]
+    i32 = lambda *shape: torch.zeros(*shape, dtype=torch.int32)
+    out = torch.empty(n, 4, 64, dtype=torch.bfloat16)
+    if prefill:
+        cache.wkv_paged_prefill(0, q, k, v, i32(n + 1), i32(n, 5), i32(n), out)
+    else:
+        cache.wkv_paged_decode(0, q, k, v, i32(n, 5), i32(n), out)
+    return cache._lib.calls[-1][1]
+
+
+@pytest.mark.parametrize("prefill", [False, True])
+@pytest.mark.parametrize("which", ["q", "k", "v", "kv"])
+def test_rows_broadcast_over_the_batch_are_refused(cache, prefill, which):
+    """x.expand(n, heads, d) has row stride 0, which the C call reads as packed rows: n - 1 rows behind the tensor's only one."""
+    rows = {x: torch.zeros(3, h, 64, dtype=torch.bfloat16) for x, h in (("q", 4), ("k", 2), ("v", 2))}
+    for x in which:
+        rows[x] = rows[x][:1].expand_as(rows[x])
+    with pytest.raises(binding.WkvError) as e:
+        call(cache, **rows, prefill=prefill)
+    assert e.value.code == binding.WKV_ERR_INVALID and not cache._lib.calls
+
+
+@pytest.mark.parametrize("prefill", [False, True])
+def test_row_strides_that_are_handed_on(cache, prefill):
+    wide = torch.zeros(3, 10, 64, dtype=torch.bfloat16)
+    a = call(cache, wide[:, :4], wide[:, 4:6], wide[:, 6:8], prefill)
+    assert a[4] == 640 and a[7] == 640
+    one = wide[:1].expand(1, 10, 64)                       # a single row: its stride says nothing
+    a = call(cache, one[:, :4], one[:, 4:6], one[:, 6:8], prefill)
+    assert a[4] == 4 * 64 and a[7] == 2 * 64
