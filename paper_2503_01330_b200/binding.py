@@ -401,10 +401,13 @@ class PagedCache:
 
     # -- the C ABI, same names ----------------------------------------------------------------------
     def wkv_set_stream(self, stream):
-        if isinstance(stream, torch.cuda.Stream):
-            for buf in self._bufs.values():          # workspaces freed while that stream still uses them wait for it
-                buf.record_stream(stream)
-        self._check(lib().wkv_paged_set_stream(self._h, C.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else stream)))
+        """A torch stream, or a cudaStream_t as a number (None, 0: the default stream)."""
+        handle = (stream.cuda_stream if hasattr(stream, "cuda_stream") else stream) or 0
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(handle, device=self.device) if handle > 1 else torch.cuda.default_stream(self.device)
+        for buf in (*self._bufs.values(), self.k_pool, self.v_pool):     # freed while that stream still uses them, they wait for it
+            buf.record_stream(stream)
+        self._check(lib().wkv_paged_set_stream(self._h, C.c_void_p(handle)))
 
     def wkv_paged_decode(self, layer, q, k, v, block_table, seq_lens, out, window=0, sink=0, scores=None, lse=None):
         """q [B, Hq, d], k, v [B, Hkv, d] or None, block_table [B, width] and seq_lens [B] int32 (with the new token)."""

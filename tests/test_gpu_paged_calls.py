@@ -1,0 +1,56 @@
+"""Paged calls as programs make them: streams, status, shared and released pages, bad pages, scales, many items a CTA.  Results
+are held against the definition of tests/paged_util.py."""
+import pytest
+import torch
+
+from paged_util import Case
+from paper_2503_01330_b200 import binding
+
+pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------- arguments
+
+@pytest.mark.parametrize("prefill", [False, True])
+@pytest.mark.parametrize("which", ["q", "k", "v", "kv"])
+def test_rows_broadcast_over_the_batch_are_refused(prefill, which):
+    c = Case(lens=[40, 20, 33], new=[1, 1, 1], page=16, prefill=prefill)
+    cache = c.cache()
+    rows = dict(zip("qkv", c.rows()))
+    for x in which:
+        rows[x] = rows[x][:1].expand_as(rows[x])
+    i32 = dict(dtype=torch.int32, device="cuda")
+    table, lens, out = c.table.cuda(), torch.tensor(c.lens, **i32), torch.empty(3, 4, 64, dtype=c.tdt, device="cuda")
+    with pytest.raises(binding.WkvError) as e:
+        if prefill:
+            cache.wkv_paged_prefill(0, **rows, q_start=torch.tensor([0, 1, 2, 3], **i32), block_table=table, seq_lens=lens, out=out)
+        else:
+            cache.wkv_paged_decode(0, **rows, block_table=table, seq_lens=lens, out=out)
+    assert e.value.code == binding.WKV_ERR_INVALID and cache.wkv_launch_count() == 0
+    cache.close()
+
+
+# ---------------------------------------------------------------- streams, status
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_pools_of_a_dropped_cache_wait_for_its_stream(raw):
+    """Pools that the cache made itself go back to torch's allocator with it, but not to a new tensor while the stream that the
+    cache ran on still has work."""
+    cache = binding.PagedCache(1, 1000, 16, 4, 2, 64, 2, 4)
+    nbytes, addresses = cache.k_pool.nbytes, {cache.k_pool.data_ptr(), cache.v_pool.data_ptr()}
+    q, k = torch.zeros(2, 4, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(2, 2, 64, dtype=torch.bfloat16, device="cuda")
+    table, lens, out = (torch.zeros(*s, dtype=t, device="cuda") for s, t in (((2, 4), torch.int32), ((2,), torch.int32), ((2, 4, 64), torch.bfloat16)))
+    table[1] += 1
+    lens += 1
+    side = torch.cuda.Stream()
+    cache.wkv_set_stream(side.cuda_stream if raw else side)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(1_000_000_000)
+    cache.wkv_paged_decode(0, q, k, k, table, lens, out)
+    cache.close()
+    del cache
+    later = [torch.empty(nbytes, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    assert not side.query()
+    assert not addresses & {x.data_ptr() for x in later}
+    torch.cuda.synchronize()

@@ -62,3 +62,35 @@ def test_row_strides_that_are_handed_on(cache, prefill):
     one = wide[:1].expand(1, 10, 64)                       # a single row: its stride says nothing
     a = call(cache, one[:, :4], one[:, 4:6], one[:, 6:8], prefill)
     assert a[4] == 4 * 64 and a[7] == 2 * 64
+
+
+class Block:
+    """A device tensor as far as its allocator's stream records go."""
+
+    def __init__(self):
+        self.streams = []
+
+    def record_stream(self, stream):
+        self.streams.append(stream)
+
+
+class Stream:
+    def __init__(self, handle, device=None):
+        self.cuda_stream, self.device = handle, device
+
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_all_memory_is_kept_for_a_changed_stream(cache, monkeypatch, raw):
+    """Workspaces and pools that are freed while the new stream still uses them wait for it, a raw handle's stream too."""
+    monkeypatch.setattr(binding.torch.cuda, "Stream", Stream)
+    monkeypatch.setattr(binding.torch.cuda, "ExternalStream", type("ExternalStream", (Stream,), {}))
+    monkeypatch.setattr(binding.torch.cuda, "default_stream", lambda device: Stream(0, device))
+    cache._bufs, cache.k_pool, cache.v_pool = {1: Block(), 2: Block()}, Block(), Block()
+    for handle in (4096, 0):
+        cache.wkv_set_stream(handle if raw else Stream(handle))
+        name, args = cache._lib.calls[-1]
+        assert name == "wkv_paged_set_stream" and (args[1].value or 0) == handle
+        for block in (*cache._bufs.values(), cache.k_pool, cache.v_pool):
+            assert block.streams[-1].cuda_stream == handle
+    cache.wkv_set_stream(None)                              # the default stream
+    assert (cache._lib.calls[-1][1][1].value or 0) == 0 and cache.k_pool.streams[-1].cuda_stream == 0
