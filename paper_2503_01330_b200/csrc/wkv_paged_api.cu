@@ -522,14 +522,16 @@ int wkv_paged_status(wkv_paged* c) {
   DeviceGuard on(c->device);
   WKV_CUDA(c, on.err);
   uint32_t w = 0;
+  WKV_CUDA(c, cudaMemcpyAsync(&w, c->status, 4, cudaMemcpyDeviceToHost, c->stream));
   WKV_CUDA(c, cudaStreamSynchronize(c->stream));
-  WKV_CUDA(c, cudaMemcpy(&w, c->status, 4, cudaMemcpyDeviceToHost));
   if (w) {
-    WKV_CUDA(c, cudaMemset(c->status, 0, 4));
-    // a piece that gave up may have left its lane's arrivals uncounted
+    // On the handle's stream, ahead of the next call: a clear on the default stream is not ordered with streams that do not wait for
+    // that one, and could take back the next call's report, or its counts.
+    WKV_CUDA(c, cudaMemsetAsync(c->status, 0, 4, c->stream));
+    // a call that gave up may have left arrivals, items or rows uncounted
     if (w & wkv::kStatusWaitTimeout) {
-      WKV_CUDA(c, cudaMemset(c->arrived, 0, (size_t)c->cfg.max_batch * c->cfg.n_kv_heads * 4));
-      WKV_CUDA(c, cudaMemset(c->item_counter, 0, 8));
+      WKV_CUDA(c, cudaMemsetAsync(c->arrived, 0, (size_t)c->cfg.max_batch * c->cfg.n_kv_heads * 4, c->stream));
+      WKV_CUDA(c, cudaMemsetAsync(c->item_counter, 0, 8, c->stream));
     }
     if (w & wkv::kStatusWaitTimeout) return fail(c, WKV_ERR_TIMEOUT, "a bounded wait inside a kernel gave up");
     return fail(c, WKV_ERR_STATE, "a page number, length or row offset was out of range, or an eviction's tables overlap");

@@ -54,3 +54,23 @@ def test_pools_of_a_dropped_cache_wait_for_its_stream(raw):
     assert not side.query()
     assert not addresses & {x.data_ptr() for x in later}
     torch.cuda.synchronize()
+
+
+def test_status_on_a_side_stream_keeps_the_next_report():
+    """wkv_paged_status clears what it reports in the order of the handle's stream, so a bad call right behind it is reported too,
+    also on a stream that does not wait for the default one."""
+    c = Case(lens=[40, 20], new=[1, 1], page=16)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        cache = c.cache()
+        q, k, v = c.rows()
+        table, lens, out = c.table.cuda(), torch.tensor(c.lens, dtype=torch.int32, device="cuda"), torch.empty(2, 4, 64, dtype=c.tdt, device="cuda")
+        bad = table.clone()
+        bad[0, 1] = -1
+        for i in range(200):
+            cache.wkv_paged_decode(0, q, k, v, bad, lens, out)
+            assert cache.wkv_status() == binding.WKV_ERR_STATE, i
+        cache.wkv_paged_decode(0, q, k, v, table, lens, out)
+        assert cache.wkv_status() == 0
+        side.synchronize()
+    cache.close()
