@@ -522,6 +522,7 @@ int wkv_paged_status(wkv_paged* c) {
   DeviceGuard on(c->device);
   WKV_CUDA(c, on.err);
   uint32_t w = 0;
+  WKV_CUDA(c, cudaStreamSynchronize(c->stream));        // first: a stream that is being captured is refused here
   WKV_CUDA(c, cudaMemcpyAsync(&w, c->status, 4, cudaMemcpyDeviceToHost, c->stream));
   WKV_CUDA(c, cudaStreamSynchronize(c->stream));
   if (w) {
