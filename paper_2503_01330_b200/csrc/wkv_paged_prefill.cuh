@@ -312,12 +312,13 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  griddep_launch();
   if (warp == 8) tmem_take(tmem_slot);
   tcgen05_before_sync();
   griddep_wait();
   __syncthreads();
   tcgen05_after_sync();
+  // behind the allocation: a kernel that starts early and takes TMEM here first would keep it until this one ends
+  griddep_launch();
   const uint32_t tmem = __shfl_sync(~0u, *tmem_slot, 0);
 
   // the n-th item of this CTA, once it is there; every reader tells when it has its copy
@@ -746,7 +747,6 @@ __global__ void __launch_bounds__(kWeightsThreads, 1) paged_weights_tc_kernel(co
 
   const PagedParams& A = P.A;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, G = 1 << P.g_shift;
-  griddep_launch();
   griddep_wait();
   const int head = blockIdx.x % A.n_kv_heads, b = blockIdx.x / A.n_kv_heads % A.batch, e0 = blockIdx.x / A.n_kv_heads / A.batch * 256;
   const SeqRows s = seq_rows(A, b);
@@ -768,6 +768,7 @@ __global__ void __launch_bounds__(kWeightsThreads, 1) paged_weights_tc_kernel(co
   tcgen05_before_sync();
   __syncthreads();
   tcgen05_after_sync();
+  griddep_launch();                                                   // behind the allocation, as in the kernel above
   const uint32_t tmem = __shfl_sync(~0u, *tmem_slot, 0);
 
   if (warp == 17) {
