@@ -346,8 +346,10 @@ int wkv_paged_evict(wkv_paged* c, int32_t layer, int32_t batch, const int32_t* s
                     int32_t recent, int32_t sink, const float* scores, int64_t score_stride, float* scores_out,
                     int64_t out_stride, int32_t* kept);
 
-/* As their namesakes without _paged. */
+/* As their namesakes without _paged.  A wait inside a kernel that gave up (WKV_ERR_TIMEOUT) ends its block's work; what the calls
+ * since the last status wrote is then undefined, and the handle can be used again. */
 int wkv_paged_status(wkv_paged* c);
+int wkv_paged_selftest_wait_timeout(wkv_paged* c);
 int64_t wkv_paged_launch_count(const wkv_paged* c);
 int64_t wkv_paged_device_bytes(const wkv_paged* c);
 const char* wkv_paged_last_error(const wkv_paged* c);

@@ -40,8 +40,8 @@ EXPORTS = ["wkv_config_error", "wkv_create", "wkv_destroy", "wkv_reset", "wkv_se
            "wkv_decode_step_layers", "wkv_decode_step_static", "wkv_decode_step_host", "wkv_decode_step_layers_host", "wkv_prefill", "wkv_prefill_bulk", "wkv_prefill_bulk_layers", "wkv_export_state", "wkv_export_slots", "wkv_import_state",
            "wkv_status", "wkv_selftest_wait_timeout", "wkv_launch_count", "wkv_device_bytes", "wkv_splits", "wkv_strerror", "wkv_last_error",
            "wkv_paged_config_error", "wkv_paged_create", "wkv_paged_destroy", "wkv_paged_set_stream", "wkv_paged_pools",
-           "wkv_paged_decode", "wkv_paged_prefill", "wkv_paged_evict", "wkv_paged_status", "wkv_paged_launch_count",
-           "wkv_paged_device_bytes", "wkv_paged_last_error"]
+           "wkv_paged_decode", "wkv_paged_prefill", "wkv_paged_evict", "wkv_paged_status", "wkv_paged_selftest_wait_timeout",
+           "wkv_paged_launch_count", "wkv_paged_device_bytes", "wkv_paged_last_error"]
 
 _lib = None
 
@@ -96,6 +96,7 @@ def lib():
         L.wkv_paged_prefill.argtypes = [vp, i32, i32, vp, i64, vp, vp, i64, vp, i32, vp, i32, vp, i32, i32, vp, i64, vp, vp]
         L.wkv_paged_evict.argtypes = [vp, i32, i32, vp, i32, vp, i32, vp, vp, i32, i32, i32, vp, i64, vp, i64, vp]
         L.wkv_paged_status.argtypes = [vp]
+        L.wkv_paged_selftest_wait_timeout.argtypes = [vp]
         L.wkv_paged_launch_count.restype = i64
         L.wkv_paged_launch_count.argtypes = [vp]
         L.wkv_paged_device_bytes.restype = i64
@@ -449,6 +450,9 @@ class PagedCache:
 
     def wkv_status(self):
         return lib().wkv_paged_status(self._h)
+
+    def wkv_selftest_wait_timeout(self):
+        self._check(lib().wkv_paged_selftest_wait_timeout(self._h))
 
     def wkv_launch_count(self):
         return int(lib().wkv_paged_launch_count(self._h))

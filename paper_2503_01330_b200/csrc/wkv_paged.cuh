@@ -93,6 +93,20 @@ __device__ __forceinline__ bool visible(int i, int pos, int window, int sink) {
   return i <= pos && (window == 0 || i > pos - window || i < sink);
 }
 
+// For tests: a warp's and a thread's wait for barriers that nothing arrives at.
+__global__ void __launch_bounds__(64) paged_wait_selftest_kernel(uint32_t* status) {
+  __shared__ uint64_t bars[2];
+  if (threadIdx.x == 0) {
+    mbar_init(&bars[0], 1);
+    mbar_init(&bars[1], 1);
+  }
+  griddep_wait();
+  __syncthreads();
+  const WaitLimit waits{status, 400};
+  if (threadIdx.x < 32) warp_wait(&bars[0], 0, waits);
+  else if (threadIdx.x == 32) thread_wait(&bars[1], 0, waits);
+}
+
 // ------------------------------------------------------------------------------------------------
 // append
 // ------------------------------------------------------------------------------------------------

@@ -292,6 +292,8 @@ int prefill_params(wkv_paged* c, wkv::PrefillParams& P, const wkv::PagedParams& 
   if (*units > 0x3fffffff) return fail(c, WKV_ERR_INVALID, "total_q * n_q_heads is too large");
   const long long tiles = ((long long)A.width * A.page + keys - 1) / keys;
   *items = std::max<long long>(*units, std::min<long long>(P.slots, *units * tiles));
+  // An item may walk the whole table, at 1.6 us a tile of 128 entries and more at low clocks: 20 us a tile, 131072 tiles at most.
+  P.polls = wkv::kWaitPolls + (uint32_t)((long long)A.width * A.page / 128 * 4);
   P.counter = c->item_counter; P.part = c->run_part; P.part_ml = c->run_ml;
   P.oob_chunk = c->cfg.n_layers * c->cfg.n_pages * c->cfg.n_kv_heads;
   P.chunk0 = chunk0(c, A);
@@ -537,6 +539,14 @@ int wkv_paged_status(wkv_paged* c) {
     if (w & wkv::kStatusWaitTimeout) return fail(c, WKV_ERR_TIMEOUT, "a bounded wait inside a kernel gave up");
     return fail(c, WKV_ERR_STATE, "a page number, length or row offset was out of range, or an eviction's tables overlap");
   }
+  return WKV_OK;
+}
+
+int wkv_paged_selftest_wait_timeout(wkv_paged* c) {
+  if (!c) return WKV_ERR_INVALID;
+  DeviceGuard on(c->device);
+  WKV_CUDA(c, on.err);
+  WKV_CUDA(c, launch(c, wkv::paged_wait_selftest_kernel, 1, 64, 0, c->status));
   return WKV_OK;
 }
 

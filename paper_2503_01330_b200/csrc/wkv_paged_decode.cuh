@@ -429,6 +429,10 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
   int head = (int)((t0 - (long long)cum[b] * H) / s.tiles), v = (int)((t0 - (long long)cum[b] * H) % s.tiles);
   const int pr = min(A.page, TILE), pr_shift = min(A.page_shift, TILE == 64 ? 6 : 5);
   const int boxes = TILE >> pr_shift;
+  // No copy is in flight when the CTA ends, without a wait of its own for that: a consumer has waited for each, and where one or the
+  // producer gave up, the last copy was issued ahead of that wait, a whole limit ago (a stage that is not released takes no other).
+  // (Of a warp's two forms of wait the one by mbar_wait is the faster here: one sequence of 611 tokens 9.0 us, with the other 9.3.)
+  auto wait = [&](uint64_t* bar, uint32_t parity) { return (bool)__all_sync(~0u, mbar_wait(bar, parity, A.status, kWaitPolls)); };
 
   if (warp == kDecodeWarps) {                              // ---- producer
     const uint64_t policy = l2_policy_evict_first();
@@ -445,7 +449,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
         const int pg = page_of(A, b, i);
         if (pg >= 0) { chunk_no = P.chunk0 + pg * H + head; row = i & (A.page - 1); }
       }
-      if (it >= STAGES) mbar_wait(&empty[st], ((it / STAGES) & 1) ^ 1, A.status);
+      if (it >= STAGES && !wait(&empty[st], ((it / STAGES) & 1) ^ 1)) break;
       unsigned char* dst = ring + st * 2 * Sh::kTileBytes;
       if (lane == 0) mbar_expect_tx(&full[st], 2 * Sh::kTileBytes);
       __syncwarp();
@@ -466,6 +470,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
   // ---- consumers
   Warp w;
   const float scale_log2 = A.scale_log2;
+  bool ok = true;          // else a wait gave up: this warp keeps the others' barriers company, and counts its pieces, but reads no more tiles
   int it = 0;
   for (long long t = t0; t < t1;) {
     const int first_v = v;
@@ -497,7 +502,8 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
       const int st = it % STAGES;
       unsigned char* tk = ring + st * 2 * Sh::kTileBytes;
       unsigned char* tv = tk + Sh::kTileBytes;
-      mbar_wait(&full[st], (it / STAGES) & 1, A.status);
+      ok = ok && wait(&full[st], (it / STAGES) & 1);
+      if (!ok) continue;
       const int row0 = warp * Sh::kEach, i0 = s.tile(v) * TILE + row0;
       // entries [i0, i0 + kEach) against the visible ones
       const bool any = i0 < s.len && (i0 + Sh::kEach > s.lo || i0 < s.sinks);

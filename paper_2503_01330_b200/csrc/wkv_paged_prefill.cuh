@@ -48,6 +48,7 @@ struct PrefillParams {
   float2* part_ml;           // [item][rows] (maximum in base-2 logits, sum)
   int oob_chunk, chunk0;
   int append;                // the call brings k and v, and this kernel stores what paged_append_edge_kernel has not
+  uint32_t polls;            // limit of the kernels' waits; some of them last as long as an item, so it grows with the table's width
   alignas(64) unsigned char qmap[128];   // q as [part][token][head][64 elements], boxes of a row tile
   alignas(64) unsigned char kmap[128];   // pool as [chunk][part][row][64 elements], boxes of a page x one part
   alignas(64) unsigned char vmap[128];
@@ -61,7 +62,7 @@ struct PrefillShape {
   static constexpr int kPartBytes = 128 * 128;                    // 128 rows x 128 bytes
   static constexpr int kTileBytes = kParts * kPartBytes;          // of Q (one row tile), K or V
   static constexpr int kStages = D == 128 ? 5 : 8;
-  static constexpr int kSmem = 2 * kTileBytes + kStages * kTileBytes + (2 * kStages + 19) * 8 + 16 + 2 * 64;
+  static constexpr int kSmem = 2 * kTileBytes + kStages * kTileBytes + (2 * kStages + 17) * 8 + 16 + 2 * 64;
 };
 
 __device__ __forceinline__ void tensor_g2s_4d(void* dst, const void* tmap, int x, int y, int z, int w, uint64_t* bar) {
@@ -296,7 +297,8 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
   uint64_t* o_free = o_full + 2;       // [2] a row tile's output has been read
   uint64_t* item_full = o_free + 2;    // [2]
   uint64_t* item_empty = item_full + 2;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(item_empty + 2);
+  uint64_t* drained = item_empty + 2;  // all matrix instructions are done
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drained + 1);
   unsigned char* item_smem = reinterpret_cast<unsigned char*>(tmem_slot + 4);
 
   const PagedParams& A = P.A;
@@ -305,6 +307,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
     for (int i = 0; i < STAGES; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
     mbar_init(q_full, 1);
     mbar_init(q_free, 1);
+    mbar_init(drained, 1);
     for (int t = 0; t < 2; ++t) {
       mbar_init(&o_full[t], 1);
       mbar_init(&s_full[t], 1); mbar_init(&p_ready[2 * t], 4); mbar_init(&p_ready[2 * t + 1], 4); mbar_init(&o_free[t], 4);
@@ -321,10 +324,15 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
   griddep_launch();
   const uint32_t tmem = __shfl_sync(~0u, *tmem_slot, 0);
 
-  // the n-th item of this CTA, once it is there; every reader tells when it has its copy
+  // A warp's work is a lambda that returns early where a wait gives up.
+  const WaitLimit waits{A.status, P.polls};
+  // the n-th item of this CTA for a warp, once it is there; every reader tells when it has its copy.  false: there are no more.
   auto take_item = [&](int n, PrefillItem& item) {
-    mbar_wait_fast(&item_full[n & 1], (n >> 1) & 1, A.status);
+    if (!warp_wait(&item_full[n & 1], (n >> 1) & 1, waits)) return false;
     item = *reinterpret_cast<const PrefillItem*>(item_smem + (n & 1) * 64);
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&item_empty[n & 1]);
+    return item.slot >= 0;
   };
 
   if (warp >= 8) {
@@ -352,7 +360,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
           item.slot = (int)w;
           break;
         }
-        if (n >= 2) mbar_wait_fast(&item_empty[n & 1], ((n >> 1) & 1) ^ 1, A.status);
+        if (n >= 2 && !warp_wait(&item_empty[n & 1], ((n >> 1) & 1) ^ 1, waits)) break;
         if (lane == 0) {
           *reinterpret_cast<PrefillItem*>(item_smem + (n & 1) * 64) = item;
           mbar_arrive(&item_full[n & 1]);
@@ -366,43 +374,46 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
       const bool mine = lane < boxes * Sh::kParts;
       const int box = lane & (boxes - 1), part = mine ? lane / boxes : 0;
       fence_proxy_async();                                     // rows that the append kernel stored
-      int it = 0;
-      for (int n = 0;; ++n) {
-        PrefillItem item;
-        take_item(n, item);
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&item_empty[n & 1]);
-        if (item.slot < 0) break;
-        const PrefillBlock& B = item.B;
-        if (n > 0) mbar_wait_fast(q_free, (n & 1) ^ 1, A.status);
-        if (lane == 0) {
-          const int tiles = B.row0 + 128 < B.n << P.g_shift ? 2 : 1;
-          mbar_expect_tx(q_full, tiles * Sh::kTileBytes);
-          for (int t = 0; t < tiles; ++t)
-            for (int p = 0; p < Sh::kParts; ++p)
-              tensor_g2s_4d(sq + t * Sh::kTileBytes + p * Sh::kPartBytes, P.qmap, 0, B.head * G, B.first + ((B.row0 + t * 128) >> P.g_shift), p, q_full);
-        }
-        __syncwarp();
-        for (int v = item.v0; v < item.v1; ++v) {
-          const int i = B.entry(v * kPrefillKeys + box * pr);
-          const bool fresh = P.append && i >= B.old;            // a box of the call's own rows (tokens behind the chunk: never used)
-          int chunk = P.oob_chunk;
-          if (mine && i < B.len && !fresh) {
-            const int pg = page_of(A, B.b, i);
-            if (pg >= 0) chunk = P.chunk0 + pg * A.n_kv_heads + B.head;
+      int it = 0, q_fills = 0;                                 // copies issued: ring stages, row blocks
+      [&] {
+        for (int n = 0;; ++n) {
+          PrefillItem item;
+          if (!take_item(n, item)) return;
+          const PrefillBlock& B = item.B;
+          if (n > 0 && !warp_wait(q_free, (n & 1) ^ 1, waits)) return;
+          ++q_fills;
+          if (lane == 0) {
+            const int tiles = B.row0 + 128 < B.n << P.g_shift ? 2 : 1;
+            mbar_expect_tx(q_full, tiles * Sh::kTileBytes);
+            for (int t = 0; t < tiles; ++t)
+              for (int p = 0; p < Sh::kParts; ++p)
+                tensor_g2s_4d(sq + t * Sh::kTileBytes + p * Sh::kPartBytes, P.qmap, 0, B.head * G, B.first + ((B.row0 + t * 128) >> P.g_shift), p, q_full);
           }
+          __syncwarp();
+          for (int v = item.v0; v < item.v1; ++v) {
+            const int i = B.entry(v * kPrefillKeys + box * pr);
+            const bool fresh = P.append && i >= B.old;          // a box of the call's own rows (tokens behind the chunk: never used)
+            int chunk = P.oob_chunk;
+            if (mine && i < B.len && !fresh) {
+              const int pg = page_of(A, B.b, i);
+              if (pg >= 0) chunk = P.chunk0 + pg * A.n_kv_heads + B.head;
+            }
 #pragma unroll
-          for (int kv = 0; kv < 2; ++kv, ++it) {
-            const int st = it % STAGES;
-            if (it >= STAGES) mbar_wait_fast(&empty[st], ((it / STAGES) & 1) ^ 1, A.status);
-            if (lane == 0) mbar_expect_tx(&full[st], Sh::kTileBytes);
-            __syncwarp();
-            unsigned char* dst = ring + st * Sh::kTileBytes + part * Sh::kPartBytes + box * pr * 128;
-            if (mine && fresh) tensor_g2s_4d(dst, kv ? P.vinmap : P.kinmap, 0, B.head, B.first + i - B.old, part, &full[st]);
-            else if (mine) tensor_g2s_4d(dst, kv ? P.vmap : P.kmap, 0, 0, part, chunk, &full[st]);
+            for (int kv = 0; kv < 2; ++kv, ++it) {
+              const int st = it % STAGES;
+              if (it >= STAGES && !warp_wait(&empty[st], ((it / STAGES) & 1) ^ 1, waits)) return;
+              if (lane == 0) mbar_expect_tx(&full[st], Sh::kTileBytes);
+              __syncwarp();
+              unsigned char* dst = ring + st * Sh::kTileBytes + part * Sh::kPartBytes + box * pr * 128;
+              if (mine && fresh) tensor_g2s_4d(dst, kv ? P.vinmap : P.kinmap, 0, B.head, B.first + i - B.old, part, &full[st]);
+              else if (mine) tensor_g2s_4d(dst, kv ? P.vmap : P.kmap, 0, 0, part, chunk, &full[st]);
+            }
           }
         }
-      }
+      }();
+      // they land before the CTA ends, whoever gave up
+      bool landed = q_fills == 0 || drain_wait(q_full, (q_fills & 1) ^ 1, A.status);
+      for (int f = max(0, it - STAGES); f < it && landed; ++f) landed = drain_wait(&full[f % STAGES], (f / STAGES) & 1, A.status);
     } else if (warp == 11) {
       // ---- the call's new rows into their pages
       if (P.append) append_rows<D>(P, 1 + kPrefillSoftmaxWarps);
@@ -414,74 +425,78 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
         const uint64_t k_ring = smem_matrix(smem_u32(ring), 16), v_ring = smem_matrix(smem_u32(ring), Sh::kPartBytes);
         uint32_t p_phase[2] = {0, 0};
         int it = 0;
-        for (int n = 0;; ++n) {
-          PrefillItem item;
-          take_item(n, item);
-          mbar_arrive(&item_empty[n & 1]);
-          if (item.slot < 0) {
-            for (int t = 0; t < 2 && n > 0; ++t) mbar_wait_fast(&o_full[t], (n & 1) ^ 1, A.status);      // nothing is in flight when the CTA ends
-            break;
-          }
-          const PrefillBlock& B = item.B;
-          const RowTile rt[2] = {row_tile(B, B.row0, P.g_shift), row_tile(B, B.row0 + 128, P.g_shift)};
-          bool pending[2] = {false, false}, started[2] = {false, false};
-          uint64_t vd = 0;                                        // values of the tile before
-          auto weights_times_values = [&](int t) {
-            if (!started[t] && n > 0) mbar_wait_fast(&o_free[t], (n & 1) ^ 1, A.status);
+        [&] {
+          for (int n = 0;; ++n) {
+            PrefillItem item;
+            if (!thread_wait(&item_full[n & 1], (n >> 1) & 1, waits)) return;
+            item = *reinterpret_cast<const PrefillItem*>(item_smem + (n & 1) * 64);
+            mbar_arrive(&item_empty[n & 1]);
+            if (item.slot < 0) return;
+            const PrefillBlock& B = item.B;
+            const RowTile rt[2] = {row_tile(B, B.row0, P.g_shift), row_tile(B, B.row0 + 128, P.g_shift)};
+            bool pending[2] = {false, false}, started[2] = {false, false};
+            uint64_t vd = 0;                                        // values of the tile before
+            auto weights_times_values = [&](int t) {
+              if (!started[t] && n > 0 && !thread_wait(&o_free[t], (n & 1) ^ 1, waits)) return false;
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              mbar_wait_fast(&p_ready[2 * t + half], p_phase[t], A.status);
-              tcgen05_after_sync();
+              for (int half = 0; half < 2; ++half) {
+                if (!thread_wait(&p_ready[2 * t + half], p_phase[t], waits)) return false;
+                tcgen05_after_sync();
 #pragma unroll
-              for (int k = half * 4; k < half * 4 + 4; ++k) mma_tmem(o_at[t], s_at[t] + k * 8, vd + k * 128, mma_shape(D, true), started[t] || k > 0);
-            }
-            p_phase[t] ^= 1;
-            started[t] = true;
-            pending[t] = false;
-          };
-          mbar_wait_fast(q_full, n & 1, A.status);
-          for (int v = item.v0; v < item.v1; ++v, it += 2) {
-            const int st = it % STAGES;
-            const uint64_t kd = k_ring + (uint32_t)(st * (Sh::kTileBytes >> 4));
-            // both copies ahead of the weights, so that P.V and the next logits of a row tile are issued in one go
-            mbar_wait_fast(&full[st], (it / STAGES) & 1, A.status);
-            if (v > item.v0) mbar_wait_fast(&full[(it - 1) % STAGES], ((it - 1) / STAGES) & 1, A.status);
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-              if (pending[t]) weights_times_values(t);
-              if (!tile_seen(B, rt[t], v, A.window, A.sink)) continue;
-              tcgen05_after_sync();
-#pragma unroll
-              for (int k = 0; k < D / 16; ++k) {
-                constexpr int kPart = Sh::kPartBytes >> 4;
-                mma_smem(s_at[t], q_at[t] + (k >> 2) * kPart + (k & 3) * 2, kd + (k >> 2) * kPart + (k & 3) * 2, mma_shape(kPrefillKeys, false), k > 0);
+                for (int k = half * 4; k < half * 4 + 4; ++k) mma_tmem(o_at[t], s_at[t] + k * 8, vd + k * 128, mma_shape(D, true), started[t] || k > 0);
               }
-              tcgen05_commit(&s_full[t]);
-              pending[t] = true;
-            }
-            tcgen05_commit(&empty[st]);
-            if (v > item.v0) tcgen05_commit(&empty[(it - 1) % STAGES]);
-            vd = v_ring + (uint32_t)(((it + 1) % STAGES) * (Sh::kTileBytes >> 4));
-          }
-          tcgen05_commit(q_free);
-          bool told = false;
-          if (item.v1 > item.v0) {
-            mbar_wait_fast(&full[(it - 1) % STAGES], ((it - 1) / STAGES) & 1, A.status);
+              p_phase[t] ^= 1;
+              started[t] = true;
+              pending[t] = false;
+              return true;
+            };
+            if (!thread_wait(q_full, n & 1, waits)) return;
+            for (int v = item.v0; v < item.v1; ++v, it += 2) {
+              const int st = it % STAGES;
+              const uint64_t kd = k_ring + (uint32_t)(st * (Sh::kTileBytes >> 4));
+              // both copies ahead of the weights, so that P.V and the next logits of a row tile are issued in one go
+              if (!thread_wait(&full[st], (it / STAGES) & 1, waits)) return;
+              if (v > item.v0 && !thread_wait(&full[(it - 1) % STAGES], ((it - 1) / STAGES) & 1, waits)) return;
 #pragma unroll
+              for (int t = 0; t < 2; ++t) {
+                if (pending[t] && !weights_times_values(t)) return;
+                if (!tile_seen(B, rt[t], v, A.window, A.sink)) continue;
+                tcgen05_after_sync();
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                  constexpr int kPart = Sh::kPartBytes >> 4;
+                  mma_smem(s_at[t], q_at[t] + (k >> 2) * kPart + (k & 3) * 2, kd + (k >> 2) * kPart + (k & 3) * 2, mma_shape(kPrefillKeys, false), k > 0);
+                }
+                tcgen05_commit(&s_full[t]);
+                pending[t] = true;
+              }
+              tcgen05_commit(&empty[st]);
+              if (v > item.v0) tcgen05_commit(&empty[(it - 1) % STAGES]);
+              vd = v_ring + (uint32_t)(((it + 1) % STAGES) * (Sh::kTileBytes >> 4));
+            }
+            tcgen05_commit(q_free);
+            bool told = false;
+            if (item.v1 > item.v0) {
+              if (!thread_wait(&full[(it - 1) % STAGES], ((it - 1) / STAGES) & 1, waits)) return;
+#pragma unroll
+              for (int t = 0; t < 2; ++t)
+                if (pending[t]) {
+                  if (!weights_times_values(t)) return;
+                  if (t == 0) tcgen05_commit(&o_full[0]);        // its rows need not wait for the other row tile
+                  told = told || t == 0;
+                }
+              tcgen05_commit(&empty[(it - 1) % STAGES]);
+            }
+            // a row tile without products in this item: its readers' word on the last item is still due
             for (int t = 0; t < 2; ++t)
-              if (pending[t]) {
-                weights_times_values(t);
-                if (t == 0) tcgen05_commit(&o_full[0]);        // its rows need not wait for the other row tile
-                told = told || t == 0;
-              }
-            tcgen05_commit(&empty[(it - 1) % STAGES]);
+              if (!started[t] && n > 0 && !thread_wait(&o_free[t], (n & 1) ^ 1, waits)) return;
+            if (!told) tcgen05_commit(&o_full[0]);
+            tcgen05_commit(&o_full[1]);
           }
-          // a row tile without products in this item: its readers' word on the last item is still due
-          for (int t = 0; t < 2; ++t)
-            if (!started[t] && n > 0) mbar_wait_fast(&o_free[t], (n & 1) ^ 1, A.status);
-          if (!told) tcgen05_commit(&o_full[0]);
-          tcgen05_commit(&o_full[1]);
-        }
+        }();
+        // nothing is in flight when the CTA ends
+        tcgen05_commit(drained);
+        drain_wait(drained, 0, A.status);
       }
       __syncwarp();
     }
@@ -494,165 +509,164 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
     const float c = A.scale_log2;
     uint32_t phase = 0;
     int it = 1;                                                 // ring position of the item's first values
-    for (int n = 0;; ++n) {
-      PrefillItem item;
-      take_item(n, item);
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&item_empty[n & 1]);
-      if (item.slot < 0) break;
-      const PrefillBlock& B = item.B;
-      const int R = B.row0 + t * 128 + row;
-      const RowTile my = row_tile(B, B.row0 + t * 128, P.g_shift);
-      const int pos = B.old + (R >> P.g_shift);
-      const bool live = R < B.n << P.g_shift;
-      const int lo_key = A.window > 0 ? max(0, pos - A.window + 1) : 0;
-      float m = -INFINITY, l = 0.f;                             // m: reference of the exponentials, in logits
-      bool first = true;
-      for (int v = item.v0; v < item.v1; ++v) {
-        const int v_at = v * kPrefillKeys;
-        if (!tile_seen(B, my, v, A.window, A.sink)) continue;
-        mbar_wait_fast(&s_full[t], phase, A.status);
-        phase ^= 1;
-        tcgen05_after_sync();
-        uint32_t x[128];
+    [&] {
+      for (int n = 0;; ++n) {
+        PrefillItem item;
+        if (!take_item(n, item)) return;
+        const PrefillBlock& B = item.B;
+        const int R = B.row0 + t * 128 + row;
+        const RowTile my = row_tile(B, B.row0 + t * 128, P.g_shift);
+        const int pos = B.old + (R >> P.g_shift);
+        const bool live = R < B.n << P.g_shift;
+        const int lo_key = A.window > 0 ? max(0, pos - A.window + 1) : 0;
+        float m = -INFINITY, l = 0.f;                             // m: reference of the exponentials, in logits
+        bool first = true;
+        for (int v = item.v0; v < item.v1; ++v) {
+          const int v_at = v * kPrefillKeys;
+          if (!tile_seen(B, my, v, A.window, A.sink)) continue;
+          if (!warp_wait(&s_full[t], phase, waits)) return;
+          phase ^= 1;
+          tcgen05_after_sync();
+          uint32_t x[128];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) tmem_load32(s_at + i * 32, x + i * 32);
-        tmem_wait_loads();
-        // a tile that every row of the row tile sees whole needs no mask
-        if (!tile_whole(B, my, v, A.window, A.sink)) {
+          for (int i = 0; i < 4; ++i) tmem_load32(s_at + i * 32, x + i * 32);
+          tmem_wait_loads();
+          // a tile that every row of the row tile sees whole needs no mask
+          if (!tile_whole(B, my, v, A.window, A.sink)) {
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+              const int at = v_at + h * 32, e0 = at - B.sink_rows + B.start;      // of the entries behind the sinks' pages
+              uint32_t see = low_bits(pos + 1 - e0) & (~low_bits(lo_key - e0) | low_bits(A.sink - e0));
+              if (at < B.sink_rows) {
+                const uint32_t front = low_bits(B.sink_rows - at);
+                see = (front & low_bits(min(A.sink, pos + 1) - at)) | (~front & see);
+              }
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (!(see >> i & 1)) x[h * 32 + i] = 0xff800000u;
+            }
+          }
+          float mx4[4];                                           // four chains: the latency of one would show
+#pragma unroll
+          for (int i = 0; i < 4; ++i) mx4[i] = max3(__uint_as_float(x[i]), __uint_as_float(x[4 + i]), __uint_as_float(x[8 + i]));
+#pragma unroll
+          for (int i = 12; i < 124; i += 8)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mx4[e] = max3(mx4[e], __uint_as_float(x[i + e]), __uint_as_float(x[i + 4 + e]));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) mx4[e] = fmaxf(mx4[e], __uint_as_float(x[124 + e]));
+          const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
+          if (first) {
+            m = mx;
+            first = false;
+          } else {
+            const bool grow = (mx - m) * c > 8.f;                 // true too where m is still -infinity and mx is not
+            if (__any_sync(~0u, grow)) {
+              const float f = grow ? exp2_fast((m - mx) * c) : 1.f;
+              if (grow) m = mx;
+              l *= f;
+#pragma unroll
+              for (int i = 0; i < D / 16; ++i) {
+                uint32_t o[16];
+                tmem_load16(o_at + i * 16, o);
+                tmem_wait_loads();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                tmem_store16(o_at + i * 16, o);
+              }
+            }
+          }
+          const int v_len = B.len - B.start + B.sink_rows;          // where the sequence ends
+          if (v_at + kPrefillKeys > v_len) {
+            // rows behind the sequence may hold anything: their weights are zero, their values have to be finite
+            const int at = it + 2 * (v - item.v0), st = at % STAGES;
+            if (!warp_wait(&full[st], (at / STAGES) & 1, waits)) return;
+            for (int e = row + (v_len - v_at) * 8 * Sh::kParts; e < kPrefillKeys * 8 * Sh::kParts; e += 128) {
+              const int r = e / (8 * Sh::kParts), piece = e % (8 * Sh::kParts);
+              *reinterpret_cast<uint4*>(ring + st * Sh::kTileBytes + (piece >> 3) * Sh::kPartBytes + r * 128 + (piece & 7) * 16) = make_uint4(0, 0, 0, 0);
+            }
+            fence_proxy_async();
+          }
+          const float shift = m == -INFINITY ? 0.f : -m * c;
+          const uint64_t c2 = pair(c, c), shift2 = pair(shift, shift);
+          uint64_t sum2[4] = {0, 0, 0, 0};
 #pragma unroll
           for (int h = 0; h < 4; ++h) {
-            const int at = v_at + h * 32, e0 = at - B.sink_rows + B.start;      // of the entries behind the sinks' pages
-            uint32_t see = low_bits(pos + 1 - e0) & (~low_bits(lo_key - e0) | low_bits(A.sink - e0));
-            if (at < B.sink_rows) {
-              const uint32_t front = low_bits(B.sink_rows - at);
-              see = (front & low_bits(min(A.sink, pos + 1) - at)) | (~front & see);
+            uint32_t w[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              float p0, p1;
+              unpair(fma2_(pair(__uint_as_float(x[h * 32 + 2 * i]), __uint_as_float(x[h * 32 + 2 * i + 1])), c2, shift2), p0, p1);
+              p0 = exp2_fast(p0);
+              p1 = exp2_fast(p1);
+              sum2[i & 3] = add2(sum2[i & 3], pair(p0, p1));
+              w[i] = pack_bf16(p0, p1);
             }
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (!(see >> i & 1)) x[h * 32 + i] = 0xff800000u;
+            tmem_store16(s_at + h * 16, w);
+            if (h & 1) {                                          // half of the weights: its products may start
+              tmem_wait_stores();
+              tcgen05_before_sync();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&p_ready[2 * t + (h >> 1)]);
+            }
           }
+          float a0, a1;
+          unpair(add2(add2(sum2[0], sum2[1]), add2(sum2[2], sum2[3])), a0, a1);
+          l += a0 + a1;
         }
-        float mx4[4];                                           // four chains: the latency of one would show
+        it += 2 * (item.v1 - item.v0);
+        // ---- output
+        if (!warp_wait(&o_full[t], n & 1, waits)) return;
+        tcgen05_after_sync();
+        const bool seen = !(l <= 0.f);                            // else the row's TMEM lane may hold anything
+        const float inv = seen ? 1.f / l : 0.f;
+        // rows of the eight lanes that exchange pieces, and this lane's 16-byte piece of 128
+        const int row8 = t * 128 + (row & ~7), piece = lane & 7;
+        if (item.whole) {
+#pragma unroll 1
+          for (int i = 0; i < D / 64; ++i) {
+            uint32_t o[64], y[8][4];
+            tmem_load32(o_at + i * 64, o);
+            tmem_load32(o_at + i * 64 + 32, o + 32);
+            tmem_wait_loads();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) mx4[i] = max3(__uint_as_float(x[i]), __uint_as_float(x[4 + i]), __uint_as_float(x[8 + i]));
+            for (int e = 0; e < 32; ++e)
+              y[e >> 2][e & 3] = seen ? pack_bf16(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv) : 0u;
+            exchange_pieces(y);
 #pragma unroll
-        for (int i = 12; i < 124; i += 8)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) mx4[e] = max3(mx4[e], __uint_as_float(x[i + e]), __uint_as_float(x[i + 4 + e]));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) mx4[e] = fmaxf(mx4[e], __uint_as_float(x[124 + e]));
-        const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
-        if (first) {
-          m = mx;
-          first = false;
+            for (int r = 0; r < 8; ++r) {
+              const int Rr = B.row0 + row8 + r, tok = Rr >> P.g_shift;
+              if (tok >= B.n) break;
+              __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + ((long long)(B.first + tok) * A.n_q_heads + B.head * G + (Rr & (G - 1))) * D + i * 64;
+              reinterpret_cast<uint4*>(out)[piece] = make_uint4(y[r][0], y[r][1], y[r][2], y[r][3]);
+            }
+          }
+          if (live && A.lse) {
+            const long long at = (long long)(B.first + (R >> P.g_shift)) * A.n_q_heads + B.head * G + (R & (G - 1));
+            A.lse[at] = seen ? (m * c + log2f(l)) * kLn2 : -INFINITY;
+          }
         } else {
-          const bool grow = (mx - m) * c > 8.f;                 // true too where m is still -infinity and mx is not
-          if (__any_sync(~0u, grow)) {
-            const float f = grow ? exp2_fast((m - mx) * c) : 1.f;
-            if (grow) m = mx;
-            l *= f;
+          // a warp's store covers 32 rows' same four channels, which lie side by side
+          float4* part = P.part + (long long)item.slot * (D / 4) * kPrefillRows + t * 128 + row;
+#pragma unroll 1
+          for (int i = 0; i < D / 32; ++i) {
+            uint32_t o[32];
+            tmem_load32(o_at + i * 32, o);
+            tmem_wait_loads();
+            if (live && seen) {
 #pragma unroll
-            for (int i = 0; i < D / 16; ++i) {
-              uint32_t o[16];
-              tmem_load16(o_at + i * 16, o);
-              tmem_wait_loads();
-#pragma unroll
-              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-              tmem_store16(o_at + i * 16, o);
+              for (int e = 0; e < 8; ++e)
+                part[(i * 8 + e) * kPrefillRows] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]),
+                                                               __uint_as_float(o[4 * e + 3]));
             }
           }
+          if (live) P.part_ml[(long long)item.slot * kPrefillRows + t * 128 + row] = make_float2(seen ? m * c : -INFINITY, seen ? l : 0.f);
         }
-        const int v_len = B.len - B.start + B.sink_rows;          // where the sequence ends
-        if (v_at + kPrefillKeys > v_len) {
-          // rows behind the sequence may hold anything: their weights are zero, their values have to be finite
-          const int at = it + 2 * (v - item.v0), st = at % STAGES;
-          mbar_wait_fast(&full[st], (at / STAGES) & 1, A.status);
-          for (int e = row + (v_len - v_at) * 8 * Sh::kParts; e < kPrefillKeys * 8 * Sh::kParts; e += 128) {
-            const int r = e / (8 * Sh::kParts), piece = e % (8 * Sh::kParts);
-            *reinterpret_cast<uint4*>(ring + st * Sh::kTileBytes + (piece >> 3) * Sh::kPartBytes + r * 128 + (piece & 7) * 16) = make_uint4(0, 0, 0, 0);
-          }
-          fence_proxy_async();
-        }
-        const float shift = m == -INFINITY ? 0.f : -m * c;
-        const uint64_t c2 = pair(c, c), shift2 = pair(shift, shift);
-        uint64_t sum2[4] = {0, 0, 0, 0};
-#pragma unroll
-        for (int h = 0; h < 4; ++h) {
-          uint32_t w[16];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            float p0, p1;
-            unpair(fma2_(pair(__uint_as_float(x[h * 32 + 2 * i]), __uint_as_float(x[h * 32 + 2 * i + 1])), c2, shift2), p0, p1);
-            p0 = exp2_fast(p0);
-            p1 = exp2_fast(p1);
-            sum2[i & 3] = add2(sum2[i & 3], pair(p0, p1));
-            w[i] = pack_bf16(p0, p1);
-          }
-          tmem_store16(s_at + h * 16, w);
-          if (h & 1) {                                          // half of the weights: its products may start
-            tmem_wait_stores();
-            tcgen05_before_sync();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&p_ready[2 * t + (h >> 1)]);
-          }
-        }
-        float a0, a1;
-        unpair(add2(add2(sum2[0], sum2[1]), add2(sum2[2], sum2[3])), a0, a1);
-        l += a0 + a1;
+        tcgen05_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&o_free[t]);
       }
-      it += 2 * (item.v1 - item.v0);
-      // ---- output
-      mbar_wait_fast(&o_full[t], n & 1, A.status);
-      tcgen05_after_sync();
-      const bool seen = !(l <= 0.f);                            // else the row's TMEM lane may hold anything
-      const float inv = seen ? 1.f / l : 0.f;
-      // rows of the eight lanes that exchange pieces, and this lane's 16-byte piece of 128
-      const int row8 = t * 128 + (row & ~7), piece = lane & 7;
-      if (item.whole) {
-#pragma unroll 1
-        for (int i = 0; i < D / 64; ++i) {
-          uint32_t o[64], y[8][4];
-          tmem_load32(o_at + i * 64, o);
-          tmem_load32(o_at + i * 64 + 32, o + 32);
-          tmem_wait_loads();
-#pragma unroll
-          for (int e = 0; e < 32; ++e)
-            y[e >> 2][e & 3] = seen ? pack_bf16(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv) : 0u;
-          exchange_pieces(y);
-#pragma unroll
-          for (int r = 0; r < 8; ++r) {
-            const int Rr = B.row0 + row8 + r, tok = Rr >> P.g_shift;
-            if (tok >= B.n) break;
-            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + ((long long)(B.first + tok) * A.n_q_heads + B.head * G + (Rr & (G - 1))) * D + i * 64;
-            reinterpret_cast<uint4*>(out)[piece] = make_uint4(y[r][0], y[r][1], y[r][2], y[r][3]);
-          }
-        }
-        if (live && A.lse) {
-          const long long at = (long long)(B.first + (R >> P.g_shift)) * A.n_q_heads + B.head * G + (R & (G - 1));
-          A.lse[at] = seen ? (m * c + log2f(l)) * kLn2 : -INFINITY;
-        }
-      } else {
-        // a warp's store covers 32 rows' same four channels, which lie side by side
-        float4* part = P.part + (long long)item.slot * (D / 4) * kPrefillRows + t * 128 + row;
-#pragma unroll 1
-        for (int i = 0; i < D / 32; ++i) {
-          uint32_t o[32];
-          tmem_load32(o_at + i * 32, o);
-          tmem_wait_loads();
-          if (live && seen) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              part[(i * 8 + e) * kPrefillRows] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]),
-                                                             __uint_as_float(o[4 * e + 3]));
-          }
-        }
-        if (live) P.part_ml[(long long)item.slot * kPrefillRows + t * 128 + row] = make_float2(seen ? m * c : -INFINITY, seen ? l : 0.f);
-      }
-      tcgen05_before_sync();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&o_free[t]);
-    }
+    }();
     if (P.append) append_rows<D>(P, 1 + kPrefillSoftmaxWarps);     // what warp 11 has not come to
   }
   tcgen05_before_sync();
@@ -741,8 +755,9 @@ __global__ void __launch_bounds__(kWeightsThreads, 1) paged_weights_tc_kernel(co
   uint64_t* s_full = k_full + 1;       // [key tile][buffer]
   uint64_t* s_empty = s_full + 4;
   uint64_t* lse_full = s_empty + 4;    // [buffer]
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(lse_full + 2);
-  float* lse = reinterpret_cast<float*>(tmem_slot + 6);                 // [buffer][128] base-2 log-sums of a row tile
+  uint64_t* drained = lse_full + 2;    // all matrix instructions are done
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drained + 1);
+  float* lse = reinterpret_cast<float*>(tmem_slot + 4);               // [buffer][128] base-2 log-sums of a row tile
   float* sums = lse + 256;                                            // [key tile][128] from the second halves
 
   const PagedParams& A = P.A;
@@ -762,6 +777,7 @@ __global__ void __launch_bounds__(kWeightsThreads, 1) paged_weights_tc_kernel(co
     mbar_init(k_full, 1);
     for (int i = 0; i < 4; ++i) { mbar_init(&s_full[i], 1); mbar_init(&s_empty[i], 8); }
     for (int i = 0; i < 2; ++i) mbar_init(&lse_full[i], 1);
+    mbar_init(drained, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 16) tmem_take(tmem_slot);
@@ -770,6 +786,8 @@ __global__ void __launch_bounds__(kWeightsThreads, 1) paged_weights_tc_kernel(co
   tcgen05_after_sync();
   griddep_launch();                                                   // behind the allocation, as in the kernel above
   const uint32_t tmem = __shfl_sync(~0u, *tmem_slot, 0);
+
+  const WaitLimit waits{A.status, P.polls};
 
   if (warp == 17) {
     // ---- copies
@@ -786,14 +804,18 @@ __global__ void __launch_bounds__(kWeightsThreads, 1) paged_weights_tc_kernel(co
       }
       tensor_g2s_4d(sk + (at >> 7) * Sh::kTileBytes + part * Sh::kPartBytes + (at & 127) * 128, P.kmap, 0, 0, part, chunk, k_full);
     }
-    for (int it = 0; it < tiles; ++it) {
+    int it = 0;
+    for (; it < tiles; ++it) {
       const int st = it % STAGES;
-      if (it >= STAGES) mbar_wait_fast(&empty[st], ((it / STAGES) & 1) ^ 1, A.status);
+      if (it >= STAGES && !warp_wait(&empty[st], ((it / STAGES) & 1) ^ 1, waits)) break;
       if (lane == 0) mbar_expect_tx(&full[st], Sh::kTileBytes);
       __syncwarp();
       if (lane < D / 64)
         tensor_g2s_4d(ring + st * Sh::kTileBytes + lane * Sh::kPartBytes, P.qmap, 0, head * G, s.first + (((tile0 + it) * 128) >> P.g_shift), lane, &full[st]);
     }
+    // they land before the CTA ends, whoever gave up
+    bool landed = drain_wait(k_full, 0, A.status);
+    for (int f = max(0, it - STAGES); f < it && landed; ++f) landed = drain_wait(&full[f % STAGES], (f / STAGES) & 1, A.status);
   } else if (warp == 18) {
     // ---- log-sums of the row tiles
     for (int it = 0; it < tiles; ++it) {
@@ -804,8 +826,7 @@ __global__ void __launch_bounds__(kWeightsThreads, 1) paged_weights_tc_kernel(co
         const int R = (tile0 + it) * 128 + j * 32 + lane, tok = R >> P.g_shift;
         x[j] = tok < s.n ? A.lse[(long long)(s.first + tok) * A.n_q_heads + head * G + (R & (G - 1))] * kLog2e : 0.f;
       }
-      if (it >= 2)
-        for (int t = 0; t < 2; ++t) mbar_wait_fast(&s_empty[t * 2 + buf], ((it >> 1) & 1) ^ 1, A.status);
+      if (it >= 2 && (!warp_wait(&s_empty[buf], ((it >> 1) & 1) ^ 1, waits) || !warp_wait(&s_empty[2 + buf], ((it >> 1) & 1) ^ 1, waits))) break;
 #pragma unroll
       for (int j = 0; j < 4; ++j) lse[buf * 128 + j * 32 + lane] = x[j];
       __syncwarp();
@@ -815,26 +836,29 @@ __global__ void __launch_bounds__(kWeightsThreads, 1) paged_weights_tc_kernel(co
     // ---- matrix instructions, all by one elected thread
     if (elect_one()) {
       const uint64_t k_at[2] = {smem_matrix(smem_u32(sk), 16), smem_matrix(smem_u32(sk + Sh::kTileBytes), 16)}, q_ring = smem_matrix(smem_u32(ring), 16);
-      mbar_wait_fast(k_full, 0, A.status);
-      for (int it = 0; it < tiles; ++it) {
-        const int st = it % STAGES, buf = it & 1;
-        const uint64_t qd = q_ring + (uint32_t)(st * (Sh::kTileBytes >> 4));
-        mbar_wait_fast(&full[st], (it / STAGES) & 1, A.status);
+      [&] {
+        if (!thread_wait(k_full, 0, waits)) return;
+        for (int it = 0; it < tiles; ++it) {
+          const int st = it % STAGES, buf = it & 1;
+          const uint64_t qd = q_ring + (uint32_t)(st * (Sh::kTileBytes >> 4));
+          if (!thread_wait(&full[st], (it / STAGES) & 1, waits)) return;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          if (it >= 2) mbar_wait_fast(&s_empty[t * 2 + buf], ((it >> 1) & 1) ^ 1, A.status);
-          tcgen05_after_sync();
+          for (int t = 0; t < 2; ++t) {
+            if (it >= 2 && !thread_wait(&s_empty[t * 2 + buf], ((it >> 1) & 1) ^ 1, waits)) return;
+            tcgen05_after_sync();
 #pragma unroll
-          for (int k = 0; k < D / 16; ++k) {
-            constexpr int kPart = Sh::kPartBytes >> 4;
-            mma_smem(tmem + (t * 2 + buf) * 128, k_at[t] + (k >> 2) * kPart + (k & 3) * 2, qd + (k >> 2) * kPart + (k & 3) * 2, mma_shape(128, false), k > 0);
+            for (int k = 0; k < D / 16; ++k) {
+              constexpr int kPart = Sh::kPartBytes >> 4;
+              mma_smem(tmem + (t * 2 + buf) * 128, k_at[t] + (k >> 2) * kPart + (k & 3) * 2, qd + (k >> 2) * kPart + (k & 3) * 2, mma_shape(128, false), k > 0);
+            }
+            tcgen05_commit(&s_full[t * 2 + buf]);
           }
-          tcgen05_commit(&s_full[t * 2 + buf]);
+          tcgen05_commit(&empty[st]);
         }
-        tcgen05_commit(&empty[st]);
-      }
-      // the last copies and instructions are done before the CTA ends
-      for (int t = 0; t < 2; ++t) mbar_wait_fast(&s_full[t * 2 + ((tiles - 1) & 1)], ((tiles - 1) >> 1) & 1, A.status);
+      }();
+      // nothing is in flight when the CTA ends
+      tcgen05_commit(drained);
+      drain_wait(drained, 0, A.status);
     }
     __syncwarp();
   } else if (warp < 16) {
@@ -847,10 +871,11 @@ __global__ void __launch_bounds__(kWeightsThreads, 1) paged_weights_tc_kernel(co
     const long long t_hi = A.window == 0 || e < A.sink ? s.n : min((long long)s.n, (long long)e - old + A.window);
     const int r_hi = e < s.len ? (int)(max(t_hi, 0LL) << P.g_shift) : 0;
     float total = 0.f;
+    bool ok = true;
     for (int it = 0; it < tiles; ++it) {
       const int buf = it & 1, row0 = (tile0 + it) * 128 + half * 64;
-      mbar_wait_fast(&lse_full[buf], (it >> 1) & 1, A.status);
-      mbar_wait_fast(&s_full[t * 2 + buf], (it >> 1) & 1, A.status);
+      ok = warp_wait(&lse_full[buf], (it >> 1) & 1, waits) && warp_wait(&s_full[t * 2 + buf], (it >> 1) & 1, waits);
+      if (!ok) break;
       tcgen05_after_sync();
       const bool whole = __all_sync(~0u, row0 >= r_lo && row0 + 64 <= r_hi);
       float sum[4] = {0.f, 0.f, 0.f, 0.f};
@@ -890,7 +915,7 @@ __global__ void __launch_bounds__(kWeightsThreads, 1) paged_weights_tc_kernel(co
     }
     if (half) sums[t * 128 + (tid & 127)] = total;
     asm volatile("bar.sync 1, 512;" ::: "memory");
-    if (!half && e < s.len) {
+    if (ok && !half && e < s.len) {
       float* a = A.scores + ((long long)b * A.n_kv_heads + head) * A.score_stride + e;
       *a = (A.k && e >= old ? 0.f : *a) + (total + sums[t * 128 + (tid & 127)]) * (1.f / G);
     }

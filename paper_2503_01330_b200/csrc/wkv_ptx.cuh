@@ -5,7 +5,7 @@
 
 namespace wkv {
 
-constexpr uint32_t kSpinLimit = 1u << 22;             // polls of a bounded wait (mbarrier, or a lane's arrival counter; each poll sleeps briefly)
+constexpr uint32_t kSpinLimit = 1u << 22;             // polls of a bounded wait (mbarrier: some 20 s, see below; or a lane's arrival counter)
 
 enum StatusBits : uint32_t { kStatusWaitTimeout = 1u, kStatusBadLink = 2u, kStatusBadTable = 4u };
 
@@ -43,11 +43,19 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, uint32
   atomicOr(status, kStatusWaitTimeout);
   return false;
 }
-// The same for waits on a kernel's critical path: one instruction when the barrier is ready (a fifth of mbar_wait's cycles, whose
-// loop the compiler guards for divergence), no sleeping while it is not.  At most kFastPolls polls (some tenths
-// of a second, where a wait in a working kernel takes microseconds).
-constexpr uint32_t kFastPolls = 1u << 23;
-__device__ __forceinline__ bool mbar_wait_fast(uint64_t* bar, uint32_t parity, uint32_t* status) {
+// Waits of warps that work for one another.  A wait that returns false has used up its limit and recorded it in the status word, and
+// means "leave": who gets it neither touches what it waited for nor arrives anywhere any more, so the others' waits run out in turn
+// and the CTA ends within a few limits.  Who has copies or matrix instructions in flight waits for those (drain_wait) before that.
+// The polls do not sleep and are one instruction when the barrier is ready (a fifth of mbar_wait's cycles, whose loop the compiler
+// guards for divergence); anything but straight code behind them, such as a second loop or a look at a flag of the CTA, cost the
+// prompt kernel 4 to 6 %.  A poll in vain was measured to take 5 us (the instruction suspends the thread).
+constexpr uint32_t kWaitPolls = 1u << 17;             // 0.7 s
+constexpr uint32_t kDrainPolls = 1u << 15;
+struct WaitLimit {
+  uint32_t* status;
+  uint32_t polls;
+};
+__device__ __forceinline__ bool mbar_poll(uint64_t* bar, uint32_t parity, uint32_t polls) {
   uint32_t left;
   asm volatile(
       "{\n\t.reg .pred done, more;\n\t.reg .u32 n;\n\tmov.u32 n, %3;\n"
@@ -55,10 +63,24 @@ __device__ __forceinline__ bool mbar_wait_fast(uint64_t* bar, uint32_t parity, u
       "sub.u32 n, n, 1;\n\tsetp.ne.u32 more, n, 0;\n\t@more bra POLL;\n"
       "OUT:\n\tmov.u32 %0, n;\n\t}"
       : "=r"(left)
-      : "r"(smem_u32(bar)), "r"(parity), "n"(kFastPolls)
+      : "r"(smem_u32(bar)), "r"(parity), "r"(polls)
       : "memory");
-  if (left == 0) atomicOr(status, kStatusWaitTimeout);
   return left != 0;
+}
+// By one thread ...
+__device__ __forceinline__ bool thread_wait(uint64_t* bar, uint32_t parity, const WaitLimit& w) {
+  if (mbar_poll(bar, parity, w.polls)) return true;
+  atomicOr(w.status, kStatusWaitTimeout);
+  return false;
+}
+// ... and by a converged warp, which gets one answer.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const WaitLimit& w) {
+  if (__all_sync(~0u, mbar_poll(bar, parity, w.polls))) return true;
+  atomicOr(w.status, kStatusWaitTimeout);
+  return false;
+}
+__device__ __forceinline__ bool drain_wait(uint64_t* bar, uint32_t parity, uint32_t* status) {
+  return thread_wait(bar, parity, WaitLimit{status, kDrainPolls});
 }
 // A consumer warp hands a ring stage back to the producer.  The fence puts every lane's reads of the stage ahead of
 // lane 0's arrival whatever instruction did the reading: with fragment loads (ldmatrix) in place of plain loads, the

@@ -74,3 +74,21 @@ def test_status_on_a_side_stream_keeps_the_next_report():
         assert cache.wkv_status() == 0
         side.synchronize()
     cache.close()
+
+
+def test_a_wait_that_gives_up_is_reported_and_the_handle_goes_on():
+    """The self-test's waits, of 400 polls, are for barriers that nothing arrives at."""
+    for prefill in (False, True):
+        c = Case(lens=[300, 20], new=[200, 9] if prefill else [1, 1], page=16, prefill=prefill, scores=True)
+        cache = c.cache()
+        cache.wkv_selftest_wait_timeout()                  # loads the kernel
+        assert cache.wkv_status() == binding.WKV_ERR_TIMEOUT and cache.wkv_status() == 0
+        start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        start.record()
+        cache.wkv_selftest_wait_timeout()
+        end.record()
+        assert cache.wkv_status() == binding.WKV_ERR_TIMEOUT and cache.wkv_status() == 0
+        ms = start.elapsed_time(end)
+        assert ms < 500, f"{ms:.3f} ms"
+        c.check(*c.run(cache), "afterwards")
+        cache.close()

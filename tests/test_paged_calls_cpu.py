@@ -94,3 +94,9 @@ def test_all_memory_is_kept_for_a_changed_stream(cache, monkeypatch, raw):
             assert block.streams[-1].cuda_stream == handle
     cache.wkv_set_stream(None)                              # the default stream
     assert (cache._lib.calls[-1][1][1].value or 0) == 0 and cache.k_pool.streams[-1].cuda_stream == 0
+
+
+def test_selftest_refuses_null():
+    from paper_2503_01330_b200.build import build_library
+    build_library()
+    assert binding.lib().wkv_paged_selftest_wait_timeout(None) == binding.WKV_ERR_INVALID
