@@ -92,6 +92,10 @@ __device__ __forceinline__ int seq_of_row(const PagedParams& P, int r) {
 __device__ __forceinline__ bool visible(int i, int pos, int window, int sink) {
   return i <= pos && (window == 0 || i > pos - window || i < sink);
 }
+// Does any token from position `pos` on see one of the n entries from i on?  Pages of which none does are not looked up.
+__device__ __forceinline__ bool seen_from(int i, int n, int pos, int window, int sink) {
+  return window == 0 || i + n > pos - window + 1 || i < sink;
+}
 
 // For tests: a warp's and a thread's wait for barriers that nothing arrives at.
 __global__ void __launch_bounds__(64) paged_wait_selftest_kernel(uint32_t* status) {

@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(kF32Groups * kF32Threads) paged_weights_f32_ke
 #pragma unroll 8
   for (int r = threadIdx.x / kVec; r < kF32Rows; r += kF32Groups * kRowsPerPass) {
     const int i = e0 + r;
-    const int pg = i < s.len ? page_of(A, b, i) : -1;
+    const int pg = i < s.len && seen_from(i, 1, old, A.window, A.sink) ? page_of(A, b, i) : -1;
     const float* kp = static_cast<const float*>(A.k_pool);
     stage_piece(sk + r * Sh::kStride + vec * 4, pg < 0 ? nullptr : kp + row_offset(A, pg, head, i, D) + vec * 4, kp);
   }

@@ -798,7 +798,7 @@ __global__ void __launch_bounds__(kWeightsThreads, 1) paged_weights_tc_kernel(co
     for (int j = lane; j < boxes * (D / 64); j += 32) {
       const int box = j & (boxes - 1), part = j / boxes, i = e0 + box * pr, at = box * pr;      // row of the block
       int chunk = P.oob_chunk;
-      if (i < s.len) {
+      if (i < s.len && seen_from(i, pr, old, A.window, A.sink)) {
         const int pg = page_of(A, b, i);
         if (pg >= 0) chunk = P.chunk0 + pg * A.n_kv_heads + head;
       }

@@ -92,3 +92,25 @@ def test_a_wait_that_gives_up_is_reported_and_the_handle_goes_on():
         assert ms < 500, f"{ms:.3f} ms"
         c.check(*c.run(cache), "afterwards")
         cache.close()
+
+
+# ---------------------------------------------------------------- released and bad pages
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("prefill,scores", [(False, False), (False, True), (True, False), (True, True)])
+@pytest.mark.parametrize("page,window,sink", [(16, 100, 4), (16, 1, 0), (32, 200, 33), (64, 64, 0)])
+def test_pages_that_nobody_sees_may_be_released(dtype, prefill, scores, page, window, sink):
+    """A window's cache gives back the pages behind it: any number may stand in the table there, with and without weights."""
+    new = [300, 140, 3, 33] if prefill else [1] * 4
+    c = Case(lens=[300, 1513, 600, 33], new=new, hq=8, hk=2, d=64, dtype=dtype, page=page, window=window, sink=sink, scores=scores,
+             seed=window, prefill=prefill)
+    table, released = c.table, c.table.clone()
+    for b, (n, t) in enumerate(zip(c.lens, c.new)):
+        for p in range(-(-n // page)):
+            if p * page >= sink and (p + 1) * page <= n - t - window + 1:
+                released[b, p] = (-1, c.n_pages, 2 ** 31 - 1)[p % 3]
+    assert (released != table).sum() > 10
+    c.table = released
+    result = c.run()                                       # asserts the status
+    c.table = table
+    c.check(*result, "released")
