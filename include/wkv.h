@@ -341,7 +341,8 @@ int wkv_paged_prefill(wkv_paged* c, int32_t layer, int32_t batch, const void* q,
  *   src_table [batch, src_width], dst_table [batch, dst_width];  seq_lens [batch];  new_lens [batch] out: min(len, budget)
  *   scores [batch, n_kv_heads, score_stride];  scores_out [batch, n_kv_heads, out_stride] or NULL: the kept entries' scores
  *   kept [batch, n_kv_heads, budget] int32 or NULL: their indexes.  Behind a sequence's new length both are left as they were.
- * out_stride >= min(budget, src_width * page_size); scores_out must not overlap scores. */
+ * out_stride >= min(budget, src_width * page_size); scores_out must not overlap scores.  No page may stand twice among those that
+ * dst_table's sequences get. */
 int wkv_paged_evict(wkv_paged* c, int32_t layer, int32_t batch, const int32_t* src_table, int32_t src_width,
                     const int32_t* dst_table, int32_t dst_width, const int32_t* seq_lens, int32_t* new_lens, int32_t budget,
                     int32_t recent, int32_t sink, const float* scores, int64_t score_stride, float* scores_out,

@@ -373,10 +373,9 @@ __global__ void __launch_bounds__(kMoveThreads) paged_move_kernel(const EvictPar
     const int src = P.kept[(long long)bh * P.kept_stride + i];
     const int sp = P.src_table[(long long)b * P.src_width + (src >> P.page_shift)];
     const int dp = P.dst_table[(long long)b * P.dst_width + (i >> P.page_shift)];
-    if ((unsigned)sp < (unsigned)P.n_pages && (unsigned)dp < (unsigned)P.n_pages) {
-      from = (((uint32_t)sp * P.n_kv_heads + head) << P.page_shift) + (src & (P.page - 1));
-      to = (((uint32_t)dp * P.n_kv_heads + head) << P.page_shift) + (i & (P.page - 1));
-    }
+    // an entry of a bad page counts as zeros, and its place in the destination must not keep what was there
+    if ((unsigned)sp < (unsigned)P.n_pages) from = (((uint32_t)sp * P.n_kv_heads + head) << P.page_shift) + (src & (P.page - 1));
+    if ((unsigned)dp < (unsigned)P.n_pages) to = (((uint32_t)dp * P.n_kv_heads + head) << P.page_shift) + (i & (P.page - 1));
   }
   constexpr int kVec = 2 * D * (int)sizeof(T) / 16;    // 16-byte pieces of an entry: K row, then V row
   constexpr int kEach = 16 / (int)sizeof(T);
@@ -388,7 +387,7 @@ __global__ void __launch_bounds__(kMoveThreads) paged_move_kernel(const EvictPar
       const int at = (s0 + k) * 32 + lane, c = at % kVec;
       const uint32_t row = __shfl_sync(~0u, from, at / kVec);
       const T* pool = static_cast<const T*>(c < kVec / 2 ? P.k_pool : P.v_pool);
-      if (row != kNone) piece[k] = __ldcs(reinterpret_cast<const uint4*>(pool + (long long)row * D + c % (kVec / 2) * kEach));
+      piece[k] = row != kNone ? __ldcs(reinterpret_cast<const uint4*>(pool + (long long)row * D + c % (kVec / 2) * kEach)) : make_uint4(0, 0, 0, 0);
     }
 #pragma unroll
     for (int k = 0; k < kMoveSteps; ++k) {

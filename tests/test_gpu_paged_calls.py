@@ -114,3 +114,40 @@ def test_pages_that_nobody_sees_may_be_released(dtype, prefill, scores, page, wi
     result = c.run()                                       # asserts the status
     c.table = table
     c.check(*result, "released")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_evict_from_and_to_bad_pages(dtype):
+    """An entry of a bad source page counts as zeros: its place in the destination holds zeros, and not what was there.  What goes
+    to a bad destination page goes nowhere."""
+    page, hk, d, budget = 16, 2, 64, 40
+    c = Case(lens=[100, 70], new=[1, 1], hq=hk, hk=hk, d=d, dtype=dtype, page=page, append=False, scores=True, spare=8, seed=21)
+    cache = c.cache()
+    dst = c.free_pages[:6].reshape(2, 3).clone()
+    good_dst = dst.clone()
+    table = c.table.clone()
+    table[0, 0], table[0, 5] = -1, c.n_pages               # sequence 0: two bad source pages
+    dst[1, 1] = 2 ** 31 - 1                                # sequence 1: a bad destination page
+    new_lens = torch.zeros(2, dtype=torch.int32, device="cuda")
+    kept = torch.full((2, hk, budget), -1, dtype=torch.int32, device="cuda")
+    lens = torch.tensor(c.lens, dtype=torch.int32, device="cuda")
+    cache.wkv_paged_evict(0, table.cuda(), dst.cuda(), lens, new_lens, budget, 6, 3, scores=c.scores.cuda(), kept=kept)
+    assert cache.wkv_status() == binding.WKV_ERR_STATE and cache.wkv_status() == 0
+    assert new_lens.tolist() == [budget, budget]
+    kept = kept.cpu()
+    want_k, want_v = c.k_pool.clone(), c.v_pool.clone()
+    zeroed = 0
+    for b in range(2):
+        for h in range(hk):
+            for at, i in enumerate(kept[b, h].tolist()):
+                if b == 1 and at // page == 1:
+                    continue
+                bad = b == 0 and i // page in (0, 5)
+                zeroed += bad
+                pg = int(good_dst[b, at // page])
+                want_k[0, pg, h, at % page] = torch.zeros(d) if bad else c.K[b][i, h]
+                want_v[0, pg, h, at % page] = torch.zeros(d) if bad else c.V[b][i, h]
+    assert zeroed >= 4
+    as_int = torch.int16 if dtype == "bf16" else torch.int32
+    assert torch.equal(c.gk.cpu().view(as_int), want_k.view(as_int)) and torch.equal(c.gv.cpu().view(as_int), want_v.view(as_int))
+    cache.close()
