@@ -260,7 +260,8 @@ const char* wkv_last_error(const wkv_ctx* ctx);
  * Conventions of these calls, beside those at the top of this file:
  *   - Tables, lengths and offsets are read on the device, so a captured call can be replayed with new ones.  A page number,
  *     length or offset out of range never leads to an access outside the pool or the call's buffers: that page counts as
- *     zeros, the length or offset is clamped, and wkv_paged_status reports WKV_ERR_STATE.  Columns of a table behind a
+ *     zeros (entries that the call brings for it are stored nowhere and count as zeros too), the length or offset is clamped,
+ *     and wkv_paged_status reports WKV_ERR_STATE.  Columns of a table behind a
  *     sequence's last page are not read; nor are those of pages of which no token of an attention call sees an entry, so a
  *     windowed cache may give back the pages behind its window.
  *   - Pool rows behind a sequence's length are never used, whatever bits they hold.  Rows inside it are expected to be finite.

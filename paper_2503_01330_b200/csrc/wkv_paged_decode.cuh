@@ -523,7 +523,8 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
               const int e = lane + 32 * j;
               if (e >= 2 * kPieces) continue;
               const bool is_v = e >= kPieces;
-              *reinterpret_cast<uint4*>((is_v ? tv : tk) + tile_offset<Sh::kParts>(s.len - 1 - i0 + row0, e % kPieces, pr, pr_shift)) = news[j];
+              *reinterpret_cast<uint4*>((is_v ? tv : tk) + tile_offset<Sh::kParts>(s.len - 1 - i0 + row0, e % kPieces, pr, pr_shift)) =
+                  new_page >= 0 ? news[j] : make_uint4(0, 0, 0, 0);
               if (new_page >= 0)
                 *reinterpret_cast<uint4*>(static_cast<T*>(is_v ? A.v_pool : A.k_pool) + row_offset(A, new_page, head, s.len - 1, D) +
                                           e % kPieces * (16 / (int)sizeof(T))) = news[j];

@@ -392,12 +392,9 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
           __syncwarp();
           for (int v = item.v0; v < item.v1; ++v) {
             const int i = B.entry(v * kPrefillKeys + box * pr);
-            const bool fresh = P.append && i >= B.old;          // a box of the call's own rows (tokens behind the chunk: never used)
-            int chunk = P.oob_chunk;
-            if (mine && i < B.len && !fresh) {
-              const int pg = page_of(A, B.b, i);
-              if (pg >= 0) chunk = P.chunk0 + pg * A.n_kv_heads + B.head;
-            }
+            const int pg = mine && i < B.len ? page_of(A, B.b, i) : -1;
+            const bool fresh = P.append && i >= B.old && pg >= 0;      // a box of the call's own rows (tokens behind the chunk: never used)
+            const int chunk = pg >= 0 ? P.chunk0 + pg * A.n_kv_heads + B.head : P.oob_chunk;
 #pragma unroll
             for (int kv = 0; kv < 2; ++kv, ++it) {
               const int st = it % STAGES;

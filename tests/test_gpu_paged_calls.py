@@ -151,3 +151,44 @@ def test_evict_from_and_to_bad_pages(dtype):
     as_int = torch.int16 if dtype == "bf16" else torch.int32
     assert torch.equal(c.gk.cpu().view(as_int), want_k.view(as_int)) and torch.equal(c.gv.cpu().view(as_int), want_v.view(as_int))
     cache.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("prefill", [False, True])
+@pytest.mark.parametrize("window,sink", [(0, 0), (30, 4)])
+def test_entries_of_bad_pages_count_as_zeros(dtype, prefill, window, sink):
+    """Outputs, log-sums and weights of a sequence with bad pages are those of a cache that holds zeros there, the call's own new
+    entries among them; nothing else is touched."""
+    new = [60, 30, 20] if prefill else [1, 1, 1]
+    c = Case(lens=[100, 90, 80], new=new, hq=4, hk=2, d=64, dtype=dtype, page=16, scores=True, seed=22, prefill=prefill, window=window,
+             sink=sink)
+    cache = c.cache()
+    q, k, v = c.rows()
+    table = c.table.clone()
+    bad = {0: [4, 6], 1: [1, 5], 2: [0, 3]} if prefill else {0: [6], 1: [1, 5], 2: [0, 3]}
+    for b, pages in bad.items():
+        for p in pages:
+            table[b, p] = (-1, c.n_pages, 2 ** 31 - 1, -2 ** 31)[(b + p) % 4]
+            c.K[b][p * 16:(p + 1) * 16] = 0
+            c.V[b][p * 16:(p + 1) * 16] = 0
+    out, lse = torch.full((c.T, 4, 64), 7.0, dtype=c.tdt, device="cuda"), torch.full((c.T, 4), 7.0, device="cuda")
+    scores, lens = c.scores.cuda(), torch.tensor(c.lens, dtype=torch.int32, device="cuda")
+    if prefill:
+        cache.wkv_paged_prefill(0, q, k, v, torch.tensor(c.starts, dtype=torch.int32, device="cuda"), table.cuda(), lens, out, window, sink, scores, lse)
+    else:
+        cache.wkv_paged_decode(0, q, k, v, table.cuda(), lens, out, window, sink, scores, lse)
+    assert cache.wkv_status() == binding.WKV_ERR_STATE
+    rows_k, rows_v = c.K, c.V
+    was_k, was_v = c.k_pool, c.v_pool
+    # the bad pages' rows stay as they were, whatever the definition counts there
+    want_k, want_v = was_k.clone(), was_v.clone()
+    for b, n in enumerate(c.lens):
+        for i in range(n - c.new[b], n):
+            if i // 16 not in bad[b]:
+                pg = int(c.table[b, i // 16])
+                want_k[0, pg, :, i % 16], want_v[0, pg, :, i % 16] = rows_k[b][i], rows_v[b][i]
+    as_int = torch.int16 if dtype == "bf16" else torch.int32
+    assert torch.equal(c.gk.cpu().view(as_int), want_k.view(as_int)) and torch.equal(c.gv.cpu().view(as_int), want_v.view(as_int))
+    c.check_pool = lambda what="": None
+    c.check(out, lse, scores, "bad pages")
+    cache.close()
