@@ -150,7 +150,7 @@ __device__ __forceinline__ WorkPlan work_plan(const PagedParams& A, int g_shift,
     w.items = (int)((pass == 0 ? units : all) * A.n_kv_heads);
     if (pass == 1) break;
     const long long more = (long long)slots - w.items;
-    if (more < w.items) break;                         // the row blocks are many enough
+    if (w.items == 0 || more < w.items) break;         // nothing to do, or row blocks enough
     w.run = (int)max(KEYS < 64 ? 2LL : 4LL, (all * A.n_kv_heads + more - 1) / more);
   }
   return w;

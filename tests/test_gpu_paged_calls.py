@@ -192,3 +192,23 @@ def test_entries_of_bad_pages_count_as_zeros(dtype, prefill, window, sink):
     c.check_pool = lambda what="": None
     c.check(out, lse, scores, "bad pages")
     cache.close()
+
+
+# ---------------------------------------------------------------- sizes
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("total_q", [5, 40000])
+def test_prompt_call_without_tokens(dtype, total_q):
+    """A captured call's batch may be all padding: rows of no sequence are left alone, whether the call is one that is cut or not,
+    and the next call on the handle is right."""
+    c = Case(lens=[300, 40], new=[200, 40], hq=4, hk=2, d=64, dtype=dtype, page=16, scores=True, seed=51)
+    cache = c.cache()
+    q, k, v = (torch.zeros(total_q, h, 64, dtype=c.tdt, device="cuda") for h in (4, 2, 2))
+    out, lse, scores = torch.full_like(q, 7.0), torch.full((total_q, 4), 7.0, device="cuda"), c.scores.cuda()
+    none, lens = torch.zeros(3, dtype=torch.int32, device="cuda"), torch.tensor(c.lens, dtype=torch.int32, device="cuda")
+    for n in (lens, torch.zeros_like(lens)):
+        cache.wkv_paged_prefill(0, q, k, v, none, c.table.cuda(), n, out, scores=scores, lse=lse)
+        assert cache.wkv_status() == 0
+        assert (out == 7).all() and (lse == 7).all() and torch.equal(scores.cpu(), c.scores)
+    c.check(*c.run(cache), "afterwards")
+    cache.close()
