@@ -212,3 +212,115 @@ def test_prompt_call_without_tokens(dtype, total_q):
         assert (out == 7).all() and (lse == 7).all() and torch.equal(scores.cpu(), c.scores)
     c.check(*c.run(cache), "afterwards")
     cache.close()
+
+
+MANY = [
+    # one kv head per query head; the last block of a sequence has one row tile (1 and 76 rows), or is full
+    dict(hq=32, hk=32, d=64, page=16, lens=[1537, 2300, 128, 1740, 40], new=[1537, 1100, 128, 1024, 0]),
+    # grouped heads under a window with sinks: row tiles that see nothing of a block's first or last tiles
+    dict(hq=32, hk=4, d=128, page=64, lens=[2100, 1001, 3000], new=[2100, 1001, 1290], window=300, sink=70),
+    # entries that are in the pool already, behind contexts, rows of q apart
+    dict(hq=40, hk=10, d=128, page=32, lens=[2500, 1500, 700], new=[1210, 1500, 333], append=False, strided=True),
+]
+
+
+@pytest.mark.parametrize("case", range(len(MANY)))
+@pytest.mark.parametrize("scores", [False, True])
+def test_prompts_of_many_items_a_cta(case, scores):
+    """The prompt kernel's CTAs, one per SM, take several row blocks each: what one leaves behind (barrier phases, ring positions,
+    item slots, counters) carries over to the next, and to the next call, whose results are the same bit for bit."""
+    c = Case(**MANY[case], scores=scores, seed=60 + case, prefill=True, extra_rows=2)
+    items = sum(-(-t * c.G // 256) for t in c.new) * c.hk
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    assert items > 3 * sms
+    cache = c.cache()
+    first = c.run(cache)
+    c.check(*first, f"{items} items")
+    small = Case(lens=[90], new=[90], hq=c.hq, hk=c.hk, d=c.d, page=c.page)
+    for _ in range(3):
+        again = c.run(cache)
+        for x, y in zip(first, again):
+            assert x is None or torch.equal(x, y)
+    cache.close()
+    small.check(*small.run(), "a handle of its own")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("prefill", [False, True])
+@pytest.mark.parametrize("scale", [0.5, 0.01, 0.73])
+def test_scales(dtype, prefill, scale):
+    """A softmax scale of the caller's: the definition, whose scale is 1 / sqrt(d), on queries that are scale * sqrt(d) times as large."""
+    c = Case(lens=[300, 70], new=[200, 9] if prefill else [1, 1], hq=8, hk=2, d=64, dtype=dtype, page=16, scores=True, seed=71, prefill=prefill)
+    cache = c.cache(scale=scale)
+    result = c.run(cache)
+    c.buf = c.buf.double()
+    c.buf[:, :c.hq] *= scale * c.d ** 0.5
+    c.check(*result, f"scale {scale}")
+    cache.close()
+
+
+# ---------------------------------------------------------------- shared pages
+
+def _shared(page, entries, **kw):
+    """Two sequences whose first `entries` entries (whole pages) are the same ones."""
+    c = Case(page=page, scores=True, **kw)
+    c.K[1][:entries], c.V[1][:entries] = c.K[0][:entries], c.V[0][:entries]
+    c.table[1, :entries // page] = c.table[0, :entries // page]
+    return c
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("prefill", [False, True])
+@pytest.mark.parametrize("window,sink", [(0, 0), (100, 20)])
+def test_sequences_share_context_pages(dtype, prefill, window, sink):
+    """Each sequence's weights are its own, and the shared pages stay as they were."""
+    c = _shared(16, 128, lens=[300, 200, 20], new=[150, 60, 20] if prefill else [1, 1, 1], hq=8, hk=2, d=64, dtype=dtype, window=window,
+                sink=sink, seed=81, prefill=prefill)
+    c.check(*c.run(), "shared")                            # the whole pool among it
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_sequences_that_share_pages_are_evicted_by_their_own_weights(dtype):
+    page, hk, d, budget, recent, sink = 32, 2, 64, 70, 20, 3
+    c = _shared(page, 96, lens=[200, 150], new=[1, 1], hq=hk, hk=hk, d=d, dtype=dtype, append=False, spare=8, seed=82)
+    cache = c.cache()
+    dst = c.free_pages[:6].reshape(2, 3)
+    new_lens, kept = torch.zeros(2, dtype=torch.int32, device="cuda"), torch.zeros(2, hk, budget, dtype=torch.int32, device="cuda")
+    cache.wkv_paged_evict(0, c.table.cuda(), dst.cuda(), torch.tensor(c.lens, dtype=torch.int32, device="cuda"), new_lens, budget, recent, sink,
+                          scores=c.scores.cuda(), kept=kept)
+    assert cache.wkv_status() == 0 and new_lens.tolist() == [budget, budget]
+    want_k, want_v = c.k_pool.clone(), c.v_pool.clone()
+    for b, n in enumerate(c.lens):
+        for h in range(hk):
+            order = sorted(range(sink, n - recent), key=lambda i: (float(c.scores[b, h, i]), i))
+            stay = sorted(set(range(n)) - set(order[:n - budget]))
+            assert kept[b, h].tolist() == stay
+            for at, i in enumerate(stay):
+                pg = int(dst[b, at // page])
+                want_k[0, pg, h, at % page], want_v[0, pg, h, at % page] = c.K[b][i, h], c.V[b][i, h]
+    as_int = torch.int16 if dtype == "bf16" else torch.int32
+    assert torch.equal(c.gk.cpu().view(as_int), want_k.view(as_int)) and torch.equal(c.gv.cpu().view(as_int), want_v.view(as_int))
+    cache.close()
+
+
+# ---------------------------------------------------------------- eviction around its shared memory
+
+@pytest.mark.parametrize("n", [32767, 32768, 32769, 33792, 33793])
+def test_evict_around_the_staged_length(n):
+    """Lanes of up to 32768 entries are selected from shared memory, longer ones from the scores themselves."""
+    from test_gpu_paged import _evict
+    _evict([n, 5], 900, 50, 4, hk=1, d=64, page=64, seed=n)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("window", [0, 300])
+def test_decode_repeats_bit_for_bit(dtype, window):
+    """Lanes cut over many CTAs: whichever piece comes last joins them, in the order of the pieces."""
+    c = Case(lens=[5000, 1200, 3, 2500], new=[1] * 4, hq=16, hk=4, d=128, dtype=dtype, page=32, scores=True, seed=91, window=window, sink=9 if window else 0)
+    cache = c.cache()
+    first = c.run(cache)
+    c.check(*first, "first")
+    for _ in range(20):
+        for x, y in zip(first, c.run(cache)):
+            assert torch.equal(x, y)
+    cache.close()
