@@ -261,10 +261,12 @@ const char* wkv_last_error(const wkv_ctx* ctx);
  *   - Tables, lengths and offsets are read on the device, so a captured call can be replayed with new ones.  A page number,
  *     length or offset out of range never leads to an access outside the pool or the call's buffers: that page counts as
  *     zeros (entries that the call brings for it are stored nowhere and count as zeros too), the length or offset is clamped,
- *     and wkv_paged_status reports WKV_ERR_STATE.  Columns of a table behind a
- *     sequence's last page are not read; nor are those of pages of which no token of an attention call sees an entry, so a
- *     windowed cache may give back the pages behind its window.
- *   - Pool rows behind a sequence's length are never used, whatever bits they hold.  Rows inside it are expected to be finite.
+ *     and wkv_paged_status reports WKV_ERR_STATE.  Columns of a table behind a sequence's last page are not read; nor are those
+ *     of pages of which no token of an attention call sees an entry, so a windowed cache may give back the pages behind its
+ *     window (an eviction reads its source table's columns up to the sequence's last page).
+ *   - Pool rows behind a sequence's length are never used, whatever bits they hold.  Rows inside it are expected to be finite:
+ *     an infinity or NaN in one may make any output of that sequence NaN, also of tokens that do not see the entry.
+ *   - out, lse and scores must not overlap a call's other arguments.
  *   - A row that sees no entry (a padded sequence of length 0) gets output 0 and log-sum -infinity.
  *   - The token at position p sees entry i if i <= p and (window == 0, or i > p - window, or i < sink).
  *   - scores [batch, n_kv_heads, score_stride] fp32, or NULL: the attention weight of every entry, averaged over the kv
