@@ -107,8 +107,8 @@ __global__ void __launch_bounds__(64) paged_wait_selftest_kernel(uint32_t* statu
   griddep_wait();
   __syncthreads();
   const WaitLimit waits{status, 400};
-  if (threadIdx.x < 32) warp_wait(&bars[0], 0, waits);
-  else if (threadIdx.x == 32) thread_wait(&bars[1], 0, waits);
+  if (threadIdx.x < 32) (void)warp_wait(&bars[0], 0, waits);
+  else if (threadIdx.x == 32) (void)thread_wait(&bars[1], 0, waits);
 }
 
 // ------------------------------------------------------------------------------------------------

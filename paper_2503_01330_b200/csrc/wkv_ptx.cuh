@@ -68,13 +68,13 @@ __device__ __forceinline__ bool mbar_poll(uint64_t* bar, uint32_t parity, uint32
   return left != 0;
 }
 // By one thread ...
-__device__ __forceinline__ bool thread_wait(uint64_t* bar, uint32_t parity, const WaitLimit& w) {
+[[nodiscard]] __device__ __forceinline__ bool thread_wait(uint64_t* bar, uint32_t parity, const WaitLimit& w) {
   if (mbar_poll(bar, parity, w.polls)) return true;
   atomicOr(w.status, kStatusWaitTimeout);
   return false;
 }
 // ... and by a converged warp, which gets one answer.
-__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const WaitLimit& w) {
+[[nodiscard]] __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const WaitLimit& w) {
   if (__all_sync(~0u, mbar_poll(bar, parity, w.polls))) return true;
   atomicOr(w.status, kStatusWaitTimeout);
   return false;

@@ -1,10 +1,13 @@
 """The binding's checks of a paged call's arguments, without a GPU: a cache on CPU tensors whose C calls are recorded."""
 import ctypes as C
+import os
+import re
 
 import pytest
 import torch
 
 from paper_2503_01330_b200 import binding
+from paper_2503_01330_b200.build import CSRC
 
 
 class Recorder:
@@ -100,3 +103,28 @@ def test_selftest_refuses_null():
     from paper_2503_01330_b200.build import build_library
     build_library()
     assert binding.lib().wkv_paged_selftest_wait_timeout(None) == binding.WKV_ERR_INVALID
+
+
+# What only a race or a hang on the GPU would show is checked in the source.
+
+def test_dependent_kernels_start_behind_the_tmem_allocation():
+    """A kernel that may start early and takes TMEM first would keep it until the one that it waits for has ended."""
+    kernels = open(os.path.join(CSRC, "wkv_paged_prefill.cuh")).read().split("__global__")[1:]
+    with_tmem = [k for k in kernels if "tmem_take(" in k]
+    assert len(with_tmem) == 2
+    for k in with_tmem:
+        assert k.count("griddep_launch();") == 1 and k.index("griddep_launch();") > k.index("tmem_take(")
+
+
+def test_nothing_runs_on_the_default_stream():
+    """Calls on the default stream are not ordered with the handle's where that one does not wait for it."""
+    text = open(os.path.join(CSRC, "wkv_paged_api.cu")).read()
+    assert not re.search(r"cudaMem(set|cpy)\(", text) and "<<<" not in text
+
+
+def test_waits_that_give_up_are_heeded():
+    """No paged kernel ignores what a wait says: its result is tested where it stands (mbar_wait's in the decode kernel's vote)."""
+    for name in ("wkv_paged_prefill.cuh", "wkv_paged_decode.cuh", "wkv_paged_f32.cuh"):
+        for line in open(os.path.join(CSRC, name)):
+            for call in re.finditer(r"\b(warp_wait|thread_wait|mbar_wait|wait)\(&?[a-z]", line):
+                assert re.search(r"if \(|= |return |&& |\|\| ", line[:call.start()]), line
