@@ -23,7 +23,7 @@
 // operand of P.V straight from TMEM) and both outputs (D columns each).  An output is rescaled in place, and only when a row's
 // maximum has grown by more than 2^8 since its reference was taken.
 //
-// Measured: 8192 tokens, 32 x 128 heads, 495 us = 1110 TFLOP/s in a row of up to 100 passes, 557..580 us on four GPUs in a long series
+// Measured: 8192 tokens, 32 x 128 heads, 495 us = 1110 TFLOP/s in a row of up to 100 passes, 557..586 us on five GPUs in a long series
 // at the power limit; a pair of tiles takes 2900..3100 cycles (tensor cores 2048): TMEM holds no third row tile that could hide the
 // chain logits, softmax, weights.
 #pragma once
