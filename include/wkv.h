@@ -31,7 +31,11 @@ extern "C" {
 
 typedef struct wkv_ctx wkv_ctx; /* opaque, library-owned */
 
-typedef enum { WKV_F32 = 0, WKV_BF16 = 1 } wkv_dtype;
+typedef enum {
+  WKV_F32 = 0,
+  WKV_BF16 = 1,
+  WKV_KV4 = 4 /* paged caches only: q, k, v, out in bf16, the pool's rows in 4 bits (see "Rows in 4 bits") */
+} wkv_dtype;
 
 typedef enum {
   WKV_OK = 0,
@@ -289,7 +293,7 @@ typedef struct {
   int32_t dtype;      /* wkv_dtype of q, k, v, out and the pool                                                   */
   float scale;        /* softmax scale; 0 selects 1/sqrt(head_dim)                                                */
   int32_t scores;     /* 1: calls may accumulate weights and evict (adds a workspace of 4 * max_batch * n_q_heads *
-                         max_pages * page_size bytes)                                                             */
+                         max_pages * page_size bytes); 0 with WKV_KV4                                             */
   void* stream;       /* cudaStream_t                                                                             */
   void* k_pool;       /* the caller's pools, 16-byte aligned device memory; both NULL: taken from the provider    */
   void* v_pool;
@@ -350,6 +354,77 @@ int wkv_paged_evict(wkv_paged* c, int32_t layer, int32_t batch, const int32_t* s
                     const int32_t* dst_table, int32_t dst_width, const int32_t* seq_lens, int32_t* new_lens, int32_t budget,
                     int32_t recent, int32_t sink, const float* scores, int64_t score_stride, float* scores_out,
                     int64_t out_stride, int32_t* kept);
+
+/* Rows in 4 bits (WKV_KV4).  32 neighbouring channels of a row share a scale s and a zero point z, a code n in 0..15 stands for
+ * s (n - z).  With lo = min(0, least) and hi = max(0, largest of the 32): s = (hi - lo) * (1/15) rounded up to four significant
+ * bits, and into 2^-17 .. 4096 (below 2^-14 to a multiple of 2^-17); z = rint(-lo * (1/s)), n = rint(x * (1/s)) + z, both clamped to
+ * 0..15; all of it in binary32, each operation rounded by itself.  Values beyond 15 * 4096 saturate.  s (n - z) is a bf16 number.
+ * A pool is [n_layers, n_pages, n_kv_heads, page_size * (head_dim / 2 + head_dim / 16)] bytes: of one kv head's part of a page first
+ * the codes, head_dim / 2 bytes a row, then a pair of bytes per row and group: bits 14..7 of s as a binary16 number; z.
+ * With D = head_dim, S = D / 32 groups, row i of the page, channel c = 32 g + r:
+ *   keys    r = 8 w + e: in the 32-bit word at byte 16 (g ^ x) + 4 w of the row, bits 4 (e / 2) + 16 (e % 2) and the three above;
+ *           x = (i / 2) % 4 for D = 128, (i / 4) % 2 for D = 64
+ *   values  r = 4 u + e: in the 16-bit word at byte (2 S u + 2 g) ^ x of the row, bits 4 e and the three above;
+ *           x = 32 ((i / 2) % 2) for D = 128, 0 for D = 64
+ * Such a handle takes wkv_paged_append, wkv_paged_decode (k and v, where given, are stored in 4 bits first, and the new token sees its
+ * entry as stored), wkv_paged_select, wkv_paged_decode_pages and wkv_paged_expand; prompts run on bf16 rows (wkv_paged_expand). */
+
+/* Rotary position embedding: channels are turned in pairs by the angles of the token's position,
+ * (a, b) -> (a cos - b sin, b cos + a sin), in binary32, each product rounded by itself. */
+typedef struct {
+  const float* table; /* device [rows, dim], 16-byte aligned: per position dim / 2 cosines, then dim / 2 sines           */
+  int32_t rows;       /* positions 0 .. rows - 1                                                                        */
+  int32_t dim;        /* channels that are turned, the first ones of a head: a multiple of 16, <= head_dim              */
+  int32_t paired;     /* 1: angle i turns channels 2i and 2i + 1;  0: channels i and i + dim / 2                        */
+} wkv_rope;
+
+/* Appends new entries, turned to their position on the way, and turns the queries that go with them; no attention.  Asynchronous.
+ * What follows is a wkv_paged_decode or wkv_paged_prefill with k and v NULL.
+ *   q [total_q, n_q_heads, head_dim], k, v [total_q, n_kv_heads, head_dim]: rows q_stride, kv_stride elements apart (0: packed),
+ *        16-byte aligned;  q NULL: no queries;  k and v NULL: only the queries
+ *   q_start device [batch + 1] int32: sequence b's tokens are rows q_start[b] .. q_start[b+1]-1 and become its last entries;
+ *        NULL: one token per sequence, row b, total_q = batch.  seq_lens counts the new entries; 0 = padding
+ *   rope NULL: nothing is turned.  positions device [total_q] int32, NULL: a token's position is its entry's index.  A position
+ *        outside of the table leaves the row as it is, and wkv_paged_status reports WKV_ERR_STATE
+ *   q_out [total_q, n_q_heads, head_dim], rows q_out_stride elements apart (0: packed); may be q itself (same stride), and must
+ *        not overlap the call's other arguments otherwise.  Rows of no sequence are left as they were
+ *   page_bounds device [n_layers, n_pages, n_kv_heads, 2, head_dim] int8 and page_scale [n_layers, n_pages, n_kv_heads], or both
+ *        NULL: of every page that gets an entry the bounds of its keys, as stored, up to the sequence's length: page_scale =
+ *        (largest magnitude) * (1/127), and per channel the largest key / page_scale rounded up and the least rounded down.  A page
+ *        that another sequence shares must hold the same entries for both. */
+int wkv_paged_append(wkv_paged* c, int32_t layer, int32_t batch, const void* q, int64_t q_stride, const void* k, const void* v,
+                     int64_t kv_stride, const int32_t* q_start, int32_t total_q, const int32_t* block_table, int32_t table_width,
+                     const int32_t* seq_lens, const wkv_rope* rope, const int32_t* positions, void* q_out, int64_t q_out_stride,
+                     int8_t* page_bounds, float* page_scale);
+
+/* Chooses the pages that a decode step's query attends to, for every (sequence, kv head) by itself: the first `sink` and the newest
+ * `recent` pages, then those with the best scores, of equal scores the lowest page.  Asynchronous.  A page's score is page_scale
+ * times the whole number sum over channels of (u hi + w lo), with hi, lo the page's bounds and u, w the sums over the kv head's
+ * query heads of max(q, 0) and min(q, 0), both in steps of 1/127 of their largest channel: up to rounding, and a factor per query,
+ * a bound on the sum over the heads of q.k.
+ *   q as in wkv_paged_decode;  page_bounds, page_scale as wkv_paged_append keeps them
+ *   n_select in [1, 2^20]; recent >= 1, recent + sink <= n_select
+ *   page_scores [batch, n_kv_heads, page_score_stride] fp32 out: the score of every page (page_score_stride >= table_width);
+ *        behind a sequence's last page left as it was
+ *   pages [batch, n_kv_heads, n_select] int32 out: indexes into the sequence's table row, rising; -1 behind the last */
+int wkv_paged_select(wkv_paged* c, int32_t layer, int32_t batch, const void* q, int64_t q_stride, const int32_t* block_table,
+                     int32_t table_width, const int32_t* seq_lens, const int8_t* page_bounds, const float* page_scale, int32_t n_select,
+                     int32_t recent, int32_t sink, float* page_scores, int64_t page_score_stride, int32_t* pages);
+
+/* Attention of one token per sequence to the entries of chosen pages, each kv head its own.  Stores nothing.  Asynchronous.
+ *   pages [batch, n_kv_heads, n_select] int32: indexes into the sequence's table row; of a list as many places are read as the
+ *        sequence has pages.  Numbers outside of the sequence count as none; one that stands twice counts twice
+ *   q, block_table, seq_lens, out and lse as in wkv_paged_decode */
+int wkv_paged_decode_pages(wkv_paged* c, int32_t layer, int32_t batch, const void* q, int64_t q_stride, const int32_t* block_table,
+                           int32_t table_width, const int32_t* seq_lens, const int32_t* pages, int32_t n_select, void* out, float* lse);
+
+/* Spreads rows in 4 bits out to the bf16 pages of another handle on the same device (same n_kv_heads and head_dim; the page size
+ * may differ), where prompts can attend to them.  Runs on c's stream; the caller orders dst's.  Asynchronous.
+ *   block_table, seq_lens as in wkv_paged_decode;  dst_table device [batch, dst_width] int32, pages for every sequence's length (entries
+ *        that it has no page for are stored nowhere, and c's wkv_paged_status reports WKV_ERR_STATE)
+ * Rows behind a sequence's length are left as they were. */
+int wkv_paged_expand(wkv_paged* c, int32_t layer, int32_t batch, const int32_t* block_table, int32_t table_width, const int32_t* seq_lens,
+                     wkv_paged* dst, int32_t dst_layer, const int32_t* dst_table, int32_t dst_width);
 
 /* As their namesakes without _paged.  A wait inside a kernel that gave up (WKV_ERR_TIMEOUT) ends its block's work; what the calls
  * since the last status wrote is then undefined, and the handle can be used again. */

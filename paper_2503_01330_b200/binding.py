@@ -13,7 +13,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libwkv.so")
 
-WKV_F32, WKV_BF16 = 0, 1
+WKV_F32, WKV_BF16, WKV_KV4 = 0, 1, 4
 WKV_SCHEDULE_AUTO, WKV_SCHEDULE_SPLIT, WKV_SCHEDULE_CLUSTER, WKV_SCHEDULE_FLAT = 0, 1, 2, 3
 WKV_OK, WKV_ERR_INVALID, WKV_ERR_ALLOC, WKV_ERR_CUDA, WKV_ERR_STATE, WKV_ERR_TIMEOUT = 0, -1, -2, -3, -4, -5
 
@@ -36,11 +36,16 @@ class wkv_paged_config(C.Structure):
                 ("user", C.c_void_p)]
 
 
+class wkv_rope(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("rows", C.c_int32), ("dim", C.c_int32), ("paired", C.c_int32)]
+
+
 EXPORTS = ["wkv_config_error", "wkv_create", "wkv_destroy", "wkv_reset", "wkv_set_stream", "wkv_decode_step",
            "wkv_decode_step_layers", "wkv_decode_step_static", "wkv_decode_step_host", "wkv_decode_step_layers_host", "wkv_prefill", "wkv_prefill_bulk", "wkv_prefill_bulk_layers", "wkv_export_state", "wkv_export_slots", "wkv_import_state",
            "wkv_status", "wkv_selftest_wait_timeout", "wkv_launch_count", "wkv_device_bytes", "wkv_splits", "wkv_strerror", "wkv_last_error",
            "wkv_paged_config_error", "wkv_paged_create", "wkv_paged_destroy", "wkv_paged_set_stream", "wkv_paged_pools",
-           "wkv_paged_decode", "wkv_paged_prefill", "wkv_paged_evict", "wkv_paged_status", "wkv_paged_selftest_wait_timeout",
+           "wkv_paged_decode", "wkv_paged_prefill", "wkv_paged_evict", "wkv_paged_append", "wkv_paged_select",
+           "wkv_paged_decode_pages", "wkv_paged_expand", "wkv_paged_status", "wkv_paged_selftest_wait_timeout",
            "wkv_paged_launch_count", "wkv_paged_device_bytes", "wkv_paged_last_error"]
 
 _lib = None
@@ -95,6 +100,10 @@ def lib():
         L.wkv_paged_decode.argtypes = [vp, i32, i32, vp, i64, vp, vp, i64, vp, i32, vp, i32, i32, vp, i64, vp, vp]
         L.wkv_paged_prefill.argtypes = [vp, i32, i32, vp, i64, vp, vp, i64, vp, i32, vp, i32, vp, i32, i32, vp, i64, vp, vp]
         L.wkv_paged_evict.argtypes = [vp, i32, i32, vp, i32, vp, i32, vp, vp, i32, i32, i32, vp, i64, vp, i64, vp]
+        L.wkv_paged_append.argtypes = [vp, i32, i32, vp, i64, vp, vp, i64, vp, i32, vp, i32, vp, vp, vp, vp, i64, vp, vp]
+        L.wkv_paged_select.argtypes = [vp, i32, i32, vp, i64, vp, i32, vp, vp, vp, i32, i32, i32, vp, i64, vp]
+        L.wkv_paged_decode_pages.argtypes = [vp, i32, i32, vp, i64, vp, i32, vp, vp, i32, vp, vp]
+        L.wkv_paged_expand.argtypes = [vp, i32, i32, vp, i32, vp, vp, i32, vp, i32]
         L.wkv_paged_status.argtypes = [vp]
         L.wkv_paged_selftest_wait_timeout.argtypes = [vp]
         L.wkv_paged_launch_count.restype = i64
@@ -297,15 +306,17 @@ class PagedCache:
     """One wkv_paged: a key/value cache in pages and the attention over it.
 
     `k_pool`, `v_pool` [n_layers, n_pages, n_kv_heads, page_size, head_dim] are the caller's tensors where given, else made
-    here (zeros).  The handle runs on the stream that is current when it is made (wkv_set_stream changes that); the caller
+    here (zeros); with WKV_KV4 they are uint8 [n_layers, n_pages, n_kv_heads, page_size * (head_dim / 2 + head_dim / 16)].  The handle runs on the stream that is current when it is made (wkv_set_stream changes that); the caller
     orders other streams' work, as for Context."""
 
     def __init__(self, n_layers, n_pages, page_size, n_q_heads, n_kv_heads, head_dim, max_batch, max_pages, dtype=WKV_BF16,
                  scale=0.0, scores=False, device="cuda:0", k_pool=None, v_pool=None):
         self.device = torch.device(device)
         self.dtype = dtype
-        self.tdtype = torch.bfloat16 if dtype == WKV_BF16 else torch.float32
-        self.shape = (n_layers, n_pages, n_kv_heads, page_size, head_dim)
+        self.tdtype = torch.float32 if dtype == WKV_F32 else torch.bfloat16
+        four = dtype == WKV_KV4
+        self.shape = (n_layers, n_pages, n_kv_heads, *((page_size * (head_dim // 2 + head_dim // 16),) if four else (page_size, head_dim)))
+        pool_dtype = torch.uint8 if four else self.tdtype
         self.n_q_heads, self.n_kv_heads, self.head_dim, self.page_size = n_q_heads, n_kv_heads, head_dim, page_size
         self._bufs = {}
         cfg = make_paged_config(n_layers, n_pages, page_size, n_q_heads, n_kv_heads, head_dim, max_batch, max_pages, dtype,
@@ -318,11 +329,11 @@ class PagedCache:
         self._index = self.device.index
         with torch.cuda.device(self.device):
             if k_pool is None:
-                k_pool = torch.zeros(self.shape, dtype=self.tdtype, device=self.device)
-                v_pool = torch.zeros(self.shape, dtype=self.tdtype, device=self.device)
+                k_pool = torch.zeros(self.shape, dtype=pool_dtype, device=self.device)
+                v_pool = torch.zeros(self.shape, dtype=pool_dtype, device=self.device)
             for name, p in (("k_pool", k_pool), ("v_pool", v_pool)):
-                _need(tuple(p.shape) == self.shape and p.dtype == self.tdtype and p.device == self.device and p.is_contiguous(),
-                      f"{name} must be a contiguous {self.tdtype} tensor {self.shape} on {self.device}")
+                _need(tuple(p.shape) == self.shape and p.dtype == pool_dtype and p.device == self.device and p.is_contiguous(),
+                      f"{name} must be a contiguous {pool_dtype} tensor {self.shape} on {self.device}")
             self.k_pool, self.v_pool = k_pool, v_pool
             cfg.k_pool, cfg.v_pool = k_pool.data_ptr(), v_pool.data_ptr()
             cfg.stream = torch.cuda.current_stream(self.device).cuda_stream
@@ -447,6 +458,65 @@ class PagedCache:
             self._packed("dst_table", dst_table, torch.int32, B, -1), dst_table.shape[1],
             self._packed("seq_lens", seq_lens, torch.int32, B), self._packed("new_lens", new_lens, torch.int32, B), budget,
             recent, sink, sp, ss, op, os_, self._packed("kept", kept, torch.int32, B, self.n_kv_heads, budget)))
+
+    def wkv_paged_append(self, layer, q, k, v, block_table, seq_lens, q_start=None, rope=None, paired=False, positions=None, q_out=None,
+                         page_bounds=None, page_scale=None):
+        """q [T, Hq, d] or None, k, v [T, Hkv, d] or None; q_start [B + 1] int32, or None: row b is sequence b's only token.
+        rope [rows, dim] float32: cosines, then sines, of every position's angles; q_out [T, Hq, d], q itself included;
+        page_bounds [layers, pages, Hkv, 2, d] int8 and page_scale [layers, pages, Hkv] float32 are kept up to date."""
+        _need(q is not None or k is not None, "q or k and v must be given")
+        _need((q is None) == (q_out is None), "q and q_out must both be given or both be None")
+        B, T = block_table.shape[0], (k if q is None else q).shape[0]
+        qp, qs = self._rows("q", q, T, self.n_q_heads) if q is not None else (None, 0)
+        op, os_ = self._rows("q_out", q_out, T, self.n_q_heads) if q is not None else (None, 0)
+        kp, vp, ks = self._new_rows(k, v, T)
+        turn = None
+        if rope is not None:
+            if rope.dim() != 2:
+                raise WkvError(WKV_ERR_INVALID, "rope must be [rows, dim]")
+            turn = wkv_rope(self._packed("rope", rope, torch.float32, rope.shape[0], -1), rope.shape[0], rope.shape[1], int(paired))
+            turn = C.byref(turn)
+        _need((page_bounds is None) == (page_scale is None), "page_bounds and page_scale must both be given or both be None")
+        self._check(self._lib.wkv_paged_append(
+            self._h, layer, B, qp, qs, kp, vp, ks, self._packed("q_start", q_start, torch.int32, B + 1), T,
+            self._packed("block_table", block_table, torch.int32, B, -1), block_table.shape[1],
+            self._packed("seq_lens", seq_lens, torch.int32, B), turn, self._packed("positions", positions, torch.int32, T), op, os_,
+            *self._bounds(page_bounds, page_scale)))
+
+    def _bounds(self, page_bounds, page_scale):
+        layers, pages, heads = self.shape[:3]
+        return (self._packed("page_bounds", page_bounds, torch.int8, layers, pages, heads, 2, self.head_dim),
+                self._packed("page_scale", page_scale, torch.float32, layers, pages, heads))
+
+    def wkv_paged_select(self, layer, q, block_table, seq_lens, page_bounds, page_scale, page_scores, pages, recent=1, sink=0):
+        """q [B, Hq, d]; page_scores [B, Hkv, >= width] float32 and pages [B, Hkv, n_select] int32 are written: every page's score, and the
+        chosen ones' places in the table row, rising, -1 behind the last."""
+        B = q.shape[0]
+        qp, qs = self._rows("q", q, B, self.n_q_heads)
+        bp, sp = self._bounds(page_bounds, page_scale)
+        self._check(self._lib.wkv_paged_select(
+            self._h, layer, B, qp, qs, self._packed("block_table", block_table, torch.int32, B, -1), block_table.shape[1],
+            self._packed("seq_lens", seq_lens, torch.int32, B), bp, sp, pages.shape[-1], recent, sink,
+            *self._scores("page_scores", page_scores, B), self._packed("pages", pages, torch.int32, B, self.n_kv_heads, -1)))
+
+    def wkv_paged_decode_pages(self, layer, q, block_table, seq_lens, pages, out, lse=None):
+        """q [B, Hq, d] attends to the entries of the pages [B, Hkv, n_select], places in the table row (-1: none)."""
+        B = q.shape[0]
+        qp, qs = self._rows("q", q, B, self.n_q_heads)
+        self._check(self._lib.wkv_paged_decode_pages(
+            self._h, layer, B, qp, qs, self._packed("block_table", block_table, torch.int32, B, -1), block_table.shape[1],
+            self._packed("seq_lens", seq_lens, torch.int32, B), self._packed("pages", pages, torch.int32, B, self.n_kv_heads, -1),
+            pages.shape[-1], self._packed("out", out, self.tdtype, B, self.n_q_heads, self.head_dim),
+            self._packed("lse", lse, torch.float32, B, self.n_q_heads)))
+
+    def wkv_paged_expand(self, layer, block_table, seq_lens, dst, dst_layer, dst_table):
+        """Rows in 4 bits to the pages `dst_table` [B, width] of `dst`, a PagedCache with bf16 rows."""
+        B = block_table.shape[0]
+        _need(isinstance(dst, PagedCache), "dst must be a PagedCache")
+        self._check(self._lib.wkv_paged_expand(
+            self._h, layer, B, self._packed("block_table", block_table, torch.int32, B, -1), block_table.shape[1],
+            self._packed("seq_lens", seq_lens, torch.int32, B), dst._h, dst_layer,
+            self._packed("dst_table", dst_table, torch.int32, B, -1), dst_table.shape[1]))
 
     def wkv_status(self):
         return lib().wkv_paged_status(self._h)

@@ -10,11 +10,15 @@ CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libwkv.so")
 OBJ_DIR = os.path.join(_HERE, "_build")
 HEADER = os.path.join("..", "..", "include", "wkv.h")
+PAGED = ["wkv_ptx.cuh", "wkv_paged.cuh", "wkv_paged_host.cuh", HEADER]
 # source -> what it includes; each is compiled to an object of its own, rebuilt when one of them is newer
 UNITS = {
     "wkv_api.cu": ["wkv_ptx.cuh", "wkv_kernels.cuh", "wkv_prefill.cuh", "wkv_block.cuh", HEADER],
-    "wkv_paged_api.cu": ["wkv_ptx.cuh", "wkv_paged.cuh", "wkv_paged_decode.cuh",
-                         "wkv_paged_prefill.cuh", "wkv_paged_f32.cuh", "wkv_tcgen05.cuh", HEADER],
+    "wkv_paged_api.cu": [*PAGED, "wkv_paged_decode.cuh", "wkv_paged_evict.cuh", "wkv_paged_prefill.cuh", "wkv_paged_f32.cuh",
+                         "wkv_tcgen05.cuh"],
+    "wkv_paged_rows.cu": [*PAGED, "wkv_paged_kv4.cuh", "wkv_paged_rows.cuh"],
+    "wkv_paged_kv4.cu": [*PAGED, "wkv_paged_kv4.cuh", "wkv_paged_decode.cuh", "wkv_paged_decode_kv4.cuh"],
+    "wkv_paged_pages.cu": [*PAGED, "wkv_paged_choose.cuh", "wkv_paged_decode.cuh"],
 }
 SOURCES = list(UNITS)
 DEPS = sorted(set(SOURCES) | {d for deps in UNITS.values() for d in deps})

@@ -1,84 +1,20 @@
 // Host side of the paged cache declared in include/wkv.h: configuration checks, workspaces, launches.
 #include <algorithm>
-#include <cmath>
 #include <cstdint>
 #include <cstring>
 #include <new>
 #include <string>
-#include <vector>
 
 #include <cuda.h>                      // tensor-map types only; the driver entry point is looked up at run time
 
-#include "../../include/wkv.h"
-#include "wkv_paged.cuh"
+#include "wkv_paged_host.cuh"
 #include "wkv_paged_decode.cuh"
+#include "wkv_paged_evict.cuh"
 #include "wkv_paged_prefill.cuh"
 #include "wkv_paged_f32.cuh"
 
-struct wkv_paged {
-  wkv_paged_config cfg;
-  int device = 0;
-  int sm_count = 148;
-  int group = 1;
-  int page_shift = 4;
-  float scale = 0.f;
-  size_t elem = 2;
-  cudaStream_t stream = nullptr;
-  void* k_pool = nullptr;
-  void* v_pool = nullptr;
-  uint32_t* status = nullptr;
-  float* logits = nullptr;             // [max_batch][Hq][max_pages * page_size]: a decode step's; kept indexes of an eviction
-  float2* head_ml = nullptr;           // [max_batch][Hq]: a decode step's (max, 1 / sum), for the weights
-  // decode: partials of the pieces, arrivals per lane
-  const void* decode_kernel = nullptr;
-  const void* fold_kernel = nullptr;
-  int decode_ctas = 0, decode_smem = 0;
-  float* part = nullptr;
-  float2* part_ml = nullptr;
-  uint32_t* arrived = nullptr;
-  // prompts: the runs' outputs, next item
-  float4* run_part = nullptr;
-  float2* run_ml = nullptr;
-  uint32_t* item_counter = nullptr;
-  // the pools as [chunk][part][row][128 bytes], boxes of a page's rows (at most a decode tile's) x all parts
-  alignas(64) unsigned char page_kmap[128] = {};
-  alignas(64) unsigned char page_vmap[128] = {};
-  // ... in boxes of one part, for prompts on bf16 rows
-  alignas(64) unsigned char part_kmap[128] = {};
-  alignas(64) unsigned char part_vmap[128] = {};
-  void* encode = nullptr;              // the driver's cuTensorMapEncodeTiled
-  int32_t* n_moved = nullptr;          // [max_batch][Hkv]
-  std::vector<void*> owned;
-  long long device_bytes = 0;
-  long long launches = 0;
-  std::string last_error;
-};
-
 namespace {
-
-int fail(wkv_paged* c, int code, const std::string& msg) {
-  if (c) c->last_error = msg;
-  return code;
-}
-int cuda_fail(wkv_paged* c, cudaError_t e, const char* what) {
-  return fail(c, WKV_ERR_CUDA, std::string(what) + ": " + cudaGetErrorString(e));
-}
-#define WKV_CUDA(ctx, expr)                                   \
-  do {                                                        \
-    cudaError_t e_ = (expr);                                  \
-    if (e_ != cudaSuccess) return cuda_fail(ctx, e_, #expr);  \
-  } while (0)
-
-// Calls may come with another device current than the handle's.
-struct DeviceGuard {
-  int was = -1;
-  cudaError_t err;
-  explicit DeviceGuard(int device) {
-    err = cudaGetDevice(&was);
-    if (err == cudaSuccess && was != device) err = cudaSetDevice(device); else was = -1;
-  }
-  ~DeviceGuard() { if (was >= 0) cudaSetDevice(was); }
-};
+using namespace wkv::host;
 
 void* default_alloc(size_t bytes, void*) {
   void* p = nullptr;
@@ -110,9 +46,10 @@ const char* check_config(const wkv_paged_config* c) {
   if (c->max_batch < 1 || c->max_batch > 1024) return "max_batch must be in [1, 1024]";
   if (c->max_pages < 1 || (long long)c->max_pages * c->page_size > (1 << 24)) return "max_pages must be >= 1 and max_pages * page_size at most 2^24";
   if ((long long)c->n_layers * c->n_pages >= 0x7fffffffLL / c->n_kv_heads) return "n_layers * n_pages * n_kv_heads must stay below 2^31";
-  if (c->dtype != WKV_F32 && c->dtype != WKV_BF16) return "dtype must be WKV_F32 or WKV_BF16";
+  if (c->dtype != WKV_F32 && c->dtype != WKV_BF16 && c->dtype != WKV_KV4) return "dtype must be WKV_F32, WKV_BF16 or WKV_KV4";
   if (!(c->scale >= 0.f) || std::isinf(c->scale)) return "scale must be finite and >= 0";
   if (c->scores != 0 && c->scores != 1) return "scores must be 0 or 1";
+  if (c->scores && c->dtype == WKV_KV4) return "scores must be 0 with rows in 4 bits";
   if ((c->k_pool == nullptr) != (c->v_pool == nullptr)) return "k_pool and v_pool must both be set or both be NULL";
   if (((uintptr_t)c->k_pool | (uintptr_t)c->v_pool) & 15) return "k_pool and v_pool must be 16-byte aligned";
   if ((c->alloc == nullptr) != (c->release == nullptr)) return "alloc and release must both be set or both be NULL";
@@ -197,67 +134,12 @@ cudaError_t pick_by_group(wkv_paged* c) {
   }
 }
 
-bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
-
-// Arguments that decode and prefill share; fills P.  `rows`: rows of q.
-int attention_params(wkv_paged* c, wkv::PagedParams& P, int32_t layer, int32_t batch, int32_t rows, const void* q, int64_t q_stride,
-                     const void* k, const void* v, int64_t kv_stride, const int32_t* table, int32_t width, const int32_t* seq_lens,
-                     int32_t window, int32_t sink, float* scores, int64_t score_stride, void* out, float* lse) {
-  const wkv_paged_config& f = c->cfg;
-  if (layer < 0 || layer >= f.n_layers) return fail(c, WKV_ERR_INVALID, "layer out of range");
-  if (batch < 0 || batch > f.max_batch) return fail(c, WKV_ERR_INVALID, "batch must be in [0, max_batch]");
-  if (rows < 0) return fail(c, WKV_ERR_INVALID, "the number of rows must be >= 0");
-  if (width < 1 || width > f.max_pages) return fail(c, WKV_ERR_INVALID, "table_width must be in [1, max_pages]");
-  if (window < 0 || sink < 0) return fail(c, WKV_ERR_INVALID, "window and sink must be >= 0");
-  if ((k == nullptr) != (v == nullptr)) return fail(c, WKV_ERR_INVALID, "k and v must both be given or both be NULL");
-  if (batch > 0 && rows > 0 && (!q || !table || !seq_lens || !out)) return fail(c, WKV_ERR_INVALID, "q, block_table, seq_lens and out must not be NULL");
-  const int64_t q_row = (int64_t)f.n_q_heads * f.head_dim, kv_row = (int64_t)f.n_kv_heads * f.head_dim;
-  if (q_stride == 0) q_stride = q_row;
-  if (kv_stride == 0) kv_stride = kv_row;
-  if (q_stride < q_row || kv_stride < kv_row) return fail(c, WKV_ERR_INVALID, "a row stride is smaller than the row");
-  if (q_stride * (int64_t)c->elem % 16 || kv_stride * (int64_t)c->elem % 16 || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out))
-    return fail(c, WKV_ERR_INVALID, "rows of q, k, v and out must be 16-byte aligned");
-  if (scores) {
-    if (!f.scores) return fail(c, WKV_ERR_INVALID, "scores need a handle created with scores = 1");
-    if (score_stride < (int64_t)width * f.page_size) return fail(c, WKV_ERR_INVALID, "score_stride must be >= table_width * page_size");
-  }
-  std::memset(&P, 0, sizeof(P));
-  const size_t layer_bytes = (size_t)f.n_pages * f.n_kv_heads * f.page_size * f.head_dim * c->elem;
-  P.k_pool = (char*)c->k_pool + layer * layer_bytes;
-  P.v_pool = (char*)c->v_pool + layer * layer_bytes;
-  P.q = q; P.k = k; P.v = v; P.q_stride = q_stride; P.kv_stride = kv_stride;
-  P.table = table; P.seq_lens = seq_lens; P.out = out; P.lse = lse; P.scores = scores; P.score_stride = score_stride;
-  P.status = c->status; P.batch = batch; P.rows = rows; P.width = width; P.n_pages = f.n_pages;
-  P.n_q_heads = f.n_q_heads; P.n_kv_heads = f.n_kv_heads; P.page = f.page_size; P.page_shift = c->page_shift;
-  P.window = window; P.sink = sink; P.scale_log2 = c->scale * wkv::kLog2e;
-  return WKV_OK;
-}
-
-// All launches: programmatic stream serialization, each kernel waits for its predecessor first thing.
-template <typename... A, typename... B>
-cudaError_t launch(wkv_paged* c, void (*kernel)(A...), long long grid, int threads, size_t smem, B&&... args) {
-  if (grid < 1 || grid > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
-  cudaLaunchConfig_t lc = {};
-  lc.gridDim = dim3((unsigned)grid);
-  lc.blockDim = dim3((unsigned)threads);
-  lc.dynamicSmemBytes = smem;
-  lc.stream = c->stream;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  lc.attrs = at;
-  lc.numAttrs = 1;
-  c->launches++;
-  return cudaLaunchKernelEx(&lc, kernel, std::forward<B>(args)...);
-}
-
-// The layer's first chunk.
-int chunk0(const wkv_paged* c, const wkv::PagedParams& P) {
-  return (int)(((char*)P.k_pool - (char*)c->k_pool) / ((size_t)P.page * c->cfg.head_dim * c->elem));
-}
-
 int decode(wkv_paged* c, const wkv::PagedParams& A) {
   if (A.batch == 0) return WKV_OK;
+  if (c->cfg.dtype == WKV_KV4) {
+    const int rc = A.k ? append_rows(c, A) : WKV_OK;
+    return rc != WKV_OK ? rc : decode_kv4(c, A, nullptr, 0);
+  }
   wkv::DecodeParams P;
   std::memset(&P, 0, sizeof(P));
   P.A = A;
@@ -368,17 +250,21 @@ int wkv_paged_create(const wkv_paged_config* cfg, wkv_paged** out) {
   c->group = cfg->n_q_heads / cfg->n_kv_heads;
   c->page_shift = cfg->page_size == 16 ? 4 : cfg->page_size == 32 ? 5 : 6;
   c->scale = cfg->scale != 0.f ? cfg->scale : (float)(1.0 / std::sqrt((double)cfg->head_dim));
-  c->elem = cfg->dtype == WKV_BF16 ? 2 : 4;
+  const bool four = cfg->dtype == WKV_KV4;
+  c->elem = cfg->dtype == WKV_F32 ? 4 : 2;
+  c->chunk_bytes = (size_t)cfg->page_size * (four ? cfg->head_dim / 2 + cfg->head_dim / 16 : cfg->head_dim * c->elem);
   c->stream = reinterpret_cast<cudaStream_t>(cfg->stream);
   c->k_pool = cfg->k_pool;
   c->v_pool = cfg->v_pool;
-  const size_t pool = (size_t)cfg->n_layers * cfg->n_pages * cfg->n_kv_heads * cfg->page_size * cfg->head_dim * c->elem;
+  const size_t pool = (size_t)cfg->n_layers * cfg->n_pages * cfg->n_kv_heads * c->chunk_bytes;
   const size_t lanes = (size_t)cfg->max_batch * cfg->n_kv_heads, heads = (size_t)cfg->max_batch * cfg->n_q_heads;
   const bool wide = cfg->head_dim == 128;
   e = cudaFuncSetAttribute(wkv::paged_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, wkv::kSelectStaged * 4);
   if (e != cudaSuccess) { delete c; return WKV_ERR_CUDA; }
-  if (cfg->dtype == WKV_BF16) e = wide ? pick_by_group<__nv_bfloat16, 128>(c) : pick_by_group<__nv_bfloat16, 64>(c);
+  if (four) e = pick_kv4(c);
+  else if (cfg->dtype == WKV_BF16) e = wide ? pick_by_group<__nv_bfloat16, 128>(c) : pick_by_group<__nv_bfloat16, 64>(c);
   else e = wide ? pick_by_group<float, 128>(c) : pick_by_group<float, 64>(c);
+  if (e == cudaSuccess && !four) e = pick_pages(c);
   if (e != cudaSuccess) { delete c; return WKV_ERR_CUDA; }
   int rc = WKV_OK;
 #define WKV_TAKE(dst, bytes) do { if (rc == WKV_OK) rc = take(c, dst, bytes); } while (0)
@@ -391,8 +277,10 @@ int wkv_paged_create(const wkv_paged_config* cfg, wkv_paged** out) {
   WKV_TAKE(&c->part, ((size_t)c->decode_ctas + lanes) * c->group * cfg->head_dim * 4);
   WKV_TAKE(&c->part_ml, ((size_t)c->decode_ctas + lanes) * c->group * 8);
   WKV_TAKE(&c->arrived, lanes * 4);
-  WKV_TAKE(&c->run_part, run_rows(c) * cfg->head_dim * 4);
-  WKV_TAKE(&c->run_ml, run_rows(c) * 8);
+  if (!four) {
+    WKV_TAKE(&c->run_part, run_rows(c) * cfg->head_dim * 4);
+    WKV_TAKE(&c->run_ml, run_rows(c) * 8);
+  }
   WKV_TAKE(&c->item_counter, 12);
   const bool own_pools = !c->k_pool;
   if (own_pools) {
@@ -408,7 +296,7 @@ int wkv_paged_create(const wkv_paged_config* cfg, wkv_paged** out) {
     if (e == cudaSuccess && own_pools) e = cudaMemsetAsync(c->v_pool, 0, pool, c->stream);
     if (e != cudaSuccess) rc = WKV_ERR_CUDA;
   }
-  {
+  if (!four) {
     const int rows = cfg->dtype == WKV_BF16 ? cfg->page_size : std::min(cfg->page_size, 32), parts = (int)(cfg->head_dim * c->elem / 128);
     if (rc == WKV_OK) rc = encode_pool(c, c->page_kmap, c->k_pool, rows, parts);
     if (rc == WKV_OK) rc = encode_pool(c, c->page_vmap, c->v_pool, rows, parts);
@@ -460,6 +348,7 @@ int wkv_paged_prefill(wkv_paged* c, int32_t layer, int32_t batch, const void* q,
                       int32_t table_width, const int32_t* seq_lens, int32_t window, int32_t sink, float* scores,
                       int64_t score_stride, void* out, float* lse) {
   if (!c) return WKV_ERR_INVALID;
+  if (c->cfg.dtype == WKV_KV4) return fail(c, WKV_ERR_INVALID, "prompts attend to bf16 or fp32 rows: see wkv_paged_expand");
   DeviceGuard on(c->device);
   WKV_CUDA(c, on.err);
   wkv::PagedParams P;
@@ -495,7 +384,7 @@ int wkv_paged_evict(wkv_paged* c, int32_t layer, int32_t batch, const int32_t* s
   if (scores_out == scores || (const int32_t*)new_lens == seq_lens) return fail(c, WKV_ERR_INVALID, "scores_out and new_lens must not be the arrays that the call reads");
   wkv::EvictParams P;
   std::memset(&P, 0, sizeof(P));
-  const size_t layer_bytes = (size_t)f.n_pages * f.n_kv_heads * f.page_size * f.head_dim * c->elem;
+  const size_t layer_bytes = (size_t)f.n_pages * f.n_kv_heads * c->chunk_bytes;
   P.k_pool = (char*)c->k_pool + layer * layer_bytes;
   P.v_pool = (char*)c->v_pool + layer * layer_bytes;
   P.src_table = src_table; P.dst_table = dst_table; P.seq_lens = seq_lens; P.new_lens = new_lens;

@@ -37,6 +37,8 @@ struct DecodeParams {
   int fold_inside;           // the CTA that completes a lane folds its weights, no second kernel
   int oob_chunk;             // a chunk number outside the pool
   int chunk0;                // the layer's first chunk
+  const int32_t* pages;      // [lanes][n_select] chosen pages of the sequence, -1: none (the kernel over chosen pages)
+  int n_select;
   alignas(64) unsigned char kmap[128];   // pool as [chunk][part][row][128 bytes], boxes of one page (or tile) x all parts
   alignas(64) unsigned char vmap[128];
 };
@@ -86,6 +88,17 @@ __device__ __forceinline__ DecodeSpan decode_span(int len, int window, int sink)
   s.first_tile = s.lo / TILE;
   s.sink_tiles = min((s.sinks + TILE - 1) / TILE, s.first_tile);
   s.tiles = max(1, s.sink_tiles + (len + TILE - 1) / TILE - s.first_tile);   // a padded row's one tile is empty: it writes zeros
+  return s;
+}
+
+// ... of chosen pages: the list's pages end to end, as many as the sequence can have.
+template <int TILE>
+__device__ __forceinline__ DecodeSpan chosen_span(const PagedParams& A, int len, int n_select) {
+  DecodeSpan s;
+  s.len = len;
+  s.lo = s.sinks = s.sink_tiles = s.first_tile = 0;
+  const int n = min(n_select, (len + A.page - 1) >> A.page_shift);
+  s.tiles = max(1, (int)((((long long)n << A.page_shift) + TILE - 1) / TILE));
   return s;
 }
 
@@ -356,7 +369,8 @@ __device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, 128
 template <typename T, int D, int G>
 constexpr int decode_smem() { return DecodeShape<T, D>::template smem<G>() + kDecodeWarps * DecodeWarp<T, D, G>::kScratch * 4; }
 
-template <typename T, int D, int G>
+// CHOSEN: over the pages of a list per lane instead of all of a sequence's; brings no entries and parks no logits.
+template <typename T, int D, int G, bool CHOSEN = false>
 __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const __grid_constant__ DecodeParams P) {
   using Sh = DecodeShape<T, D>;
   using Warp = DecodeWarp<T, D, G>;
@@ -374,6 +388,12 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
   float* scratch = reinterpret_cast<float*>(sm_last + 4);
 
   const PagedParams& A = P.A;
+  // CHOSEN: the first entry in each of a stage's boxes, the sequence's length where there is none
+  __shared__ int box_entry[CHOSEN ? STAGES : 1][4];
+  auto span = [&](int len) {
+    if constexpr (CHOSEN) return chosen_span<TILE>(A, len, P.n_select);
+    else return decode_span<TILE>(len, A.window, A.sink);
+  };
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     for (int i = 0; i < STAGES; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], kDecodeWarps); }
@@ -387,7 +407,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
     int run = 0, most = 0;
     for (int base = 0; base < A.batch; base += 32) {
       const int b = base + lane;
-      int n = b < A.batch ? decode_span<TILE>(lens[b], A.window, A.sink).tiles : 0;
+      int n = b < A.batch ? span(lens[b]).tiles : 0;
       int x = n;
 #pragma unroll
       for (int off = 1; off < 32; off <<= 1) {
@@ -425,7 +445,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
     }
     b = lo;
   }
-  DecodeSpan s = decode_span<TILE>(lens[b], A.window, A.sink);
+  DecodeSpan s = span(lens[b]);
   int head = (int)((t0 - (long long)cum[b] * H) / s.tiles), v = (int)((t0 - (long long)cum[b] * H) % s.tiles);
   const int pr = min(A.page, TILE), pr_shift = min(A.page_shift, TILE == 64 ? 6 : 5);
   const int boxes = TILE >> pr_shift;
@@ -442,7 +462,13 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
       const int st = it % STAGES;
       // box of this lane: boxes of K first, then of V
       const bool mine = lane < 2 * boxes;
-      const int box = lane & (boxes - 1), i = s.tile(v) * TILE + box * pr;
+      const int box = lane & (boxes - 1);
+      int i = s.tile(v) * TILE + box * pr;
+      if constexpr (CHOSEN) {
+        const int at = i >> A.page_shift, pages = (s.len + A.page - 1) >> A.page_shift;      // place in the list
+        const int pg = mine && at < min(P.n_select, pages) ? P.pages[((long long)b * H + head) * P.n_select + at] : -1;
+        i = (unsigned)pg < (unsigned)pages ? (pg << A.page_shift) + (i & (A.page - 1)) : s.len;
+      }
       // does the box hold a visible entry?  [i, i + pr) against [lo, len) and [0, sinks)
       int chunk_no = P.oob_chunk, row = 0;
       if (mine && i < s.len && (i + pr > s.lo || i < s.sinks)) {
@@ -451,6 +477,11 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
       }
       if (it >= STAGES && !wait(&empty[st], ((it / STAGES) & 1) ^ 1)) break;
       unsigned char* dst = ring + st * 2 * Sh::kTileBytes;
+      if constexpr (CHOSEN) {
+        if (lane < boxes) box_entry[st][lane] = i;
+        __threadfence_block();
+        __syncwarp();
+      }
       if (lane == 0) mbar_expect_tx(&full[st], 2 * Sh::kTileBytes);
       __syncwarp();
       if (mine)
@@ -460,7 +491,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
         v = 0;
         if (++head == H && t + 1 < t1) {
           head = 0;
-          s = decode_span<TILE>(lens[++b], A.window, A.sink);
+          s = span(lens[++b]);
         }
       }
     }
@@ -479,11 +510,11 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
     const int hq0 = head * G;
     w.begin(static_cast<const T*>(A.q) + (long long)b * A.q_stride + (long long)hq0 * D, scratch + warp * Warp::kScratch);
     const long long logit_stride = (long long)A.width << A.page_shift;
-    float* logits = P.logits ? P.logits + lane_no * G * logit_stride : nullptr;
+    float* logits = !CHOSEN && P.logits ? P.logits + lane_no * G * logit_stride : nullptr;
     // the call's own entry: the warp that owns it in the piece's last tile fetches its rows now, and stores them when it comes to
     // that tile
     constexpr int kPieces = Sh::kRowBytes / 16, kNew = 2 * kPieces / 32 > 0 ? 2 * kPieces / 32 : 1;
-    const bool brings = A.k && s.len > 0 && v + n == s.tiles && (s.len - 1) % TILE / Sh::kEach == warp;
+    const bool brings = !CHOSEN && A.k && s.len > 0 && v + n == s.tiles && (s.len - 1) % TILE / Sh::kEach == warp;
     uint4 news[kNew];
     int new_page = -1;
     if (brings) {
@@ -504,7 +535,8 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
       unsigned char* tv = tk + Sh::kTileBytes;
       ok = ok && wait(&full[st], (it / STAGES) & 1);
       if (!ok) continue;
-      const int row0 = warp * Sh::kEach, i0 = s.tile(v) * TILE + row0;
+      const int row0 = warp * Sh::kEach;
+      const int i0 = CHOSEN ? box_entry[CHOSEN ? st : 0][row0 >> pr_shift] + (row0 & (pr - 1)) : s.tile(v) * TILE + row0;
       // entries [i0, i0 + kEach) against the visible ones
       const bool any = i0 < s.len && (i0 + Sh::kEach > s.lo || i0 < s.sinks);
       if (any) {
@@ -625,7 +657,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
         if (A.lse) A.lse[at] = sm_l[tid] > 0.f ? (sm_m[tid] + log2f(sm_l[tid])) * kLn2 : -INFINITY;
         if (P.logits && !P.fold_inside) P.head_ml[at] = make_float2(sm_m[tid], sm_l[tid] > 0.f ? 1.f / sm_l[tid] : 0.f);
       }
-      if (P.fold_inside) {
+      if (!CHOSEN && P.fold_inside) {
         float2 ml[G];
 #pragma unroll
         for (int g = 0; g < G; ++g) ml[g] = make_float2(sm_m[g], sm_l[g] > 0.f ? 1.f / sm_l[g] : 0.f);
@@ -638,7 +670,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
       v = 0;
       if (++head == H && t < t1) {
         head = 0;
-        s = decode_span<TILE>(lens[++b], A.window, A.sink);
+        s = span(lens[++b]);
       }
     }
   }
