@@ -8,9 +8,11 @@ numpy binary32 and compared bit for bit.  The rest is compared with 64-bit arith
     2^-35 of the head's largest channel, which adds scale 2^-33 max|q| sum_c s (n_c + z);
   - bf16 rows: weights go as bf16 high and low parts, 2^-9 of 2^-9: 2^-17 A with room for one more rounding;
   - a weight: E = 2 |ds| + 2^-20 + (n + 8 + 2 T) u relative, as for bf16 rows;
-  - an output: (E + 2^-11) A for the weights and their rounding to fp16 (A = sum p s |n - z|: the same rounded weights multiply codes and
-    zero points), 2 (n + 16) u B for the sums (B = sum p s (n + z)), n 2^-28 s_max for weights below fp16's normal range, half a step
-    of bf16;
+  - an output: (E + 2 * 2^-11) A for the weights and the rounding of p and of p s to fp16, half a step each (A = sum p s |n - z|: the same
+    rounded weights multiply codes and zero points), 2 (n + 16) u B for the sums (B = sum p s (n + z)), half a step of bf16; and for
+    what is below fp16's normal range: p is held times 2^14 and s times a power of two that brings the largest, s_max, to [1, 2), so p s is
+    off by 2^-25 2^-14 s_max more per entry, and p s_max 2^-25 where s is below 2^-21 s_max (above that its four bits are exact): times
+    |n - z| <= 15, under (n + 128) 2^-28 s_max in all;
   - a prompt on bf16 rows rounds its weights to bf16: half a step, 2^-8, of each, so 2^-8 A more (round_p);
   - a log-sum: |ds| + (n + 8) u + 2^-20 + 2u |lse|."""
 import math
@@ -173,7 +175,7 @@ def attend(q, K, V, see, scale, half, Kabs=None, Vabs=None, s_max=0.0, round_p=0
     out = p @ V
     A = p @ np.abs(V)
     B = p @ Vabs if four else A
-    bound = (E + round_p + (2.0 ** -11 if four else 2.0 ** -17 if half > 2.0 ** -20 else 0.0)) * A + 2 * (n + 16) * U * B + (n * 2.0 ** -28 * s_max if four else 0.0)
+    bound = (E + round_p + (2.0 ** -10 if four else 2.0 ** -17 if half > 2.0 ** -20 else 0.0)) * A + 2 * (n + 16) * U * B + ((n + 128) * 2.0 ** -28 * s_max if four else 0.0)
     bound = bound * (1 + half) + half * np.abs(out) + 1e-37
     return out, z, bound, ds + (n + 8) * U + 2.0 ** -20 + 2 * U * abs(z)
 
