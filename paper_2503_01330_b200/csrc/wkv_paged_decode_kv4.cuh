@@ -3,13 +3,14 @@
 //   o = sum_i p_i v_i,  p = softmax(scale q.k_i),  k_i = s_ig (n - z_ig) per group g of 32 channels, v_i likewise
 //
 // Bound: HBM at 4.5 bits a number; instruction issue close behind it, since a number may cost no more than about three lane instructions.
-// Codes are never converted: a masked word is two fp16 subnormals n 2^-24 (or n 2^-20), which mma.sync m16n8k16 takes exactly.  Scales and
-// zero points stay outside of the products:
-//   q.k_i  = sum_g s_ig (q_g.n_ig - z_ig sum q_g)        groups' products in accumulators of their own
+// Codes are never converted: a masked word is two fp16 subnormals n 2^-24 (or n 2^-20), which mma.sync m16n8k16 takes exactly.  (As e4m3
+// numbers four codes come out of a mask, but the matrix instruction on them is split into fp16 ones with conversions: 196 -> 211 us.)
+// Scales and zero points stay outside of the products:
+//   q.k_i  = sum_g s_ig (q_g.n_ig - z_ig sum q_g)
 //   o_g    = sum_i (p_i s_ig) n_ig - sum_i (p_i s_ig) z_ig   the weights p s in fp16, the same rounded ones in both sums
 // p and p s are rounded to fp16, 2^-11 each, together a quarter of what rounding the output to bf16 costs.  The weights are kept in fp16's
-// range by a power of two that follows the largest value scale seen.  Queries become fp16 by a power of two per head (exact down to 2^-28 of the
-// head's largest channel).
+// range by a power of two that follows the largest value scale seen.  Queries become fp16 by a power of two per head (exact down to 2^-28 of
+// the head's largest channel).
 //
 // The deal of tiles to CTAs, pieces of a lane and their join are those of the bf16 rows' kernel.  A CTA: one producer warp, which looks up 32
 // pages at a time and copies their chunks into a ring (cp.async.bulk), and eight consumer warps, four for a tile of 128 entries.
@@ -30,11 +31,13 @@ struct Kv4Shape {
   using Row = Kv4Row<D>;
   static constexpr int kHalf = kKv4Tile * Row::kBytes;    // keys of a tile; values
   static constexpr int kStage = 2 * kHalf;
-  static constexpr int kStages = (G == 8 && D == 128 ? 54 : 72) * 1024 / kStage;
-  static constexpr int kOut = kKv4Warps * G * D * 4;      // the warps' outputs
-  static constexpr int kScratch = kKv4Warps * 32 * G * 4; // a warp's weights, then zero points' sums
+  static constexpr int kStages = 72 * 1024 / kStage;      // 4 or 8
+  static constexpr int kOuts = G == 8 ? kKv4Warps / 2 : kKv4Warps;      // outputs side by side in the join: the warps', or of pairs of them
+  static constexpr int kOut = kOuts * G * D * 4;
+  static constexpr int kScratch = kKv4Warps * 16 * G * 4; // a warp's weights, then zero points' sums
   static constexpr int kSmem = kStages * kStage + kOut + kScratch + 2 * kKv4Warps * 8 * 4 + (2 * kMaxSequences + 8) * 4 + 2 * kStages * 8 +
                                kStages * kKv4MaxSlots * 4 + 16;
+  static_assert((kStages & (kStages - 1)) == 0, "stages by masks");
 };
 
 __device__ __forceinline__ void mma_m16n8k16_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -48,59 +51,103 @@ __device__ __forceinline__ uint32_t half_pair(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
+// Shared memory by 32-bit address: a generic pointer would double the address arithmetic.
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t lds16(uint32_t a) {
+  uint16_t v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts16(uint32_t a, __half x) {
+  asm volatile("st.shared.u16 [%0], %1;" ::"r"(a), "h"(__half_as_ushort(x)) : "memory");
+}
 __device__ __forceinline__ uint32_t half_mul(uint32_t a, uint32_t b) {
   const __half2 x = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&x);
+}
+__device__ __forceinline__ uint32_t half_max(uint32_t a, uint32_t b) {
+  const __half2 x = __hmax2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
   return *reinterpret_cast<const uint32_t*>(&x);
 }
 __device__ __forceinline__ float2 half_pair_f(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2*>(&x)); }
 
 // A consumer warp's share of a piece: 32 entries of a tile at a time.  Lane 4 r + j.
 //
-// Keys: entries are rows of the product.  A lane's 16 channels of two, D / 4 in all, are the quarter j of an entry's channels.
-//   G <= 2: the columns of q are (quarter, head) pairs -- (quarter, even or odd steps) for one head -- with zeros in the other quarters'
-//   channels, so that a lane gets the products of quarter j alone and applies that quarter's scale and zero point only.  Sums over the
-//   quarters by an exchange among four lanes that leaves each with the logit of one entry.
-//   G >= 4: the columns are heads (repeated where G = 4); every group of channels has an accumulator, scaled by all lanes.
-// Values: channels are rows, entries the inner dimension, and the columns of the weights are (group, head) pairs, G = 1: groups.  The zero
-// points' part of the sum is one more product, of the zero points of the columns' groups with the weights.
+// Keys: entries are rows of the product.
+//   G <= 2: a column has a quarter of a head's channels (one head: of the even or of the odd steps), with zeros elsewhere, so that a lane
+//   gets the products of quarter j alone and applies that quarter's scale and zero point only.  Sums over the quarters by an
+//   exchange among four lanes that leaves each with the logit of one entry.
+//   G >= 4: a column has a head's channels (G = 4: of the even or of the odd steps); every group of channels has an accumulator.  A lane
+//   has the logits of head j (and j + 4) and four entries.
+// Values: channels are rows, entries the inner dimension, and the columns of the weights are (group, head) pairs.  The zero points' part
+// of the sum is one more product, of the zero points of the columns' groups with the weights.
 template <int D, int G>
 struct Kv4Warp {
   using Row = Kv4Row<D>;
   static constexpr bool kMasked = G <= 2;
-  static constexpr int kGroups = Row::kGroups, kSteps = D / 16;
-  static constexpr int kFrags = G * kGroups > 8 ? G * kGroups / 8 : 1;
-  static constexpr int kHeads = kMasked ? G : 2;           // heads of a lane's statistics: all, or 2j and 2j + 1 (of G)
+  static constexpr int kGroups = Row::kGroups, kHeads = kMasked ? G : G / 4;       // heads of a lane's statistics: all; j and j + 4
+  static constexpr int kFrags = G * kGroups > 8 ? G * kGroups / 8 : 1, kPer = kGroups / kFrags;   // fragments of weights; groups of one
   static constexpr float kHeadroom = 14.f;                 // weights are held times 2^14: fp16 numbers down to 2^-28
-  uint32_t q[kSteps][2];       // keys' products: the B operand of a step
-  float qsum[kMasked ? 1 : kGroups][kHeads];   // sum of the quarter's, or a group's, channels
+  static constexpr int kSteps = D / 16;
+  uint32_t q[kSteps][2];       // keys' products: the B operand of a step (16 channels, 4 of each lane's)
+  float qsum[kHeads][kMasked ? 1 : kGroups];   // sum of the quarter's, or a group's, channels
   float factor[kHeads];        // accumulator -> base-2 logit
   float o[D / 16][4];          // values' products: tile (group, half): channels 4r + 2 half and + 1, columns 2j and 2j + 1
   float zo[kFrags][4];         // zero points' products: row r is the group of column r; rows 8 .. 15 are nothing
   float m[kHeads], l[kHeads];
   uint32_t largest;            // twice the bits of the largest value scale seen, which the weights' power of two follows
   uint32_t shift;              // that power of two, twice
-  int lane;
 
-  // Group and head of column n of fragment f.
-  __device__ __forceinline__ static int group_of(int f, int n) { return G == 1 ? n % kGroups : (f * (8 / G) + n / G) % kGroups; }
-  __device__ __forceinline__ static int head_of(int n) { return n % G; }
-  __device__ __forceinline__ static int frag_of(int g) { return kFrags == 1 ? 0 : g * G / 8; }
+  // Where the lane's words lie in a stage: codes and pairs of its first 16 entries' keys (values: `half` bytes behind), and how far behind
+  // them those of the other 16 are.
+  struct Offsets {
+    int kc, kp, vc, vp, next_c, next_p;
+  };
+  __device__ __forceinline__ static Offsets offsets(int page, int page_shift, int row, int half) {
+    const int lane = threadIdx.x & 31, r = lane >> 2, j = lane & 3, first = row & (page - 1), chunk = page * Row::kBytes;
+    const int codes = (row >> page_shift) * chunk + first * Row::kCodes, pairs = (row >> page_shift) * chunk + Row::pairs(page, first);
+    Offsets a;
+    // (swizzles depend on rows mod 16 only)
+    a.kc = codes + (!kMasked ? r * Row::kCodes + 4 * j : kGroups == 4 ? Row::k_piece(r, j) : Row::k_piece(r, j >> 1) + (j & 1) * 8);
+    a.kp = pairs + r * Row::kPairs + (kMasked ? 2 * (j * kGroups / 4) : 0);
+    a.vc = half + codes + Row::v_unit(j, 0, r);
+    a.vp = half + pairs + j * Row::kPairs + (kFrags == 1 ? 2 * group_of(0, r) : G == 4 ? 2 * (r & 1) : 0);
+    a.next_c = page == 16 ? chunk : 16 * Row::kCodes;
+    a.next_p = page == 16 ? chunk : 16 * Row::kPairs;
+    return a;
+  }
+
+  // Group and head of column n of fragment f: a lane's columns 2j and 2j + 1 are of the heads whose statistics it has.
+  __device__ __forceinline__ static int group_of(int f, int n) {
+    return (G == 1 ? n : G == 2 ? n >> 1 : G == 4 ? 2 * f + (n & 1) : f) % kGroups;
+  }
+  __device__ __forceinline__ static int head_of(int n) { return G == 1 ? 0 : G == 2 ? n & 1 : G == 4 ? n >> 1 : (n >> 1) + 4 * (n & 1); }
 
   __device__ __forceinline__ void begin(const __nv_bfloat16* qrow, float scale_log2) {
-    lane = threadIdx.x & 31;
-    const int r = lane >> 2, j = lane & 3;
-    // column r: its head, and 16-channel pieces of it: of a quarter's, or of every group
-    const __nv_bfloat16* mine = qrow + (kMasked ? (G == 2 ? r & 1 : 0) : r % G) * D;
+    const int lane = threadIdx.x & 31, r = lane >> 2, j = lane & 3;
+    // the head of column r, and of its channels those that meet this lane's codes
+    const __nv_bfloat16* mine = qrow + (kMasked ? (G == 2 ? r & 1 : 0) : head_of(r)) * D + (kMasked ? j * (D / 4) : 8 * j);
     float x[kSteps][4], most = 0.f;
 #pragma unroll
     for (int t = 0; t < kSteps; t += 2) {
-      const uint4 u = *reinterpret_cast<const uint4*>(mine + (kMasked ? j * (D / 4) + 4 * t : 16 * t + 8 * j));
-      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+      const uint4 y = *reinterpret_cast<const uint4*>(mine + (kMasked ? 4 : 16) * t);
+      const uint32_t w[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        x[t + i / 2][i % 2 * 2] = __uint_as_float(w[i] << 16);
-        x[t + i / 2][i % 2 * 2 + 1] = __uint_as_float(w[i] & 0xffff0000u);
-      }
+      for (int i = 0; i < 4; ++i) { x[t + i / 2][i % 2 * 2] = __uint_as_float(w[i] << 16); x[t + i / 2][i % 2 * 2 + 1] = __uint_as_float(w[i] & 0xffff0000u); }
     }
 #pragma unroll
     for (int t = 0; t < kSteps; ++t)
@@ -121,20 +168,21 @@ struct Kv4Warp {
       const float2 a = half_pair_f(q[t][0]), b = half_pair_f(odd);
       sum += (a.x + a.y) + (b.x + b.y);
       q[t][1] = half_pair(b.x * 0.0625f, b.y * 0.0625f);  // meets codes in bits 4..7
-      if (!here || (G == 1 && (r & 1) != (t & 1))) q[t][0] = q[t][1] = 0u;
+      if (!here || (kHeads == 1 && (r & 1) != (t & 1))) q[t][0] = q[t][1] = 0u;
       if (!kMasked && t % 2 == 1) {
         sum += __shfl_xor_sync(~0u, sum, 1);
         sum += __shfl_xor_sync(~0u, sum, 2);
-        qsum[t / 2][0] = __shfl_sync(~0u, sum, 8 * j);
-        qsum[t / 2][kHeads - 1] = __shfl_sync(~0u, sum, 8 * j + 4);
+#pragma unroll
+        for (int u = 0; u < kHeads; ++u) qsum[u][kMasked ? 0 : t / 2] = __shfl_sync(~0u, sum, 8 * j + 4 * u);
       }
     }
 #pragma unroll
-    for (int c = 0; c < kHeads; ++c) {
-      if (kMasked) qsum[0][c] = __shfl_sync(~0u, sum, 4 * c + j);          // column c is head c; every column has the lane's quarter's sum
-      factor[c] = __shfl_sync(~0u, f, kMasked ? 4 * c : 8 * j + 4 * c);
-      m[c] = -INFINITY;
-      l[c] = 0.f;
+    for (int u = 0; u < kHeads; ++u) {
+      // (column u is head u where all lanes have the quarter's sum of their column's head)
+      if (kMasked) qsum[u][0] = __shfl_sync(~0u, sum, 4 * u + j);
+      factor[u] = __shfl_sync(~0u, f, kMasked ? 4 * u : 8 * j + 4 * u);
+      m[u] = -INFINITY;
+      l[u] = 0.f;
     }
 #pragma unroll
     for (int n = 0; n < D / 16; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
@@ -149,46 +197,44 @@ struct Kv4Warp {
     mma_m16n8k16_f16(d, a & 0x000f000fu, b & 0x000f000fu, a & 0x00f000f0u, b & 0x00f000f0u, q[t][0], q[t][1]);
     mma_m16n8k16_f16(d, a8 & 0x000f000fu, b8 & 0x000f000fu, a8 & 0x00f000f0u, b8 & 0x00f000f0u, q[t + 1][0], q[t + 1][1]);
   }
+  // A head's product of row half h.
+  __device__ __forceinline__ static float product(const float (&d)[4], int h, int u) { return kHeads == 1 ? d[2 * h] + d[2 * h + 1] : d[2 * h + u]; }
   // Scale, and zero point times 2^-24, of a pair.
   __device__ __forceinline__ static float pair_scale(uint32_t pair) { return kv4_scale(pair & 255); }
   __device__ __forceinline__ static float pair_zero(uint32_t pair) { return __half2float(__ushort_as_half((unsigned short)(pair >> 8 & 255))); }
 
-  // 32 entries from i0 on.  at[sub]: where each half's 16 entries lie: the page's chunk of keys in shared memory (that of the values is
-  // `half` bytes behind) and the first row in it.  bad: the page's number is none, its entries count as zeros.
-  struct Place {
-    const unsigned char* chunk;
-    int row, entry;
-    bool any, all, bad;
-  };
-  __device__ __forceinline__ void tile(const Place (&at)[2], int half, int page, const DecodeSpan& s, __half* weights) {
-    const int r = lane >> 2, j = lane & 3;
+  // 32 entries of the stage at shared memory address `stage`, the halves' first ones entry[0] and entry[1]; ~entry: the page's number is
+  // none, its entries count as zeros.  EVERY: all of them are seen (code for the others in the way cost a fifth of all instructions).
+  template <bool EVERY>
+  __device__ __forceinline__ void tile(uint32_t stage, const Offsets& at, int entry0, int entry1, const DecodeSpan& s, uint32_t weights) {
+    const int lane = threadIdx.x & 31, r = lane >> 2, j = lane & 3;
     constexpr int kMine = kMasked ? 1 : 4;                 // logits per lane and head: entries of sub 0: r, r + 8; of sub 1
+    constexpr int k8 = 8 * Row::kCodes, p8 = 8 * Row::kPairs;
     float x[kMine][kHeads];
     if constexpr (kMasked) {
       float v[4][G];
 #pragma unroll
       for (int sub = 0; sub < 2; ++sub) {
-        const unsigned char* tk = at[sub].chunk;
-        const int row = at[sub].row + r;
-        float d[4] = {};
+        const uint32_t tk = stage + at.kc + sub * at.next_c, tp = stage + at.kp + sub * at.next_p;
+        uint32_t a[kGroups], b[kGroups];
         if constexpr (kGroups == 4) {
-          const uint4 a = *reinterpret_cast<const uint4*>(tk + Row::k_piece(row, j)), b = *reinterpret_cast<const uint4*>(tk + Row::k_piece(row + 8, j));
-          two_steps(d, a.x, b.x, 0);
-          two_steps(d, a.y, b.y, 2);
-          two_steps(d, a.z, b.z, 4);
-          two_steps(d, a.w, b.w, 6);
+          const uint4 y = lds128(tk), w = lds128(tk + k8);
+          a[0] = y.x; a[1] = y.y; a[2] = y.z; a[3] = y.w;
+          b[0] = w.x; b[1] = w.y; b[2] = w.z; b[3] = w.w;
         } else {
-          const uint2 a = *reinterpret_cast<const uint2*>(tk + Row::k_piece(row, j >> 1) + (j & 1) * 8),
-                      b = *reinterpret_cast<const uint2*>(tk + Row::k_piece(row + 8, j >> 1) + (j & 1) * 8);
-          two_steps(d, a.x, b.x, 0);
-          two_steps(d, a.y, b.y, 2);
+          const uint2 y = lds64(tk), w = lds64(tk + k8);
+          a[0] = y.x; a[1] = y.y;
+          b[0] = w.x; b[1] = w.y;
         }
+        float d[4] = {};
+#pragma unroll
+        for (int t = 0; t < kGroups; ++t) two_steps(d, a[t], b[t], 2 * t);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const uint32_t pair = *reinterpret_cast<const uint16_t*>(tk + Row::pairs(page, row + 8 * h) + 2 * (j * kGroups / 4));
+          const uint32_t pair = lds16(tp + h * p8);
           const float sc = pair_scale(pair), z = pair_zero(pair);
 #pragma unroll
-          for (int c = 0; c < G; ++c) v[2 * sub + h][c] = sc * fmaf(-z, qsum[0][c], G == 1 ? d[2 * h] + d[2 * h + 1] : d[2 * h + c]);
+          for (int u = 0; u < G; ++u) v[2 * sub + h][u] = sc * fmaf(-z, qsum[u][0], product(d, h, u));
         }
       }
       // sums over the quarters: lane j keeps entry r + 8 (j % 2) of sub j / 2
@@ -201,112 +247,107 @@ struct Kv4Warp {
     } else {
 #pragma unroll
       for (int sub = 0; sub < 2; ++sub) {
-        const unsigned char* tk = at[sub].chunk;
-        const int row = at[sub].row + r;
+        const uint32_t tk = stage + at.kc + sub * at.next_c, tp = stage + at.kp + sub * at.next_p;
+        const int swizzle = Row::k_piece(r, 0) - r * Row::kCodes;
         uint32_t pairs[2][kGroups / 2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const unsigned char* p = tk + Row::pairs(page, row + 8 * h);
           if constexpr (kGroups == 4) {
-            const uint2 y = *reinterpret_cast<const uint2*>(p);
+            const uint2 y = lds64(tp + h * p8);
             pairs[h][0] = y.x;
             pairs[h][1] = y.y;
           } else {
-            pairs[h][0] = *reinterpret_cast<const uint32_t*>(p);
+            pairs[h][0] = lds32(tp + h * p8);
           }
-          x[2 * sub + h][0] = x[2 * sub + h][1] = 0.f;
+#pragma unroll
+          for (int u = 0; u < kHeads; ++u) x[2 * sub + h][u] = 0.f;
         }
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
+          const uint32_t piece = tk + (16 * g ^ swizzle);
           float d[4] = {};
-          two_steps(d, *reinterpret_cast<const uint32_t*>(tk + Row::k_piece(row, g) + 4 * j), *reinterpret_cast<const uint32_t*>(tk + Row::k_piece(row + 8, g) + 4 * j), 2 * g);
+          two_steps(d, lds32(piece), lds32(piece + k8), 2 * g);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const uint32_t pair = g & 1 ? pairs[h][g / 2] >> 16 : pairs[h][g / 2];
             const float sc = pair_scale(pair), z = pair_zero(pair);
 #pragma unroll
-            for (int c = 0; c < 2; ++c) x[2 * sub + h][c] = fmaf(sc, fmaf(-z, qsum[g][c], d[2 * h + c]), x[2 * sub + h][c]);
+            for (int u = 0; u < kHeads; ++u)
+              x[2 * sub + h][u] = fmaf(sc, fmaf(-z, qsum[u][g], product(d, h, u)), x[2 * sub + h][u]);
           }
         }
       }
     }
-    const bool every = at[0].all && at[1].all && !at[0].bad && !at[1].bad;
-    auto entry = [&](int k) {                              // of logit k
-      const int sub = kMasked ? j >> 1 : k >> 1, h = kMasked ? j & 1 : k & 1;
-      return (sub ? at[1].entry : at[0].entry) + r + 8 * h;
-    };
+    bool more = false;
 #pragma unroll
     for (int k = 0; k < kMine; ++k)
 #pragma unroll
       for (int c = 0; c < kHeads; ++c) {
         x[k][c] *= factor[c];
-        if (!every) {
-          const bool second = kMasked ? j >> 1 : k >> 1;
-          if (second ? at[1].bad : at[0].bad) x[k][c] = 0.f;
-          if (!s.sees(entry(k))) x[k][c] = -INFINITY;
+        if constexpr (!EVERY) {
+          const int e = (kMasked ? j >> 1 : k >> 1) ? entry1 : entry0, i = (e < 0 ? ~e : e) + r + 8 * (kMasked ? j & 1 : k & 1);
+          x[k][c] = !s.sees(i) ? -INFINITY : e < 0 ? 0.f : x[k][c];
         }
+        more = more || x[k][c] > m[c];
       }
-    // scales of the values: entries j + 4t, the group of column r, two entries to a word
-    uint32_t scale2[2][kFrags][2], zero2[2][kFrags][2], top = largest;
+    if (__any_sync(~0u, more)) raise(x);
+    // weights: entry e of a half at place (e % 4) * 4 + e / 4
+    __syncwarp();
+#pragma unroll
+    for (int c = 0; c < kHeads; ++c) {
+      const float ref = m[c] == -INFINITY ? 0.f : m[c] - kHeadroom;
+#pragma unroll
+      for (int k = 0; k < kMine; ++k) {
+        const float p = exp2_fast(x[k][c] - ref);
+        l[c] += p;
+        const int sub = kMasked ? j >> 1 : k >> 1, h = kMasked ? j & 1 : k & 1;
+        sts16(weights + 2 * ((kMasked ? c : j + 4 * c) * 32 + sub * 16 + (r & 3) * 4 + (r >> 2) + 2 * h), __float2half_rn(p));
+      }
+    }
+    __syncwarp();
 #pragma unroll
     for (int sub = 0; sub < 2; ++sub) {
-      const unsigned char* tv = at[sub].chunk + half;
+      // scales and zero points of the values: entries j + 4t, the group of column r, two entries to a word
+      const uint32_t tp = stage + at.vp + sub * at.next_p;
+      uint32_t scale2[kFrags][2], zero2[kFrags][2], top = largest;
 #pragma unroll
       for (int f = 0; f < kFrags; ++f) {
         uint32_t pair[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-          pair[t] = *reinterpret_cast<const uint16_t*>(tv + Row::pairs(page, at[sub].row + j + 4 * t) + 2 * group_of(f, r));
-          if (!every && (at[sub].bad || !s.sees(at[sub].entry + j + 4 * t))) pair[t] = 0u;
+          pair[t] = lds16(tp + 2 * f * kPer + t * 4 * Row::kPairs);
+          if constexpr (!EVERY) {
+            const int e = sub ? entry1 : entry0;
+            pair[t] = e >= 0 && s.sees(e + j + 4 * t) ? pair[t] : 0u;
+          }
         }
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          scale2[sub][f][t] = __byte_perm(pair[2 * t], pair[2 * t + 1], 0x4302) >> 1;
-          zero2[sub][f][t] = __byte_perm(pair[2 * t], pair[2 * t + 1], 0x3521);
-          top = __vmaxu2(top, scale2[sub][f][t]);
+          scale2[f][t] = __byte_perm(pair[2 * t], pair[2 * t + 1], 0x4302) >> 1;
+          zero2[f][t] = __byte_perm(pair[2 * t], pair[2 * t + 1], 0x3521);
+          top = half_max(top, scale2[f][t]);
         }
       }
-    }
-    bool more = top != largest;
-#pragma unroll
-    for (int k = 0; k < kMine; ++k)
-#pragma unroll
-      for (int c = 0; c < kHeads; ++c) more = more || x[k][c] > m[c];
-    if (__any_sync(~0u, more)) raise(x, top);
-    // weights: entry e of a half at place (e % 4) * 4 + e / 4
-    __syncwarp();
-#pragma unroll
-    for (int k = 0; k < kMine; ++k)
-#pragma unroll
-      for (int c = 0; c < kHeads; ++c) {
-        const float p = exp2_fast(x[k][c] - (m[c] == -INFINITY ? 0.f : m[c] - kHeadroom));
-        l[c] += p;
-        const int sub = kMasked ? j >> 1 : k >> 1, h = kMasked ? j & 1 : k & 1;
-        if (kMasked || 2 * j + c < G) weights[(kMasked ? c : 2 * j + c) * 32 + sub * 16 + (r & 3) * 4 + (r >> 2) + 2 * h] = __float2half_rn(p);
-      }
-    __syncwarp();
-#pragma unroll
-    for (int sub = 0; sub < 2; ++sub) {
-      const uint2 p = *reinterpret_cast<const uint2*>(weights + head_of(r) * 32 + sub * 16 + 4 * j);
+      if (__any_sync(~0u, top != largest)) widen(top);
+      const uint2 p = lds64(weights + 2 * (head_of(r) * 32 + sub * 16 + 4 * j));
       uint32_t b[kFrags][2];
 #pragma unroll
       for (int f = 0; f < kFrags; ++f) {
-        b[f][0] = half_mul(p.x, half_mul(scale2[sub][f][0], shift));
-        b[f][1] = half_mul(p.y, half_mul(scale2[sub][f][1], shift));
-        mma_m16n8k16_f16(zo[f], zero2[sub][f][0], 0u, zero2[sub][f][1], 0u, b[f][0], b[f][1]);
+        b[f][0] = half_mul(p.x, half_mul(scale2[f][0], shift));
+        b[f][1] = half_mul(p.y, half_mul(scale2[f][1], shift));
+        mma_m16n8k16_f16(zo[f], zero2[f][0], 0u, zero2[f][1], 0u, b[f][0], b[f][1]);
       }
       // units r of every group, of entries j + 4t
-      const unsigned char* tv = at[sub].chunk + half;
+      const uint32_t tv = stage + at.vc + sub * at.next_c;
       uint32_t w[4][kGroups / 2];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        const unsigned char* p4 = tv + Row::v_unit(at[sub].row + j + 4 * t, 0, r);
         if constexpr (kGroups == 4) {
-          const uint2 y = *reinterpret_cast<const uint2*>(p4);
+          const uint2 y = lds64(tv + t * 4 * Row::kCodes);
           w[t][0] = y.x;
           w[t][1] = y.y;
         } else {
-          w[t][0] = *reinterpret_cast<const uint32_t*>(p4);
+          w[t][0] = lds32(tv + t * 4 * Row::kCodes);
         }
       }
 #pragma unroll
@@ -314,19 +355,22 @@ struct Kv4Warp {
         // entries j | j + 4 and j + 8 | j + 12 side by side
         const uint32_t lo = __byte_perm(w[0][g / 2], w[1][g / 2], g & 1 ? 0x7632 : 0x5410), hi = __byte_perm(w[2][g / 2], w[3][g / 2], g & 1 ? 0x7632 : 0x5410);
         const uint32_t lo8 = lo >> 8, hi8 = hi >> 8;
-        const int f = frag_of(g);
+        const int f = g / kPer;
         mma_m16n8k16_f16(o[2 * g], lo & 0x000f000fu, lo & 0x00f000f0u, hi & 0x000f000fu, hi & 0x00f000f0u, b[f][0], b[f][1]);
         mma_m16n8k16_f16(o[2 * g + 1], lo8 & 0x000f000fu, lo8 & 0x00f000f0u, hi8 & 0x000f000fu, hi8 & 0x00f000f0u, b[f][0], b[f][1]);
       }
     }
   }
 
-  // A larger logit, or value scale, than any before: sums so far follow.
+  __device__ __forceinline__ void scale_sums(float f0, float f1) {         // of columns 2j and 2j + 1
+#pragma unroll
+    for (int n = 0; n < D / 16; ++n) { o[n][0] *= f0; o[n][1] *= f1; o[n][2] *= f0; o[n][3] *= f1; }
+#pragma unroll
+    for (int n = 0; n < kFrags; ++n) { zo[n][0] *= f0; zo[n][1] *= f1; }
+  }
+  // A larger logit than any before: sums so far follow.
   template <int K>
-  __device__ __forceinline__ void raise(const float (&x)[K][kHeads], uint32_t top) {
-    top = __reduce_max_sync(~0u, max(top & 0xffffu, top >> 16));
-    // the largest scale comes to [1, 2): 2^(15 - its exponent field), as a half
-    const float was = half_pair_f(shift).x, to = pow2f(15 - max(1, (int)(top >> 10))), ratio = largest ? to / was : 0.f;
+  __device__ __forceinline__ void raise(const float (&x)[K][kHeads]) {
     float f[kHeads];
 #pragma unroll
     for (int c = 0; c < kHeads; ++c) {
@@ -336,62 +380,65 @@ struct Kv4Warp {
 #pragma unroll
       for (int off = kMasked ? 1 : 4; off < 32; off <<= 1) mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, off));
       mx = fmaxf(mx, m[c]);
-      const float g = exp2_fast(m[c] - (mx == -INFINITY ? 0.f : mx));
-      l[c] *= g;
-      f[c] = g * ratio;
+      f[c] = exp2_fast(m[c] - (mx == -INFINITY ? 0.f : mx));
+      l[c] *= f[c];
       m[c] = mx;
     }
-    const float f0 = f[0], f1 = f[kHeads - 1];             // of columns 2j and 2j + 1
-#pragma unroll
-    for (int n = 0; n < D / 16; ++n) { o[n][0] *= f0; o[n][1] *= f1; o[n][2] *= f0; o[n][3] *= f1; }
-#pragma unroll
-    for (int n = 0; n < kFrags; ++n) { zo[n][0] *= f0; zo[n][1] *= f1; }
-    if (top) {
-      largest = top | top << 16;
-      shift = half_pair(to, to);
-    }
+    scale_sums(f[0], f[kHeads - 1]);
+  }
+  // A larger value scale: it comes to [1, 2) by 2^(15 - its exponent field).
+  __device__ __forceinline__ void widen(uint32_t top) {
+    top = __reduce_max_sync(~0u, max(top & 0xffffu, top >> 16));
+    const float was = half_pair_f(shift).x, to = pow2f(15 - max(1, (int)(top >> 10))), ratio = largest ? to / was : 0.f;
+    scale_sums(ratio, ratio);
+    largest = top | top << 16;
+    shift = half_pair(to, to);
   }
 
   // (max, sum) of the heads over this warp's entries to [8] each
   __device__ __forceinline__ void stats(float* sm_m, float* sm_l) {
-    const int j = lane & 3;
+    const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int c = 0; c < kHeads; ++c) {
 #pragma unroll
       for (int off = kMasked ? 1 : 4; off < 32; off <<= 1) l[c] += __shfl_xor_sync(~0u, l[c], off);
-      const int head = kMasked ? c : 2 * j + c;
-      if (lane < (kMasked ? 1 : 4) && head < G) { sm_m[head] = m[c]; sm_l[head] = l[c] * 0x1p-14f; }
+      if (lane < (kMasked ? 1 : 4)) {
+        sm_m[kMasked ? c : lane + 4 * c] = m[c];
+        sm_l[kMasked ? c : lane + 4 * c] = l[c] * 0x1p-14f;
+      }
     }
   }
-  // The warp's output [G][D], relative to the heads' maxima big[G]; zeros: scratch, [groups][G].
-  __device__ __forceinline__ void write(float* out, const float* big, float* zeros) {
-    const int r = lane >> 2, j = lane & 3;
+  // The warp's output [G][D], relative to the heads' maxima big[G], to `out` or (ADD) on top of what is there; zeros: scratch, [groups][G].
+  template <bool ADD>
+  __device__ __forceinline__ void write(float* out, const float* big, float* zeros) const {
+    const int lane = threadIdx.x & 31, r = lane >> 2, j = lane & 3;
     __syncwarp();
 #pragma unroll
     for (int f = 0; f < kFrags; ++f)                       // column r meets its own group in row r
-      if (j == r >> 1 && (G == 1 ? r < kGroups : f * (8 / G) + r / G < kGroups)) zeros[group_of(f, r) * G + head_of(r)] = r & 1 ? zo[f][1] : zo[f][0];
+      if (j == r >> 1 && (G == 1 ? r < kGroups : G == 2 ? r >> 1 < kGroups : true)) zeros[group_of(f, r) * G + head_of(r)] = r & 1 ? zo[f][1] : zo[f][0];
     __syncwarp();
     const float back = largest ? 0x1p10f / half_pair_f(shift).x : 0.f;     // codes' 2^24, weights' 2^-14
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      const int col = 2 * j + c, head = head_of(col);
-      const float mm = m[c < kHeads ? c : 0], f = mm == -INFINITY ? 0.f : exp2_fast(mm - big[head]) * back;
-      // of a fragment's groups the one of this column, by selection: registers have no indexes
-      constexpr int kPer = kGroups / kFrags;
-      const int which = G == 1 ? col : col / G;
+      const int head = head_of(2 * j + c), which = G == 1 ? 2 * j + c : G == 2 ? j : G == 4 ? c : 0;     // the column's group in its fragment
+      const float mm = m[kHeads == 2 ? c : 0], f = mm == -INFINITY ? 0.f : exp2_fast(mm - big[head]) * back;
 #pragma unroll
       for (int f8 = 0; f8 < kFrags; ++f8) {
         float a[4] = {};
 #pragma unroll
-        for (int i = 0; i < kPer; ++i)
+        for (int i = 0; i < kPer; ++i)                     // by selection: registers have no indexes
 #pragma unroll
           for (int h = 0; h < 4; ++h) a[h] = i == which ? o[2 * (f8 * kPer + i) + h / 2][c + h % 2 * 2] : a[h];
         if (which >= kPer) continue;
         const int g = f8 * kPer + which;
         const float z = zeros[g * G + head];
-        float2* to = reinterpret_cast<float2*>(out + head * D + g * 32 + 4 * r);
-        to[0] = make_float2((a[0] - z) * f, (a[1] * 0x1p-4f - z) * f);
-        to[1] = make_float2((a[2] - z) * f, (a[3] * 0x1p-4f - z) * f);
+        float4* to = reinterpret_cast<float4*>(out + head * D + g * 32 + 4 * r);
+        float4 y = make_float4((a[0] - z) * f, (a[1] * 0x1p-4f - z) * f, (a[2] - z) * f, (a[3] * 0x1p-4f - z) * f);
+        if constexpr (ADD) {
+          const float4 was = *to;
+          y.x += was.x; y.y += was.y; y.z += was.z; y.w += was.w;
+        }
+        *to = y;
       }
     }
   }
@@ -406,9 +453,9 @@ __global__ void __launch_bounds__(kKv4Threads, 2) paged_decode_kv4_kernel(const 
   using Warp = Kv4Warp<D, G>;
   constexpr int TILE = kKv4Tile, STAGES = Sh::kStages;
   extern __shared__ __align__(128) unsigned char ring[];
-  float* sm_out = reinterpret_cast<float*>(ring + STAGES * Sh::kStage);         // [warps][G][D]
-  float* scratch = sm_out + kKv4Warps * G * D;                                  // [warps][G][32]
-  float* sm_m = scratch + kKv4Warps * 32 * G;                                   // [warps][8]
+  float* sm_out = reinterpret_cast<float*>(ring + STAGES * Sh::kStage);         // [outs][G][D]
+  float* scratch = sm_out + Sh::kOuts * G * D;                                  // [warps][G][16]
+  float* sm_m = scratch + kKv4Warps * 16 * G;                                   // [warps][8]
   float* sm_l = sm_m + kKv4Warps * 8;
   int* lens = reinterpret_cast<int*>(sm_l + kKv4Warps * 8);                     // [batch]
   int* cum = lens + kMaxSequences;                                              // [batch + 1] tiles of one head before b, then the most
@@ -540,33 +587,37 @@ __global__ void __launch_bounds__(kKv4Threads, 2) paged_decode_kv4_kernel(const 
   Warp w;
   bool ok = true;          // else a wait gave up: this warp keeps the others' barriers company, and counts its pieces, but reads no more tiles
   int it = 0;
-  float* mine = scratch + warp * 32 * G;
+  float* mine = scratch + warp * 16 * G;
   const int team = warp / kKv4TileWarps, row = warp % kKv4TileWarps * kKv4Share;       // the tiles, and rows of a tile, that are this warp's
+  const typename Warp::Offsets at = Warp::offsets(A.page, A.page_shift, row, Sh::kHalf);
+  const int* entries = slot_entry + (row >> A.page_shift);
+  const int first = row & (A.page - 1), second = A.page == 16 ? 0 : first + 16;        // of the halves' pages
+  const int next_slot = A.page == 16 ? 1 : 0;
+  const uint32_t ring0 = smem_u32(ring);
   for (long long t = t0; t < t1;) {
     const int first_v = v;
     const int n = (int)min((long long)(s.tiles - v), t1 - t);            // tiles of this piece
     const long long lane_no = (long long)b * H + head;
     const int hq0 = head * G;
     w.begin(static_cast<const __nv_bfloat16*>(A.q) + (long long)b * A.q_stride + (long long)hq0 * D, A.scale_log2);
-    for (int k = 0; k < n; ++k, ++it) {
-      if ((it & 1) != team) continue;
-      const int st = it % STAGES;
-      ok = ok && wait(&full[st], (it / STAGES) & 1);
+    const unsigned fit = (unsigned)max(0, s.len - 15 - s.lo);            // places for 16 entries, all of them seen, from s.lo on
+    for (int k = (it ^ team) & 1; k < n; k += 2) {
+      const int st = (it + k) & (STAGES - 1);
+      ok = ok && wait(&full[st], ((it + k) / STAGES) & 1);
       if (!ok) continue;
-      typename Warp::Place at[2];
-#pragma unroll
-      for (int sub = 0; sub < 2; ++sub) {
-        const int from = row + 16 * sub, slot = from >> A.page_shift, e = slot_entry[st * kKv4MaxSlots + slot];
-        at[sub].bad = e < 0;
-        at[sub].row = from & (A.page - 1);
-        at[sub].entry = (e < 0 ? ~e : e) + at[sub].row;
-        at[sub].chunk = ring + st * Sh::kStage + slot * chunk_bytes;
-        at[sub].any = at[sub].entry < s.len && (at[sub].entry + 16 > s.lo || at[sub].entry < s.sinks);
-        at[sub].all = at[sub].entry + 16 <= s.len && (at[sub].entry >= s.lo || at[sub].entry + 16 <= s.sinks);
+      const int e0 = entries[st * kKv4MaxSlots], e1 = entries[st * kKv4MaxSlots + next_slot];
+      const uint32_t stage = ring0 + st * Sh::kStage;
+      if ((unsigned)(e0 + first - s.lo) < fit && (unsigned)(e1 + second - s.lo) < fit) {
+        w.template tile<true>(stage, at, 0, 0, s, smem_u32(mine));
+      } else {
+        // first entries, complements for bad pages
+        const int i0 = e0 < 0 ? e0 - first : e0 + first, i1 = e1 < 0 ? e1 - second : e1 + second;
+        auto any = [&](int e) { const int i = e < 0 ? ~e : e; return i < s.len && (i + 16 > s.lo || i < s.sinks); };
+        if (any(i0) || any(i1)) w.template tile<false>(stage, at, i0, i1, s, smem_u32(mine));
       }
-      if (at[0].any || at[1].any) w.tile(at, Sh::kHalf, A.page, s, reinterpret_cast<__half*>(mine));
       release_stage(&empty[st]);
     }
+    it += n;
     v += n;
     // join the eight warps
     w.stats(sm_m + warp * 8, sm_l + warp * 8);
@@ -591,14 +642,18 @@ __global__ void __launch_bounds__(kKv4Threads, 2) paged_decode_kv4_kernel(const 
       sm_l[tid] = sl;
     }
     kv4_consumers_sync();
-    w.write(sm_out + warp * G * D, sm_m, mine);
+    if (warp < Sh::kOuts) w.template write<false>(sm_out + warp * G * D, sm_m, mine);
     kv4_consumers_sync();
+    if constexpr (Sh::kOuts < kKv4Warps) {
+      if (warp >= Sh::kOuts) w.template write<true>(sm_out + (warp - Sh::kOuts) * G * D, sm_m, mine);
+      kv4_consumers_sync();
+    }
     const bool whole = n == s.tiles;
     constexpr int kVecs = G * D / 4;                       // float4s of a lane's output
     auto warps_sum = [&](int e) {
       float4 x = reinterpret_cast<const float4*>(sm_out)[e];
 #pragma unroll
-      for (int i = 1; i < kKv4Warps; ++i) {
+      for (int i = 1; i < Sh::kOuts; ++i) {
         const float4 y = reinterpret_cast<const float4*>(sm_out + i * G * D)[e];
         x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
       }
