@@ -35,8 +35,9 @@ struct Kv4Shape {
   static constexpr int kOuts = G == 8 ? kKv4Warps / 2 : kKv4Warps;      // outputs side by side in the join: the warps', or of pairs of them
   static constexpr int kOut = kOuts * G * D * 4;
   static constexpr int kScratch = kKv4Warps * 16 * G * 4; // a warp's weights, then zero points' sums
-  static constexpr int kSmem = kStages * kStage + kOut + kScratch + 2 * kKv4Warps * 8 * 4 + (2 * kMaxSequences + 8) * 4 + 2 * kStages * 8 +
-                               kStages * kKv4MaxSlots * 4 + 16;
+  static constexpr int kQuery = D / 32 * 512;             // Kv4Warp::kQuery
+  static constexpr int kSmem = kStages * kStage + kOut + kScratch + kQuery + 2 * kKv4Warps * 8 * 4 + (2 * kMaxSequences + 8) * 4 + 2 * kStages * 8 +
+                               kStages * kKv4MaxSlots * 4 + 64;
   static_assert((kStages & (kStages - 1)) == 0, "stages by masks");
 };
 
@@ -99,11 +100,12 @@ template <int D, int G>
 struct Kv4Warp {
   using Row = Kv4Row<D>;
   static constexpr bool kMasked = G <= 2;
-  static constexpr int kGroups = Row::kGroups, kHeads = kMasked ? G : G / 4;       // heads of a lane's statistics: all; j and j + 4
+  static constexpr int kSteps = D / 16, kGroups = Row::kGroups, kHeads = kMasked ? G : G / 4;       // heads of a lane's statistics: all; j and j + 4
   static constexpr int kFrags = G * kGroups > 8 ? G * kGroups / 8 : 1, kPer = kGroups / kFrags;   // fragments of weights; groups of one
+  // The keys' products' B operands (a step: 16 channels, 4 of each lane's) are in shared memory, one copy for all warps, two steps to a
+  // lane's 16 bytes: they would take a sixth of the registers.
+  static constexpr int kQuery = kSteps / 2 * 32 * 16;      // bytes
   static constexpr float kHeadroom = 14.f;                 // weights are held times 2^14: fp16 numbers down to 2^-28
-  static constexpr int kSteps = D / 16;
-  uint32_t q[kSteps][2];       // keys' products: the B operand of a step (16 channels, 4 of each lane's)
   float qsum[kHeads][kMasked ? 1 : kGroups];   // sum of the quarter's, or a group's, channels
   float factor[kHeads];        // accumulator -> base-2 logit
   float o[D / 16][4];          // values' products: tile (group, half): channels 4r + 2 half and + 1, columns 2j and 2j + 1
@@ -137,7 +139,7 @@ struct Kv4Warp {
   }
   __device__ __forceinline__ static int head_of(int n) { return G == 1 ? 0 : G == 2 ? n & 1 : G == 4 ? n >> 1 : (n >> 1) + 4 * (n & 1); }
 
-  __device__ __forceinline__ void begin(const __nv_bfloat16* qrow, float scale_log2) {
+  __device__ __forceinline__ void begin(const __nv_bfloat16* qrow, float scale_log2, uint4* query, bool stores) {
     const int lane = threadIdx.x & 31, r = lane >> 2, j = lane & 3;
     // the head of column r, and of its channels those that meet this lane's codes
     const __nv_bfloat16* mine = qrow + (kMasked ? (G == 2 ? r & 1 : 0) : head_of(r)) * D + (kMasked ? j * (D / 4) : 8 * j);
@@ -160,15 +162,18 @@ struct Kv4Warp {
     const float up = pow2f(e), f = scale_log2 * pow2f(-e) * 0x1p24f;
     const bool here = !kMasked || r >> 1 == j;             // does column r hold the lane's quarter?
     float sum = 0.f;
+    uint32_t q[2][2];
 #pragma unroll
     for (int t = 0; t < kSteps; ++t) {
       if (!kMasked && t % 2 == 0) sum = 0.f;
-      q[t][0] = half_pair(x[t][0] * up, x[t][1] * up);
+      uint32_t (&w)[2] = q[t & 1];
+      w[0] = half_pair(x[t][0] * up, x[t][1] * up);
       const uint32_t odd = half_pair(x[t][2] * up, x[t][3] * up);
-      const float2 a = half_pair_f(q[t][0]), b = half_pair_f(odd);
+      const float2 a = half_pair_f(w[0]), b = half_pair_f(odd);
       sum += (a.x + a.y) + (b.x + b.y);
-      q[t][1] = half_pair(b.x * 0.0625f, b.y * 0.0625f);  // meets codes in bits 4..7
-      if (!here || (kHeads == 1 && (r & 1) != (t & 1))) q[t][0] = q[t][1] = 0u;
+      w[1] = half_pair(b.x * 0.0625f, b.y * 0.0625f);     // meets codes in bits 4..7
+      if (!here || (kHeads == 1 && (r & 1) != (t & 1))) w[0] = w[1] = 0u;
+      if (t % 2 == 1 && stores) query[t / 2 * 32 + lane] = make_uint4(q[0][0], q[0][1], q[1][0], q[1][1]);
       if (!kMasked && t % 2 == 1) {
         sum += __shfl_xor_sync(~0u, sum, 1);
         sum += __shfl_xor_sync(~0u, sum, 2);
@@ -192,10 +197,10 @@ struct Kv4Warp {
   }
 
   // Products of two steps: words a and b hold eight codes each of rows r and r + 8.
-  __device__ __forceinline__ void two_steps(float (&d)[4], uint32_t a, uint32_t b, int t) const {
+  __device__ __forceinline__ static void two_steps(float (&d)[4], uint32_t a, uint32_t b, const uint4& q) {
     const uint32_t a8 = a >> 8, b8 = b >> 8;
-    mma_m16n8k16_f16(d, a & 0x000f000fu, b & 0x000f000fu, a & 0x00f000f0u, b & 0x00f000f0u, q[t][0], q[t][1]);
-    mma_m16n8k16_f16(d, a8 & 0x000f000fu, b8 & 0x000f000fu, a8 & 0x00f000f0u, b8 & 0x00f000f0u, q[t + 1][0], q[t + 1][1]);
+    mma_m16n8k16_f16(d, a & 0x000f000fu, b & 0x000f000fu, a & 0x00f000f0u, b & 0x00f000f0u, q.x, q.y);
+    mma_m16n8k16_f16(d, a8 & 0x000f000fu, b8 & 0x000f000fu, a8 & 0x00f000f0u, b8 & 0x00f000f0u, q.z, q.w);
   }
   // A head's product of row half h.
   __device__ __forceinline__ static float product(const float (&d)[4], int h, int u) { return kHeads == 1 ? d[2 * h] + d[2 * h + 1] : d[2 * h + u]; }
@@ -206,11 +211,14 @@ struct Kv4Warp {
   // 32 entries of the stage at shared memory address `stage`, the halves' first ones entry[0] and entry[1]; ~entry: the page's number is
   // none, its entries count as zeros.  EVERY: all of them are seen (code for the others in the way cost a fifth of all instructions).
   template <bool EVERY>
-  __device__ __forceinline__ void tile(uint32_t stage, const Offsets& at, int entry0, int entry1, const DecodeSpan& s, uint32_t weights) {
+  __device__ __forceinline__ void tile(uint32_t stage, const Offsets& at, int entry0, int entry1, const DecodeSpan& s, uint32_t weights, uint32_t query) {
     const int lane = threadIdx.x & 31, r = lane >> 2, j = lane & 3;
     constexpr int kMine = kMasked ? 1 : 4;                 // logits per lane and head: entries of sub 0: r, r + 8; of sub 1
     constexpr int k8 = 8 * Row::kCodes, p8 = 8 * Row::kPairs;
     float x[kMine][kHeads];
+    uint4 q[kGroups];
+#pragma unroll
+    for (int t = 0; t < kGroups; ++t) q[t] = lds128(query + (t * 32 + lane) * 16);
     if constexpr (kMasked) {
       float v[4][G];
 #pragma unroll
@@ -228,7 +236,7 @@ struct Kv4Warp {
         }
         float d[4] = {};
 #pragma unroll
-        for (int t = 0; t < kGroups; ++t) two_steps(d, a[t], b[t], 2 * t);
+        for (int t = 0; t < kGroups; ++t) two_steps(d, a[t], b[t], q[t]);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const uint32_t pair = lds16(tp + h * p8);
@@ -266,7 +274,7 @@ struct Kv4Warp {
         for (int g = 0; g < kGroups; ++g) {
           const uint32_t piece = tk + (16 * g ^ swizzle);
           float d[4] = {};
-          two_steps(d, lds32(piece), lds32(piece + k8), 2 * g);
+          two_steps(d, lds32(piece), lds32(piece + k8), q[g]);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const uint32_t pair = g & 1 ? pairs[h][g / 2] >> 16 : pairs[h][g / 2];
@@ -444,6 +452,13 @@ struct Kv4Warp {
   }
 };
 
+struct Kv4Piece {
+  long long chunk;           // tiles per CTA of the deal
+  int b, head, v, left;      // lane, first tile, tiles until the end of the CTA's run
+  int last;                  // is it the last piece of its lane?
+  DecodeSpan s;
+};
+
 __device__ __forceinline__ void kv4_consumers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kKv4Warps * 32) : "memory"); }
 
 template <int D, int G, bool CHOSEN>
@@ -454,7 +469,8 @@ __global__ void __launch_bounds__(kKv4Threads, 2) paged_decode_kv4_kernel(const 
   constexpr int TILE = kKv4Tile, STAGES = Sh::kStages;
   extern __shared__ __align__(128) unsigned char ring[];
   float* sm_out = reinterpret_cast<float*>(ring + STAGES * Sh::kStage);         // [outs][G][D]
-  float* scratch = sm_out + Sh::kOuts * G * D;                                  // [warps][G][16]
+  uint4* query = reinterpret_cast<uint4*>(sm_out + Sh::kOuts * G * D);
+  float* scratch = reinterpret_cast<float*>(query + Sh::kQuery / 16);           // [warps][G][16]
   float* sm_m = scratch + kKv4Warps * 16 * G;                                   // [warps][8]
   float* sm_l = sm_m + kKv4Warps * 8;
   int* lens = reinterpret_cast<int*>(sm_l + kKv4Warps * 8);                     // [batch]
@@ -462,13 +478,17 @@ __global__ void __launch_bounds__(kKv4Threads, 2) paged_decode_kv4_kernel(const 
   int* slot_entry = cum + kMaxSequences + 8;                                    // [stages][slots] first entry of a page, see below
   uint64_t* full = reinterpret_cast<uint64_t*>(slot_entry + STAGES * kKv4MaxSlots);
   uint64_t* empty = full + STAGES;
-  int* sm_last = reinterpret_cast<int*>(empty + STAGES);
+  // the consumers' piece: little of it is needed inside the loop over tiles, whose registers are short
+  Kv4Piece* piece = reinterpret_cast<Kv4Piece*>(empty + STAGES);
 
   const PagedParams& A = P.A;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   auto span = [&](int len) {
-    if constexpr (CHOSEN) return chosen_span<TILE>(A, len, P.n_select);
-    else return decode_span<TILE>(len, A.window, A.sink);
+    DecodeSpan x;
+    if constexpr (CHOSEN) x = chosen_span<TILE>(A, len, P.n_select);
+    else x = decode_span<TILE>(len, A.window, A.sink);
+    if (len == 0) x.tiles = 0;                             // padding costs no piece
+    return x;
   };
   if (tid == 0) {
     for (int i = 0; i < STAGES; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], kKv4TileWarps); }
@@ -500,8 +520,14 @@ __global__ void __launch_bounds__(kKv4Threads, 2) paged_decode_kv4_kernel(const 
   const long long total = (long long)cum[A.batch] * H;
   const long long chunk = (total + gridDim.x - 1) / gridDim.x;
   long long t0 = cta * chunk, t1 = min(total, t0 + chunk);
-  // few lanes of nearly equal length: a lane each, as in the bf16 rows' kernel
   const long long lanes = (long long)A.batch * H;
+  for (long long e = cta; e < lanes; e += gridDim.x) {     // padded rows
+    if (lens[e / H] != 0) continue;
+    const long long to = (e / H * A.n_q_heads + e % H * G) * D;
+    for (int i = tid; i < G * D / 8; i += kKv4Threads) reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(A.out) + to)[i] = make_uint4(0, 0, 0, 0);
+    if (A.lse && tid < G) A.lse[to / D + tid] = -INFINITY;
+  }
+  // few lanes of nearly equal length: a lane each, as in the bf16 rows' kernel
   if (lanes <= gridDim.x && cum[A.batch + 1] <= chunk + kJoinTiles) {
     if (cta >= lanes) return;
     const int bb = cta / H, tiles = cum[bb + 1] - cum[bb];
@@ -524,14 +550,19 @@ __global__ void __launch_bounds__(kKv4Threads, 2) paged_decode_kv4_kernel(const 
   const uint32_t chunk_bytes = (uint32_t)A.page * Row::kBytes;
   // copies in flight at the end: as in the bf16 rows' kernel, there are none
   auto wait = [&](uint64_t* bar, uint32_t parity) { return (bool)__all_sync(~0u, mbar_wait(bar, parity, A.status, kWaitPolls)); };
+  if (tid == 0) {
+    piece->chunk = chunk;
+    piece->b = b; piece->head = head; piece->v = v; piece->left = (int)(t1 - t0);
+    piece->s = s;
+  }
   // Where page `slot` of a tile starts: its first entry, which is seen or not; of a bad page ~entry; the sequence's length if the page
   // holds nothing visible (so that no entry in it is).
   if (warp == kKv4Warps) {                                 // ---- producer
     const uint64_t policy = l2_policy_evict_first();
     fence_proxy_async();                                   // rows that earlier kernels stored are read by the copies
     int it = 0;
-    for (long long t = t0; t < t1;) {
-      const int n = (int)min((long long)(s.tiles - v), t1 - t);
+    for (int left = (int)(t1 - t0); left > 0;) {
+      const int n = min(s.tiles - v, left);
       const int per = 32 >> slot_shift;                    // tiles whose pages are looked up together
       const long long lane_no = (long long)b * H + head;
       for (int k0 = 0; k0 < n; k0 += per) {
@@ -570,13 +601,13 @@ __global__ void __launch_bounds__(kKv4Threads, 2) paged_decode_kv4_kernel(const 
           }
         }
       }
-      t += n;
+      left -= n;
       v += n;
-      if (v == s.tiles) {
+      if (v == s.tiles && left > 0) {
         v = 0;
-        if (++head == H && t < t1) {
+        if (++head == H) {
           head = 0;
-          s = span(lens[++b]);
+          do s = span(lens[++b]); while (s.tiles == 0);
         }
       }
     }
@@ -590,35 +621,34 @@ __global__ void __launch_bounds__(kKv4Threads, 2) paged_decode_kv4_kernel(const 
   float* mine = scratch + warp * 16 * G;
   const int team = warp / kKv4TileWarps, row = warp % kKv4TileWarps * kKv4Share;       // the tiles, and rows of a tile, that are this warp's
   const typename Warp::Offsets at = Warp::offsets(A.page, A.page_shift, row, Sh::kHalf);
-  const int* entries = slot_entry + (row >> A.page_shift);
   const int first = row & (A.page - 1), second = A.page == 16 ? 0 : first + 16;        // of the halves' pages
-  const int next_slot = A.page == 16 ? 1 : 0;
-  const uint32_t ring0 = smem_u32(ring);
-  for (long long t = t0; t < t1;) {
-    const int first_v = v;
-    const int n = (int)min((long long)(s.tiles - v), t1 - t);            // tiles of this piece
-    const long long lane_no = (long long)b * H + head;
-    const int hq0 = head * G;
-    w.begin(static_cast<const __nv_bfloat16*>(A.q) + (long long)b * A.q_stride + (long long)hq0 * D, A.scale_log2);
-    const unsigned fit = (unsigned)max(0, s.len - 15 - s.lo);            // places for 16 entries, all of them seen, from s.lo on
+  const uint32_t ring0 = smem_u32(ring), entry0 = smem_u32(slot_entry + (row >> A.page_shift)), entry1 = entry0 + (A.page == 16 ? 4 : 0);
+  for (;;) {
+    kv4_consumers_sync();                                  // the piece is there, sm_* are free
+    if (piece->left <= 0) break;
+    const int n = min(piece->s.tiles - piece->v, piece->left);           // tiles of this piece
+    w.begin(static_cast<const __nv_bfloat16*>(A.q) + (long long)piece->b * A.q_stride + (long long)piece->head * G * D, A.scale_log2, query, warp == 0);
+    kv4_consumers_sync();
+    const int lo = piece->s.lo;
+    const unsigned fit = (unsigned)max(0, piece->s.len - 15 - lo);       // places for 16 entries, all of them seen, from lo on
     for (int k = (it ^ team) & 1; k < n; k += 2) {
       const int st = (it + k) & (STAGES - 1);
       ok = ok && wait(&full[st], ((it + k) / STAGES) & 1);
       if (!ok) continue;
-      const int e0 = entries[st * kKv4MaxSlots], e1 = entries[st * kKv4MaxSlots + next_slot];
+      const int e0 = (int)lds32(entry0 + st * (kKv4MaxSlots * 4)), e1 = (int)lds32(entry1 + st * (kKv4MaxSlots * 4));
       const uint32_t stage = ring0 + st * Sh::kStage;
-      if ((unsigned)(e0 + first - s.lo) < fit && (unsigned)(e1 + second - s.lo) < fit) {
-        w.template tile<true>(stage, at, 0, 0, s, smem_u32(mine));
+      if ((unsigned)(e0 + first - lo) < fit && (unsigned)(e1 + second - lo) < fit) {
+        w.template tile<true>(stage, at, 0, 0, DecodeSpan(), smem_u32(mine), smem_u32(query));
       } else {
         // first entries, complements for bad pages
         const int i0 = e0 < 0 ? e0 - first : e0 + first, i1 = e1 < 0 ? e1 - second : e1 + second;
+        const DecodeSpan s = piece->s;
         auto any = [&](int e) { const int i = e < 0 ? ~e : e; return i < s.len && (i + 16 > s.lo || i < s.sinks); };
-        if (any(i0) || any(i1)) w.template tile<false>(stage, at, i0, i1, s, smem_u32(mine));
+        if (any(i0) || any(i1)) w.template tile<false>(stage, at, i0, i1, s, smem_u32(mine), smem_u32(query));
       }
       release_stage(&empty[st]);
     }
     it += n;
-    v += n;
     // join the eight warps
     w.stats(sm_m + warp * 8, sm_l + warp * 8);
     kv4_consumers_sync();
@@ -648,7 +678,9 @@ __global__ void __launch_bounds__(kKv4Threads, 2) paged_decode_kv4_kernel(const 
       if (warp >= Sh::kOuts) w.template write<true>(sm_out + (warp - Sh::kOuts) * G * D, sm_m, mine);
       kv4_consumers_sync();
     }
-    const bool whole = n == s.tiles;
+    const int b = piece->b, head = piece->head, hq0 = head * G, tiles = piece->s.tiles;
+    const long long lane_no = (long long)b * H + head;
+    const bool whole = n == tiles;
     constexpr int kVecs = G * D / 4;                       // float4s of a lane's output
     auto warps_sum = [&](int e) {
       float4 x = reinterpret_cast<const float4*>(sm_out)[e];
@@ -677,15 +709,15 @@ __global__ void __launch_bounds__(kKv4Threads, 2) paged_decode_kv4_kernel(const 
       __threadfence();
       kv4_consumers_sync();
       // pieces of the lane: its tiles lie at [off, off + tiles) of the deal
-      const long long off = (long long)cum[b] * H + (long long)head * s.tiles;
-      const int c0 = (int)(off / chunk), pieces = (int)((off + s.tiles - 1) / chunk) - c0 + 1;
+      const long long off = (long long)cum[b] * H + (long long)head * tiles, chunk = piece->chunk;
+      const int c0 = (int)(off / chunk), pieces = (int)((off + tiles - 1) / chunk) - c0 + 1;
       if (tid == 0) {
         const bool last = atomicAdd(P.arrived + lane_no, 1u) == (uint32_t)pieces - 1;
         if (last) P.arrived[lane_no] = 0;
-        *sm_last = last;
+        piece->last = last;
       }
       kv4_consumers_sync();
-      if (*sm_last) {
+      if (piece->last) {
         __threadfence();
         const long long slot0 = c0 + lane_no;
         for (int e = tid; e < kVecs; e += kKv4Warps * 32) {
@@ -720,13 +752,16 @@ __global__ void __launch_bounds__(kKv4Threads, 2) paged_decode_kv4_kernel(const 
         }
       }
     }
-    kv4_consumers_sync();                                  // sm_* are free for the next piece
-    t += n;
-    if (first_v + n == s.tiles) {
-      v = 0;
-      if (++head == H && t < t1) {
-        head = 0;
-        s = span(lens[++b]);
+    kv4_consumers_sync();
+    if (tid == 0) {                                        // the next piece
+      piece->left -= n;
+      piece->v += n;
+      if (piece->v == tiles && piece->left > 0) {
+        piece->v = 0;
+        if (++piece->head == H) {
+          piece->head = 0;
+          do piece->s = span(lens[++piece->b]); while (piece->s.tiles == 0);
+        }
       }
     }
   }
