@@ -94,7 +94,9 @@ __device__ __forceinline__ float2 half_pair_f(uint32_t x) { return __half22float
 //   exchange among four lanes that leaves each with the logit of one entry.
 //   G >= 4: a column has a head's channels (G = 4: of the even or of the odd steps); every group of channels has an accumulator.  A lane
 //   has the logits of head j (and j + 4) and four entries.
-// Values: channels are rows, entries the inner dimension, and the columns of the weights are (group, head) pairs.  The zero points' part
+// Values: channels are rows, entries the inner dimension, and the columns of the weights are (group, head) pairs.  The products of a
+// fragment's groups share accumulators: each takes the weights of its own columns and zeros for the others (with accumulators of their
+// own, mostly of columns that nobody reads, a third of the registers went there).  The zero points' part
 // of the sum is one more product, of the zero points of the columns' groups with the weights.
 template <int D, int G>
 struct Kv4Warp {
@@ -108,7 +110,7 @@ struct Kv4Warp {
   static constexpr float kHeadroom = 14.f;                 // weights are held times 2^14: fp16 numbers down to 2^-28
   float qsum[kHeads][kMasked ? 1 : kGroups];   // sum of the quarter's, or a group's, channels
   float factor[kHeads];        // accumulator -> base-2 logit
-  float o[D / 16][4];          // values' products: tile (group, half): channels 4r + 2 half and + 1, columns 2j and 2j + 1
+  float o[kFrags][2][4];       // values' products: channels 4r + 2 half and + 1 of the column's group, columns 2j and 2j + 1
   float zo[kFrags][4];         // zero points' products: row r is the group of column r; rows 8 .. 15 are nothing
   float m[kHeads], l[kHeads];
   uint32_t largest;            // twice the bits of the largest value scale seen, which the weights' power of two follows
@@ -137,6 +139,8 @@ struct Kv4Warp {
   __device__ __forceinline__ static int group_of(int f, int n) {
     return (G == 1 ? n : G == 2 ? n >> 1 : G == 4 ? 2 * f + (n & 1) : f) % kGroups;
   }
+  // Is column n of the i-th group of its fragment?
+  __device__ __forceinline__ static bool of_group(int i, int n) { return G == 1 ? n % kGroups == i : G == 2 ? n >> 1 == i : G == 4 ? (n & 1) == i : true; }
   __device__ __forceinline__ static int head_of(int n) { return G == 1 ? 0 : G == 2 ? n & 1 : G == 4 ? n >> 1 : (n >> 1) + 4 * (n & 1); }
 
   __device__ __forceinline__ void begin(const __nv_bfloat16* qrow, float scale_log2, uint4* query, bool stores) {
@@ -190,7 +194,9 @@ struct Kv4Warp {
       l[u] = 0.f;
     }
 #pragma unroll
-    for (int n = 0; n < D / 16; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
+    for (int f = 0; f < kFrags; ++f)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[f][i / 4][i % 4] = 0.f;
 #pragma unroll
     for (int n = 0; n < kFrags; ++n) zo[n][0] = zo[n][1] = zo[n][2] = zo[n][3] = 0.f;
     largest = shift = 0;
@@ -364,17 +370,22 @@ struct Kv4Warp {
         const uint32_t lo = __byte_perm(w[0][g / 2], w[1][g / 2], g & 1 ? 0x7632 : 0x5410), hi = __byte_perm(w[2][g / 2], w[3][g / 2], g & 1 ? 0x7632 : 0x5410);
         const uint32_t lo8 = lo >> 8, hi8 = hi >> 8;
         const int f = g / kPer;
-        mma_m16n8k16_f16(o[2 * g], lo & 0x000f000fu, lo & 0x00f000f0u, hi & 0x000f000fu, hi & 0x00f000f0u, b[f][0], b[f][1]);
-        mma_m16n8k16_f16(o[2 * g + 1], lo8 & 0x000f000fu, lo8 & 0x00f000f0u, hi8 & 0x000f000fu, hi8 & 0x00f000f0u, b[f][0], b[f][1]);
+        const bool mine = of_group(g % kPer, r);
+        const uint32_t b0 = mine ? b[f][0] : 0u, b1 = mine ? b[f][1] : 0u;
+        mma_m16n8k16_f16(o[f][0], lo & 0x000f000fu, lo & 0x00f000f0u, hi & 0x000f000fu, hi & 0x00f000f0u, b0, b1);
+        mma_m16n8k16_f16(o[f][1], lo8 & 0x000f000fu, lo8 & 0x00f000f0u, hi8 & 0x000f000fu, hi8 & 0x00f000f0u, b0, b1);
       }
     }
   }
 
   __device__ __forceinline__ void scale_sums(float f0, float f1) {         // of columns 2j and 2j + 1
 #pragma unroll
-    for (int n = 0; n < D / 16; ++n) { o[n][0] *= f0; o[n][1] *= f1; o[n][2] *= f0; o[n][3] *= f1; }
+    for (int f = 0; f < kFrags; ++f) {
 #pragma unroll
-    for (int n = 0; n < kFrags; ++n) { zo[n][0] *= f0; zo[n][1] *= f1; }
+      for (int i = 0; i < 8; ++i) o[f][i / 4][i % 4] *= i & 1 ? f1 : f0;
+      zo[f][0] *= f0;
+      zo[f][1] *= f1;
+    }
   }
   // A larger logit than any before: sums so far follow.
   template <int K>
@@ -432,16 +443,12 @@ struct Kv4Warp {
       const float mm = m[kHeads == 2 ? c : 0], f = mm == -INFINITY ? 0.f : exp2_fast(mm - big[head]) * back;
 #pragma unroll
       for (int f8 = 0; f8 < kFrags; ++f8) {
-        float a[4] = {};
-#pragma unroll
-        for (int i = 0; i < kPer; ++i)                     // by selection: registers have no indexes
-#pragma unroll
-          for (int h = 0; h < 4; ++h) a[h] = i == which ? o[2 * (f8 * kPer + i) + h / 2][c + h % 2 * 2] : a[h];
         if (which >= kPer) continue;
         const int g = f8 * kPer + which;
         const float z = zeros[g * G + head];
         float4* to = reinterpret_cast<float4*>(out + head * D + g * 32 + 4 * r);
-        float4 y = make_float4((a[0] - z) * f, (a[1] * 0x1p-4f - z) * f, (a[2] - z) * f, (a[3] * 0x1p-4f - z) * f);
+        const float (&a)[2][4] = o[f8];
+        float4 y = make_float4((a[0][c] - z) * f, (a[0][2 + c] * 0x1p-4f - z) * f, (a[1][c] - z) * f, (a[1][2 + c] * 0x1p-4f - z) * f);
         if constexpr (ADD) {
           const float4 was = *to;
           y.x += was.x; y.y += was.y; y.z += was.z; y.w += was.w;
