@@ -31,14 +31,17 @@ struct Kv4Shape {
   using Row = Kv4Row<D>;
   static constexpr int kHalf = kKv4Tile * Row::kBytes;    // keys of a tile; values
   static constexpr int kStage = 2 * kHalf;
-  static constexpr int kStages = 72 * 1024 / kStage;      // 4 or 8
-  static constexpr int kOuts = G == 8 ? kKv4Warps / 2 : kKv4Warps;      // outputs side by side in the join: the warps', or of pairs of them
+  static constexpr int kOuts = G >= 4 ? kKv4Warps / 2 : kKv4Warps;      // outputs side by side in the join: the warps', or of pairs of them
   static constexpr int kOut = kOuts * G * D * 4;
   static constexpr int kScratch = kKv4Warps * 16 * G * 4; // a warp's weights, then zero points' sums
   static constexpr int kQuery = D / 32 * 512;             // Kv4Warp::kQuery
-  static constexpr int kSmem = kStages * kStage + kOut + kScratch + kQuery + 2 * kKv4Warps * 8 * 4 + (2 * kMaxSequences + 8) * 4 + 2 * kStages * 8 +
-                               kStages * kKv4MaxSlots * 4 + 64;
-  static_assert((kStages & (kStages - 1)) == 0, "stages by masks");
+  static constexpr int kOther = kOut + kScratch + kQuery + 2 * kKv4Warps * 8 * 4 + (2 * kMaxSequences + 8) * 4 + 64;
+  // Two CTAs an SM; a stage's slot entries and barriers beside it.  An even number: a stage then belongs to one team of warps, which cannot
+  // be more than one of its barrier's phases ahead (with an odd one the teams take turns on it, and a wait that looks at the
+  // phase's parity could be let through by the phase before the other team's).
+  static constexpr int kStages = (113 * 1024 - kOther) / (kStage + kKv4MaxSlots * 4 + 16) / 2 * 2;
+  static_assert(kKv4Warps == 2 * kKv4TileWarps && kStages >= 2, "two teams");
+  static constexpr int kSmem = kStages * (kStage + kKv4MaxSlots * 4 + 16) + kOther;
 };
 
 __device__ __forceinline__ void mma_m16n8k16_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -567,7 +570,8 @@ __global__ void __launch_bounds__(kKv4Threads, 2) paged_decode_kv4_kernel(const 
   if (warp == kKv4Warps) {                                 // ---- producer
     const uint64_t policy = l2_policy_evict_first();
     fence_proxy_async();                                   // rows that earlier kernels stored are read by the copies
-    int it = 0;
+    int st = 0;
+    uint32_t round = 0;                                    // how often the ring was filled
     for (int left = (int)(t1 - t0); left > 0;) {
       const int n = min(s.tiles - v, left);
       const int per = 32 >> slot_shift;                    // tiles whose pages are looked up together
@@ -589,11 +593,10 @@ __global__ void __launch_bounds__(kKv4Threads, 2) paged_decode_kv4_kernel(const 
             }
           }
         }
-        for (int k = k0; k < min(n, k0 + per); ++k, ++it) {
-          const int st = it % STAGES;
+        for (int k = k0; k < min(n, k0 + per); ++k) {
           const int mine = (k - k0) << slot_shift | (lane & (slots - 1));
           const int e = __shfl_sync(~0u, entry, mine), pg = __shfl_sync(~0u, page_no, mine);
-          if (it >= STAGES && !wait(&empty[st], ((it / STAGES) & 1) ^ 1)) return;
+          if (round > 0 && !wait(&empty[st], (round & 1) ^ 1)) return;
           const bool copies = lane < 2 * slots && pg >= 0;
           const uint32_t bytes = __popc(__ballot_sync(~0u, copies)) * chunk_bytes;
           if (lane < slots) slot_entry[st * kKv4MaxSlots + lane] = e;
@@ -606,6 +609,7 @@ __global__ void __launch_bounds__(kKv4Threads, 2) paged_decode_kv4_kernel(const 
             const unsigned char* src = static_cast<const unsigned char*>(is_v ? A.v_pool : A.k_pool) + ((long long)pg * H + head) * chunk_bytes;
             bulk_g2s_hint(ring + st * Sh::kStage + (is_v ? Sh::kHalf : 0) + (lane & (slots - 1)) * chunk_bytes, src, chunk_bytes, &full[st], policy);
           }
+          if (++st == STAGES) { st = 0; ++round; }
         }
       }
       left -= n;
@@ -624,11 +628,12 @@ __global__ void __launch_bounds__(kKv4Threads, 2) paged_decode_kv4_kernel(const 
   // ---- consumers
   Warp w;
   bool ok = true;          // else a wait gave up: this warp keeps the others' barriers company, and counts its pieces, but reads no more tiles
-  int it = 0;
   float* mine = scratch + warp * 16 * G;
   const int team = warp / kKv4TileWarps, row = warp % kKv4TileWarps * kKv4Share;       // the tiles, and rows of a tile, that are this warp's
   const typename Warp::Offsets at = Warp::offsets(A.page, A.page_shift, row, Sh::kHalf);
   const int first = row & (A.page - 1), second = A.page == 16 ? 0 : first + 16;        // of the halves' pages
+  int st = team, skip = team;                              // stage and parity of this warp's next tile; tiles of a piece before it
+  uint32_t phase = 0;
   const uint32_t ring0 = smem_u32(ring), entry0 = smem_u32(slot_entry + (row >> A.page_shift)), entry1 = entry0 + (A.page == 16 ? 4 : 0);
   for (;;) {
     kv4_consumers_sync();                                  // the piece is there, sm_* are free
@@ -638,12 +643,15 @@ __global__ void __launch_bounds__(kKv4Threads, 2) paged_decode_kv4_kernel(const 
     kv4_consumers_sync();
     const int lo = piece->s.lo;
     const unsigned fit = (unsigned)max(0, piece->s.len - 15 - lo);       // places for 16 entries, all of them seen, from lo on
-    for (int k = (it ^ team) & 1; k < n; k += 2) {
-      const int st = (it + k) & (STAGES - 1);
-      ok = ok && wait(&full[st], ((it + k) / STAGES) & 1);
+    int k = skip;
+    for (; k < n; k += 2) {
+      const int at_stage = st;
+      ok = ok && wait(&full[at_stage], phase);
+      st += 2;
+      if (st >= STAGES) { st -= STAGES; phase ^= 1; }
       if (!ok) continue;
-      const int e0 = (int)lds32(entry0 + st * (kKv4MaxSlots * 4)), e1 = (int)lds32(entry1 + st * (kKv4MaxSlots * 4));
-      const uint32_t stage = ring0 + st * Sh::kStage;
+      const int e0 = (int)lds32(entry0 + at_stage * (kKv4MaxSlots * 4)), e1 = (int)lds32(entry1 + at_stage * (kKv4MaxSlots * 4));
+      const uint32_t stage = ring0 + at_stage * Sh::kStage;
       if ((unsigned)(e0 + first - lo) < fit && (unsigned)(e1 + second - lo) < fit) {
         w.template tile<true>(stage, at, 0, 0, DecodeSpan(), smem_u32(mine), smem_u32(query));
       } else {
@@ -653,9 +661,9 @@ __global__ void __launch_bounds__(kKv4Threads, 2) paged_decode_kv4_kernel(const 
         auto any = [&](int e) { const int i = e < 0 ? ~e : e; return i < s.len && (i + 16 > s.lo || i < s.sinks); };
         if (any(i0) || any(i1)) w.template tile<false>(stage, at, i0, i1, s, smem_u32(mine), smem_u32(query));
       }
-      release_stage(&empty[st]);
+      release_stage(&empty[at_stage]);
     }
-    it += n;
+    skip = k - n;
     // join the eight warps
     w.stats(sm_m + warp * 8, sm_l + warp * 8);
     kv4_consumers_sync();
