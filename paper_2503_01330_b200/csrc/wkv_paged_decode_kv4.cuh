@@ -3,14 +3,17 @@
 //   o = sum_i p_i v_i,  p = softmax(scale q.k_i),  k_i = s_ig (n - z_ig) per group g of 32 channels, v_i likewise
 //
 // Bound: HBM at 4.5 bits a number; instruction issue close behind it, since a number may cost no more than about three lane instructions.
-// Codes are never converted: a masked word is two fp16 subnormals n 2^-24 (or n 2^-20), which mma.sync m16n8k16 takes exactly.  (As e4m3
-// numbers four codes come out of a mask, but the matrix instruction on them is split into fp16 ones with conversions: 196 -> 211 us.)
-// Scales and zero points stay outside of the products:
+// Codes are never converted.  Keys: a masked word is four bytes for mma.sync m16n8k32 on integers, against queries of 16 bits in two columns
+// of eight; exact, until a group's product becomes fp32.  Values: a masked word is two fp16 subnormals n 2^-24 (or n 2^-20), which m16n8k16
+// takes exactly.  Scales and zero points stay outside of the products:
 //   q.k_i  = sum_g s_ig (q_g.n_ig - z_ig sum q_g)
 //   o_g    = sum_i (p_i s_ig) n_ig - sum_i (p_i s_ig) z_ig   the weights p s in fp16, the same rounded ones in both sums
-// p and p s are rounded to fp16, 2^-11 each, together a quarter of what rounding the output to bf16 costs.  The weights are kept in fp16's
-// range by a power of two that follows the largest value scale seen.  Queries become fp16 by a power of two per head (exact down to 2^-28 of
-// the head's largest channel).
+// A query's group of 32 channels (half of one for 64-channel heads with one or two heads a key) becomes whole numbers by a power of two that
+// brings its largest to [2^13, 2^14): bf16 channels down to 2^-6 of it stay exact, smaller ones are off by up to 2^-14 of it.  p and p s are
+// rounded to fp16, 2^-11 each, together a quarter of what rounding the output to bf16 costs.  The weights are kept in fp16's range
+// by a power of two that follows the largest value scale seen.
+// (Keys as fp16 subnormals: 163 us of arithmetic in the 16 x 8192..16384 case, masks at half rate above all.  As e4m3 numbers the matrix
+// instruction is split into fp16 ones with conversions.)
 //
 // The deal of tiles to CTAs, pieces of a lane and their join are those of the bf16 rows' kernel.  A CTA: one producer warp, which looks up 32
 // pages at a time and copies their chunks into a ring (cp.async.bulk), and eight consumer warps, four for a tile of 128 entries.
@@ -34,7 +37,7 @@ struct Kv4Shape {
   static constexpr int kOuts = G >= 4 ? kKv4Warps / 2 : kKv4Warps;      // outputs side by side in the join: the warps', or of pairs of them
   static constexpr int kOut = kOuts * G * D * 4;
   static constexpr int kScratch = kKv4Warps * 16 * G * 4; // a warp's weights, then zero points' sums
-  static constexpr int kQuery = D / 32 * 512;             // Kv4Warp::kQuery
+  static constexpr int kQuery = (G == 2 || G == 8 ? 2 : 1) * D / 64 * 512;      // Kv4Warp::kQuery
   static constexpr int kOther = kOut + kScratch + kQuery + 2 * kKv4Warps * 8 * 4 + (2 * kMaxSequences + 8) * 4 + 64;
   // Two CTAs an SM; a stage's slot entries and barriers beside it.  An even number: a stage then belongs to one team of warps, which cannot
   // be more than one of its barrier's phases ahead (with an odd one the teams take turns on it, and a wait that looks at the
@@ -48,6 +51,11 @@ __device__ __forceinline__ void mma_m16n8k16_f16(float (&d)[4], uint32_t a0, uin
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_m16n8k32_u8s8(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ float pow2f(int e) { return __int_as_float((e + 127) << 23); }       // -126 <= e <= 127
 __device__ __forceinline__ uint32_t half_pair(float lo, float hi) {
@@ -91,12 +99,12 @@ __device__ __forceinline__ float2 half_pair_f(uint32_t x) { return __half22float
 
 // A consumer warp's share of a piece: 32 entries of a tile at a time.  Lane 4 r + j.
 //
-// Keys: entries are rows of the product.
-//   G <= 2: a column has a quarter of a head's channels (one head: of the even or of the odd steps), with zeros elsewhere, so that a lane
-//   gets the products of quarter j alone and applies that quarter's scale and zero point only.  Sums over the quarters by an
-//   exchange among four lanes that leaves each with the logit of one entry.
-//   G >= 4: a column has a head's channels (G = 4: of the even or of the odd steps); every group of channels has an accumulator.  A lane
-//   has the logits of head j (and j + 4) and four entries.
+// Keys: entries are rows of the product, and two columns the high and low bytes of a query.
+//   G <= 2: a head's eight columns have a quarter of its channels each, zeros elsewhere, so that a lane gets the products of quarter j alone
+//   and applies that quarter's scale and zero point only.  Sums over the quarters by an exchange among four lanes that leaves each with
+//   the logit of one entry.
+//   G >= 4: eight columns are four heads; every group of channels has an accumulator.  A lane has the logits of head j (and j + 4) and
+//   four entries.
 // Values: channels are rows, entries the inner dimension, and the columns of the weights are (group, head) pairs.  The products of a
 // fragment's groups share accumulators: each takes the weights of its own columns and zeros for the others (with accumulators of their
 // own, mostly of columns that nobody reads, a third of the registers went there).  The zero points' part
@@ -105,14 +113,14 @@ template <int D, int G>
 struct Kv4Warp {
   using Row = Kv4Row<D>;
   static constexpr bool kMasked = G <= 2;
-  static constexpr int kSteps = D / 16, kGroups = Row::kGroups, kHeads = kMasked ? G : G / 4;       // heads of a lane's statistics: all; j and j + 4
+  static constexpr int kGroups = Row::kGroups, kHeads = kMasked ? G : G / 4;       // heads of a lane's statistics: all; j and j + 4
   static constexpr int kFrags = G * kGroups > 8 ? G * kGroups / 8 : 1, kPer = kGroups / kFrags;   // fragments of weights; groups of one
-  // The keys' products' B operands (a step: 16 channels, 4 of each lane's) are in shared memory, one copy for all warps, two steps to a
+  // The keys' products' B operands (a step: 32 channels, 8 of each lane's) are in shared memory, one copy for all warps, two steps to a
   // lane's 16 bytes: they would take a sixth of the registers.
-  static constexpr int kQuery = kSteps / 2 * 32 * 16;      // bytes
+  static constexpr int kQuery = kHeads * kGroups / 2 * 32 * 16;          // bytes
   static constexpr float kHeadroom = 14.f;                 // weights are held times 2^14: fp16 numbers down to 2^-28
-  float qsum[kHeads][kMasked ? 1 : kGroups];   // sum of the quarter's, or a group's, channels
-  float factor[kHeads];        // accumulator -> base-2 logit
+  int qsum[kHeads][kMasked ? 1 : kGroups];     // sum of the quarter's, or a group's, channels
+  float factor[kHeads][kMasked ? 1 : kGroups]; // whole numbers -> base-2 logits
   float o[kFrags][2][4];       // values' products: channels 4r + 2 half and + 1 of the column's group, columns 2j and 2j + 1
   float zo[kFrags][4];         // zero points' products: row r is the group of column r; rows 8 .. 15 are nothing
   float m[kHeads], l[kHeads];
@@ -148,51 +156,61 @@ struct Kv4Warp {
 
   __device__ __forceinline__ void begin(const __nv_bfloat16* qrow, float scale_log2, uint4* query, bool stores) {
     const int lane = threadIdx.x & 31, r = lane >> 2, j = lane & 3;
-    // the head of column r, and of its channels those that meet this lane's codes
-    const __nv_bfloat16* mine = qrow + (kMasked ? (G == 2 ? r & 1 : 0) : head_of(r)) * D + (kMasked ? j * (D / 4) : 8 * j);
-    float x[kSteps][4], most = 0.f;
-#pragma unroll
-    for (int t = 0; t < kSteps; t += 2) {
-      const uint4 y = *reinterpret_cast<const uint4*>(mine + (kMasked ? 4 : 16) * t);
-      const uint32_t w[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) { x[t + i / 2][i % 2 * 2] = __uint_as_float(w[i] << 16); x[t + i / 2][i % 2 * 2 + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-    }
-#pragma unroll
-    for (int t = 0; t < kSteps; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(x[t][i]));
-    most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
-    most = fmaxf(most, __shfl_xor_sync(~0u, most, 2));
-    // the head's largest channel comes to [2^14, 2^15)
-    const int e = max(-100, min(100, 14 - ((int)(__float_as_uint(most) >> 23) - 127)));
-    const float up = pow2f(e), f = scale_log2 * pow2f(-e) * 0x1p24f;
     const bool here = !kMasked || r >> 1 == j;             // does column r hold the lane's quarter?
-    float sum = 0.f;
-    uint32_t q[2][2];
-#pragma unroll
-    for (int t = 0; t < kSteps; ++t) {
-      if (!kMasked && t % 2 == 0) sum = 0.f;
-      uint32_t (&w)[2] = q[t & 1];
-      w[0] = half_pair(x[t][0] * up, x[t][1] * up);
-      const uint32_t odd = half_pair(x[t][2] * up, x[t][3] * up);
-      const float2 a = half_pair_f(w[0]), b = half_pair_f(odd);
-      sum += (a.x + a.y) + (b.x + b.y);
-      w[1] = half_pair(b.x * 0.0625f, b.y * 0.0625f);     // meets codes in bits 4..7
-      if (!here || (kHeads == 1 && (r & 1) != (t & 1))) w[0] = w[1] = 0u;
-      if (t % 2 == 1 && stores) query[t / 2 * 32 + lane] = make_uint4(q[0][0], q[0][1], q[1][0], q[1][1]);
-      if (!kMasked && t % 2 == 1) {
-        sum += __shfl_xor_sync(~0u, sum, 1);
-        sum += __shfl_xor_sync(~0u, sum, 2);
-#pragma unroll
-        for (int u = 0; u < kHeads; ++u) qsum[u][kMasked ? 0 : t / 2] = __shfl_sync(~0u, sum, 8 * j + 4 * u);
-      }
-    }
 #pragma unroll
     for (int u = 0; u < kHeads; ++u) {
-      // (column u is head u where all lanes have the quarter's sum of their column's head)
-      if (kMasked) qsum[u][0] = __shfl_sync(~0u, sum, 4 * u + j);
-      factor[u] = __shfl_sync(~0u, f, kMasked ? 4 * u : 8 * j + 4 * u);
+      // the head of column r of tile u, and of its channels those that meet this lane's codes
+      const __nv_bfloat16* mine = qrow + (kMasked ? u : 4 * u + (r >> 1)) * D + (kMasked ? j * (D / 4) : 8 * j);
+      float x[kGroups][8], most[kGroups];
+#pragma unroll
+      for (int t = 0; t < kGroups; ++t) {
+        const uint4 y = *reinterpret_cast<const uint4*>(mine + (kMasked ? 8 : 32) * t);
+        const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+        most[t] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { x[t][2 * i] = __uint_as_float(w[i] << 16); x[t][2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most[t] = fmaxf(most[t], x[t][i] == x[t][i] ? fabsf(x[t][i]) : INFINITY);
+      }
+      int sum = 0;
+#pragma unroll
+      for (int t = 0; t < kGroups; ++t) {
+        float top = most[t];
+        if constexpr (kMasked) {
+#pragma unroll
+          for (int k = 0; k < kGroups; ++k) top = fmaxf(top, most[k]);
+        } else {
+          top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
+          top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
+          sum = 0;
+        }
+        const int e = max(-100, min(100, 13 - ((int)(__float_as_uint(top) >> 23) - 127)));
+        const float up = pow2f(e), f = top < INFINITY ? scale_log2 * pow2f(-e) : __int_as_float(0x7fffffff);
+        // in the order of the codes' bytes: channels 0, 4, 1, 5 from the low halves of a word's bytes, 2, 6, 3, 7 from the high ones
+        constexpr int kAt[8] = {0, 4, 1, 5, 2, 6, 3, 7};
+        uint32_t word[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          word[h] = 0;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int y = __float2int_rn(x[t][kAt[4 * h + i]] * up), high = (y + 128) >> 8;
+            sum += y;
+            word[h] |= (uint32_t)((r & 1 ? y - high * 256 : high) & 255) << 8 * i;
+          }
+          if (!here) word[h] = 0;
+        }
+        if (stores) reinterpret_cast<uint2*>(query)[((u * kGroups + t) / 2 * 32 + lane) * 2 + (t & 1)] = make_uint2(word[0], word[1]);
+        if constexpr (!kMasked) {
+          sum += __shfl_xor_sync(~0u, sum, 1);
+          sum += __shfl_xor_sync(~0u, sum, 2);
+          qsum[u][t] = __shfl_sync(~0u, sum, 8 * j);
+          factor[u][t] = __shfl_sync(~0u, f, 8 * j);
+        } else {
+          factor[u][0] = f;
+        }
+      }
+      if constexpr (kMasked) qsum[u][0] = sum;
       m[u] = -INFINITY;
       l[u] = 0.f;
     }
@@ -205,17 +223,15 @@ struct Kv4Warp {
     largest = shift = 0;
   }
 
-  // Products of two steps: words a and b hold eight codes each of rows r and r + 8.
-  __device__ __forceinline__ static void two_steps(float (&d)[4], uint32_t a, uint32_t b, const uint4& q) {
-    const uint32_t a8 = a >> 8, b8 = b >> 8;
-    mma_m16n8k16_f16(d, a & 0x000f000fu, b & 0x000f000fu, a & 0x00f000f0u, b & 0x00f000f0u, q.x, q.y);
-    mma_m16n8k16_f16(d, a8 & 0x000f000fu, b8 & 0x000f000fu, a8 & 0x00f000f0u, b8 & 0x00f000f0u, q.z, q.w);
+  // A step's products: words a and b hold eight codes each of rows r and r + 8.
+  __device__ __forceinline__ static void step(int (&d)[4], uint32_t a, uint32_t b, uint32_t q0, uint32_t q1) {
+    constexpr uint32_t kLow = 0x0f0f0f0fu;
+    mma_m16n8k32_u8s8(d, a & kLow, b & kLow, a >> 4 & kLow, b >> 4 & kLow, q0, q1);
   }
-  // A head's product of row half h.
-  __device__ __forceinline__ static float product(const float (&d)[4], int h, int u) { return kHeads == 1 ? d[2 * h] + d[2 * h + 1] : d[2 * h + u]; }
-  // Scale, and zero point times 2^-24, of a pair.
-  __device__ __forceinline__ static float pair_scale(uint32_t pair) { return kv4_scale(pair & 255); }
-  __device__ __forceinline__ static float pair_zero(uint32_t pair) { return __half2float(__ushort_as_half((unsigned short)(pair >> 8 & 255))); }
+  // s (q.n - z sum q) of row half h, base-2 logits.
+  __device__ __forceinline__ static float part(const int (&d)[4], int h, uint32_t pair, int sum, float f) {
+    return kv4_scale(pair & 255) * f * (float)(d[2 * h] * 256 + d[2 * h + 1] - (int)(pair >> 8 & 255) * sum);
+  }
 
   // 32 entries of the stage at shared memory address `stage`, the halves' first ones entry[0] and entry[1]; ~entry: the page's number is
   // none, its entries count as zeros.  EVERY: all of them are seen (code for the others in the way cost a fifth of all instructions).
@@ -225,9 +241,14 @@ struct Kv4Warp {
     constexpr int kMine = kMasked ? 1 : 4;                 // logits per lane and head: entries of sub 0: r, r + 8; of sub 1
     constexpr int k8 = 8 * Row::kCodes, p8 = 8 * Row::kPairs;
     float x[kMine][kHeads];
-    uint4 q[kGroups];
+    uint32_t q[kHeads][kGroups][2];
 #pragma unroll
-    for (int t = 0; t < kGroups; ++t) q[t] = lds128(query + (t * 32 + lane) * 16);
+    for (int i = 0; i < kHeads * kGroups / 2; ++i) {
+      const uint4 y = lds128(query + (i * 32 + lane) * 16);
+      uint32_t (&to)[kGroups][2] = q[2 * i / kGroups];
+      to[2 * i % kGroups][0] = y.x; to[2 * i % kGroups][1] = y.y;
+      to[2 * i % kGroups + 1][0] = y.z; to[2 * i % kGroups + 1][1] = y.w;
+    }
     if constexpr (kMasked) {
       float v[4][G];
 #pragma unroll
@@ -243,15 +264,14 @@ struct Kv4Warp {
           a[0] = y.x; a[1] = y.y;
           b[0] = w.x; b[1] = w.y;
         }
-        float d[4] = {};
+        const uint32_t pair0 = lds16(tp), pair1 = lds16(tp + p8);
 #pragma unroll
-        for (int t = 0; t < kGroups; ++t) two_steps(d, a[t], b[t], q[t]);
+        for (int u = 0; u < G; ++u) {
+          int d[4] = {};
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t pair = lds16(tp + h * p8);
-          const float sc = pair_scale(pair), z = pair_zero(pair);
-#pragma unroll
-          for (int u = 0; u < G; ++u) v[2 * sub + h][u] = sc * fmaf(-z, qsum[u][0], product(d, h, u));
+          for (int t = 0; t < kGroups; ++t) step(d, a[t], b[t], q[u][t][0], q[u][t][1]);
+          v[2 * sub][u] = part(d, 0, pair0, qsum[u][0], factor[u][0]);
+          v[2 * sub + 1][u] = part(d, 1, pair1, qsum[u][0], factor[u][0]);
         }
       }
       // sums over the quarters: lane j keeps entry r + 8 (j % 2) of sub j / 2
@@ -282,15 +302,14 @@ struct Kv4Warp {
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
           const uint32_t piece = tk + (16 * g ^ swizzle);
-          float d[4] = {};
-          two_steps(d, lds32(piece), lds32(piece + k8), q[g]);
+          const uint32_t a = lds32(piece), b = lds32(piece + k8);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t pair = g & 1 ? pairs[h][g / 2] >> 16 : pairs[h][g / 2];
-            const float sc = pair_scale(pair), z = pair_zero(pair);
+          for (int u = 0; u < kHeads; ++u) {
+            int d[4] = {};
+            step(d, a, b, q[u][g][0], q[u][g][1]);
 #pragma unroll
-            for (int u = 0; u < kHeads; ++u)
-              x[2 * sub + h][u] = fmaf(sc, fmaf(-z, qsum[u][g], product(d, h, u)), x[2 * sub + h][u]);
+            for (int h = 0; h < 2; ++h)
+              x[2 * sub + h][u] += part(d, h, g & 1 ? pairs[h][g / 2] >> 16 : pairs[h][g / 2], qsum[u][g], factor[u][g]);
           }
         }
       }
@@ -300,7 +319,6 @@ struct Kv4Warp {
     for (int k = 0; k < kMine; ++k)
 #pragma unroll
       for (int c = 0; c < kHeads; ++c) {
-        x[k][c] *= factor[c];
         if constexpr (!EVERY) {
           const int e = (kMasked ? j >> 1 : k >> 1) ? entry1 : entry0, i = (e < 0 ? ~e : e) + r + 8 * (kMasked ? j & 1 : k & 1);
           x[k][c] = !s.sees(i) ? -INFINITY : e < 0 ? 0.f : x[k][c];
