@@ -229,8 +229,8 @@ struct Kv4Warp {
     mma_m16n8k32_u8s8(d, a & kLow, b & kLow, a >> 4 & kLow, b >> 4 & kLow, q0, q1);
   }
   // s (q.n - z sum q) of row half h, base-2 logits.
-  __device__ __forceinline__ static float part(const int (&d)[4], int h, uint32_t pair, int sum, float f) {
-    return kv4_scale(pair & 255) * f * (float)(d[2 * h] * 256 + d[2 * h + 1] - (int)(pair >> 8 & 255) * sum);
+  __device__ __forceinline__ static float part(const int (&d)[4], int h, float scale, uint32_t zero, int sum, float f) {
+    return scale * f * (float)(d[2 * h] * 256 + d[2 * h + 1] - (int)zero * sum);
   }
 
   // 32 entries of the stage at shared memory address `stage`, the halves' first ones entry[0] and entry[1]; ~entry: the page's number is
@@ -270,8 +270,8 @@ struct Kv4Warp {
           int d[4] = {};
 #pragma unroll
           for (int t = 0; t < kGroups; ++t) step(d, a[t], b[t], q[u][t][0], q[u][t][1]);
-          v[2 * sub][u] = part(d, 0, pair0, qsum[u][0], factor[u][0]);
-          v[2 * sub + 1][u] = part(d, 1, pair1, qsum[u][0], factor[u][0]);
+          v[2 * sub][u] = part(d, 0, kv4_scale(pair0 & 255), pair0 >> 8, qsum[u][0], factor[u][0]);
+          v[2 * sub + 1][u] = part(d, 1, kv4_scale(pair1 & 255), pair1 >> 8, qsum[u][0], factor[u][0]);
         }
       }
       // sums over the quarters: lane j keeps entry r + 8 (j % 2) of sub j / 2
@@ -287,6 +287,7 @@ struct Kv4Warp {
         const uint32_t tk = stage + at.kc + sub * at.next_c, tp = stage + at.kp + sub * at.next_p;
         const int swizzle = Row::k_piece(r, 0) - r * Row::kCodes;
         uint32_t pairs[2][kGroups / 2];
+        float2 scales[2][kGroups / 2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           if constexpr (kGroups == 4) {
@@ -296,6 +297,8 @@ struct Kv4Warp {
           } else {
             pairs[h][0] = lds32(tp + h * p8);
           }
+#pragma unroll
+          for (int i = 0; i < kGroups / 2; ++i) scales[h][i] = half_pair_f((pairs[h][i] & 0x00ff00ffu) << 7);
 #pragma unroll
           for (int u = 0; u < kHeads; ++u) x[2 * sub + h][u] = 0.f;
         }
@@ -309,7 +312,8 @@ struct Kv4Warp {
             step(d, a, b, q[u][g][0], q[u][g][1]);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-              x[2 * sub + h][u] += part(d, h, g & 1 ? pairs[h][g / 2] >> 16 : pairs[h][g / 2], qsum[u][g], factor[u][g]);
+              x[2 * sub + h][u] += part(d, h, g & 1 ? scales[h][g / 2].y : scales[h][g / 2].x, __byte_perm(pairs[h][g / 2], 0u, g & 1 ? 0x4443 : 0x4441),
+                                        qsum[u][g], factor[u][g]);
           }
         }
       }
@@ -391,8 +395,9 @@ struct Kv4Warp {
         const uint32_t lo = __byte_perm(w[0][g / 2], w[1][g / 2], g & 1 ? 0x7632 : 0x5410), hi = __byte_perm(w[2][g / 2], w[3][g / 2], g & 1 ? 0x7632 : 0x5410);
         const uint32_t lo8 = lo >> 8, hi8 = hi >> 8;
         const int f = g / kPer;
-        const bool mine = of_group(g % kPer, r);
-        const uint32_t b0 = mine ? b[f][0] : 0u, b1 = mine ? b[f][1] : 0u;
+        // (times 1 or 0: the other pipe has room)
+        const uint32_t mine = of_group(g % kPer, r) ? 0x3c003c00u : 0u, b0 = kPer > 1 ? half_mul(b[f][0], mine) : b[f][0],
+                       b1 = kPer > 1 ? half_mul(b[f][1], mine) : b[f][1];
         mma_m16n8k16_f16(o[f][0], lo & 0x000f000fu, lo & 0x00f000f0u, hi & 0x000f000fu, hi & 0x00f000f0u, b0, b1);
         mma_m16n8k16_f16(o[f][1], lo8 & 0x000f000fu, lo8 & 0x00f000f0u, hi8 & 0x000f000fu, hi8 & 0x00f000f0u, b0, b1);
       }
