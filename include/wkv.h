@@ -369,23 +369,18 @@ int wkv_paged_evict(wkv_paged* c, int32_t layer, int32_t batch, const int32_t* s
  * Such a handle takes wkv_paged_append, wkv_paged_decode (k and v, where given, are stored in 4 bits first, and the new token sees its
  * entry as stored), wkv_paged_select, wkv_paged_decode_pages and wkv_paged_expand; prompts run on bf16 rows (wkv_paged_expand). */
 
-/* Rotary position embedding: channels are turned in pairs by the angles of the token's position,
- * (a, b) -> (a cos - b sin, b cos + a sin), in binary32, each product rounded by itself. */
-typedef struct {
-  const float* table; /* device [rows, dim], 16-byte aligned: per position dim / 2 cosines, then dim / 2 sines           */
-  int32_t rows;       /* positions 0 .. rows - 1                                                                        */
-  int32_t dim;        /* channels that are turned, the first ones of a head: a multiple of 16, <= head_dim              */
-  int32_t paired;     /* 1: angle i turns channels 2i and 2i + 1;  0: channels i and i + dim / 2                        */
-} wkv_rope;
-
 /* Appends new entries, turned to their position on the way, and turns the queries that go with them; no attention.  Asynchronous.
  * What follows is a wkv_paged_decode or wkv_paged_prefill with k and v NULL.
  *   q [total_q, n_q_heads, head_dim], k, v [total_q, n_kv_heads, head_dim]: rows q_stride, kv_stride elements apart (0: packed),
  *        16-byte aligned;  q NULL: no queries;  k and v NULL: only the queries
  *   q_start device [batch + 1] int32: sequence b's tokens are rows q_start[b] .. q_start[b+1]-1 and become its last entries;
  *        NULL: one token per sequence, row b, total_q = batch.  seq_lens counts the new entries; 0 = padding
- *   rope NULL: nothing is turned.  positions device [total_q] int32, NULL: a token's position is its entry's index.  A position
- *        outside of the table leaves the row as it is, and wkv_paged_status reports WKV_ERR_STATE
+ *   rope device [rope_rows, rope_dim] fp32, 16-byte aligned: for every position rope_dim / 2 cosines, then as many sines; NULL: nothing is
+ *        turned.  The first rope_dim channels of a head (a multiple of 16, <= head_dim) are turned in pairs,
+ *        (a, b) -> (a cos - b sin, b cos + a sin), in binary32, each product rounded by itself; rope_paired = 1: angle i turns channels
+ *        2i and 2i + 1, 0: channels i and i + rope_dim / 2
+ *   positions device [total_q] int32, NULL: a token's position is its entry's index.  A position outside of the table leaves the row as
+ *        it is, and wkv_paged_status reports WKV_ERR_STATE
  *   q_out [total_q, n_q_heads, head_dim], rows q_out_stride elements apart (0: packed); may be q itself (same stride), and must
  *        not overlap the call's other arguments otherwise.  Rows of no sequence are left as they were
  *   page_bounds device [n_layers, n_pages, n_kv_heads, 2, head_dim] int8 and page_scale [n_layers, n_pages, n_kv_heads], or both
@@ -394,8 +389,8 @@ typedef struct {
  *        that another sequence shares must hold the same entries for both. */
 int wkv_paged_append(wkv_paged* c, int32_t layer, int32_t batch, const void* q, int64_t q_stride, const void* k, const void* v,
                      int64_t kv_stride, const int32_t* q_start, int32_t total_q, const int32_t* block_table, int32_t table_width,
-                     const int32_t* seq_lens, const wkv_rope* rope, const int32_t* positions, void* q_out, int64_t q_out_stride,
-                     int8_t* page_bounds, float* page_scale);
+                     const int32_t* seq_lens, const float* rope, int32_t rope_rows, int32_t rope_dim, int32_t rope_paired,
+                     const int32_t* positions, void* q_out, int64_t q_out_stride, int8_t* page_bounds, float* page_scale);
 
 /* Chooses the pages that a decode step's query attends to, for every (sequence, kv head) by itself: the first `sink` and the newest
  * `recent` pages, then those with the best scores, of equal scores the lowest page.  Asynchronous.  A page's score is page_scale

@@ -36,10 +36,6 @@ class wkv_paged_config(C.Structure):
                 ("user", C.c_void_p)]
 
 
-class wkv_rope(C.Structure):
-    _fields_ = [("table", C.c_void_p), ("rows", C.c_int32), ("dim", C.c_int32), ("paired", C.c_int32)]
-
-
 EXPORTS = ["wkv_config_error", "wkv_create", "wkv_destroy", "wkv_reset", "wkv_set_stream", "wkv_decode_step",
            "wkv_decode_step_layers", "wkv_decode_step_static", "wkv_decode_step_host", "wkv_decode_step_layers_host", "wkv_prefill", "wkv_prefill_bulk", "wkv_prefill_bulk_layers", "wkv_export_state", "wkv_export_slots", "wkv_import_state",
            "wkv_status", "wkv_selftest_wait_timeout", "wkv_launch_count", "wkv_device_bytes", "wkv_splits", "wkv_strerror", "wkv_last_error",
@@ -100,7 +96,7 @@ def lib():
         L.wkv_paged_decode.argtypes = [vp, i32, i32, vp, i64, vp, vp, i64, vp, i32, vp, i32, i32, vp, i64, vp, vp]
         L.wkv_paged_prefill.argtypes = [vp, i32, i32, vp, i64, vp, vp, i64, vp, i32, vp, i32, vp, i32, i32, vp, i64, vp, vp]
         L.wkv_paged_evict.argtypes = [vp, i32, i32, vp, i32, vp, i32, vp, vp, i32, i32, i32, vp, i64, vp, i64, vp]
-        L.wkv_paged_append.argtypes = [vp, i32, i32, vp, i64, vp, vp, i64, vp, i32, vp, i32, vp, vp, vp, vp, i64, vp, vp]
+        L.wkv_paged_append.argtypes = [vp, i32, i32, vp, i64, vp, vp, i64, vp, i32, vp, i32, vp, vp, i32, i32, i32, vp, vp, i64, vp, vp]
         L.wkv_paged_select.argtypes = [vp, i32, i32, vp, i64, vp, i32, vp, vp, vp, i32, i32, i32, vp, i64, vp]
         L.wkv_paged_decode_pages.argtypes = [vp, i32, i32, vp, i64, vp, i32, vp, vp, i32, vp, vp]
         L.wkv_paged_expand.argtypes = [vp, i32, i32, vp, i32, vp, vp, i32, vp, i32]
@@ -459,34 +455,57 @@ class PagedCache:
             self._packed("seq_lens", seq_lens, torch.int32, B), self._packed("new_lens", new_lens, torch.int32, B), budget,
             recent, sink, sp, ss, op, os_, self._packed("kept", kept, torch.int32, B, self.n_kv_heads, budget)))
 
+    # The checks of the calls of a decode loop, as short as they can be.
+    def _exact(self, name, t, dtype, shape):
+        if t.dtype is dtype and t.shape == shape and t.get_device() == self._index and t.is_contiguous():
+            return t.data_ptr()
+        raise WkvError(WKV_ERR_INVALID, f"{name} must be a contiguous {dtype} tensor of shape {list(shape)} on {self.device}")
+
+    def _wide(self, name, t, dtype, shape):
+        """Address and last size of a packed tensor of shape [*shape, any]."""
+        got = t.shape
+        if t.dtype is dtype and got[:-1] == shape and t.get_device() == self._index and t.is_contiguous():
+            return t.data_ptr(), got[-1]
+        raise WkvError(WKV_ERR_INVALID, f"{name} must be a contiguous {dtype} tensor of shape {[*shape, 'any']} on {self.device}")
+
+    def _bounds(self, page_bounds, page_scale):
+        pages = self.shape[:3]
+        return (self._exact("page_bounds", page_bounds, torch.int8, (*pages, 2, self.head_dim)),
+                self._exact("page_scale", page_scale, torch.float32, pages))
+
     def wkv_paged_append(self, layer, q, k, v, block_table, seq_lens, q_start=None, rope=None, paired=False, positions=None, q_out=None,
                          page_bounds=None, page_scale=None):
         """q [T, Hq, d] or None, k, v [T, Hkv, d] or None; q_start [B + 1] int32, or None: row b is sequence b's only token.
         rope [rows, dim] float32: cosines, then sines, of every position's angles; q_out [T, Hq, d], q itself included;
         page_bounds [layers, pages, Hkv, 2, d] int8 and page_scale [layers, pages, Hkv] float32 are kept up to date."""
-        _need(q is not None or k is not None, "q or k and v must be given")
-        _need((q is None) == (q_out is None), "q and q_out must both be given or both be None")
-        B, T = block_table.shape[0], (k if q is None else q).shape[0]
-        qp, qs = self._rows("q", q, T, self.n_q_heads) if q is not None else (None, 0)
-        op, os_ = self._rows("q_out", q_out, T, self.n_q_heads) if q is not None else (None, 0)
-        kp, vp, ks = self._new_rows(k, v, T)
-        turn = None
+        rows, B = self._rows, block_table.shape[0]
+        qp = op = kp = vp = None
+        qs = os_ = ks = 0
+        if q is not None:
+            T = q.shape[0]
+            if q_out is None:
+                raise WkvError(WKV_ERR_INVALID, "q and q_out must both be given or both be None")
+            qp, qs = rows("q", q, T, self.n_q_heads)
+            op, os_ = (qp, qs) if q_out is q else rows("q_out", q_out, T, self.n_q_heads)
+        elif q_out is not None or k is None:
+            raise WkvError(WKV_ERR_INVALID, "q and q_out, or k and v, or all of them must be given")
+        else:
+            T = k.shape[0]
+        if k is not None or v is not None:
+            kp, vp, ks = self._new_rows(k, v, T)
+        tp, width = self._wide("block_table", block_table, torch.int32, (B,))
+        turn = None, 0, 0
         if rope is not None:
-            if rope.dim() != 2:
-                raise WkvError(WKV_ERR_INVALID, "rope must be [rows, dim]")
-            turn = wkv_rope(self._packed("rope", rope, torch.float32, rope.shape[0], -1), rope.shape[0], rope.shape[1], int(paired))
-            turn = C.byref(turn)
-        _need((page_bounds is None) == (page_scale is None), "page_bounds and page_scale must both be given or both be None")
-        self._check(self._lib.wkv_paged_append(
-            self._h, layer, B, qp, qs, kp, vp, ks, self._packed("q_start", q_start, torch.int32, B + 1), T,
-            self._packed("block_table", block_table, torch.int32, B, -1), block_table.shape[1],
-            self._packed("seq_lens", seq_lens, torch.int32, B), turn, self._packed("positions", positions, torch.int32, T), op, os_,
-            *self._bounds(page_bounds, page_scale)))
-
-    def _bounds(self, page_bounds, page_scale):
-        layers, pages, heads = self.shape[:3]
-        return (self._packed("page_bounds", page_bounds, torch.int8, layers, pages, heads, 2, self.head_dim),
-                self._packed("page_scale", page_scale, torch.float32, layers, pages, heads))
+            turn = *self._wide("rope", rope, torch.float32, (rope.shape[0],)), rope.shape[0]
+        if (page_bounds is None) != (page_scale is None):
+            raise WkvError(WKV_ERR_INVALID, "page_bounds and page_scale must both be given or both be None")
+        bp, sp = (None, None) if page_bounds is None else self._bounds(page_bounds, page_scale)
+        rc = self._lib.wkv_paged_append(
+            self._h, layer, B, qp, qs, kp, vp, ks, None if q_start is None else self._exact("q_start", q_start, torch.int32, (B + 1,)), T,
+            tp, width, self._exact("seq_lens", seq_lens, torch.int32, (B,)), turn[0], turn[2], turn[1], 1 if paired else 0,
+            None if positions is None else self._exact("positions", positions, torch.int32, (T,)), op, os_, bp, sp)
+        if rc:
+            self._check(rc)
 
     def wkv_paged_select(self, layer, q, block_table, seq_lens, page_bounds, page_scale, page_scores, pages, recent=1, sink=0):
         """q [B, Hq, d]; page_scores [B, Hkv, >= width] float32 and pages [B, Hkv, n_select] int32 are written: every page's score, and the
@@ -494,29 +513,37 @@ class PagedCache:
         B = q.shape[0]
         qp, qs = self._rows("q", q, B, self.n_q_heads)
         bp, sp = self._bounds(page_bounds, page_scale)
-        self._check(self._lib.wkv_paged_select(
-            self._h, layer, B, qp, qs, self._packed("block_table", block_table, torch.int32, B, -1), block_table.shape[1],
-            self._packed("seq_lens", seq_lens, torch.int32, B), bp, sp, pages.shape[-1], recent, sink,
-            *self._scores("page_scores", page_scores, B), self._packed("pages", pages, torch.int32, B, self.n_kv_heads, -1)))
+        lanes = (B, self.n_kv_heads)
+        tp, width = self._wide("block_table", block_table, torch.int32, (B,))
+        op, stride = self._wide("page_scores", page_scores, torch.float32, lanes)
+        pp, n_select = self._wide("pages", pages, torch.int32, lanes)
+        rc = self._lib.wkv_paged_select(self._h, layer, B, qp, qs, tp, width, self._exact("seq_lens", seq_lens, torch.int32, (B,)), bp, sp,
+                                        n_select, recent, sink, op, stride, pp)
+        if rc:
+            self._check(rc)
 
     def wkv_paged_decode_pages(self, layer, q, block_table, seq_lens, pages, out, lse=None):
         """q [B, Hq, d] attends to the entries of the pages [B, Hkv, n_select], places in the table row (-1: none)."""
-        B = q.shape[0]
-        qp, qs = self._rows("q", q, B, self.n_q_heads)
-        self._check(self._lib.wkv_paged_decode_pages(
-            self._h, layer, B, qp, qs, self._packed("block_table", block_table, torch.int32, B, -1), block_table.shape[1],
-            self._packed("seq_lens", seq_lens, torch.int32, B), self._packed("pages", pages, torch.int32, B, self.n_kv_heads, -1),
-            pages.shape[-1], self._packed("out", out, self.tdtype, B, self.n_q_heads, self.head_dim),
-            self._packed("lse", lse, torch.float32, B, self.n_q_heads)))
+        B, Hq = q.shape[0], self.n_q_heads
+        qp, qs = self._rows("q", q, B, Hq)
+        tp, width = self._wide("block_table", block_table, torch.int32, (B,))
+        pp, n_select = self._wide("pages", pages, torch.int32, (B, self.n_kv_heads))
+        rc = self._lib.wkv_paged_decode_pages(self._h, layer, B, qp, qs, tp, width, self._exact("seq_lens", seq_lens, torch.int32, (B,)), pp,
+                                              n_select, self._exact("out", out, self.tdtype, (B, Hq, self.head_dim)),
+                                              None if lse is None else self._exact("lse", lse, torch.float32, (B, Hq)))
+        if rc:
+            self._check(rc)
 
     def wkv_paged_expand(self, layer, block_table, seq_lens, dst, dst_layer, dst_table):
         """Rows in 4 bits to the pages `dst_table` [B, width] of `dst`, a PagedCache with bf16 rows."""
         B = block_table.shape[0]
         _need(isinstance(dst, PagedCache), "dst must be a PagedCache")
-        self._check(self._lib.wkv_paged_expand(
-            self._h, layer, B, self._packed("block_table", block_table, torch.int32, B, -1), block_table.shape[1],
-            self._packed("seq_lens", seq_lens, torch.int32, B), dst._h, dst_layer,
-            self._packed("dst_table", dst_table, torch.int32, B, -1), dst_table.shape[1]))
+        tp, width = self._wide("block_table", block_table, torch.int32, (B,))
+        to, to_width = self._wide("dst_table", dst_table, torch.int32, (B,))
+        rc = self._lib.wkv_paged_expand(self._h, layer, B, tp, width, self._exact("seq_lens", seq_lens, torch.int32, (B,)), dst._h, dst_layer,
+                                        to, to_width)
+        if rc:
+            self._check(rc)
 
     def wkv_status(self):
         return lib().wkv_paged_status(self._h)

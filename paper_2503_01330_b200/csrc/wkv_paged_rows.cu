@@ -64,8 +64,8 @@ extern "C" {
 
 int wkv_paged_append(wkv_paged* c, int32_t layer, int32_t batch, const void* q, int64_t q_stride, const void* k, const void* v,
                      int64_t kv_stride, const int32_t* q_start, int32_t total_q, const int32_t* block_table, int32_t table_width,
-                     const int32_t* seq_lens, const wkv_rope* rope, const int32_t* positions, void* q_out, int64_t q_out_stride,
-                     int8_t* page_bounds, float* page_scale) {
+                     const int32_t* seq_lens, const float* rope, int32_t rope_rows, int32_t rope_dim, int32_t rope_paired,
+                     const int32_t* positions, void* q_out, int64_t q_out_stride, int8_t* page_bounds, float* page_scale) {
   if (!c) return WKV_ERR_INVALID;
   DeviceGuard on(c->device);
   WKV_CUDA(c, on.err);
@@ -88,11 +88,11 @@ int wkv_paged_append(wkv_paged* c, int32_t layer, int32_t batch, const void* q, 
     P.A.q = q; P.A.q_stride = q_stride; P.q_out = q_out; P.q_out_stride = q_out_stride;
   }
   if (rope) {
-    if (!rope->table || !aligned16(rope->table)) return fail(c, WKV_ERR_INVALID, "rope->table must be 16-byte aligned device memory");
-    if (rope->rows < 1) return fail(c, WKV_ERR_INVALID, "rope->rows must be >= 1");
-    if (rope->dim < 16 || rope->dim > f.head_dim || rope->dim % 16) return fail(c, WKV_ERR_INVALID, "rope->dim must be a multiple of 16 in [16, head_dim]");
-    if (rope->paired != 0 && rope->paired != 1) return fail(c, WKV_ERR_INVALID, "rope->paired must be 0 or 1");
-    P.rope = rope->table; P.rope_rows = rope->rows; P.rope_dim = rope->dim; P.paired = rope->paired;
+    if (!aligned16(rope)) return fail(c, WKV_ERR_INVALID, "rope must be 16-byte aligned");
+    if (rope_rows < 1) return fail(c, WKV_ERR_INVALID, "rope_rows must be >= 1");
+    if (rope_dim < 16 || rope_dim > f.head_dim || rope_dim % 16) return fail(c, WKV_ERR_INVALID, "rope_dim must be a multiple of 16 in [16, head_dim]");
+    if (rope_paired != 0 && rope_paired != 1) return fail(c, WKV_ERR_INVALID, "rope_paired must be 0 or 1");
+    P.rope = rope; P.rope_rows = rope_rows; P.rope_dim = rope_dim; P.paired = rope_paired;
     P.positions = positions;
   }
   if ((page_bounds == nullptr) != (page_scale == nullptr)) return fail(c, WKV_ERR_INVALID, "page_bounds and page_scale must both be given or both be NULL");

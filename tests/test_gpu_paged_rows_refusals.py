@@ -31,19 +31,17 @@ def test_append(bf16):
     gb = torch.zeros(2, P.n_pages, 2, 2, 128, dtype=torch.int8, device="cuda")
     gs = torch.zeros(2, P.n_pages, 2, device="cuda")
     p, t, l = buf.data_ptr(), table.data_ptr(), n.data_ptr()
-    turn = lambda **k: C.byref(binding.wkv_rope(**{**dict(table=rope.data_ptr(), rows=40, dim=128, paired=0), **k}))
-    good = dict(layer=0, batch=3, q=p, q_stride=1024, k=p, v=p, kv_stride=1024, q_start=None, total=3, table=t, width=P.width, lens=l, rope=turn(),
-                pos=None, q_out=p, q_out_stride=1024, gb=gb.data_ptr(), gs=gs.data_ptr())
+    good = dict(layer=0, batch=3, q=p, q_stride=1024, k=p, v=p, kv_stride=1024, q_start=None, total=3, table=t, width=P.width, lens=l, rope=rope.data_ptr(),
+                rows=40, dim=128, paired=0, pos=None, q_out=p, q_out_stride=1024, gb=gb.data_ptr(), gs=gs.data_ptr())
     for text, change in (("layer", dict(layer=2)), ("layer", dict(layer=-1)), ("batch", dict(batch=4)), ("batch", dict(batch=-1)),
                          ("rows must", dict(total=-1)), ("one token per sequence", dict(total=2)), ("table_width", dict(width=0)),
                          ("table_width", dict(width=P.width + 1)), ("k and v", dict(k=None)), ("q and q_out", dict(q=None)),
                          ("q and q_out", dict(q_out=None)), ("block_table", dict(table=None)), ("seq_lens", dict(lens=None)),
                          ("smaller", dict(q_stride=256)), ("smaller", dict(kv_stride=128)), ("smaller", dict(q_out_stride=8)),
                          ("aligned", dict(q=p + 2)), ("aligned", dict(v=p + 8)), ("aligned", dict(q_out=p + 4)), ("aligned", dict(q_stride=1025)),
-                         ("aligned", dict(kv_stride=1026)), ("in place", dict(q_out_stride=2048)), ("rope->table", dict(rope=turn(table=None))),
-                         ("rope->table", dict(rope=turn(table=rope.data_ptr() + 4))), ("rope->rows", dict(rope=turn(rows=0))),
-                         ("rope->dim", dict(rope=turn(dim=0))), ("rope->dim", dict(rope=turn(dim=24))), ("rope->dim", dict(rope=turn(dim=144))),
-                         ("paired", dict(rope=turn(paired=2))), ("page_bounds", dict(gb=None)), ("page_bounds", dict(gs=None)),
+                         ("aligned", dict(kv_stride=1026)), ("in place", dict(q_out_stride=2048)), ("rope must", dict(rope=rope.data_ptr() + 4)),
+                         ("rope_rows", dict(rows=0)), ("rope_dim", dict(dim=0)), ("rope_dim", dict(dim=24)), ("rope_dim", dict(dim=144)),
+                         ("rope_paired", dict(paired=2)), ("page_bounds", dict(gb=None)), ("page_bounds", dict(gs=None)),
                          ("page_bounds", dict(gb=gb.data_ptr() + 8)), ("page bounds need", dict(k=None, v=None)),
                          ("2^24", dict(q_start=l, total=(1 << 24) + 1))):
         refused(c, text, "wkv_paged_append", *{**good, **change}.values())

@@ -38,7 +38,7 @@ def test_merged_cache_takes_no_4_bit_rows(lib):
 
 def test_null_handles(lib):
     N = NULL
-    assert lib.wkv_paged_append(N, 0, 1, N, 0, N, N, 0, N, 1, N, 1, N, N, N, N, 0, N, N) == binding.WKV_ERR_INVALID
+    assert lib.wkv_paged_append(N, 0, 1, N, 0, N, N, 0, N, 1, N, 1, N, N, 0, 0, 0, N, N, 0, N, N) == binding.WKV_ERR_INVALID
     assert lib.wkv_paged_select(N, 0, 1, N, 0, N, 1, N, N, N, 1, 1, 0, N, 1, N) == binding.WKV_ERR_INVALID
     assert lib.wkv_paged_decode_pages(N, 0, 1, N, 0, N, 1, N, N, 1, N, N) == binding.WKV_ERR_INVALID
     assert lib.wkv_paged_expand(N, 0, 1, N, 1, N, N, 0, N, 1) == binding.WKV_ERR_INVALID
@@ -90,16 +90,15 @@ def test_append_hands_on(cache):
     cache.wkv_paged_append(1, paired=True, **a)
     name, c = cache._lib.calls[-1]
     assert name == "wkv_paged_append" and c[1:3] == (1, 3) and c[3] == a["q"].data_ptr() and c[9] == 6 and c[11] == 5
-    assert c[4] == 256 and c[7] == 128 and c[16] == 256 and c[17] == a["page_bounds"].data_ptr()
-    r = c[13]._obj
-    assert (r.table, r.rows, r.dim, r.paired) == (a["rope"].data_ptr(), 100, 32, 1)
+    assert c[4] == 256 and c[7] == 128 and c[19] == 256 and c[20] == a["page_bounds"].data_ptr()
+    assert c[13:17] == (a["rope"].data_ptr(), 100, 32, 1) and c[17] == a["positions"].data_ptr()
     wide = torch.zeros(3, 10, 64, dtype=torch.bfloat16)
     cache.wkv_paged_append(0, wide[:, :4], wide[:, 4:6], wide[:, 6:8], i32(3, 5), i32(3), q_out=wide[:, :4])
     c = cache._lib.calls[-1][1]
-    assert c[4] == c[7] == c[16] == 640 and c[8] is None and c[13] is None and c[17] is None and c[18] is None
+    assert c[4] == c[7] == c[19] == 640 and c[8] is None and c[13] is None and c[17] is None and c[20] is None and c[21] is None
     cache.wkv_paged_append(0, None, wide[:, 4:6], wide[:, 6:8], i32(3, 5), i32(3))
     c = cache._lib.calls[-1][1]
-    assert c[3] is None and c[15] is None
+    assert c[3] is None and c[18] is None
 
 
 def good_select(**change):
