@@ -264,7 +264,7 @@ int wkv_paged_create(const wkv_paged_config* cfg, wkv_paged** out) {
   if (four) e = pick_kv4(c);
   else if (cfg->dtype == WKV_BF16) e = wide ? pick_by_group<__nv_bfloat16, 128>(c) : pick_by_group<__nv_bfloat16, 64>(c);
   else e = wide ? pick_by_group<float, 128>(c) : pick_by_group<float, 64>(c);
-  if (e == cudaSuccess && !four) e = pick_pages(c);
+  if (e == cudaSuccess) e = four ? prepare_rows(c) : pick_pages(c);
   if (e != cudaSuccess) { delete c; return WKV_ERR_CUDA; }
   int rc = WKV_OK;
 #define WKV_TAKE(dst, bytes) do { if (rc == WKV_OK) rc = take(c, dst, bytes); } while (0)

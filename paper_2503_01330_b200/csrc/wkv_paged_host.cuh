@@ -163,7 +163,8 @@ inline int chunk0(const wkv_paged* c, const PagedParams& P) {
 cudaError_t pick_pages(wkv_paged* c);                       // wkv_paged_pages.cu: the kernel over chosen pages, bf16 and fp32 rows
 cudaError_t pick_kv4(wkv_paged* c);                         // wkv_paged_kv4.cu: the kernel on rows in 4 bits
 int decode_kv4(wkv_paged* c, const PagedParams& A, const int32_t* pages, int n_select);
-int append_rows(wkv_paged* c, const PagedParams& A);        // wkv_paged_rows.cu: k and v to their pages, nothing turned
+cudaError_t prepare_rows(wkv_paged* c);                     // wkv_paged_rows.cu: shared memory of its kernels
+int append_rows(wkv_paged* c, const PagedParams& A);        // ... k and v to their pages, nothing turned
 
 }  // namespace host
 }  // namespace wkv

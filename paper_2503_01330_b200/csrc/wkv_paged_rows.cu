@@ -47,6 +47,12 @@ int append(wkv_paged* c, AppendParams& P) {
 
 }  // namespace
 
+cudaError_t prepare_rows(wkv_paged* c) {
+  if (c->cfg.dtype != WKV_KV4) return cudaSuccess;
+  return c->cfg.head_dim == 128 ? cudaFuncSetAttribute(paged_rows_kernel<__nv_bfloat16, 128, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, rows_smem<__nv_bfloat16, 128, true>())
+                                : cudaFuncSetAttribute(paged_rows_kernel<__nv_bfloat16, 64, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, rows_smem<__nv_bfloat16, 64, true>());
+}
+
 int append_rows(wkv_paged* c, const PagedParams& A) {
   AppendParams P;
   std::memset(&P, 0, sizeof(P));

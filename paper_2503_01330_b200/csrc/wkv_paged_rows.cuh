@@ -171,45 +171,61 @@ __device__ __forceinline__ void turn_queries(const AppendParams& P, int block, i
   }
 }
 
-// ---- bounds of a page's n keys, key(row, channel) in shared memory
-template <int D, typename At>
-__device__ __forceinline__ void write_bounds(const AppendParams& P, At key, int n, float* work, long long chunk) {
-  // largest and least of every channel over a share of the rows, then over the shares
-  constexpr int kShares = kRowsThreads / D;
-  const int c = threadIdx.x % D, share = threadIdx.x / D;
-  float hi = -INFINITY, lo = INFINITY;
-  for (int r = share; r < n; r += kShares) {
-    const float x = key(r, c);
-    hi = fmaxf(hi, x);
-    lo = fminf(lo, x);
+// ---- bounds of the n keys of a page, for several heads at once: keys(head, row, pair of channels) from shared memory
+// Pairs of channels as they lie there, with the largest and the least of two of them.
+__device__ __forceinline__ __nv_bfloat162 pair_max(__nv_bfloat162 a, __nv_bfloat162 b) { return __hmax2(a, b); }
+__device__ __forceinline__ __nv_bfloat162 pair_min(__nv_bfloat162 a, __nv_bfloat162 b) { return __hmin2(a, b); }
+__device__ __forceinline__ float2 pair_floats(__nv_bfloat162 a) { return __bfloat1622float2(a); }
+__device__ __forceinline__ float2 pair_max(float2 a, float2 b) { return make_float2(fmaxf(a.x, b.x), fmaxf(a.y, b.y)); }
+__device__ __forceinline__ float2 pair_min(float2 a, float2 b) { return make_float2(fminf(a.x, b.x), fminf(a.y, b.y)); }
+__device__ __forceinline__ float2 pair_floats(float2 a) { return a; }
+template <typename T> struct PairOf { typedef __nv_bfloat162 type; };
+template <> struct PairOf<float> { typedef float2 type; };
+
+// work: [2][threads] pairs and [warps] floats.  heads: 1, 2 or 4, of which the first `valid` are written; heads * rows at most as many as one pass of the CTA takes.  A thread
+// owns a pair of channels of a head over a share of the rows; the shares meet in shared memory.  One barrier; the caller's next one
+// protects the keys and the work.
+template <typename T, int D, typename Keys>
+__device__ __forceinline__ void write_bounds(const AppendParams& P, Keys keys, int n, int heads, int valid, unsigned char* work, long long chunk) {
+  typedef typename PairOf<T>::type Pair;
+  constexpr int kPairs = D / 2;
+  Pair* his = reinterpret_cast<Pair*>(work);
+  Pair* los = his + kRowsThreads;
+  float* mosts = reinterpret_cast<float*>(los + kRowsThreads);
+  const int c = threadIdx.x % kPairs, of = threadIdx.x / kPairs, shares = kRowsThreads / kPairs / heads, head = of / shares, share = of % shares;
+  Pair hi = keys(head, min(share, n - 1), c), lo = hi;
+  for (int r = share + shares; r < n; r += shares) {
+    const Pair x = keys(head, r, c);
+    hi = pair_max(hi, x);
+    lo = pair_min(lo, x);
   }
-  work[threadIdx.x] = hi;
-  work[kRowsThreads + threadIdx.x] = lo;
-  __syncthreads();
-  float most = 0.f;
-  if (share == 0) {
+  his[threadIdx.x] = hi;
+  los[threadIdx.x] = lo;
+  float2 up = pair_floats(hi), down = pair_floats(lo);
+  float most = fmaxf(fmaxf(fabsf(up.x), fabsf(up.y)), fmaxf(fabsf(down.x), fabsf(down.y)));
 #pragma unroll
-    for (int k = 1; k < kShares; ++k) {
-      hi = fmaxf(hi, work[k * D + c]);
-      lo = fminf(lo, work[kRowsThreads + k * D + c]);
+  for (int off = 16; off; off >>= 1) most = fmaxf(most, __shfl_xor_sync(~0u, most, off));
+  if ((threadIdx.x & 31) == 0) mosts[threadIdx.x >> 5] = most;
+  __syncthreads();
+  if (share == 0 && head < valid) {
+    for (int k = 1; k < shares; ++k) {
+      hi = pair_max(hi, his[threadIdx.x + k * kPairs]);
+      lo = pair_min(lo, los[threadIdx.x + k * kPairs]);
     }
-    most = fmaxf(fabsf(hi), fabsf(lo));
-#pragma unroll
-    for (int off = 16; off; off >>= 1) most = fmaxf(most, __shfl_xor_sync(~0u, most, off));
-    if ((c & 31) == 0) work[2 * kRowsThreads + c / 32] = most;
-  }
-  __syncthreads();
-  if (share == 0) {
-#pragma unroll
-    for (int k = 0; k < D / 32; ++k) most = fmaxf(most, work[2 * kRowsThreads + k]);
+    const int warps = kRowsThreads / 32 / heads;           // of the head
+    most = 0.f;
+    for (int k = 0; k < warps; ++k) most = fmaxf(most, mosts[head * warps + k]);
     const float scale = __fmul_rn(most, 1.f / 127.f), inv = scale >= 0x1p-100f ? __frcp_rn(scale) : 0.f;
     // outwards; what is not finite ends at the border
-    const float up = fminf(fmaxf(ceilf(__fmul_rn(hi, inv)), -127.f), 127.f), down = fmaxf(fminf(floorf(__fmul_rn(lo, inv)), 127.f), -127.f);
-    P.bounds[chunk * 2 * D + c] = (int8_t)(int)up;
-    P.bounds[chunk * 2 * D + D + c] = (int8_t)(int)down;
-    if (c == 0) P.bound_scale[chunk] = scale;
+    up = pair_floats(hi);
+    down = pair_floats(lo);
+    auto above = [&](float x) { return (int)fminf(fmaxf(ceilf(__fmul_rn(x, inv)), -127.f), 127.f) & 255; };
+    auto below = [&](float x) { return (int)fmaxf(fminf(floorf(__fmul_rn(x, inv)), 127.f), -127.f) & 255; };
+    uint16_t* to = reinterpret_cast<uint16_t*>(P.bounds + (chunk + head) * 2 * D);
+    to[c] = (uint16_t)(above(up.x) | above(up.y) << 8);
+    to[kPairs + c] = (uint16_t)(below(down.x) | below(down.y) << 8);
+    if (c == 0) P.bound_scale[chunk + head] = scale;
   }
-  __syncthreads();
 }
 
 // ---- new entries in the storage type
@@ -218,7 +234,7 @@ struct RowsShape {
   static constexpr int kUnits = D / 16, kSlots = kRowsThreads / kUnits, kVec = 16 / (int)sizeof(T);
   static constexpr int kStride = D + kVec;
   static constexpr int kBounds = 64 * kStride * (int)sizeof(T);         // staged keys of a page
-  static constexpr int kWork = (2 * kRowsThreads + 8) * 4;
+  static constexpr int kWork = 2 * kRowsThreads * 2 * (int)sizeof(T) + 32;
 };
 // 4 bits: fp32 keys of a page, then the codes and pairs of its keys and values.  A group's 32 keys lie 36 floats behind the last one's:
 // the threads of a row's groups read them from different banks.
@@ -231,7 +247,7 @@ struct Rows4Shape {
 };
 template <typename T, int D, bool FOUR>
 constexpr int rows_smem() {
-  return FOUR ? Rows4Shape<D>::kKeys + 2 * Rows4Shape<D>::kImage + RowsShape<T, D>::kWork : RowsShape<T, D>::kBounds + RowsShape<T, D>::kWork;
+  return FOUR ? Rows4Shape<D>::kKeys + 2 * Rows4Shape<D>::kImage + RowsShape<float, D>::kWork : RowsShape<T, D>::kBounds + RowsShape<T, D>::kWork;
 }
 
 struct PagePart {
@@ -239,68 +255,89 @@ struct PagePart {
   int e0, n, old;              // index of the first new entry, number of new entries, entries of the page before them
 };
 
-// The (row, head) pairs k0, k0 + step, .. of a part, rows fastest; keys are staged too where `rows` is given (one head).
+// One row's unit of a head: read, turned and stored; keys are staged too where `rows` is given.
 template <typename T, int D>
-__device__ __forceinline__ void append_pairs(const AppendParams& P, const PagePart& w, int h0, int items, T* rows) {
-  using Sh = RowsShape<T, D>;
-  const PagedParams& A = P.A;
-  const int u = threadIdx.x % Sh::kUnits, slot = threadIdx.x / Sh::kUnits, i0 = w.e0 & (A.page - 1);
-  const int2 at = unit_pieces<D>(u, P.rope ? P.rope_dim : 0);
-  constexpr int kSteps = 2;                                // pairs in flight
-  for (int base = slot; base < items; base += kSteps * Sh::kSlots) {
-    Piece<T> ka[kSteps], kb[kSteps], va[kSteps], vb[kSteps];
-#pragma unroll
-    for (int j = 0; j < kSteps; ++j) {
-      const int k = base + j * Sh::kSlots;
-      if (k >= items) continue;
-      const long long src = (long long)(w.first + k % w.n) * A.kv_stride + (long long)(h0 + k / w.n) * D;
-      ka[j].load(static_cast<const T*>(A.k) + src + 8 * at.x);
-      kb[j].load(static_cast<const T*>(A.k) + src + 8 * at.y);
-      va[j].load(static_cast<const T*>(A.v) + src + 16 * u);
-      vb[j].load(static_cast<const T*>(A.v) + src + 16 * u + 8);
-    }
-#pragma unroll
-    for (int j = 0; j < kSteps; ++j) {
-      const int k = base + j * Sh::kSlots;
-      if (k >= items) continue;
-      const int r = k % w.n;
-      const long long dst = row_offset(A, w.page, h0 + k / w.n, i0 + r, D);
-      Row8 a = ka[j].row(), b = kb[j].row();
-      turn_unit(a, b, angles_of(P, w.first + r, w.e0 + r), u, P.rope_dim, P.paired);
-      store8(static_cast<T*>(A.k_pool) + dst + 8 * at.x, a);
-      store8(static_cast<T*>(A.k_pool) + dst + 8 * at.y, b);
-      va[j].store(static_cast<T*>(A.v_pool) + dst + 16 * u);
-      vb[j].store(static_cast<T*>(A.v_pool) + dst + 16 * u + 8);
-      if (rows) {
-        store8(rows + (w.old + r) * Sh::kStride + 8 * at.x, a);
-        store8(rows + (w.old + r) * Sh::kStride + 8 * at.y, b);
-      }
+struct RowUnit {
+  Piece<T> ka, kb, va, vb;
+  __device__ __forceinline__ void load(const PagedParams& A, long long src, int2 at, int u) {
+    ka.load(static_cast<const T*>(A.k) + src + 8 * at.x);
+    kb.load(static_cast<const T*>(A.k) + src + 8 * at.y);
+    va.load(static_cast<const T*>(A.v) + src + 16 * u);
+    vb.load(static_cast<const T*>(A.v) + src + 16 * u + 8);
+  }
+  __device__ __forceinline__ void store(const AppendParams& P, long long dst, int2 at, int u, const float* angles, T* row) const {
+    Row8 a = ka.row(), b = kb.row();
+    turn_unit(a, b, angles, u, P.rope_dim, P.paired);
+    store8(static_cast<T*>(P.A.k_pool) + dst + 8 * at.x, a);
+    store8(static_cast<T*>(P.A.k_pool) + dst + 8 * at.y, b);
+    va.store(static_cast<T*>(P.A.v_pool) + dst + 16 * u);
+    vb.store(static_cast<T*>(P.A.v_pool) + dst + 16 * u + 8);
+    if (row) {
+      store8(row + 8 * at.x, a);
+      store8(row + 8 * at.y, b);
     }
   }
-}
+};
+// Threads are (row of the page, unit), as many heads at once as there are threads for.
 template <typename T, int D>
 __device__ __forceinline__ void append_part(const AppendParams& P, const PagePart& w, int h0, int h1, unsigned char* smem) {
   using Sh = RowsShape<T, D>;
   const PagedParams& A = P.A;
-  if (!P.bounds) {
-    append_pairs<T, D>(P, w, h0, w.n * (h1 - h0), (T*)nullptr);
+  const int u = threadIdx.x % Sh::kUnits, slot = threadIdx.x / Sh::kUnits, page = min(A.page, Sh::kSlots);
+  const int at_once = Sh::kSlots / page, mine = slot & (page - 1), sub = slot / page;
+  const int2 at = unit_pieces<D>(u, P.rope ? P.rope_dim : 0);
+  const long long dst0 = row_offset(A, w.page, 0, w.e0, D), head_step = (long long)A.page * D;
+  T* rows = P.bounds ? reinterpret_cast<T*>(smem) : nullptr;
+  unsigned char* work = smem + Sh::kBounds;
+  if (w.n <= page) {
+    // the next heads' rows are read while these are turned, stored and looked over
+    const bool on = mine < w.n;
+    const float* angles = on ? angles_of(P, w.first + mine, w.e0 + mine) : nullptr;
+    const long long src = (long long)(w.first + mine) * A.kv_stride, dst = dst0 + (long long)mine * D;
+    auto heads = [&](RowUnit<T, D>& x, RowUnit<T, D>& next, int hb) {
+      const int h = hb + sub;
+      if (on && h + at_once < h1) next.load(A, src + (long long)(h + at_once) * D, at, u);
+      if (on && h < h1) x.store(P, dst + h * head_step, at, u, angles, rows ? rows + (sub * A.page + w.old + mine) * Sh::kStride : nullptr);
+      if (!rows) return;
+      for (int r = mine; r < w.old && h < h1; r += page) {
+        const T* from = static_cast<const T*>(A.k_pool) + row_offset(A, w.page, h, r, D) + 16 * u;
+        Piece<T> a, b;
+        a.load(from);
+        b.load(from + 8);
+        a.store(rows + (sub * A.page + r) * Sh::kStride + 16 * u);
+        b.store(rows + (sub * A.page + r) * Sh::kStride + 16 * u + 8);
+      }
+      __syncthreads();
+      write_bounds<T, D>(P, [&](int s, int r, int c) { return *reinterpret_cast<const typename PairOf<T>::type*>(rows + (s * A.page + r) * Sh::kStride + 2 * c); },
+                         w.old + w.n, at_once, h1 - hb, work, (long long)w.page * A.n_kv_heads + hb);
+    };
+    RowUnit<T, D> x0, x1;
+    if (on && h0 + sub < h1) x0.load(A, src + (long long)(h0 + sub) * D, at, u);
+    for (int hb = h0; hb < h1; hb += 2 * at_once) {
+      heads(x0, x1, hb);
+      if (hb + at_once < h1) heads(x1, x0, hb + at_once);
+    }
     return;
   }
-  T* rows = reinterpret_cast<T*>(smem);
-  float* work = reinterpret_cast<float*>(smem + Sh::kBounds);
-  const int u = threadIdx.x % Sh::kUnits, slot = threadIdx.x / Sh::kUnits;
+  // a page of more rows than threads for them: one head at a time
   for (int h = h0; h < h1; ++h) {
-    for (int r = slot; r < w.old; r += Sh::kSlots) {
-      const T* src = static_cast<const T*>(A.k_pool) + row_offset(A, w.page, h, r, D) + 16 * u;
+    for (int r = mine; r < w.n; r += page) {
+      RowUnit<T, D> x;
+      x.load(A, (long long)(w.first + r) * A.kv_stride + (long long)h * D, at, u);
+      x.store(P, dst0 + (long long)r * D + h * head_step, at, u, angles_of(P, w.first + r, w.e0 + r), rows ? rows + (w.old + r) * Sh::kStride : nullptr);
+    }
+    if (!rows) continue;
+    for (int r = mine; r < w.old; r += page) {
+      const T* from = static_cast<const T*>(A.k_pool) + row_offset(A, w.page, h, r, D) + 16 * u;
       Piece<T> a, b;
-      a.load(src);
-      b.load(src + 8);
+      a.load(from);
+      b.load(from + 8);
       a.store(rows + r * Sh::kStride + 16 * u);
       b.store(rows + r * Sh::kStride + 16 * u + 8);
     }
-    append_pairs<T, D>(P, w, h, w.n, rows);
     __syncthreads();
-    write_bounds<D>(P, [&](int r, int c) { return (float)rows[r * Sh::kStride + c]; }, w.old + w.n, work, (long long)w.page * A.n_kv_heads + h);
+    write_bounds<T, D>(P, [&](int, int r, int c) { return *reinterpret_cast<const typename PairOf<T>::type*>(rows + r * Sh::kStride + 2 * c); }, w.old + w.n, 1, 1, work,
+                       (long long)w.page * A.n_kv_heads + h);
   }
 }
 
@@ -412,14 +449,16 @@ __device__ __forceinline__ void append_part4(const AppendParams& P, const PagePa
       *reinterpret_cast<uint32_t*>((key ? kc : vc) + Row::pairs(A.page, i0) + e * 4) =
           *reinterpret_cast<const uint32_t*>(image + (key ? 0 : Rows4Shape<D>::kImage) + w.n * Row::kCodes + e * 4);
     }
-    if (P.bounds) write_bounds<D>(P, [&](int r, int c) { return keys[R4::at(r, c)]; }, w.old + w.n, work, chunk);
+    if (P.bounds)
+      write_bounds<float, D>(P, [&](int, int r, int c) { return *reinterpret_cast<const float2*>(keys + R4::at(r, 2 * c)); }, w.old + w.n, 1, 1,
+                             reinterpret_cast<unsigned char*>(work), chunk);
     __syncthreads();
   }
 }
 
 // CTAs: queries first, then the slots for parts of pages, kv_splits CTAs each.
 template <typename T, int D, bool FOUR>
-__global__ void __launch_bounds__(kRowsThreads) paged_rows_kernel(const __grid_constant__ AppendParams P) {
+__global__ void __launch_bounds__(kRowsThreads, sizeof(T) == 2 && !FOUR ? 3 : 2) paged_rows_kernel(const __grid_constant__ AppendParams P) {
   extern __shared__ __align__(16) unsigned char smem[];
   griddep_launch();
   griddep_wait();
@@ -469,60 +508,69 @@ struct ExpandParams {
   int blocks;                    // CTAs per (sequence, kv head): 64 entries each
 };
 
-// Eight neighbouring channels per thread and step: a word of a key, two units of a value.  Bound: the bf16 rows' writes.
+// Eight channels per thread and row: a word of a key, or one of a value, which has four channels of two groups.  All of it is exact in
+// bf16: 128 + n and 128 + z are such numbers, and so are their difference and its product with s.  Bound: the bf16 rows' writes.
+__device__ __forceinline__ uint32_t kv4_values(uint32_t codes, uint32_t zeros, uint32_t scales) {      // pairs; zeros: 128 + z
+  const uint32_t n = codes | 0x43004300u;
+  const __nv_bfloat162 y = __hmul2(__hsub2(*reinterpret_cast<const __nv_bfloat162*>(&n), *reinterpret_cast<const __nv_bfloat162*>(&zeros)),
+                                   *reinterpret_cast<const __nv_bfloat162*>(&scales));
+  return *reinterpret_cast<const uint32_t*>(&y);
+}
 template <int D>
 __global__ void __launch_bounds__(kRowsThreads) paged_expand_kernel(const __grid_constant__ ExpandParams P) {
   using Row = Kv4Row<D>;
-  constexpr int kPieces = D / 8;
+  constexpr int kWords = D / 8, kRows = kRowsThreads / kWords, kSteps = 64 / kRows;
+  constexpr uint32_t kLow = 0x000f000fu;
   griddep_launch();
   griddep_wait();
   const PagedParams& A = P.A;
   const int bh = blockIdx.x / P.blocks, b = bh / A.n_kv_heads, h = bh % A.n_kv_heads, first = blockIdx.x % P.blocks * 64;
-  const int len = clamped_len(A, b);
+  const int len = clamped_len(A, b), c = threadIdx.x % kWords, r0 = first + threadIdx.x / kWords;
   if (first >= len) return;
-  const int n = min(64, len - first);
   const long long chunk_bytes = (long long)A.page * Row::kBytes;
-  constexpr int kSteps = 4;                                // pieces in flight
-  for (int base = threadIdx.x; base < 2 * n * kPieces; base += kSteps * kRowsThreads) {
-    uint32_t x[kSteps], pair[kSteps];
-    __nv_bfloat16* dst[kSteps];
+  // of a key: channels 8c .. 8c + 7; of a value: channels 4u .. 4u + 3 of groups g0 and g0 + 1
+  const int g = c / 4, u = c / (Row::kGroups / 2), g0 = 2 * (c % (Row::kGroups / 2));
+  uint32_t key[kSteps], key_pair[kSteps], value[kSteps], value_pairs[kSteps];
+  long long to[kSteps];
 #pragma unroll
-    for (int j = 0; j < kSteps; ++j) {
-      const int k = base + j * kRowsThreads;
-      dst[j] = nullptr;
-      x[j] = pair[j] = 0;
-      if (k >= 2 * n * kPieces) continue;
-      const bool key = k < n * kPieces;
-      const int e = key ? k : k - n * kPieces, i = first + e / kPieces, c = e % kPieces, g = c / 4;
-      const int col = i >> P.to_shift, to = col < P.to_width ? P.to_table[(long long)b * P.to_width + col] : -1, from = page_of(A, b, i);
-      if ((unsigned)to >= (unsigned)P.to_pages) {
-        flag_bad_table(A.status);
-        continue;
-      }
-      dst[j] = (key ? P.k_to : P.v_to) + ((((long long)to * A.n_kv_heads + h) << P.to_shift) + (i & (P.to_page - 1))) * D + 8 * c;
-      if (from < 0) continue;                              // counts as zeros
-      const unsigned char* src = static_cast<const unsigned char*>(key ? A.k_pool : A.v_pool) + ((long long)from * A.n_kv_heads + h) * chunk_bytes;
-      const int row = i & (A.page - 1);
-      pair[j] = *reinterpret_cast<const uint16_t*>(src + Row::pairs(A.page, row) + 2 * g);
-      if (key)
-        x[j] = *reinterpret_cast<const uint32_t*>(src + Row::k_piece(row, g) + (c & 3) * 4);
-      else
-        x[j] = *reinterpret_cast<const uint16_t*>(src + Row::v_unit(row, g, 2 * (c & 3))) |
-               (uint32_t)*reinterpret_cast<const uint16_t*>(src + Row::v_unit(row, g, 2 * (c & 3) + 1)) << 16;
+  for (int k = 0; k < kSteps; ++k) {
+    const int i = r0 + k * kRows;
+    to[k] = -1;
+    key[k] = key_pair[k] = value[k] = value_pairs[k] = 0;
+    if (i >= len) continue;
+    const int col = i >> P.to_shift, pg = col < P.to_width ? P.to_table[(long long)b * P.to_width + col] : -1, from = page_of(A, b, i);
+    if ((unsigned)pg >= (unsigned)P.to_pages) {
+      flag_bad_table(A.status);
+      continue;
     }
+    to[k] = ((((long long)pg * A.n_kv_heads + h) << P.to_shift) + (i & (P.to_page - 1))) * D;
+    if (from < 0) continue;                                // counts as zeros
+    const int row = i & (A.page - 1);
+    const long long at = ((long long)from * A.n_kv_heads + h) * chunk_bytes;
+    const unsigned char* kc = static_cast<const unsigned char*>(A.k_pool) + at;
+    const unsigned char* vc = static_cast<const unsigned char*>(A.v_pool) + at;
+    key[k] = *reinterpret_cast<const uint32_t*>(kc + Row::k_piece(row, g) + (c & 3) * 4);
+    key_pair[k] = *reinterpret_cast<const uint16_t*>(kc + Row::pairs(A.page, row) + 2 * g);
+    value[k] = *reinterpret_cast<const uint32_t*>(vc + Row::v_unit(row, g0, u));
+    value_pairs[k] = *reinterpret_cast<const uint32_t*>(vc + Row::pairs(A.page, row) + 2 * g0);
+  }
 #pragma unroll
-    for (int j = 0; j < kSteps; ++j) {
-      if (!dst[j]) continue;
-      const bool key = base + j * kRowsThreads < n * kPieces;
-      const float s = kv4_scale(pair[j] & 255), z = (float)(pair[j] >> 8);
-      uint32_t out[4];
+  for (int k = 0; k < kSteps; ++k) {
+    if (to[k] < 0) continue;
+    {
+      const uint32_t s = __float_as_uint(kv4_scale(key_pair[k] & 255)), s2 = __byte_perm(s, s, 0x3232), z2 = __byte_perm(key_pair[k], 0x43u, 0x4141);
+      *reinterpret_cast<uint4*>(P.k_to + to[k] + 8 * c) =
+          make_uint4(kv4_values(key[k] & kLow, z2, s2), kv4_values(key[k] >> 4 & kLow, z2, s2), kv4_values(key[k] >> 8 & kLow, z2, s2), kv4_values(key[k] >> 12 & kLow, z2, s2));
+    }
+    {
+      const uint32_t s2 = __byte_perm(__float_as_uint(kv4_scale(value_pairs[k] & 255)), __float_as_uint(kv4_scale(value_pairs[k] >> 16 & 255)), 0x7632);
+      const uint32_t z2 = (value_pairs[k] >> 8 & 0x00ff00ffu) | 0x43004300u;
+      uint32_t y[4];                                       // channel m of group g0 | of group g0 + 1
 #pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        // channels 2m and 2m + 1
-        const uint32_t n0 = (key ? x[j] >> 4 * m : x[j] >> 8 * m) & 15, n1 = (key ? x[j] >> (4 * m + 16) : x[j] >> (8 * m + 4)) & 15;
-        out[m] = bf16_pair(((float)n0 - z) * s, ((float)n1 - z) * s);
-      }
-      *reinterpret_cast<uint4*>(dst[j]) = make_uint4(out[0], out[1], out[2], out[3]);
+      for (int m = 0; m < 4; ++m) y[m] = kv4_values(value[k] >> 4 * m & kLow, z2, s2);
+      __nv_bfloat16* out = P.v_to + to[k] + 32 * g0 + 4 * u;
+      *reinterpret_cast<uint2*>(out) = make_uint2(__byte_perm(y[0], y[1], 0x5410), __byte_perm(y[2], y[3], 0x5410));
+      *reinterpret_cast<uint2*>(out + 32) = make_uint2(__byte_perm(y[0], y[1], 0x7632), __byte_perm(y[2], y[3], 0x7632));
     }
   }
 }
