@@ -12,14 +12,14 @@ template <typename T, int D, bool FOUR>
 int append_typed(wkv_paged* c, AppendParams& P) {
   const PagedParams& A = P.A;
   constexpr int kSlots = RowsShape<T, D>::kSlots;
-  static_assert(rows_smem<T, D, FOUR>() >= (1024 + 1) * 4, "the queries' CTAs hold the offsets there");
+  static_assert(rows_smem<T, D, FOUR>() >= (2 * kMostSequences + 1) * 4, "the queries' CTAs hold offsets and lengths there");
   long long blocks = 0;
   if (A.q) {
-    // heads per CTA: eight rows a thread where that leaves two CTAs an SM, four, or one
+    // heads per CTA: sixteen rows a thread where that leaves four CTAs an SM, else eight, four, two or one
     const int tokens = std::min(A.rows, kSlots), at_once = kSlots / tokens;
     const long long tiles = ((long long)A.rows + tokens - 1) / tokens;
-    int steps = 8;
-    while (steps > 1 && tiles * ((A.n_q_heads + at_once * steps - 1) / (at_once * steps)) < 2 * c->sm_count) steps >>= 1;
+    int steps = 16;
+    while (steps > 1 && tiles * ((A.n_q_heads + at_once * steps - 1) / (at_once * steps)) < 4 * c->sm_count) steps >>= 1;
     P.q_heads = at_once * steps;
     blocks = tiles * ((A.n_q_heads + P.q_heads - 1) / P.q_heads);
     P.q_blocks = (int)blocks;

@@ -23,7 +23,7 @@ struct AppendParams {
   int q_blocks, q_heads, kv_heads, kv_splits;   // CTAs for queries; heads per CTA; CTAs per page part
 };
 
-constexpr int kRowsThreads = 256;
+constexpr int kRowsThreads = 256, kMostSequences = 1024;
 
 // Eight channels in fp32.
 struct Row8 {
@@ -116,58 +116,77 @@ __device__ __forceinline__ const float* angles_of(const AppendParams& P, int r, 
 // n of them, lie in (n - 2) / page + 2 pages at most, rounded down.
 __device__ __forceinline__ int first_slot(int row, int b, int page_shift) { return (row >> page_shift) + 2 * b; }
 
-// ---- queries: 32 (token, head) rows at once, a unit per thread
+// ---- queries: 32 (token, head) rows at once, a unit per thread.  The rows that a thread takes do not depend on whose they are: the first
+// ones are on their way while that is found out, then always the next ones while some are turned.
 template <typename T, int D>
 __device__ __forceinline__ void turn_queries(const AppendParams& P, int block, int* starts) {
   const PagedParams& A = P.A;
-  constexpr int kUnits = D / 16, kSlots = kRowsThreads / kUnits;
+  constexpr int kUnits = D / 16, kSlots = kRowsThreads / kUnits, kSteps = sizeof(T) == 2 ? 2 : 1;
   const int per = (A.n_q_heads + P.q_heads - 1) / P.q_heads;
   const int tokens = min(A.rows, kSlots), t0 = block / per * tokens, h0 = block % per * P.q_heads, h1 = min(A.n_q_heads, h0 + P.q_heads);
-  if (A.q_start) {
-    for (int b = threadIdx.x; b <= A.batch; b += kRowsThreads) starts[b] = A.q_start[b];
-    __syncthreads();
-  }
   const int u = threadIdx.x % kUnits, slot = threadIdx.x / kUnits, lanes = kSlots / tokens;     // heads at once
   const int r = t0 + slot % tokens;
-  if (slot >= lanes * tokens || r >= A.rows) return;
+  const bool on = slot < lanes * tokens && r < A.rows;
+  const int2 at = unit_pieces<D>(u, P.rope ? P.rope_dim : 0);
+  const T* from = static_cast<const T*>(A.q) + (long long)r * A.q_stride;
+  T* to = static_cast<T*>(P.q_out) + (long long)r * P.q_out_stride;
+  struct Rows {
+    Piece<T> a[kSteps], b[kSteps];
+  } x0, x1;
+  auto load = [&](Rows& x, int base) {
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+      const int h = base + k * lanes;
+      if (h >= h1) continue;
+      x.a[k].load(from + h * D + 8 * at.x);
+      x.b[k].load(from + h * D + 8 * at.y);
+    }
+  };
+  int base = h0 + slot / tokens;
+  if (on) load(x0, base);
   int entry;
   if (A.q_start) {
+    int* lens = starts + kMostSequences + 1;
+    for (int b = threadIdx.x; b <= A.batch; b += kRowsThreads) {
+      starts[b] = A.q_start[b];
+      if (b < A.batch) lens[b] = A.seq_lens[b];
+    }
+    __syncthreads();
+    if (!on) return;
     int lo = 0, hi = A.batch;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (starts[mid] <= r) lo = mid; else hi = mid;
     }
-    if (r < starts[lo] || r >= starts[lo + 1]) return;
-    const SeqRows s = seq_rows(A, lo);
-    if (r < s.first || r >= s.first + s.n) return;
-    entry = s.len - s.n + (r - s.first);
+    const int s0 = max(0, starts[lo]), s1 = min(starts[lo + 1], A.rows);   // as seq_rows has them; the appending CTAs, or this, report
+    const long long most = (long long)A.width << A.page_shift;
+    const int len = lens[lo] < 0 ? 0 : lens[lo] > most ? (int)most : lens[lo];
+    if (s0 != starts[lo] || s1 != starts[lo + 1] || s1 < s0 || len != lens[lo] || s1 - s0 > len) flag_bad_table(A.status);
+    if (r < s0 || r >= s1) return;
+    entry = len - (s1 - s0) + (r - s0);
   } else {
+    if (!on) return;
     entry = clamped_len(A, r) - 1;
     if (entry < 0) return;
   }
   const float* angles = angles_of(P, r, entry);
-  const int2 at = unit_pieces<D>(u, P.rope ? P.rope_dim : 0);
-  const T* from = static_cast<const T*>(A.q) + (long long)r * A.q_stride;
-  T* to = static_cast<T*>(P.q_out) + (long long)r * P.q_out_stride;
-  constexpr int kSteps = 4;                                // rows in flight
-  for (int base = h0 + slot / tokens; base < h1; base += kSteps * lanes) {
-    Piece<T> pa[kSteps], pb[kSteps];
+  auto store = [&](const Rows& x, int at_head) {
 #pragma unroll
     for (int k = 0; k < kSteps; ++k) {
-      const int h = base + k * lanes;
+      const int h = at_head + k * lanes;
       if (h >= h1) continue;
-      pa[k].load(from + h * D + 8 * at.x);
-      pb[k].load(from + h * D + 8 * at.y);
-    }
-#pragma unroll
-    for (int k = 0; k < kSteps; ++k) {
-      const int h = base + k * lanes;
-      if (h >= h1) continue;
-      Row8 a = pa[k].row(), b = pb[k].row();
+      Row8 a = x.a[k].row(), b = x.b[k].row();
       turn_unit(a, b, angles, u, P.rope_dim, P.paired);
       store8(to + h * D + 8 * at.x, a);
       store8(to + h * D + 8 * at.y, b);
     }
+  };
+  const int step = kSteps * lanes;
+  for (; base < h1; base += 2 * step) {
+    load(x1, base + step);
+    store(x0, base);
+    load(x0, base + 2 * step);
+    store(x1, base + step);
   }
 }
 
@@ -251,7 +270,7 @@ constexpr int rows_smem() {
 }
 
 struct PagePart {
-  int b, first, page;          // row of the first new entry; the pool's page
+  int b, first, page;          // row of the first new entry; the pool's page (-1: not looked up yet)
   int e0, n, old;              // index of the first new entry, number of new entries, entries of the page before them
 };
 
@@ -280,20 +299,25 @@ struct RowUnit {
 };
 // Threads are (row of the page, unit), as many heads at once as there are threads for.
 template <typename T, int D>
-__device__ __forceinline__ void append_part(const AppendParams& P, const PagePart& w, int h0, int h1, unsigned char* smem) {
+__device__ __forceinline__ void append_part(const AppendParams& P, PagePart w, int h0, int h1, unsigned char* smem) {
   using Sh = RowsShape<T, D>;
   const PagedParams& A = P.A;
   const int u = threadIdx.x % Sh::kUnits, slot = threadIdx.x / Sh::kUnits, page = min(A.page, Sh::kSlots);
   const int at_once = Sh::kSlots / page, mine = slot & (page - 1), sub = slot / page;
   const int2 at = unit_pieces<D>(u, P.rope ? P.rope_dim : 0);
-  const long long dst0 = row_offset(A, w.page, 0, w.e0, D), head_step = (long long)A.page * D;
+  const long long head_step = (long long)A.page * D;
   T* rows = P.bounds ? reinterpret_cast<T*>(smem) : nullptr;
   unsigned char* work = smem + Sh::kBounds;
   if (w.n <= page) {
     // the next heads' rows are read while these are turned, stored and looked over
     const bool on = mine < w.n;
+    const long long src = (long long)(w.first + mine) * A.kv_stride;
+    RowUnit<T, D> x0, x1;
+    if (on && h0 + sub < h1) x0.load(A, src + (long long)(h0 + sub) * D, at, u);
+    w.page = page_of(A, w.b, w.e0);                        // (the first rows are on their way)
+    if (w.page < 0) return;
     const float* angles = on ? angles_of(P, w.first + mine, w.e0 + mine) : nullptr;
-    const long long src = (long long)(w.first + mine) * A.kv_stride, dst = dst0 + (long long)mine * D;
+    const long long dst = row_offset(A, w.page, 0, w.e0, D) + (long long)mine * D;
     auto heads = [&](RowUnit<T, D>& x, RowUnit<T, D>& next, int hb) {
       const int h = hb + sub;
       if (on && h + at_once < h1) next.load(A, src + (long long)(h + at_once) * D, at, u);
@@ -311,8 +335,6 @@ __device__ __forceinline__ void append_part(const AppendParams& P, const PagePar
       write_bounds<T, D>(P, [&](int s, int r, int c) { return *reinterpret_cast<const typename PairOf<T>::type*>(rows + (s * A.page + r) * Sh::kStride + 2 * c); },
                          w.old + w.n, at_once, h1 - hb, work, (long long)w.page * A.n_kv_heads + hb);
     };
-    RowUnit<T, D> x0, x1;
-    if (on && h0 + sub < h1) x0.load(A, src + (long long)(h0 + sub) * D, at, u);
     for (int hb = h0; hb < h1; hb += 2 * at_once) {
       heads(x0, x1, hb);
       if (hb + at_once < h1) heads(x1, x0, hb + at_once);
@@ -320,6 +342,9 @@ __device__ __forceinline__ void append_part(const AppendParams& P, const PagePar
     return;
   }
   // a page of more rows than threads for them: one head at a time
+  w.page = page_of(A, w.b, w.e0);
+  if (w.page < 0) return;
+  const long long dst0 = row_offset(A, w.page, 0, w.e0, D);
   for (int h = h0; h < h1; ++h) {
     for (int r = mine; r < w.n; r += page) {
       RowUnit<T, D> x;
@@ -361,7 +386,7 @@ __device__ __forceinline__ void pack_group(const float (&x)[32], uint32_t (&word
 }
 
 template <typename T, int D>
-__device__ __forceinline__ void append_part4(const AppendParams& P, const PagePart& w, int h0, int h1, unsigned char* smem) {
+__device__ __forceinline__ void append_part4(const AppendParams& P, PagePart w, int h0, int h1, unsigned char* smem) {
   using Sh = RowsShape<T, D>;
   using Row = Kv4Row<D>;
   using R4 = Rows4Shape<D>;
@@ -374,6 +399,8 @@ __device__ __forceinline__ void append_part4(const AppendParams& P, const PagePa
   const int2 at = unit_pieces<D>(u, P.rope ? P.rope_dim : 0);
   const int i0 = w.e0 & (A.page - 1);
   const long long chunk_bytes = (long long)A.page * Row::kBytes;
+  w.page = page_of(A, w.b, w.e0);
+  if (w.page < 0) return;
   for (int h = h0; h < h1; ++h) {
     const long long chunk = (long long)w.page * A.n_kv_heads + h;
     unsigned char* kc = static_cast<unsigned char*>(A.k_pool) + chunk * chunk_bytes;
@@ -490,8 +517,7 @@ __global__ void __launch_bounds__(kRowsThreads, sizeof(T) == 2 && !FOUR ? 3 : 2)
   if (w.n <= 0) return;
   w.first = s.first + (w.e0 - old);
   w.old = w.e0 & (A.page - 1);
-  w.page = page_of(A, w.b, w.e0);
-  if (w.page < 0) return;
+  w.page = -1;
   if constexpr (FOUR) append_part4<T, D>(P, w, h0, h1, smem);
   else append_part<T, D>(P, w, h0, h1, smem);
 }
