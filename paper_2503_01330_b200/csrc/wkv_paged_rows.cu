@@ -11,9 +11,9 @@ namespace {
 template <typename T, int D, bool FOUR>
 int append_typed(wkv_paged* c, AppendParams& P) {
   const PagedParams& A = P.A;
-  constexpr int kSlots = RowsShape<T, D>::kSlots;
-  static_assert(rows_smem<T, D, FOUR>() >= (2 * kMostSequences + 1) * 4, "the queries' CTAs hold offsets and lengths there");
-  long long blocks = 0;
+  constexpr int kSlots = RowsShape<D>::kSlots;
+  static_assert(rows_smem<D, FOUR>() >= RowsShape<D>::kOffsets, "the queries' CTAs hold offsets and lengths there");
+  long long entries = 0;
   if (A.q) {
     // heads per CTA: sixteen rows a thread where that leaves four CTAs an SM, else eight, four, two or one
     const int tokens = std::min(A.rows, kSlots), at_once = kSlots / tokens;
@@ -21,18 +21,23 @@ int append_typed(wkv_paged* c, AppendParams& P) {
     int steps = 16;
     while (steps > 1 && tiles * ((A.n_q_heads + at_once * steps - 1) / (at_once * steps)) < 4 * c->sm_count) steps >>= 1;
     P.q_heads = at_once * steps;
-    blocks = tiles * ((A.n_q_heads + P.q_heads - 1) / P.q_heads);
+    const long long blocks = tiles * ((A.n_q_heads + P.q_heads - 1) / P.q_heads);
+    if (blocks > 0x7fffffffLL) return fail(c, WKV_ERR_INVALID, "total_q * heads is too large");
     P.q_blocks = (int)blocks;
   }
   if (A.k) {
-    const long long slots = A.q_start ? ((long long)A.rows >> A.page_shift) + 2LL * A.batch : A.batch;
-    P.kv_heads = 8;
-    while (P.kv_heads > 1 && slots * ((A.n_kv_heads + P.kv_heads - 1) / P.kv_heads) < 4 * c->sm_count) P.kv_heads >>= 1;
-    P.kv_splits = (A.n_kv_heads + P.kv_heads - 1) / P.kv_heads;
-    blocks += slots * P.kv_splits;
+    P.kv_slots = A.q_start ? (A.rows >> A.page_shift) + 2 * A.batch : A.batch;
+    if constexpr (FOUR) {
+      P.kv_heads = 8;
+      while (P.kv_heads > 1 && (long long)P.kv_slots * ((A.n_kv_heads + P.kv_heads - 1) / P.kv_heads) < 4 * c->sm_count) P.kv_heads >>= 1;
+      P.kv_splits = (A.n_kv_heads + P.kv_heads - 1) / P.kv_heads;
+      entries = (long long)P.kv_slots * P.kv_splits;
+    } else {
+      entries = ((long long)P.kv_slots * A.n_kv_heads + kRowsThreads / 32 - 1) / (kRowsThreads / 32);
+    }
   }
-  if (blocks > 0x7fffffffLL) return fail(c, WKV_ERR_INVALID, "total_q * heads is too large");
-  WKV_CUDA(c, launch(c, paged_rows_kernel<T, D, FOUR>, blocks, kRowsThreads, (size_t)rows_smem<T, D, FOUR>(), P));
+  if (P.q_blocks + entries > 0x7fffffffLL) return fail(c, WKV_ERR_INVALID, "total_q * heads is too large");
+  WKV_CUDA(c, launch(c, paged_rows_kernel<T, D, FOUR>, P.q_blocks + entries, kRowsThreads, (size_t)rows_smem<D, FOUR>(), P));
   return WKV_OK;
 }
 int append(wkv_paged* c, AppendParams& P) {
@@ -49,8 +54,8 @@ int append(wkv_paged* c, AppendParams& P) {
 
 cudaError_t prepare_rows(wkv_paged* c) {
   if (c->cfg.dtype != WKV_KV4) return cudaSuccess;
-  return c->cfg.head_dim == 128 ? cudaFuncSetAttribute(paged_rows_kernel<__nv_bfloat16, 128, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, rows_smem<__nv_bfloat16, 128, true>())
-                                : cudaFuncSetAttribute(paged_rows_kernel<__nv_bfloat16, 64, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, rows_smem<__nv_bfloat16, 64, true>());
+  return c->cfg.head_dim == 128 ? cudaFuncSetAttribute(paged_rows_kernel<__nv_bfloat16, 128, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, rows_smem<128, true>())
+                                : cudaFuncSetAttribute(paged_rows_kernel<__nv_bfloat16, 64, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, rows_smem<64, true>());
 }
 
 int append_rows(wkv_paged* c, const PagedParams& A) {

@@ -20,7 +20,7 @@ struct AppendParams {
   int8_t* bounds;                // the layer's [pages][Hkv][2][D], or NULL
   float* bound_scale;            // [pages][Hkv]
   int rope_rows, rope_dim, paired;
-  int q_blocks, q_heads, kv_heads, kv_splits;   // CTAs for queries; heads per CTA; CTAs per page part
+  int q_blocks, q_heads, kv_heads, kv_splits, kv_slots;   // CTAs for queries; heads per CTA; CTAs per page part; parts, at most
 };
 
 constexpr int kRowsThreads = 256, kMostSequences = 1024;
@@ -80,27 +80,39 @@ __device__ __forceinline__ void turn(float& a, float& b, float c, float s) {
   b = __fadd_rn(__fmul_rn(b, c), __fmul_rn(a, s));
   a = y;
 }
-// Rotation of a unit's two pieces; `angles`: the position's row of the table.
-__device__ __forceinline__ void turn_unit(Row8& a, Row8& b, const float* angles, int u, int dim, int paired) {
-  const int h = dim >> 4;
-  if (!angles || u >= h) return;
-  if (!paired) {
-    const Row8 c = load8(angles + 8 * u), s = load8(angles + (dim >> 1) + 8 * u);
+// A unit's angles: of channel i of both pieces cos c[i], sin s[i]; paired: of channels 2i, 2i + 1 of the first piece c[i], s[i], of the
+// second one's c[4 + i], s[4 + i].
+struct Turn {
+  bool on;
+  Row8 c, s;
+  __device__ __forceinline__ void load(const float* angles, int u, int dim, int paired) {      // angles: the position's row, or NULL
+    const int h = dim >> 4;
+    on = angles && u < h;
+    if (!on) return;
+    const float* sines = angles + (dim >> 1);
+    const float4* at[4] = {reinterpret_cast<const float4*>(angles + (paired ? 4 * u : 8 * u)), reinterpret_cast<const float4*>(angles + (paired ? 4 * (u + h) : 8 * u + 4)),
+                           reinterpret_cast<const float4*>(sines + (paired ? 4 * u : 8 * u)), reinterpret_cast<const float4*>(sines + (paired ? 4 * (u + h) : 8 * u + 4))};
+    const float4 y[4] = {*at[0], *at[1], *at[2], *at[3]};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) turn(a.x[i], b.x[i], c.x[i], s.x[i]);
-  } else {
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int at = 4 * (u + half * h);
-      const float4 c = *reinterpret_cast<const float4*>(angles + at), s = *reinterpret_cast<const float4*>(angles + (dim >> 1) + at);
-      Row8& r = half ? b : a;
-      turn(r.x[0], r.x[1], c.x, s.x);
-      turn(r.x[2], r.x[3], c.y, s.y);
-      turn(r.x[4], r.x[5], c.z, s.z);
-      turn(r.x[6], r.x[7], c.w, s.w);
+    for (int k = 0; k < 2; ++k) {
+      c.x[4 * k] = y[k].x; c.x[4 * k + 1] = y[k].y; c.x[4 * k + 2] = y[k].z; c.x[4 * k + 3] = y[k].w;
+      s.x[4 * k] = y[2 + k].x; s.x[4 * k + 1] = y[2 + k].y; s.x[4 * k + 2] = y[2 + k].z; s.x[4 * k + 3] = y[2 + k].w;
     }
   }
-}
+  __device__ __forceinline__ void turn_unit(Row8& a, Row8& b, int paired) const {
+    if (!on) return;
+    if (!paired) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) turn(a.x[i], b.x[i], c.x[i], s.x[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        turn(a.x[2 * i], a.x[2 * i + 1], c.x[i], s.x[i]);
+        turn(b.x[2 * i], b.x[2 * i + 1], c.x[4 + i], s.x[4 + i]);
+      }
+    }
+  }
+};
 // The table's row for token r with entry index i; NULL, reported, if the position is outside of it.
 __device__ __forceinline__ const float* angles_of(const AppendParams& P, int r, int i) {
   if (!P.rope) return nullptr;
@@ -169,14 +181,15 @@ __device__ __forceinline__ void turn_queries(const AppendParams& P, int block, i
     entry = clamped_len(A, r) - 1;
     if (entry < 0) return;
   }
-  const float* angles = angles_of(P, r, entry);
+  Turn angles;
+  angles.load(angles_of(P, r, entry), u, P.rope_dim, P.paired);
   auto store = [&](const Rows& x, int at_head) {
 #pragma unroll
     for (int k = 0; k < kSteps; ++k) {
       const int h = at_head + k * lanes;
       if (h >= h1) continue;
       Row8 a = x.a[k].row(), b = x.b[k].row();
-      turn_unit(a, b, angles, u, P.rope_dim, P.paired);
+      angles.turn_unit(a, b, P.paired);
       store8(to + h * D + 8 * at.x, a);
       store8(to + h * D + 8 * at.y, b);
     }
@@ -190,70 +203,76 @@ __device__ __forceinline__ void turn_queries(const AppendParams& P, int block, i
   }
 }
 
-// ---- bounds of the n keys of a page, for several heads at once: keys(head, row, pair of channels) from shared memory
-// Pairs of channels as they lie there, with the largest and the least of two of them.
+// ---- bounds of the n keys of a page: key(row, pair of channels) in shared memory.  Pairs of channels as they lie in a row:
 __device__ __forceinline__ __nv_bfloat162 pair_max(__nv_bfloat162 a, __nv_bfloat162 b) { return __hmax2(a, b); }
 __device__ __forceinline__ __nv_bfloat162 pair_min(__nv_bfloat162 a, __nv_bfloat162 b) { return __hmin2(a, b); }
 __device__ __forceinline__ float2 pair_floats(__nv_bfloat162 a) { return __bfloat1622float2(a); }
 __device__ __forceinline__ float2 pair_max(float2 a, float2 b) { return make_float2(fmaxf(a.x, b.x), fmaxf(a.y, b.y)); }
 __device__ __forceinline__ float2 pair_min(float2 a, float2 b) { return make_float2(fminf(a.x, b.x), fminf(a.y, b.y)); }
 __device__ __forceinline__ float2 pair_floats(float2 a) { return a; }
+__device__ __forceinline__ __nv_bfloat162 pair_shuffle(__nv_bfloat162 a, int off) { return __shfl_xor_sync(~0u, a, off); }
+__device__ __forceinline__ float2 pair_shuffle(float2 a, int off) { return make_float2(__shfl_xor_sync(~0u, a.x, off), __shfl_xor_sync(~0u, a.y, off)); }
 template <typename T> struct PairOf { typedef __nv_bfloat162 type; };
 template <> struct PairOf<float> { typedef float2 type; };
 
-// work: [2][threads] pairs and [warps] floats.  heads: 1, 2 or 4, of which the first `valid` are written; heads * rows at most as many as one pass of the CTA takes.  A thread
-// owns a pair of channels of a head over a share of the rows; the shares meet in shared memory.  One barrier; the caller's next one
-// protects the keys and the work.
-template <typename T, int D, typename Keys>
-__device__ __forceinline__ void write_bounds(const AppendParams& P, Keys keys, int n, int heads, int valid, unsigned char* work, long long chunk) {
-  typedef typename PairOf<T>::type Pair;
-  constexpr int kPairs = D / 2;
-  Pair* his = reinterpret_cast<Pair*>(work);
-  Pair* los = his + kRowsThreads;
+// A page's scale and its inverse; a bound in steps of it, outwards (what is not finite ends at the border).
+struct BoundScale {
+  float scale, inv;
+  __device__ __forceinline__ uint32_t up(float x) const { return (uint32_t)(int)fminf(fmaxf(ceilf(__fmul_rn(x, inv)), -127.f), 127.f) & 255; }
+  __device__ __forceinline__ uint32_t down(float x) const { return (uint32_t)(int)fmaxf(fminf(floorf(__fmul_rn(x, inv)), 127.f), -127.f) & 255; }
+};
+
+__device__ __forceinline__ BoundScale bound_scale(float most) {
+  BoundScale q;
+  q.scale = __fmul_rn(most, 1.f / 127.f);
+  q.inv = q.scale >= 0x1p-100f ? __frcp_rn(q.scale) : 0.f;
+  return q;
+}
+
+// By a CTA.  work: [2][threads] pairs and [warps] floats.  A thread owns a pair of channels over a share of the rows; the shares meet in
+// shared memory.  One barrier; the caller's next one protects the keys and the work.
+template <int D, typename Keys>
+__device__ __forceinline__ void write_bounds(const AppendParams& P, Keys key, int n, float2* work, long long chunk) {
+  constexpr int kPairs = D / 2, kShares = kRowsThreads / kPairs;
+  float2* his = work;
+  float2* los = his + kRowsThreads;
   float* mosts = reinterpret_cast<float*>(los + kRowsThreads);
-  const int c = threadIdx.x % kPairs, of = threadIdx.x / kPairs, shares = kRowsThreads / kPairs / heads, head = of / shares, share = of % shares;
-  Pair hi = keys(head, min(share, n - 1), c), lo = hi;
-  for (int r = share + shares; r < n; r += shares) {
-    const Pair x = keys(head, r, c);
+  const int c = threadIdx.x % kPairs, share = threadIdx.x / kPairs;
+  float2 hi = key(min(share, n - 1), c), lo = hi;
+  for (int r = share + kShares; r < n; r += kShares) {
+    const float2 x = key(r, c);
     hi = pair_max(hi, x);
     lo = pair_min(lo, x);
   }
   his[threadIdx.x] = hi;
   los[threadIdx.x] = lo;
-  float2 up = pair_floats(hi), down = pair_floats(lo);
-  float most = fmaxf(fmaxf(fabsf(up.x), fabsf(up.y)), fmaxf(fabsf(down.x), fabsf(down.y)));
+  float most = fmaxf(fmaxf(fabsf(hi.x), fabsf(hi.y)), fmaxf(fabsf(lo.x), fabsf(lo.y)));
 #pragma unroll
   for (int off = 16; off; off >>= 1) most = fmaxf(most, __shfl_xor_sync(~0u, most, off));
   if ((threadIdx.x & 31) == 0) mosts[threadIdx.x >> 5] = most;
   __syncthreads();
-  if (share == 0 && head < valid) {
-    for (int k = 1; k < shares; ++k) {
+  if (share == 0) {
+#pragma unroll
+    for (int k = 1; k < kShares; ++k) {
       hi = pair_max(hi, his[threadIdx.x + k * kPairs]);
       lo = pair_min(lo, los[threadIdx.x + k * kPairs]);
     }
-    const int warps = kRowsThreads / 32 / heads;           // of the head
     most = 0.f;
-    for (int k = 0; k < warps; ++k) most = fmaxf(most, mosts[head * warps + k]);
-    const float scale = __fmul_rn(most, 1.f / 127.f), inv = scale >= 0x1p-100f ? __frcp_rn(scale) : 0.f;
-    // outwards; what is not finite ends at the border
-    up = pair_floats(hi);
-    down = pair_floats(lo);
-    auto above = [&](float x) { return (int)fminf(fmaxf(ceilf(__fmul_rn(x, inv)), -127.f), 127.f) & 255; };
-    auto below = [&](float x) { return (int)fmaxf(fminf(floorf(__fmul_rn(x, inv)), 127.f), -127.f) & 255; };
-    uint16_t* to = reinterpret_cast<uint16_t*>(P.bounds + (chunk + head) * 2 * D);
-    to[c] = (uint16_t)(above(up.x) | above(up.y) << 8);
-    to[kPairs + c] = (uint16_t)(below(down.x) | below(down.y) << 8);
-    if (c == 0) P.bound_scale[chunk + head] = scale;
+#pragma unroll
+    for (int k = 0; k < kRowsThreads / 32; ++k) most = fmaxf(most, mosts[k]);
+    const BoundScale q = bound_scale(most);
+    uint16_t* to = reinterpret_cast<uint16_t*>(P.bounds + chunk * 2 * D);
+    to[c] = (uint16_t)(q.up(hi.x) | q.up(hi.y) << 8);
+    to[kPairs + c] = (uint16_t)(q.down(lo.x) | q.down(lo.y) << 8);
+    if (c == 0) P.bound_scale[chunk] = q.scale;
   }
 }
 
 // ---- new entries in the storage type
-template <typename T, int D>
+template <int D>
 struct RowsShape {
-  static constexpr int kUnits = D / 16, kSlots = kRowsThreads / kUnits, kVec = 16 / (int)sizeof(T);
-  static constexpr int kStride = D + kVec;
-  static constexpr int kBounds = 64 * kStride * (int)sizeof(T);         // staged keys of a page
-  static constexpr int kWork = 2 * kRowsThreads * 2 * (int)sizeof(T) + 32;
+  static constexpr int kUnits = D / 16, kSlots = kRowsThreads / kUnits;
+  static constexpr int kOffsets = (2 * kMostSequences + 1) * 4;         // of the queries' CTAs: offsets and lengths
 };
 // 4 bits: fp32 keys of a page, then the codes and pairs of its keys and values.  A group's 32 keys lie 36 floats behind the last one's:
 // the threads of a row's groups read them from different banks.
@@ -263,106 +282,130 @@ struct Rows4Shape {
   __device__ __forceinline__ static int at(int r, int c) { return r * kStride + c / 32 * 36 + c % 32; }
   static constexpr int kKeys = 64 * kStride * 4;
   static constexpr int kImage = 64 * Kv4Row<D>::kBytes;
+  static constexpr int kWork = 2 * kRowsThreads * 8 + 32;
 };
-template <typename T, int D, bool FOUR>
-constexpr int rows_smem() {
-  return FOUR ? Rows4Shape<D>::kKeys + 2 * Rows4Shape<D>::kImage + RowsShape<float, D>::kWork : RowsShape<T, D>::kBounds + RowsShape<T, D>::kWork;
-}
+template <int D, bool FOUR>
+constexpr int rows_smem() { return FOUR ? Rows4Shape<D>::kKeys + 2 * Rows4Shape<D>::kImage + Rows4Shape<D>::kWork : RowsShape<D>::kOffsets; }
 
 struct PagePart {
-  int b, first, page;          // row of the first new entry; the pool's page (-1: not looked up yet)
+  int b, first;                // sequence; row of the first new entry
   int e0, n, old;              // index of the first new entry, number of new entries, entries of the page before them
 };
 
-// One row's unit of a head: read, turned and stored; keys are staged too where `rows` is given.
+// A head's rows of a part, by one warp: four (or eight) rows at once, a unit per lane; the next rows are read while these are turned and
+// stored.  The largest and least keys of a channel stay in registers until the end: no barriers (a CTA per part, keys staged in shared
+// memory, took 203 us for the kv half of 4 x 2048..8191 tokens, 32 heads, where 152 are without bounds).
 template <typename T, int D>
-struct RowUnit {
-  Piece<T> ka, kb, va, vb;
-  __device__ __forceinline__ void load(const PagedParams& A, long long src, int2 at, int u) {
-    ka.load(static_cast<const T*>(A.k) + src + 8 * at.x);
-    kb.load(static_cast<const T*>(A.k) + src + 8 * at.y);
-    va.load(static_cast<const T*>(A.v) + src + 16 * u);
-    vb.load(static_cast<const T*>(A.v) + src + 16 * u + 8);
-  }
-  __device__ __forceinline__ void store(const AppendParams& P, long long dst, int2 at, int u, const float* angles, T* row) const {
-    Row8 a = ka.row(), b = kb.row();
-    turn_unit(a, b, angles, u, P.rope_dim, P.paired);
-    store8(static_cast<T*>(P.A.k_pool) + dst + 8 * at.x, a);
-    store8(static_cast<T*>(P.A.k_pool) + dst + 8 * at.y, b);
-    va.store(static_cast<T*>(P.A.v_pool) + dst + 16 * u);
-    vb.store(static_cast<T*>(P.A.v_pool) + dst + 16 * u + 8);
-    if (row) {
-      store8(row + 8 * at.x, a);
-      store8(row + 8 * at.y, b);
-    }
-  }
-};
-// Threads are (row of the page, unit), as many heads at once as there are threads for.
-template <typename T, int D>
-__device__ __forceinline__ void append_part(const AppendParams& P, PagePart w, int h0, int h1, unsigned char* smem) {
-  using Sh = RowsShape<T, D>;
+__device__ __forceinline__ void append_head(const AppendParams& P, const PagePart& w, int h) {
+  typedef typename PairOf<T>::type Pair;
+  constexpr int kUnits = D / 16, kRows = 32 / kUnits;
   const PagedParams& A = P.A;
-  const int u = threadIdx.x % Sh::kUnits, slot = threadIdx.x / Sh::kUnits, page = min(A.page, Sh::kSlots);
-  const int at_once = Sh::kSlots / page, mine = slot & (page - 1), sub = slot / page;
+  const int lane = threadIdx.x & 31, u = lane % kUnits, sub = lane / kUnits;
   const int2 at = unit_pieces<D>(u, P.rope ? P.rope_dim : 0);
-  const long long head_step = (long long)A.page * D;
-  T* rows = P.bounds ? reinterpret_cast<T*>(smem) : nullptr;
-  unsigned char* work = smem + Sh::kBounds;
-  if (w.n <= page) {
-    // the next heads' rows are read while these are turned, stored and looked over
-    const bool on = mine < w.n;
-    const long long src = (long long)(w.first + mine) * A.kv_stride;
-    RowUnit<T, D> x0, x1;
-    if (on && h0 + sub < h1) x0.load(A, src + (long long)(h0 + sub) * D, at, u);
-    w.page = page_of(A, w.b, w.e0);                        // (the first rows are on their way)
-    if (w.page < 0) return;
-    const float* angles = on ? angles_of(P, w.first + mine, w.e0 + mine) : nullptr;
-    const long long dst = row_offset(A, w.page, 0, w.e0, D) + (long long)mine * D;
-    auto heads = [&](RowUnit<T, D>& x, RowUnit<T, D>& next, int hb) {
-      const int h = hb + sub;
-      if (on && h + at_once < h1) next.load(A, src + (long long)(h + at_once) * D, at, u);
-      if (on && h < h1) x.store(P, dst + h * head_step, at, u, angles, rows ? rows + (sub * A.page + w.old + mine) * Sh::kStride : nullptr);
-      if (!rows) return;
-      for (int r = mine; r < w.old && h < h1; r += page) {
-        const T* from = static_cast<const T*>(A.k_pool) + row_offset(A, w.page, h, r, D) + 16 * u;
-        Piece<T> a, b;
-        a.load(from);
-        b.load(from + 8);
-        a.store(rows + (sub * A.page + r) * Sh::kStride + 16 * u);
-        b.store(rows + (sub * A.page + r) * Sh::kStride + 16 * u + 8);
-      }
-      __syncthreads();
-      write_bounds<T, D>(P, [&](int s, int r, int c) { return *reinterpret_cast<const typename PairOf<T>::type*>(rows + (s * A.page + r) * Sh::kStride + 2 * c); },
-                         w.old + w.n, at_once, h1 - hb, work, (long long)w.page * A.n_kv_heads + hb);
-    };
-    for (int hb = h0; hb < h1; hb += 2 * at_once) {
-      heads(x0, x1, hb);
-      if (hb + at_once < h1) heads(x1, x0, hb + at_once);
+  struct Unit {
+    Piece<T> ka, kb, va, vb;
+    Turn angles;
+  } x0, x1;
+  auto load = [&](Unit& x, int r) {
+    if (r >= w.n) return;
+    x.angles.load(angles_of(P, w.first + r, w.e0 + r), u, P.rope_dim, P.paired);
+    const long long src = (long long)(w.first + r) * A.kv_stride + (long long)h * D;
+    x.ka.load(static_cast<const T*>(A.k) + src + 8 * at.x);
+    x.kb.load(static_cast<const T*>(A.k) + src + 8 * at.y);
+    x.va.load(static_cast<const T*>(A.v) + src + 16 * u);
+    x.vb.load(static_cast<const T*>(A.v) + src + 16 * u + 8);
+  };
+  load(x0, sub);
+  const int page = page_of(A, w.b, w.e0);                  // (the first rows are on their way)
+  if (page < 0) return;
+  const long long dst = row_offset(A, page, h, w.e0, D);
+  Pair up[8], down[8];                                     // of pieces at.x and at.y
+  {
+    const float2 least = make_float2(-INFINITY, -INFINITY), most = make_float2(INFINITY, INFINITY);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (sizeof(T) == 2) { up[i] = __float22bfloat162_rn(least); down[i] = __float22bfloat162_rn(most); }
+      else { up[i] = least; down[i] = most; }
     }
-    return;
   }
-  // a page of more rows than threads for them: one head at a time
-  w.page = page_of(A, w.b, w.e0);
-  if (w.page < 0) return;
-  const long long dst0 = row_offset(A, w.page, 0, w.e0, D);
-  for (int h = h0; h < h1; ++h) {
-    for (int r = mine; r < w.n; r += page) {
-      RowUnit<T, D> x;
-      x.load(A, (long long)(w.first + r) * A.kv_stride + (long long)h * D, at, u);
-      x.store(P, dst0 + (long long)r * D + h * head_step, at, u, angles_of(P, w.first + r, w.e0 + r), rows ? rows + (w.old + r) * Sh::kStride : nullptr);
+  auto look = [&](const Piece<T>& a, const Piece<T>& b) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const Pair y = reinterpret_cast<const Pair*>(i < 4 ? a.w : b.w)[i & 3];
+      up[i] = pair_max(up[i], y);
+      down[i] = pair_min(down[i], y);
     }
-    if (!rows) continue;
-    for (int r = mine; r < w.old; r += page) {
-      const T* from = static_cast<const T*>(A.k_pool) + row_offset(A, w.page, h, r, D) + 16 * u;
-      Piece<T> a, b;
-      a.load(from);
-      b.load(from + 8);
-      a.store(rows + r * Sh::kStride + 16 * u);
-      b.store(rows + r * Sh::kStride + 16 * u + 8);
+  };
+  auto store = [&](const Unit& x, int r) {
+    if (r >= w.n) return;
+    Row8 a = x.ka.row(), b = x.kb.row();
+    x.angles.turn_unit(a, b, P.paired);
+    Piece<T> pa, pb;
+    store8(reinterpret_cast<T*>(pa.w), a);
+    store8(reinterpret_cast<T*>(pb.w), b);
+    const long long to = dst + (long long)r * D;
+    pa.store(static_cast<T*>(A.k_pool) + to + 8 * at.x);
+    pb.store(static_cast<T*>(A.k_pool) + to + 8 * at.y);
+    x.va.store(static_cast<T*>(A.v_pool) + to + 16 * u);
+    x.vb.store(static_cast<T*>(A.v_pool) + to + 16 * u + 8);
+    if (P.bounds) look(pa, pb);
+  };
+  if (P.bounds) {
+    constexpr int kSteps = sizeof(T) == 2 ? 4 : 2;         // entries of the page that are there already
+    for (int base = sub; base < w.old; base += kSteps * kRows) {
+      Piece<T> a[kSteps], b[kSteps];
+#pragma unroll
+      for (int k = 0; k < kSteps; ++k) {
+        const T* from = static_cast<const T*>(A.k_pool) + row_offset(A, page, h, min(base + k * kRows, w.old - 1), D);      // (one twice: no matter)
+        a[k].load(from + 8 * at.x);
+        b[k].load(from + 8 * at.y);
+      }
+#pragma unroll
+      for (int k = 0; k < kSteps; ++k) look(a[k], b[k]);
     }
-    __syncthreads();
-    write_bounds<T, D>(P, [&](int, int r, int c) { return *reinterpret_cast<const typename PairOf<T>::type*>(rows + r * Sh::kStride + 2 * c); }, w.old + w.n, 1, 1, work,
-                       (long long)w.page * A.n_kv_heads + h);
+  }
+  if constexpr (sizeof(T) == 2) {
+    for (int r = sub; r < w.n; r += 2 * kRows) {
+      load(x1, r + kRows);
+      store(x0, r);
+      load(x0, r + 2 * kRows);
+      store(x1, r + kRows);
+    }
+  } else {
+    // (two fp32 rows would not fit into the registers)
+    for (int r = sub; r < w.n; r += kRows) {
+      store(x0, r);
+      load(x0, r + kRows);
+    }
+  }
+  if (!P.bounds) return;
+  __syncwarp();
+  float most = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+#pragma unroll
+    for (int off = kUnits; off < 32; off <<= 1) {
+      up[i] = pair_max(up[i], pair_shuffle(up[i], off));
+      down[i] = pair_min(down[i], pair_shuffle(down[i], off));
+    }
+    const float2 a = pair_floats(up[i]), b = pair_floats(down[i]);
+    most = fmaxf(most, fmaxf(fmaxf(fabsf(a.x), fabsf(a.y)), fmaxf(fabsf(b.x), fabsf(b.y))));
+  }
+#pragma unroll
+  for (int off = 1; off < kUnits; off <<= 1) most = fmaxf(most, __shfl_xor_sync(~0u, most, off));
+  const BoundScale q = bound_scale(most);
+  const long long chunk = (long long)page * A.n_kv_heads + h;
+  // the rows' lanes share the writing: largest and least of piece at.x, of piece at.y
+  if (sub < 4) {
+    uint32_t word[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 hi = pair_floats(sub & 2 ? up[4 + i] : up[i]), lo = pair_floats(sub & 2 ? down[4 + i] : down[i]);
+      const uint32_t two = sub & 1 ? q.down(lo.x) | q.down(lo.y) << 8 : q.up(hi.x) | q.up(hi.y) << 8;
+      word[i / 2] |= two << 16 * (i & 1);
+    }
+    *reinterpret_cast<uint2*>(P.bounds + (chunk * 2 + (sub & 1)) * D + 8 * (sub & 2 ? at.y : at.x)) = make_uint2(word[0], word[1]);
+    if (lane == 0) P.bound_scale[chunk] = q.scale;
   }
 }
 
@@ -386,29 +429,31 @@ __device__ __forceinline__ void pack_group(const float (&x)[32], uint32_t (&word
 }
 
 template <typename T, int D>
-__device__ __forceinline__ void append_part4(const AppendParams& P, PagePart w, int h0, int h1, unsigned char* smem) {
-  using Sh = RowsShape<T, D>;
+__device__ __forceinline__ void append_part4(const AppendParams& P, const PagePart& w, int h0, int h1, unsigned char* smem) {
+  using Sh = RowsShape<D>;
   using Row = Kv4Row<D>;
   using R4 = Rows4Shape<D>;
   constexpr int G = Row::kGroups;
   const PagedParams& A = P.A;
   float* keys = reinterpret_cast<float*>(smem);
   unsigned char* image = smem + Rows4Shape<D>::kKeys;      // codes [n][kCodes] and pairs [n][kPairs] of the keys, then of the values
-  float* work = reinterpret_cast<float*>(smem + Rows4Shape<D>::kKeys + 2 * Rows4Shape<D>::kImage);
+  float2* work = reinterpret_cast<float2*>(smem + Rows4Shape<D>::kKeys + 2 * Rows4Shape<D>::kImage);
   const int u = threadIdx.x % Sh::kUnits, slot = threadIdx.x / Sh::kUnits;
   const int2 at = unit_pieces<D>(u, P.rope ? P.rope_dim : 0);
   const int i0 = w.e0 & (A.page - 1);
   const long long chunk_bytes = (long long)A.page * Row::kBytes;
-  w.page = page_of(A, w.b, w.e0);
-  if (w.page < 0) return;
+  const int page = page_of(A, w.b, w.e0);
+  if (page < 0) return;
   for (int h = h0; h < h1; ++h) {
-    const long long chunk = (long long)w.page * A.n_kv_heads + h;
+    const long long chunk = (long long)page * A.n_kv_heads + h;
     unsigned char* kc = static_cast<unsigned char*>(A.k_pool) + chunk * chunk_bytes;
     unsigned char* vc = static_cast<unsigned char*>(A.v_pool) + chunk * chunk_bytes;
     for (int r = slot; r < w.n; r += Sh::kSlots) {
       const T* src = static_cast<const T*>(A.k) + (long long)(w.first + r) * A.kv_stride + (long long)h * D;
       Row8 a = load8(src + 8 * at.x), b = load8(src + 8 * at.y);
-      turn_unit(a, b, angles_of(P, w.first + r, w.e0 + r), u, P.rope_dim, P.paired);
+      Turn angles;
+      angles.load(angles_of(P, w.first + r, w.e0 + r), u, P.rope_dim, P.paired);
+      angles.turn_unit(a, b, P.paired);
       store8(keys + R4::at(w.old + r, 8 * at.x), a);
       store8(keys + R4::at(w.old + r, 8 * at.y), b);
     }
@@ -477,15 +522,38 @@ __device__ __forceinline__ void append_part4(const AppendParams& P, PagePart w, 
           *reinterpret_cast<const uint32_t*>(image + (key ? 0 : Rows4Shape<D>::kImage) + w.n * Row::kCodes + e * 4);
     }
     if (P.bounds)
-      write_bounds<float, D>(P, [&](int, int r, int c) { return *reinterpret_cast<const float2*>(keys + R4::at(r, 2 * c)); }, w.old + w.n, 1, 1,
-                             reinterpret_cast<unsigned char*>(work), chunk);
+      write_bounds<D>(P, [&](int r, int c) { return *reinterpret_cast<const float2*>(keys + R4::at(r, 2 * c)); }, w.old + w.n, work, chunk);
     __syncthreads();
   }
 }
 
-// CTAs: queries first, then the slots for parts of pages, kv_splits CTAs each.
+// The part that slot `slot` stands for; n = 0: none.  count: of `n` sequences those for which f(b) holds, by the whole CTA or a warp.
+template <typename Count>
+__device__ __forceinline__ PagePart find_part(const PagedParams& A, int slot, Count count) {
+  PagePart w;
+  int part = 0;
+  w.b = slot;
+  w.n = 0;
+  if (A.q_start) {
+    // the last sequence whose first slot is not behind this one (offsets that do not rise are reported by seq_rows)
+    auto first = [&](int b) { return first_slot(min(max(A.q_start[b], 0), A.rows), b, A.page_shift); };
+    w.b = max(0, count([&](int b) { return first(b) <= slot; }) - 1);
+    part = slot - first(w.b);
+  }
+  const SeqRows s = seq_rows(A, w.b);
+  const int old = s.len - s.n, p = (max(old, 0) >> A.page_shift) + part;
+  if (part < 0 || s.n <= 0 || old < 0) return w;
+  w.e0 = max(old, p << A.page_shift);
+  w.n = max(0, min(s.len, (p + 1) << A.page_shift) - w.e0);
+  w.first = s.first + (w.e0 - old);
+  w.old = w.e0 & (A.page - 1);
+  return w;
+}
+
+// CTAs: queries first, then the slots for parts of pages: in 4 bits kv_splits CTAs each, else a warp for each kv head.  Two CTAs an SM, so
+// that the rows in flight and their angles stay in registers (three: 282 us for prompts of 2048..8191 tokens where two take 230).
 template <typename T, int D, bool FOUR>
-__global__ void __launch_bounds__(kRowsThreads, sizeof(T) == 2 && !FOUR ? 3 : 2) paged_rows_kernel(const __grid_constant__ AppendParams P) {
+__global__ void __launch_bounds__(kRowsThreads, 2) paged_rows_kernel(const __grid_constant__ AppendParams P) {
   extern __shared__ __align__(16) unsigned char smem[];
   griddep_launch();
   griddep_wait();
@@ -494,32 +562,25 @@ __global__ void __launch_bounds__(kRowsThreads, sizeof(T) == 2 && !FOUR ? 3 : 2)
     turn_queries<T, D>(P, blockIdx.x, reinterpret_cast<int*>(smem));
     return;
   }
-  const int k = blockIdx.x - P.q_blocks, slot = k / P.kv_splits, h0 = k % P.kv_splits * P.kv_heads, h1 = min(A.n_kv_heads, h0 + P.kv_heads);
-  PagePart w;
-  int part = 0;
-  if (A.q_start) {
-    // the last sequence whose first slot is not behind this one (offsets that do not rise are reported by seq_rows)
-    int below = 0;
-    for (int base = 0; base < A.batch; base += kRowsThreads) {
-      const int b = base + threadIdx.x;
-      below += __syncthreads_count(b < A.batch && first_slot(min(max(A.q_start[min(b, A.batch)], 0), A.rows), b, A.page_shift) <= slot);
-    }
-    w.b = max(0, below - 1);
-    part = slot - first_slot(min(max(A.q_start[w.b], 0), A.rows), w.b, A.page_shift);
+  const int k = (int)blockIdx.x - P.q_blocks;
+  if constexpr (FOUR) {
+    const PagePart w = find_part(A, k / P.kv_splits, [&](auto f) {
+      int n = 0;
+      for (int base = 0; base < A.batch; base += kRowsThreads) n += __syncthreads_count(base + (int)threadIdx.x < A.batch && f(base + threadIdx.x));
+      return n;
+    });
+    const int h0 = k % P.kv_splits * P.kv_heads;
+    if (w.n > 0) append_part4<T, D>(P, w, h0, min(A.n_kv_heads, h0 + P.kv_heads), smem);
   } else {
-    w.b = slot;
+    const int warp = k * (kRowsThreads / 32) + (threadIdx.x >> 5), slot = warp / A.n_kv_heads;
+    if (slot >= P.kv_slots) return;
+    const PagePart w = find_part(A, slot, [&](auto f) {
+      int n = 0;
+      for (int base = 0; base < A.batch; base += 32) n += __popc(__ballot_sync(~0u, base + (int)(threadIdx.x & 31) < A.batch && f(base + (threadIdx.x & 31))));
+      return n;
+    });
+    if (w.n > 0) append_head<T, D>(P, w, warp % A.n_kv_heads);
   }
-  const SeqRows s = seq_rows(A, w.b);
-  const int old = s.len - s.n, p = (max(old, 0) >> A.page_shift) + part;
-  if (part < 0 || s.n <= 0 || old < 0) return;
-  w.e0 = max(old, p << A.page_shift);
-  w.n = min(s.len, (p + 1) << A.page_shift) - w.e0;
-  if (w.n <= 0) return;
-  w.first = s.first + (w.e0 - old);
-  w.old = w.e0 & (A.page - 1);
-  w.page = -1;
-  if constexpr (FOUR) append_part4<T, D>(P, w, h0, h1, smem);
-  else append_part<T, D>(P, w, h0, h1, smem);
 }
 
 // ------------------------------------------------------------------------------------------------
