@@ -614,26 +614,31 @@ __global__ void __launch_bounds__(kRowsThreads) paged_expand_kernel(const __grid
   const int bh = blockIdx.x / P.blocks, b = bh / A.n_kv_heads, h = bh % A.n_kv_heads, first = blockIdx.x % P.blocks * 64;
   const int len = clamped_len(A, b), c = threadIdx.x % kWords, r0 = first + threadIdx.x / kWords;
   if (first >= len) return;
-  const long long chunk_bytes = (long long)A.page * Row::kBytes;
+  // 16 entries share a page on both sides: where the head's rows of it start, -1 for none
+  __shared__ long long from_at[4], to_at[4];
+  if (threadIdx.x < 4) {
+    const int i = first + threadIdx.x * 16, col = i >> P.to_shift;
+    from_at[threadIdx.x] = to_at[threadIdx.x] = -1;
+    if (i < len) {
+      const int pg = col < P.to_width ? P.to_table[(long long)b * P.to_width + col] : -1, from = page_of(A, b, i);
+      if ((unsigned)pg < (unsigned)P.to_pages) to_at[threadIdx.x] = (((long long)pg * A.n_kv_heads + h) << P.to_shift) * D;
+      else flag_bad_table(A.status);
+      if (from >= 0) from_at[threadIdx.x] = ((long long)from * A.n_kv_heads + h) * A.page * Row::kBytes;
+    }
+  }
+  __syncthreads();
   // of a key: channels 8c .. 8c + 7; of a value: channels 4u .. 4u + 3 of groups g0 and g0 + 1
   const int g = c / 4, u = c / (Row::kGroups / 2), g0 = 2 * (c % (Row::kGroups / 2));
   uint32_t key[kSteps], key_pair[kSteps], value[kSteps], value_pairs[kSteps];
   long long to[kSteps];
 #pragma unroll
   for (int k = 0; k < kSteps; ++k) {
-    const int i = r0 + k * kRows;
-    to[k] = -1;
+    const int i = r0 + k * kRows, group = (i - first) >> 4;
+    const long long base = to_at[group], at = from_at[group];
+    to[k] = i < len && base >= 0 ? base + (i & (P.to_page - 1)) * D : -1;
     key[k] = key_pair[k] = value[k] = value_pairs[k] = 0;
-    if (i >= len) continue;
-    const int col = i >> P.to_shift, pg = col < P.to_width ? P.to_table[(long long)b * P.to_width + col] : -1, from = page_of(A, b, i);
-    if ((unsigned)pg >= (unsigned)P.to_pages) {
-      flag_bad_table(A.status);
-      continue;
-    }
-    to[k] = ((((long long)pg * A.n_kv_heads + h) << P.to_shift) + (i & (P.to_page - 1))) * D;
-    if (from < 0) continue;                                // counts as zeros
+    if (to[k] < 0 || at < 0) continue;                     // (a bad page counts as zeros)
     const int row = i & (A.page - 1);
-    const long long at = ((long long)from * A.n_kv_heads + h) * chunk_bytes;
     const unsigned char* kc = static_cast<const unsigned char*>(A.k_pool) + at;
     const unsigned char* vc = static_cast<const unsigned char*>(A.v_pool) + at;
     key[k] = *reinterpret_cast<const uint32_t*>(kc + Row::k_piece(row, g) + (c & 3) * 4);
