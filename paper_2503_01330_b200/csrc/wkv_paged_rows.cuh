@@ -614,44 +614,48 @@ __global__ void __launch_bounds__(kRowsThreads) paged_expand_kernel(const __grid
   const int bh = blockIdx.x / P.blocks, b = bh / A.n_kv_heads, h = bh % A.n_kv_heads, first = blockIdx.x % P.blocks * 64;
   const int len = clamped_len(A, b), c = threadIdx.x % kWords, r0 = first + threadIdx.x / kWords;
   if (first >= len) return;
-  // 16 entries share a page on both sides: where the head's rows of it start, -1 for none
-  __shared__ long long from_at[4], to_at[4];
+  // 16 entries share a page on both sides: where their codes, pairs and values start, -1 for none
+  __shared__ long long codes_at[4], pairs_at[4], to_at[4];
   if (threadIdx.x < 4) {
     const int i = first + threadIdx.x * 16, col = i >> P.to_shift;
-    from_at[threadIdx.x] = to_at[threadIdx.x] = -1;
+    codes_at[threadIdx.x] = to_at[threadIdx.x] = -1;
     if (i < len) {
-      const int pg = col < P.to_width ? P.to_table[(long long)b * P.to_width + col] : -1, from = page_of(A, b, i);
-      if ((unsigned)pg < (unsigned)P.to_pages) to_at[threadIdx.x] = (((long long)pg * A.n_kv_heads + h) << P.to_shift) * D;
+      const int pg = col < P.to_width ? P.to_table[(long long)b * P.to_width + col] : -1, from = page_of(A, b, i), row = i & (A.page - 1);
+      if ((unsigned)pg < (unsigned)P.to_pages) to_at[threadIdx.x] = ((((long long)pg * A.n_kv_heads + h) << P.to_shift) + (i & (P.to_page - 1))) * D;
       else flag_bad_table(A.status);
-      if (from >= 0) from_at[threadIdx.x] = ((long long)from * A.n_kv_heads + h) * A.page * Row::kBytes;
+      const long long chunk = ((long long)from * A.n_kv_heads + h) * A.page * Row::kBytes;
+      if (from >= 0) codes_at[threadIdx.x] = chunk + row * Row::kCodes;
+      pairs_at[threadIdx.x] = chunk + Row::pairs(A.page, row);
     }
   }
   __syncthreads();
-  // of a key: channels 8c .. 8c + 7; of a value: channels 4u .. 4u + 3 of groups g0 and g0 + 1
-  const int g = c / 4, u = c / (Row::kGroups / 2), g0 = 2 * (c % (Row::kGroups / 2));
+  // of a key: channels 8c .. 8c + 7; of a value: channels 4u .. 4u + 3 of groups g0 and g0 + 1; of the row's 16 (swizzles depend on no more)
+  const int g = c / 4, u = c / (Row::kGroups / 2), g0 = 2 * (c % (Row::kGroups / 2)), in16 = (threadIdx.x / kWords) & 15;
+  const unsigned char* kc = static_cast<const unsigned char*>(A.k_pool) + Row::k_piece(in16, g) + (c & 3) * 4;
+  const unsigned char* kp = static_cast<const unsigned char*>(A.k_pool) + in16 * Row::kPairs + 2 * g;
+  const unsigned char* vc = static_cast<const unsigned char*>(A.v_pool) + Row::v_unit(in16, g0, u);
+  const unsigned char* vp = static_cast<const unsigned char*>(A.v_pool) + in16 * Row::kPairs + 2 * g0;
   uint32_t key[kSteps], key_pair[kSteps], value[kSteps], value_pairs[kSteps];
   long long to[kSteps];
 #pragma unroll
   for (int k = 0; k < kSteps; ++k) {
     const int i = r0 + k * kRows, group = (i - first) >> 4;
-    const long long base = to_at[group], at = from_at[group];
-    to[k] = i < len && base >= 0 ? base + (i & (P.to_page - 1)) * D : -1;
+    const long long base = to_at[group], at = codes_at[group];
+    to[k] = i < len && base >= 0 ? base + in16 * D : -1;
     key[k] = key_pair[k] = value[k] = value_pairs[k] = 0;
     if (to[k] < 0 || at < 0) continue;                     // (a bad page counts as zeros)
-    const int row = i & (A.page - 1);
-    const unsigned char* kc = static_cast<const unsigned char*>(A.k_pool) + at;
-    const unsigned char* vc = static_cast<const unsigned char*>(A.v_pool) + at;
-    key[k] = *reinterpret_cast<const uint32_t*>(kc + Row::k_piece(row, g) + (c & 3) * 4);
-    key_pair[k] = *reinterpret_cast<const uint16_t*>(kc + Row::pairs(A.page, row) + 2 * g);
-    value[k] = *reinterpret_cast<const uint32_t*>(vc + Row::v_unit(row, g0, u));
-    value_pairs[k] = *reinterpret_cast<const uint32_t*>(vc + Row::pairs(A.page, row) + 2 * g0);
+    const long long pair_at = pairs_at[group];
+    key[k] = *reinterpret_cast<const uint32_t*>(kc + at);
+    key_pair[k] = *reinterpret_cast<const uint16_t*>(kp + pair_at);
+    value[k] = *reinterpret_cast<const uint32_t*>(vc + at);
+    value_pairs[k] = *reinterpret_cast<const uint32_t*>(vp + pair_at);
   }
 #pragma unroll
   for (int k = 0; k < kSteps; ++k) {
     if (to[k] < 0) continue;
     {
       const uint32_t s = __float_as_uint(kv4_scale(key_pair[k] & 255)), s2 = __byte_perm(s, s, 0x3232), z2 = __byte_perm(key_pair[k], 0x43u, 0x4141);
-      *reinterpret_cast<uint4*>(P.k_to + to[k] + 8 * c) =
+      *reinterpret_cast<uint4*>(P.k_to + 8 * c + to[k]) =
           make_uint4(kv4_values(key[k] & kLow, z2, s2), kv4_values(key[k] >> 4 & kLow, z2, s2), kv4_values(key[k] >> 8 & kLow, z2, s2), kv4_values(key[k] >> 12 & kLow, z2, s2));
     }
     {
@@ -660,7 +664,7 @@ __global__ void __launch_bounds__(kRowsThreads) paged_expand_kernel(const __grid
       uint32_t y[4];                                       // channel m of group g0 | of group g0 + 1
 #pragma unroll
       for (int m = 0; m < 4; ++m) y[m] = kv4_values(value[k] >> 4 * m & kLow, z2, s2);
-      __nv_bfloat16* out = P.v_to + to[k] + 32 * g0 + 4 * u;
+      __nv_bfloat16* out = P.v_to + 32 * g0 + 4 * u + to[k];
       *reinterpret_cast<uint2*>(out) = make_uint2(__byte_perm(y[0], y[1], 0x5410), __byte_perm(y[2], y[3], 0x5410));
       *reinterpret_cast<uint2*>(out + 32) = make_uint2(__byte_perm(y[0], y[1], 0x7632), __byte_perm(y[2], y[3], 0x7632));
     }
