@@ -27,108 +27,179 @@ struct ChooseParams {
 
 constexpr int kChooseThreads = 256, kChooseWarps = kChooseThreads / 32;
 constexpr int kChooseHeld = 8;         // scores per thread that stay in registers
+constexpr int kChooseBins = 1024;
 
-// As the eviction's order of scores: -0 like +0, NaN above all numbers; pages that are taken anyway above that.
-constexpr uint32_t kTakenKey = 0xffffffffu;
+// As the eviction's order of scores: -0 like +0, NaN above all numbers.
 __device__ __forceinline__ uint32_t page_key(float x) {
   const uint32_t u = __float_as_uint(x + 0.f);
   return x != x ? 0xfffffffeu : u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
-// The `want` largest of n keys, in order of their index, of equal keys the lowest indexes.  A thread owns `per` consecutive ones: in
-// registers (HELD), where there are few, or looked up each time.  sums: [2][3 * warps].
-template <bool HELD, typename KeyAt>
-__device__ __forceinline__ void choose(KeyAt key_at, int per, int n, int want, int32_t* to, int* sums) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, first = tid * per;
-  const int count = min(per, max(0, n - first));
-  uint32_t held[kChooseHeld];
+struct ChooseShared {
+  int bins[kChooseBins];
+  unsigned long long candidates[kChooseThreads];
+  unsigned long long cutoff;
+  float least[kChooseWarps], most[kChooseWarps];
+  int sums[2][3 * kChooseWarps];
+  int bin, above, n_candidates;
+};
+
+// Exclusive sum over the threads; total: of all.  `at`: the warps' sums.  One barrier.
+__device__ __forceinline__ int sum_before(int x, int* at, int& total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int y = x;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const int z = __shfl_up_sync(~0u, y, off);
+    if (lane >= off) y += z;
+  }
+  if (lane == 31) at[warp] = y;
+  __syncthreads();
+  total = 0;
+  y -= x;
+#pragma unroll
+  for (int w = 0; w < kChooseWarps; ++w) {
+    if (w < warp) y += at[w];
+    total += at[w];
+  }
+  return y;
+}
+
+// Order of pages: better score, then lower index.
+__device__ __forceinline__ unsigned long long page_rank(float x, int i) { return (unsigned long long)page_key(x) << 32 | (uint32_t)~i; }
+
+// The cutoff among keys that do not spread well (all equal, not finite, far outliers): the `want`-th best of n, two bits of the key a round.
+template <typename Each>
+__device__ __forceinline__ unsigned long long cutoff_by_digits(Each each, int n, int want, ChooseShared& sh) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  unsigned long long least = 0;
+  int at_least = n, turn = 0;
+#pragma unroll 1
+  for (int shift = 62; shift >= 0 && at_least != want; shift -= 2) {
+    const unsigned long long k1 = least + (1ull << shift), k2 = least + (2ull << shift), k3 = least + (3ull << shift);
+    int c1 = 0, c2 = 0, c3 = 0;
+    each([&](int i, float x) {
+      const unsigned long long k = page_rank(x, i);
+      c1 += k >= k1; c2 += k >= k2; c3 += k >= k3;
+    });
+    int* mine = sh.sums[turn];
+    turn ^= 1;
+    c1 = __reduce_add_sync(~0u, c1); c2 = __reduce_add_sync(~0u, c2); c3 = __reduce_add_sync(~0u, c3);
+    if (lane == 0) { mine[warp] = c1; mine[kChooseWarps + warp] = c2; mine[2 * kChooseWarps + warp] = c3; }
+    __syncthreads();
+    c1 = c2 = c3 = 0;
+#pragma unroll
+    for (int w = 0; w < kChooseWarps; ++w) { c1 += mine[w]; c2 += mine[kChooseWarps + w]; c3 += mine[2 * kChooseWarps + w]; }
+    if (c3 >= want) { least = k3; at_least = c3; }
+    else if (c2 >= want) { least = k2; at_least = c2; }
+    else if (c1 >= want) { least = k1; at_least = c1; }
+  }
+  __syncthreads();
+  return least;
+}
+
+// The `want` best of n pages (more than that), the n_taken with taken(i) among them in any case, in order of their index.  A thread owns `per`
+// consecutive ones: their scores in registers (HELD), where they are few, or looked up each time.  Scores are counted in bins of equal
+// width between the least and the largest; the bin that holds the last one to be chosen is settled by comparing its few pages with
+// one another (digit by digit over all pages where they are many: 9 us for 2048 pages, this one 2).
+template <bool HELD, typename ScoreAt, typename Taken>
+__device__ __forceinline__ void choose(ScoreAt score_at, Taken taken, int n_taken, int per, int n, int want, int32_t* to, ChooseShared& sh) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, first = tid * per, count = min(per, max(0, n - first));
+  float held[kChooseHeld];
   if constexpr (HELD) {
 #pragma unroll
-    for (int i = 0; i < kChooseHeld; ++i) held[i] = i < count ? key_at(first + i) : 0u;
+    for (int i = 0; i < kChooseHeld; ++i) held[i] = i < count ? score_at(first + i) : 0.f;
   }
-  auto each = [&](auto f) {                                // f(index, key) for this thread's keys
+  auto all = [&](auto f) {                                 // f(index, score) for this thread's pages
     if constexpr (HELD) {
 #pragma unroll
       for (int i = 0; i < kChooseHeld; ++i)
         if (i < count) f(first + i, held[i]);
     } else {
-      for (int i = 0; i < count; ++i) f(first + i, key_at(first + i));
+      for (int i = 0; i < count; ++i) f(first + i, score_at(first + i));
     }
   };
-  // the want-th largest key, two bits a round; done as soon as exactly `want` keys are not below the digits found
-  uint32_t least = 0;
-  int at_least = n, turn = 0;
-#pragma unroll 1
-  for (int shift = 30; shift >= 0 && at_least != want; shift -= 2) {
-    const uint32_t k1 = least + (1u << shift), k2 = least + (2u << shift), k3 = least + (3u << shift);
-    int c1 = 0, c2 = 0, c3 = 0;
-    each([&](int, uint32_t k) { c1 += k >= k1; c2 += k >= k2; c3 += k >= k3; });
-    int* mine = sums + turn * 3 * kChooseWarps;
-    turn ^= 1;
-    if constexpr (HELD) {
-      const int c = __reduce_add_sync(~0u, c1 | c2 << 10 | c3 << 20);     // 256 of a warp's keys at most
-      if (lane == 0) mine[warp] = c;
-      __syncthreads();
-      c1 = c2 = c3 = 0;
+  auto each = [&](auto f) { all([&](int i, float x) { if (!taken(i)) f(i, x); }); };
+  float least = INFINITY, most = -INFINITY;
+  bool odd = false;
+  each([&](int, float x) {
+    least = fminf(least, x);
+    most = fmaxf(most, x);
+    odd = odd || !(fabsf(x) < INFINITY);
+  });
 #pragma unroll
-      for (int w = 0; w < kChooseWarps; ++w) { c1 += mine[w] & 1023; c2 += mine[w] >> 10 & 1023; c3 += mine[w] >> 20; }
-    } else {
-      c1 = __reduce_add_sync(~0u, c1); c2 = __reduce_add_sync(~0u, c2); c3 = __reduce_add_sync(~0u, c3);
-      if (lane == 0) { mine[warp] = c1; mine[kChooseWarps + warp] = c2; mine[2 * kChooseWarps + warp] = c3; }
-      __syncthreads();
-      c1 = c2 = c3 = 0;
+  for (int off = 16; off; off >>= 1) {
+    least = fminf(least, __shfl_xor_sync(~0u, least, off));
+    most = fmaxf(most, __shfl_xor_sync(~0u, most, off));
+  }
+  if (lane == 0) { sh.least[warp] = least; sh.most[warp] = most; }
+  for (int i = tid; i < kChooseBins; i += kChooseThreads) sh.bins[i] = 0;
+  if (tid == 0) sh.n_candidates = 0;
+  odd = __syncthreads_or(odd);
+  want -= n_taken;
 #pragma unroll
-      for (int w = 0; w < kChooseWarps; ++w) { c1 += mine[w]; c2 += mine[kChooseWarps + w]; c3 += mine[2 * kChooseWarps + w]; }
+  for (int w = 0; w < kChooseWarps; ++w) { least = fminf(least, sh.least[w]); most = fmaxf(most, sh.most[w]); }
+  const float range = most - least, per_bin = range > 0.f && range < INFINITY ? kChooseBins / range : 0.f;
+  odd = odd || !(per_bin > 0.f && per_bin < INFINITY);
+  unsigned long long cutoff = ~0ull;                       // want = 0: none but the taken ones
+  // (x - least, times a constant, cut to a whole number: each step keeps the order)
+  auto bin_of = [&](float x) { return min(kChooseBins - 1, (int)((x - least) * per_bin)); };
+  bool settled = want == 0;
+  if (want > 0 && !odd) {
+    each([&](int, float x) { atomicAdd(&sh.bins[bin_of(x)], 1); });
+    __syncthreads();
+    constexpr int kMine = kChooseBins / kChooseThreads;    // bins of this thread, from the top down
+    int mine[kMine], sum = 0, total;
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) { mine[i] = sh.bins[kChooseBins - 1 - (tid * kMine + i)]; sum += mine[i]; }
+    int before = sum_before(sum, sh.sums[1], total);
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      if (before < want && want <= before + mine[i]) { sh.bin = kChooseBins - 1 - (tid * kMine + i); sh.above = before; }
+      before += mine[i];
     }
-    if (c3 >= want) { least = k3; at_least = c3; }
-    else if (c2 >= want) { least = k2; at_least = c2; }
-    else if (c1 >= want) { least = k1; at_least = c1; }
+    __syncthreads();
+    const int bin = sh.bin, need = want - sh.above, in_bin = sh.bins[bin];
+    if (in_bin <= kChooseThreads) {
+      each([&](int i, float x) { if (bin_of(x) == bin) sh.candidates[atomicAdd(&sh.n_candidates, 1)] = page_rank(x, i); });
+      __syncthreads();
+      if (tid < in_bin) {
+        const unsigned long long me = sh.candidates[tid];
+        int better = 0;
+        for (int k = 0; k < in_bin; ++k) better += sh.candidates[k] > me;
+        if (better == need - 1) sh.cutoff = me;
+      }
+      __syncthreads();
+      cutoff = sh.cutoff;
+      settled = true;
+    }
   }
-  // keys above `least`, then of those equal to it the first ones: places by exclusive sums over the threads
-  int above = 0, equal = 0;
-  each([&](int, uint32_t k) { above += k > least; equal += k == least; });
-  int a = above, e = equal;
-#pragma unroll
-  for (int off = 1; off < 32; off <<= 1) {
-    const int x = __shfl_up_sync(~0u, a, off), y = __shfl_up_sync(~0u, e, off);
-    if (lane >= off) { a += x; e += y; }
-  }
-  int* mine = sums + turn * 3 * kChooseWarps;
-  if (lane == 31) { mine[warp] = a; mine[kChooseWarps + warp] = e; }
-  __syncthreads();
-  int total_above = 0;
-  a -= above;
-  e -= equal;
-#pragma unroll
-  for (int w = 0; w < kChooseWarps; ++w) {
-    if (w < warp) { a += mine[w]; e += mine[kChooseWarps + w]; }
-    total_above += mine[w];
-  }
-  const int ties = want - total_above;
-  each([&](int i, uint32_t k) {
-    if (k > least || (k == least && e < ties)) to[a + min(e, ties)] = i;
-    a += k > least;
-    e += k == least;
+  if (!settled) cutoff = cutoff_by_digits(each, n - n_taken, want, sh);
+  int chosen = 0, total;
+  all([&](int i, float x) { chosen += taken(i) || (want > 0 && page_rank(x, i) >= cutoff); });
+  int at = sum_before(chosen, sh.sums[0], total);
+  all([&](int i, float x) {
+    if (taken(i) || (want > 0 && page_rank(x, i) >= cutoff)) to[at++] = i;
   });
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kChooseThreads) paged_choose_kernel(const __grid_constant__ ChooseParams P) {
+__global__ void __launch_bounds__(kChooseThreads, 4) paged_choose_kernel(const __grid_constant__ ChooseParams P) {
   __shared__ __align__(16) int8_t code[2][D];
   __shared__ float part[kChooseWarps];
-  __shared__ int sums[6 * kChooseWarps];
+  __shared__ ChooseShared sh;
+  __shared__ float near[kChooseHeld * kChooseThreads];     // the scores of a lane that one CTA has to itself
   __shared__ int is_last;
   griddep_launch();
   griddep_wait();
   const PagedParams& A = P.A;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int lane_no = blockIdx.x / P.splits, split = blockIdx.x % P.splits, b = lane_no / A.n_kv_heads, h = lane_no % A.n_kv_heads;
-  const int len = clamped_len(A, b), n = (len + A.page - 1) >> A.page_shift;
-  // the query's codes
+  // the query's codes (its row is there, whatever the length)
   {
     const int G = A.n_q_heads / A.n_kv_heads;
     float up = 0.f, down = 0.f;
-    if (tid < D && n > 0) {
+    if (tid < D) {
       const T* q = static_cast<const T*>(A.q) + (long long)b * A.q_stride + (long long)h * G * D + tid;
       for (int g = 0; g < G; ++g) {
         const float x = (float)q[g * D];
@@ -151,6 +222,7 @@ __global__ void __launch_bounds__(kChooseThreads) paged_choose_kernel(const __gr
     }
     __syncthreads();
   }
+  const int len = clamped_len(A, b), n = (len + A.page - 1) >> A.page_shift;
   float* scores = P.page_scores + (long long)lane_no * P.page_score_stride;
   // scores: eight lanes a page, D / 8 channels each
   {
@@ -197,7 +269,11 @@ __global__ void __launch_bounds__(kChooseThreads) paged_choose_kernel(const __gr
         sum += __shfl_xor_sync(~0u, sum, 1);
         sum += __shfl_xor_sync(~0u, sum, 2);
         sum += __shfl_xor_sync(~0u, sum, 4);
-        if (sub == 0 && p < p1) scores[p] = __fmul_rn((float)sum, scale[k]);
+        if (sub == 0 && p < p1) {
+          const float x = __fmul_rn((float)sum, scale[k]);
+          scores[p] = x;
+          if (p < kChooseHeld * kChooseThreads) near[p] = x;
+        }
       }
     }
   }
@@ -221,10 +297,12 @@ __global__ void __launch_bounds__(kChooseThreads) paged_choose_kernel(const __gr
     for (int i = tid; i < n; i += kChooseThreads) to[i] = i;
     return;
   }
-  auto key_of = [&](int p) { return p < P.sink || p >= n - P.recent ? kTakenKey : page_key(__ldcg(scores + p)); };
+  const bool alone = P.splits == 1 && n <= kChooseHeld * kChooseThreads;
+  auto score_at = [&](int p) { return alone ? near[p] : __ldcg(scores + p); };
+  auto taken = [&](int p) { return p < P.sink || p >= n - P.recent; };
   const int per = (n + kChooseThreads - 1) / kChooseThreads;
-  if (per <= kChooseHeld) choose<true>(key_of, per, n, want, to, sums);
-  else choose<false>(key_of, per, n, want, to, sums);
+  if (per <= kChooseHeld) choose<true>(score_at, taken, P.sink + P.recent, per, n, want, to, sh);
+  else choose<false>(score_at, taken, P.sink + P.recent, per, n, want, to, sh);
 }
 
 }  // namespace wkv
