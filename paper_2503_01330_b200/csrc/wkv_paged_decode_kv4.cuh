@@ -8,10 +8,9 @@
 // takes exactly.  Scales and zero points stay outside of the products:
 //   q.k_i  = sum_g s_ig (q_g.n_ig - z_ig sum q_g)
 //   o_g    = sum_i (p_i s_ig) n_ig - sum_i (p_i s_ig) z_ig   the weights p s in fp16, the same rounded ones in both sums
-// A query's group of 32 channels (half of one for 64-channel heads with one or two heads a key) becomes whole numbers by a power of two that
-// brings its largest to [2^13, 2^14): bf16 channels down to 2^-6 of it stay exact, smaller ones are off by up to 2^-14 of it.  p and p s are
-// rounded to fp16, 2^-11 each, together a quarter of what rounding the output to bf16 costs.  The weights are kept in fp16's range
-// by a power of two that follows the largest value scale seen.
+// A query head becomes whole numbers by a power of two that brings its largest channel to [2^13, 2^14): bf16 channels down to 2^-6 of it stay
+// exact, smaller ones are off by up to 2^-14 of it.  p and p s are rounded to fp16, 2^-11 each, together a quarter of what
+// rounding the output to bf16 costs.  The weights are kept in fp16's range by a power of two that follows the largest value scale seen.
 // (Keys as fp16 subnormals: 163 us of arithmetic in the 16 x 8192..16384 case, masks at half rate above all.  As e4m3 numbers the matrix
 // instruction is split into fp16 ones with conversions.)
 //
@@ -120,7 +119,7 @@ struct Kv4Warp {
   static constexpr int kQuery = kHeads * kGroups / 2 * 32 * 16;          // bytes
   static constexpr float kHeadroom = 14.f;                 // weights are held times 2^14: fp16 numbers down to 2^-28
   int qsum[kHeads][kMasked ? 1 : kGroups];     // sum of the quarter's, or a group's, channels
-  float factor[kHeads][kMasked ? 1 : kGroups]; // whole numbers -> base-2 logits
+  float factor[kHeads];        // whole numbers -> base-2 logits
   float o[kFrags][2][4];       // values' products: channels 4r + 2 half and + 1 of the column's group, columns 2j and 2j + 1
   float zo[kFrags][4];         // zero points' products: row r is the group of column r; rows 8 .. 15 are nothing
   float m[kHeads], l[kHeads];
@@ -161,31 +160,25 @@ struct Kv4Warp {
     for (int u = 0; u < kHeads; ++u) {
       // the head of column r of tile u, and of its channels those that meet this lane's codes
       const __nv_bfloat16* mine = qrow + (kMasked ? u : 4 * u + (r >> 1)) * D + (kMasked ? j * (D / 4) : 8 * j);
-      float x[kGroups][8], most[kGroups];
+      float x[kGroups][8], top = 0.f;
 #pragma unroll
       for (int t = 0; t < kGroups; ++t) {
         const uint4 y = *reinterpret_cast<const uint4*>(mine + (kMasked ? 8 : 32) * t);
         const uint32_t w[4] = {y.x, y.y, y.z, y.w};
-        most[t] = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) { x[t][2 * i] = __uint_as_float(w[i] << 16); x[t][2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) most[t] = fmaxf(most[t], x[t][i] == x[t][i] ? fabsf(x[t][i]) : INFINITY);
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, x[t][i] == x[t][i] ? fabsf(x[t][i]) : INFINITY);
       }
+      top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));      // of all quarters, or of the lanes that share a head's groups
+      top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
+      const int e = max(-100, min(100, 13 - ((int)(__float_as_uint(top) >> 23) - 127)));
+      const float up = pow2f(e), f = top < INFINITY ? scale_log2 * pow2f(-e) : __int_as_float(0x7fffffff);
+      factor[u] = kMasked ? f : __shfl_sync(~0u, f, 8 * j);
       int sum = 0;
 #pragma unroll
       for (int t = 0; t < kGroups; ++t) {
-        float top = most[t];
-        if constexpr (kMasked) {
-#pragma unroll
-          for (int k = 0; k < kGroups; ++k) top = fmaxf(top, most[k]);
-        } else {
-          top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
-          top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
-          sum = 0;
-        }
-        const int e = max(-100, min(100, 13 - ((int)(__float_as_uint(top) >> 23) - 127)));
-        const float up = pow2f(e), f = top < INFINITY ? scale_log2 * pow2f(-e) : __int_as_float(0x7fffffff);
+        if (!kMasked) sum = 0;
         // in the order of the codes' bytes: channels 0, 4, 1, 5 from the low halves of a word's bytes, 2, 6, 3, 7 from the high ones
         constexpr int kAt[8] = {0, 4, 1, 5, 2, 6, 3, 7};
         uint32_t word[2];
@@ -205,9 +198,6 @@ struct Kv4Warp {
           sum += __shfl_xor_sync(~0u, sum, 1);
           sum += __shfl_xor_sync(~0u, sum, 2);
           qsum[u][t] = __shfl_sync(~0u, sum, 8 * j);
-          factor[u][t] = __shfl_sync(~0u, f, 8 * j);
-        } else {
-          factor[u][0] = f;
         }
       }
       if constexpr (kMasked) qsum[u][0] = sum;
@@ -228,9 +218,9 @@ struct Kv4Warp {
     constexpr uint32_t kLow = 0x0f0f0f0fu;
     mma_m16n8k32_u8s8(d, a & kLow, b & kLow, a >> 4 & kLow, b >> 4 & kLow, q0, q1);
   }
-  // s (q.n - z sum q) of row half h, base-2 logits.
-  __device__ __forceinline__ static float part(const int (&d)[4], int h, float scale, uint32_t zero, int sum, float f) {
-    return scale * f * (float)(d[2 * h] * 256 + d[2 * h + 1] - (int)zero * sum);
+  // q.n - z sum q of row half h.
+  __device__ __forceinline__ static float part(const int (&d)[4], int h, uint32_t zero, int sum) {
+    return (float)(d[2 * h] * 256 + d[2 * h + 1] - (int)zero * sum);
   }
 
   // 32 entries of the stage at shared memory address `stage`, the halves' first ones entry[0] and entry[1]; ~entry: the page's number is
@@ -270,8 +260,8 @@ struct Kv4Warp {
           int d[4] = {};
 #pragma unroll
           for (int t = 0; t < kGroups; ++t) step(d, a[t], b[t], q[u][t][0], q[u][t][1]);
-          v[2 * sub][u] = part(d, 0, kv4_scale(pair0 & 255), pair0 >> 8, qsum[u][0], factor[u][0]);
-          v[2 * sub + 1][u] = part(d, 1, kv4_scale(pair1 & 255), pair1 >> 8, qsum[u][0], factor[u][0]);
+          v[2 * sub][u] = kv4_scale(pair0 & 255) * part(d, 0, pair0 >> 8, qsum[u][0]);
+          v[2 * sub + 1][u] = kv4_scale(pair1 & 255) * part(d, 1, pair1 >> 8, qsum[u][0]);
         }
       }
       // sums over the quarters: lane j keeps entry r + 8 (j % 2) of sub j / 2
@@ -312,8 +302,8 @@ struct Kv4Warp {
             step(d, a, b, q[u][g][0], q[u][g][1]);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-              x[2 * sub + h][u] += part(d, h, g & 1 ? scales[h][g / 2].y : scales[h][g / 2].x, __byte_perm(pairs[h][g / 2], 0u, g & 1 ? 0x4443 : 0x4441),
-                                        qsum[u][g], factor[u][g]);
+              x[2 * sub + h][u] = fmaf(g & 1 ? scales[h][g / 2].y : scales[h][g / 2].x,
+                                       part(d, h, __byte_perm(pairs[h][g / 2], 0u, g & 1 ? 0x4443 : 0x4441), qsum[u][g]), x[2 * sub + h][u]);
           }
         }
       }
@@ -323,6 +313,7 @@ struct Kv4Warp {
     for (int k = 0; k < kMine; ++k)
 #pragma unroll
       for (int c = 0; c < kHeads; ++c) {
+        x[k][c] *= factor[c];
         if constexpr (!EVERY) {
           const int e = (kMasked ? j >> 1 : k >> 1) ? entry1 : entry0, i = (e < 0 ? ~e : e) + r + 8 * (kMasked ? j & 1 : k & 1);
           x[k][c] = !s.sees(i) ? -INFINITY : e < 0 ? 0.f : x[k][c];

@@ -3,10 +3,9 @@
 What is specified operation by operation (codes, scales, zero points, bounds of pages, scores and choice of pages) is restated here in
 numpy binary32 and compared bit for bit.  The rest is compared with 64-bit arithmetic within (u = 2^-24, half a step of fp32):
   - a turned channel: two products and a sum, each rounded: 2u (|a cos| + |b sin|), then half a step of the storage type;
-  - a logit over 4-bit keys: products of whole numbers, exact but for the query's: a group of its channels (32; 16 in 64-channel heads
-    with one or two heads a key) becomes whole numbers with the largest in [2^13, 2^14), so a channel is off by half of 1, 2^-14 of the
-    group's largest: scale 2^-14 sum_g max|q_g| sum_c |k_c|.  Then fp32: |ds| <= 2 (d + 16) u T with T = scale sum_c |q_c| s (n_c + z)
-    is more than the few operations per group need;
+  - a logit over 4-bit keys: products of whole numbers, exact but for the query's: its channels become whole numbers with the head's largest
+    in [2^13, 2^14), so a channel is off by half of 1, 2^-14 of the largest: scale 2^-14 max|q| sum_c |k_c|.  Then fp32: |ds| <=
+    2 (d + 16) u T with T = scale sum_c |q_c| s (n_c + z) is more than the few operations per group need;
   - bf16 rows: weights go as bf16 high and low parts, 2^-9 of 2^-9: 2^-17 A with room for one more rounding;
   - a weight: E = 2 |ds| + 2^-20 + (n + 8 + 2 T) u relative, as for bf16 rows;
   - an output: (E + 2 * 2^-11) A for the weights and the rounding of p and of p s to fp16, half a step each (A = sum p s |n - z|: the same
@@ -171,8 +170,7 @@ def attend(q, K, V, see, scale, half, Kabs=None, Vabs=None, s_max=0.0, round_p=0
     T = float((np.abs(q) @ (Kabs if four else np.abs(K)).T)[see].max()) * scale
     ds = 2 * (d + 16) * U * T
     if four:
-        m = np.abs(q).reshape(-1, 32).max(-1).repeat(32)       # (a half's largest is no more)
-        ds += scale * 2.0 ** -14 * float((np.abs(K) @ m)[see].max())
+        ds += scale * 2.0 ** -14 * float(np.abs(q).max()) * float(np.abs(K).sum(-1)[see].max())
     E = 2 * ds + 2.0 ** -20 + (n + 8 + 2 * T) * U
     out = p @ V
     A = p @ np.abs(V)
