@@ -96,6 +96,20 @@ __device__ __forceinline__ uint32_t half_max(uint32_t a, uint32_t b) {
 }
 __device__ __forceinline__ float2 half_pair_f(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2*>(&x)); }
 
+// Largest logit of a head over the warps, and its sum relative to that.
+__device__ __forceinline__ float warps_max(const float* sm_m, int head) {
+  float m = sm_m[head];
+#pragma unroll
+  for (int i = 1; i < kKv4Warps; ++i) m = fmaxf(m, sm_m[i * 8 + head]);
+  return m;
+}
+__device__ __forceinline__ float warps_l(const float* sm_m, const float* sm_l, int head, float big) {
+  float l = 0.f;
+#pragma unroll
+  for (int i = 0; i < kKv4Warps; ++i) l += sm_m[i * 8 + head] == -INFINITY ? 0.f : sm_l[i * 8 + head] * exp2_fast(sm_m[i * 8 + head] - big);
+  return l;
+}
+
 // A consumer warp's share of a piece: 32 entries of a tile at a time.  Lane 4 r + j.
 //
 // Keys: entries are rows of the product, and two columns the high and low bytes of a query.
@@ -444,9 +458,9 @@ struct Kv4Warp {
       }
     }
   }
-  // The warp's output [G][D], relative to the heads' maxima big[G], to `out` or (ADD) on top of what is there; zeros: scratch, [groups][G].
+  // The warp's output [G][D], relative to the heads' maxima over the warps (sm_m), to `out` or (ADD) on top of what is there; zeros: scratch, [groups][G].
   template <bool ADD>
-  __device__ __forceinline__ void write(float* out, const float* big, float* zeros) const {
+  __device__ __forceinline__ void write(float* out, const float* sm_m, float* zeros) const {
     const int lane = threadIdx.x & 31, r = lane >> 2, j = lane & 3;
     __syncwarp();
 #pragma unroll
@@ -457,7 +471,7 @@ struct Kv4Warp {
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       const int head = head_of(2 * j + c), which = G == 1 ? 2 * j + c : G == 2 ? j : G == 4 ? c : 0;     // the column's group in its fragment
-      const float mm = m[kHeads == 2 ? c : 0], f = mm == -INFINITY ? 0.f : exp2_fast(mm - big[head]) * back;
+      const float mm = m[kHeads == 2 ? c : 0], f = mm == -INFINITY ? 0.f : exp2_fast(mm - warps_max(sm_m, head)) * back;
 #pragma unroll
       for (int f8 = 0; f8 < kFrags; ++f8) {
         if (which >= kPer) continue;
@@ -482,6 +496,11 @@ struct Kv4Piece {
   int last;                  // is it the last piece of its lane?
   DecodeSpan s;
 };
+
+// Quotient of numbers >= 0; 64-bit division takes some 500 cycles, which a short call would notice.
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+  return ((a | b) >> 31) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
 
 __device__ __forceinline__ void kv4_consumers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kKv4Warps * 32) : "memory"); }
 
@@ -542,12 +561,12 @@ __global__ void __launch_bounds__(kKv4Threads, 2) paged_decode_kv4_kernel(const 
   __syncthreads();
   const int H = A.n_kv_heads, cta = blockIdx.x;
   const long long total = (long long)cum[A.batch] * H;
-  const long long chunk = (total + gridDim.x - 1) / gridDim.x;
+  const long long chunk = quotient(total + gridDim.x - 1, gridDim.x);
   long long t0 = cta * chunk, t1 = min(total, t0 + chunk);
   const long long lanes = (long long)A.batch * H;
-  for (long long e = cta; e < lanes; e += gridDim.x) {     // padded rows
+  for (int e = cta; e < (int)lanes; e += gridDim.x) {      // padded rows
     if (lens[e / H] != 0) continue;
-    const long long to = (e / H * A.n_q_heads + e % H * G) * D;
+    const long long to = ((long long)(e / H) * A.n_q_heads + e % H * G) * D;
     for (int i = tid; i < G * D / 8; i += kKv4Threads) reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(A.out) + to)[i] = make_uint4(0, 0, 0, 0);
     if (A.lse && tid < G) A.lse[to / D + tid] = -INFINITY;
   }
@@ -569,7 +588,8 @@ __global__ void __launch_bounds__(kKv4Threads, 2) paged_decode_kv4_kernel(const 
     b = lo;
   }
   DecodeSpan s = span(lens[b]);
-  int head = (int)((t0 - (long long)cum[b] * H) / s.tiles), v = (int)((t0 - (long long)cum[b] * H) % s.tiles);
+  const long long into = t0 - (long long)cum[b] * H;
+  int head = (int)quotient(into, s.tiles), v = (int)(into - (long long)head * s.tiles);
   const int slots = TILE >> A.page_shift, slot_shift = 7 - A.page_shift;
   const uint32_t chunk_bytes = (uint32_t)A.page * Row::kBytes;
   // copies in flight at the end: as in the bf16 rows' kernel, there are none
@@ -681,26 +701,6 @@ __global__ void __launch_bounds__(kKv4Threads, 2) paged_decode_kv4_kernel(const 
     // join the eight warps
     w.stats(sm_m + warp * 8, sm_l + warp * 8);
     kv4_consumers_sync();
-    float big[G], sum[G];
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
-      big[g] = -INFINITY;
-      sum[g] = 0.f;
-#pragma unroll
-      for (int i = 0; i < kKv4Warps; ++i) big[g] = fmaxf(big[g], sm_m[i * 8 + g]);
-#pragma unroll
-      for (int i = 0; i < kKv4Warps; ++i) sum[g] += sm_m[i * 8 + g] == -INFINITY ? 0.f : sm_l[i * 8 + g] * exp2_fast(sm_m[i * 8 + g] - big[g]);
-    }
-    kv4_consumers_sync();
-    if (tid < G) {
-      // of the piece (a choice among registers: no local memory)
-      float bm = big[0], sl = sum[0];
-#pragma unroll
-      for (int g = 1; g < G; ++g) { bm = tid == g ? big[g] : bm; sl = tid == g ? sum[g] : sl; }
-      sm_m[tid] = bm;
-      sm_l[tid] = sl;
-    }
-    kv4_consumers_sync();
     if (warp < Sh::kOuts) w.template write<false>(sm_out + warp * G * D, sm_m, mine);
     kv4_consumers_sync();
     if constexpr (Sh::kOuts < kKv4Warps) {
@@ -729,17 +729,24 @@ __global__ void __launch_bounds__(kKv4Threads, 2) paged_decode_kv4_kernel(const 
       if (A.lse) A.lse[(long long)b * A.n_q_heads + hq0 + g] = ll > 0.f ? (mm + log2f(ll)) * kLn2 : -INFINITY;
     };
     if (whole) {
-      for (int e = tid; e < kVecs; e += kKv4Warps * 32) finish(e, warps_sum(e), sm_l[e / (D / 4)]);
-      if (tid < G) finish_lse(tid, sm_m[tid], sm_l[tid]);
+      for (int e = tid; e < kVecs; e += kKv4Warps * 32) {
+        const int g = e / (D / 4);
+        const float big = warps_max(sm_m, g), l = warps_l(sm_m, sm_l, g, big);
+        finish(e, warps_sum(e), l);
+        if (e % (D / 4) == 0) finish_lse(g, big, l);
+      }
     } else {
       const long long slot = cta + lane_no;
       for (int e = tid; e < kVecs; e += kKv4Warps * 32) reinterpret_cast<float4*>(P.part + slot * G * D)[e] = warps_sum(e);
-      if (tid < G) P.part_ml[slot * G + tid] = make_float2(sm_m[tid], sm_l[tid]);
+      if (tid < G) {
+        const float big = warps_max(sm_m, tid);
+        P.part_ml[slot * G + tid] = make_float2(big, warps_l(sm_m, sm_l, tid, big));
+      }
       __threadfence();
       kv4_consumers_sync();
       // pieces of the lane: its tiles lie at [off, off + tiles) of the deal
       const long long off = (long long)cum[b] * H + (long long)head * tiles, chunk = piece->chunk;
-      const int c0 = (int)(off / chunk), pieces = (int)((off + tiles - 1) / chunk) - c0 + 1;
+      const int c0 = (int)quotient(off, chunk), pieces = (int)quotient(off + tiles - 1, chunk) - c0 + 1;
       if (tid == 0) {
         const bool last = atomicAdd(P.arrived + lane_no, 1u) == (uint32_t)pieces - 1;
         if (last) P.arrived[lane_no] = 0;
