@@ -73,6 +73,11 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return y;
 }
 
+// Quotient of numbers >= 0; 64-bit division takes some 500 cycles, which a short call would notice.
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+  return ((a | b) >> 31) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
 // What a decode step sees of a sequence, in tiles: those with sinks first, then those from the window's first entry on.
 struct DecodeSpan {
   int len, lo, sinks, sink_tiles, first_tile, tiles;
@@ -423,7 +428,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
   __syncthreads();
   const int H = A.n_kv_heads, cta = blockIdx.x;
   const long long total = (long long)cum[A.batch] * H;
-  const long long chunk = (total + gridDim.x - 1) / gridDim.x;
+  const long long chunk = quotient(total + gridDim.x - 1, gridDim.x);
   long long t0 = cta * chunk, t1 = min(total, t0 + chunk);
   // Few lanes of nearly equal length: a lane each.  Joining a lane costs about as much as four tiles (7000 cycles; under a window of
   // 508, 232 lanes of ten tiles, 21.5 us with lanes cut every eight tiles, 17.2 us whole).
@@ -446,7 +451,8 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
     b = lo;
   }
   DecodeSpan s = span(lens[b]);
-  int head = (int)((t0 - (long long)cum[b] * H) / s.tiles), v = (int)((t0 - (long long)cum[b] * H) % s.tiles);
+  const long long into = t0 - (long long)cum[b] * H;
+  int head = (int)quotient(into, s.tiles), v = (int)(into - (long long)head * s.tiles);
   const int pr = min(A.page, TILE), pr_shift = min(A.page_shift, TILE == 64 ? 6 : 5);
   const int boxes = TILE >> pr_shift;
   // No copy is in flight when the CTA ends, without a wait of its own for that: a consumer has waited for each, and where one or the
@@ -458,20 +464,39 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
     const uint64_t policy = l2_policy_evict_first();
     fence_proxy_async();                                   // rows that earlier kernels stored are read by the copies
     int it = 0;
+    // CHOSEN: entries and pages of the next tiles' boxes, looked up by all lanes together (one tile's at a time, list and then table,
+    // take longer than its copy)
+    int ahead = 0, next = 0, ahead_entry = 0, ahead_page = -1;
     for (long long t = t0; t < t1; ++t, ++it) {
       const int st = it % STAGES;
       // box of this lane: boxes of K first, then of V
       const bool mine = lane < 2 * boxes;
       const int box = lane & (boxes - 1);
       int i = s.tile(v) * TILE + box * pr;
-      if constexpr (CHOSEN) {
-        const int at = i >> A.page_shift, pages = (s.len + A.page - 1) >> A.page_shift;      // place in the list
-        const int pg = mine && at < min(P.n_select, pages) ? P.pages[((long long)b * H + head) * P.n_select + at] : -1;
-        i = (unsigned)pg < (unsigned)pages ? (pg << A.page_shift) + (i & (A.page - 1)) : s.len;
-      }
-      // does the box hold a visible entry?  [i, i + pr) against [lo, len) and [0, sinks)
       int chunk_no = P.oob_chunk, row = 0;
-      if (mine && i < s.len && (i + pr > s.lo || i < s.sinks)) {
+      if constexpr (CHOSEN) {
+        if (next == ahead) {
+          const int per = 32 / boxes, k = lane / boxes;
+          ahead = min(per, s.tiles - v);
+          next = 0;
+          ahead_entry = s.len;
+          ahead_page = -1;
+          const int first = (v + k) * TILE + box * pr, at = first >> A.page_shift, pages = (s.len + A.page - 1) >> A.page_shift;      // place in the list
+          const int pg = k < ahead && at < min(P.n_select, pages) ? P.pages[((long long)b * H + head) * P.n_select + at] : -1;
+          if ((unsigned)pg < (unsigned)pages) {
+            const int e = (pg << A.page_shift) + (first & (A.page - 1));
+            if (e < s.len) {
+              ahead_entry = e;
+              ahead_page = page_of(A, b, e);
+            }
+          }
+        }
+        i = __shfl_sync(~0u, ahead_entry, next * boxes + box);
+        const int pg = __shfl_sync(~0u, ahead_page, next * boxes + box);
+        ++next;
+        if (pg >= 0) { chunk_no = P.chunk0 + pg * H + head; row = i & (A.page - 1); }
+      } else if (mine && i < s.len && (i + pr > s.lo || i < s.sinks)) {
+        // does the box hold a visible entry?  [i, i + pr) against [lo, len) and [0, sinks)
         const int pg = page_of(A, b, i);
         if (pg >= 0) { chunk_no = P.chunk0 + pg * H + head; row = i & (A.page - 1); }
       }
@@ -600,7 +625,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
       consumers_sync();
       // pieces of the lane: its tiles lie at [off, off + tiles) of the deal
       const long long off = (long long)cum[b] * H + (long long)head * s.tiles;
-      const int c0 = (int)(off / chunk), pieces = (int)((off + s.tiles - 1) / chunk) - c0 + 1;
+      const int c0 = (int)quotient(off, chunk), pieces = (int)quotient(off + s.tiles - 1, chunk) - c0 + 1;
       if (tid == 0) {
         const bool last = atomicAdd(P.arrived + lane_no, 1u) == (uint32_t)pieces - 1;
         if (last) P.arrived[lane_no] = 0;

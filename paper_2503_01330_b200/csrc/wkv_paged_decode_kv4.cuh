@@ -497,11 +497,6 @@ struct Kv4Piece {
   DecodeSpan s;
 };
 
-// Quotient of numbers >= 0; 64-bit division takes some 500 cycles, which a short call would notice.
-__device__ __forceinline__ long long quotient(long long a, long long b) {
-  return ((a | b) >> 31) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
-}
-
 __device__ __forceinline__ void kv4_consumers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kKv4Warps * 32) : "memory"); }
 
 template <int D, int G, bool CHOSEN>
