@@ -26,7 +26,7 @@ struct ChooseParams {
 };
 
 constexpr int kChooseThreads = 256, kChooseWarps = kChooseThreads / 32;
-constexpr int kChooseHeld = 8;         // scores per thread that stay in registers
+constexpr int kChooseNear = 2048;      // scores that are held in shared memory
 constexpr int kChooseBins = 1024;
 
 // As the eviction's order of scores: -0 like +0, NaN above all numbers.
@@ -98,28 +98,18 @@ __device__ __forceinline__ unsigned long long cutoff_by_digits(Each each, int n,
   return least;
 }
 
-// The `want` best of n pages (more than that), the n_taken with taken(i) among them in any case, in order of their index.  A thread owns `per`
-// consecutive ones: their scores in registers (HELD), where they are few, or looked up each time.  Scores are counted in bins of equal
-// width between the least and the largest; the bin that holds the last one to be chosen is settled by comparing its few pages with
-// one another (digit by digit over all pages where they are many: 9 us for 2048 pages, this one 2).
-template <bool HELD, typename ScoreAt, typename Taken>
-__device__ __forceinline__ void choose(ScoreAt score_at, Taken taken, int n_taken, int per, int n, int want, int32_t* to, ChooseShared& sh) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, first = tid * per, count = min(per, max(0, n - first));
-  float held[kChooseHeld];
-  if constexpr (HELD) {
-#pragma unroll
-    for (int i = 0; i < kChooseHeld; ++i) held[i] = i < count ? score_at(first + i) : 0.f;
-  }
-  auto all = [&](auto f) {                                 // f(index, score) for this thread's pages
-    if constexpr (HELD) {
-#pragma unroll
-      for (int i = 0; i < kChooseHeld; ++i)
-        if (i < count) f(first + i, held[i]);
-    } else {
-      for (int i = 0; i < count; ++i) f(first + i, score_at(first + i));
-    }
+// The `want` best of n pages (more than that), the n_taken with taken(i) among them in any case, in order of their index.  Scores are
+// counted in bins of equal width between the least and the largest; the bin that holds the last one to be chosen is settled by comparing
+// its few pages with one another (digit by digit over all pages where they are many).  Loops are kept rolled: code that runs once costs
+// its way into the instruction caches (with eight scores a thread in registers and all loops unrolled the choice took 5 us).
+template <typename ScoreAt, typename Taken>
+__device__ __forceinline__ void choose(ScoreAt score_at, Taken taken, int n_taken, int n, int want, int32_t* to, ChooseShared& sh) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  auto each = [&](auto f) {                                // f(index, score) for the free pages
+#pragma unroll 2
+    for (int i = tid; i < n; i += kChooseThreads)
+      if (!taken(i)) f(i, score_at(i));
   };
-  auto each = [&](auto f) { all([&](int i, float x) { if (!taken(i)) f(i, x); }); };
   float least = INFINITY, most = -INFINITY;
   bool odd = false;
   each([&](int, float x) {
@@ -133,6 +123,7 @@ __device__ __forceinline__ void choose(ScoreAt score_at, Taken taken, int n_take
     most = fmaxf(most, __shfl_xor_sync(~0u, most, off));
   }
   if (lane == 0) { sh.least[warp] = least; sh.most[warp] = most; }
+#pragma unroll
   for (int i = tid; i < kChooseBins; i += kChooseThreads) sh.bins[i] = 0;
   if (tid == 0) sh.n_candidates = 0;
   odd = __syncthreads_or(odd);
@@ -142,10 +133,10 @@ __device__ __forceinline__ void choose(ScoreAt score_at, Taken taken, int n_take
   const float range = most - least, per_bin = range > 0.f && range < INFINITY ? kChooseBins / range : 0.f;
   odd = odd || !(per_bin > 0.f && per_bin < INFINITY);
   unsigned long long cutoff = ~0ull;                       // want = 0: none but the taken ones
-  // (x - least, times a constant, cut to a whole number: each step keeps the order)
-  auto bin_of = [&](float x) { return min(kChooseBins - 1, (int)((x - least) * per_bin)); };
   bool settled = want == 0;
   if (want > 0 && !odd) {
+    // (x - least, times a constant, cut to a whole number: each step keeps the order)
+    auto bin_of = [&](float x) { return min(kChooseBins - 1, (int)((x - least) * per_bin)); };
     each([&](int, float x) { atomicAdd(&sh.bins[bin_of(x)], 1); });
     __syncthreads();
     constexpr int kMine = kChooseBins / kChooseThreads;    // bins of this thread, from the top down
@@ -175,12 +166,25 @@ __device__ __forceinline__ void choose(ScoreAt score_at, Taken taken, int n_take
     }
   }
   if (!settled) cutoff = cutoff_by_digits(each, n - n_taken, want, sh);
-  int chosen = 0, total;
-  all([&](int i, float x) { chosen += taken(i) || (want > 0 && page_rank(x, i) >= cutoff); });
-  int at = sum_before(chosen, sh.sums[0], total);
-  all([&](int i, float x) {
-    if (taken(i) || (want > 0 && page_rank(x, i) >= cutoff)) to[at++] = i;
-  });
+  // a warp's pages lie in a row: their number, then their places by ballots
+  const int run = (n + kChooseThreads - 1) / kChooseThreads, first = warp * run * 32 + lane;
+  auto chosen = [&](int i) { return i < n && (taken(i) || (want > 0 && page_rank(score_at(i), i) >= cutoff)); };
+  int count = 0;
+#pragma unroll 2
+  for (int k = 0; k < run; ++k) count += __popc(__ballot_sync(~0u, chosen(first + k * 32)));
+  if (lane == 0) sh.sums[0][warp] = count;
+  __syncthreads();
+  int at = 0;
+#pragma unroll
+  for (int w = 0; w < kChooseWarps; ++w) at += w < warp ? sh.sums[0][w] : 0;
+#pragma unroll 2
+  for (int k = 0; k < run; ++k) {
+    const int i = first + k * 32;
+    const bool in = chosen(i);
+    const uint32_t all = __ballot_sync(~0u, in);
+    if (in) to[at + __popc(all & ((1u << lane) - 1))] = i;
+    at += __popc(all);
+  }
 }
 
 template <typename T, int D>
@@ -188,7 +192,7 @@ __global__ void __launch_bounds__(kChooseThreads, 4) paged_choose_kernel(const _
   __shared__ __align__(16) int8_t code[2][D];
   __shared__ float part[kChooseWarps];
   __shared__ ChooseShared sh;
-  __shared__ float near[kChooseHeld * kChooseThreads];     // the scores of a lane that one CTA has to itself
+  __shared__ float near[kChooseNear];
   __shared__ int is_last;
   griddep_launch();
   griddep_wait();
@@ -272,7 +276,7 @@ __global__ void __launch_bounds__(kChooseThreads, 4) paged_choose_kernel(const _
         if (sub == 0 && p < p1) {
           const float x = __fmul_rn((float)sum, scale[k]);
           scores[p] = x;
-          if (p < kChooseHeld * kChooseThreads) near[p] = x;
+          if (p < kChooseNear) near[p] = x;
         }
       }
     }
@@ -297,12 +301,12 @@ __global__ void __launch_bounds__(kChooseThreads, 4) paged_choose_kernel(const _
     for (int i = tid; i < n; i += kChooseThreads) to[i] = i;
     return;
   }
-  const bool alone = P.splits == 1 && n <= kChooseHeld * kChooseThreads;
-  auto score_at = [&](int p) { return alone ? near[p] : __ldcg(scores + p); };
-  auto taken = [&](int p) { return p < P.sink || p >= n - P.recent; };
-  const int per = (n + kChooseThreads - 1) / kChooseThreads;
-  if (per <= kChooseHeld) choose<true>(score_at, taken, P.sink + P.recent, per, n, want, to, sh);
-  else choose<false>(score_at, taken, P.sink + P.recent, per, n, want, to, sh);
+  const bool is_near = n <= kChooseNear;
+  if (is_near && P.splits > 1) {
+    for (int i = tid; i < n; i += kChooseThreads) near[i] = __ldcg(scores + i);
+    __syncthreads();
+  }
+  choose([&](int p) { return is_near ? near[p] : __ldcg(scores + p); }, [&](int p) { return p < P.sink || p >= n - P.recent; }, P.sink + P.recent, n, want, to, sh);
 }
 
 }  // namespace wkv
