@@ -6,9 +6,10 @@
 // u and w to 1/127 of their largest.  Everything under the sum is an int8 number: the sum is exact in any order (dp4a), so that which
 // pages are chosen does not depend on how the work is cut.
 //
-// Bound: the bounds, 2 D bytes a page and kv head, 1/32 of a bf16 cache in pages of 16; for one sequence latency: bounds -> scores ->
-// choice.  Eight lanes share a page; the pages of a lane (sequence, kv head) are cut over CTAs, of which the last to arrive (by a
-// counter that nobody waits on) chooses.
+// Bound: the bounds, 2 D bytes a page and kv head, 1/32 of a bf16 cache in pages of 16; for one sequence latency: length -> table -> bounds
+// -> scores -> choice.  Eight lanes share a page; the pages of a lane (sequence, kv head) are cut over CTAs, of which the last to arrive
+// (by a counter that nobody waits on) chooses.  (A cluster whose CTAs put their scores into the first one's shared memory saves 2 us of
+// that, and costs them again where the launch follows one that fills the SMs: 2048 pages, then 64 of them attended to, 21.3 us for 20.)
 #pragma once
 #include "wkv_paged.cuh"
 
@@ -26,7 +27,7 @@ struct ChooseParams {
 };
 
 constexpr int kChooseThreads = 256, kChooseWarps = kChooseThreads / 32;
-constexpr int kChooseNear = 2048;      // scores that are held in shared memory
+constexpr int kChooseNear = 2048;      // pages of a lane whose scores are held in shared memory
 constexpr int kChooseBins = 1024;
 
 // As the eviction's order of scores: -0 like +0, NaN above all numbers.
@@ -98,17 +99,21 @@ __device__ __forceinline__ unsigned long long cutoff_by_digits(Each each, int n,
   return least;
 }
 
-// The `want` best of n pages (more than that), the n_taken with taken(i) among them in any case, in order of their index.  Scores are
+// The `want` best of n pages (more than that), the first `sink` and the last `recent` among them in any case, in order of their index.  Scores are
 // counted in bins of equal width between the least and the largest; the bin that holds the last one to be chosen is settled by comparing
-// its few pages with one another (digit by digit over all pages where they are many).  Loops are kept rolled: code that runs once costs
-// its way into the instruction caches (with eight scores a thread in registers and all loops unrolled the choice took 5 us).
-template <typename ScoreAt, typename Taken>
-__device__ __forceinline__ void choose(ScoreAt score_at, Taken taken, int n_taken, int n, int want, int32_t* to, ChooseShared& sh) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+// its few pages with one another (digit by digit over all pages where they are many).  NEAR: the scores are in shared memory.  The loops
+// are short and rolled: between other kernels a launch finds none of its code in the instruction caches, and unrolled ones, the faster by
+// 3 us when nothing else ran in between, then were no faster at all.
+template <bool NEAR, typename ScoreAt>
+__device__ __forceinline__ void choose(ScoreAt score_at, int sink, int recent, int n, int want, int32_t* to, ChooseShared& sh) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, hi = n - recent, steps = (n + kChooseThreads - 1) / kChooseThreads;
+  auto is_free = [&](int i) { return i >= sink && i < hi; };      // neither behind the last page nor taken anyway
   auto each = [&](auto f) {                                // f(index, score) for the free pages
 #pragma unroll 2
-    for (int i = tid; i < n; i += kChooseThreads)
-      if (!taken(i)) f(i, score_at(i));
+    for (int i = tid; i < hi; i += kChooseThreads) {
+      const float x = score_at(i);
+      if (i >= sink) f(i, x);
+    }
   };
   float least = INFINITY, most = -INFINITY;
   bool odd = false;
@@ -124,10 +129,10 @@ __device__ __forceinline__ void choose(ScoreAt score_at, Taken taken, int n_take
   }
   if (lane == 0) { sh.least[warp] = least; sh.most[warp] = most; }
 #pragma unroll
-  for (int i = tid; i < kChooseBins; i += kChooseThreads) sh.bins[i] = 0;
+  for (int i = 0; i < kChooseBins / kChooseThreads; ++i) sh.bins[tid + i * kChooseThreads] = 0;
   if (tid == 0) sh.n_candidates = 0;
   odd = __syncthreads_or(odd);
-  want -= n_taken;
+  want -= sink + recent;
 #pragma unroll
   for (int w = 0; w < kChooseWarps; ++w) { least = fminf(least, sh.least[w]); most = fmaxf(most, sh.most[w]); }
   const float range = most - least, per_bin = range > 0.f && range < INFINITY ? kChooseBins / range : 0.f;
@@ -165,48 +170,107 @@ __device__ __forceinline__ void choose(ScoreAt score_at, Taken taken, int n_take
       settled = true;
     }
   }
-  if (!settled) cutoff = cutoff_by_digits(each, n - n_taken, want, sh);
-  // a warp's pages lie in a row: their number, then their places by ballots
-  const int run = (n + kChooseThreads - 1) / kChooseThreads, first = warp * run * 32 + lane;
-  auto chosen = [&](int i) { return i < n && (taken(i) || (want > 0 && page_rank(score_at(i), i) >= cutoff)); };
-  int count = 0;
+  if (!settled) cutoff = cutoff_by_digits(each, n - sink - recent, want, sh);
+  auto chosen = [&](int i) { return i < n && (!is_free(i) || (want > 0 && page_rank(score_at(i), i) >= cutoff)); };
+  if constexpr (NEAR) {
+    // chosen pages by (step, warp), counted and given places in that order
+    uint32_t* masks = reinterpret_cast<uint32_t*>(sh.bins);
+    if (warp == 0) masks[lane] = masks[32 + lane] = 0;
+    __syncthreads();
 #pragma unroll 2
-  for (int k = 0; k < run; ++k) count += __popc(__ballot_sync(~0u, chosen(first + k * 32)));
-  if (lane == 0) sh.sums[0][warp] = count;
-  __syncthreads();
-  int at = 0;
+    for (int k = 0; k < steps; ++k) {
+      const uint32_t in = __ballot_sync(~0u, chosen(tid + k * kChooseThreads));
+      if (lane == 0) masks[k * kChooseWarps + warp] = in;
+    }
+    __syncthreads();
+    static_assert(kChooseNear / 32 == 64, "two masks a lane");
+    const int c0 = __popc(masks[2 * lane]), c1 = __popc(masks[2 * lane + 1]);
+    int y = c0 + c1;
 #pragma unroll
-  for (int w = 0; w < kChooseWarps; ++w) at += w < warp ? sh.sums[0][w] : 0;
-#pragma unroll 2
-  for (int k = 0; k < run; ++k) {
-    const int i = first + k * 32;
-    const bool in = chosen(i);
-    const uint32_t all = __ballot_sync(~0u, in);
-    if (in) to[at + __popc(all & ((1u << lane) - 1))] = i;
-    at += __popc(all);
+    for (int off = 1; off < 32; off <<= 1) {
+      const int z = __shfl_up_sync(~0u, y, off);
+      if (lane >= off) y += z;
+    }
+    y -= c0 + c1;                                          // before mask 2 lane
+    for (int k = 0; k < steps; ++k) {
+      const int of = k * kChooseWarps + warp, before = __shfl_sync(~0u, of & 1 ? y + c0 : y, of >> 1);
+      const uint32_t in = masks[of];
+      if (in >> lane & 1) to[before + __popc(in & ((1u << lane) - 1))] = tid + k * kChooseThreads;
+    }
+  } else {
+    // a warp's pages lie in a row: their number, then their places by ballots
+    const int first = warp * steps * 32 + lane;
+    int count = 0;
+    for (int k = 0; k < steps; ++k) count += __popc(__ballot_sync(~0u, chosen(first + k * 32)));
+    if (lane == 0) sh.sums[0][warp] = count;
+    __syncthreads();
+    int at = 0;
+#pragma unroll
+    for (int w = 0; w < kChooseWarps; ++w) at += w < warp ? sh.sums[0][w] : 0;
+    for (int k = 0; k < steps; ++k) {
+      const int i = first + k * 32;
+      const bool mine = chosen(i);
+      const uint32_t all = __ballot_sync(~0u, mine);
+      if (mine) to[at + __popc(all & ((1u << lane) - 1))] = i;
+      at += __popc(all);
+    }
   }
 }
 
+// `splits` CTAs per lane.
 template <typename T, int D>
 __global__ void __launch_bounds__(kChooseThreads, 4) paged_choose_kernel(const __grid_constant__ ChooseParams P) {
   __shared__ __align__(16) int8_t code[2][D];
   __shared__ float part[kChooseWarps];
   __shared__ ChooseShared sh;
   __shared__ float near[kChooseNear];
-  __shared__ int is_last;
+  __shared__ bool is_last;
   griddep_launch();
   griddep_wait();
   const PagedParams& A = P.A;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, sub = lane & 7;
   const int lane_no = blockIdx.x / P.splits, split = blockIdx.x % P.splits, b = lane_no / A.n_kv_heads, h = lane_no % A.n_kv_heads;
-  // the query's codes (its row is there, whatever the length)
+  // the query's row is there, whatever the length
+  const int G = A.n_q_heads / A.n_kv_heads;
+  float up = 0.f, down = 0.f;
+  const T* q = static_cast<const T*>(A.q) + (long long)b * A.q_stride + (long long)h * G * D + (tid < D ? tid : 0);
+  float q0 = (float)q[0];
+  const int len = clamped_len(A, b), n = (len + A.page - 1) >> A.page_shift;
+  // bounds: eight lanes a page, D / 8 channels each, kSteps pages in flight, kStride apart; the first ones are on their way while the query's
+  // codes are made
+  constexpr int kWords = D / 32, kSteps = 4, kStride = kChooseWarps * 4;   // words per lane, of the largest and of the least
+  const int each = ((n + P.splits - 1) / P.splits + 31) & ~31, p1 = min(n, (split + 1) * each);
+  int hi[kSteps][kWords], lo[kSteps][kWords];
+  float scale[kSteps];
+  auto load = [&](int base) {
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+      const int p = base + k * kStride;
+      const int pg = p < p1 ? page_of(A, b, p << A.page_shift) : -1;
+      const long long chunk = (long long)pg * A.n_kv_heads + h;
+      scale[k] = 0.f;
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) hi[k][i] = lo[k][i] = 0;
+      if (pg < 0) continue;
+      scale[k] = P.bound_scale[chunk];
+      const int8_t* at = P.bounds + chunk * 2 * D + sub * kWords * 4;
+      if constexpr (kWords == 4) {
+        const int4 x = *reinterpret_cast<const int4*>(at), y = *reinterpret_cast<const int4*>(at + D);
+        hi[k][0] = x.x; hi[k][1] = x.y; hi[k][2] = x.z; hi[k][3] = x.w;
+        lo[k][0] = y.x; lo[k][1] = y.y; lo[k][2] = y.z; lo[k][3] = y.w;
+      } else {
+        const int2 x = *reinterpret_cast<const int2*>(at), y = *reinterpret_cast<const int2*>(at + D);
+        hi[k][0] = x.x; hi[k][1] = x.y;
+        lo[k][0] = y.x; lo[k][1] = y.y;
+      }
+    }
+  };
+  const int first = split * each + warp * 4;               // of this warp's four pages
+  load(first + (lane >> 3));
   {
-    const int G = A.n_q_heads / A.n_kv_heads;
-    float up = 0.f, down = 0.f;
     if (tid < D) {
-      const T* q = static_cast<const T*>(A.q) + (long long)b * A.q_stride + (long long)h * G * D + tid;
       for (int g = 0; g < G; ++g) {
-        const float x = (float)q[g * D];
+        const float x = g == 0 ? q0 : (float)q[g * D];
         up = __fadd_rn(up, fmaxf(x, 0.f));
         down = __fadd_rn(down, fminf(x, 0.f));
       }
@@ -226,47 +290,19 @@ __global__ void __launch_bounds__(kChooseThreads, 4) paged_choose_kernel(const _
     }
     __syncthreads();
   }
-  const int len = clamped_len(A, b), n = (len + A.page - 1) >> A.page_shift;
   float* scores = P.page_scores + (long long)lane_no * P.page_score_stride;
-  // scores: eight lanes a page, D / 8 channels each
   {
-    constexpr int kWords = D / 32;                         // per lane, of the largest and of the least
-    const int sub = lane & 7;
     int u[kWords], w[kWords];
 #pragma unroll
     for (int i = 0; i < kWords; ++i) {
       u[i] = reinterpret_cast<const int*>(code[0])[sub * kWords + i];
       w[i] = reinterpret_cast<const int*>(code[1])[sub * kWords + i];
     }
-    const int each = ((n + P.splits - 1) / P.splits + 31) & ~31, p1 = min(n, (split + 1) * each);
-    constexpr int kSteps = 4, kStride = kChooseWarps * 4;  // pages in flight; pages a step apart
-    for (int base = split * each + warp * 4 + (lane >> 3); base - (lane >> 3) < p1; base += kSteps * kStride) {
-      int hi[kSteps][kWords], lo[kSteps][kWords];
-      float scale[kSteps];
+    for (int base = first; base < p1; base += kSteps * kStride) {
+      if (base != first) load(base + (lane >> 3));
 #pragma unroll
       for (int k = 0; k < kSteps; ++k) {
-        const int p = base + k * kStride;
-        const int pg = p < p1 ? page_of(A, b, p << A.page_shift) : -1;
-        const long long chunk = (long long)pg * A.n_kv_heads + h;
-        scale[k] = 0.f;
-#pragma unroll
-        for (int i = 0; i < kWords; ++i) hi[k][i] = lo[k][i] = 0;
-        if (pg < 0) continue;
-        scale[k] = P.bound_scale[chunk];
-        const int8_t* at = P.bounds + chunk * 2 * D + sub * kWords * 4;
-        if constexpr (kWords == 4) {
-          const int4 x = *reinterpret_cast<const int4*>(at), y = *reinterpret_cast<const int4*>(at + D);
-          hi[k][0] = x.x; hi[k][1] = x.y; hi[k][2] = x.z; hi[k][3] = x.w;
-          lo[k][0] = y.x; lo[k][1] = y.y; lo[k][2] = y.z; lo[k][3] = y.w;
-        } else {
-          const int2 x = *reinterpret_cast<const int2*>(at), y = *reinterpret_cast<const int2*>(at + D);
-          hi[k][0] = x.x; hi[k][1] = x.y;
-          lo[k][0] = y.x; lo[k][1] = y.y;
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < kSteps; ++k) {
-        const int p = base + k * kStride;
+        const int p = base + (lane >> 3) + k * kStride;
         int sum = 0;
 #pragma unroll
         for (int i = 0; i < kWords; ++i) sum = __dp4a(u[i], hi[k][i], __dp4a(w[i], lo[k][i], sum));
@@ -292,6 +328,8 @@ __global__ void __launch_bounds__(kChooseThreads, 4) paged_choose_kernel(const _
     __syncthreads();
     if (!is_last) return;
     __threadfence();
+#pragma unroll 4
+    for (int i = tid; i < min(n, kChooseNear); i += kChooseThreads) near[i] = __ldcg(scores + i);
   }
   __syncthreads();
   const int want = min(P.n_select, n);
@@ -301,12 +339,8 @@ __global__ void __launch_bounds__(kChooseThreads, 4) paged_choose_kernel(const _
     for (int i = tid; i < n; i += kChooseThreads) to[i] = i;
     return;
   }
-  const bool is_near = n <= kChooseNear;
-  if (is_near && P.splits > 1) {
-    for (int i = tid; i < n; i += kChooseThreads) near[i] = __ldcg(scores + i);
-    __syncthreads();
-  }
-  choose([&](int p) { return is_near ? near[p] : __ldcg(scores + p); }, [&](int p) { return p < P.sink || p >= n - P.recent; }, P.sink + P.recent, n, want, to, sh);
+  if (n <= kChooseNear) choose<true>([&](int p) { return near[p]; }, P.sink, P.recent, n, want, to, sh);
+  else choose<false>([&](int p) { return __ldcg(scores + p); }, P.sink, P.recent, n, want, to, sh);
 }
 
 }  // namespace wkv

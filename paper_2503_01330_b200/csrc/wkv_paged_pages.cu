@@ -27,6 +27,15 @@ cudaError_t pick_by_group(wkv_paged* c) {
 
 }  // namespace
 
+namespace {
+typedef void (*choose_fn)(const ChooseParams);
+choose_fn choose_kernel(const wkv_paged* c) {
+  const bool wide = c->cfg.head_dim == 128;
+  return c->cfg.dtype == WKV_F32 ? (wide ? paged_choose_kernel<float, 128> : paged_choose_kernel<float, 64>)
+                                 : (wide ? paged_choose_kernel<__nv_bfloat16, 128> : paged_choose_kernel<__nv_bfloat16, 64>);
+}
+}  // namespace
+
 cudaError_t pick_pages(wkv_paged* c) {
   const bool wide = c->cfg.head_dim == 128;
   if (c->cfg.dtype == WKV_BF16) return wide ? pick_by_group<__nv_bfloat16, 128>(c) : pick_by_group<__nv_bfloat16, 64>(c);
@@ -67,10 +76,7 @@ int wkv_paged_select(wkv_paged* c, int32_t layer, int32_t batch, const void* q, 
   // CTAs per lane: 64 pages each at least, two CTAs an SM in all where the lanes are few
   const long long lanes = (long long)batch * f.n_kv_heads;
   P.splits = (int)std::max<long long>(1, std::min<long long>((table_width + 63) / 64, 2 * c->sm_count / lanes));
-  const bool wide = f.head_dim == 128;
-  auto kernel = f.dtype == WKV_F32 ? (wide ? wkv::paged_choose_kernel<float, 128> : wkv::paged_choose_kernel<float, 64>)
-                                   : (wide ? wkv::paged_choose_kernel<__nv_bfloat16, 128> : wkv::paged_choose_kernel<__nv_bfloat16, 64>);
-  WKV_CUDA(c, launch(c, kernel, lanes * P.splits, wkv::kChooseThreads, 0, P));
+  WKV_CUDA(c, launch(c, choose_kernel(c), lanes * P.splits, wkv::kChooseThreads, 0, P));
   return WKV_OK;
 }
 
