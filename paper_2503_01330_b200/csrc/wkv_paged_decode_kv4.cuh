@@ -38,10 +38,12 @@ struct Kv4Shape {
   static constexpr int kScratch = kKv4Warps * 16 * G * 4; // a warp's weights, then zero points' sums
   static constexpr int kQuery = (G == 2 || G == 8 ? 2 : 1) * D / 64 * 512;      // Kv4Warp::kQuery
   static constexpr int kOther = kOut + kScratch + kQuery + 2 * kKv4Warps * 8 * 4 + (2 * kMaxSequences + 8) * 4 + 64;
-  // Two CTAs an SM; a stage's slot entries and barriers beside it.  An even number: a stage then belongs to one team of warps, which cannot
+  // CTAs an SM: one where eight heads' sums of 128 channels would not fit into half of the registers (64 sequences of 8192..16384 tokens,
+  // 8 heads on one: 50 us, 64 with two); a stage's slot entries and barriers beside it.  An even number: a stage then belongs to one team of warps, which cannot
   // be more than one of its barrier's phases ahead (with an odd one the teams take turns on it, and a wait that looks at the
   // phase's parity could be let through by the phase before the other team's).
-  static constexpr int kStages = (113 * 1024 - kOther) / (kStage + kKv4MaxSlots * 4 + 16) / 2 * 2;
+  static constexpr int kCtas = G == 8 && D == 128 ? 1 : 2;
+  static constexpr int kStages = (226 / kCtas * 1024 - kOther) / (kStage + kKv4MaxSlots * 4 + 16) / 2 * 2;
   static_assert(kKv4Warps == 2 * kKv4TileWarps && kStages >= 2, "two teams");
   static constexpr int kSmem = kStages * (kStage + kKv4MaxSlots * 4 + 16) + kOther;
 };
@@ -500,7 +502,7 @@ struct Kv4Piece {
 __device__ __forceinline__ void kv4_consumers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kKv4Warps * 32) : "memory"); }
 
 template <int D, int G, bool CHOSEN>
-__global__ void __launch_bounds__(kKv4Threads, 2) paged_decode_kv4_kernel(const __grid_constant__ DecodeParams P) {
+__global__ void __launch_bounds__(kKv4Threads, (Kv4Shape<D, G>::kCtas)) paged_decode_kv4_kernel(const __grid_constant__ DecodeParams P) {
   using Sh = Kv4Shape<D, G>;
   using Row = Kv4Row<D>;
   using Warp = Kv4Warp<D, G>;
