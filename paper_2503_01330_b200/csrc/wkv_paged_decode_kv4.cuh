@@ -3,13 +3,13 @@
 //   o = sum_i p_i v_i,  p = softmax(scale q.k_i),  k_i = s_ig (n - z_ig) per group g of 32 channels, v_i likewise
 //
 // Bound: HBM at 4.5 bits a number; instruction issue close behind it, since a number may cost no more than about three lane instructions.
-// Codes are never converted.  Keys: a masked word is four bytes for mma.sync m16n8k32 on integers, against queries of 16 bits in two columns
+// Codes are never converted.  Keys: a masked word is four bytes for mma.sync m16n8k32 on integers, against queries of 23 bits in three columns
 // of eight; exact, until a group's product becomes fp32.  Values: a masked word is two fp16 subnormals n 2^-24 (or n 2^-20), which m16n8k16
 // takes exactly.  Scales and zero points stay outside of the products:
 //   q.k_i  = sum_g s_ig (q_g.n_ig - z_ig sum q_g)
 //   o_g    = sum_i (p_i s_ig) n_ig - sum_i (p_i s_ig) z_ig   the weights p s in fp16, the same rounded ones in both sums
-// A query head becomes whole numbers by a power of two that brings its largest channel to [2^13, 2^14): bf16 channels down to 2^-6 of it stay
-// exact, smaller ones are off by up to 2^-14 of it.  p and p s are rounded to fp16, 2^-11 each, together a quarter of what
+// A query head becomes whole numbers by a power of two that brings its largest channel to [2^21, 2^22): bf16 channels down to 2^-14 of it
+// stay exact, smaller ones are off by up to 2^-22 of it (two columns, 2^-14, showed in the log-sums, which are fp32).  p and p s are rounded to fp16, 2^-11 each, together a quarter of what
 // rounding the output to bf16 costs.  The weights are kept in fp16's range by a power of two that follows the largest value scale seen.
 // (Keys as fp16 subnormals: 163 us of arithmetic in the 16 x 8192..16384 case, masks at half rate above all.  As e4m3 numbers the matrix
 // instruction is split into fp16 ones with conversions.)
@@ -36,7 +36,7 @@ struct Kv4Shape {
   static constexpr int kOuts = G >= 4 ? kKv4Warps / 2 : kKv4Warps;      // outputs side by side in the join: the warps', or of pairs of them
   static constexpr int kOut = kOuts * G * D * 4;
   static constexpr int kScratch = kKv4Warps * 16 * G * 4; // a warp's weights, then zero points' sums
-  static constexpr int kQuery = (G == 2 || G == 8 ? 2 : 1) * D / 64 * 512;      // Kv4Warp::kQuery
+  static constexpr int kQuery = (G == 2 || G == 8 ? 3 : 2) * D / 64 * 512;      // Kv4Warp::kQuery
   static constexpr int kOther = kOut + kScratch + kQuery + 2 * kKv4Warps * 8 * 4 + (2 * kMaxSequences + 8) * 4 + 64;
   // CTAs an SM: one where eight heads' sums of 128 channels would not fit into half of the registers (64 sequences of 8192..16384 tokens,
   // 8 heads on one: 50 us, 64 with two); a stage's slot entries and barriers beside it.  An even number: a stage then belongs to one team of warps, which cannot
@@ -114,7 +114,8 @@ __device__ __forceinline__ float warps_l(const float* sm_m, const float* sm_l, i
 
 // A consumer warp's share of a piece: 32 entries of a tile at a time.  Lane 4 r + j.
 //
-// Keys: entries are rows of the product, and two columns the high and low bytes of a query.
+// Keys: entries are rows of the product, and columns bytes of the queries: the highest two of a head side by side, the lowest ones in a tile
+// of columns of their own.
 //   G <= 2: a head's eight columns have a quarter of its channels each, zeros elsewhere, so that a lane gets the products of quarter j alone
 //   and applies that quarter's scale and zero point only.  Sums over the quarters by an exchange among four lanes that leaves each with
 //   the logit of one entry.
@@ -132,9 +133,10 @@ struct Kv4Warp {
   static constexpr int kFrags = G * kGroups > 8 ? G * kGroups / 8 : 1, kPer = kGroups / kFrags;   // fragments of weights; groups of one
   // The keys' products' B operands (a step: 32 channels, 8 of each lane's) are in shared memory, one copy for all warps, two steps to a
   // lane's 16 bytes: they would take a sixth of the registers.
-  static constexpr int kQuery = kHeads * kGroups / 2 * 32 * 16;          // bytes
+  static constexpr int kTiles = kHeads + 1;                // of columns
+  static constexpr int kQuery = kTiles * kGroups / 2 * 32 * 16;          // bytes
   static constexpr float kHeadroom = 14.f;                 // weights are held times 2^14: fp16 numbers down to 2^-28
-  int qsum[kHeads][kMasked ? 1 : kGroups];     // sum of the quarter's, or a group's, channels
+  int qsum[kHeads][kMasked ? 1 : kGroups], qlow[kHeads][kMasked ? 1 : kGroups];       // sums of the quarter's, or a group's, channels: q / 256, rest
   float factor[kHeads];        // whole numbers -> base-2 logits
   float o[kFrags][2][4];       // values' products: channels 4r + 2 half and + 1 of the column's group, columns 2j and 2j + 1
   float zo[kFrags][4];         // zero points' products: row r is the group of column r; rows 8 .. 15 are nothing
@@ -172,6 +174,7 @@ struct Kv4Warp {
   __device__ __forceinline__ void begin(const __nv_bfloat16* qrow, float scale_log2, uint4* query, bool stores) {
     const int lane = threadIdx.x & 31, r = lane >> 2, j = lane & 3;
     const bool here = !kMasked || r >> 1 == j;             // does column r hold the lane's quarter?
+    uint32_t low[kGroups][2] = {};                         // of column r of the lowest bytes' tile
 #pragma unroll
     for (int u = 0; u < kHeads; ++u) {
       // the head of column r of tile u, and of its channels those that meet this lane's codes
@@ -188,38 +191,51 @@ struct Kv4Warp {
       }
       top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));      // of all quarters, or of the lanes that share a head's groups
       top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
-      const int e = max(-100, min(100, 13 - ((int)(__float_as_uint(top) >> 23) - 127)));
+      const int e = max(-100, min(100, 21 - ((int)(__float_as_uint(top) >> 23) - 127)));
       const float up = pow2f(e), f = top < INFINITY ? scale_log2 * pow2f(-e) : __int_as_float(0x7fffffff);
       factor[u] = kMasked ? f : __shfl_sync(~0u, f, 8 * j);
-      int sum = 0;
+      int sum = 0, sum_low = 0;
 #pragma unroll
       for (int t = 0; t < kGroups; ++t) {
-        if (!kMasked) sum = 0;
+        if (!kMasked) sum = sum_low = 0;
         // in the order of the codes' bytes: channels 0, 4, 1, 5 from the low halves of a word's bytes, 2, 6, 3, 7 from the high ones
         constexpr int kAt[8] = {0, 4, 1, 5, 2, 6, 3, 7};
         uint32_t word[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           word[h] = 0;
+          uint32_t rest = 0;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int y = __float2int_rn(x[t][kAt[4 * h + i]] * up), high = (y + 128) >> 8;
-            sum += y;
-            word[h] |= (uint32_t)((r & 1 ? y - high * 256 : high) & 255) << 8 * i;
+            const int y = __float2int_rn(x[t][kAt[4 * h + i]] * up), y1 = (y + 128) >> 8, y0 = y - y1 * 256, high = (y1 + 128) >> 8;
+            sum += y1;
+            sum_low += y0;
+            word[h] |= (uint32_t)((r & 1 ? y1 - high * 256 : high) & 255) << 8 * i;
+            rest |= (uint32_t)(y0 & 255) << 8 * i;
           }
           if (!here) word[h] = 0;
+          if (here && (r & 1) == u) low[t][h] = rest;
         }
         if (stores) reinterpret_cast<uint2*>(query)[((u * kGroups + t) / 2 * 32 + lane) * 2 + (t & 1)] = make_uint2(word[0], word[1]);
         if constexpr (!kMasked) {
           sum += __shfl_xor_sync(~0u, sum, 1);
           sum += __shfl_xor_sync(~0u, sum, 2);
+          sum_low += __shfl_xor_sync(~0u, sum_low, 1);
+          sum_low += __shfl_xor_sync(~0u, sum_low, 2);
           qsum[u][t] = __shfl_sync(~0u, sum, 8 * j);
+          qlow[u][t] = __shfl_sync(~0u, sum_low, 8 * j);
         }
       }
-      if constexpr (kMasked) qsum[u][0] = sum;
+      if constexpr (kMasked) {
+        qsum[u][0] = sum;
+        qlow[u][0] = sum_low;
+      }
       m[u] = -INFINITY;
       l[u] = 0.f;
     }
+#pragma unroll
+    for (int t = 0; t < kGroups; ++t)
+      if (stores) reinterpret_cast<uint2*>(query)[((kHeads * kGroups + t) / 2 * 32 + lane) * 2 + (t & 1)] = make_uint2(low[t][0], low[t][1]);
 #pragma unroll
     for (int f = 0; f < kFrags; ++f)
 #pragma unroll
@@ -230,13 +246,15 @@ struct Kv4Warp {
   }
 
   // A step's products: words a and b hold eight codes each of rows r and r + 8.
-  __device__ __forceinline__ static void step(int (&d)[4], uint32_t a, uint32_t b, uint32_t q0, uint32_t q1) {
+  __device__ __forceinline__ static void step(int (&d)[kTiles][4], uint32_t a, uint32_t b, const uint32_t (&q)[kTiles][kGroups][2], int t) {
     constexpr uint32_t kLow = 0x0f0f0f0fu;
-    mma_m16n8k32_u8s8(d, a & kLow, b & kLow, a >> 4 & kLow, b >> 4 & kLow, q0, q1);
+    const uint32_t a0 = a & kLow, a1 = b & kLow, a2 = a >> 4 & kLow, a3 = b >> 4 & kLow;
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) mma_m16n8k32_u8s8(d[i], a0, a1, a2, a3, q[i][t][0], q[i][t][1]);
   }
-  // q.n - z sum q of row half h.
-  __device__ __forceinline__ static float part(const int (&d)[4], int h, uint32_t zero, int sum) {
-    return (float)(d[2 * h] * 256 + d[2 * h + 1] - (int)zero * sum);
+  // q.n - z sum q of row half h, head u; each of the two whole numbers is below 2^24.
+  __device__ __forceinline__ static float part(const int (&d)[kTiles][4], int h, int u, int zero, int sum, int sum_low) {
+    return fmaf((float)(d[u][2 * h] * 256 + d[u][2 * h + 1] - zero * sum), 256.f, (float)(d[kHeads][2 * h + u] - zero * sum_low));
   }
 
   // 32 entries of the stage at shared memory address `stage`, the halves' first ones entry[0] and entry[1]; ~entry: the page's number is
@@ -247,9 +265,9 @@ struct Kv4Warp {
     constexpr int kMine = kMasked ? 1 : 4;                 // logits per lane and head: entries of sub 0: r, r + 8; of sub 1
     constexpr int k8 = 8 * Row::kCodes, p8 = 8 * Row::kPairs;
     float x[kMine][kHeads];
-    uint32_t q[kHeads][kGroups][2];
+    uint32_t q[kTiles][kGroups][2];
 #pragma unroll
-    for (int i = 0; i < kHeads * kGroups / 2; ++i) {
+    for (int i = 0; i < kTiles * kGroups / 2; ++i) {
       const uint4 y = lds128(query + (i * 32 + lane) * 16);
       uint32_t (&to)[kGroups][2] = q[2 * i / kGroups];
       to[2 * i % kGroups][0] = y.x; to[2 * i % kGroups][1] = y.y;
@@ -271,13 +289,13 @@ struct Kv4Warp {
           b[0] = w.x; b[1] = w.y;
         }
         const uint32_t pair0 = lds16(tp), pair1 = lds16(tp + p8);
+        int d[kTiles][4] = {};
+#pragma unroll
+        for (int t = 0; t < kGroups; ++t) step(d, a[t], b[t], q, t);
 #pragma unroll
         for (int u = 0; u < G; ++u) {
-          int d[4] = {};
-#pragma unroll
-          for (int t = 0; t < kGroups; ++t) step(d, a[t], b[t], q[u][t][0], q[u][t][1]);
-          v[2 * sub][u] = kv4_scale(pair0 & 255) * part(d, 0, pair0 >> 8, qsum[u][0]);
-          v[2 * sub + 1][u] = kv4_scale(pair1 & 255) * part(d, 1, pair1 >> 8, qsum[u][0]);
+          v[2 * sub][u] = kv4_scale(pair0 & 255) * part(d, 0, u, pair0 >> 8, qsum[u][0], qlow[u][0]);
+          v[2 * sub + 1][u] = kv4_scale(pair1 & 255) * part(d, 1, u, pair1 >> 8, qsum[u][0], qlow[u][0]);
         }
       }
       // sums over the quarters: lane j keeps entry r + 8 (j % 2) of sub j / 2
@@ -312,15 +330,14 @@ struct Kv4Warp {
         for (int g = 0; g < kGroups; ++g) {
           const uint32_t piece = tk + (16 * g ^ swizzle);
           const uint32_t a = lds32(piece), b = lds32(piece + k8);
+          int d[kTiles][4] = {};
+          step(d, a, b, q, g);
 #pragma unroll
-          for (int u = 0; u < kHeads; ++u) {
-            int d[4] = {};
-            step(d, a, b, q[u][g][0], q[u][g][1]);
+          for (int u = 0; u < kHeads; ++u)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
               x[2 * sub + h][u] = fmaf(g & 1 ? scales[h][g / 2].y : scales[h][g / 2].x,
-                                       part(d, h, __byte_perm(pairs[h][g / 2], 0u, g & 1 ? 0x4443 : 0x4441), qsum[u][g]), x[2 * sub + h][u]);
-          }
+                                       part(d, h, u, __byte_perm(pairs[h][g / 2], 0u, g & 1 ? 0x4443 : 0x4441), qsum[u][g], qlow[u][g]), x[2 * sub + h][u]);
         }
       }
     }
