@@ -302,8 +302,9 @@ class PagedCache:
     """One wkv_paged: a key/value cache in pages and the attention over it.
 
     `k_pool`, `v_pool` [n_layers, n_pages, n_kv_heads, page_size, head_dim] are the caller's tensors where given, else made
-    here (zeros); with WKV_KV4 they are uint8 [n_layers, n_pages, n_kv_heads, page_size * (head_dim / 2 + head_dim / 16)].  The handle runs on the stream that is current when it is made (wkv_set_stream changes that); the caller
-    orders other streams' work, as for Context."""
+    here (zeros); with WKV_KV4 they are uint8 [n_layers, n_pages, n_kv_heads, page_size * (head_dim / 2 + head_dim / 16)].
+    The handle runs on the stream that is current when it is made (wkv_set_stream changes that); the caller orders other streams' work,
+    as for Context."""
 
     def __init__(self, n_layers, n_pages, page_size, n_q_heads, n_kv_heads, head_dim, max_batch, max_pages, dtype=WKV_BF16,
                  scale=0.0, scores=False, device="cuda:0", k_pool=None, v_pool=None):
@@ -332,7 +333,8 @@ class PagedCache:
                       f"{name} must be a contiguous {pool_dtype} tensor {self.shape} on {self.device}")
             self.k_pool, self.v_pool = k_pool, v_pool
             cfg.k_pool, cfg.v_pool = k_pool.data_ptr(), v_pool.data_ptr()
-            cfg.stream = torch.cuda.current_stream(self.device).cuda_stream
+            self._stream = torch.cuda.current_stream(self.device)
+            cfg.stream = self._stream.cuda_stream
 
             def _alloc(nbytes, _user):
                 try:
@@ -416,6 +418,7 @@ class PagedCache:
         for buf in (*self._bufs.values(), self.k_pool, self.v_pool):     # freed while that stream still uses them, they wait for it
             buf.record_stream(stream)
         self._check(lib().wkv_paged_set_stream(self._h, C.c_void_p(handle)))
+        self._stream = stream
 
     def wkv_paged_decode(self, layer, q, k, v, block_table, seq_lens, out, window=0, sink=0, scores=None, lse=None):
         """q [B, Hq, d], k, v [B, Hkv, d] or None, block_table [B, width] and seq_lens [B] int32 (with the new token)."""
@@ -544,6 +547,9 @@ class PagedCache:
                                         to, to_width)
         if rc:
             self._check(rc)
+        if dst._stream != self._stream:                    # dst's pools, dropped while this handle's stream writes to them, wait for it
+            dst.k_pool.record_stream(self._stream)
+            dst.v_pool.record_stream(self._stream)
 
     def wkv_status(self):
         return lib().wkv_paged_status(self._h)

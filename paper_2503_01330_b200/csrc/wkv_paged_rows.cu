@@ -108,7 +108,7 @@ int wkv_paged_append(wkv_paged* c, int32_t layer, int32_t batch, const void* q, 
   }
   if ((page_bounds == nullptr) != (page_scale == nullptr)) return fail(c, WKV_ERR_INVALID, "page_bounds and page_scale must both be given or both be NULL");
   if (page_bounds) {
-    if (!k) return fail(c, WKV_ERR_INVALID, "page bounds need k and v");
+    if (!k && total_q > 0) return fail(c, WKV_ERR_INVALID, "page bounds need k and v");      // (an empty tensor's address may be NULL)
     if (!aligned16(page_bounds)) return fail(c, WKV_ERR_INVALID, "page_bounds must be 16-byte aligned");
     const size_t chunks = (size_t)layer * f.n_pages * f.n_kv_heads;
     P.bounds = page_bounds + chunks * 2 * f.head_dim;

@@ -296,3 +296,36 @@ def test_captured_append_follows_lengths():
                 want = rotate32(q[b].float().cpu().numpy(), rope[m - 1].numpy(), False)
                 assert torch.equal(q_out[b].cpu(), torch.from_numpy(want).bfloat16())
     assert c.wkv_status() == 0
+
+
+def test_calls_of_no_tokens():
+    P = Pool([0, 0], kind="bf16", seed=25)
+    c = P.cache()
+    table, n = P.dev()
+    q, k = (torch.zeros(0, h, 128, dtype=torch.bfloat16, device="cuda") for h in (4, 2))
+    gb, gs = torch.zeros(1, P.n_pages, 2, 2, 128, dtype=torch.int8, device="cuda"), torch.zeros(1, P.n_pages, 2, device="cuda")
+    before = c.wkv_launch_count()
+    c.wkv_paged_append(0, q, k, k, table, n, torch.zeros(3, dtype=torch.int32, device="cuda"), angle_table(4, 128).cuda(), q_out=q,
+                       page_bounds=gb, page_scale=gs)
+    assert c.wkv_status() == 0 and c.wkv_launch_count() == before
+
+
+def test_calls_on_another_stream_than_their_pools():
+    """A handle moved to another stream, and a destination that lives on the first one."""
+    P, Q = Pool([300, 77], seed=26), Pool([300, 77], kind="bf16", seed=27)
+    a, b = P.cache(), Q.cache()
+    table, n = P.dev()
+    to = Q.table.cuda()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    a.wkv_set_stream(s)
+    a.wkv_paged_expand(0, table, n, b, 0, to)
+    torch.cuda.current_stream().wait_stream(s)
+    assert a.wkv_status() == 0
+    for q, m in enumerate(P.lens):
+        for h in range(2):
+            K, V = P.rows(q, h)[:2]
+            for i in (0, 15, 16, m - 1):
+                pg = int(Q.table[q, i // 16])
+                assert torch.equal(Q.gk[0, pg, h, i % 16].double().cpu(), torch.from_numpy(K[i]))
+                assert torch.equal(Q.gv[0, pg, h, i % 16].double().cpu(), torch.from_numpy(V[i]))

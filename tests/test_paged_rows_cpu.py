@@ -1,6 +1,9 @@
 """Appending, 4-bit rows and page selection, what needs no GPU: refused configurations and arguments, and the format's definition."""
 import ctypes as C
 
+import os
+import re
+
 import numpy as np
 import pytest
 import torch
@@ -141,6 +144,55 @@ def test_expand_refuses(cache):
         with pytest.raises(binding.WkvError):
             cache.wkv_paged_expand(0, **a)
     assert not cache._lib.calls
+
+
+def test_expand_keeps_pools_for_its_stream(cache):
+    """A destination of another stream may be dropped right after the call."""
+    class Pool:
+        def __init__(self):
+            self.streams = []
+
+        def record_stream(self, s):
+            self.streams.append(s)
+    cache._stream = "a"
+    dst = binding.PagedCache.__new__(binding.PagedCache)
+    dst._h = None
+    for theirs, want in (("a", []), ("b", ["a"])):
+        dst._stream, dst.k_pool, dst.v_pool = theirs, Pool(), Pool()
+        cache.wkv_paged_expand(0, i32(3, 5), i32(3), dst, 0, i32(3, 5))
+        assert dst.k_pool.streams == want and dst.v_pool.streams == want
+
+
+# ---------------------------------------------------------------- the kernels' source
+
+CSRC = os.path.join(os.path.dirname(os.path.abspath(binding.__file__)), "csrc")
+HOST = ("wkv_paged_host.cuh", "wkv_paged_rows.cu", "wkv_paged_pages.cu", "wkv_paged_kv4.cu")
+
+
+def source(name):
+    return open(os.path.join(CSRC, name)).read()
+
+
+def test_nothing_runs_on_the_default_stream():
+    for name in HOST:
+        assert not re.search(r"cudaMem(set|cpy)\(", source(name)) and "<<<" not in source(name), name
+
+
+def test_waits_that_give_up_are_heeded_and_kernels_wait_for_the_one_before():
+    for line in source("wkv_paged_decode_kv4.cuh").splitlines():
+        for call in re.finditer(r"\b(mbar_wait|wait)\(&?[a-z]", line):
+            assert re.search(r"if \(|= |return |&& |\|\| ", line[:call.start()]), line
+    for name, kernels in (("wkv_paged_rows.cuh", 2), ("wkv_paged_choose.cuh", 1), ("wkv_paged_decode_kv4.cuh", 1)):
+        bodies = re.split(r"\b__global__\b", source(name))[1:]
+        assert len(bodies) == kernels
+        for body in bodies:
+            assert body.index("griddep_launch();") < body.index("griddep_wait();"), name
+
+
+def test_rings_have_an_even_number_of_stages():
+    """Two teams take turns on the stages: with an odd number they would share one, and a barrier's parity would not tell their phases apart."""
+    text = source("wkv_paged_decode_kv4.cuh")
+    assert re.search(r"kStages = .*/ 2 \* 2;", text) and "kKv4Warps == 2 * kKv4TileWarps" in text
 
 
 # ---------------------------------------------------------------- the format
