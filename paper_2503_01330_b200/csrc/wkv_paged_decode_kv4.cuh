@@ -14,8 +14,10 @@
 // (Keys as fp16 subnormals: 163 us of arithmetic in the 16 x 8192..16384 case, masks at half rate above all.  As e4m3 numbers the matrix
 // instruction is split into fp16 ones with conversions.)
 //
-// The deal of tiles to CTAs, pieces of a lane and their join are those of the bf16 rows' kernel.  A CTA: one producer warp, which looks up 32
-// pages at a time and copies their chunks into a ring (cp.async.bulk), and eight consumer warps, four for a tile of 128 entries.
+// The deal of tiles to CTAs, pieces of a lane and their join are those of the bf16 rows' kernel.  A CTA: eight consumer warps in
+// two teams, which take tiles of 128 entries in turn, and a producer warp for each team, which looks up 32 pages at a time and copies their
+// chunks into the team's stages of a ring (cp.async.bulk).  (One producer for both: 174 us where two take 167, 40 where they take 32 in pages
+// of 16: a tile costs it some 700 cycles.)
 #pragma once
 #include "wkv_paged_decode.cuh"
 #include "wkv_paged_kv4.cuh"
@@ -23,7 +25,7 @@
 namespace wkv {
 
 constexpr int kKv4Warps = 8;                              // consumers
-constexpr int kKv4Threads = (kKv4Warps + 1) * 32;
+constexpr int kKv4Threads = (kKv4Warps + 2) * 32;         // and a producer for each team
 constexpr int kKv4Tile = 128;                             // of four warps, 32 entries each: odd and even tiles have their own warps
 constexpr int kKv4Share = 32, kKv4TileWarps = kKv4Tile / kKv4Share;
 constexpr int kKv4MaxSlots = kKv4Tile / 16;               // pages of a tile
@@ -615,19 +617,21 @@ __global__ void __launch_bounds__(kKv4Threads, (Kv4Shape<D, G>::kCtas)) paged_de
   }
   // Where page `slot` of a tile starts: its first entry, which is seen or not; of a bad page ~entry; the sequence's length if the page
   // holds nothing visible (so that no entry in it is).
-  if (warp == kKv4Warps) {                                 // ---- producer
+  if (warp >= kKv4Warps) {                                 // ---- a team's producer: every second tile
     const uint64_t policy = l2_policy_evict_first();
     fence_proxy_async();                                   // rows that earlier kernels stored are read by the copies
-    int st = 0;
+    const int team = warp - kKv4Warps;
+    int st = team, skip = team;                            // the next tile's stage; tiles of the piece before it
     uint32_t round = 0;                                    // how often the ring was filled
     for (int left = (int)(t1 - t0); left > 0;) {
       const int n = min(s.tiles - v, left);
       const int per = 32 >> slot_shift;                    // tiles whose pages are looked up together
       const long long lane_no = (long long)b * H + head;
-      for (int k0 = 0; k0 < n; k0 += per) {
+      int k0 = skip;
+      for (; k0 < n; k0 += 2 * per) {
         int entry = s.len, page_no = -1;
         {
-          const int k = k0 + (lane >> slot_shift), slot = lane & (slots - 1);
+          const int k = k0 + 2 * (lane >> slot_shift), slot = lane & (slots - 1);
           if (k < n) {
             int i = s.tile(v + k) * TILE + (slot << A.page_shift);
             if constexpr (CHOSEN) {
@@ -641,8 +645,8 @@ __global__ void __launch_bounds__(kKv4Threads, (Kv4Shape<D, G>::kCtas)) paged_de
             }
           }
         }
-        for (int k = k0; k < min(n, k0 + per); ++k) {
-          const int mine = (k - k0) << slot_shift | (lane & (slots - 1));
+        for (int i = 0; i < per && k0 + 2 * i < n; ++i) {
+          const int mine = i << slot_shift | (lane & (slots - 1));
           const int e = __shfl_sync(~0u, entry, mine), pg = __shfl_sync(~0u, page_no, mine);
           if (round > 0 && !wait(&empty[st], (round & 1) ^ 1)) return;
           const bool copies = lane < 2 * slots && pg >= 0;
@@ -657,9 +661,11 @@ __global__ void __launch_bounds__(kKv4Threads, (Kv4Shape<D, G>::kCtas)) paged_de
             const unsigned char* src = static_cast<const unsigned char*>(is_v ? A.v_pool : A.k_pool) + ((long long)pg * H + head) * chunk_bytes;
             bulk_g2s_hint(ring + st * Sh::kStage + (is_v ? Sh::kHalf : 0) + (lane & (slots - 1)) * chunk_bytes, src, chunk_bytes, &full[st], policy);
           }
-          if (++st == STAGES) { st = 0; ++round; }
+          st += 2;
+          if (st >= STAGES) { st -= STAGES; ++round; }
         }
       }
+      skip = (skip + n) & 1;
       left -= n;
       v += n;
       if (v == s.tiles && left > 0) {
