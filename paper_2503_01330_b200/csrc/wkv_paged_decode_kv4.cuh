@@ -8,9 +8,10 @@
 // takes exactly.  Scales and zero points stay outside of the products:
 //   q.k_i  = sum_g s_ig (q_g.n_ig - z_ig sum q_g)
 //   o_g    = sum_i (p_i s_ig) n_ig - sum_i (p_i s_ig) z_ig   the weights p s in fp16, the same rounded ones in both sums
-// A query head becomes whole numbers by a power of two that brings its largest channel to [2^21, 2^22): bf16 channels down to 2^-14 of it
-// stay exact, smaller ones are off by up to 2^-22 of it (two columns, 2^-14, showed in the log-sums, which are fp32).  p and p s are rounded to fp16, 2^-11 each, together a quarter of what
-// rounding the output to bf16 costs.  The weights are kept in fp16's range by a power of two that follows the largest value scale seen.
+// A query head becomes whole numbers by a power of two that brings its largest channel to [2^17, 2^18), and those that meet the high halves
+// of bytes, whose codes come out as 16 n, stay a sixteenth of the others (shifts cost 5 us of 167): bf16 channels down to 2^-10 of the largest
+// stay exact, smaller ones are off by up to 2^-18 of it, less than the log-sums, which are fp32, show (two columns, 2^-14, did show).
+// p and p s are rounded to fp16, 2^-11 each, together a quarter of what rounding the output to bf16 costs.  The weights are kept in fp16's range by a power of two that follows the largest value scale seen.
 // (Keys as fp16 subnormals: 163 us of arithmetic in the 16 x 8192..16384 case, masks at half rate above all.  As e4m3 numbers the matrix
 // instruction is split into fp16 ones with conversions.)
 //
@@ -193,8 +194,8 @@ struct Kv4Warp {
       }
       top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));      // of all quarters, or of the lanes that share a head's groups
       top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
-      const int e = max(-100, min(100, 21 - ((int)(__float_as_uint(top) >> 23) - 127)));
-      const float up = pow2f(e), f = top < INFINITY ? scale_log2 * pow2f(-e) : __int_as_float(0x7fffffff);
+      const int e = max(-100, min(100, 17 - ((int)(__float_as_uint(top) >> 23) - 127)));
+      const float up = pow2f(e), f = top < INFINITY ? scale_log2 * 0x1p-4f * pow2f(-e) : __int_as_float(0x7fffffff);
       factor[u] = kMasked ? f : __shfl_sync(~0u, f, 8 * j);
       int sum = 0, sum_low = 0;
 #pragma unroll
@@ -209,9 +210,10 @@ struct Kv4Warp {
           uint32_t rest = 0;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int y = __float2int_rn(x[t][kAt[4 * h + i]] * up), y1 = (y + 128) >> 8, y0 = y - y1 * 256, high = (y1 + 128) >> 8;
-            sum += y1;
-            sum_low += y0;
+            // 16 q; q itself where it meets 16 n
+            const int y = __float2int_rn(x[t][kAt[4 * h + i]] * up) << (h ? 0 : 4), y1 = (y + 128) >> 8, y0 = y - y1 * 256, high = (y1 + 128) >> 8;
+            sum += h ? 16 * y1 : y1;
+            sum_low += h ? 16 * y0 : y0;
             word[h] |= (uint32_t)((r & 1 ? y1 - high * 256 : high) & 255) << 8 * i;
             rest |= (uint32_t)(y0 & 255) << 8 * i;
           }
@@ -250,11 +252,11 @@ struct Kv4Warp {
   // A step's products: words a and b hold eight codes each of rows r and r + 8.
   __device__ __forceinline__ static void step(int (&d)[kTiles][4], uint32_t a, uint32_t b, const uint32_t (&q)[kTiles][kGroups][2], int t) {
     constexpr uint32_t kLow = 0x0f0f0f0fu;
-    const uint32_t a0 = a & kLow, a1 = b & kLow, a2 = a >> 4 & kLow, a3 = b >> 4 & kLow;
+    const uint32_t a0 = a & kLow, a1 = b & kLow, a2 = a & ~kLow, a3 = b & ~kLow;      // the high halves' codes times 16
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) mma_m16n8k32_u8s8(d[i], a0, a1, a2, a3, q[i][t][0], q[i][t][1]);
   }
-  // q.n - z sum q of row half h, head u; each of the two whole numbers is below 2^24.
+  // 16 (q.n - z sum q) of row half h, head u; each of the two whole numbers is below 2^24.
   __device__ __forceinline__ static float part(const int (&d)[kTiles][4], int h, int u, int zero, int sum, int sum_low) {
     return fmaf((float)(d[u][2 * h] * 256 + d[u][2 * h + 1] - zero * sum), 256.f, (float)(d[kHeads][2 * h + u] - zero * sum_low));
   }
