@@ -3,14 +3,14 @@
 //   o = sum_i p_i v_i,  p = softmax(scale q.k_i),  k_i = s_ig (n - z_ig) per group g of 32 channels, v_i likewise
 //
 // Bound: HBM at 4.5 bits a number; instruction issue close behind it, since a number may cost no more than about three lane instructions.
-// Codes are never converted.  Keys: a masked word is four bytes for mma.sync m16n8k32 on integers, against queries of 23 bits in three columns
+// Codes are never converted.  Keys: a masked word is four bytes for mma.sync m16n8k32 on integers, against queries of 22 bits in three columns
 // of eight; exact, until a group's product becomes fp32.  Values: a masked word is two fp16 subnormals n 2^-24 (or n 2^-20), which m16n8k16
 // takes exactly.  Scales and zero points stay outside of the products:
 //   q.k_i  = sum_g s_ig (q_g.n_ig - z_ig sum q_g)
 //   o_g    = sum_i (p_i s_ig) n_ig - sum_i (p_i s_ig) z_ig   the weights p s in fp16, the same rounded ones in both sums
-// A query head becomes whole numbers by a power of two that brings its largest channel to [2^17, 2^18), and those that meet the high halves
-// of bytes, whose codes come out as 16 n, stay a sixteenth of the others (shifts cost 5 us of 167): bf16 channels down to 2^-10 of the largest
-// stay exact, smaller ones are off by up to 2^-18 of it, less than the log-sums, which are fp32, show (two columns, 2^-14, did show).
+// A query head becomes whole numbers by a power of two that brings its largest channel to [2^16, 2^17), and those that meet the high halves
+// of bytes, whose codes come out as 16 n, stay a sixteenth of the others (shifts cost 5 us of 167): bf16 channels down to 2^-9 of the largest
+// stay exact, smaller ones are off by up to 2^-17 of it, less than the log-sums, which are fp32, show (two columns, 2^-14, did show).
 // p and p s are rounded to fp16, 2^-11 each, together a quarter of what rounding the output to bf16 costs.  The weights are kept in fp16's range by a power of two that follows the largest value scale seen.
 // (Keys as fp16 subnormals: 163 us of arithmetic in the 16 x 8192..16384 case, masks at half rate above all.  As e4m3 numbers the matrix
 // instruction is split into fp16 ones with conversions.)
@@ -139,7 +139,7 @@ struct Kv4Warp {
   static constexpr int kTiles = kHeads + 1;                // of columns
   static constexpr int kQuery = kTiles * kGroups / 2 * 32 * 16;          // bytes
   static constexpr float kHeadroom = 14.f;                 // weights are held times 2^14: fp16 numbers down to 2^-28
-  int qsum[kHeads][kMasked ? 1 : kGroups], qlow[kHeads][kMasked ? 1 : kGroups];       // sums of the quarter's, or a group's, channels: q / 256, rest
+  int qsum[kHeads][kMasked ? 1 : kGroups];     // sum of the quarter's, or a group's, channels, times 16
   float factor[kHeads];        // whole numbers -> base-2 logits
   float o[kFrags][2][4];       // values' products: channels 4r + 2 half and + 1 of the column's group, columns 2j and 2j + 1
   float zo[kFrags][4];         // zero points' products: row r is the group of column r; rows 8 .. 15 are nothing
@@ -194,13 +194,13 @@ struct Kv4Warp {
       }
       top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));      // of all quarters, or of the lanes that share a head's groups
       top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
-      const int e = max(-100, min(100, 17 - ((int)(__float_as_uint(top) >> 23) - 127)));
+      const int e = max(-100, min(100, 16 - ((int)(__float_as_uint(top) >> 23) - 127)));
       const float up = pow2f(e), f = top < INFINITY ? scale_log2 * 0x1p-4f * pow2f(-e) : __int_as_float(0x7fffffff);
       factor[u] = kMasked ? f : __shfl_sync(~0u, f, 8 * j);
-      int sum = 0, sum_low = 0;
+      int sum = 0;
 #pragma unroll
       for (int t = 0; t < kGroups; ++t) {
-        if (!kMasked) sum = sum_low = 0;
+        if (!kMasked) sum = 0;
         // in the order of the codes' bytes: channels 0, 4, 1, 5 from the low halves of a word's bytes, 2, 6, 3, 7 from the high ones
         constexpr int kAt[8] = {0, 4, 1, 5, 2, 6, 3, 7};
         uint32_t word[2];
@@ -212,8 +212,7 @@ struct Kv4Warp {
           for (int i = 0; i < 4; ++i) {
             // 16 q; q itself where it meets 16 n
             const int y = __float2int_rn(x[t][kAt[4 * h + i]] * up) << (h ? 0 : 4), y1 = (y + 128) >> 8, y0 = y - y1 * 256, high = (y1 + 128) >> 8;
-            sum += h ? 16 * y1 : y1;
-            sum_low += h ? 16 * y0 : y0;
+            sum += h ? 16 * y : y;
             word[h] |= (uint32_t)((r & 1 ? y1 - high * 256 : high) & 255) << 8 * i;
             rest |= (uint32_t)(y0 & 255) << 8 * i;
           }
@@ -224,16 +223,10 @@ struct Kv4Warp {
         if constexpr (!kMasked) {
           sum += __shfl_xor_sync(~0u, sum, 1);
           sum += __shfl_xor_sync(~0u, sum, 2);
-          sum_low += __shfl_xor_sync(~0u, sum_low, 1);
-          sum_low += __shfl_xor_sync(~0u, sum_low, 2);
           qsum[u][t] = __shfl_sync(~0u, sum, 8 * j);
-          qlow[u][t] = __shfl_sync(~0u, sum_low, 8 * j);
         }
       }
-      if constexpr (kMasked) {
-        qsum[u][0] = sum;
-        qlow[u][0] = sum_low;
-      }
+      if constexpr (kMasked) qsum[u][0] = sum;
       m[u] = -INFINITY;
       l[u] = 0.f;
     }
@@ -256,9 +249,9 @@ struct Kv4Warp {
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) mma_m16n8k32_u8s8(d[i], a0, a1, a2, a3, q[i][t][0], q[i][t][1]);
   }
-  // 16 (q.n - z sum q) of row half h, head u; each of the two whole numbers is below 2^24.
-  __device__ __forceinline__ static float part(const int (&d)[kTiles][4], int h, int u, int zero, int sum, int sum_low) {
-    return fmaf((float)(d[u][2 * h] * 256 + d[u][2 * h + 1] - zero * sum), 256.f, (float)(d[kHeads][2 * h + u] - zero * sum_low));
+  // 16 (q.n - z sum q) of row half h, head u: below 2^30, whatever its parts, which wrap around, are.
+  __device__ __forceinline__ static float part(const int (&d)[kTiles][4], int h, int u, uint32_t zero, int sum) {
+    return (float)(int)(((uint32_t)d[u][2 * h] * 256 + (uint32_t)d[u][2 * h + 1]) * 256 + (uint32_t)d[kHeads][2 * h + u] - zero * (uint32_t)sum);
   }
 
   // 32 entries of the stage at shared memory address `stage`, the halves' first ones entry[0] and entry[1]; ~entry: the page's number is
@@ -298,8 +291,8 @@ struct Kv4Warp {
         for (int t = 0; t < kGroups; ++t) step(d, a[t], b[t], q, t);
 #pragma unroll
         for (int u = 0; u < G; ++u) {
-          v[2 * sub][u] = kv4_scale(pair0 & 255) * part(d, 0, u, pair0 >> 8, qsum[u][0], qlow[u][0]);
-          v[2 * sub + 1][u] = kv4_scale(pair1 & 255) * part(d, 1, u, pair1 >> 8, qsum[u][0], qlow[u][0]);
+          v[2 * sub][u] = kv4_scale(pair0 & 255) * part(d, 0, u, pair0 >> 8, qsum[u][0]);
+          v[2 * sub + 1][u] = kv4_scale(pair1 & 255) * part(d, 1, u, pair1 >> 8, qsum[u][0]);
         }
       }
       // sums over the quarters: lane j keeps entry r + 8 (j % 2) of sub j / 2
@@ -341,7 +334,7 @@ struct Kv4Warp {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
               x[2 * sub + h][u] = fmaf(g & 1 ? scales[h][g / 2].y : scales[h][g / 2].x,
-                                       part(d, h, u, __byte_perm(pairs[h][g / 2], 0u, g & 1 ? 0x4443 : 0x4441), qsum[u][g], qlow[u][g]), x[2 * sub + h][u]);
+                                       part(d, h, u, __byte_perm(pairs[h][g / 2], 0u, g & 1 ? 0x4443 : 0x4441), qsum[u][g]), x[2 * sub + h][u]);
         }
       }
     }
