@@ -134,12 +134,15 @@ struct Kv4Warp {
   static constexpr bool kMasked = G <= 2;
   static constexpr int kGroups = Row::kGroups, kHeads = kMasked ? G : G / 4;       // heads of a lane's statistics: all; j and j + 4
   static constexpr int kFrags = G * kGroups > 8 ? G * kGroups / 8 : 1, kPer = kGroups / kFrags;   // fragments of weights; groups of one
-  // The keys' products' B operands (a step: 32 channels, 8 of each lane's) are in shared memory, one copy for all warps, two steps to a
-  // lane's 16 bytes: they would take a sixth of the registers.
+  // The keys' products' B operands (a step: 32 channels, 8 of each lane's) are made once for all warps, in shared memory, two steps to a
+  // lane's 16 bytes.  One head keeps them in registers (177 us under load where reading them for each tile takes 180); more heads read
+  // them for each tile (four heads: 101 us, 104 with them in registers, which then spill).
+  static constexpr bool kHolds = G == 1;
   static constexpr int kTiles = kHeads + 1;                // of columns
   static constexpr int kQuery = kTiles * kGroups / 2 * 32 * 16;          // bytes
   static constexpr float kHeadroom = 14.f;                 // weights are held times 2^14: fp16 numbers down to 2^-28
   int qsum[kHeads][kMasked ? 1 : kGroups];     // sum of the quarter's, or a group's, channels, times 16
+  uint32_t q[kTiles][kGroups][2];
   float factor[kHeads];        // whole numbers -> base-2 logits
   float o[kFrags][2][4];       // values' products: channels 4r + 2 half and + 1 of the column's group, columns 2j and 2j + 1
   float zo[kFrags][4];         // zero points' products: row r is the group of column r; rows 8 .. 15 are nothing
@@ -249,6 +252,16 @@ struct Kv4Warp {
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) mma_m16n8k32_u8s8(d[i], a0, a1, a2, a3, q[i][t][0], q[i][t][1]);
   }
+  __device__ __forceinline__ void load_query(uint32_t query) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < kTiles * kGroups / 2; ++i) {
+      const uint4 y = lds128(query + (i * 32 + lane) * 16);
+      uint32_t (&to)[kGroups][2] = q[2 * i / kGroups];
+      to[2 * i % kGroups][0] = y.x; to[2 * i % kGroups][1] = y.y;
+      to[2 * i % kGroups + 1][0] = y.z; to[2 * i % kGroups + 1][1] = y.w;
+    }
+  }
   // 16 (q.n - z sum q) of row half h, head u: below 2^30, whatever its parts, which wrap around, are.
   __device__ __forceinline__ static float part(const int (&d)[kTiles][4], int h, int u, uint32_t zero, int sum) {
     return (float)(int)(((uint32_t)d[u][2 * h] * 256 + (uint32_t)d[u][2 * h + 1]) * 256 + (uint32_t)d[kHeads][2 * h + u] - zero * (uint32_t)sum);
@@ -262,14 +275,7 @@ struct Kv4Warp {
     constexpr int kMine = kMasked ? 1 : 4;                 // logits per lane and head: entries of sub 0: r, r + 8; of sub 1
     constexpr int k8 = 8 * Row::kCodes, p8 = 8 * Row::kPairs;
     float x[kMine][kHeads];
-    uint32_t q[kTiles][kGroups][2];
-#pragma unroll
-    for (int i = 0; i < kTiles * kGroups / 2; ++i) {
-      const uint4 y = lds128(query + (i * 32 + lane) * 16);
-      uint32_t (&to)[kGroups][2] = q[2 * i / kGroups];
-      to[2 * i % kGroups][0] = y.x; to[2 * i % kGroups][1] = y.y;
-      to[2 * i % kGroups + 1][0] = y.z; to[2 * i % kGroups + 1][1] = y.w;
-    }
+    if constexpr (!kHolds) load_query(query);
     if constexpr (kMasked) {
       float v[4][G];
 #pragma unroll
@@ -690,6 +696,7 @@ __global__ void __launch_bounds__(kKv4Threads, (Kv4Shape<D, G>::kCtas)) paged_de
     const int n = min(piece->s.tiles - piece->v, piece->left);           // tiles of this piece
     w.begin(static_cast<const __nv_bfloat16*>(A.q) + (long long)piece->b * A.q_stride + (long long)piece->head * G * D, A.scale_log2, query, warp == 0);
     kv4_consumers_sync();
+    if constexpr (Warp::kHolds) w.load_query(smem_u32(query));
     const int lo = piece->s.lo;
     const unsigned fit = (unsigned)max(0, piece->s.len - 15 - lo);       // places for 16 entries, all of them seen, from lo on
     int k = skip;
