@@ -3,15 +3,17 @@
 //   o = sum_i p_i v_i,  p = softmax(scale q.k_i),  k_i = s_ig (n - z_ig) per group g of 32 channels, v_i likewise
 //
 // Bound: HBM at 4.5 bits a number; instruction issue close behind it, since a number may cost no more than about three lane instructions.
-// Codes are never converted.  Keys: a masked word is four bytes for mma.sync m16n8k32 on integers, against queries of 22 bits in three columns
+// Codes are never converted.  Keys: a masked word is four bytes for mma.sync m16n8k32 on integers, against queries of 23 bits in three columns
 // of eight; exact, until a group's product becomes fp32.  Values: a masked word is two fp16 subnormals n 2^-24 (or n 2^-20), which m16n8k16
 // takes exactly.  Scales and zero points stay outside of the products:
 //   q.k_i  = sum_g s_ig (q_g.n_ig - z_ig sum q_g)
 //   o_g    = sum_i (p_i s_ig) n_ig - sum_i (p_i s_ig) z_ig   the weights p s in fp16, the same rounded ones in both sums
-// A query head becomes whole numbers by a power of two that brings its largest channel to [2^16, 2^17), and those that meet the high halves
-// of bytes, whose codes come out as 16 n, stay a sixteenth of the others (shifts cost 5 us of 167): bf16 channels down to 2^-9 of the largest
-// stay exact, smaller ones are off by up to 2^-17 of it, less than the log-sums, which are fp32, show (two columns, 2^-14, did show).
-// p and p s are rounded to fp16, 2^-11 each, together a quarter of what rounding the output to bf16 costs.  The weights are kept in fp16's range by a power of two that follows the largest value scale seen.
+// A query head becomes whole numbers by a power of two that brings its largest channel to [2^21, 2^22), the largest that a group's sum leaves
+// room for in 32 bits: bf16 channels down to 2^-14 of it stay exact, smaller ones are off by up to 2^-22 of it.  (Fewer bits show in the
+// log-sums, which are fp32: 14 in two columns, 12 us of 174 faster, and 17 with the high halves' codes taken times 16 instead of shifted, 3
+// us, were 1e-6 and more off in sequences of one token.)
+// p and p s are rounded to fp16, 2^-11 each, together a quarter of what rounding the output to bf16 costs.  The weights are kept in
+// fp16's range by a power of two that follows the largest value scale seen.
 // (Keys as fp16 subnormals: 163 us of arithmetic in the 16 x 8192..16384 case, masks at half rate above all.  As e4m3 numbers the matrix
 // instruction is split into fp16 ones with conversions.)
 //
@@ -135,13 +137,13 @@ struct Kv4Warp {
   static constexpr int kGroups = Row::kGroups, kHeads = kMasked ? G : G / 4;       // heads of a lane's statistics: all; j and j + 4
   static constexpr int kFrags = G * kGroups > 8 ? G * kGroups / 8 : 1, kPer = kGroups / kFrags;   // fragments of weights; groups of one
   // The keys' products' B operands (a step: 32 channels, 8 of each lane's) are made once for all warps, in shared memory, two steps to a
-  // lane's 16 bytes.  One head keeps them in registers (177 us under load where reading them for each tile takes 180); more heads read
+  // lane's 16 bytes.  One head keeps them in registers (3 us of 180 under load); more heads read
   // them for each tile (four heads: 101 us, 104 with them in registers, which then spill).
   static constexpr bool kHolds = G == 1;
   static constexpr int kTiles = kHeads + 1;                // of columns
   static constexpr int kQuery = kTiles * kGroups / 2 * 32 * 16;          // bytes
   static constexpr float kHeadroom = 14.f;                 // weights are held times 2^14: fp16 numbers down to 2^-28
-  int qsum[kHeads][kMasked ? 1 : kGroups];     // sum of the quarter's, or a group's, channels, times 16
+  int qsum[kHeads][kMasked ? 1 : kGroups];     // sum of the quarter's, or a group's, channels
   uint32_t q[kTiles][kGroups][2];
   float factor[kHeads];        // whole numbers -> base-2 logits
   float o[kFrags][2][4];       // values' products: channels 4r + 2 half and + 1 of the column's group, columns 2j and 2j + 1
@@ -197,8 +199,8 @@ struct Kv4Warp {
       }
       top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));      // of all quarters, or of the lanes that share a head's groups
       top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
-      const int e = max(-100, min(100, 16 - ((int)(__float_as_uint(top) >> 23) - 127)));
-      const float up = pow2f(e), f = top < INFINITY ? scale_log2 * 0x1p-4f * pow2f(-e) : __int_as_float(0x7fffffff);
+      const int e = max(-100, min(100, 21 - ((int)(__float_as_uint(top) >> 23) - 127)));
+      const float up = pow2f(e), f = top < INFINITY ? scale_log2 * pow2f(-e) : __int_as_float(0x7fffffff);
       factor[u] = kMasked ? f : __shfl_sync(~0u, f, 8 * j);
       int sum = 0;
 #pragma unroll
@@ -213,9 +215,8 @@ struct Kv4Warp {
           uint32_t rest = 0;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            // 16 q; q itself where it meets 16 n
-            const int y = __float2int_rn(x[t][kAt[4 * h + i]] * up) << (h ? 0 : 4), y1 = (y + 128) >> 8, y0 = y - y1 * 256, high = (y1 + 128) >> 8;
-            sum += h ? 16 * y : y;
+            const int y = __float2int_rn(x[t][kAt[4 * h + i]] * up), y1 = (y + 128) >> 8, y0 = y - y1 * 256, high = (y1 + 128) >> 8;
+            sum += y;
             word[h] |= (uint32_t)((r & 1 ? y1 - high * 256 : high) & 255) << 8 * i;
             rest |= (uint32_t)(y0 & 255) << 8 * i;
           }
@@ -248,7 +249,7 @@ struct Kv4Warp {
   // A step's products: words a and b hold eight codes each of rows r and r + 8.
   __device__ __forceinline__ static void step(int (&d)[kTiles][4], uint32_t a, uint32_t b, const uint32_t (&q)[kTiles][kGroups][2], int t) {
     constexpr uint32_t kLow = 0x0f0f0f0fu;
-    const uint32_t a0 = a & kLow, a1 = b & kLow, a2 = a & ~kLow, a3 = b & ~kLow;      // the high halves' codes times 16
+    const uint32_t a0 = a & kLow, a1 = b & kLow, a2 = a >> 4 & kLow, a3 = b >> 4 & kLow;
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) mma_m16n8k32_u8s8(d[i], a0, a1, a2, a3, q[i][t][0], q[i][t][1]);
   }
@@ -262,7 +263,7 @@ struct Kv4Warp {
       to[2 * i % kGroups + 1][0] = y.z; to[2 * i % kGroups + 1][1] = y.w;
     }
   }
-  // 16 (q.n - z sum q) of row half h, head u: below 2^30, whatever its parts, which wrap around, are.
+  // q.n - z sum q of row half h, head u: below 2^22 * 15 * 32 < 2^31, whatever its parts, which wrap around, are.
   __device__ __forceinline__ static float part(const int (&d)[kTiles][4], int h, int u, uint32_t zero, int sum) {
     return (float)(int)(((uint32_t)d[u][2 * h] * 256 + (uint32_t)d[u][2 * h + 1]) * 256 + (uint32_t)d[kHeads][2 * h + u] - zero * (uint32_t)sum);
   }

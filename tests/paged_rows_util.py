@@ -4,7 +4,7 @@ What is specified operation by operation (codes, scales, zero points, bounds of 
 numpy binary32 and compared bit for bit.  The rest is compared with 64-bit arithmetic within (u = 2^-24, half a step of fp32):
   - a turned channel: two products and a sum, each rounded: 2u (|a cos| + |b sin|), then half a step of the storage type;
   - a logit over 4-bit keys: products of whole numbers, exact but for the query's: its channels become whole numbers with the head's largest
-    in [2^16, 2^17), so a channel is off by half of 1, 2^-17 of the largest: scale 2^-17 max|q| sum_c |k_c|.  Then fp32: |ds| <=
+    in [2^21, 2^22), so a channel is off by half of 1, 2^-22 of the largest: scale 2^-22 max|q| sum_c |k_c|.  Then fp32: |ds| <=
     2 (d + 16) u T with T = scale sum_c |q_c| s (n_c + z) is more than the few operations per group need;
   - bf16 rows: weights go as bf16 high and low parts, 2^-9 of 2^-9: 2^-17 A with room for one more rounding;
   - a weight: E = 2 |ds| + 2^-20 + (n + 8 + 2 T) u relative, as for bf16 rows;
@@ -170,7 +170,7 @@ def attend(q, K, V, see, scale, half, Kabs=None, Vabs=None, s_max=0.0, round_p=0
     T = float((np.abs(q) @ (Kabs if four else np.abs(K)).T)[see].max()) * scale
     ds = 2 * (d + 16) * U * T
     if four:
-        ds += scale * 2.0 ** -17 * float(np.abs(q).max()) * float(np.abs(K).sum(-1)[see].max())
+        ds += scale * 2.0 ** -22 * float(np.abs(q).max()) * float(np.abs(K).sum(-1)[see].max())
     E = 2 * ds + 2.0 ** -20 + (n + 8 + 2 * T) * U
     out = p @ V
     A = p @ np.abs(V)
