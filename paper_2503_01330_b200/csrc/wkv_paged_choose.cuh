@@ -10,6 +10,8 @@
 // -> scores -> choice.  Eight lanes share a page; the pages of a lane (sequence, kv head) are cut over CTAs, of which the last to arrive
 // (by a counter that nobody waits on) chooses.  (A cluster whose CTAs put their scores into the first one's shared memory saves 2 us of
 // that, and costs them again where the launch follows one that fills the SMs: 2048 pages, then 64 of them attended to, 21.3 us for 20.)
+//
+// Measured: one sequence of 2048 pages, 8 kv heads, 10.5 us; 16 of 256..512 pages, 32 kv heads, 14 us.
 #pragma once
 #include "wkv_paged.cuh"
 

@@ -15,7 +15,8 @@
 // carry the weights' low halves, p - bf16(p), so that the output keeps fp32-like weights at no extra instruction.
 //
 // Measured: 16 sequences of 8192..16384 tokens, 32 x 128 heads, 487 us = 6.66 TB/s (1.02 of the measured copy rate); one sequence of
-// 611 tokens, 32/8 heads, 8.7 us in a captured graph, the length of its chain of dependent loads.
+// 611 tokens, 32/8 heads, 8.7 us in a captured graph, the length of its chain of dependent loads.  Of
+// chosen pages: 64 of 256..512 pages of 32, 512 lanes, 89 us = 6.1 TB/s; 64 of 2048 pages of 16, 8 lanes, 9.2 us.
 #pragma once
 #include "wkv_paged.cuh"
 
