@@ -140,8 +140,8 @@ struct Kv4Warp {
   static constexpr int kGroups = Row::kGroups, kHeads = kMasked ? G : G / 4;       // heads of a lane's statistics: all; j and j + 4
   static constexpr int kFrags = G * kGroups > 8 ? G * kGroups / 8 : 1, kPer = kGroups / kFrags;   // fragments of weights; groups of one
   // The keys' products' B operands (a step: 32 channels, 8 of each lane's) are made once for all warps, in shared memory, two steps to a
-  // lane's 16 bytes.  One head keeps them in registers (3 us of 180 under load); more heads read
-  // them for each tile (four heads: 101 us, 104 with them in registers, which then spill).
+  // lane's 16 bytes.  One head keeps them in registers (3 us of 180 under load); more heads read them for each tile (four heads: 101 us, 104
+  // with them in registers, which then spill).
   static constexpr bool kHolds = G == 1;
   static constexpr int kTiles = kHeads + 1;                // of columns
   static constexpr int kQuery = kTiles * kGroups / 2 * 32 * 16;          // bytes

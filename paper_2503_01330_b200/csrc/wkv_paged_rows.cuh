@@ -2,10 +2,10 @@
 //
 //   y_2i = x_2i cos - x_2i+1 sin, y_2i+1 = x_2i+1 cos + x_2i sin     (or channels i and i + dim/2), angles by position from a table
 //
-// Bound: HBM; a number is read once and written once.  One launch does the queries and the new entries.  A CTA takes the part of a page
-// that one call fills (so that it owns the page's bounds, and all rows of a 4-bit page are written in full lines), for a few kv heads: the
-// angles of its rows then come from L1 after the first.  Products are rounded one by one (no fused multiply-add), so that the result is
-// the same as that of elementwise fp32 arithmetic, code for code where rows are held in 4 bits.
+// Bound: HBM; a number is read once and written once.  One launch does the queries and the new entries.  The part of a page that one call
+// fills belongs to one warp for each kv head (which so owns the page's bounds; the warps of a CTA share the rows' angles in L1), or, in 4
+// bits, to a CTA for a few kv heads, which writes all rows in full lines.  Products are rounded one by one (no fused multiply-add), so that
+// the result is the same as that of elementwise fp32 arithmetic, code for code where rows are held in 4 bits.
 //
 // Measured: prompts of 2048..8191 tokens, 4 x 32/32 heads x 128, bf16 with bounds, 220 us = 5.6 TB/s (0.86 of the measured copy rate); one
 // token each of 19 sequences 3.8 us in a captured graph; chunks of 17..61 tokens in 4 bits 8.6 us; 8 x 1638..8192 entries, 8 heads x 128,
