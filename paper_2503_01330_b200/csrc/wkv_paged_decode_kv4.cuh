@@ -23,7 +23,7 @@
 // of 16: a tile costs it some 700 cycles.)
 //
 // Measured: 16 sequences of 8192..16384 tokens, 32 x 128 heads, 161 us = 5.7 TB/s (0.87 of the measured copy rate; 180 us at the power limit
-// under load); 19 of 12000..32768, 32/8 heads, 98 us = 4.3 TB/s, bound by issue; one of 611 tokens 10.2 us in a captured graph.
+// under load); 16 of 12000..32768, 32/8 heads, 98 us = 4.3 TB/s, bound by issue; one of 611 tokens 10.2 us in a captured graph.
 #pragma once
 #include "wkv_paged_decode.cuh"
 #include "wkv_paged_kv4.cuh"
