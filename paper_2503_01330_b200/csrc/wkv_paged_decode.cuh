@@ -108,6 +108,27 @@ __device__ __forceinline__ DecodeSpan chosen_span(const PagedParams& A, int len,
   return s;
 }
 
+// CTAs for each lane, none with tiles of two, 0: runs of `chunk` tiles wherever they lie.  Few lanes whose longest has `most` tiles: one
+// where that adds no more tiles to a CTA than a join costs, else (SEVERAL) as many as there are for each by the same rule: a run of chunk
+// tiles is mostly of two lanes and joins both (128 lanes of 19 tiles in 4 bits: 24.0 us, 20.6 so; of 32
+// tiles of chosen bf16 pages, with their choice: 43.0, 41.1).
+__device__ __forceinline__ int lane_ctas(long long lanes, long long total, int most, long long chunk, bool several) {
+  if (lanes > gridDim.x) return 0;
+  if (most <= chunk + kJoinTiles) return 1;
+  if (!several || (total == lanes * most && most % (int)chunk == 0)) return 0;         // (as they are, none has tiles of two)
+  const int each = (int)(gridDim.x / (unsigned)lanes), per = (most + each - 1) / each;
+  return per <= chunk + kJoinTiles ? (most + per - 1) / per : 0;       // (no more of them than have tiles: the others' SMs would idle)
+}
+// Tiles of lane cta / cut that are this CTA's share, in the numbering of all lanes' tiles; false: none.
+__device__ __forceinline__ bool own_tiles(int cta, int cut, int H, long long lanes, const int* cum, long long& t0, long long& t1) {
+  const int lane_no = cut == 1 ? cta : cta / cut;
+  if (lane_no >= lanes) return false;
+  const int b = lane_no / H, tiles = cum[b + 1] - cum[b], per = cut == 1 ? tiles : (tiles + cut - 1) / cut, from = (cta - lane_no * cut) * per;
+  t0 = (long long)cum[b] * H + (long long)(lane_no % H) * tiles + from;
+  t1 = t0 + min(per, tiles - from);
+  return true;
+}
+
 template <typename T, int D>
 struct DecodeShape {
   static constexpr int kTile = sizeof(T) == 2 ? 64 : 32;
@@ -434,12 +455,8 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
   // Few lanes of nearly equal length: a lane each.  Joining a lane costs about as much as four tiles (7000 cycles; under a window of
   // 508, 232 lanes of ten tiles, 21.5 us with lanes cut every eight tiles, 17.2 us whole).
   const long long lanes = (long long)A.batch * H;
-  if (lanes <= gridDim.x && cum[A.batch + 1] <= chunk + kJoinTiles) {
-    if (cta >= lanes) return;
-    const int bb = cta / H, tiles = cum[bb + 1] - cum[bb];
-    t0 = (long long)cum[bb] * H + (long long)(cta % H) * tiles;
-    t1 = t0 + tiles;
-  }
+  const int cut = lane_ctas(lanes, total, cum[A.batch + 1], chunk, CHOSEN);
+  if (cut && !own_tiles(cta, cut, H, lanes, cum, t0, t1)) return;
   if (t0 >= t1) return;
   // the first piece: sequence, head, tile
   int b = 0;
@@ -626,7 +643,15 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
       consumers_sync();
       // pieces of the lane: its tiles lie at [off, off + tiles) of the deal
       const long long off = (long long)cum[b] * H + (long long)head * s.tiles;
-      const int c0 = (int)quotient(off, chunk), pieces = (int)quotient(off + s.tiles - 1, chunk) - c0 + 1;
+      int c0, pieces;
+      if (CHOSEN && cut) {
+        const int per = (s.tiles + cut - 1) / cut;
+        c0 = (int)lane_no * cut;
+        pieces = (s.tiles + per - 1) / per;
+      } else {
+        c0 = (int)quotient(off, chunk);
+        pieces = (int)quotient(off + s.tiles - 1, chunk) - c0 + 1;
+      }
       if (tid == 0) {
         const bool last = atomicAdd(P.arrived + lane_no, 1u) == (uint32_t)pieces - 1;
         if (last) P.arrived[lane_no] = 0;

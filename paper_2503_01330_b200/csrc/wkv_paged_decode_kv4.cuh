@@ -517,7 +517,8 @@ struct Kv4Warp {
 };
 
 struct Kv4Piece {
-  long long chunk;           // tiles per CTA of the deal
+  long long chunk;           // tiles per CTA of the deal, or
+  int cut;                   // CTAs for each lane
   int b, head, v, left;      // lane, first tile, tiles until the end of the CTA's run
   int last;                  // is it the last piece of its lane?
   DecodeSpan s;
@@ -591,13 +592,8 @@ __global__ void __launch_bounds__(kKv4Threads, (Kv4Shape<D, G>::kCtas)) paged_de
     for (int i = tid; i < G * D / 8; i += kKv4Threads) reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(A.out) + to)[i] = make_uint4(0, 0, 0, 0);
     if (A.lse && tid < G) A.lse[to / D + tid] = -INFINITY;
   }
-  // few lanes of nearly equal length: a lane each, as in the bf16 rows' kernel
-  if (lanes <= gridDim.x && cum[A.batch + 1] <= chunk + kJoinTiles) {
-    if (cta >= lanes) return;
-    const int bb = cta / H, tiles = cum[bb + 1] - cum[bb];
-    t0 = (long long)cum[bb] * H + (long long)(cta % H) * tiles;
-    t1 = t0 + tiles;
-  }
+  const int cut = lane_ctas(lanes, total, cum[A.batch + 1], chunk, true);
+  if (cut && !own_tiles(cta, cut, H, lanes, cum, t0, t1)) return;
   if (t0 >= t1) return;
   int b = 0;
   {
@@ -617,6 +613,7 @@ __global__ void __launch_bounds__(kKv4Threads, (Kv4Shape<D, G>::kCtas)) paged_de
   auto wait = [&](uint64_t* bar, uint32_t parity) { return (bool)__all_sync(~0u, mbar_wait(bar, parity, A.status, kWaitPolls)); };
   if (tid == 0) {
     piece->chunk = chunk;
+    piece->cut = cut;
     piece->b = b; piece->head = head; piece->v = v; piece->left = (int)(t1 - t0);
     piece->s = s;
   }
@@ -772,7 +769,8 @@ __global__ void __launch_bounds__(kKv4Threads, (Kv4Shape<D, G>::kCtas)) paged_de
       kv4_consumers_sync();
       // pieces of the lane: its tiles lie at [off, off + tiles) of the deal
       const long long off = (long long)cum[b] * H + (long long)head * tiles, chunk = piece->chunk;
-      const int c0 = (int)quotient(off, chunk), pieces = (int)quotient(off + tiles - 1, chunk) - c0 + 1;
+      const int cut = piece->cut, per = cut ? (tiles + cut - 1) / cut : 1;
+      const int c0 = cut ? (int)lane_no * cut : (int)quotient(off, chunk), pieces = cut ? (tiles + per - 1) / per : (int)quotient(off + tiles - 1, chunk) - c0 + 1;
       if (tid == 0) {
         const bool last = atomicAdd(P.arrived + lane_no, 1u) == (uint32_t)pieces - 1;
         if (last) P.arrived[lane_no] = 0;

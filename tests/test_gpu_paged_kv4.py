@@ -52,6 +52,12 @@ def test_long_lanes_in_pieces():
     go([3333, 4444, 1234, 0, 2222], hq=4, hk=4, page=64, seed=5)
 
 
+@pytest.mark.parametrize("lens", [[2368] * 16, [2400, 2304, 1, 0, 130, 2399, 2305, 257, 2300, 2300, 2300, 2300, 2300, 2300, 2300, 2300], [1500] * 9])
+def test_lanes_of_nearly_equal_length(lens):
+    """A few CTAs for each lane, of which short lanes use some; more than one tile each."""
+    go(lens, hq=16, hk=8, d=64, page=32, seed=7)
+
+
 def test_many_short_lanes_and_layers():
     go([(i * 37) % 90 for i in range(70)], hq=8, hk=4, layers=2, extra_cols=3, seed=6)
 
