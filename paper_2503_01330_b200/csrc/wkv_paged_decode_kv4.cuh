@@ -523,6 +523,7 @@ struct Kv4Piece {
   int last;                  // is it the last piece of its lane?
   DecodeSpan s;
 };
+static_assert(sizeof(Kv4Piece) <= 64, "Kv4Shape::kOther");
 
 __device__ __forceinline__ void kv4_consumers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kKv4Warps * 32) : "memory"); }
 
