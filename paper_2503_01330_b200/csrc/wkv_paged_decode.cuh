@@ -456,7 +456,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
   // 508, 232 lanes of ten tiles, 21.5 us with lanes cut every eight tiles, 17.2 us whole).
   const long long lanes = (long long)A.batch * H;
   const int cut = lane_ctas(lanes, total, cum[A.batch + 1], chunk, CHOSEN);
-  if (cut && !own_tiles(cta, cut, H, lanes, cum, t0, t1)) return;
+  if (cut && !own_tiles(cta, CHOSEN ? cut : 1, H, lanes, cum, t0, t1)) return;
   if (t0 >= t1) return;
   // the first piece: sequence, head, tile
   int b = 0;
