@@ -96,6 +96,12 @@ def test_long_sequences(kind):
     go([5000], 40, 2, 1, kind=kind, hq=8, hk=2, page=64, seed=32)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+def test_lanes_that_share_the_sms_evenly(kind):
+    """A hundred lanes of the same number of chosen pages, and some of less: a few CTAs for each, more than a tile each."""
+    go([1900, 1500, 1000, 1100, 0, 16, 1200, 300, 1300, 1000, 1001, 1002, 1400], 60, 2, 1, kind=kind, hq=8, hk=8, d=64, page=16, seed=9)
+
+
 def test_many_pages_and_ties():
     """Scores held in registers and looked up; whole bits of equal scores, negative and signed zeros among them."""
     for n, n_select in ((2048, 64), (2049, 64), (9999, 5), (9999, 4321)):
