@@ -710,7 +710,8 @@ __global__ void __launch_bounds__(kKv4Threads, (Kv4Shape<D, G>::kCtas)) paged_de
       if (!ok) continue;
       const int e0 = (int)lds32(entry0 + at_stage * (kKv4MaxSlots * 4)), e1 = (int)lds32(entry1 + at_stage * (kKv4MaxSlots * 4));
       const uint32_t stage = ring0 + at_stage * Sh::kStage;
-      if ((unsigned)(e0 + first - lo) < fit && (unsigned)(e1 + second - lo) < fit) {
+      // (no bad page: the complement of a first entry 0 would be a place like others, 31 or 47 rows into a page of 64)
+      if ((e0 | e1) >= 0 && (unsigned)(e0 + first - lo) < fit && (unsigned)(e1 + second - lo) < fit) {
         w.template tile<true>(stage, at, 0, 0, DecodeSpan(), smem_u32(mine), smem_u32(query));
       } else {
         // first entries, complements for bad pages
