@@ -202,7 +202,8 @@ struct Kv4Warp {
       }
       top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));      // of all quarters, or of the lanes that share a head's groups
       top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
-      const int e = max(-100, min(100, 21 - ((int)(__float_as_uint(top) >> 23) - 127)));
+      // (-106: up to the largest finite bf16 number; queries of less than 2^-99 keep fewer bits, so that 2^-e stays clear of subnormals)
+      const int e = max(-106, min(120, 21 - ((int)(__float_as_uint(top) >> 23) - 127)));
       const float up = pow2f(e), f = top < INFINITY ? scale_log2 * pow2f(-e) : __int_as_float(0x7fffffff);
       factor[u] = kMasked ? f : __shfl_sync(~0u, f, 8 * j);
       int sum = 0;

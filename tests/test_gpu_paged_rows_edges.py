@@ -81,3 +81,23 @@ def test_bad_page_counts_as_zeros_wherever_it_lies(page, hq, hk, d, column):
                 for r in range(h * P.G, (h + 1) * P.G):
                     w, z, bo, bz = attend(P.q[b, r].double().numpy(), K, V, window_sees(n, window, sink), P.scale, P.half, Ka, Va, sm)
                     assert (np.abs(out[b, r] - w) <= bo).all() and abs(lse[b, r] - z) <= bz, (b, r, window, sink)
+
+
+# ---- queries of any finite size
+
+@pytest.mark.parametrize("hq,hk", [(2, 2), (4, 2), (8, 2), (8, 1)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_queries_and_softmax_scale_by_inverse_powers_of_two(hq, hk, d):
+    """Queries times 2^n and the softmax scale times 2^-n are the same attention, bit for bit: the codes' products take a power of two of the
+    query into the scale."""
+    scale = float(np.float32(1 / np.sqrt(d)))
+    P = Pool([300, 17, 2000], hq=hq, hk=hk, d=d, page=32, seed=d + hq)
+    P.q = (P.q.float().sign() * (P.q.float().abs() + 2.0 ** -6)).bfloat16()        # no channel so small that 2^-96 of it has fewer bits
+    want = decode(P, P.cache(scale=scale))
+    assert want[2] == 0
+    P.check(want[0], want[1], lambda b, h: window_sees(P.lens[b], 0, 0))
+    for n in (60, 114, 119, 121, 123, -60, -96):
+        q = (P.q.float() * 2.0 ** n).bfloat16()
+        assert torch.isfinite(q.float()).all() and torch.equal(q.double() * 2.0 ** -n, P.q.double())
+        got = decode(P, P.cache(scale=scale * 2.0 ** -n), q)
+        assert got[2] == 0 and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), n
