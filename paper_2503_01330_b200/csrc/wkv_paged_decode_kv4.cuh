@@ -106,7 +106,8 @@ __device__ __forceinline__ uint32_t half_max(uint32_t a, uint32_t b) {
 }
 __device__ __forceinline__ float2 half_pair_f(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2*>(&x)); }
 
-// Largest logit of a head over the warps, and its sum relative to that.
+// Largest logit of a head over the warps, and its sum relative to that.  (A sum is 0 where nothing is seen; logits that are no numbers, and
+// so never the largest, leave one that is none either, which goes on into outputs and log-sums.)
 __device__ __forceinline__ float warps_max(const float* sm_m, int head) {
   float m = sm_m[head];
 #pragma unroll
@@ -116,7 +117,7 @@ __device__ __forceinline__ float warps_max(const float* sm_m, int head) {
 __device__ __forceinline__ float warps_l(const float* sm_m, const float* sm_l, int head, float big) {
   float l = 0.f;
 #pragma unroll
-  for (int i = 0; i < kKv4Warps; ++i) l += sm_m[i * 8 + head] == -INFINITY ? 0.f : sm_l[i * 8 + head] * exp2_fast(sm_m[i * 8 + head] - big);
+  for (int i = 0; i < kKv4Warps; ++i) l += sm_l[i * 8 + head] == 0.f ? 0.f : sm_l[i * 8 + head] * exp2_fast(sm_m[i * 8 + head] - big);
   return l;
 }
 
@@ -747,12 +748,12 @@ __global__ void __launch_bounds__(kKv4Threads, (Kv4Shape<D, G>::kCtas)) paged_de
       return x;
     };
     auto finish = [&](int e, float4 x, float total_l) {
-      const float inv = total_l > 0.f ? 1.f / total_l : 0.f;
+      const float inv = total_l == 0.f ? 0.f : 1.f / total_l;
       __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + ((long long)b * A.n_q_heads + hq0) * D + e * 4;
       *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));
     };
     auto finish_lse = [&](int g, float mm, float ll) {
-      if (A.lse) A.lse[(long long)b * A.n_q_heads + hq0 + g] = ll > 0.f ? (mm + log2f(ll)) * kLn2 : -INFINITY;
+      if (A.lse) A.lse[(long long)b * A.n_q_heads + hq0 + g] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * kLn2;
     };
     if (whole) {
       for (int e = tid; e < kVecs; e += kKv4Warps * 32) {

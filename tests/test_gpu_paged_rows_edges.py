@@ -101,3 +101,31 @@ def test_queries_and_softmax_scale_by_inverse_powers_of_two(hq, hk, d):
         assert torch.isfinite(q.float()).all() and torch.equal(q.double() * 2.0 ** -n, P.q.double())
         got = decode(P, P.cache(scale=scale * 2.0 ** -n), q)
         assert got[2] == 0 and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), n
+
+
+# ---- queries that are no numbers
+
+def check_nan_queries(kind, hq, hk, page=16):
+    """The heads that have a NaN, or logits without a largest number, get NaN for output and log-sum, whole or cut into pieces; the
+    others and padded rows what they got without it."""
+    P = Pool([5000, 40, 0, 300], hq=hq, hk=hk, kind=kind, page=page, seed=5)
+    c = P.cache()
+    lists = shuffled_lists(P, 1, False)
+    q = P.q.clone()
+    q[0, 0, 3] = q[1, hq - 1, 70] = q[2, 0, 0] = float("nan")
+    q[3, 1 % hq] = float("inf")
+    hit = torch.zeros(4, hq, dtype=torch.bool)
+    hit[0, 0] = hit[1, hq - 1] = hit[3, 1 % hq] = True
+    for over in (None, lists):
+        out, lse, status = decode(P, c, None, lists=over)
+        nan_out, nan_lse, nan_status = decode(P, c, q, lists=over)
+        assert status == 0 and nan_status == 0
+        assert torch.isnan(nan_out.float().cpu()[hit]).all() and torch.isnan(nan_lse.cpu()[hit]).all()
+        assert torch.equal(nan_out.cpu()[~hit], out.cpu()[~hit]) and torch.equal(nan_lse.cpu()[~hit], lse.cpu()[~hit])
+        assert (out[2] == 0).all() and (lse[2] == -float("inf")).all()
+
+
+@pytest.mark.parametrize("hq,hk", [(2, 2), (4, 2), (8, 2), (8, 1)])
+def test_queries_with_a_nan_show_in_log_sums_of_4_bit_rows(hq, hk):
+    check_nan_queries("kv4", hq, hk)
+    check_nan_queries("kv4", hq, hk, 64)
