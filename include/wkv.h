@@ -271,7 +271,8 @@ const char* wkv_last_error(const wkv_ctx* ctx);
  *   - Pool rows behind a sequence's length are never used, whatever bits they hold.  Rows inside it are expected to be finite:
  *     an infinity or NaN in one may make any output of that sequence NaN, also of tokens that do not see the entry.
  *   - out, lse and scores must not overlap a call's other arguments.
- *   - A row that sees no entry (a padded sequence of length 0) gets output 0 and log-sum -infinity.
+ *   - A row that sees no entry (a padded sequence of length 0) gets output 0 and log-sum -infinity; a decode step's whose query has a NaN gets
+ *     NaN for both.
  *   - The token at position p sees entry i if i <= p and (window == 0, or i > p - window, or i < sink).
  *   - scores [batch, n_kv_heads, score_stride] fp32, or NULL: the attention weight of every entry, averaged over the kv
  *     head's query heads, is added to it, the sum over the call's tokens in a fixed order.  Entries that the call appends

@@ -620,8 +620,9 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
       my_M = piece_max(sm_m, tid);
 #pragma unroll
       for (int i = 0; i < kDecodeWarps; ++i) {
-        const float mi = sm_m[i * 8 + tid];
-        my_L += mi == -INFINITY ? 0.f : sm_l[i * 8 + tid] * exp2_fast(mi - my_M);
+        // 0: nothing seen; logits that are no numbers, and so never the largest, leave a sum that is none, which goes on into the output
+        const float li = sm_l[i * 8 + tid];
+        my_L += li == 0.f ? 0.f : li * exp2_fast(sm_m[i * 8 + tid] - my_M);
       }
     }
 #pragma unroll
@@ -698,14 +699,14 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) paged_decode_kernel(const _
       for (int e = tid; e < G * D / 4; e += 128) {
         const int g = e / (D / 4), c = e % (D / 4) * 4;
         const float4 x = *reinterpret_cast<const float4*>(sm_out + g * Sh::kOutStride + c);
-        const float inv = sm_l[g] > 0.f ? 1.f / sm_l[g] : 0.f;
+        const float inv = sm_l[g] == 0.f ? 0.f : 1.f / sm_l[g];
         T* out = static_cast<T*>(A.out) + ((long long)b * A.n_q_heads + hq0 + g) * D + c;
         if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));
         else *reinterpret_cast<float4*>(out) = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
       }
       if (tid < G) {
         const long long at = (long long)b * A.n_q_heads + hq0 + tid;
-        if (A.lse) A.lse[at] = sm_l[tid] > 0.f ? (sm_m[tid] + log2f(sm_l[tid])) * kLn2 : -INFINITY;
+        if (A.lse) A.lse[at] = sm_l[tid] == 0.f ? -INFINITY : (sm_m[tid] + log2f(sm_l[tid])) * kLn2;
         if (P.logits && !P.fold_inside) P.head_ml[at] = make_float2(sm_m[tid], sm_l[tid] > 0.f ? 1.f / sm_l[tid] : 0.f);
       }
       if (!CHOSEN && P.fold_inside) {

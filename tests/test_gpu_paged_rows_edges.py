@@ -129,3 +129,9 @@ def check_nan_queries(kind, hq, hk, page=16):
 def test_queries_with_a_nan_show_in_log_sums_of_4_bit_rows(hq, hk):
     check_nan_queries("kv4", hq, hk)
     check_nan_queries("kv4", hq, hk, 64)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hk", [(2, 2), (4, 2), (8, 2), (8, 1)])
+def test_queries_with_a_nan_show_in_log_sums(kind, hq, hk):
+    check_nan_queries(kind, hq, hk)
