@@ -386,7 +386,9 @@ int wkv_paged_evict(wkv_paged* c, int32_t layer, int32_t batch, const int32_t* s
  *        not overlap the call's other arguments otherwise.  Rows of no sequence are left as they were
  *   page_bounds device [n_layers, n_pages, n_kv_heads, 2, head_dim] int8 and page_scale [n_layers, n_pages, n_kv_heads], or both
  *        NULL: of every page that gets an entry the bounds of its keys, as stored, up to the sequence's length: page_scale =
- *        (largest magnitude) * (1/127), and per channel the largest key / page_scale rounded up and the least rounded down.  A page
+ *        (largest magnitude) * (1/127), and per channel the largest key / page_scale rounded up and the least rounded down (0 where
+ *        page_scale is below 2^-100).  Of rows that are not finite: a NaN counts as no key, an infinite key, or a channel without a
+ *        number, makes page_scale infinite and the page's score infinity or NaN, which rank above all others.  A page
  *        that another sequence shares must hold the same entries for both.  Calls that store or move entries otherwise (wkv_paged_decode
  *        and wkv_paged_prefill with k and v, wkv_paged_evict) keep no bounds; a page's are whole again once it gets an entry here. */
 int wkv_paged_append(wkv_paged* c, int32_t layer, int32_t batch, const void* q, int64_t q_stride, const void* k, const void* v,

@@ -219,11 +219,13 @@ __device__ __forceinline__ float2 pair_shuffle(float2 a, int off) { return make_
 template <typename T> struct PairOf { typedef __nv_bfloat162 type; };
 template <> struct PairOf<float> { typedef float2 type; };
 
-// A page's scale and its inverse; a bound in steps of it, outwards (what is not finite ends at the border).
+// A page's scale and its inverse; a bound in steps of it, outwards.  An infinite key makes the scale infinite and its own products no
+// numbers: those end at the outer border, here the largest at 127 and the least at -127 (minima and maxima drop what is no number), all
+// others are 0, so that the page's score is infinity or no number, and the page among the chosen.
 struct BoundScale {
   float scale, inv;
-  __device__ __forceinline__ uint32_t up(float x) const { return (uint32_t)(int)fminf(fmaxf(ceilf(__fmul_rn(x, inv)), -127.f), 127.f) & 255; }
-  __device__ __forceinline__ uint32_t down(float x) const { return (uint32_t)(int)fmaxf(fminf(floorf(__fmul_rn(x, inv)), 127.f), -127.f) & 255; }
+  __device__ __forceinline__ uint32_t up(float x) const { return (uint32_t)(int)fmaxf(fminf(ceilf(__fmul_rn(x, inv)), 127.f), -127.f) & 255; }
+  __device__ __forceinline__ uint32_t down(float x) const { return (uint32_t)(int)fminf(fmaxf(floorf(__fmul_rn(x, inv)), -127.f), 127.f) & 255; }
 };
 
 __device__ __forceinline__ BoundScale bound_scale(float most) {

@@ -135,3 +135,42 @@ def test_queries_with_a_nan_show_in_log_sums_of_4_bit_rows(hq, hk):
 @pytest.mark.parametrize("hq,hk", [(2, 2), (4, 2), (8, 2), (8, 1)])
 def test_queries_with_a_nan_show_in_log_sums(kind, hq, hk):
     check_nan_queries(kind, hq, hk)
+
+
+# ---- keys that are not finite
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_pages_with_an_infinite_key_are_chosen_first(kind, d):
+    """Their scale is infinite and their bounds lie outwards, so that their score is +infinity or no number, which both rank above all."""
+    P = Pool([600, 77], hq=4, hk=2, d=d, kind=kind, seed=d)
+    g = torch.Generator().manual_seed(2)
+    k, v = (torch.randn(677, 2, d, generator=g).to(P.tdt) for _ in range(2))
+    up, down, both = [(0, 33, 1, 5)], [(0, 100, 0, d - 1), (1, 20, 1, 0)], [(0, 330, 1, 17), (0, 331, 1, 17)]      # sequence, entry, head, channel
+    for (b, i, h, ch), x in [*((e, np.inf) for e in up), *((e, -np.inf) for e in down), (both[0], np.inf), (both[1], -np.inf)]:
+        k[600 * b + i, h, ch] = x
+    c = P.cache()
+    table, n = P.dev()
+    gb = torch.zeros(1, P.n_pages, 2, 2, d, dtype=torch.int8, device="cuda")
+    gs = torch.zeros(1, P.n_pages, 2, device="cuda")
+    start = torch.tensor([0, 600, 677], dtype=torch.int32, device="cuda")
+    c.wkv_paged_append(0, None, k.cuda(), v.cuda(), table, n, start, page_bounds=gb, page_scale=gs)
+    bounds, scale = gb.cpu()[0], gs.cpu()[0]
+    loud = {(b, i // 16, h) for b, i, h, _ in up + down + both}
+    for b in range(2):
+        for p in range(-(-P.lens[b] // 16)):
+            for h in range(2):
+                assert torch.isinf(scale[int(P.table[b, p]), h]) == ((b, p, h) in loud)
+    for b, i, h, ch in up + both[:1]:
+        assert bounds[int(P.table[b, i // 16]), h, 0, ch] == 127
+    for b, i, h, ch in down + both[:1]:
+        assert bounds[int(P.table[b, i // 16]), h, 1, ch] == -127
+    for seed in range(3):
+        q = torch.randn(2, 4, d, generator=g).to(P.tdt)
+        if seed == 2:
+            q[:] = 0
+        ps, pages = torch.zeros(2, 2, P.width, device="cuda"), torch.zeros(2, 2, 4, dtype=torch.int32, device="cuda")
+        c.wkv_paged_select(0, q.cuda(), table, n, gb, gs, ps, pages, recent=1)
+        for b, p, h in loud:
+            assert not ps[b, h, p] < float("inf") and p in pages[b, h].tolist()
+    assert c.wkv_status() == 0
