@@ -367,6 +367,8 @@ int wkv_paged_evict(wkv_paged* c, int32_t layer, int32_t batch, const int32_t* s
  *           x = (i / 2) % 4 for D = 128, (i / 4) % 2 for D = 64
  *   values  r = 4 u + e: in the 16-bit word at byte (2 S u + 2 g) ^ x of the row, bits 4 e and the three above;
  *           x = 32 ((i / 2) % 2) for D = 128, 0 for D = 64
+ * A decode step rounds an entry's weight times a value scale by 2^-10 of itself at most, or, where that is more, by 2^-34 of the head's
+ * largest weight times the largest value scale in sight.
  * Such a handle takes wkv_paged_append, wkv_paged_decode (k and v, where given, are stored in 4 bits first, and the new token sees its
  * entry as stored), wkv_paged_select, wkv_paged_decode_pages and wkv_paged_expand; prompts run on bf16 rows (wkv_paged_expand). */
 

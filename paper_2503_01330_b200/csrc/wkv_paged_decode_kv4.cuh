@@ -13,7 +13,8 @@
 // log-sums, which are fp32: 14 in two columns, 12 us of 174 faster, and 17 with the high halves' codes taken times 16 instead of shifted, 3
 // us, were 1e-6 and more off in sequences of one token.)
 // p and p s are rounded to fp16, 2^-11 each, together a quarter of what rounding the output to bf16 costs.  The weights are kept in
-// fp16's range by a power of two that follows the largest value scale seen.
+// fp16's range by a power of two that follows the largest value scale seen, whatever weight its row has: p s is also off by up to 2^-39 of that
+// scale times the largest weight (p by 2^-34 of the latter where that scale is 256 or more).
 // (Keys as fp16 subnormals: 163 us of arithmetic in the 16 x 8192..16384 case, masks at half rate above all.  As e4m3 numbers the matrix
 // instruction is split into fp16 ones with conversions.)
 //
@@ -154,7 +155,7 @@ struct Kv4Warp {
   float zo[kFrags][4];         // zero points' products: row r is the group of column r; rows 8 .. 15 are nothing
   float m[kHeads], l[kHeads];
   uint32_t largest;            // twice the bits of the largest value scale seen, which the weights' power of two follows
-  uint32_t shift;              // that power of two, twice
+  uint32_t shift;              // what of that power of two the scales take, twice: multiples of 2^-17 of four bits, they stay exact down to 2^-7
 
   // Where the lane's words lie in a stage: codes and pairs of its first 16 entries' keys (values: `half` bytes behind), and how far behind
   // them those of the other 16 are.
@@ -401,7 +402,12 @@ struct Kv4Warp {
         }
       }
       if (__any_sync(~0u, top != largest)) widen(top);
-      const uint2 p = lds64(weights + 2 * (head_of(r) * 32 + sub * 16 + 4 * j));
+      uint2 p = lds64(weights + 2 * (head_of(r) * 32 + sub * 16 + 4 * j));
+      if (largest >= 0x5c000000u) {                        // 256 and more: the weights take the rest, 2^-1 .. 2^-5
+        const uint32_t rest = (37 - (largest >> 26)) * 0x04000400u;
+        p.x = half_mul(p.x, rest);
+        p.y = half_mul(p.y, rest);
+      }
       uint32_t b[kFrags][2];
 #pragma unroll
       for (int f = 0; f < kFrags; ++f) {
@@ -464,13 +470,16 @@ struct Kv4Warp {
     }
     scale_sums(f[0], f[kHeads - 1]);
   }
-  // A larger value scale: it comes to [1, 2) by 2^(15 - its exponent field).
+  // The power of two that brings the largest value scale to [1, 2).
+  __device__ __forceinline__ static float power(uint32_t largest) { return pow2f(15 - max(1, (int)(largest >> 26))); }
+  // A larger value scale.
   __device__ __forceinline__ void widen(uint32_t top) {
     top = __reduce_max_sync(~0u, max(top & 0xffffu, top >> 16));
-    const float was = half_pair_f(shift).x, to = pow2f(15 - max(1, (int)(top >> 10))), ratio = largest ? to / was : 0.f;
+    top |= top << 16;
+    const float to = power(top), ratio = largest ? to / power(largest) : 0.f, part = fmaxf(to, 0x1p-7f);
     scale_sums(ratio, ratio);
-    largest = top | top << 16;
-    shift = half_pair(to, to);
+    largest = top;
+    shift = half_pair(part, part);
   }
 
   // (max, sum) of the heads over this warp's entries to [8] each
@@ -495,7 +504,7 @@ struct Kv4Warp {
     for (int f = 0; f < kFrags; ++f)                       // column r meets its own group in row r
       if (j == r >> 1 && (G == 1 ? r < kGroups : G == 2 ? r >> 1 < kGroups : true)) zeros[group_of(f, r) * G + head_of(r)] = r & 1 ? zo[f][1] : zo[f][0];
     __syncwarp();
-    const float back = largest ? 0x1p10f / half_pair_f(shift).x : 0.f;     // codes' 2^24, weights' 2^-14
+    const float back = largest ? 0x1p10f / power(largest) : 0.f;     // codes' 2^24, weights' 2^-14
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       const int head = head_of(2 * j + c), which = G == 1 ? 2 * j + c : G == 2 ? j : G == 4 ? c : 0;     // the column's group in its fragment

@@ -174,3 +174,41 @@ def test_pages_with_an_infinite_key_are_chosen_first(kind, d):
         for b, p, h in loud:
             assert not ps[b, h, p] < float("inf") and p in pages[b, h].tolist()
     assert c.wkv_status() == 0
+
+
+# ---- value scales far apart
+
+@pytest.mark.parametrize("hq,hk,d,page", [(2, 2, 128, 16), (4, 2, 64, 64), (8, 2, 128, 32), (8, 1, 128, 64)])
+@pytest.mark.parametrize("n", [40, 600])
+@pytest.mark.parametrize("small", [2.0 ** -11, 2.0 ** -13, 2.0 ** -15])
+def test_large_values_without_weight_leave_small_ones_their_bits(hq, hk, d, page, n, small):
+    """Entry 0 has value scales at the format's upper end and next to no weight.  A weight times a scale, fp16 times a power of two that
+    brings the largest scale S to [1, 2) and weights of 1 to 2^14, is off by 2^-25 at most where it is below fp16's normal range: 2^-39 S,
+    or by all of it; the weight itself by 2^-25 2^-9 of the largest at most.  The other roundings are relative."""
+    from paged_rows_util import pack_chunks
+    P = Pool([n], hq=hq, hk=hk, d=d, page=page, seed=n + hq)
+    g = torch.Generator().manual_seed(n)
+    shape = (1, P.n_pages, hk, page, d)
+    K, V = torch.randn(shape, generator=g), torch.randn(shape, generator=g) * small
+    q = torch.randn(1, hq, d, generator=g) * 2
+    K[..., 0], q[..., 0] = 0.0, 16.0
+    first = int(P.table[0, 0])
+    K[0, first, :, 0, 0] = -120.0
+    V[0, first, :, 0] = 6e4 * torch.randn(hk, d, generator=g).sign()
+    P.k_pool, P.v_pool = (torch.from_numpy(pack_chunks(w, x.bfloat16().float().numpy())[0]) for w, x in (("k", K), ("v", V)))
+    q = q.bfloat16()
+    out, lse, status = decode(P, P.cache(), q)
+    assert status == 0
+    out = out.double().cpu().numpy()
+    for h in range(hk):
+        K64, V64, Ka, Va, _ = P.rows(0, h)
+        for r in range(h * P.G, (h + 1) * P.G):
+            x = q[0, r].double().numpy()
+            w, z, bo, _ = attend(x, K64, V64, np.ones(n, bool), P.scale, P.half, Ka, Va, 0.0)
+            p = np.exp(K64 @ x * P.scale - z)
+            top = p.max()
+            assert p[0] < 1e-30
+            step = np.abs(Va)                                                  # s (n + z), 0 .. 30 s
+            lost = np.minimum(p[:, None] * step, 15 * 2.0 ** -39 * 4096.0 * 2 * top)[1:].sum(0) + 2.0 ** -34 * top * step[1:].sum(0)
+            e = np.abs(out[0, r] - w) / (bo + lost)
+            assert (e <= 1).all(), f"head {r}: {e.max():.3g} of the bound"
