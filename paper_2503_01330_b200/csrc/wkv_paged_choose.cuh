@@ -270,9 +270,10 @@ __global__ void __launch_bounds__(kChooseThreads, 4) paged_choose_kernel(const _
   const int first = split * each + warp * 4;               // of this warp's four pages
   load(first + (lane >> 3));
   {
+    // (an eighth of the query: up to eight heads' sums stay finite, and the codes are the same)
     if (tid < D) {
       for (int g = 0; g < G; ++g) {
-        const float x = g == 0 ? q0 : (float)q[g * D];
+        const float x = 0.125f * (g == 0 ? q0 : (float)q[g * D]);
         up = __fadd_rn(up, fmaxf(x, 0.f));
         down = __fadd_rn(down, fminf(x, 0.f));
       }
@@ -285,7 +286,7 @@ __global__ void __launch_bounds__(kChooseThreads, 4) paged_choose_kernel(const _
     most = 0.f;
 #pragma unroll
     for (int w = 0; w < D / 32; ++w) most = fmaxf(most, part[w]);
-    const float step = __fmul_rn(most, 1.f / 127.f), inv = step >= 0x1p-100f ? __frcp_rn(step) : 0.f;
+    const float step = __fmul_rn(most, 1.f / 127.f), inv = step >= 0x1p-103f ? __frcp_rn(step) : 0.f;
     if (tid < D) {
       code[0][tid] = (int8_t)(int)fminf(fmaxf(rintf(__fmul_rn(up, inv)), 0.f), 127.f);
       code[1][tid] = (int8_t)(int)fmaxf(fminf(rintf(__fmul_rn(down, inv)), 0.f), -127.f);

@@ -212,3 +212,29 @@ def test_large_values_without_weight_leave_small_ones_their_bits(hq, hk, d, page
             lost = np.minimum(p[:, None] * step, 15 * 2.0 ** -39 * 4096.0 * 2 * top)[1:].sum(0) + 2.0 ** -34 * top * step[1:].sum(0)
             e = np.abs(out[0, r] - w) / (bo + lost)
             assert (e <= 1).all(), f"head {r}: {e.max():.3g} of the bound"
+
+
+# ---- choosing pages
+
+@pytest.mark.parametrize("kind", ["bf16", "f32", "kv4"])
+@pytest.mark.parametrize("hq,hk", [(8, 1), (4, 2)])
+def test_choice_does_not_depend_on_a_factor_of_the_query(kind, hq, hk):
+    """Scores are in steps of the query's largest channel sum: whatever its size, the sum over the heads beyond fp32 included."""
+    P = Pool([1000, 90], hq=hq, hk=hk, kind=kind, seed=8)
+    g = torch.Generator().manual_seed(1)
+    bounds = torch.randint(-127, 128, (1, P.n_pages, hk, 2, P.d), generator=g, dtype=torch.int8).cuda()
+    scale = torch.rand(1, P.n_pages, hk, generator=g).cuda()
+    base = (P.q.float().abs().clamp(2.0 ** -3, 1.75) * P.q.float().sign()).to(P.tdt)
+    base[0, :, 5] = 1.75                                     # the sum over the heads: 1.75 * 8
+    c = P.cache()
+    table, n = P.dev()
+    got = []
+    for f in (1.0, 2.0 ** 100, 2.0 ** 124, 2.0 ** 127, 2.0 ** -80):
+        q = (base.double() * f).to(P.tdt)
+        assert torch.equal(q.double(), base.double() * f)
+        ps, pages = torch.zeros(2, hk, P.width, device="cuda"), torch.zeros(2, hk, 9, dtype=torch.int32, device="cuda")
+        c.wkv_paged_select(0, q.cuda(), table, n, bounds, scale, ps, pages, recent=1)
+        assert c.wkv_status() == 0
+        got.append((ps, pages))
+    for ps, pages in got[1:]:
+        assert torch.equal(ps, got[0][0]) and torch.equal(pages, got[0][1])
