@@ -423,7 +423,8 @@ int wkv_paged_decode_pages(wkv_paged* c, int32_t layer, int32_t batch, const voi
  * may differ), where prompts can attend to them.  Runs on c's stream; the caller orders dst's.  Asynchronous.
  *   block_table, seq_lens as in wkv_paged_decode;  dst_table device [batch, dst_width] int32, pages for every sequence's length (entries
  *        that it has no page for are stored nowhere, and c's wkv_paged_status reports WKV_ERR_STATE)
- * Rows behind a sequence's length are left as they were. */
+ * Rows behind a sequence's length are left as they were.  batch * n_kv_heads * (table_width * page_size / 64, rounded up) must stay
+ * below 2^31. */
 int wkv_paged_expand(wkv_paged* c, int32_t layer, int32_t batch, const int32_t* block_table, int32_t table_width, const int32_t* seq_lens,
                      wkv_paged* dst, int32_t dst_layer, const int32_t* dst_table, int32_t dst_width);
 

@@ -143,6 +143,7 @@ int wkv_paged_expand(wkv_paged* c, int32_t layer, int32_t batch, const int32_t* 
   P.to_table = dst_table; P.to_width = dst_width; P.to_pages = g.n_pages; P.to_page = g.page_size; P.to_shift = dst->page_shift;
   P.blocks = (table_width * f.page_size + 63) / 64;
   const long long grid = (long long)batch * f.n_kv_heads * P.blocks;
+  if (grid > 0x7fffffffLL) return fail(c, WKV_ERR_INVALID, "batch * n_kv_heads * table_width is too large");
   WKV_CUDA(c, f.head_dim == 128 ? launch(c, wkv::paged_expand_kernel<128>, grid, wkv::kRowsThreads, 0, P)
                                 : launch(c, wkv::paged_expand_kernel<64>, grid, wkv::kRowsThreads, 0, P));
   return WKV_OK;

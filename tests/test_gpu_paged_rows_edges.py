@@ -238,3 +238,18 @@ def test_choice_does_not_depend_on_a_factor_of_the_query(kind, hq, hk):
         got.append((ps, pages))
     for ps, pages in got[1:]:
         assert torch.equal(ps, got[0][0]) and torch.equal(pages, got[0][1])
+
+
+# ---- sizes
+
+def test_spreading_out_refuses_what_a_launch_cannot_hold():
+    """batch * n_kv_heads * (table_width * page_size / 64) CTAs: at most 2^31 - 1."""
+    heads, width, batch = 32, 1 << 18, 1024
+    args = dict(n_layers=1, n_pages=1, page_size=64, n_q_heads=heads, n_kv_heads=heads, head_dim=64, max_batch=batch, max_pages=width)
+    a, b = binding.PagedCache(dtype=binding.WKV_KV4, **args), binding.PagedCache(dtype=binding.WKV_BF16, **{**args, "max_batch": 1})
+    one = torch.zeros(batch, dtype=torch.int32, device="cuda")
+    for n in (256, batch):                                   # 2^31 CTAs, 2^33 (nothing is read: the call ends on the host)
+        before = a.wkv_launch_count()
+        rc = binding.lib().wkv_paged_expand(a._h, 0, n, one.data_ptr(), width, one.data_ptr(), b._h, 0, one.data_ptr(), 1)
+        assert rc == binding.WKV_ERR_INVALID and "too large" in binding.lib().wkv_paged_last_error(a._h).decode()
+        assert a.wkv_launch_count() == before and a.wkv_status() == 0
