@@ -3,9 +3,12 @@
 //   o = sum_i p_i v_i,  p = softmax(scale q.k_i),  k_i = s_ig (n - z_ig) per group g of 32 channels, v_i likewise
 //
 // Bound: HBM at 4.5 bits a number; instruction issue close behind it, since a number may cost no more than about three lane instructions.
-// Codes are never converted.  Keys: a masked word is four bytes for mma.sync m16n8k32 on integers, against queries of 23 bits in three columns
-// of eight; exact, until a group's product becomes fp32.  Values: a masked word is two fp16 subnormals n 2^-24 (or n 2^-20), which m16n8k16
-// takes exactly.  Scales and zero points stay outside of the products:
+// Keys: a masked word is four bytes for mma.sync m16n8k32 on integers, against queries of 23 bits in three columns of eight; exact, until
+// a group's product becomes fp32.  Values: a masked word is two fp16 subnormals n 2^-24 (or n 2^-20), and one multiplication by 2^14 (2^10)
+// makes them normal numbers for m16n8k16.  (That takes subnormals too, but lines products up as if theirs had no leading zeros, and cuts the
+// sum 25 bits below: weights below 2^-15 of a step's largest were gone from the zero points' sum and from half of the codes', and, beside an
+// entry of nearly all weight, the rest of the output with them.  Normal numbers cost 6 us of 161, and 4 of 99.)
+// Scales and zero points stay outside of the products:
 //   q.k_i  = sum_g s_ig (q_g.n_ig - z_ig sum q_g)
 //   o_g    = sum_i (p_i s_ig) n_ig - sum_i (p_i s_ig) z_ig   the weights p s in fp16, the same rounded ones in both sums
 // A query head becomes whole numbers by a power of two that brings its largest channel to [2^21, 2^22), the largest that a group's sum leaves
@@ -413,7 +416,7 @@ struct Kv4Warp {
       for (int f = 0; f < kFrags; ++f) {
         b[f][0] = half_mul(p.x, half_mul(scale2[f][0], shift));
         b[f][1] = half_mul(p.y, half_mul(scale2[f][1], shift));
-        mma_m16n8k16_f16(zo[f], zero2[f][0], 0u, zero2[f][1], 0u, b[f][0], b[f][1]);
+        mma_m16n8k16_f16(zo[f], even_codes(zero2[f][0]), 0u, even_codes(zero2[f][1]), 0u, b[f][0], b[f][1]);
       }
       // units r of every group, of entries j + 4t
       const uint32_t tv = stage + at.vc + sub * at.next_c;
@@ -437,12 +440,15 @@ struct Kv4Warp {
         // (times 1 or 0: the other pipe has room)
         const uint32_t mine = of_group(g % kPer, r) ? 0x3c003c00u : 0u, b0 = kPer > 1 ? half_mul(b[f][0], mine) : b[f][0],
                        b1 = kPer > 1 ? half_mul(b[f][1], mine) : b[f][1];
-        mma_m16n8k16_f16(o[f][0], lo & 0x000f000fu, lo & 0x00f000f0u, hi & 0x000f000fu, hi & 0x00f000f0u, b0, b1);
-        mma_m16n8k16_f16(o[f][1], lo8 & 0x000f000fu, lo8 & 0x00f000f0u, hi8 & 0x000f000fu, hi8 & 0x00f000f0u, b0, b1);
+        mma_m16n8k16_f16(o[f][0], even_codes(lo), odd_codes(lo), even_codes(hi), odd_codes(hi), b0, b1);
+        mma_m16n8k16_f16(o[f][1], even_codes(lo8), odd_codes(lo8), even_codes(hi8), odd_codes(hi8), b0, b1);
       }
     }
   }
 
+  // Codes (or zero points) in bits 0 .. 3, or 4 .. 7, of both halves as n 2^-10.
+  __device__ __forceinline__ static uint32_t even_codes(uint32_t w) { return half_mul(w & 0x000f000fu, 0x74007400u); }
+  __device__ __forceinline__ static uint32_t odd_codes(uint32_t w) { return half_mul(w & 0x00f000f0u, 0x64006400u); }
   __device__ __forceinline__ void scale_sums(float f0, float f1) {         // of columns 2j and 2j + 1
 #pragma unroll
     for (int f = 0; f < kFrags; ++f) {
@@ -504,7 +510,7 @@ struct Kv4Warp {
     for (int f = 0; f < kFrags; ++f)                       // column r meets its own group in row r
       if (j == r >> 1 && (G == 1 ? r < kGroups : G == 2 ? r >> 1 < kGroups : true)) zeros[group_of(f, r) * G + head_of(r)] = r & 1 ? zo[f][1] : zo[f][0];
     __syncwarp();
-    const float back = largest ? 0x1p10f / power(largest) : 0.f;     // codes' 2^24, weights' 2^-14
+    const float back = largest ? 0x1p-4f / power(largest) : 0.f;     // codes' 2^10, weights' 2^-14
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       const int head = head_of(2 * j + c), which = G == 1 ? 2 * j + c : G == 2 ? j : G == 4 ? c : 0;     // the column's group in its fragment
@@ -516,7 +522,7 @@ struct Kv4Warp {
         const float z = zeros[g * G + head];
         float4* to = reinterpret_cast<float4*>(out + head * D + g * 32 + 4 * r);
         const float (&a)[2][4] = o[f8];
-        float4 y = make_float4((a[0][c] - z) * f, (a[0][2 + c] * 0x1p-4f - z) * f, (a[1][c] - z) * f, (a[1][2 + c] * 0x1p-4f - z) * f);
+        float4 y = make_float4((a[0][c] - z) * f, (a[0][2 + c] - z) * f, (a[1][c] - z) * f, (a[1][2 + c] - z) * f);
         if constexpr (ADD) {
           const float4 was = *to;
           y.x += was.x; y.y += was.y; y.z += was.z; y.w += was.w;

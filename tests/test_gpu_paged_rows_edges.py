@@ -253,3 +253,33 @@ def test_spreading_out_refuses_what_a_launch_cannot_hold():
         rc = binding.lib().wkv_paged_expand(a._h, 0, n, one.data_ptr(), width, one.data_ptr(), b._h, 0, one.data_ptr(), 1)
         assert rc == binding.WKV_ERR_INVALID and "too large" in binding.lib().wkv_paged_last_error(a._h).decode()
         assert a.wkv_launch_count() == before and a.wkv_status() == 0
+
+
+# ---- one entry with nearly all weight
+
+@pytest.mark.parametrize("hq,hk,d,page", [(2, 2, 128, 16), (2, 2, 64, 32), (4, 2, 128, 64), (4, 2, 64, 16), (8, 2, 128, 32), (8, 2, 64, 64), (8, 1, 128, 16)])
+def test_small_weights_beside_one_large_one(hq, hk, d, page):
+    """The entry with nearly all weight holds zeros (codes equal to the zero point, not 0), so that the others' weights, 2^-8 to 2^-24 of it,
+    are all there is: sums of codes and of zero points must hold both to fp32's bits."""
+    from paged_rows_util import pack_chunks
+    gaps = list(range(8, 25, 2))
+    lens = [16, 40, 300] * 3
+    P = Pool(lens, hq=hq, hk=hk, d=d, page=page, seed=d + hq)
+    g = torch.Generator().manual_seed(hq)
+    shape = (1, P.n_pages, hk, page, d)
+    K, V = torch.zeros(shape), torch.randn(shape, generator=g)
+    q = torch.zeros(len(lens), hq, d)
+    for b, (n, gap) in enumerate(zip(lens, gaps)):
+        at = (5 * b + 3) % n
+        pg, row = int(P.table[b, at // page]), at % page
+        K[0, pg, :, row, 0] = 64.0
+        V[0, pg, :, row] = 0.0
+        V[0, pg, :, row, 3::32], V[0, pg, :, row, 20::32] = 2.0, -2.0
+        q[b, :, 0] = gap * np.log(2.0) / (64.0 * P.scale)
+    P.k_pool, P.v_pool = (torch.from_numpy(pack_chunks(w, x.bfloat16().float().numpy())[0]) for w, x in (("k", K), ("v", V)))
+    P.q = q.bfloat16()
+    c = P.cache()
+    for lists in (None, shuffled_lists(P, 3)):
+        out, lse, status = decode(P, c, lists=lists)
+        assert status == 0
+        P.check(out, lse, lambda b, h: np.ones(P.lens[b], bool))
