@@ -7,7 +7,7 @@
 // a group's product becomes fp32.  Values: a masked word is two fp16 subnormals n 2^-24 (or n 2^-20), and one multiplication by 2^14 (2^10)
 // makes them normal numbers for m16n8k16.  (That takes subnormals too, but lines products up as if theirs had no leading zeros, and cuts the
 // sum 25 bits below: weights below 2^-15 of a step's largest were gone from the zero points' sum and from half of the codes', and, beside an
-// entry of nearly all weight, the rest of the output with them.  Normal numbers cost 6 us of 161, and 4 of 99.)
+// entry of nearly all weight, the rest of the output with them.  Normal numbers cost 6 us of 160, and 4 of 99.)
 // Scales and zero points stay outside of the products:
 //   q.k_i  = sum_g s_ig (q_g.n_ig - z_ig sum q_g)
 //   o_g    = sum_i (p_i s_ig) n_ig - sum_i (p_i s_ig) z_ig   the weights p s in fp16, the same rounded ones in both sums
@@ -15,9 +15,9 @@
 // room for in 32 bits: bf16 channels down to 2^-14 of it stay exact, smaller ones are off by up to 2^-22 of it.  (Fewer bits show in the
 // log-sums, which are fp32: 14 in two columns, 12 us of 174 faster, and 17 with the high halves' codes taken times 16 instead of shifted, 3
 // us, were 1e-6 and more off in sequences of one token.)
-// p and p s are rounded to fp16, 2^-11 each, together a quarter of what rounding the output to bf16 costs.  The weights are kept in
-// fp16's range by a power of two that follows the largest value scale seen, whatever weight its row has: p s is also off by up to 2^-39 of that
-// scale times the largest weight (p by 2^-34 of the latter where that scale is 256 or more).
+// p and p s are rounded to fp16, 2^-11 each, together a quarter of what rounding the output to bf16 costs.  Weights are held times 2^9 and
+// scales times a power of two that brings the largest one seen, whatever weight its row has, to [2^5, 2^6): all scales of the format are
+// exact beside it, and p s is also off by up to 2^-39 of that scale times the largest weight, p by 2^-34 of the latter.
 // (Keys as fp16 subnormals: 163 us of arithmetic in the 16 x 8192..16384 case, masks at half rate above all.  As e4m3 numbers the matrix
 // instruction is split into fp16 ones with conversions.)
 //
@@ -150,7 +150,7 @@ struct Kv4Warp {
   static constexpr bool kHolds = G == 1;
   static constexpr int kTiles = kHeads + 1;                // of columns
   static constexpr int kQuery = kTiles * kGroups / 2 * 32 * 16;          // bytes
-  static constexpr float kHeadroom = 14.f;                 // weights are held times 2^14: fp16 numbers down to 2^-28
+  static constexpr float kHeadroom = 9.f;                  // weights are held times 2^9: normal fp16 numbers down to 2^-23
   int qsum[kHeads][kMasked ? 1 : kGroups];     // sum of the quarter's, or a group's, channels
   uint32_t q[kTiles][kGroups][2];
   float factor[kHeads];        // whole numbers -> base-2 logits
@@ -158,7 +158,7 @@ struct Kv4Warp {
   float zo[kFrags][4];         // zero points' products: row r is the group of column r; rows 8 .. 15 are nothing
   float m[kHeads], l[kHeads];
   uint32_t largest;            // twice the bits of the largest value scale seen, which the weights' power of two follows
-  uint32_t shift;              // what of that power of two the scales take, twice: multiples of 2^-17 of four bits, they stay exact down to 2^-7
+  uint32_t shift;              // that power of two, twice: 2^-7 or more, so that scales, multiples of 2^-17 of four bits, stay exact
 
   // Where the lane's words lie in a stage: codes and pairs of its first 16 entries' keys (values: `half` bytes behind), and how far behind
   // them those of the other 16 are.
@@ -405,12 +405,7 @@ struct Kv4Warp {
         }
       }
       if (__any_sync(~0u, top != largest)) widen(top);
-      uint2 p = lds64(weights + 2 * (head_of(r) * 32 + sub * 16 + 4 * j));
-      if (largest >= 0x5c000000u) {                        // 256 and more: the weights take the rest, 2^-1 .. 2^-5
-        const uint32_t rest = (37 - (largest >> 26)) * 0x04000400u;
-        p.x = half_mul(p.x, rest);
-        p.y = half_mul(p.y, rest);
-      }
+      const uint2 p = lds64(weights + 2 * (head_of(r) * 32 + sub * 16 + 4 * j));
       uint32_t b[kFrags][2];
 #pragma unroll
       for (int f = 0; f < kFrags; ++f) {
@@ -476,16 +471,16 @@ struct Kv4Warp {
     }
     scale_sums(f[0], f[kHeads - 1]);
   }
-  // The power of two that brings the largest value scale to [1, 2).
-  __device__ __forceinline__ static float power(uint32_t largest) { return pow2f(15 - max(1, (int)(largest >> 26))); }
+  // The power of two that brings the largest value scale to [2^5, 2^6), or as near as fp16 has one.
+  __device__ __forceinline__ static float power(uint32_t largest) { return pow2f(20 - max(5, (int)(largest >> 26))); }
   // A larger value scale.
   __device__ __forceinline__ void widen(uint32_t top) {
     top = __reduce_max_sync(~0u, max(top & 0xffffu, top >> 16));
     top |= top << 16;
-    const float to = power(top), ratio = largest ? to / power(largest) : 0.f, part = fmaxf(to, 0x1p-7f);
+    const float to = power(top), ratio = largest ? to / power(largest) : 0.f;
     scale_sums(ratio, ratio);
     largest = top;
-    shift = half_pair(part, part);
+    shift = half_pair(to, to);
   }
 
   // (max, sum) of the heads over this warp's entries to [8] each
@@ -497,7 +492,7 @@ struct Kv4Warp {
       for (int off = kMasked ? 1 : 4; off < 32; off <<= 1) l[c] += __shfl_xor_sync(~0u, l[c], off);
       if (lane < (kMasked ? 1 : 4)) {
         sm_m[kMasked ? c : lane + 4 * c] = m[c];
-        sm_l[kMasked ? c : lane + 4 * c] = l[c] * 0x1p-14f;
+        sm_l[kMasked ? c : lane + 4 * c] = l[c] * 0x1p-9f;
       }
     }
   }
@@ -510,7 +505,7 @@ struct Kv4Warp {
     for (int f = 0; f < kFrags; ++f)                       // column r meets its own group in row r
       if (j == r >> 1 && (G == 1 ? r < kGroups : G == 2 ? r >> 1 < kGroups : true)) zeros[group_of(f, r) * G + head_of(r)] = r & 1 ? zo[f][1] : zo[f][0];
     __syncwarp();
-    const float back = largest ? 0x1p-4f / power(largest) : 0.f;     // codes' 2^10, weights' 2^-14
+    const float back = largest ? 0x1p1f / power(largest) : 0.f;      // codes' 2^10, weights' 2^-9
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       const int head = head_of(2 * j + c), which = G == 1 ? 2 * j + c : G == 2 ? j : G == 4 ? c : 0;     // the column's group in its fragment
