@@ -376,8 +376,8 @@ int wkv_paged_evict(wkv_paged* c, int32_t layer, int32_t batch, const int32_t* s
  * What follows is a wkv_paged_decode or wkv_paged_prefill with k and v NULL.
  *   q [total_q, n_q_heads, head_dim], k, v [total_q, n_kv_heads, head_dim]: rows q_stride, kv_stride elements apart (0: packed),
  *        16-byte aligned;  q NULL: no queries;  k and v NULL: only the queries
- *   q_start device [batch + 1] int32: sequence b's tokens are rows q_start[b] .. q_start[b+1]-1 and become its last entries;
- *        NULL: one token per sequence, row b, total_q = batch.  seq_lens counts the new entries; 0 = padding
+ *   q_start device [batch + 1] int32: sequence b's tokens are rows q_start[b] .. q_start[b+1]-1 and become its last entries
+ *        (total_q at most 2^24); NULL: one token per sequence, row b, total_q = batch.  seq_lens counts the new entries; 0 = padding
  *   rope device [rope_rows, rope_dim] fp32, 16-byte aligned: for every position rope_dim / 2 cosines, then as many sines; NULL: nothing is
  *        turned.  The first rope_dim channels of a head (a multiple of 16, <= head_dim) are turned in pairs,
  *        (a, b) -> (a cos - b sin, b cos + a sin), in binary32, each product rounded by itself; rope_paired = 1: angle i turns channels
@@ -403,7 +403,8 @@ int wkv_paged_append(wkv_paged* c, int32_t layer, int32_t batch, const void* q, 
  * times the whole number sum over channels of (u hi + w lo), with hi, lo the page's bounds and u, w the sums over the kv head's
  * query heads of max(q, 0) and min(q, 0), both in steps of 1/127 of their largest channel: up to rounding, and a factor per query,
  * a bound on the sum over the heads of q.k.
- *   q as in wkv_paged_decode;  page_bounds, page_scale as wkv_paged_append keeps them
+ *   q as in wkv_paged_decode;  page_bounds, page_scale as wkv_paged_append keeps them: of a page that got entries by another call, an
+ *        eviction above all, they are those of what it held before, and nothing reports that
  *   n_select in [1, 2^20]; recent >= 1, recent + sink <= n_select
  *   page_scores [batch, n_kv_heads, page_score_stride] fp32 out: the score of every page (page_score_stride >= table_width);
  *        behind a sequence's last page left as it was

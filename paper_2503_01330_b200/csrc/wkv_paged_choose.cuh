@@ -11,7 +11,8 @@
 // (by a counter that nobody waits on) chooses.  (A cluster whose CTAs put their scores into the first one's shared memory saves 2 us of
 // that, and costs them again where the launch follows one that fills the SMs: 2048 pages, then 64 of them attended to, 21.3 us for 20.)
 //
-// Measured: one sequence of 2048 pages, 8 kv heads, 10.5 us; 16 of 256..512 pages, 32 kv heads, 14 us.
+// Measured: one sequence of 2048 pages, 8 kv heads, 10.5 us; 16 of 256..512 pages, 32 kv heads, 14 us.  Longer ones, whose scores do not fit
+// into shared memory and are read again from L2 by the one CTA that chooses: 2049 pages 16 us, 4096 24, 8192 39, 32768 139 (its bounds: 11).
 #pragma once
 #include "wkv_paged.cuh"
 

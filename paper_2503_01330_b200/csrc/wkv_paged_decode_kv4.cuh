@@ -2,7 +2,9 @@
 //
 //   o = sum_i p_i v_i,  p = softmax(scale q.k_i),  k_i = s_ig (n - z_ig) per group g of 32 channels, v_i likewise
 //
-// Bound: HBM at 4.5 bits a number; instruction issue close behind it, since a number may cost no more than about three lane instructions.
+// Bound: HBM at 4.5 bits a number, and arithmetic close behind it, since a number may cost no more than about three lane instructions: issue is
+// active in 62 to 67 % of the cycles and the ALU pipe in 55 to 57 %, with four to five warps a scheduler that wait for fixed latencies, memory and
+// that pipe in turn; no pipe is full.
 // Keys: a masked word is four bytes for mma.sync m16n8k32 on integers, against queries of 23 bits in three columns of eight; exact, until
 // a group's product becomes fp32.  Values: a masked word is two fp16 subnormals n 2^-24 (or n 2^-20), and one multiplication by 2^14 (2^10)
 // makes them normal numbers for m16n8k16.  (That takes subnormals too, but lines products up as if theirs had no leading zeros, and cuts the
@@ -26,8 +28,8 @@
 // chunks into the team's stages of a ring (cp.async.bulk).  (One producer for both: 174 us where two take 167, 40 where they take 32 in pages
 // of 16: a tile costs it some 700 cycles.)
 //
-// Measured: 16 sequences of 8192..16384 tokens, 32 x 128 heads, 161 us = 5.7 TB/s (0.87 of the measured copy rate; 180 us at the power limit
-// under load); 16 of 12000..32768, 32/8 heads, 98 us = 4.3 TB/s, bound by issue; one of 611 tokens 10.2 us in a captured graph.
+// Measured: 16 sequences of 8192..16384 tokens, 32 x 128 heads, 166 us = 5.5 TB/s (0.84 of the measured copy rate; 190 us at the power limit
+// under load); 16 of 12000..32768, 32/8 heads, 102 us = 4.1 TB/s (108 under load); one of 611 tokens 10.3 us in a captured graph.
 #pragma once
 #include "wkv_paged_decode.cuh"
 #include "wkv_paged_kv4.cuh"
