@@ -182,9 +182,9 @@ def test_pages_with_an_infinite_key_are_chosen_first(kind, d):
 @pytest.mark.parametrize("n", [40, 600])
 @pytest.mark.parametrize("small", [2.0 ** -11, 2.0 ** -13, 2.0 ** -15])
 def test_large_values_without_weight_leave_small_ones_their_bits(hq, hk, d, page, n, small):
-    """Entry 0 has value scales at the format's upper end and next to no weight.  A weight times a scale, fp16 times a power of two that
-    brings the largest scale S to [1, 2) and weights of 1 to 2^14, is off by 2^-25 at most where it is below fp16's normal range: 2^-39 S,
-    or by all of it; the weight itself by 2^-25 2^-9 of the largest at most.  The other roundings are relative."""
+    """Entry 0 has value scales at the format's upper end and next to no weight.  A weight times a scale, fp16 times powers of two that bring
+    the largest scale S to [2^5, 2^6) and weights of 1 to 2^9, is off by 2^-25 at most where it is below fp16's normal range: 2^-39 S, or by
+    all of it; the weight itself by 2^-25 2^-9 of the largest at most.  The other roundings are relative."""
     from paged_rows_util import pack_chunks
     P = Pool([n], hq=hq, hk=hk, d=d, page=page, seed=n + hq)
     g = torch.Generator().manual_seed(n)
